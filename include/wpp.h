@@ -58,7 +58,13 @@ typedef enum {
     WPP_ERR_ALIASED_APPEND = 9      /* wpp_validate_batch: two writers, or a writer and a reader, share a slot */
 } wpp_status;
 
-enum { WPP_BF16 = 1 };
+/* wpp_batch_desc.dtype: what the KV pools hold (q, out and the new rows are bf16 in any case).
+ *   WPP_BF16  rows of head_dim bf16 numbers.
+ *   WPP_KV4   rows of head_dim codes c_e of 4 bits and two bf16 numbers; a row stands for least + scale * c_e.  For each
+ *             (page, KV head) a block of wpp_kv4_block_bytes(page_size, head_dim) bytes:
+ *             page_size rows of head_dim / 2 bytes (element 2i in the low half of byte i, 2i + 1 in the high half), then
+ *             page_size pairs (least, scale). */
+enum { WPP_BF16 = 1, WPP_KV4 = 2 };
 
 /* Opaque per-device context: SM count, shared-memory limit, driver entry points.  Owns host memory only. */
 typedef struct wpp_ctx wpp_ctx;
@@ -80,11 +86,16 @@ const char* wpp_status_string(int status);
 /* Last cudaError_t / CUresult seen by this context (0 if none). */
 int wpp_last_cuda_error(const wpp_ctx* ctx);
 
+/* Bytes of a block of a WPP_KV4 pool; 0 for a page size or head_dim outside the supported set. */
+size_t wpp_kv4_block_bytes(int32_t page_size, int32_t head_dim);
+
 /* Description of one wave.  Strides are in ELEMENTS (bf16), inner dim contiguous.
  * Pools: element (page, kv_head, slot, e) of K lives at
  *   k_cache + page*kv_page_stride + kv_head*kv_head_stride + slot*kv_token_stride + e,
  * V likewise in v_cache with the same strides.  A stride of 0 selects the dense default
- * of the layouts [num_pages][Hkv][B][d] (pools) and [T][H][d] (q, k_new/v_new, out). */
+ * of the layouts [num_pages][Hkv][B][d] (pools) and [T][H][d] (q, k_new/v_new, out).
+ * WPP_KV4 pools: the block of (page, kv_head) begins at byte page*kv_page_stride + kv_head*kv_head_stride of its pool: these two
+ * strides count BYTES (multiples of 16, at least a block), and kv_token_stride has to be 0. */
 typedef struct {
     int32_t num_requests;        /* R >= 0 */
     int32_t num_q_heads;         /* Hq, a multiple of num_kv_heads */
@@ -93,7 +104,7 @@ typedef struct {
     int32_t page_size;           /* B in {16, 32, 64, 128} tokens per page */
     int32_t max_blocks_per_req;  /* row stride of block_tables, in elements */
     int32_t num_pages;           /* pool size, for bounds checks */
-    int32_t dtype;               /* WPP_BF16 */
+    int32_t dtype;               /* WPP_BF16 or WPP_KV4 */
     float sm_scale;              /* 0 selects 1/sqrt(head_dim) */
     int32_t reserved0;
     int64_t kv_page_stride, kv_head_stride, kv_token_stride;
@@ -102,7 +113,8 @@ typedef struct {
     int64_t o_token_stride, o_head_stride;
 } wpp_batch_desc;
 
-/* Planner knobs; a zero field selects the library default. */
+/* Planner knobs; a zero field selects the library default.  (A description with WPP_KV4 has kernels of its own: of these fields
+ * only force_kv_splits and max_ctas say something there.) */
 typedef struct {
     int32_t tile_m;           /* query rows per work tile: 128 or 256 (default 256: two 128-row halves) */
     int32_t tile_n;           /* keys per inner step: 128 */
@@ -132,7 +144,7 @@ typedef struct {
     int64_t total_new_tokens;   /* T */
     int64_t key_steps;          /* sum over tiles of 128-row x 128-key steps (work incl. tile quantisation) */
     int64_t flops;              /* algorithmic: 4 * d * Hq * sum_i (C_i P_i + C_i (C_i + 1) / 2) */
-    int64_t shape;              /* attention kernel the plan is for: 1 or 2, see wpp_plan_opts.shape */
+    int64_t shape;              /* attention kernel the plan is for: 1 or 2, see wpp_plan_opts.shape; 3: those of a WPP_KV4 cache */
     size_t workspace_bytes;     /* device scratch wpp_prefill_attention_varlen needs for this plan (never 0) */
     size_t plan_bytes;          /* bytes of plan_host actually used; copy that many to the device */
 } wpp_plan_info;
@@ -177,7 +189,12 @@ int wpp_validate_batch(const wpp_batch_desc* desc, const int32_t* block_tables_h
  * One kernel on cuda_stream, 16-byte vector copies.  A page id outside [0, num_pages) sets
  * *status_dev = WPP_ERR_BOUNDS and that token is skipped.  A request whose prefix_lens[i] or chunk_lens[i] on the
  * device differ from the lengths the plan was made for sets WPP_ERR_PLAN_MISMATCH and none of its tokens is written
- * (Section 4.6: a position mismatch fails execution rather than writing against the wrong cache state). */
+ * (Section 4.6: a position mismatch fails execution rather than writing against the wrong cache state).
+ * WPP_KV4: of a row x (one token, head, K or V) these are stored, defined to the bit:
+ *     least = min x, as bf16 (+0 where it is -0);   scale = bf16((max x - least) / 15), the quotient in fp32;
+ *     c_e   = (x_e - least) / scale, difference and quotient in fp32, rounded to the nearest integer (halves to the even one).
+ * scale < 2^-100: scale and codes are 0.  A row with a NaN or an infinity, or whose max x - least is not a finite float:
+ * least = NaN (0x7fc0), scale and codes 0.  No other byte of a pool is written. */
 int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* k_new, const void* v_new,
                   void* k_cache, void* v_cache, const int32_t* block_tables, const int32_t* prefix_lens,
                   const int32_t* chunk_lens, const void* plan_host, const void* plan_dev, int32_t* status_dev,
@@ -204,7 +221,9 @@ int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* k_
  * plan has split tiles.  The kernels may be set up on the GPU while the kernel before them in the stream still runs;
  * they wait for its end before they touch memory.
  * Results are bit-reproducible for a given plan, whichever CTA takes which tile (no atomics on outputs; partials
- * are merged in a fixed order). */
+ * are merged in a fixed order).
+ * WPP_KV4: K_j[g] and V_j[g] are the rows that codes, least and scale stand for.  Slots >= P_i + C_i never influence the result, and
+ * a NaN row only the query rows that see it.  One or two kernels, one more iff the plan has split tiles. */
 int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* q, void* out,
                                  float* lse_or_null, const void* k_cache, const void* v_cache,
                                  const int32_t* block_tables, const int32_t* prefix_lens,

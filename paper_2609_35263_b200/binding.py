@@ -18,6 +18,7 @@ LIB_PATH = os.environ.get("WPP_LIB_PATH") or os.path.join(_HERE, "libwpp.so")   
 
 WPP_OK = 0
 WPP_BF16 = 1
+WPP_KV4 = 2            # a cache held in 4 bits: make_desc(..., dtype=WPP_KV4)
 STATUS_NAMES = {
     0: "WPP_OK", 1: "WPP_ERR_INVALID_ARG", 2: "WPP_ERR_UNSUPPORTED", 3: "WPP_ERR_BOUNDS",
     4: "WPP_ERR_POSITION_MISMATCH", 5: "WPP_ERR_WORKSPACE_TOO_SMALL", 6: "WPP_ERR_PLAN_MISMATCH",
@@ -84,7 +85,7 @@ class KdaDesc(ctypes.Structure):
 WAVE_RING_BUSY, WAVE_ADMISSION_PENDING, WAVE_ALREADY_DEFERRED = 1, 2, 4
 
 EXPORTS = ["wpp_create", "wpp_destroy", "wpp_status_string", "wpp_last_cuda_error", "wpp_plan_bytes",
-           "wpp_plan_tiles", "wpp_validate_batch", "wpp_kv_append", "wpp_prefill_attention_varlen",
+           "wpp_plan_tiles", "wpp_kv4_block_bytes", "wpp_validate_batch", "wpp_kv_append", "wpp_prefill_attention_varlen",
            "wpp_launch_count", "wpp_set_rescale_mode", "wpp_rescale_stats", "wpp_prefill_attention_varlen_static",
            "wpp_static_scratch_bytes",
            "wpp_selftest_bounded_wait", "wpp_wave_ladder", "wpp_plan_waves",
@@ -117,6 +118,8 @@ def load_library() -> ctypes.CDLL:
                                           ctypes.POINTER(ctypes.c_int)]
         lib.wpp_plan_bytes.restype = ctypes.c_size_t
         lib.wpp_plan_bytes.argtypes = [vp, ctypes.POINTER(BatchDesc), ctypes.c_int64, ctypes.POINTER(PlanOpts)]
+        lib.wpp_kv4_block_bytes.restype = ctypes.c_size_t
+        lib.wpp_kv4_block_bytes.argtypes = [ctypes.c_int32, ctypes.c_int32]
         lib.wpp_plan_tiles.argtypes = [vp, ctypes.POINTER(BatchDesc), i32p, i32p, i32p, ctypes.POINTER(PlanOpts),
                                        vp, ctypes.c_size_t, ctypes.POINTER(PlanInfo)]
         lib.wpp_validate_batch.argtypes = [ctypes.POINTER(BatchDesc), i32p, i32p, i32p]
@@ -207,13 +210,19 @@ class Context:
             pass
 
 
+def wpp_kv4_block_bytes(page_size: int, head_dim: int) -> int:
+    """Bytes of a (page, KV head) block of a cache held in 4 bits: pools are uint8 [num_pages, Hkv, wpp_kv4_block_bytes(...)]."""
+    return int(load_library().wpp_kv4_block_bytes(int(page_size), int(head_dim)))
+
+
 def make_desc(num_requests, num_q_heads, num_kv_heads, head_dim, page_size, max_blocks_per_req, num_pages,
-              sm_scale: float = 0.0, **strides) -> BatchDesc:
+              sm_scale: float = 0.0, dtype: int = WPP_BF16, **strides) -> BatchDesc:
+    """dtype: what the KV pools hold, WPP_BF16 or WPP_KV4 (whose kv_page_stride and kv_head_stride count bytes)."""
     d = BatchDesc()
     d.num_requests, d.num_q_heads, d.num_kv_heads = int(num_requests), int(num_q_heads), int(num_kv_heads)
     d.head_dim, d.page_size = int(head_dim), int(page_size)
     d.max_blocks_per_req, d.num_pages = int(max_blocks_per_req), int(num_pages)
-    d.dtype = WPP_BF16
+    d.dtype = int(dtype)
     d.sm_scale = float(sm_scale)
     for k, v in strides.items():
         setattr(d, k, int(v))

@@ -322,6 +322,109 @@ static int make_map(const wpp_ctx* cctx, CUtensorMap* m, const void* base, int r
     return WPP_OK;
 }
 
+// ---------------------------------------------------------------------------------------------------------------
+// Cache held in 4 bits: the same calls, told apart by the description's dtype.
+static int kv4_append(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlanHeader* hd, const void* k_new, const void* v_new,
+                      void* k_cache, void* v_cache, const int32_t* block_tables, const int32_t* prefix_lens, const int32_t* chunk_lens,
+                      const void* plan_dev, int32_t* status_dev, void* cuda_stream) {
+    wpp::Kv4AppendParams p;
+    memset(&p, 0, sizeof(p));
+    p.plan = plan_dev;
+    p.k_new = static_cast<const __nv_bfloat16*>(k_new);
+    p.v_new = static_cast<const __nv_bfloat16*>(v_new);
+    p.k_cache = static_cast<uint8_t*>(k_cache);
+    p.v_cache = static_cast<uint8_t*>(v_cache);
+    p.block_tables = block_tables;
+    p.prefix_lens = prefix_lens;
+    p.chunk_lens = chunk_lens;
+    p.status = status_dev;
+    p.kvnew_token_stride = d.kvnew_token_stride;
+    p.kvnew_head_stride = d.kvnew_head_stride;
+    p.page_bytes = d.kv_page_stride;
+    p.head_bytes = d.kv_head_stride;
+    p.num_requests = d.num_requests;
+    p.num_kv_heads = d.num_kv_heads;
+    p.page_size = d.page_size;
+    p.max_blocks = d.max_blocks_per_req;
+    p.num_pages = d.num_pages;
+    p.off_q_offsets = hd->off_q_offsets;
+    p.off_prefix = hd->off_prefix;
+    p.total_new_tokens = hd->total_new_tokens;
+    const int e = wpp_launch_kv4_append(d.head_dim, &p, ctx->sm_count, cuda_stream);
+    if (e != 0) return cuda_fail(ctx, e);
+    const_cast<wpp_ctx*>(ctx)->launches += 1;
+    return WPP_OK;
+}
+
+static float scale_log2_of(const wpp_batch_desc& d) {
+    const double scale = d.sm_scale > 0.f ? (double)d.sm_scale : 1.0 / sqrt((double)d.head_dim);
+    return (float)(scale * 1.4426950408889634);
+}
+
+static int combine_parts(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlanHeader* hd, const void* plan_dev, const float* ws_o,
+                         const float* ws_lse, void* out, float* lse_or_null, void* cuda_stream) {
+    if (hd->num_combine == 0) return WPP_OK;
+    wpp::CombineParams c;
+    memset(&c, 0, sizeof(c));
+    c.plan = plan_dev;
+    c.ws_o = ws_o;
+    c.ws_lse = ws_lse;
+    c.out = static_cast<__nv_bfloat16*>(out);
+    c.lse = lse_or_null;
+    c.o_token_stride = d.o_token_stride;
+    c.o_head_stride = d.o_head_stride;
+    c.num_q_heads = d.num_q_heads;
+    c.head_dim = d.head_dim;
+    c.max_rows = hd->max_combine_rows;
+    c.off_q_offsets = hd->off_q_offsets;
+    c.off_combine = hd->off_combine;
+    const int e = wpp_launch_combine(&c, hd->num_combine, cuda_stream);
+    if (e != 0) return cuda_fail(ctx, e);
+    const_cast<wpp_ctx*>(ctx)->launches += 1;
+    return WPP_OK;
+}
+
+static int kv4_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlanHeader* hd, const void* q, void* out,
+                         float* lse_or_null, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                         const int32_t* prefix_lens, const int32_t* chunk_lens, const void* plan_dev, void* workspace,
+                         int32_t* status_dev, void* cuda_stream) {
+    wpp::Kv4AttnParams p;
+    memset(&p, 0, sizeof(p));
+    p.plan = plan_dev;
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k_cache = static_cast<const uint8_t*>(k_cache);
+    p.v_cache = static_cast<const uint8_t*>(v_cache);
+    p.block_tables = block_tables;
+    p.prefix_lens = prefix_lens;
+    p.chunk_lens = chunk_lens;
+    p.out = static_cast<__nv_bfloat16*>(out);
+    p.lse = lse_or_null;
+    p.ws_o = reinterpret_cast<float*>(static_cast<char*>(workspace) + WPP_WS_HEADER_BYTES);
+    p.ws_lse = p.ws_o + (size_t)hd->num_split_slots * 2 * WPP_HALF_M * d.head_dim;
+    p.status = status_dev;
+    p.q_token_stride = d.q_token_stride;
+    p.q_head_stride = d.q_head_stride;
+    p.o_token_stride = d.o_token_stride;
+    p.o_head_stride = d.o_head_stride;
+    p.page_bytes = d.kv_page_stride;
+    p.head_bytes = d.kv_head_stride;
+    p.num_q_heads = d.num_q_heads;
+    p.group = d.num_q_heads / d.num_kv_heads;
+    p.page_size = d.page_size;
+    p.max_blocks = d.max_blocks_per_req;
+    p.num_pages = d.num_pages;
+    p.off_q_offsets = hd->off_q_offsets;
+    p.off_prefix = hd->off_prefix;
+    p.off_units = hd->off_units;
+    p.scale_log2 = scale_log2_of(d);
+    if (hd->num_few_units > 0) {
+        const int e = wpp_launch_kv4_few(d.head_dim, &p, hd->num_few_units, hd->max_few_rows, cuda_stream);
+        if (e != 0) return cuda_fail(ctx, e);
+        const_cast<wpp_ctx*>(ctx)->launches += 1;
+    }
+    return combine_parts(ctx, d, hd, plan_dev, p.ws_o, p.ws_lse, out, lse_or_null, cuda_stream);
+}
+
 extern "C" int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* k_new, const void* v_new,
                              void* k_cache, void* v_cache, const int32_t* block_tables, const int32_t* prefix_lens,
                              const int32_t* chunk_lens, const void* plan_host, const void* plan_dev,
@@ -338,6 +441,9 @@ extern "C" int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, con
         return WPP_ERR_INVALID_ARG;
     if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(plan_dev))
         return WPP_ERR_INVALID_ARG;
+    if (d.dtype == WPP_KV4)
+        return kv4_append(ctx, d, hd, k_new, v_new, k_cache, v_cache, block_tables, prefix_lens, chunk_lens, plan_dev, status_dev,
+                          cuda_stream);
     wpp::AppendParams p;
     memset(&p, 0, sizeof(p));
     p.plan = plan_dev;
@@ -381,7 +487,8 @@ extern "C" int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_
     if (rc != WPP_OK) return rc;
     const WppPlanHeader* hd = nullptr;
     if ((rc = wpp_check_plan(plan_host, &d, &hd)) != WPP_OK) return rc;
-    if (hd->tile_m > WPP_MAX_TILE_M || hd->shape < 1 || hd->shape > 2) return WPP_ERR_PLAN_MISMATCH;
+    const bool kv4 = d.dtype == WPP_KV4;
+    if (hd->tile_m > WPP_MAX_TILE_M || hd->shape < (kv4 ? 3 : 1) || hd->shape > (kv4 ? 3 : 2)) return WPP_ERR_PLAN_MISMATCH;
     if (hd->total_new_tokens == 0 || hd->num_units == 0) return WPP_OK;
     if ((rc = wpp_ctx_check_device(ctx)) != WPP_OK) return rc;
     if (!q || !out || !k_cache || !v_cache || !block_tables || !prefix_lens || !chunk_lens || !plan_dev)
@@ -392,6 +499,9 @@ extern "C" int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return WPP_ERR_INVALID_ARG;
     if (workspace_bytes < hd->workspace_bytes) return WPP_ERR_WORKSPACE_TOO_SMALL;
     if (d.num_pages == 0) return WPP_ERR_INVALID_ARG;
+    if (kv4)
+        return kv4_attention(ctx, d, hd, q, out, lse_or_null, k_cache, v_cache, block_tables, prefix_lens, chunk_lens, plan_dev,
+                             workspace, status_dev, cuda_stream);
 
     CUtensorMap tq[4], tk, tv;
     for (int i = 0; i < 4; ++i) {       // boxes of 128, 64, 32, 16 query rows (packed heads take fewer rows per head)
@@ -431,8 +541,7 @@ extern "C" int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_
     p.page_size = d.page_size;
     p.max_blocks = d.max_blocks_per_req;
     p.num_pages = d.num_pages;
-    const double scale = d.sm_scale > 0.f ? (double)d.sm_scale : 1.0 / sqrt((double)d.head_dim);
-    p.scale_log2 = (float)(scale * 1.4426950408889634);
+    p.scale_log2 = scale_log2_of(d);
 
     p.off_q_offsets = hd->off_q_offsets;
     p.off_prefix = hd->off_prefix;
@@ -457,26 +566,7 @@ extern "C" int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_
                        : wpp_launch_attention(d.head_dim, tq, &tk, &tv, &p, num_ctas, late, cuda_stream);
     if (e != 0) return cuda_fail(ctx, e);
     const_cast<wpp_ctx*>(ctx)->launches += 1;
-    if (hd->num_combine > 0) {
-        wpp::CombineParams c;
-        memset(&c, 0, sizeof(c));
-        c.plan = plan_dev;
-        c.ws_o = p.ws_o;
-        c.ws_lse = p.ws_lse;
-        c.out = p.out;
-        c.lse = lse_or_null;
-        c.o_token_stride = d.o_token_stride;
-        c.o_head_stride = d.o_head_stride;
-        c.num_q_heads = d.num_q_heads;
-        c.head_dim = d.head_dim;
-        c.max_rows = hd->max_combine_rows;
-        c.off_q_offsets = hd->off_q_offsets;
-        c.off_combine = hd->off_combine;
-        e = wpp_launch_combine(&c, hd->num_combine, cuda_stream);
-        if (e != 0) return cuda_fail(ctx, e);
-        const_cast<wpp_ctx*>(ctx)->launches += 1;
-    }
-    return WPP_OK;
+    return combine_parts(ctx, d, hd, plan_dev, p.ws_o, p.ws_lse, out, lse_or_null, cuda_stream);
 }
 
 // ---------------------------------------------------------------------------------------------------------------

@@ -58,6 +58,45 @@ struct AppendParams {
     int64_t total_new_tokens;
 };
 
+// 4-bit cache.  Pools in bytes; a block (page, KV head) is page_size rows of head_dim / 2 bytes and, behind them, as many pairs of
+// bf16 numbers (least value, scale).
+struct Kv4AppendParams {
+    const void* plan;
+    const __nv_bfloat16* k_new;
+    const __nv_bfloat16* v_new;
+    uint8_t* k_cache;
+    uint8_t* v_cache;
+    const int32_t* block_tables;
+    const int32_t* prefix_lens;
+    const int32_t* chunk_lens;
+    int32_t* status;
+    int64_t kvnew_token_stride, kvnew_head_stride;       // in elements
+    int64_t page_bytes, head_bytes;
+    int32_t num_requests, num_kv_heads, page_size, max_blocks, num_pages;
+    uint32_t off_q_offsets, off_prefix;
+    int64_t total_new_tokens;
+};
+
+struct Kv4AttnParams {
+    const void* plan;
+    const __nv_bfloat16* q;
+    const uint8_t* k_cache;
+    const uint8_t* v_cache;
+    const int32_t* block_tables;
+    const int32_t* prefix_lens;
+    const int32_t* chunk_lens;
+    __nv_bfloat16* out;
+    float* lse;                      // [T][Hq] or null
+    float* ws_o;                     // split partials: [slots][2][128][d]
+    float* ws_lse;                   // [slots][2][128], log2 units
+    int32_t* status;
+    int64_t q_token_stride, q_head_stride, o_token_stride, o_head_stride;      // in elements
+    int64_t page_bytes, head_bytes;
+    int32_t num_q_heads, group, page_size, max_blocks, num_pages;
+    uint32_t off_q_offsets, off_prefix, off_units;
+    float scale_log2;
+};
+
 struct CombineParams {
     const void* plan;
     const float* ws_o;
@@ -136,6 +175,8 @@ int wpp_launch_attention(int head_dim, const CUtensorMap* tq, const CUtensorMap*
 int wpp_launch_attention_small(int head_dim, const CUtensorMap* tq, const CUtensorMap* tk, const CUtensorMap* tv,
                                const wpp::SmallAttnParams* p, int num_ctas, void* stream);
 int wpp_launch_append(const wpp::AppendParams* p, int num_sms, void* stream);
+int wpp_launch_kv4_append(int head_dim, const wpp::Kv4AppendParams* p, int num_sms, void* stream);
+int wpp_launch_kv4_few(int head_dim, const wpp::Kv4AttnParams* p, int num_units, int max_rows, void* stream);
 int wpp_launch_combine(const wpp::CombineParams* p, int num_combine, void* stream);
 // maps: q, k, v, alpha; form: 1, 2, 3 = CTAs of 128, 64, 32 columns of the state
 int wpp_launch_kda_group(const wpp::KdaGroupParams* p, const CUtensorMap* maps, int form, void* stream);

@@ -26,6 +26,11 @@ const char* wpp_status_string(int s) {
     }
 }
 
+size_t wpp_kv4_block_bytes(int32_t page_size, int32_t head_dim) {
+    if ((head_dim != 64 && head_dim != 128) || (page_size != 16 && page_size != 32 && page_size != 64 && page_size != 128)) return 0;
+    return (size_t)page_size * (size_t)(head_dim / 2 + 4);
+}
+
 // Fill in default strides and check what the host can check about a description.
 int wpp_resolve_desc(const wpp_batch_desc* in, wpp_batch_desc* d) {
     if (!in) return WPP_ERR_INVALID_ARG;
@@ -33,13 +38,22 @@ int wpp_resolve_desc(const wpp_batch_desc* in, wpp_batch_desc* d) {
     if (d->num_requests < 0 || d->num_q_heads <= 0 || d->num_kv_heads <= 0 || d->max_blocks_per_req < 0 ||
         d->num_pages < 0 || d->head_dim <= 0 || d->page_size <= 0 || !(d->sm_scale >= 0.0f))
         return WPP_ERR_INVALID_ARG;
-    if (d->dtype != WPP_BF16) return WPP_ERR_UNSUPPORTED;
+    if (d->dtype != WPP_BF16 && d->dtype != WPP_KV4) return WPP_ERR_UNSUPPORTED;
     if (d->head_dim != 64 && d->head_dim != 128) return WPP_ERR_UNSUPPORTED;
     if (d->page_size != 16 && d->page_size != 32 && d->page_size != 64 && d->page_size != 128)
         return WPP_ERR_UNSUPPORTED;
     if (d->num_q_heads % d->num_kv_heads != 0) return WPP_ERR_UNSUPPORTED;
     const int64_t dd = d->head_dim;
-    if (!d->kv_token_stride) d->kv_token_stride = dd;
+    const bool kv4 = d->dtype == WPP_KV4;      // the pools' strides count bytes then, and a block's rows have theirs from the format
+    if (kv4) {
+        const int64_t block = (int64_t)wpp_kv4_block_bytes(d->page_size, d->head_dim);
+        if (d->kv_token_stride) return WPP_ERR_INVALID_ARG;
+        if (!d->kv_head_stride) d->kv_head_stride = block;
+        if (!d->kv_page_stride) d->kv_page_stride = d->kv_head_stride * d->num_kv_heads;
+        if (d->kv_head_stride < block || d->kv_page_stride < block || d->kv_head_stride % 16 != 0 || d->kv_page_stride % 16 != 0)
+            return WPP_ERR_INVALID_ARG;
+    }
+    if (!kv4 && !d->kv_token_stride) d->kv_token_stride = dd;
     if (!d->kv_head_stride) d->kv_head_stride = d->kv_token_stride * d->page_size;
     if (!d->kv_page_stride) d->kv_page_stride = d->kv_head_stride * d->num_kv_heads;
     if (!d->q_head_stride) d->q_head_stride = dd;
@@ -48,8 +62,8 @@ int wpp_resolve_desc(const wpp_batch_desc* in, wpp_batch_desc* d) {
     if (!d->kvnew_token_stride) d->kvnew_token_stride = d->kvnew_head_stride * d->num_kv_heads;
     if (!d->o_head_stride) d->o_head_stride = dd;
     if (!d->o_token_stride) d->o_token_stride = d->o_head_stride * d->num_q_heads;
-    const int64_t strides[] = {d->kv_page_stride, d->kv_head_stride, d->kv_token_stride, d->q_token_stride,
-                               d->q_head_stride, d->kvnew_token_stride, d->kvnew_head_stride,
+    const int64_t strides[] = {kv4 ? dd : d->kv_page_stride, kv4 ? dd : d->kv_head_stride, kv4 ? dd : d->kv_token_stride,
+                               d->q_token_stride, d->q_head_stride, d->kvnew_token_stride, d->kvnew_head_stride,
                                d->o_token_stride, d->o_head_stride};
     for (int64_t s : strides)
         if (s < dd || (s % 8) != 0) return WPP_ERR_INVALID_ARG;  // 8 bf16 = 16 bytes
@@ -189,6 +203,7 @@ size_t wpp_plan_bytes(const wpp_ctx* ctx, const wpp_batch_desc* desc, int64_t to
     wpp_plan_opts o;
     if (wpp_resolve_desc(desc, &d) != WPP_OK || total_new_tokens < 0) return 0;
     if (resolve_opts(ctx, opts_or_null, &o) != WPP_OK) return 0;
+    if (d.dtype == WPP_KV4) return wpp_kv4_plan_bytes(&d, &o, total_new_tokens);
     return plan_bytes_bound(&d, &o, total_new_tokens);
 }
 
@@ -218,6 +233,8 @@ int wpp_plan_tiles(const wpp_ctx* ctx, const wpp_batch_desc* desc, const int32_t
         pairs += C * P + C * (C + 1) / 2;
     }
     if (T > 0x7fffffff) return WPP_ERR_INVALID_ARG;
+    if (d.dtype == WPP_KV4)
+        return wpp_kv4_plan(&d, &o, prefix_lens, chunk_lens, T, pairs, plan_host, plan_host_bytes, info);
     if (plan_host_bytes < plan_bytes_bound(&d, &o, T)) return WPP_ERR_PLAN_MISMATCH;
 
     // ---- row blocks of every request.  A tile is a row block times the heads it takes (one head, or 2..16 heads of

@@ -23,11 +23,13 @@ struct WppPlanHeader {
                                     //               the row offsets) with the lengths they are launched with
     uint32_t off_units;             // WppUnit [num_units] in the order the persistent CTAs take them
     uint32_t off_combine;           // WppCombine [num_combine]
-    int32_t shape;                  // 1: two-half CTAs, one per SM; 2: single-half CTAs, two per SM (work item = half a unit)
+    int32_t shape;                  // 1: two-half CTAs, one per SM; 2: single-half CTAs, two per SM (work item = half a unit); 3: 4-bit cache
     int32_t nonempty_halves;
     int32_t max_combine_rows;       // most rows of a combine record (sizes the combine pass's grid)
     int32_t deal_items;             // small shape: its items are dealt out to the CTAs, without the workspace's counter
-    uint32_t pad[4];
+    int32_t num_few_units;          // 4-bit cache: the first of the units are of the kernel for few rows ...
+    int32_t max_few_rows;           // ... and the most rows one of them has
+    uint32_t pad[2];
 };
 
 // One work tile = two 128-row "halves" that share one K/V stream (same request, same KV head).  Each half
@@ -46,6 +48,12 @@ struct WppUnit {
     int32_t cost;                   // 128x128 steps over both halves
     int32_t pack;                   // places for query heads per half: 1, 2, 4 or 8
 };
+
+// 4-bit cache (shape 3): a unit of the kernel for few rows is rows[0] tokens from row0[0] on of each of the rows[1] heads from head[0]
+// on (one KV group's; WPP_FEW_ROWS rows at most), row k * rows[0] + t being token t of head k; its partial results are at
+// [split_slot][row0[1]][head[1] ..] of the workspace's arrays (slot, half, row): units of one number of parts share slots.  Its key
+// range is in steps of WPP_TILE_N keys too.
+#define WPP_FEW_ROWS 16
 
 // One half tile whose key range was split: partial slots [slot0, slot0+num_splits) merged in increasing order.
 struct WppCombine {

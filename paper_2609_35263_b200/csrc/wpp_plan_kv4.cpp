@@ -1,0 +1,160 @@
+// Work split of a wave over a cache held in 4 bits (part of wpp_plan_tiles; integer arithmetic only).
+#include <algorithm>
+#include <cstring>
+#include <vector>
+
+#include "../../include/wpp.h"
+#include "wpp_host.h"
+#include "wpp_plan_format.h"
+
+static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+
+constexpr int kFewCtas = 4;              // CTAs of the kernel for few rows that an SM holds
+constexpr int32_t kMaxParts = 64;
+
+// Row blocks of the kernel for few rows: heads of a KV group, and tokens, WPP_FEW_ROWS rows at most.
+static int32_t few_heads(int32_t group) { return std::min<int32_t>(group, WPP_FEW_ROWS); }
+static int32_t few_tokens(int32_t group) { return std::max<int32_t>(1, WPP_FEW_ROWS / few_heads(group)); }
+
+static int64_t few_blocks(const wpp_batch_desc* d, int64_t C) {
+    const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
+    return (C + t - 1) / t * ((G + h - 1) / h) * d->num_kv_heads;
+}
+
+size_t wpp_kv4_plan_bytes(const wpp_batch_desc* d, const wpp_plan_opts* o, int64_t T) {
+    const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
+    const int64_t base = (T / t + d->num_requests) * ((G + h - 1) / h) * d->num_kv_heads;
+    const int64_t units = o->force_kv_splits >= 2 ? base * o->force_kv_splits : 2 * base + 2 * kFewCtas * (int64_t)o->max_ctas;
+    size_t n = sizeof(WppPlanHeader) + 2 * align_up(sizeof(int32_t) * (size_t)(d->num_requests + 1), 16);
+    n += sizeof(WppUnit) * (size_t)units;
+    n += sizeof(WppCombine) * (size_t)(T * d->num_q_heads / t + (int64_t)d->num_requests * d->num_q_heads);
+    return align_up(n, 256);
+}
+
+int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t* prefix_lens, const int32_t* chunk_lens, int64_t T,
+                 int64_t pairs, void* plan_host, size_t plan_host_bytes, wpp_plan_info* info) {
+    const int R = d->num_requests, Hq = d->num_q_heads, Hkv = d->num_kv_heads, G = Hq / Hkv;
+    if (plan_host_bytes < wpp_kv4_plan_bytes(d, o, T)) return WPP_ERR_PLAN_MISMATCH;
+    auto steps_for = [](int64_t keys) { return (int32_t)((keys + WPP_TILE_N - 1) / WPP_TILE_N); };
+
+    const int32_t heads = few_heads(G), toks = few_tokens(G);
+    // parts: of equal length, so many that the SMs' CTAs have one each
+    int64_t n_base = 0, all_steps = 0;
+    for (int i = 0; i < R; ++i) {
+        const int64_t n = few_blocks(d, chunk_lens[i]);
+        n_base += n;
+        all_steps += n * steps_for((int64_t)prefix_lens[i] + chunk_lens[i]);
+    }
+    if (n_base > 0x3fffffff) return WPP_ERR_INVALID_ARG;
+    const int64_t slots_at_once = (int64_t)kFewCtas * o->max_ctas;
+    const int64_t part = std::max<int64_t>(1, (all_steps + slots_at_once - 1) / slots_at_once);
+
+    WppPlanHeader hd;
+    std::memset(&hd, 0, sizeof(hd));
+    size_t off = sizeof(WppPlanHeader);
+    hd.off_q_offsets = (uint32_t)off;
+    off += align_up(sizeof(int32_t) * (size_t)(R + 1), 16);
+    hd.off_prefix = (uint32_t)off;
+    off += align_up(sizeof(int32_t) * (size_t)(R + 1), 16);
+    hd.off_units = (uint32_t)off;
+    char* p = static_cast<char*>(plan_host);
+    std::memset(p, 0, off);
+    const int64_t unit_cap = ((int64_t)plan_host_bytes - (int64_t)off) / (int64_t)sizeof(WppUnit);
+    WppUnit* us = reinterpret_cast<WppUnit*>(p + hd.off_units);
+    std::vector<WppCombine> combines;
+    int64_t n_units = 0, n_split = 0, key_steps = 0;
+    int32_t max_rows = 0;
+    int32_t slots = 0, slot0 = 0, slot_parts = 0, slot_row = 2 * WPP_HALF_M;      // the slots that have room: from slot0 on, row slot_row
+    for (int i = 0; i < R; ++i) {
+        const int64_t P = prefix_lens[i], C = chunk_lens[i];
+        for (int64_t r0 = 0; r0 < C; r0 += toks) {
+            const int32_t rows = (int32_t)std::min<int64_t>(toks, C - r0), steps = steps_for(P + r0 + rows);
+            int32_t parts = (int32_t)std::min<int64_t>({(steps + part - 1) / part, steps, kMaxParts});
+            if (o->force_kv_splits >= 1) parts = std::min(o->force_kv_splits, steps);
+            for (int32_t kvh = 0; kvh < Hkv; ++kvh) {
+                for (int32_t h = 0; h < G; h += heads) {
+                    const int32_t nh = std::min(heads, G - h);
+                    if (n_units + parts > unit_cap) return WPP_ERR_PLAN_MISMATCH;
+                    WppUnit u;
+                    std::memset(&u, 0, sizeof(u));
+                    u.request = i;
+                    u.row0[0] = (int32_t)r0;
+                    u.rows[0] = rows;
+                    u.rows[1] = nh;
+                    u.head[0] = kvh * G + h;
+                    u.split_slot = -1;
+                    u.pack = 1;
+                    max_rows = std::max(max_rows, rows * nh);
+                    if (parts > 1) {
+                        if (parts > slot_parts || slot_row + WPP_FEW_ROWS > 2 * WPP_HALF_M) {
+                            slot0 = slots;
+                            slot_parts = parts;
+                            slot_row = 0;
+                            slots += parts;
+                        }
+                        u.row0[1] = slot_row / WPP_HALF_M;
+                        u.head[1] = slot_row % WPP_HALF_M;
+                        slot_row += WPP_FEW_ROWS;
+                        for (int32_t k = 0; k < nh; ++k)
+                            combines.push_back({i, (int32_t)r0, rows, u.head[0] + k, slot0, parts, u.row0[1], u.head[1] + k * rows});
+                    }
+                    for (int32_t q = 0; q < parts; ++q) {
+                        u.kv_begin = (int32_t)((int64_t)steps * q / parts);
+                        u.kv_end = (int32_t)((int64_t)steps * (q + 1) / parts);
+                        if (parts > 1) u.split_slot = slot0 + q;
+                        u.cost = u.kv_end - u.kv_begin;
+                        us[n_units++] = u;
+                        key_steps += u.cost;
+                        n_split += parts > 1;
+                    }
+                }
+            }
+        }
+    }
+    if (n_units > 0x3fffffff) return WPP_ERR_INVALID_ARG;
+    off += sizeof(WppUnit) * (size_t)n_units;
+    hd.off_combine = (uint32_t)off;
+    off += sizeof(WppCombine) * combines.size();
+    hd.plan_bytes = align_up(off, 16);
+    if (hd.plan_bytes > plan_host_bytes) return WPP_ERR_PLAN_MISMATCH;
+    if (!combines.empty()) std::memcpy(p + hd.off_combine, combines.data(), sizeof(WppCombine) * combines.size());
+    std::memset(p + off, 0, hd.plan_bytes - off);
+
+    hd.magic = WPP_PLAN_MAGIC;
+    hd.version = WPP_PLAN_VERSION;
+    hd.desc_hash = wpp_desc_hash(d);
+    hd.num_requests = R;
+    hd.num_ctas = (int32_t)std::max<int64_t>(1, std::min<int64_t>(o->max_ctas, n_units));
+    hd.num_units = (int32_t)n_units;
+    hd.num_few_units = (int32_t)n_units;
+    hd.max_few_rows = max_rows;
+    hd.num_combine = (int32_t)combines.size();
+    hd.num_split_slots = slots;
+    for (const WppCombine& c : combines) hd.max_combine_rows = std::max(hd.max_combine_rows, c.rows);
+    hd.tile_m = o->tile_m;
+    hd.tile_n = WPP_TILE_N;
+    hd.head_dim = d->head_dim;
+    hd.shape = 3;
+    hd.total_new_tokens = T;
+    hd.key_steps = key_steps;
+    hd.flops = 4 * (int64_t)d->head_dim * Hq * pairs;
+    hd.workspace_bytes = WPP_WS_HEADER_BYTES + align_up((size_t)slots * 2 * WPP_HALF_M * (d->head_dim + 1) * sizeof(float), 256);
+    std::memcpy(p, &hd, sizeof(hd));
+    int32_t* qo = reinterpret_cast<int32_t*>(p + hd.off_q_offsets);
+    qo[0] = 0;
+    for (int i = 0; i < R; ++i) qo[i + 1] = qo[i] + chunk_lens[i];
+    int32_t* pp = reinterpret_cast<int32_t*>(p + hd.off_prefix);
+    for (int i = 0; i < R; ++i) pp[i] = prefix_lens[i];
+
+    info->num_tiles = n_units;
+    info->num_split_tiles = n_split;
+    info->num_combine_tiles = (int64_t)combines.size();
+    info->num_ctas = hd.num_ctas;
+    info->total_new_tokens = T;
+    info->key_steps = key_steps;
+    info->flops = hd.flops;
+    info->shape = hd.shape;
+    info->workspace_bytes = hd.workspace_bytes;
+    info->plan_bytes = hd.plan_bytes;
+    return WPP_OK;
+}

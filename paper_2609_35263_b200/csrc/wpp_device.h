@@ -93,8 +93,9 @@ struct Kv4AttnParams {
     int64_t q_token_stride, q_head_stride, o_token_stride, o_head_stride;      // in elements
     int64_t page_bytes, head_bytes;
     int32_t num_q_heads, group, page_size, max_blocks, num_pages;
-    uint32_t off_q_offsets, off_prefix, off_units;
+    uint32_t off_q_offsets, off_prefix, off_units, off_few_ctas;
     float scale_log2;
+    uint32_t f16_1024;               // 1024 in both halves of a word (from here, and not a constant: see codes_low)
 };
 
 struct CombineParams {
@@ -176,7 +177,7 @@ int wpp_launch_attention_small(int head_dim, const CUtensorMap* tq, const CUtens
                                const wpp::SmallAttnParams* p, int num_ctas, void* stream);
 int wpp_launch_append(const wpp::AppendParams* p, int num_sms, void* stream);
 int wpp_launch_kv4_append(int head_dim, const wpp::Kv4AppendParams* p, int num_sms, void* stream);
-int wpp_launch_kv4_few(int head_dim, const wpp::Kv4AttnParams* p, int num_units, int max_rows, void* stream);
+int wpp_launch_kv4_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream);
 int wpp_launch_combine(const wpp::CombineParams* p, int num_combine, void* stream);
 // maps: q, k, v, alpha; form: 1, 2, 3 = CTAs of 128, 64, 32 columns of the state
 int wpp_launch_kda_group(const wpp::KdaGroupParams* p, const CUtensorMap* maps, int form, void* stream);

@@ -6,11 +6,16 @@
 // so the tensor cores multiply the codes themselves, which bf16 holds exactly, and two numbers per key finish the score in fp32;
 // in the same way sum_j p_j v_j = sum_j (p_j scale_j) c_j + sum_j p_j least_j, of which only p_j scale_j is rounded to bf16.
 //
-// What bounds it is the cache's bytes, and next to them the instructions that make bf16 numbers of codes: about one per code.  So
-// nothing else is done per code: a warp takes 16 keys at a time straight from global memory in the order the tensor cores' fragments
-// want (which element of a row stands at which place of a product does not matter as long as both factors agree), keys are the
-// rows and query rows the columns of the products (S^T = K Q^T, O^T = V^T P^T: eight columns, of which the group's heads fill all),
-// and the two products share no data but P, which a transposing move turns round in registers.
+// What bounds it is the cache's bytes, and close behind them the ALU's instructions that turn codes into numbers a product takes.  So
+// nothing else is done per code: a warp takes 32 keys at a time straight from global memory in the order the tensor cores' fragments
+// want (which element of a row stands at which place of a product does not matter as long as both factors agree); keys are the
+// rows and query rows the columns of the products (S^T = K Q^T, O^T = V^T P^T: eight columns, of which the group's heads fill all);
+// the two products share no data but P, which a transposing move turns round in registers.
+// A mask makes the codes f16 numbers 1024 + c or 1024 + 16 c, a packed f16 operation c - 8, both exact.  (As e4m3 numbers, which
+// bytes below 16 are with no operation at all, they come to more: the products of 8-bit numbers take them apart into f16 ones by
+// themselves.)  V's codes of two keys first stand above one another by a byte permutation.  Q is taken as f16 times a power of two
+// per row, P scale_j is rounded to f16 (2^-11).
+
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -22,11 +27,13 @@
 namespace wpp {
 
 constexpr int kFewWarps = 4;
-constexpr float kFewSlack = 16.f;          // a row keeps its reference while its scores stay below reference + 16 (log2)
+constexpr int kFewKeys = 32;               // a warp's keys at a time
+constexpr float kFewSlack = 8.f;           // a row keeps its reference while its scores stay below reference + 8 (log2)
+constexpr float kFewScaleSlack = 128.f;    // and a warp its reference of V's scales while they stay below so many times that: p scale < 2^15
 
-// D += A B, 16 x 8 x 16, bf16 in, fp32 out
-__device__ __forceinline__ void mma_16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+// D += A B, 16 x 8 x 16, f16 in, fp32 out
+__device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -35,58 +42,226 @@ __device__ __forceinline__ uint32_t transpose_8x8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-// Two codes of a word, four bits each at bits s and s + 16, as the bf16 numbers 128 + code (exact).
-__device__ __forceinline__ uint32_t codes_128(uint32_t w, int s) { return ((w >> s) & 0x000f000fu) | 0x43004300u; }
-// The same as code - 8 (exact).
-__device__ __forceinline__ uint32_t codes_8(uint32_t w, int s) {
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
     uint32_t r;
-    asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(codes_128(w, s)), "r"(0x43084308u));
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// Two codes, one at bits 0 to 3 or 4 to 7 of either half of a word, as f16 numbers code - 8 (exact).  `k1024` is 1024 in both halves, a
+// kernel parameter: of two constants the compiler makes two operations (167 us for the 64 requests' tokens, so 150).
+__device__ __forceinline__ uint32_t and_or(uint32_t a, uint32_t mask, uint32_t b) {
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(a), "r"(mask), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t codes_low(uint32_t u, uint32_t k1024) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(and_or(u, 0x000f000fu, k1024)), "r"(0x64086408u));                   // - 1032
+    return r;
+}
+__device__ __forceinline__ uint32_t codes_high(uint32_t u, uint32_t k1024) {
+    uint32_t r;
+    asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(and_or(u, 0x00f000f0u, k1024)), "r"(0x2c002c00u), "r"(0xd480d480u));   // / 16 - 72
     return r;
 }
 template <int kWords>
-__device__ __forceinline__ void load_words(uint32_t (&w)[kWords], const uint8_t* at) {
+__device__ __forceinline__ void load_words(uint32_t (&w)[kWords], uint32_t at) {
     if constexpr (kWords == 4) {
-        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "l"(at));
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(at));
     } else if constexpr (kWords == 2) {
-        asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "l"(at));
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at));
     } else {
-        asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(w[0]) : "l"(at));
+        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(at));
     }
 }
 
-// What a thread holds of 16 keys: lane 4 g + t has, of keys g and g + 8, columns [t D / 4, (t + 1) D / 4) of K; of keys 2 t, 2 t + 1,
-// 2 t + 8, 2 t + 9, columns [g D / 8, (g + 1) D / 8) of V; and the number pairs of keys g and g + 8.
-template <int D>
-struct FewKeys {
-    uint32_t k[2][D / 32];
-    uint32_t v[4][D / 64];
-    uint32_t kp[2], vp[2];
-    __device__ __forceinline__ void load(const uint8_t* kb, const uint8_t* vb, int slot, int page_size, int g, int t) {
-        const uint8_t* pairs = kb + page_size * (D / 2);
-        const uint8_t* vpairs = vb + page_size * (D / 2);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) load_words<D / 32>(k[i], kb + (slot + g + 8 * i) * (D / 2) + t * (D / 8));
-#pragma unroll
-        for (int i = 0; i < 4; ++i) load_words<D / 64>(v[i], vb + (slot + 2 * t + (i & 1) + 8 * (i >> 1)) * (D / 2) + g * (D / 16));
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            kp[i] = *reinterpret_cast<const uint32_t*>(pairs + (slot + g + 8 * i) * 4);
-            vp[i] = *reinterpret_cast<const uint32_t*>(vpairs + (slot + g + 8 * i) * 4);
-        }
-    }
+// A warp's 32 keys in shared memory: K's rows, V's rows, K's pairs, V's pairs.  They come by bulk copies, so that no thread's
+// registers or address arithmetic are spent on what is under way.
+template <int D, int NT>
+struct FewSmem {
+    static constexpr int kRows = kFewKeys * (D / 2), kPairs = kFewKeys * 4, kStage = 2 * kRows + 2 * kPairs;
+    static constexpr int kDepth = 2;                                   // stages of a warp
+    static constexpr int kOffO = kFewWarps * kDepth * kStage;          // float [warps][8 NT][D + 4]
+    static constexpr int kOffMl = kOffO + kFewWarps * 8 * NT * (D + 4) * 4;      // float2 [warps][8 NT]
+    static constexpr int kOffBars = kOffMl + kFewWarps * 8 * NT * 8;
+    static constexpr int kOffAbort = kOffBars + kFewWarps * kDepth * 8;
+    static constexpr int kBytes = kOffAbort + 16;
 };
+
+// Which key stands in row r of a 16-key tile of the products: rows 2 and 3, 6 and 7, ... are exchanged, so that the four keys whose V
+// a quarter of the lanes reads at once do not all begin at one bank (64 bytes a row: every second one does).
+__device__ __forceinline__ int key_of_row(int r) { return r ^ ((r >> 1) & 1); }
+
 __device__ __forceinline__ float pair_least(uint32_t p) { return __uint_as_float(p << 16); }
 __device__ __forceinline__ float pair_scale(uint32_t p) { return __uint_as_float(p & 0xffff0000u); }
 
+// The running state of a warp's columns (query rows): lane 4 g + t has columns 2 t and 2 t + 1 of every eight.
 template <int D, int NT>
-__global__ void __launch_bounds__(32 * kFewWarps) wpp_kv4_few_kernel(const Kv4AttnParams p) {
+struct FewState {
+    float o[NT][D / 16][4];            // O^T / v_ref
+    float m[NT][2], l[NT][2], off[NT][2];            // off: sum of p (least + 8 scale) over this lane's keys
+    float v_ref, v_inv;                // a power of two that V's scales are taken relative to
+};
+
+// 32 keys, at shared-memory address `at`.  Lane 4 g + t takes, of a tile's rows g and g + 8, columns [t D / 4, (t + 1) D / 4) of K; of
+// rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9, columns [g D / 8, (g + 1) D / 8) of V; and the number pairs of rows g and g + 8.
+template <int D, int NT, bool kMasked>
+__device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at, const uint32_t (&qf)[NT][D / 16][2],
+                                         const float (&q_sum)[NT][2], const float (&q_scale)[NT][2], int key0, int first_pos, int toks, int last,
+                                         float scale_log2, uint32_t k1024, int g, int t) {
+    using M = FewSmem<D, NT>;
+    const int kg = key_of_row(g), kt = key_of_row(2 * t);
+    int limit[NT][2];                                                  // last key that the column's row sees
+    if (kMasked) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) limit[nt][c] = first_pos + (8 * nt + 2 * t + c) % toks;
+    }
+    // ---- S^T = (codes - 8) Q^T, then the scores in log2 units
+    float s[2][NT][4];
+    float vs[2][2], vo[2][2];
+    const uint32_t k_at = at + kg * (D / 2) + t * (D / 8), p_at = at + 2 * M::kRows + kg * 4;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t k[2][D / 32];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) load_words<D / 32>(k[i], k_at + (16 * h + 8 * i) * (D / 2));
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[h][nt][i] = 0.f;
+#pragma unroll
+        for (int w = 0; w < D / 32; ++w) {
+            uint32_t wa = k[0][w], wb = k[1][w];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint32_t a0 = codes_low(wa, k1024), a1 = codes_low(wb, k1024), a2 = codes_high(wa, k1024), a3 = codes_high(wb, k1024);
+                wa >>= 8;
+                wb >>= 8;
+#pragma unroll
+                for (int nt = 0; nt < NT; ++nt) mma_f16(s[h][nt], a0, a1, a2, a3, qf[nt][2 * w + u][0], qf[nt][2 * w + u][1]);
+            }
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int key = key0 + 16 * h + 8 * i + kg;
+            uint32_t kp[1], vp[1];
+            load_words<1>(kp, p_at + (16 * h + 8 * i) * 4);
+            load_words<1>(vp, p_at + M::kPairs + (16 * h + 8 * i) * 4);
+            const float ks = pair_scale(kp[0]) * scale_log2, ko = fmaf(8.f, ks, pair_least(kp[0]) * scale_log2);
+            vs[h][i] = pair_scale(vp[0]);
+            if (kMasked && key > last) vs[h][i] = 0.f;                 // (no row sees it: its pair may be anything)
+            vo[h][i] = fmaf(8.f, vs[h][i], pair_least(vp[0]));
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    float& y = s[h][nt][2 * i + c];
+                    y = fmaf(y, ks * q_scale[nt][c], ko * q_sum[nt][c]);
+                    if (kMasked && key > limit[nt][c]) y = -INFINITY;
+                }
+        }
+    // ---- references move only where a score or a scale is far above them
+    bool move = false;
+    float mx[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            mx[nt][c] = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
+            move |= mx[nt][c] > st.m[nt][c] + kFewSlack;
+        }
+    float v = fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[1][0], vs[1][1]));
+    move |= v * st.v_inv > kFewScaleSlack;
+    if (__any_sync(0xffffffffu, move)) {
+#pragma unroll
+        for (int w = 4; w < 32; w *= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, w));
+        float shrink = 1.f;
+        if (v * st.v_inv > 1.f) {
+            const float ref = __uint_as_float(min((__float_as_uint(v) & 0x7f800000u) + 0x00800000u, 0x7e800000u));     // (2^126 at most)
+            shrink = st.v_ref * __frcp_rn(ref);
+            st.v_ref = ref;
+            st.v_inv = __frcp_rn(ref);
+        }
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float y = fmaxf(st.m[nt][c], mx[nt][c]);
+#pragma unroll
+                for (int w = 4; w < 32; w *= 2) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, w));
+                const float a = st.m[nt][c] == -INFINITY ? 1.f : fast_exp2(st.m[nt][c] - y);        // (without a reference there is nothing to scale)
+                st.m[nt][c] = y;
+                st.l[nt][c] *= a;
+                st.off[nt][c] *= a;
+#pragma unroll
+                for (int mt = 0; mt < D / 16; ++mt) {
+                    st.o[nt][mt][c] *= a * shrink;
+                    st.o[nt][mt][2 + c] *= a * shrink;
+                }
+            }
+    }
+    // ---- P^T, its rows times the keys' V scales, turned round into the second factor of O^T = V^T P^T
+    uint32_t pb[2][NT][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float vi = vs[h][i] * st.v_inv;
+#pragma unroll
+            for (int nt = 0; nt < NT; ++nt) {
+                float e[2];
+#pragma unroll
+                for (int c = 0; c < 2; ++c) {
+                    const bool out = kMasked && key0 + 16 * h + 8 * i + kg > limit[nt][c];
+                    const float ref = kMasked && st.m[nt][c] == -INFINITY ? 0.f : st.m[nt][c];
+                    e[c] = out ? 0.f : fast_exp2(s[h][nt][2 * i + c] - ref);
+                    st.l[nt][c] += e[c];
+                    st.off[nt][c] = out ? st.off[nt][c] : fmaf(e[c], vo[h][i], st.off[nt][c]);
+                }
+                pb[h][nt][i] = transpose_8x8(pack_f16x2(e[0] * vi, e[1] * vi));
+            }
+        }
+    // ---- O^T += (codes - 8)^T P^T: a word holds four codes of one key and of the next, one above the other
+    const uint32_t v_at = at + M::kRows + g * (D / 16);
+    const int flip = kt & 1 ? -(D / 2) : D / 2;                        // from row 2 t's key to row 2 t + 1's
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t v[4][D / 64];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) load_words<D / 64>(v[i], v_at + (16 * h + kt) * (D / 2) + (i & 1) * flip + 8 * (i >> 1) * (D / 2));
+#pragma unroll
+        for (int w = 0; w < D / 64; ++w)
+#pragma unroll
+            for (int hw = 0; hw < 2; ++hw) {
+                uint32_t lo = __byte_perm(v[0][w], v[1][w], hw ? 0x7632 : 0x5410);
+                uint32_t hi = __byte_perm(v[2][w], v[3][w], hw ? 0x7632 : 0x5410);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t a0 = codes_low(lo, k1024), a1 = codes_high(lo, k1024), a2 = codes_low(hi, k1024), a3 = codes_high(hi, k1024);
+                    lo >>= 8;
+                    hi >>= 8;
+#pragma unroll
+                    for (int nt = 0; nt < NT; ++nt) mma_f16(st.o[nt][4 * w + 2 * hw + u], a0, a1, a2, a3, pb[h][nt][0], pb[h][nt][1]);
+                }
+            }
+    }
+}
+
+template <int D, int NT>
+__device__ __forceinline__ bool few_unit(const Kv4AttnParams& p, const int unit, uint8_t* smem, uint32_t& used) {
+    using M = FewSmem<D, NT>;
     constexpr int kSteps = D / 16;             // 16-wide pieces of a row
-    __shared__ float s_o[kFewWarps][8 * NT][D + 4];
-    __shared__ float2 s_ml[kFewWarps][8 * NT];
+    float (*s_o)[8 * NT][D + 4] = reinterpret_cast<float (*)[8 * NT][D + 4]>(smem + M::kOffO);
+    float2 (*s_ml)[8 * NT] = reinterpret_cast<float2 (*)[8 * NT]>(smem + M::kOffMl);
+    volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + M::kOffAbort);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    grid_dependency_wait();
     const char* plan = static_cast<const char*>(p.plan);
-    const WppUnit un = reinterpret_cast<const WppUnit*>(plan + p.off_units)[blockIdx.x];
+    const WppUnit un = reinterpret_cast<const WppUnit*>(plan + p.off_units)[unit];
     const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets);
     const int q_off = q_offsets[un.request], P = p.prefix_lens[un.request], C = p.chunk_lens[un.request];
     if (P != reinterpret_cast<const int32_t*>(plan + p.off_prefix)[un.request] || C != q_offsets[un.request + 1] - q_off) {
@@ -94,199 +269,144 @@ __global__ void __launch_bounds__(32 * kFewWarps) wpp_kv4_few_kernel(const Kv4At
         // (the combine pass reads the parts of a refused request too: none of them has seen a key)
         if (un.split_slot >= 0 && threadIdx.x < un.rows[0] * un.rows[1])
             p.ws_lse[((int64_t)un.split_slot * 2 + un.row0[1]) * 128 + un.head[1] + threadIdx.x] = -INFINITY;
-        return;
+        return true;
     }
     const int toks = un.rows[0], rows = toks * un.rows[1], first_pos = P + un.row0[0];     // first_pos: last key that token 0 sees
-    const int kv_len = min(P + C, un.kv_end * WPP_TILE_N), key_begin = un.kv_begin * WPP_TILE_N;
-    const int seen = min(kv_len, first_pos + toks);                                        // keys that some row sees end here
-    const int tiles = (max(seen - key_begin, 0) + 15) / 16;
-    const int kvh = un.head[0] / p.group, page_shift = 31 - __clz(p.page_size);
+    const int key_begin = un.kv_begin * WPP_TILE_N;
+    const int seen = min(min(P + C, un.kv_end * WPP_TILE_N), first_pos + toks);            // keys that some row sees end here
+    const int kvh = un.head[0] / p.group, page_shift = 31 - __clz(p.page_size), in_page = p.page_size - 1;
     const int32_t* table = p.block_tables + (int64_t)un.request * p.max_blocks;
 
-    // ---- Q as the products' second factor, and the sums of its rows
-    uint32_t qf[NT][kSteps][2];
-    float q_sum[NT][2];
+    // ---- the warp's keys: 32 at a time, every kFewWarps-th, in the warp's ring of stages (`used`: stages taken so far, by all units)
+    constexpr int kStride = kFewKeys * kFewWarps;
+    const uint32_t stages = smem_u32(smem) + warp * M::kDepth * M::kStage, bars = smem_u32(smem + M::kOffBars) + warp * M::kDepth * 8;
+    auto request = [&](int key, uint32_t stage) {
+        const int halves = min((seen - key + 15) / 16, 2);
+        const bool small = p.page_size == 16;                          // the second 16 keys have a page of their own then
+        if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, halves * (M::kStage / 2));
+        __syncwarp();
+        const int h = lane >> 2, what = lane & 3;                      // K's rows, V's rows, K's pairs, V's pairs
+        if (h < (small ? halves : 1)) {
+            int page = table[(key + 16 * h) >> page_shift];
+            if (page < 0 || page >= p.num_pages) {
+                if (p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
+                page = 0;
+            }
+            const int keys = small ? 16 : 16 * halves, row = what < 2 ? D / 2 : 4;
+            const uint8_t* src = (what & 1 ? p.v_cache : p.k_cache) + page * p.page_bytes + kvh * p.head_bytes + (what < 2 ? 0 : p.page_size * (D / 2)) +
+                                 ((key + 16 * h) & in_page) * row;
+            const uint32_t dst = stages + stage * M::kStage + (what < 2 ? what * M::kRows : 2 * M::kRows + (what & 1) * M::kPairs) + 16 * h * row;
+            bulk_load(dst, src, keys * row, bars + 8 * stage);
+        }
+    };
+    int key = key_begin + warp * kFewKeys;
+#pragma unroll
+    for (int i = 0; i < M::kDepth; ++i)
+        if (key + i * kStride < seen) request(key + i * kStride, (used + i) % M::kDepth);
+
+    // ---- Q as the first product's second factor: f16 numbers q 2^e, e so that the row's largest is in [2^7, 2^8) (what is less than
+    //      2^-21 of that may be off by 2^-32 of it); and the sums of its rows
+    uint32_t qf[NT][D / 16][2];
+    float q_sum[NT][2], q_scale[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int n = 8 * nt + g;
-        float sum = 0.f;
+        uint4 z[D / 32];
+        float sum = 0.f, top = 0.f;
 #pragma unroll
-        for (int w = 0; w < kSteps / 2; ++w) {
-            uint4 z = make_uint4(0, 0, 0, 0);
+        for (int w = 0; w < D / 32; ++w) {
+            z[w] = make_uint4(0, 0, 0, 0);
             if (n < rows) {
                 const int head = un.head[0] + n / toks, tok = q_off + un.row0[0] + n % toks;
-                z = *reinterpret_cast<const uint4*>(p.q + (int64_t)tok * p.q_token_stride + (int64_t)head * p.q_head_stride + t * (D / 4) + 8 * w);
+                z[w] = *reinterpret_cast<const uint4*>(p.q + (int64_t)tok * p.q_token_stride + (int64_t)head * p.q_head_stride + t * (D / 4) + 8 * w);
             }
-            // elements s and s + 4 of the eight stand side by side, as the codes of a word do
-            qf[nt][2 * w][0] = __byte_perm(z.x, z.z, 0x5410);
-            qf[nt][2 * w][1] = __byte_perm(z.x, z.z, 0x7632);
-            qf[nt][2 * w + 1][0] = __byte_perm(z.y, z.w, 0x5410);
-            qf[nt][2 * w + 1][1] = __byte_perm(z.y, z.w, 0x7632);
-            const uint32_t zz[4] = {z.x, z.y, z.z, z.w};
+            const uint32_t zz[4] = {z[w].x, z[w].y, z[w].z, z[w].w};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sum += __uint_as_float(zz[i] << 16) + __uint_as_float(zz[i] & 0xffff0000u);
+            for (int i = 0; i < 4; ++i) {
+                const float a = __uint_as_float(zz[i] << 16), b = __uint_as_float(zz[i] & 0xffff0000u);
+                sum += a + b;
+                top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
+            }
         }
-        sum += __shfl_xor_sync(0xffffffffu, sum, 1);
-        sum += __shfl_xor_sync(0xffffffffu, sum, 2);
-        q_sum[nt][0] = __shfl_sync(0xffffffffu, sum, 8 * t);            // of the columns this thread has of S^T: 2 t, 2 t + 1
-        q_sum[nt][1] = __shfl_sync(0xffffffffu, sum, 8 * t + 4);
-    }
-    int limit[NT][2];                                                  // last key that the column's row sees
 #pragma unroll
-    for (int nt = 0; nt < NT; ++nt) {
-        limit[nt][0] = first_pos + (8 * nt + 2 * t) % toks;
-        limit[nt][1] = first_pos + (8 * nt + 2 * t + 1) % toks;
+        for (int w = 1; w < 4; w *= 2) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, w);
+            top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+        }
+        // 2^e and 2^-e, both normal numbers
+        const int e = min(max(134 - (int)(__float_as_uint(top) >> 23), -119), 126);
+        const float up = __uint_as_float((uint32_t)(127 + e) << 23), down = __uint_as_float((uint32_t)(127 - e) << 23);
+#pragma unroll
+        for (int w = 0; w < D / 32; ++w) {
+            const uint32_t zz[4] = {z[w].x, z[w].y, z[w].z, z[w].w};
+            float y[8];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                y[2 * i] = __uint_as_float(zz[i] << 16) * up;
+                y[2 * i + 1] = __uint_as_float(zz[i] & 0xffff0000u) * up;
+            }
+            // elements i and i + 4 of the eight stand side by side, as the codes of a word do
+#pragma unroll
+            for (int i = 0; i < 4; ++i) qf[nt][2 * w + (i >> 1)][i & 1] = pack_f16x2(y[i], y[i + 4]);
+        }
+        // of the columns this thread has of S^T: 2 t, 2 t + 1
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+            q_sum[nt][c] = __shfl_sync(0xffffffffu, sum, 8 * t + 4 * c);
+            q_scale[nt][c] = __shfl_sync(0xffffffffu, down, 8 * t + 4 * c);
+        }
     }
-
-    float o[NT][kSteps][4], m[NT][2], l[NT][2], off[NT][2];            // off: sum of p (least + 8 scale)
+    FewState<D, NT> st;
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
 #pragma unroll
         for (int mt = 0; mt < kSteps; ++mt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) o[nt][mt][i] = 0.f;
+            for (int i = 0; i < 4; ++i) st.o[nt][mt][i] = 0.f;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            m[nt][i] = -INFINITY;
-            l[nt][i] = off[nt][i] = 0.f;
+            st.m[nt][i] = -INFINITY;
+            st.l[nt][i] = st.off[nt][i] = 0.f;
         }
     }
+    st.v_ref = 8.67361738e-19f;        // 2^-60
+    st.v_inv = 1.15292150e18f;
 
-    int bad = 0;
-    auto page_of = [&](int tile) -> int {                              // physical page of a 16-key tile, 0 if the table has none
-        if (tile >= tiles) return 0;
-        const int page = table[(key_begin + tile * 16) >> page_shift];
-        if (page >= 0 && page < p.num_pages) return page;
-        bad = 1;
-        return 0;
-    };
-    auto load = [&](FewKeys<D>& x, int tile, int page) {
-        if (tile >= tiles) return;
-        const int64_t block = page * p.page_bytes + kvh * p.head_bytes;
-        x.load(p.k_cache + block, p.v_cache + block, (key_begin + tile * 16) & (p.page_size - 1), p.page_size, g, t);
-    };
-    FewKeys<D> next;
-    int next_page = page_of(warp);
-    load(next, warp, next_page);
-    next_page = page_of(warp + kFewWarps);
-    for (int tile = warp; tile < tiles; tile += kFewWarps) {
-        FewKeys<D> x = next;
-        load(next, tile + kFewWarps, next_page);
-        next_page = page_of(tile + 2 * kFewWarps);
-        const int key0 = key_begin + tile * 16;
-
-        // ---- S^T = (128 + codes) Q^T, then the scores in log2 units
-        float s[NT][4];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[nt][i] = 0.f;
-#pragma unroll
-        for (int ks = 0; ks < kSteps; ++ks) {
-            const uint32_t wa = x.k[0][ks >> 1], wb = x.k[1][ks >> 1];
-            const int sh = 8 * (ks & 1);
-            const uint32_t a0 = codes_128(wa, sh), a1 = codes_128(wb, sh), a2 = codes_128(wa, sh + 4), a3 = codes_128(wb, sh + 4);
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt) mma_16816(s[nt], a0, a1, a2, a3, qf[nt][ks][0], qf[nt][ks][1]);
-        }
-        float vs[2], vo[2];
-        const bool masked = key0 + 15 > first_pos;                     // some row does not see every key of the tile
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float ks = pair_scale(x.kp[i]) * p.scale_log2, ko = fmaf(-128.f, ks, pair_least(x.kp[i]) * p.scale_log2);
-            vs[i] = pair_scale(x.vp[i]);
-            vo[i] = fmaf(8.f, vs[i], pair_least(x.vp[i]));
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) s[nt][2 * i + c] = fmaf(s[nt][2 * i + c], ks, ko * q_sum[nt][c]);
-        }
-        if (masked) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (key0 + g + 8 * (i >> 1) > limit[nt][i & 1]) s[nt][i] = -INFINITY;
-        }
-        // ---- references move only where a score is far above them
-        bool move = false;
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int c = 0; c < 2; ++c) move |= fmaxf(s[nt][c], s[nt][2 + c]) > m[nt][c] + kFewSlack;
-        if (__any_sync(0xffffffffu, move)) {
-#pragma unroll
-            for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    float mx = fmaxf(m[nt][c], fmaxf(s[nt][c], s[nt][2 + c]));
-#pragma unroll
-                    for (int w = 4; w < 32; w *= 2) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, w));
-                    const float a = m[nt][c] == -INFINITY ? 0.f : fast_exp2(m[nt][c] - mx);
-                    m[nt][c] = mx;
-                    l[nt][c] *= a;
-                    off[nt][c] *= a;
-#pragma unroll
-                    for (int mt = 0; mt < kSteps; ++mt) {
-                        o[nt][mt][c] *= a;
-                        o[nt][mt][2 + c] *= a;
-                    }
-                }
-        }
-        // ---- P^T, its rows times the keys' V scales, turned round into the second factor of O^T = V^T P^T
-        uint32_t pb[NT][2];
-#pragma unroll
-        for (int nt = 0; nt < NT; ++nt)
-#pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                float e[2];
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const float ref = m[nt][c] == -INFINITY ? 0.f : m[nt][c];
-                    const bool out = masked && key0 + g + 8 * i > limit[nt][c];
-                    e[c] = out ? 0.f : fast_exp2(s[nt][2 * i + c] - ref);
-                    l[nt][c] += e[c];
-                    off[nt][c] = out ? off[nt][c] : fmaf(e[c], vo[i], off[nt][c]);
-                    e[c] = out ? 0.f : e[c] * vs[i];
-                }
-                pb[nt][i] = transpose_8x8(pack_bf16x2(e[0], e[1]));
-            }
-        // ---- O^T += (codes - 8)^T P^T: a word holds two codes of one key and two of the next, one above the other
-#pragma unroll
-        for (int w = 0; w < D / 64; ++w)
-#pragma unroll
-            for (int hw = 0; hw < 2; ++hw) {
-                const uint32_t lo = __byte_perm(x.v[0][w], x.v[1][w], hw ? 0x7632 : 0x5410);
-                const uint32_t hi = __byte_perm(x.v[2][w], x.v[3][w], hw ? 0x7632 : 0x5410);
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const uint32_t a0 = codes_8(lo, 8 * u), a1 = codes_8(lo, 8 * u + 4), a2 = codes_8(hi, 8 * u), a3 = codes_8(hi, 8 * u + 4);
-#pragma unroll
-                    for (int nt = 0; nt < NT; ++nt) mma_16816(o[nt][4 * w + 2 * hw + u], a0, a1, a2, a3, pb[nt][0], pb[nt][1]);
-                }
-            }
+    bool ok = true;
+    for (; key < seen; key += kStride, ++used) {
+        const uint32_t stage = used % M::kDepth, phase = used / M::kDepth & 1u, at = stages + stage * M::kStage;
+        ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * stage, phase, abort_flag));
+        if (!ok) break;
+        if (key + kFewKeys - 1 <= first_pos && key + kFewKeys <= seen)
+            few_step<D, NT, false>(st, at, qf, q_sum, q_scale, key, first_pos, toks, seen - 1, p.scale_log2, p.f16_1024, g, t);
+        else
+            few_step<D, NT, true>(st, at, qf, q_sum, q_scale, key, first_pos, toks, seen - 1, p.scale_log2, p.f16_1024, g, t);
+        __syncwarp();                          // (every lane has read the stage)
+        if (key + M::kDepth * kStride < seen) request(key + M::kDepth * kStride, stage);
     }
-    if (bad && p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
 
     // ---- the warps' parts joined
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
+            float l = st.l[nt][c], off = st.off[nt][c];
 #pragma unroll
             for (int w = 4; w < 32; w *= 2) {
-                l[nt][c] += __shfl_xor_sync(0xffffffffu, l[nt][c], w);
-                off[nt][c] += __shfl_xor_sync(0xffffffffu, off[nt][c], w);
+                l += __shfl_xor_sync(0xffffffffu, l, w);
+                off += __shfl_xor_sync(0xffffffffu, off, w);
             }
             const int n = 8 * nt + 2 * t + c;
-            if (g == 0) s_ml[warp][n] = make_float2(m[nt][c], l[nt][c]);
+            if (g == 0) s_ml[warp][n] = make_float2(st.m[nt][c], l);
 #pragma unroll
             for (int mt = 0; mt < kSteps; ++mt) {
                 const int d0 = g * (D / 8) + 2 * mt;       // element 8 w + 4 hw + 2 u of the thread's columns, mt = 4 w + 2 hw + u
-                *reinterpret_cast<float2*>(&s_o[warp][n][d0]) = make_float2(o[nt][mt][c] + off[nt][c], o[nt][mt][2 + c] + off[nt][c]);
+                *reinterpret_cast<float2*>(&s_o[warp][n][d0]) =
+                    make_float2(fmaf(st.o[nt][mt][c], st.v_ref, off), fmaf(st.o[nt][mt][2 + c], st.v_ref, off));
             }
         }
     __syncthreads();
+    if (*abort_flag) return false;
     for (int i = threadIdx.x; i < rows * (D / 4); i += 32 * kFewWarps) {
         const int n = i / (D / 4), c = i % (D / 4) * 4;
         float mm = -INFINITY, sum = 0.f;
@@ -321,25 +441,64 @@ __global__ void __launch_bounds__(32 * kFewWarps) wpp_kv4_few_kernel(const Kv4At
             if (c == 0) p.ws_lse[row] = lse2;
         }
     }
+    return true;
 }
 
-template <int D>
-static cudaError_t launch_few(const Kv4AttnParams& p, int num_units, int max_rows, cudaStream_t stream) {
+template <int D, int NT>
+__global__ void __launch_bounds__(32 * kFewWarps, NT == 1 ? 4 : 3) wpp_kv4_few_kernel(const Kv4AttnParams p) {
+    using M = FewSmem<D, NT>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    if (threadIdx.x < kFewWarps * M::kDepth) mbar_init(smem_u32(smem + M::kOffBars) + 8 * threadIdx.x, 1);
+    if (threadIdx.x == 0) *reinterpret_cast<volatile uint32_t*>(smem + M::kOffAbort) = 0u;
+    fence_barrier_init();
+    __syncthreads();
+    grid_launch_dependents();
+    grid_dependency_wait();
+    const int32_t* first = reinterpret_cast<const int32_t*>(static_cast<const char*>(p.plan) + p.off_few_ctas) + blockIdx.x;
+    const int end = first[1];
+    uint32_t used = 0;                         // (per warp)
+    for (int u = first[0]; u < end; ++u) {
+        if (!few_unit<D, NT>(p, u, smem, used)) break;
+        __syncthreads();                       // (the next unit's parts take the place of this one's)
+    }
+    if (*reinterpret_cast<volatile uint32_t*>(smem + M::kOffAbort)) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 400000) { }    // let copies in flight land
+        if (threadIdx.x == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_TIMEOUT);
+    }
+}
+
+template <int D, int NT>
+static cudaError_t launch_few_nt(const Kv4AttnParams& p, int num_ctas, cudaStream_t stream) {
+    static bool attr_set[64] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev >= 0 && dev < 64 && !attr_set[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(wpp_kv4_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, FewSmem<D, NT>::kBytes);
+        if (e != cudaSuccess) return e;
+        attr_set[dev] = true;
+    }
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)num_units);
+    cfg.gridDim = dim3((unsigned)num_ctas);
     cfg.blockDim = dim3(32 * kFewWarps);
+    cfg.dynamicSmemBytes = FewSmem<D, NT>::kBytes;
     cfg.stream = stream;
     cudaLaunchAttribute overlap;
     overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
     overlap.val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = &overlap;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, max_rows <= 8 ? wpp_kv4_few_kernel<D, 1> : wpp_kv4_few_kernel<D, 2>, p);
+    return cudaLaunchKernelEx(&cfg, wpp_kv4_few_kernel<D, NT>, p);
+}
+
+template <int D>
+static cudaError_t launch_few(const Kv4AttnParams& p, int num_ctas, int max_rows, cudaStream_t stream) {
+    return max_rows <= 8 ? launch_few_nt<D, 1>(p, num_ctas, stream) : launch_few_nt<D, 2>(p, num_ctas, stream);
 }
 
 }  // namespace wpp
 
-extern "C" int wpp_launch_kv4_few(int head_dim, const wpp::Kv4AttnParams* p, int num_units, int max_rows, void* stream) {
-    return (int)(head_dim == 128 ? wpp::launch_few<128>(*p, num_units, max_rows, (cudaStream_t)stream)
-                                 : wpp::launch_few<64>(*p, num_units, max_rows, (cudaStream_t)stream));
+extern "C" int wpp_launch_kv4_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream) {
+    return (int)(head_dim == 128 ? wpp::launch_few<128>(*p, num_ctas, max_rows, (cudaStream_t)stream)
+                                 : wpp::launch_few<64>(*p, num_ctas, max_rows, (cudaStream_t)stream));
 }

@@ -28,8 +28,9 @@ struct WppPlanHeader {
     int32_t max_combine_rows;       // most rows of a combine record (sizes the combine pass's grid)
     int32_t deal_items;             // small shape: its items are dealt out to the CTAs, without the workspace's counter
     int32_t num_few_units;          // 4-bit cache: the first of the units are of the kernel for few rows ...
-    int32_t max_few_rows;           // ... and the most rows one of them has
-    uint32_t pad[2];
+    int32_t max_few_rows;           // ... which has so many rows at most; ...
+    int32_t num_few_ctas;
+    uint32_t off_few_ctas;          // ... int32 [num_few_ctas + 1]: every CTA's first unit
 };
 
 // One work tile = two 128-row "halves" that share one K/V stream (same request, same KV head).  Each half

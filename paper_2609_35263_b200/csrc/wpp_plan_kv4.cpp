@@ -9,8 +9,10 @@
 
 static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
-constexpr int kFewCtas = 4;              // CTAs of the kernel for few rows that an SM holds
-constexpr int32_t kMaxParts = 64;
+// The kernel for few rows: CTAs that an SM holds, of blocks of at most 8 rows and of more; what a unit costs besides its key steps, in
+// steps; and the fewest steps that a block is cut for.
+constexpr int kFewCtas = 4, kFewCtasWide = 3;
+constexpr int64_t kUnitSteps = 3, kLeastSteps = 2;
 
 // Row blocks of the kernel for few rows: heads of a KV group, and tokens, WPP_FEW_ROWS rows at most.
 static int32_t few_heads(int32_t group) { return std::min<int32_t>(group, WPP_FEW_ROWS); }
@@ -24,9 +26,9 @@ static int64_t few_blocks(const wpp_batch_desc* d, int64_t C) {
 size_t wpp_kv4_plan_bytes(const wpp_batch_desc* d, const wpp_plan_opts* o, int64_t T) {
     const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
     const int64_t base = (T / t + d->num_requests) * ((G + h - 1) / h) * d->num_kv_heads;
-    const int64_t units = o->force_kv_splits >= 2 ? base * o->force_kv_splits : 2 * base + 2 * kFewCtas * (int64_t)o->max_ctas;
+    const int64_t units = o->force_kv_splits >= 2 ? base * o->force_kv_splits : base + kFewCtas * (int64_t)o->max_ctas;
     size_t n = sizeof(WppPlanHeader) + 2 * align_up(sizeof(int32_t) * (size_t)(d->num_requests + 1), 16);
-    n += sizeof(WppUnit) * (size_t)units;
+    n += sizeof(WppUnit) * (size_t)units + align_up(sizeof(int32_t) * ((size_t)std::max(units, kFewCtas * (int64_t)o->max_ctas) + 1), 16);
     n += sizeof(WppCombine) * (size_t)(T * d->num_q_heads / t + (int64_t)d->num_requests * d->num_q_heads);
     return align_up(n, 256);
 }
@@ -38,16 +40,20 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     auto steps_for = [](int64_t keys) { return (int32_t)((keys + WPP_TILE_N - 1) / WPP_TILE_N); };
 
     const int32_t heads = few_heads(G), toks = few_tokens(G);
-    // parts: of equal length, so many that the SMs' CTAs have one each
+    // The CTAs take equal shares of the blocks' key steps, in order: a block is cut where a share ends.
     int64_t n_base = 0, all_steps = 0;
+    int32_t max_rows = 0;
     for (int i = 0; i < R; ++i) {
-        const int64_t n = few_blocks(d, chunk_lens[i]);
-        n_base += n;
-        all_steps += n * steps_for((int64_t)prefix_lens[i] + chunk_lens[i]);
+        n_base += few_blocks(d, chunk_lens[i]);
+        for (int64_t r0 = 0; r0 < chunk_lens[i]; r0 += toks) {
+            const int32_t rows = (int32_t)std::min<int64_t>(toks, chunk_lens[i] - r0);
+            all_steps += steps_for(prefix_lens[i] + r0 + rows) * (int64_t)((G + heads - 1) / heads) * Hkv;
+            max_rows = std::max(max_rows, rows * heads);
+        }
     }
     if (n_base > 0x3fffffff) return WPP_ERR_INVALID_ARG;
-    const int64_t slots_at_once = (int64_t)kFewCtas * o->max_ctas;
-    const int64_t part = std::max<int64_t>(1, (all_steps + slots_at_once - 1) / slots_at_once);
+    const int64_t most_ctas = (int64_t)(max_rows <= 8 ? kFewCtas : kFewCtasWide) * o->max_ctas;
+    const int64_t share = std::max<int64_t>((all_steps + kUnitSteps * (n_base + most_ctas) + most_ctas - 1) / most_ctas, kUnitSteps + kLeastSteps);
 
     WppPlanHeader hd;
     std::memset(&hd, 0, sizeof(hd));
@@ -63,17 +69,36 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     WppUnit* us = reinterpret_cast<WppUnit*>(p + hd.off_units);
     std::vector<WppCombine> combines;
     int64_t n_units = 0, n_split = 0, key_steps = 0;
-    int32_t max_rows = 0;
+    std::vector<int32_t> first{0};           // of every CTA's units
+    int64_t left = share;                    // of the current CTA's share
     int32_t slots = 0, slot0 = 0, slot_parts = 0, slot_row = 2 * WPP_HALF_M;      // the slots that have room: from slot0 on, row slot_row
+    std::vector<int32_t> cuts;
     for (int i = 0; i < R; ++i) {
         const int64_t P = prefix_lens[i], C = chunk_lens[i];
         for (int64_t r0 = 0; r0 < C; r0 += toks) {
             const int32_t rows = (int32_t)std::min<int64_t>(toks, C - r0), steps = steps_for(P + r0 + rows);
-            int32_t parts = (int32_t)std::min<int64_t>({(steps + part - 1) / part, steps, kMaxParts});
-            if (o->force_kv_splits >= 1) parts = std::min(o->force_kv_splits, steps);
             for (int32_t kvh = 0; kvh < Hkv; ++kvh) {
                 for (int32_t h = 0; h < G; h += heads) {
                     const int32_t nh = std::min(heads, G - h);
+                    cuts.assign(1, 0);
+                    if (o->force_kv_splits >= 1) {
+                        const int32_t n = std::min(o->force_kv_splits, steps);
+                        for (int32_t q = 1; q <= n; ++q) cuts.push_back((int32_t)((int64_t)steps * q / n));
+                    } else {
+                        for (int32_t at = 0; at < steps;) {
+                            // a CTA takes what is left of its share, no less than kLeastSteps, and the rest too if that is little
+                            if (left < kUnitSteps + kLeastSteps && (int64_t)first.size() < most_ctas && left < share) {
+                                first.push_back((int32_t)(n_units + cuts.size() - 1));
+                                left = share;
+                            }
+                            int32_t n = (int32_t)std::min<int64_t>(steps - at, std::max<int64_t>(left - kUnitSteps, kLeastSteps));
+                            if (steps - at - n < kLeastSteps || (int64_t)first.size() >= most_ctas) n = steps - at;
+                            left -= n + kUnitSteps;
+                            at += n;
+                            cuts.push_back(at);
+                        }
+                    }
+                    const int32_t parts = (int32_t)cuts.size() - 1;
                     if (n_units + parts > unit_cap) return WPP_ERR_PLAN_MISMATCH;
                     WppUnit u;
                     std::memset(&u, 0, sizeof(u));
@@ -84,7 +109,6 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
                     u.head[0] = kvh * G + h;
                     u.split_slot = -1;
                     u.pack = 1;
-                    max_rows = std::max(max_rows, rows * nh);
                     if (parts > 1) {
                         if (parts > slot_parts || slot_row + WPP_FEW_ROWS > 2 * WPP_HALF_M) {
                             slot0 = slots;
@@ -99,8 +123,8 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
                             combines.push_back({i, (int32_t)r0, rows, u.head[0] + k, slot0, parts, u.row0[1], u.head[1] + k * rows});
                     }
                     for (int32_t q = 0; q < parts; ++q) {
-                        u.kv_begin = (int32_t)((int64_t)steps * q / parts);
-                        u.kv_end = (int32_t)((int64_t)steps * (q + 1) / parts);
+                        u.kv_begin = cuts[(size_t)q];
+                        u.kv_end = cuts[(size_t)q + 1];
                         if (parts > 1) u.split_slot = slot0 + q;
                         u.cost = u.kv_end - u.kv_begin;
                         us[n_units++] = u;
@@ -113,10 +137,21 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     }
     if (n_units > 0x3fffffff) return WPP_ERR_INVALID_ARG;
     off += sizeof(WppUnit) * (size_t)n_units;
+    if (o->force_kv_splits >= 1) {
+        first.clear();
+        for (int64_t u = 0; u < n_units; ++u) first.push_back((int32_t)u);
+    }
+    const int32_t few_ctas = n_units > 0 ? (int32_t)first.size() : 0;
+    first.push_back((int32_t)n_units);
+    if (off + align_up(sizeof(int32_t) * first.size(), 16) > plan_host_bytes) return WPP_ERR_PLAN_MISMATCH;
+    hd.off_few_ctas = (uint32_t)off;
+    std::memset(p + off, 0, align_up(sizeof(int32_t) * first.size(), 16));
+    off += align_up(sizeof(int32_t) * first.size(), 16);
     hd.off_combine = (uint32_t)off;
     off += sizeof(WppCombine) * combines.size();
     hd.plan_bytes = align_up(off, 16);
     if (hd.plan_bytes > plan_host_bytes) return WPP_ERR_PLAN_MISMATCH;
+    std::memcpy(p + hd.off_few_ctas, first.data(), sizeof(int32_t) * first.size());
     if (!combines.empty()) std::memcpy(p + hd.off_combine, combines.data(), sizeof(WppCombine) * combines.size());
     std::memset(p + off, 0, hd.plan_bytes - off);
 
@@ -124,9 +159,10 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     hd.version = WPP_PLAN_VERSION;
     hd.desc_hash = wpp_desc_hash(d);
     hd.num_requests = R;
-    hd.num_ctas = (int32_t)std::max<int64_t>(1, std::min<int64_t>(o->max_ctas, n_units));
+    hd.num_ctas = std::max(1, few_ctas);
     hd.num_units = (int32_t)n_units;
     hd.num_few_units = (int32_t)n_units;
+    hd.num_few_ctas = few_ctas;
     hd.max_few_rows = max_rows;
     hd.num_combine = (int32_t)combines.size();
     hd.num_split_slots = slots;

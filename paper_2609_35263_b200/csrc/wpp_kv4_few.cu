@@ -75,18 +75,25 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[kWords], uint32_t at) {
     }
 }
 
-// A warp's 32 keys in shared memory: K's rows, V's rows, K's pairs, V's pairs.  They come by bulk copies, so that no thread's
-// registers or address arithmetic are spent on what is under way.
+// A warp's ring of stages in shared memory, kFewKeys keys each: K's rows, V's rows, K's pairs, V's pairs.  The warp copies them
+// itself, asynchronously, 16 bytes a lane: no thread's registers are spent on what is under way, and warps wait for nobody else.
+// (Bulk copies took some thirty instructions each to set up, for the 64 requests' tokens 142 us with stages of a warp's own, 144
+// with a CTA's common ones, which couple the warps besides.)
 template <int D, int NT>
 struct FewSmem {
     static constexpr int kRows = kFewKeys * (D / 2), kPairs = kFewKeys * 4, kStage = 2 * kRows + 2 * kPairs;
-    static constexpr int kDepth = 2;                                   // stages of a warp
-    static constexpr int kOffO = kFewWarps * kDepth * kStage;          // float [warps][8 NT][D + 4]
-    static constexpr int kOffMl = kOffO + kFewWarps * 8 * NT * (D + 4) * 4;      // float2 [warps][8 NT]
-    static constexpr int kOffBars = kOffMl + kFewWarps * 8 * NT * 8;
-    static constexpr int kOffAbort = kOffBars + kFewWarps * kDepth * 8;
-    static constexpr int kBytes = kOffAbort + 16;
+    static constexpr int kDepth = NT == 1 ? 3 : 4;
+    // in the stages' place, once a unit's are done with: float [warps][8 NT][D + 4], float2 [warps][8 NT]
+    static constexpr int kOffMl = kFewWarps * 8 * NT * (D + 4) * 4;
+    static constexpr int kBytes = kFewWarps * kDepth * kStage;
+    static_assert(kOffMl + kFewWarps * 8 * NT * 8 <= kBytes, "a unit's results fit the stages");
 };
+__device__ __forceinline__ void copy_16(uint32_t dst, const uint8_t* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 // Which key stands in row r of a 16-key tile of the products: rows 2 and 3, 6 and 7, ... are exchanged, so that the four keys whose V
 // a quarter of the lanes reads at once do not all begin at one bank (64 bytes a row: every second one does).
@@ -108,7 +115,7 @@ struct FewState {
 template <int D, int NT, bool kMasked>
 __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at, const uint32_t (&qf)[NT][D / 16][2],
                                          const float (&q_sum)[NT][2], const float (&q_scale)[NT][2], int key0, int first_pos, int toks, int last,
-                                         float scale_log2, uint32_t k1024, int g, int t) {
+                                         uint32_t k1024, int g, int t) {
     using M = FewSmem<D, NT>;
     const int kg = key_of_row(g), kt = key_of_row(2 * t);
     int limit[NT][2];                                                  // last key that the column's row sees
@@ -118,7 +125,7 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
 #pragma unroll
             for (int c = 0; c < 2; ++c) limit[nt][c] = first_pos + (8 * nt + 2 * t + c) % toks;
     }
-    // ---- S^T = (codes - 8) Q^T, then the scores in log2 units
+    // ---- S^T = (codes - 8) Q^T, then the scores in log2 units (q_scale and q_sum have the scale)
     float s[2][NT][4];
     float vs[2][2], vo[2][2];
     const uint32_t k_at = at + kg * (D / 2) + t * (D / 8), p_at = at + 2 * M::kRows + kg * 4;
@@ -152,7 +159,7 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
             uint32_t kp[1], vp[1];
             load_words<1>(kp, p_at + (16 * h + 8 * i) * 4);
             load_words<1>(vp, p_at + M::kPairs + (16 * h + 8 * i) * 4);
-            const float ks = pair_scale(kp[0]) * scale_log2, ko = fmaf(8.f, ks, pair_least(kp[0]) * scale_log2);
+            const float ks = pair_scale(kp[0]), ko = fmaf(8.f, ks, pair_least(kp[0]));
             vs[h][i] = pair_scale(vp[0]);
             if (kMasked && key > last) vs[h][i] = 0.f;                 // (no row sees it: its pair may be anything)
             vo[h][i] = fmaf(8.f, vs[h][i], pair_least(vp[0]));
@@ -253,12 +260,11 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
 }
 
 template <int D, int NT>
-__device__ __forceinline__ bool few_unit(const Kv4AttnParams& p, const int unit, uint8_t* smem, uint32_t& used) {
+__device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit, uint8_t* smem) {
     using M = FewSmem<D, NT>;
     constexpr int kSteps = D / 16;             // 16-wide pieces of a row
-    float (*s_o)[8 * NT][D + 4] = reinterpret_cast<float (*)[8 * NT][D + 4]>(smem + M::kOffO);
+    float (*s_o)[8 * NT][D + 4] = reinterpret_cast<float (*)[8 * NT][D + 4]>(smem);
     float2 (*s_ml)[8 * NT] = reinterpret_cast<float2 (*)[8 * NT]>(smem + M::kOffMl);
-    volatile uint32_t* abort_flag = reinterpret_cast<volatile uint32_t*>(smem + M::kOffAbort);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
     const char* plan = static_cast<const char*>(p.plan);
     const WppUnit un = reinterpret_cast<const WppUnit*>(plan + p.off_units)[unit];
@@ -269,7 +275,7 @@ __device__ __forceinline__ bool few_unit(const Kv4AttnParams& p, const int unit,
         // (the combine pass reads the parts of a refused request too: none of them has seen a key)
         if (un.split_slot >= 0 && threadIdx.x < un.rows[0] * un.rows[1])
             p.ws_lse[((int64_t)un.split_slot * 2 + un.row0[1]) * 128 + un.head[1] + threadIdx.x] = -INFINITY;
-        return true;
+        return;
     }
     const int toks = un.rows[0], rows = toks * un.rows[1], first_pos = P + un.row0[0];     // first_pos: last key that token 0 sees
     const int key_begin = un.kv_begin * WPP_TILE_N;
@@ -277,32 +283,47 @@ __device__ __forceinline__ bool few_unit(const Kv4AttnParams& p, const int unit,
     const int kvh = un.head[0] / p.group, page_shift = 31 - __clz(p.page_size), in_page = p.page_size - 1;
     const int32_t* table = p.block_tables + (int64_t)un.request * p.max_blocks;
 
-    // ---- the warp's keys: 32 at a time, every kFewWarps-th, in the warp's ring of stages (`used`: stages taken so far, by all units)
-    constexpr int kStride = kFewKeys * kFewWarps;
-    const uint32_t stages = smem_u32(smem) + warp * M::kDepth * M::kStage, bars = smem_u32(smem + M::kOffBars) + warp * M::kDepth * 8;
-    auto request = [&](int key, uint32_t stage) {
-        const int halves = min((seen - key + 15) / 16, 2);
-        const bool small = p.page_size == 16;                          // the second 16 keys have a page of their own then
-        if (lane == 0) mbar_arrive_expect_tx(bars + 8 * stage, halves * (M::kStage / 2));
-        __syncwarp();
-        const int h = lane >> 2, what = lane & 3;                      // K's rows, V's rows, K's pairs, V's pairs
-        if (h < (small ? halves : 1)) {
-            int page = table[(key + 16 * h) >> page_shift];
-            if (page < 0 || page >= p.num_pages) {
-                if (p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
-                page = 0;
-            }
-            const int keys = small ? 16 : 16 * halves, row = what < 2 ? D / 2 : 4;
-            const uint8_t* src = (what & 1 ? p.v_cache : p.k_cache) + page * p.page_bytes + kvh * p.head_bytes + (what < 2 ? 0 : p.page_size * (D / 2)) +
-                                 ((key + 16 * h) & in_page) * row;
-            const uint32_t dst = stages + stage * M::kStage + (what < 2 ? what * M::kRows : 2 * M::kRows + (what & 1) * M::kPairs) + 16 * h * row;
-            bulk_load(dst, src, keys * row, bars + 8 * stage);
+    // ---- the warp's keys: 32 at a time, every kFewWarps-th
+    constexpr int kStride = kFewKeys * kFewWarps, kRow = D / 2;
+    const uint32_t ring = smem_u32(smem) + warp * M::kDepth * M::kStage;
+    const uint8_t* const kc = p.k_cache + kvh * p.head_bytes;
+    const uint8_t* const vc = p.v_cache + kvh * p.head_bytes;
+    int bad = 0;
+    auto request16 = [&](int key, int keys, uint32_t dst, int at) {    // `keys` (16 or 32) keys of one page, `at` keys into the stage
+        int page = table[key >> page_shift];
+        if (page < 0 || page >= p.num_pages) {
+            bad = 1;
+            page = 0;
         }
+        const int64_t block = page * p.page_bytes;
+        const int slot = key & in_page;
+        const uint8_t* k = kc + block + slot * kRow + lane * 16;
+        const uint8_t* v = vc + block + slot * kRow + lane * 16;
+        const uint32_t to = dst + at * kRow + lane * 16;
+#pragma unroll
+        for (int i = 0; i < kFewKeys * kRow / 512; ++i)
+            if (i * 512 + lane * 16 < keys * kRow) {
+                copy_16(to + i * 512, k + i * 512);
+                copy_16(to + M::kRows + i * 512, v + i * 512);
+            }
+        const int l = lane & 7;                                        // lanes 0 to 7: K's pairs, 8 to 15: V's
+        if (lane < 16 && l * 4 < keys)
+            copy_16(dst + 2 * M::kRows + (lane >> 3) * M::kPairs + at * 4 + l * 16, (lane & 8 ? vc : kc) + block + p.page_size * kRow + slot * 4 + l * 16);
+    };
+    auto request = [&](int key, uint32_t dst) {
+        if (key < seen) {
+            if (p.page_size > 16) {
+                request16(key, min((seen - key + 15) & ~15, kFewKeys), dst, 0);
+            } else {
+                request16(key, 16, dst, 0);
+                if (key + 16 < seen) request16(key + 16, 16, dst, 16);
+            }
+        }
+        copies_commit();                                               // (an empty group where there is nothing: groups are counted)
     };
     int key = key_begin + warp * kFewKeys;
 #pragma unroll
-    for (int i = 0; i < M::kDepth; ++i)
-        if (key + i * kStride < seen) request(key + i * kStride, (used + i) % M::kDepth);
+    for (int i = 0; i < M::kDepth - 1; ++i) request(key + i * kStride, ring + i * M::kStage);
 
     // ---- Q as the first product's second factor: f16 numbers q 2^e, e so that the row's largest is in [2^7, 2^8) (what is less than
     //      2^-21 of that may be off by 2^-32 of it); and the sums of its rows
@@ -352,8 +373,8 @@ __device__ __forceinline__ bool few_unit(const Kv4AttnParams& p, const int unit,
         // of the columns this thread has of S^T: 2 t, 2 t + 1
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-            q_sum[nt][c] = __shfl_sync(0xffffffffu, sum, 8 * t + 4 * c);
-            q_scale[nt][c] = __shfl_sync(0xffffffffu, down, 8 * t + 4 * c);
+            q_sum[nt][c] = p.scale_log2 * __shfl_sync(0xffffffffu, sum, 8 * t + 4 * c);
+            q_scale[nt][c] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * t + 4 * c);
         }
     }
     FewState<D, NT> st;
@@ -372,18 +393,21 @@ __device__ __forceinline__ bool few_unit(const Kv4AttnParams& p, const int unit,
     st.v_ref = 8.67361738e-19f;        // 2^-60
     st.v_inv = 1.15292150e18f;
 
-    bool ok = true;
-    for (; key < seen; key += kStride, ++used) {
-        const uint32_t stage = used % M::kDepth, phase = used / M::kDepth & 1u, at = stages + stage * M::kStage;
-        ok = __all_sync(0xffffffffu, mbar_wait(bars + 8 * stage, phase, abort_flag));
-        if (!ok) break;
+    uint32_t at = 0, fill = (M::kDepth - 1) * M::kStage;               // offsets in the ring: of the keys, and of the next ones to be asked for
+    for (; key < seen; key += kStride) {
+        copies_wait<M::kDepth - 2>();
+        __syncwarp();                          // every lane's copies are here, and every lane has read the stage before
+        request(key + (M::kDepth - 1) * kStride, ring + fill);
+        fill = at;
         if (key + kFewKeys - 1 <= first_pos && key + kFewKeys <= seen)
-            few_step<D, NT, false>(st, at, qf, q_sum, q_scale, key, first_pos, toks, seen - 1, p.scale_log2, p.f16_1024, g, t);
+            few_step<D, NT, false>(st, ring + at, qf, q_sum, q_scale, key, first_pos, toks, seen - 1, p.f16_1024, g, t);
         else
-            few_step<D, NT, true>(st, at, qf, q_sum, q_scale, key, first_pos, toks, seen - 1, p.scale_log2, p.f16_1024, g, t);
-        __syncwarp();                          // (every lane has read the stage)
-        if (key + M::kDepth * kStride < seen) request(key + M::kDepth * kStride, stage);
+            few_step<D, NT, true>(st, ring + at, qf, q_sum, q_scale, key, first_pos, toks, seen - 1, p.f16_1024, g, t);
+        at = at == (M::kDepth - 1) * M::kStage ? 0u : at + M::kStage;
     }
+    if (bad && p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
+    copies_wait<0>();
+    __syncthreads();                           // the warps' results take the stages' place
 
     // ---- the warps' parts joined
 #pragma unroll
@@ -406,7 +430,6 @@ __device__ __forceinline__ bool few_unit(const Kv4AttnParams& p, const int unit,
             }
         }
     __syncthreads();
-    if (*abort_flag) return false;
     for (int i = threadIdx.x; i < rows * (D / 4); i += 32 * kFewWarps) {
         const int n = i / (D / 4), c = i % (D / 4) * 4;
         float mm = -INFINITY, sum = 0.f;
@@ -441,30 +464,18 @@ __device__ __forceinline__ bool few_unit(const Kv4AttnParams& p, const int unit,
             if (c == 0) p.ws_lse[row] = lse2;
         }
     }
-    return true;
 }
 
 template <int D, int NT>
 __global__ void __launch_bounds__(32 * kFewWarps, NT == 1 ? 4 : 3) wpp_kv4_few_kernel(const Kv4AttnParams p) {
-    using M = FewSmem<D, NT>;
     extern __shared__ __align__(128) uint8_t smem[];
-    if (threadIdx.x < kFewWarps * M::kDepth) mbar_init(smem_u32(smem + M::kOffBars) + 8 * threadIdx.x, 1);
-    if (threadIdx.x == 0) *reinterpret_cast<volatile uint32_t*>(smem + M::kOffAbort) = 0u;
-    fence_barrier_init();
-    __syncthreads();
     grid_launch_dependents();
     grid_dependency_wait();
     const int32_t* first = reinterpret_cast<const int32_t*>(static_cast<const char*>(p.plan) + p.off_few_ctas) + blockIdx.x;
     const int end = first[1];
-    uint32_t used = 0;                         // (per warp)
     for (int u = first[0]; u < end; ++u) {
-        if (!few_unit<D, NT>(p, u, smem, used)) break;
-        __syncthreads();                       // (the next unit's parts take the place of this one's)
-    }
-    if (*reinterpret_cast<volatile uint32_t*>(smem + M::kOffAbort)) {
-        const long long t0 = clock64();
-        while (clock64() - t0 < 400000) { }    // let copies in flight land
-        if (threadIdx.x == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_TIMEOUT);
+        few_unit<D, NT>(p, u, smem);
+        __syncthreads();                       // (the next unit's keys take the place of this one's results)
     }
 }
 

@@ -418,6 +418,7 @@ static int kv4_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppP
     p.off_units = hd->off_units;
     p.off_few_ctas = hd->off_few_ctas;
     p.f16_1024 = 0x64006400u;
+    p.f16_64 = 0x54005400u;
     p.scale_log2 = scale_log2_of(d);
     if (hd->num_few_units > 0) {
         const int e = wpp_launch_kv4_few(d.head_dim, &p, hd->num_few_ctas, hd->max_few_rows, cuda_stream);

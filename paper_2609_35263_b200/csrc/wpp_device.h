@@ -95,7 +95,7 @@ struct Kv4AttnParams {
     int32_t num_q_heads, group, page_size, max_blocks, num_pages;
     uint32_t off_q_offsets, off_prefix, off_units, off_few_ctas;
     float scale_log2;
-    uint32_t f16_1024;               // 1024 in both halves of a word (from here, and not a constant: see codes_low)
+    uint32_t f16_1024, f16_64;       // f16 1024 and 64 in both halves of a word (from here, and no constants: see codes_low)
 };
 
 struct CombineParams {

@@ -64,6 +64,9 @@ __device__ __forceinline__ uint32_t codes_high(uint32_t u, uint32_t k1024) {
     asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(r) : "r"(and_or(u, 0x00f000f0u, k1024)), "r"(0x2c002c00u), "r"(0xd480d480u));   // / 16 - 72
     return r;
 }
+// The same as 64 + code, for K: Q's product with the 64 is what the sums begin at, with the other sign.  (V's sums run over all keys:
+// there an offset of eight times the codes would stand above a result that averages out, and its roundings with it.)
+__device__ __forceinline__ uint32_t codes_high_64(uint32_t u, uint32_t k64) { return and_or(u, 0x00f000f0u, k64); }
 template <int kWords>
 __device__ __forceinline__ void load_words(uint32_t (&w)[kWords], uint32_t at) {
     if constexpr (kWords == 4) {
@@ -114,8 +117,8 @@ struct FewState {
 // rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9, columns [g D / 8, (g + 1) D / 8) of V; and the number pairs of rows g and g + 8.
 template <int D, int NT, bool kMasked>
 __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at, const uint32_t (&qf)[NT][D / 16][2],
-                                         const float (&q_sum)[NT][2], const float (&q_scale)[NT][2], int key0, int first_pos, int toks, int last,
-                                         uint32_t k1024, int g, int t) {
+                                         const float (&q_sum)[NT][2], const float (&q_scale)[NT][2], const float (&q_64)[NT][2], int key0, int first_pos, int toks, int last, bool first,
+                                         uint32_t k1024, uint32_t k64, int g, int t) {
     using M = FewSmem<D, NT>;
     const int kg = key_of_row(g), kt = key_of_row(2 * t);
     int limit[NT][2];                                                  // last key that the column's row sees
@@ -125,7 +128,7 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
 #pragma unroll
             for (int c = 0; c < 2; ++c) limit[nt][c] = first_pos + (8 * nt + 2 * t + c) % toks;
     }
-    // ---- S^T = (codes - 8) Q^T, then the scores in log2 units (q_scale and q_sum have the scale)
+    // ---- S^T = codes Q^T (q_64 makes up for codes less 8 and 64 + codes), then the scores in log2 units (q_scale and q_sum have the scale) above m
     float s[2][NT][4];
     float vs[2][2], vo[2][2];
     const uint32_t k_at = at + kg * (D / 2) + t * (D / 8), p_at = at + 2 * M::kRows + kg * 4;
@@ -137,13 +140,13 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) s[h][nt][i] = 0.f;
+            for (int i = 0; i < 4; ++i) s[h][nt][i] = q_64[nt][i & 1];
 #pragma unroll
         for (int w = 0; w < D / 32; ++w) {
             uint32_t wa = k[0][w], wb = k[1][w];
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const uint32_t a0 = codes_low(wa, k1024), a1 = codes_low(wb, k1024), a2 = codes_high(wa, k1024), a3 = codes_high(wb, k1024);
+                const uint32_t a0 = codes_low(wa, k1024), a1 = codes_low(wb, k1024), a2 = codes_high_64(wa, k64), a3 = codes_high_64(wb, k64);
                 wa >>= 8;
                 wb >>= 8;
 #pragma unroll
@@ -159,7 +162,7 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
             uint32_t kp[1], vp[1];
             load_words<1>(kp, p_at + (16 * h + 8 * i) * 4);
             load_words<1>(vp, p_at + M::kPairs + (16 * h + 8 * i) * 4);
-            const float ks = pair_scale(kp[0]), ko = fmaf(8.f, ks, pair_least(kp[0]));
+            const float ks = pair_scale(kp[0]), ko = pair_least(kp[0]);
             vs[h][i] = pair_scale(vp[0]);
             if (kMasked && key > last) vs[h][i] = 0.f;                 // (no row sees it: its pair may be anything)
             vo[h][i] = fmaf(8.f, vs[h][i], pair_least(vp[0]));
@@ -168,19 +171,19 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     float& y = s[h][nt][2 * i + c];
-                    y = fmaf(y, ks * q_scale[nt][c], ko * q_sum[nt][c]);
+                    y = fmaf(y, ks * q_scale[nt][c], fmaf(ko, q_sum[nt][c], -st.m[nt][c]));
                     if (kMasked && key > limit[nt][c]) y = -INFINITY;
                 }
         }
     // ---- references move only where a score or a scale is far above them
-    bool move = false;
+    bool move = first;
     float mx[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             mx[nt][c] = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
-            move |= mx[nt][c] > st.m[nt][c] + kFewSlack;
+            move |= mx[nt][c] > kFewSlack;
         }
     float v = fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[1][0], vs[1][1]));
     move |= v * st.v_inv > kFewScaleSlack;
@@ -198,11 +201,18 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
             for (int c = 0; c < 2; ++c) {
-                float y = fmaxf(st.m[nt][c], mx[nt][c]);
+                // how far the reference goes up; the first one may go down as well, and stays where the row sees nothing
+                float y = first ? mx[nt][c] : fmaxf(mx[nt][c], 0.f);
 #pragma unroll
                 for (int w = 4; w < 32; w *= 2) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, w));
-                const float a = st.m[nt][c] == -INFINITY ? 1.f : fast_exp2(st.m[nt][c] - y);        // (without a reference there is nothing to scale)
-                st.m[nt][c] = y;
+                if (kMasked && y == -INFINITY) y = 0.f;
+                const float a = first ? 1.f : fast_exp2(-y);
+                st.m[nt][c] += y;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    s[h][nt][c] -= y;
+                    s[h][nt][2 + c] -= y;
+                }
                 st.l[nt][c] *= a;
                 st.off[nt][c] *= a;
 #pragma unroll
@@ -225,8 +235,7 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
 #pragma unroll
                 for (int c = 0; c < 2; ++c) {
                     const bool out = kMasked && key0 + 16 * h + 8 * i + kg > limit[nt][c];
-                    const float ref = kMasked && st.m[nt][c] == -INFINITY ? 0.f : st.m[nt][c];
-                    e[c] = out ? 0.f : fast_exp2(s[h][nt][2 * i + c] - ref);
+                    e[c] = out ? 0.f : fast_exp2(s[h][nt][2 * i + c]);
                     st.l[nt][c] += e[c];
                     st.off[nt][c] = out ? st.off[nt][c] : fmaf(e[c], vo[h][i], st.off[nt][c]);
                 }
@@ -328,12 +337,12 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
     // ---- Q as the first product's second factor: f16 numbers q 2^e, e so that the row's largest is in [2^7, 2^8) (what is less than
     //      2^-21 of that may be off by 2^-32 of it); and the sums of its rows
     uint32_t qf[NT][D / 16][2];
-    float q_sum[NT][2], q_scale[NT][2];
+    float q_sum[NT][2], q_scale[NT][2], q_64[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
         const int n = 8 * nt + g;
         uint4 z[D / 32];
-        float sum = 0.f, top = 0.f;
+        float sum = 0.f, even = 0.f, top = 0.f;                  // even: of the elements whose codes are taken less 8
 #pragma unroll
         for (int w = 0; w < D / 32; ++w) {
             z[w] = make_uint4(0, 0, 0, 0);
@@ -346,12 +355,14 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
             for (int i = 0; i < 4; ++i) {
                 const float a = __uint_as_float(zz[i] << 16), b = __uint_as_float(zz[i] & 0xffff0000u);
                 sum += a + b;
+                even += a;
                 top = fmaxf(top, fmaxf(fabsf(a), fabsf(b)));
             }
         }
 #pragma unroll
         for (int w = 1; w < 4; w *= 2) {
             sum += __shfl_xor_sync(0xffffffffu, sum, w);
+            even += __shfl_xor_sync(0xffffffffu, even, w);
             top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
         }
         // 2^e and 2^-e, both normal numbers
@@ -374,6 +385,7 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             q_sum[nt][c] = p.scale_log2 * __shfl_sync(0xffffffffu, sum, 8 * t + 4 * c);
+            q_64[nt][c] = __shfl_sync(0xffffffffu, up * (8.f * even - 64.f * (sum - even)), 8 * t + 4 * c);
             q_scale[nt][c] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * t + 4 * c);
         }
     }
@@ -386,13 +398,14 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
             for (int i = 0; i < 4; ++i) st.o[nt][mt][i] = 0.f;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            st.m[nt][i] = -INFINITY;
+            st.m[nt][i] = 0.f;
             st.l[nt][i] = st.off[nt][i] = 0.f;
         }
     }
     st.v_ref = 8.67361738e-19f;        // 2^-60
     st.v_inv = 1.15292150e18f;
 
+    bool first = true;
     uint32_t at = 0, fill = (M::kDepth - 1) * M::kStage;               // offsets in the ring: of the keys, and of the next ones to be asked for
     for (; key < seen; key += kStride) {
         copies_wait<M::kDepth - 2>();
@@ -400,9 +413,10 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
         request(key + (M::kDepth - 1) * kStride, ring + fill);
         fill = at;
         if (key + kFewKeys - 1 <= first_pos && key + kFewKeys <= seen)
-            few_step<D, NT, false>(st, ring + at, qf, q_sum, q_scale, key, first_pos, toks, seen - 1, p.f16_1024, g, t);
+            few_step<D, NT, false>(st, ring + at, qf, q_sum, q_scale, q_64, key, first_pos, toks, seen - 1, first, p.f16_1024, p.f16_64, g, t);
         else
-            few_step<D, NT, true>(st, ring + at, qf, q_sum, q_scale, key, first_pos, toks, seen - 1, p.f16_1024, g, t);
+            few_step<D, NT, true>(st, ring + at, qf, q_sum, q_scale, q_64, key, first_pos, toks, seen - 1, first, p.f16_1024, p.f16_64, g, t);
+        first = false;
         at = at == (M::kDepth - 1) * M::kStage ? 0u : at + M::kStage;
     }
     if (bad && p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
@@ -421,7 +435,7 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
                 off += __shfl_xor_sync(0xffffffffu, off, w);
             }
             const int n = 8 * nt + 2 * t + c;
-            if (g == 0) s_ml[warp][n] = make_float2(st.m[nt][c], l);
+            if (g == 0) s_ml[warp][n] = make_float2(l == 0.f ? -INFINITY : st.m[nt][c], l);
 #pragma unroll
             for (int mt = 0; mt < kSteps; ++mt) {
                 const int d0 = g * (D / 8) + 2 * mt;       // element 8 w + 4 hw + 2 u of the thread's columns, mt = 4 w + 2 hw + u
@@ -441,7 +455,7 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
         for (int w = 0; w < kFewWarps; ++w) {
             const float2 ml = s_ml[w][n];
             if (ml.y == 0.f) continue;                     // saw no key of this row
-            const float a = ml.x == -INFINITY ? 1.f : fast_exp2(ml.x - ref);
+            const float a = fast_exp2(ml.x - ref);
             const float4 x = *reinterpret_cast<const float4*>(&s_o[w][n][c]);
             sum = fmaf(a, ml.y, sum);
             acc.x = fmaf(a, x.x, acc.x);

@@ -85,7 +85,7 @@ __device__ __forceinline__ void load_words(uint32_t (&w)[kWords], uint32_t at) {
 template <int D, int NT>
 struct FewSmem {
     static constexpr int kRows = kFewKeys * (D / 2), kPairs = kFewKeys * 4, kStage = 2 * kRows + 2 * kPairs;
-    static constexpr int kDepth = NT == 1 ? 3 : 4;
+    static constexpr int kDepth = NT == 1 ? 4 : 5;
     // in the stages' place, once a unit's are done with: float [warps][8 NT][D + 4], float2 [warps][8 NT]
     static constexpr int kOffMl = kFewWarps * 8 * NT * (D + 4) * 4;
     static constexpr int kBytes = kFewWarps * kDepth * kStage;
@@ -481,7 +481,7 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
 }
 
 template <int D, int NT>
-__global__ void __launch_bounds__(32 * kFewWarps, NT == 1 ? 4 : 3) wpp_kv4_few_kernel(const Kv4AttnParams p) {
+__global__ void __launch_bounds__(32 * kFewWarps, NT == 1 ? 3 : 2) wpp_kv4_few_kernel(const Kv4AttnParams p) {
     extern __shared__ __align__(128) uint8_t smem[];
     grid_launch_dependents();
     grid_dependency_wait();

@@ -11,7 +11,7 @@ static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // The kernel for few rows: CTAs that an SM holds, of blocks of at most 8 rows and of more; what a unit costs besides its key steps, in
 // steps; and the fewest steps that a block is cut for.
-constexpr int kFewCtas = 4, kFewCtasWide = 3;
+constexpr int kFewCtas = 3, kFewCtasWide = 2;
 constexpr int64_t kUnitSteps = 3, kLeastSteps = 2;
 
 // Row blocks of the kernel for few rows: heads of a KV group, and tokens, WPP_FEW_ROWS rows at most.

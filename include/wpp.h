@@ -472,6 +472,47 @@ int wpp_kda_chunk(const wpp_ctx* ctx, const wpp_kda_desc* desc, const void* q, c
  * num_requests, num_heads and total_tokens only); 0 for an invalid description. */
 size_t wpp_kda_workspace_bytes(const wpp_kda_desc* desc);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * Linear attention with a decay per head over a chunk: a recurrent-state layer without the delta rule, beside
+ * wpp_kda_chunk and with the same kind of state pool.  Per request and head, over the chunk's tokens,
+ *     S_t = exp(g_t) S_{t-1} + k_t v_t^T,      o_t = scale S_t^T q_t,
+ * with S (head_dim x head_dim, fp32) resumed from the state after exactly the reused prefix and written back at the
+ * chunk's end and, optionally, at sparse periodic boundaries.  g is the natural logarithm of the decay, one per head or one
+ * per token and head (a gate), -infinity among its values: it forgets everything before.  Values above 0 make the state
+ * grow and are not refused.  Heads are independent; no normalisation is applied. */
+typedef struct {
+    int32_t num_requests;   /* R >= 0 */
+    int32_t num_heads;      /* H >= 1 */
+    int32_t head_dim;       /* 64 or 128, of q, k and v */
+    int32_t num_slots;      /* slots of state_pool, each H * head_dim * head_dim floats */
+    int32_t snap_interval;  /* > 0: snapshot whenever the tokens folded into S reach a multiple of it; 0: none */
+    int32_t max_snaps;      /* row length of snap_slots (0 when snap_interval is 0) */
+    int32_t layout;         /* 0: the library chooses; 1: token by token */
+    float scale;            /* of the outputs; 0 selects 1 */
+    int64_t total_tokens;   /* T = row_offsets[R] */
+    int64_t q_token_stride, k_token_stride, v_token_stride, o_token_stride;     /* in elements, multiples of 8; 0: H * head_dim */
+    int64_t decay_token_stride;     /* in elements; 0: one decay per head */
+} wpp_linear_desc;
+
+/* The whole ragged batch on `cuda_stream`; request i owns rows [row_offsets[i], row_offsets[i+1]).
+ *   q, k, v, out : device bf16, head h of token t at t * stride + h * head_dim; 16-byte aligned.
+ *   log_decay    : device fp32 [H], or [T] rows of H decay_token_stride apart.
+ *   row_offsets, prefix_lens, state_pool, state_in, state_out, snap_slots, status_dev : as for wpp_kda_chunk (slots are
+ *                  H * head_dim * head_dim floats); no slot may be written for one request and read or written for another
+ *                  in the same call.
+ *   workspace    : device scratch, 256-byte aligned, wpp_linear_workspace_bytes(desc) bytes; may be NULL (0 bytes), which leaves
+ *                  the library fewer forms to choose from.  Calls that may overlap on the GPU need one each.
+ * A request with an empty chunk copies state_in to state_out.  Returns WPP_ERR_INVALID_ARG for null or misaligned pointers, sizes
+ * < 0 or strides that are too short, WPP_ERR_UNSUPPORTED for another head_dim, WPP_ERR_CUDA for a launch failure. */
+int wpp_linear_chunk(const wpp_ctx* ctx, const wpp_linear_desc* desc, const void* q, const void* k, const void* v,
+                     const float* log_decay, const int64_t* row_offsets, const int32_t* prefix_lens, float* state_pool,
+                     const int32_t* state_in, const int32_t* state_out, const int32_t* snap_slots, void* out, void* workspace,
+                     size_t workspace_bytes, int32_t* status_dev, void* cuda_stream);
+
+/* Bytes of workspace wpp_linear_chunk uses for a wave of this description (depends on num_requests, num_heads, head_dim and
+ * total_tokens only); 0 for an invalid description. */
+size_t wpp_linear_workspace_bytes(const wpp_linear_desc* desc);
+
 #ifdef __cplusplus
 }
 #endif

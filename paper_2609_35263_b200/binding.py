@@ -82,6 +82,14 @@ class KdaDesc(ctypes.Structure):
                 ("max_snaps", ctypes.c_int32), ("layout", ctypes.c_int32), ("total_tokens", ctypes.c_int64)]
 
 
+class LinearDesc(ctypes.Structure):
+    _fields_ = [("num_requests", ctypes.c_int32), ("num_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("num_slots", ctypes.c_int32), ("snap_interval", ctypes.c_int32), ("max_snaps", ctypes.c_int32),
+                ("layout", ctypes.c_int32), ("scale", ctypes.c_float), ("total_tokens", ctypes.c_int64),
+                ("q_token_stride", ctypes.c_int64), ("k_token_stride", ctypes.c_int64), ("v_token_stride", ctypes.c_int64),
+                ("o_token_stride", ctypes.c_int64), ("decay_token_stride", ctypes.c_int64)]
+
+
 WAVE_RING_BUSY, WAVE_ADMISSION_PENDING, WAVE_ALREADY_DEFERRED = 1, 2, 4
 
 EXPORTS = ["wpp_create", "wpp_destroy", "wpp_status_string", "wpp_last_cuda_error", "wpp_plan_bytes",
@@ -91,7 +99,8 @@ EXPORTS = ["wpp_create", "wpp_destroy", "wpp_status_string", "wpp_last_cuda_erro
            "wpp_selftest_bounded_wait", "wpp_wave_ladder", "wpp_plan_waves",
            "wpp_hash_blocks", "wpp_hash_blocks_host", "wpp_hint_index_create", "wpp_hint_index_destroy",
            "wpp_hint_index_add", "wpp_hint_index_remove", "wpp_hint_index_size", "wpp_hint_probe",
-           "wpp_hint_probe_recurrent", "wpp_kda_chunk", "wpp_kda_workspace_bytes"]
+           "wpp_hint_probe_recurrent", "wpp_kda_chunk", "wpp_kda_workspace_bytes",
+           "wpp_linear_chunk", "wpp_linear_workspace_bytes"]
 
 _lib = None
 _call = None          # the calls of every layer, marshalled in C (csrc/wpp_call.c)
@@ -151,14 +160,17 @@ def load_library() -> ctypes.CDLL:
         lib.wpp_kda_chunk.argtypes = [vp, ctypes.POINTER(KdaDesc)] + [vp] * 13 + [ctypes.c_size_t, vp, vp]
         lib.wpp_kda_workspace_bytes.restype = ctypes.c_size_t
         lib.wpp_kda_workspace_bytes.argtypes = [ctypes.POINTER(KdaDesc)]
+        lib.wpp_linear_chunk.argtypes = [vp, ctypes.POINTER(LinearDesc)] + [vp] * 12 + [ctypes.c_size_t, vp, vp]
+        lib.wpp_linear_workspace_bytes.restype = ctypes.c_size_t
+        lib.wpp_linear_workspace_bytes.argtypes = [ctypes.POINTER(LinearDesc)]
         try:
             from . import _wpp_call as call
         except ImportError as e:
             raise ImportError(f"the module _wpp_call is missing in {_HERE} (it belongs to one Python version and is needed for a "
                               "library named by WPP_LIB_PATH too): run `python -m paper_2609_35263_b200.build` "
                               "(there is no fallback path)") from e
-        call.init(*(ctypes.cast(f, vp).value for f in (lib.wpp_kv_append, lib.wpp_prefill_attention_varlen, lib.wpp_kda_chunk)),
-                  BatchDesc, KdaDesc)
+        call.init(*(ctypes.cast(f, vp).value for f in (lib.wpp_kv_append, lib.wpp_prefill_attention_varlen, lib.wpp_kda_chunk,
+                                                       lib.wpp_linear_chunk)), BatchDesc, KdaDesc, LinearDesc)
         _call, _lib = call, lib
     return _lib
 
@@ -499,4 +511,49 @@ def wpp_kda_chunk(ctx: Context, q, k, v, alpha, beta, row_offsets, state_pool, s
                          snap_slots, out, workspace, ws_bytes, status, _stream(ctx, stream))
     if st:
         _check(st, "wpp_kda_chunk")
+    return out
+
+
+def wpp_linear_workspace_bytes(num_requests: int, num_heads: int, head_dim: int, total_tokens: int) -> int:
+    """Bytes of workspace wpp_linear_chunk uses for such a wave."""
+    desc = LinearDesc(int(num_requests), int(num_heads), int(head_dim), total_tokens=int(total_tokens))
+    return int(load_library().wpp_linear_workspace_bytes(ctypes.byref(desc)))
+
+
+def _token_stride(x, where: str) -> int:
+    """Elements from a token to the next of x [T, H, d], whose heads have to lie side by side."""
+    if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
+        raise WppError(1, where)
+    return int(x.stride(0)) if x.shape[0] > 1 else int(x.shape[1] * x.shape[2])
+
+
+def wpp_linear_chunk(ctx: Context, q, k, v, log_decay, row_offsets, state_pool, state_in, state_out, out=None,
+                     prefix_lens=None, snap_interval: int = 0, snap_slots=None, status=None, stream=None, layout: int = 0,
+                     workspace=None, scale: float = 1.0):
+    """Queue the linear-attention layer of one wave on `stream`: S_t = exp(g_t) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t.
+
+    q, k, v: cuda bf16 [T, H, d], d 64 or 128 (views of a packed buffer will do: heads side by side, tokens any stride apart);
+    log_decay: cuda fp32 [H], or [T, H] for a decay per token; row_offsets: cuda int64 [R+1]; state_pool: cuda fp32
+    [slots, H, d, d] (updated in place); state_in, state_out: cuda int32 [R] (-1: zero state / do not store); snap_slots: cuda
+    int32 [R, max_snaps] with prefix_lens (cuda int32 [R]) and snap_interval > 0 for periodic snapshots; workspace: cuda
+    uint8, wpp_linear_workspace_bytes bytes, 256-byte aligned.  Returns the cuda bf16 output."""
+    T, H, d = (int(x) for x in q.shape)
+    R = int(row_offsets.numel()) - 1
+    if out is None:
+        out = torch.empty((T, H, d), dtype=torch.bfloat16, device=q.device)
+    for x in (k, v, out):
+        if tuple(x.shape) != (T, H, d):
+            raise WppError(1, "wpp_linear_chunk")
+    per_token = log_decay.dim() == 2
+    if tuple(log_decay.shape) != ((T, H) if per_token else (H,)) or (H > 1 and log_decay.stride(-1) != 1):
+        raise WppError(1, "wpp_linear_chunk")
+    decay_stride = 0 if not per_token else int(log_decay.stride(0)) if T > 1 else H
+    strides = [_token_stride(x, "wpp_linear_chunk") for x in (q, k, v, out)]
+    max_snaps = 0 if snap_slots is None else int(snap_slots.shape[1])
+    desc = LinearDesc(R, H, d, int(state_pool.shape[0]), int(snap_interval), max_snaps, int(layout), float(scale), T, *strides, decay_stride)
+    ws_bytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
+    st = _call.linear_chunk(ctx.handle.value, desc, q, k, v, log_decay, row_offsets, prefix_lens, state_pool, state_in, state_out,
+                            snap_slots, out, workspace, ws_bytes, status, _stream(ctx, stream))
+    if st:
+        _check(st, "wpp_linear_chunk")
     return out

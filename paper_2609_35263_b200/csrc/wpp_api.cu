@@ -992,3 +992,66 @@ extern "C" int wpp_kda_chunk(const wpp_ctx* ctx, const wpp_kda_desc* desc, const
     }
     return WPP_OK;
 }
+
+// ---------------------------------------------------------------------------------------------------------------
+// Linear attention with a decay per head.
+static bool linear_desc_ok(const wpp_linear_desc* d) {
+    return d && d->num_requests >= 0 && d->num_heads >= 1 && d->num_slots >= 0 && d->snap_interval >= 0 && d->max_snaps >= 0 &&
+           d->total_tokens >= 0 && d->layout >= 0 && d->layout <= 1 && d->q_token_stride >= 0 && d->k_token_stride >= 0 &&
+           d->v_token_stride >= 0 && d->o_token_stride >= 0 && d->decay_token_stride >= 0;
+}
+
+extern "C" size_t wpp_linear_workspace_bytes(const wpp_linear_desc* desc) {
+    if (!linear_desc_ok(desc) || (desc->head_dim != 64 && desc->head_dim != 128)) return 0;
+    return 256;
+}
+
+extern "C" int wpp_linear_chunk(const wpp_ctx* ctx, const wpp_linear_desc* desc, const void* q, const void* k, const void* v,
+                                const float* log_decay, const int64_t* row_offsets, const int32_t* prefix_lens, float* state_pool,
+                                const int32_t* state_in, const int32_t* state_out, const int32_t* snap_slots, void* out,
+                                void* workspace, size_t workspace_bytes, int32_t* status_dev, void* cuda_stream) {
+    if (!ctx || !linear_desc_ok(desc)) return WPP_ERR_INVALID_ARG;
+    if (desc->head_dim != 64 && desc->head_dim != 128) return WPP_ERR_UNSUPPORTED;
+    if (desc->num_requests > 65535 || desc->num_heads > 65535) return WPP_ERR_UNSUPPORTED;      // (grid dimensions)
+    if (!(fabsf(desc->scale) <= 3.402823466e+38f)) return WPP_ERR_INVALID_ARG;
+    if (desc->num_requests == 0) return WPP_OK;
+    if (int rc = wpp_ctx_check_device(ctx)) return rc;
+    if (!row_offsets || !state_in || !state_out) return WPP_ERR_INVALID_ARG;
+    if (desc->num_slots > 0 && !state_pool) return WPP_ERR_INVALID_ARG;
+    if (desc->total_tokens > 0 && (!q || !k || !v || !log_decay || !out)) return WPP_ERR_INVALID_ARG;
+    if (desc->snap_interval > 0 && !prefix_lens) return WPP_ERR_INVALID_ARG;
+    if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(state_pool)) return WPP_ERR_INVALID_ARG;
+    const int64_t row = (int64_t)desc->num_heads * desc->head_dim;
+    wpp::LinearParams p;
+    memset(&p, 0, sizeof(p));
+    p.q = static_cast<const __nv_bfloat16*>(q);
+    p.k = static_cast<const __nv_bfloat16*>(k);
+    p.v = static_cast<const __nv_bfloat16*>(v);
+    p.log_decay = log_decay;
+    p.row_offsets = row_offsets;
+    p.prefix_lens = prefix_lens;
+    p.state_pool = state_pool;
+    p.state_in = state_in;
+    p.state_out = state_out;
+    p.snap_slots = desc->max_snaps > 0 ? snap_slots : nullptr;
+    p.out = static_cast<__nv_bfloat16*>(out);
+    p.status = status_dev;
+    p.q_token_stride = desc->q_token_stride ? desc->q_token_stride : row;
+    p.k_token_stride = desc->k_token_stride ? desc->k_token_stride : row;
+    p.v_token_stride = desc->v_token_stride ? desc->v_token_stride : row;
+    p.o_token_stride = desc->o_token_stride ? desc->o_token_stride : row;
+    p.decay_token_stride = desc->decay_token_stride;
+    for (int64_t stride : {p.q_token_stride, p.k_token_stride, p.v_token_stride, p.o_token_stride})
+        if (stride < row || stride % 8 != 0) return WPP_ERR_INVALID_ARG;
+    if (p.decay_token_stride && p.decay_token_stride < desc->num_heads) return WPP_ERR_INVALID_ARG;
+    p.num_requests = desc->num_requests;
+    p.num_heads = desc->num_heads;
+    p.num_slots = desc->num_slots;
+    p.snap_interval = desc->snap_interval;
+    p.max_snaps = desc->max_snaps;
+    p.scale = desc->scale != 0.f ? desc->scale : 1.f;
+    const int e = wpp_launch_linear_token(&p, desc->head_dim, ctx->sm_count, cuda_stream);
+    if (e != 0) return cuda_fail(ctx, e);
+    const_cast<wpp_ctx*>(ctx)->launches += 1;
+    return WPP_OK;
+}

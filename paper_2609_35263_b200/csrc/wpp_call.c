@@ -16,7 +16,9 @@ static int (*p_attention)(const wpp_ctx*, const wpp_batch_desc*, const void*, vo
 static int (*p_kda)(const wpp_ctx*, const wpp_kda_desc*, const void*, const void*, const void*, const float*, const float*,
                     const int64_t*, const int32_t*, float*, const int32_t*, const int32_t*, const int32_t*, void*, void*, size_t,
                     int32_t*, void*);
-static PyObject *s_data_ptr, *t_batch, *t_kda;         /* the method's name; the binding's BatchDesc and KdaDesc */
+static int (*p_linear)(const wpp_ctx*, const wpp_linear_desc*, const void*, const void*, const void*, const float*, const int64_t*,
+                       const int32_t*, float*, const int32_t*, const int32_t*, const int32_t*, void*, void*, size_t, int32_t*, void*);
+static PyObject *s_data_ptr, *t_batch, *t_kda, *t_linear;      /* the method's name; the binding's BatchDesc, KdaDesc and LinearDesc */
 
 /* Each of these returns 0, or -1 with an exception set. */
 static int integer(PyObject* o, void** out) {           /* a context, a stream, a function: None is null */
@@ -108,20 +110,38 @@ static PyObject* kda_chunk(PyObject* self, PyObject* const* args, Py_ssize_t n) 
     return PyLong_FromLong(st);
 }
 
-/* init(append, attention, kda, BatchDesc, KdaDesc): the functions' addresses in the loaded library, the descriptions' types */
+/* linear_chunk(ctx, desc, q, k, v, decay, rows, prefix, pool, state_in, state_out, snaps, out, workspace, bytes, status, stream) */
+static PyObject* linear_chunk(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    (void)self;
+    void *ctx, *a[12], *b[2];
+    wpp_linear_desc d;
+    if (count(n, 17) || integer(args[0], &ctx) || description(args[1], t_linear, &d, sizeof(d)) || memories(args + 2, 12, a)) return NULL;
+    const size_t bytes = PyLong_AsSize_t(args[14]);
+    if ((bytes == (size_t)-1 && PyErr_Occurred()) || memories(args + 15, 1, b) || integer(args[16], &b[1])) return NULL;
+    int st;
+    Py_BEGIN_ALLOW_THREADS
+    st = p_linear(ctx, &d, a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], a[11], bytes, b[0], b[1]);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(st);
+}
+
+/* init(append, attention, kda, linear, BatchDesc, KdaDesc, LinearDesc): the functions' addresses in the loaded library, the
+ * descriptions' types */
 static PyObject* init(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     (void)self;
-    void* a[3];
-    if (count(n, 5) || integer(args[0], &a[0]) || integer(args[1], &a[1]) || integer(args[2], &a[2])) return NULL;
-    if (!PyType_Check(args[3]) || !PyType_Check(args[4])) {
+    void* a[4];
+    if (count(n, 7) || integer(args[0], &a[0]) || integer(args[1], &a[1]) || integer(args[2], &a[2]) || integer(args[3], &a[3])) return NULL;
+    if (!PyType_Check(args[4]) || !PyType_Check(args[5]) || !PyType_Check(args[6])) {
         PyErr_SetString(PyExc_TypeError, "the descriptions' types");
         return NULL;
     }
     memcpy(&p_append, &a[0], sizeof(void*));
     memcpy(&p_attention, &a[1], sizeof(void*));
     memcpy(&p_kda, &a[2], sizeof(void*));
-    Py_XSETREF(t_batch, Py_NewRef(args[3]));
-    Py_XSETREF(t_kda, Py_NewRef(args[4]));
+    memcpy(&p_linear, &a[3], sizeof(void*));
+    Py_XSETREF(t_batch, Py_NewRef(args[4]));
+    Py_XSETREF(t_kda, Py_NewRef(args[5]));
+    Py_XSETREF(t_linear, Py_NewRef(args[6]));
     Py_RETURN_NONE;
 }
 
@@ -130,6 +150,7 @@ static PyMethodDef methods[] = {
     {"kv_append", (PyCFunction)(void (*)(void))kv_append, METH_FASTCALL, NULL},
     {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, NULL},
     {"kda_chunk", (PyCFunction)(void (*)(void))kda_chunk, METH_FASTCALL, NULL},
+    {"linear_chunk", (PyCFunction)(void (*)(void))linear_chunk, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_wpp_call", NULL, -1, methods, NULL, NULL, NULL, NULL};

@@ -127,6 +127,24 @@ struct KdaParams {
     int32_t num_requests, num_heads, num_slots, snap_interval, max_snaps;
 };
 
+struct LinearParams {
+    const __nv_bfloat16* q;
+    const __nv_bfloat16* k;
+    const __nv_bfloat16* v;
+    const float* log_decay;
+    const int64_t* row_offsets;
+    const int32_t* prefix_lens;
+    float* state_pool;
+    const int32_t* state_in;
+    const int32_t* state_out;
+    const int32_t* snap_slots;
+    __nv_bfloat16* out;
+    int32_t* status;
+    int64_t q_token_stride, k_token_stride, v_token_stride, o_token_stride, decay_token_stride;      // in elements
+    int32_t num_requests, num_heads, num_slots, snap_interval, max_snaps;
+    float scale;
+};
+
 // Chunk-parallel (tensor-core) form of the recurrent layer: the inputs of KdaParams plus the workspace arrays the
 // preparation kernel fills for the chain kernel.  bh = (global block index) * num_heads + head.
 struct KdaGroupParams : KdaParams {
@@ -182,5 +200,6 @@ int wpp_launch_combine(const wpp::CombineParams* p, int num_combine, void* strea
 // maps: q, k, v, alpha; form: 1, 2, 3 = CTAs of 128, 64, 32 columns of the state
 int wpp_launch_kda_group(const wpp::KdaGroupParams* p, const CUtensorMap* maps, int form, void* stream);
 int wpp_launch_kda(const wpp::KdaParams* p, int num_sms, int layout, void* stream);
+int wpp_launch_linear_token(const wpp::LinearParams* p, int head_dim, int num_sms, void* stream);
 int wpp_launch_selftest_wait(long long limit_cycles, int32_t* status, long long* waited_cycles, void* stream);
 }

@@ -1,0 +1,175 @@
+"""Linear attention with a decay per head on the GPU against 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_35263_b200 as wpp
+from tests.linear_harness import Wave, ctx
+
+pytestmark = pytest.mark.gpu
+LAYOUTS = (0, 1)
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("chunks,H", [([1], 1), ([1] * 5, 3), ([0, 1, 0], 2), ([2, 15, 16, 17], 2), ([63, 64, 65], 2), ([128, 0, 129, 1], 3), ([300, 40], 2),
+                                      ([1000], 1)])
+@pytest.mark.parametrize("per_token", [False, True])
+def test_chunks(layout, d, chunks, H, per_token):
+    w = Wave(chunks, H, d, seed=sum(chunks) + d, per_token=per_token)
+    g = w.device()
+    out = w.run(g, layout)
+    assert int(g["status"].item()) == 0
+    w.check(out, g["pool"], w.reference())
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("chunks,prefix,interval", [([200, 70], [0, 33], 64), ([130], [5], 1), ([257, 1, 64], [100, 63, 64], 50), ([40], [7], 1000),
+                                                    ([600], [64], 128)])
+def test_snapshots(layout, chunks, prefix, interval):
+    w = Wave(chunks, 2, 64, seed=3, prefix=prefix, interval=interval, scale=0.25)
+    g = w.device()
+    out = w.run(g, layout)
+    w.check(out, g["pool"], w.reference())
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_the_zero_state_and_slots_that_are_not_stored(layout, d):
+    w = Wave([100, 3], 2, d, seed=4, resume=False)
+    w.state_out[1] = -1
+    g = w.device()
+    out = w.run(g, layout)
+    w.check(out, g["pool"], w.reference())
+    assert torch.equal(g["pool"][:2].cpu(), w.pool[:2]) and torch.equal(g["pool"][3].cpu(), w.pool[3])
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_a_state_in_place(layout):
+    w = Wave([150, 1], 3, 64, seed=5)
+    w.state_out = w.state_in.copy()
+    g = w.device()
+    out = w.run(g, layout)
+    w.check(out, g["pool"], w.reference())
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_decays_from_none_to_all(layout):
+    """No decay at all, decays that leave nothing after a few tokens, and ones that forget at once."""
+    rng = np.random.default_rng(6)
+    decay = -np.exp(rng.uniform(-12, 4, (400, 4)))
+    decay[:, 0] = 0.0
+    decay[:, 1] = -30.0
+    decay[rng.random((400, 4)) < 0.05] = -np.inf
+    decay[rng.random((400, 4)) < 0.02] = -3e38
+    decay[100:300, 2] = 0.0
+    w = Wave([270, 130], 4, 64, seed=7, decay=decay)
+    g = w.device()
+    out = w.run(g, layout)
+    w.check(out, g["pool"], w.reference())
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_views_of_packed_buffers(layout):
+    w = Wave([70, 9], 3, 64, seed=8)
+    g = w.device()
+    packed = torch.randn(w.T, 3 * 3 * 64 + 64, device="cuda").bfloat16()
+    views = [packed[:, i * 192:(i + 1) * 192].unflatten(1, (3, 64)) for i in range(3)]
+    for x, n in zip(views, "qkv"):
+        x.copy_(g[n])
+        g[n] = x
+    gates = torch.full((w.T, 8), 7.0, device="cuda")
+    gates[:, 2:5] = g["decay"]
+    g["decay"] = gates[:, 2:5]
+    wide = torch.full((w.T, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    out = w.run(g, layout, out=wide[:, :3])
+    w.check(out, g["pool"], w.reference())
+    assert bool((wide[:, 3] == 3.0).all())
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+def test_cut_chunks_end_where_whole_ones_do(layout):
+    """A prompt in three waves, each resumed from the one before, and in one."""
+    w = Wave([500], 2, 128, seed=9)
+    g = w.device()
+    ref = w.reference()
+    pool, at = g["pool"].clone(), 0
+    outs = []
+    for n in (130, 1, 369):
+        part = dict(g, pool=pool, rows=torch.tensor([0, n], device="cuda"), state_in=torch.tensor([1 if at else 0], dtype=torch.int32, device="cuda"))
+        for x in ("q", "k", "v", "decay"):
+            part[x] = g[x][at:at + n]
+        outs.append(w.run(part, layout, out=torch.empty_like(part["q"])))
+        at += n
+    w.check(torch.cat(outs), pool, ref)
+
+
+def test_bad_slots_are_reported():
+    for layout in LAYOUTS:
+        w = Wave([80, 5], 2, 64, seed=10, interval=64)
+        ref = w.reference()
+        for name in ("state_in", "state_out", "snaps"):
+            for bad in (-2, int(w.pool.shape[0]), 2 ** 31 - 1):
+                g = w.device()
+                g[name].view(-1)[0] = bad
+                pool = g["pool"].clone()
+                out = w.run(g, layout)
+                assert int(g["status"].item()) == 3
+                # the other request is not touched
+                assert np.allclose(out[80:].double().cpu().numpy(), ref[0][80:], atol=2.0 ** -8 * float(ref[1].max()))
+                assert torch.equal(g["pool"][:2], pool[:2])
+
+
+def test_refusals_before_a_launch():
+    w = Wave([20], 2, 64, seed=11, interval=16)
+    g, n = w.device(), ctx().launch_count()
+    for change in (dict(prefix=None), dict(pool=g["pool"].view(-1)[1:-127].view(-1, 2, 64, 1)), dict(q=None)):
+        with pytest.raises((wpp.WppError, AttributeError, TypeError)):
+            w.run(dict(g, **change))
+    with pytest.raises(wpp.WppError):
+        w.run(g, layout=3)
+    with pytest.raises(wpp.WppError):
+        w.run(g, out=torch.empty(20 * 128 + 8, dtype=torch.bfloat16, device="cuda")[4:-4].view(20, 2, 64))
+    assert ctx().launch_count() == n
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("chunks", [[1, 1, 1], [200, 64]])
+def test_captured_and_replayed_and_on_two_streams(layout, chunks):
+    w = Wave(chunks, 3, 128, seed=12)
+    g = w.device()
+    ref = w.reference()
+    pools = [g["pool"].clone() for _ in range(2)]
+    spaces = [w.workspace() for _ in range(2)]
+    outs = [torch.empty_like(g["q"]) for _ in range(2)]
+    torch.cuda.synchronize()
+    for s, x, ws, o in zip([torch.cuda.Stream() for _ in range(2)], pools, spaces, outs):
+        w.run(dict(g, pool=x), layout, out=o, workspace=ws, stream=s)
+    torch.cuda.synchronize()
+    w.check(outs[0], pools[0], ref)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(*pools)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        w.run(g, layout, out=outs[0], workspace=spaces[0])
+    for _ in range(3):
+        outs[0].zero_()
+        graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(outs[0], outs[1]) and torch.equal(g["pool"], pools[1])
+    assert int(g["status"].item()) == 0
+
+
+def test_beside_the_attention_of_the_same_wave():
+    """A hybrid stage's two layers of one wave: append and attention over a cache held in 4 bits, and the linear layer."""
+    from tests.kv4_harness import Wave as CacheWave
+    from oracle import kv4 as okv4
+    a = CacheWave([40, 100], [90, 1], 8, 2, 64, 32, seed=13)
+    w = Wave([90, 1], 4, 64, seed=14, prefix=[40, 100])
+    ga, g = a.device(), w.device()
+    plan = a.plan()
+    a.append(ga, plan)
+    out, lse = a.attend(ga, plan)
+    o = w.run(g)
+    a.k_pool, a.v_pool = okv4.append(a.k_new, a.v_new, a.k_pool, a.v_pool, a.table, a.P, a.C, a.B)
+    a.check(out, lse, a.reference())
+    w.check(o, g["pool"], w.reference())

@@ -997,13 +997,39 @@ extern "C" int wpp_kda_chunk(const wpp_ctx* ctx, const wpp_kda_desc* desc, const
 // Linear attention with a decay per head.
 static bool linear_desc_ok(const wpp_linear_desc* d) {
     return d && d->num_requests >= 0 && d->num_heads >= 1 && d->num_slots >= 0 && d->snap_interval >= 0 && d->max_snaps >= 0 &&
-           d->total_tokens >= 0 && d->layout >= 0 && d->layout <= 1 && d->q_token_stride >= 0 && d->k_token_stride >= 0 &&
+           d->total_tokens >= 0 && d->layout >= 0 && d->layout <= 2 && d->q_token_stride >= 0 && d->k_token_stride >= 0 &&
            d->v_token_stride >= 0 && d->o_token_stride >= 0 && d->decay_token_stride >= 0;
+}
+
+// Segments of the chains for the form in blocks.  Chains fill the SMs with two CTAs each, or are cut until they do; a segment has
+// kLinLeast tokens at least, since the first pass costs about half of what the second does.
+constexpr int64_t kLinTokenForm = 8;       // tokens per request on average from which blocks are taken
+constexpr int64_t kLinLeast = 256, kLinBlockTokens = 64;
+struct LinearSegments {
+    int64_t tokens, count;          // of a segment; of all chains of a head, at most
+    bool two_passes;
+    size_t off_log, bytes;          // of the workspace: states, logarithms of decays
+};
+static LinearSegments linear_segments(const wpp_linear_desc* d, int sms) {
+    LinearSegments g;
+    const int64_t chains = (int64_t)d->num_requests * d->num_heads, T = d->total_tokens, most = chains > 0 ? 2 * (int64_t)sms / chains : 1;
+    const int64_t mean = d->num_requests > 0 ? (T + d->num_requests - 1) / d->num_requests : 0;
+    g.two_passes = most >= 2 && mean >= 2 * kLinLeast;
+    g.tokens = (int64_t)1 << 40;
+    if (g.two_passes) {
+        const int64_t len = (mean + most - 1) / most;
+        g.tokens = (len > kLinLeast ? len + kLinBlockTokens - 1 : kLinLeast) / kLinBlockTokens * kLinBlockTokens;
+    }
+    g.count = T / g.tokens + d->num_requests;
+    g.off_log = (size_t)g.count * d->num_heads * d->head_dim * d->head_dim * sizeof(float);
+    g.bytes = g.off_log + (size_t)g.count * d->num_heads * sizeof(float);
+    return g;
 }
 
 extern "C" size_t wpp_linear_workspace_bytes(const wpp_linear_desc* desc) {
     if (!linear_desc_ok(desc) || (desc->head_dim != 64 && desc->head_dim != 128)) return 0;
-    return 256;
+    const LinearSegments g = linear_segments(desc, 148);
+    return g.two_passes ? g.bytes : 256;
 }
 
 extern "C" int wpp_linear_chunk(const wpp_ctx* ctx, const wpp_linear_desc* desc, const void* q, const void* k, const void* v,
@@ -1022,7 +1048,7 @@ extern "C" int wpp_linear_chunk(const wpp_ctx* ctx, const wpp_linear_desc* desc,
     if (desc->snap_interval > 0 && !prefix_lens) return WPP_ERR_INVALID_ARG;
     if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out) || !aligned16(state_pool)) return WPP_ERR_INVALID_ARG;
     const int64_t row = (int64_t)desc->num_heads * desc->head_dim;
-    wpp::LinearParams p;
+    wpp::LinearChunkParams p;
     memset(&p, 0, sizeof(p));
     p.q = static_cast<const __nv_bfloat16*>(q);
     p.k = static_cast<const __nv_bfloat16*>(k);
@@ -1050,8 +1076,28 @@ extern "C" int wpp_linear_chunk(const wpp_ctx* ctx, const wpp_linear_desc* desc,
     p.snap_interval = desc->snap_interval;
     p.max_snaps = desc->max_snaps;
     p.scale = desc->scale != 0.f ? desc->scale : 1.f;
-    const int e = wpp_launch_linear_token(&p, desc->head_dim, ctx->sm_count, cuda_stream);
+    // token by token where chunks are so short that a block would be mostly empty
+    if (desc->layout == 1 || (desc->layout == 0 && desc->total_tokens < kLinTokenForm * (int64_t)desc->num_requests)) {
+        const int e = wpp_launch_linear_token(&p, desc->head_dim, ctx->sm_count, cuda_stream);
+        if (e != 0) return cuda_fail(ctx, e);
+        const_cast<wpp_ctx*>(ctx)->launches += 1;
+        return WPP_OK;
+    }
+    LinearSegments g = linear_segments(desc, 148);
+    if (g.two_passes) {
+        if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return WPP_ERR_INVALID_ARG;
+        if (!workspace || workspace_bytes < g.bytes) {                 // whole chains need none
+            g.two_passes = false;
+            g.tokens = (int64_t)1 << 40;
+            g.count = desc->num_requests;
+        }
+    }
+    if (g.count > 0x7fffffff) return WPP_ERR_UNSUPPORTED;
+    p.seg_tokens = g.tokens;
+    p.ws_state = static_cast<float*>(workspace);
+    p.ws_log = reinterpret_cast<float*>(static_cast<char*>(workspace) + g.off_log);
+    const int e = wpp_launch_linear_chunk(&p, desc->head_dim, g.count, g.two_passes, cuda_stream);
     if (e != 0) return cuda_fail(ctx, e);
-    const_cast<wpp_ctx*>(ctx)->launches += 1;
+    const_cast<wpp_ctx*>(ctx)->launches += g.two_passes ? 2 : 1;
     return WPP_OK;
 }

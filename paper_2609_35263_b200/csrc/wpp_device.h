@@ -145,6 +145,12 @@ struct LinearParams {
     float scale;
 };
 
+struct LinearChunkParams : LinearParams {
+    int64_t seg_tokens;              // tokens of a chain's segments
+    float* ws_state;                 // [segments][H][d * d]
+    float* ws_log;                   // [segments][H], base 2
+};
+
 // Chunk-parallel (tensor-core) form of the recurrent layer: the inputs of KdaParams plus the workspace arrays the
 // preparation kernel fills for the chain kernel.  bh = (global block index) * num_heads + head.
 struct KdaGroupParams : KdaParams {
@@ -201,5 +207,6 @@ int wpp_launch_combine(const wpp::CombineParams* p, int num_combine, void* strea
 int wpp_launch_kda_group(const wpp::KdaGroupParams* p, const CUtensorMap* maps, int form, void* stream);
 int wpp_launch_kda(const wpp::KdaParams* p, int num_sms, int layout, void* stream);
 int wpp_launch_linear_token(const wpp::LinearParams* p, int head_dim, int num_sms, void* stream);
+int wpp_launch_linear_chunk(const wpp::LinearChunkParams* p, int head_dim, int64_t segments, int two_passes, void* stream);
 int wpp_launch_selftest_wait(long long limit_cycles, int32_t* status, long long* waited_cycles, void* stream);
 }

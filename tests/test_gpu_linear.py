@@ -7,7 +7,7 @@ import paper_2609_35263_b200 as wpp
 from tests.linear_harness import Wave, ctx
 
 pytestmark = pytest.mark.gpu
-LAYOUTS = (0, 1)
+LAYOUTS = (0, 1, 2)
 
 
 @pytest.mark.parametrize("layout", LAYOUTS)

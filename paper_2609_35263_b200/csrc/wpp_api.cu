@@ -356,6 +356,17 @@ static int kv4_append(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlan
     return WPP_OK;
 }
 
+// Maps of the queries with boxes of 128, 64, 32, 16 rows (packed heads take fewer rows per head).
+static int query_maps(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlanHeader* hd, const void* q, CUtensorMap* tq) {
+    for (int i = 0; i < 4; ++i) {
+        const uint64_t dims[3] = {(uint64_t)d.head_dim, (uint64_t)d.num_q_heads, (uint64_t)hd->total_new_tokens};
+        const uint64_t strides[2] = {(uint64_t)d.q_head_stride * 2, (uint64_t)d.q_token_stride * 2};
+        const uint32_t box[3] = {64, 1, (uint32_t)(128 >> i)};
+        if (int rc = make_map(ctx, &tq[i], q, 3, dims, strides, box)) return rc;
+    }
+    return WPP_OK;
+}
+
 static float scale_log2_of(const wpp_batch_desc& d) {
     const double scale = d.sm_scale > 0.f ? (double)d.sm_scale : 1.0 / sqrt((double)d.head_dim);
     return (float)(scale * 1.4426950408889634);
@@ -419,9 +430,24 @@ static int kv4_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppP
     p.off_few_ctas = hd->off_few_ctas;
     p.f16_1024 = 0x64006400u;
     p.f16_64 = 0x54005400u;
+    p.bf16_128 = 0x43004300u;
+    p.first_tile = hd->num_few_units;
+    p.num_tiles = hd->num_units - hd->num_few_units;
     p.scale_log2 = scale_log2_of(d);
     if (hd->num_few_units > 0) {
         const int e = wpp_launch_kv4_few(d.head_dim, &p, hd->num_few_ctas, hd->max_few_rows, cuda_stream);
+        if (e != 0) return cuda_fail(ctx, e);
+        const_cast<wpp_ctx*>(ctx)->launches += 1;
+    }
+    if (p.num_tiles > 0) {
+        CUtensorMap tq[4];
+        if (int rc = query_maps(ctx, d, hd, q, tq)) return rc;
+        if (p.num_tiles > hd->num_ctas) {
+            p.tile_counter = static_cast<uint32_t*>(workspace);
+            const int e = (int)cudaMemsetAsync(workspace, 0, WPP_WS_HEADER_BYTES, (cudaStream_t)cuda_stream);
+            if (e != 0) return cuda_fail(ctx, e);
+        }
+        const int e = wpp_launch_kv4_tiles(d.head_dim, tq, &p, p.num_tiles < hd->num_ctas ? p.num_tiles : hd->num_ctas, cuda_stream);
         if (e != 0) return cuda_fail(ctx, e);
         const_cast<wpp_ctx*>(ctx)->launches += 1;
     }
@@ -507,12 +533,7 @@ extern "C" int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_
                              workspace, status_dev, cuda_stream);
 
     CUtensorMap tq[4], tk, tv;
-    for (int i = 0; i < 4; ++i) {       // boxes of 128, 64, 32, 16 query rows (packed heads take fewer rows per head)
-        const uint64_t dims[3] = {(uint64_t)d.head_dim, (uint64_t)d.num_q_heads, (uint64_t)hd->total_new_tokens};
-        const uint64_t strides[2] = {(uint64_t)d.q_head_stride * 2, (uint64_t)d.q_token_stride * 2};
-        const uint32_t box[3] = {64, 1, (uint32_t)(128 >> i)};
-        if ((rc = make_map(ctx, &tq[i], q, 3, dims, strides, box)) != WPP_OK) return rc;
-    }
+    if ((rc = query_maps(ctx, d, hd, q, tq)) != WPP_OK) return rc;
     {
         const uint64_t dims[4] = {(uint64_t)d.head_dim, (uint64_t)d.page_size, (uint64_t)d.num_kv_heads,
                                   (uint64_t)d.num_pages};

@@ -95,6 +95,9 @@ struct Kv4AttnParams {
     int32_t num_q_heads, group, page_size, max_blocks, num_pages;
     uint32_t off_q_offsets, off_prefix, off_units, off_few_ctas;
     float scale_log2;
+    uint32_t bf16_128;               // 128 in both halves of a word; as below
+    int32_t first_tile, num_tiles;   // of the plan's units
+    uint32_t* tile_counter;          // or null: every CTA has one tile
     uint32_t f16_1024, f16_64;       // f16 1024 and 64 in both halves of a word (from here, and no constants: see codes_low)
 };
 
@@ -201,6 +204,7 @@ int wpp_launch_attention_small(int head_dim, const CUtensorMap* tq, const CUtens
                                const wpp::SmallAttnParams* p, int num_ctas, void* stream);
 int wpp_launch_append(const wpp::AppendParams* p, int num_sms, void* stream);
 int wpp_launch_kv4_append(int head_dim, const wpp::Kv4AppendParams* p, int num_sms, void* stream);
+int wpp_launch_kv4_tiles(int head_dim, const CUtensorMap* tq, const wpp::Kv4AttnParams* p, int num_ctas, void* stream);
 int wpp_launch_kv4_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream);
 int wpp_launch_combine(const wpp::CombineParams* p, int num_combine, void* stream);
 // maps: q, k, v, alpha; form: 1, 2, 3 = CTAs of 128, 64, 32 columns of the state

@@ -13,10 +13,20 @@ static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // steps; and the fewest steps that a block is cut for.
 constexpr int kFewCtas = 3, kFewCtasWide = 2;
 constexpr int64_t kUnitSteps = 3, kLeastSteps = 2;
+// A chunk is the tile kernel's if the kernel for few rows would walk its keys more often than this.
+constexpr int64_t kFewWalks = 2;
+// Tiles: fewest key steps of a part, and rounds of tiles up to which the longest come first.
+constexpr int32_t kTileLeastSteps = 4;
+constexpr int64_t kTileOrderRounds = 16;
 
 // Row blocks of the kernel for few rows: heads of a KV group, and tokens, WPP_FEW_ROWS rows at most.
 static int32_t few_heads(int32_t group) { return std::min<int32_t>(group, WPP_FEW_ROWS); }
 static int32_t few_tokens(int32_t group) { return std::max<int32_t>(1, WPP_FEW_ROWS / few_heads(group)); }
+
+static bool is_few(const wpp_batch_desc* d, int64_t C) {
+    const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
+    return (C + t - 1) / t * ((G + h - 1) / h) <= kFewWalks;
+}
 
 static int64_t few_blocks(const wpp_batch_desc* d, int64_t C) {
     const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
@@ -30,6 +40,9 @@ size_t wpp_kv4_plan_bytes(const wpp_batch_desc* d, const wpp_plan_opts* o, int64
     size_t n = sizeof(WppPlanHeader) + 2 * align_up(sizeof(int32_t) * (size_t)(d->num_requests + 1), 16);
     n += sizeof(WppUnit) * (size_t)units + align_up(sizeof(int32_t) * ((size_t)std::max(units, kFewCtas * (int64_t)o->max_ctas) + 1), 16);
     n += sizeof(WppCombine) * (size_t)(T * d->num_q_heads / t + (int64_t)d->num_requests * d->num_q_heads);
+    const int64_t tiles = (T / WPP_HALF_M + d->num_requests) * d->num_q_heads;
+    n += sizeof(WppUnit) * (size_t)(o->force_kv_splits >= 2 ? tiles * o->force_kv_splits : tiles + (int64_t)o->max_ctas);
+    n += sizeof(WppCombine) * (size_t)tiles;
     return align_up(n, 256);
 }
 
@@ -44,6 +57,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     int64_t n_base = 0, all_steps = 0;
     int32_t max_rows = 0;
     for (int i = 0; i < R; ++i) {
+        if (!is_few(d, chunk_lens[i])) continue;
         n_base += few_blocks(d, chunk_lens[i]);
         for (int64_t r0 = 0; r0 < chunk_lens[i]; r0 += toks) {
             const int32_t rows = (int32_t)std::min<int64_t>(toks, chunk_lens[i] - r0);
@@ -75,6 +89,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     std::vector<int32_t> cuts;
     for (int i = 0; i < R; ++i) {
         const int64_t P = prefix_lens[i], C = chunk_lens[i];
+        if (!is_few(d, C)) continue;
         for (int64_t r0 = 0; r0 < C; r0 += toks) {
             const int32_t rows = (int32_t)std::min<int64_t>(toks, C - r0), steps = steps_for(P + r0 + rows);
             for (int32_t kvh = 0; kvh < Hkv; ++kvh) {
@@ -135,14 +150,79 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
             }
         }
     }
+    const int64_t n_few = n_units;
+
+    // ---- tiles: two halves of 128 rows each, two heads of a KV group over the same rows where the group is even (both then end at
+    //      the same key), else two row blocks of a head; blocks of at most 64 rows take several heads in a half (see WppUnit)
+    struct Tile { WppUnit u; int32_t steps; };
+    std::vector<Tile> tiles;
+    for (int i = 0; i < R; ++i) {
+        const int64_t P = prefix_lens[i], C = chunk_lens[i];
+        if (is_few(d, C)) continue;
+        const int32_t block = G % 2 == 0 ? WPP_HALF_M : 2 * WPP_HALF_M;
+        for (int64_t r0 = 0; r0 < C; r0 += block) {
+            const int32_t rows = (int32_t)std::min<int64_t>(block, C - r0);
+            Tile t;
+            std::memset(&t, 0, sizeof(t));
+            t.u.request = i;
+            t.u.row0[0] = (int32_t)r0;
+            t.steps = steps_for(P + r0 + rows);
+            int32_t pack = 1, per_tile = 1;
+            if (rows <= WPP_HALF_M) {
+                while (pack < 8 && G % (2 * pack) == 0 && WPP_HALF_M / (2 * pack) >= rows) pack *= 2;
+                int32_t whole = 1;
+                while (whole < G) whole *= 2;
+                per_tile = G % (2 * pack) == 0 ? 2 * pack : pack;
+                if (pack < whole && whole <= 8 && WPP_HALF_M / whole >= rows) {
+                    pack = whole;
+                    per_tile = G;
+                }
+                t.u.rows[0] = rows;
+                t.u.rows[1] = per_tile == 2 * pack ? rows : 0;
+                t.u.row0[1] = (int32_t)r0;
+            } else {
+                t.u.rows[0] = WPP_HALF_M;
+                t.u.rows[1] = rows - WPP_HALF_M;
+                t.u.row0[1] = (int32_t)r0 + WPP_HALF_M;
+            }
+            t.u.pack = pack;
+            for (int32_t h = 0; h < Hq; h += per_tile) {
+                t.u.head[0] = h;
+                t.u.head[1] = h + (per_tile == 2 * pack ? pack : 0);
+                tiles.push_back(t);
+            }
+        }
+    }
+    if ((int64_t)tiles.size() <= kTileOrderRounds * o->max_ctas)
+        std::stable_sort(tiles.begin(), tiles.end(), [](const Tile& a, const Tile& b) { return a.steps > b.steps; });
+    const int64_t tile_parts = tiles.empty() ? 1 : std::max<int64_t>(1, o->max_ctas / (int64_t)tiles.size());
+    for (Tile& t : tiles) {
+        const int32_t parts = std::max(1, o->force_kv_splits >= 1 ? std::min(o->force_kv_splits, t.steps)
+                                                                  : (int32_t)std::min<int64_t>(tile_parts, t.steps / kTileLeastSteps));
+        if (n_units + parts > unit_cap) return WPP_ERR_PLAN_MISMATCH;
+        if (parts > 1)
+            for (int hf = 0; hf < 2; ++hf)
+                for (int32_t k = 0; k < std::min(t.u.pack, G) && t.u.rows[hf] > 0; ++k)
+                    combines.push_back({t.u.request, t.u.row0[hf], t.u.rows[hf], t.u.head[hf] + k, slots, parts, hf, k * (WPP_HALF_M / t.u.pack)});
+        for (int32_t q = 0; q < parts; ++q) {
+            t.u.kv_begin = (int32_t)((int64_t)t.steps * q / parts);
+            t.u.kv_end = (int32_t)((int64_t)t.steps * (q + 1) / parts);
+            t.u.split_slot = parts > 1 ? slots + q : -1;
+            t.u.cost = (t.u.kv_end - t.u.kv_begin) * ((t.u.rows[0] > 0) + (t.u.rows[1] > 0));
+            us[n_units++] = t.u;
+            key_steps += t.u.cost;
+            n_split += parts > 1;
+        }
+        if (parts > 1) slots += parts;
+    }
     if (n_units > 0x3fffffff) return WPP_ERR_INVALID_ARG;
     off += sizeof(WppUnit) * (size_t)n_units;
     if (o->force_kv_splits >= 1) {
         first.clear();
-        for (int64_t u = 0; u < n_units; ++u) first.push_back((int32_t)u);
+        for (int64_t u = 0; u < n_few; ++u) first.push_back((int32_t)u);
     }
-    const int32_t few_ctas = n_units > 0 ? (int32_t)first.size() : 0;
-    first.push_back((int32_t)n_units);
+    const int32_t few_ctas = n_few > 0 ? (int32_t)first.size() : 0;
+    first.push_back((int32_t)n_few);
     if (off + align_up(sizeof(int32_t) * first.size(), 16) > plan_host_bytes) return WPP_ERR_PLAN_MISMATCH;
     hd.off_few_ctas = (uint32_t)off;
     std::memset(p + off, 0, align_up(sizeof(int32_t) * first.size(), 16));
@@ -159,9 +239,9 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     hd.version = WPP_PLAN_VERSION;
     hd.desc_hash = wpp_desc_hash(d);
     hd.num_requests = R;
-    hd.num_ctas = std::max(1, few_ctas);
+    hd.num_ctas = (int32_t)std::max<int64_t>(1, std::min<int64_t>(o->max_ctas, n_units - n_few));
     hd.num_units = (int32_t)n_units;
-    hd.num_few_units = (int32_t)n_units;
+    hd.num_few_units = (int32_t)n_few;
     hd.num_few_ctas = few_ctas;
     hd.max_few_rows = max_rows;
     hd.num_combine = (int32_t)combines.size();
@@ -185,7 +265,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     info->num_tiles = n_units;
     info->num_split_tiles = n_split;
     info->num_combine_tiles = (int64_t)combines.size();
-    info->num_ctas = hd.num_ctas;
+    info->num_ctas = std::max(few_ctas, n_units > n_few ? hd.num_ctas : 1);
     info->total_new_tokens = T;
     info->key_steps = key_steps;
     info->flops = hd.flops;

@@ -99,6 +99,10 @@ __device__ __forceinline__ uint32_t fma_bf16x2(uint32_t a, uint32_t b, uint32_t 
     return r;
 }
 
+__device__ __forceinline__ void st_shared_16(uint32_t at, const uint32_t (&y)[4]) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+}
+
 // What a conversion thread holds of a K or V tile: 16 bytes of each of kRows rows, and their number pairs (0: no such key).
 template <int D>
 struct Raw {
@@ -308,6 +312,21 @@ wpp_kv4_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         const int dw = warp & 3, c = lane % R::kChunks, rr = lane / R::kChunks, r = threadIdx.x & 127;
         const int page_shift = 31 - __clz(p.page_size);
         const bool swap = D == 128 && (c & 2);         // of lanes 2 apart, whose pieces would meet in a bank, one begins with its second half
+        // what of a row's place does not change from key step to key step: the row in the tile, its page, its bytes in the block
+        constexpr int kApart = 32 / R::kChunks;        // rows from one of the thread's rows to the next
+        const int row0 = dw * 32 + rr, ppt = 128 >> page_shift;
+        int page_of[R::kRows], bytes_of[R::kRows], pair_of[R::kRows];
+#pragma unroll
+        for (int i = 0; i < R::kRows; ++i) {
+            const int row = row0 + i * kApart, slot = row & (p.page_size - 1);
+            page_of[i] = row >> page_shift;
+            bytes_of[i] = slot * (D / 2) + c * 16;
+            pair_of[i] = p.page_size * (D / 2) + slot * 4;
+        }
+        uint32_t piece[4];                             // where the four pieces of 8 numbers go in the tile's first row of this thread
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+            piece[q] = (uint32_t)((c >> 1) * C::kHalfBytes + row0 * 128 + ((((c & 1) * 4 + (q ^ (swap ? 2 : 0))) ^ (row0 & 7)) << 4));
         Ring ring_k = {0, 0}, ring_v = {0, 0}, ring_p[2] = {{0, 0}, {0, 0}};
         uint32_t q_phase = 0, tiles = 0;               // tiles: with work, so far
         int bad = 0;
@@ -325,19 +344,24 @@ wpp_kv4_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             int32_t* nan_at = s_nan + tiles % kNan;
             // the place of four tiles on: nobody is so far behind that it reads the one of four tiles ago, nor so far ahead
             if (r == 0) s_nan[(tiles + kNan / 2) % kNan] = 0x7fffffff;
+            const int last_page = (v.kv_len - 1) >> page_shift;
             auto fetch = [&](R& x, const uint8_t* pool, int step) {
+                const int step_at = v.kv_begin + step;
+                int page[R::kRows];
+#pragma unroll
+                for (int i = 0; i < R::kRows; ++i) page[i] = bt[min(step_at * ppt + page_of[i], last_page)];
 #pragma unroll
                 for (int i = 0; i < R::kRows; ++i) {
-                    const int key = (v.kv_begin + step) * 128 + dw * 32 + i * (32 / R::kChunks) + rr;
-                    x.pair[i] = 0u;
-                    x.x[i] = make_uint4(0, 0, 0, 0);
-                    if (key >= v.kv_len) continue;
-                    int page = bt[key >> page_shift];
-                    if (page < 0 || page >= p.num_pages) { bad = 1; page = 0; }
-                    const uint8_t* block = pool + page * p.page_bytes;
-                    const int slot = key & (p.page_size - 1);
-                    x.x[i] = *reinterpret_cast<const uint4*>(block + slot * (D / 2) + c * 16);
-                    x.pair[i] = *reinterpret_cast<const uint32_t*>(block + p.page_size * (D / 2) + slot * 4);
+                    const bool there = (uint32_t)page[i] < (uint32_t)p.num_pages;
+                    bad |= !there;
+                    const uint8_t* block = pool + (there ? page[i] : 0) * p.page_bytes;
+                    x.x[i] = *reinterpret_cast<const uint4*>(block + bytes_of[i]);
+                    x.pair[i] = *reinterpret_cast<const uint32_t*>(block + pair_of[i]);
+                }
+                if ((step_at + 1) * 128 > v.kv_len) {  // what lies behind the sequence counts as zeros
+#pragma unroll
+                    for (int i = 0; i < R::kRows; ++i)
+                        if (step_at * 128 + row0 + i * kApart >= v.kv_len) x.pair[i] = 0u;
                 }
             };
             int nk = 0, nv = 0;                        // fetched so far
@@ -388,42 +412,55 @@ wpp_kv4_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     dead = true;
                     break;
                 }
-                const uint32_t to = (cur_k ? C::kOffK : C::kOffV) + slot * C::kTileBytes;
+                const uint32_t to = (cur_k ? sK : sV) + slot * C::kTileBytes;
+                if (cur_k) {
 #pragma unroll
-                for (int i = 0; i < R::kRows; ++i) {
-                    const int row = dw * 32 + i * (32 / R::kChunks) + rr;
-                    uint8_t* dst = smem_gen + to + (c >> 1) * C::kHalfBytes + row * 128;
-                    uint32_t w[4] = {swap ? cur.x[i].z : cur.x[i].x, swap ? cur.x[i].w : cur.x[i].y, swap ? cur.x[i].x : cur.x[i].z, swap ? cur.x[i].y : cur.x[i].w};
-                    uint32_t pair = cur.pair[i];
-                    if (!cur_k && (pair & 0x7f80u) == 0x7f80u) {       // a row that stands for NaN: zero for the product, see the epilogue
-                        if (c == 0) atomicMin(nan_at, (v.kv_begin + done_v) * 128 + row);
-                        pair = 0u;
-                    }
-                    const uint32_t least2 = __byte_perm(pair, 0u, 0x1010), scale2 = __byte_perm(pair, 0u, 0x3232);
+                    for (int i = 0; i < R::kRows; ++i) {
+                        const uint32_t w[4] = {swap ? cur.x[i].z : cur.x[i].x, swap ? cur.x[i].w : cur.x[i].y, swap ? cur.x[i].x : cur.x[i].z,
+                                               swap ? cur.x[i].y : cur.x[i].w};
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        uint32_t y[4];
+                        for (int q = 0; q < 4; ++q) {
+                            uint32_t y[4];
 #pragma unroll
-                        for (int s = 0; s < 4; ++s) y[s] = codes_128(w[q] >> (4 * s), p.bf16_128);
-                        if (cur_k) {
-#pragma unroll
-                            for (int s = 0; s < 4; ++s) y[s] = sub_bf16x2(y[s], 0x43084308u);          // - 136
-                        } else {
-#pragma unroll
-                            for (int s = 0; s < 4; ++s) y[s] = fma_bf16x2(sub_bf16x2(y[s], 0x43004300u), scale2, least2);
+                            for (int s = 0; s < 4; ++s) y[s] = sub_bf16x2(codes_128(w[q] >> (4 * s), p.bf16_128), 0x43084308u);          // - 136
+                            st_shared_16(to + piece[q] + i * kApart * 128, y);
                         }
-                        const int ch = (c & 1) * 4 + (q ^ (swap ? 2 : 0));
-                        *reinterpret_cast<uint4*>(dst + ((ch ^ (row & 7)) << 4)) = make_uint4(y[0], y[1], y[2], y[3]);
-                    }
-                    if (cur_k && c == 0) {
-                        const float scale = __uint_as_float(pair & 0xffff0000u) * p.scale_log2, least = __uint_as_float(pair << 16) * p.scale_log2;
+                        if (c == 0) {
+                            const float scale = __uint_as_float(cur.pair[i] & 0xffff0000u) * p.scale_log2, least = __uint_as_float(cur.pair[i] << 16) * p.scale_log2;
+                            const int row = row0 + i * kApart;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            if (par_of[h]) {
-                                float* par = reinterpret_cast<float*>(smem_gen + C::kOffPar + (h * kPar + ring_p[h].stage) * 1024) + (row >> 1) * 4 + (row & 1);
-                                par[0] = scale;
-                                par[2] = fmaf(8.f, scale, least);
+                            for (int h = 0; h < 2; ++h)
+                                if (par_of[h]) {
+                                    float* par = reinterpret_cast<float*>(smem_gen + C::kOffPar + (h * kPar + ring_p[h].stage) * 1024) + (row >> 1) * 4 + (row & 1);
+                                    par[0] = scale;
+                                    par[2] = fmaf(8.f, scale, least);
+                                }
+                        }
+                    }
+                } else {
+                    bool nan = false;
+#pragma unroll
+                    for (int i = 0; i < R::kRows; ++i) nan |= (cur.pair[i] & 0x7f80u) == 0x7f80u;
+                    if (nan) {                         // rows that stand for NaN: zero for the product, see the epilogue
+#pragma unroll
+                        for (int i = 0; i < R::kRows; ++i)
+                            if ((cur.pair[i] & 0x7f80u) == 0x7f80u) {
+                                if (c == 0) atomicMin(nan_at, (v.kv_begin + done_v) * 128 + row0 + i * kApart);
+                                cur.pair[i] = 0u;
                             }
+                    }
+#pragma unroll
+                    for (int i = 0; i < R::kRows; ++i) {
+                        const uint32_t least2 = __byte_perm(cur.pair[i], 0u, 0x1010), scale2 = __byte_perm(cur.pair[i], 0u, 0x3232);
+                        const uint32_t w[4] = {swap ? cur.x[i].z : cur.x[i].x, swap ? cur.x[i].w : cur.x[i].y, swap ? cur.x[i].x : cur.x[i].z,
+                                               swap ? cur.x[i].y : cur.x[i].w};
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            uint32_t y[4];
+#pragma unroll
+                            for (int s = 0; s < 4; ++s) y[s] = fma_bf16x2(sub_bf16x2(codes_128(w[q] >> (4 * s), p.bf16_128), 0x43004300u), scale2, least2);
+                            st_shared_16(to + piece[q] + i * kApart * 128, y);
+                        }
                     }
                 }
                 fence_proxy_async_smem();

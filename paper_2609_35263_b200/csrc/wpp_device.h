@@ -73,6 +73,7 @@ struct Kv4AppendParams {
     int64_t kvnew_token_stride, kvnew_head_stride;       // in elements
     int64_t page_bytes, head_bytes;
     int32_t num_requests, num_kv_heads, page_size, max_blocks, num_pages;
+    int32_t few;                     // as in AppendParams
     uint32_t off_q_offsets, off_prefix;
     int64_t total_new_tokens;
 };

@@ -1022,26 +1022,39 @@ static bool linear_desc_ok(const wpp_linear_desc* d) {
            d->v_token_stride >= 0 && d->o_token_stride >= 0 && d->decay_token_stride >= 0;
 }
 
-// Segments of the chains for the form in blocks.  Chains fill the SMs with two CTAs each, or are cut until they do; a segment has
-// kLinLeast tokens at least, since the first pass costs about half of what the second does.
+// How the forms in blocks cut their chains: into so many segments of equal length that the estimated time is least.  On 148 SMs; a
+// block's time in the second pass and in the first, which leaves the segments' states, and what a CTA takes besides, us.
+//                              tokens a block   CTAs per SM   second    first   start
+struct LinearForm { double tokens, ctas, second, first, start; };
+constexpr LinearForm kLinForms[2] = {{64, 2, 4.0, 2.0, 5.0},         // products of 16 x 8 x 16
+                                     {128, 1, 2.4, 1.4, 6.0}};       // tensor memory (heads of 128)
+constexpr int64_t kLinLeast = 256, kLinMostSegments = 32;
 constexpr int64_t kLinTokenForm = 8;       // tokens per request on average from which blocks are taken
-constexpr int64_t kLinLeast = 256, kLinBlockTokens = 64;
+constexpr int64_t kLinTcTokens = 48;       // ... and from which those of 128 are
+static bool linear_uses_tc(const wpp_linear_desc* d) {
+    return d->head_dim == 128 && d->total_tokens >= kLinTcTokens * (int64_t)d->num_requests && d->total_tokens <= 0x7fffffffll;
+}
 struct LinearSegments {
     int64_t tokens, count;          // of a segment; of all chains of a head, at most
     bool two_passes;
     size_t off_log, bytes;          // of the workspace: states, logarithms of decays
 };
-static LinearSegments linear_segments(const wpp_linear_desc* d, int sms) {
+static LinearSegments linear_segments(const wpp_linear_desc* d, bool tc) {
     LinearSegments g;
-    const int64_t chains = (int64_t)d->num_requests * d->num_heads, T = d->total_tokens, most = chains > 0 ? 2 * (int64_t)sms / chains : 1;
-    const int64_t mean = d->num_requests > 0 ? (T + d->num_requests - 1) / d->num_requests : 0;
-    g.two_passes = most >= 2 && mean >= 2 * kLinLeast;
-    g.tokens = (int64_t)1 << 40;
-    if (g.two_passes) {
-        const int64_t len = (mean + most - 1) / most;
-        g.tokens = (len > kLinLeast ? len + kLinBlockTokens - 1 : kLinLeast) / kLinBlockTokens * kLinBlockTokens;
+    const LinearForm& f = kLinForms[tc ? 1 : 0];
+    const double chains = (double)d->num_requests * d->num_heads, slots = 148.0 * f.ctas;
+    const int64_t mean = d->num_requests > 0 ? (d->total_tokens + d->num_requests - 1) / d->num_requests : 0;
+    int64_t best = 1;
+    double best_us = 0.0;
+    for (int64_t s = 1; s <= kLinMostSegments && (s == 1 || mean >= kLinLeast * s); ++s) {
+        const double blocks = ceil((double)mean / (double)s / f.tokens);
+        double us = ceil(chains * (double)s / slots) * (blocks * f.second + f.start);
+        if (s > 1) us += ceil(chains * (double)(s - 1) / slots) * (blocks * f.first + f.start);
+        if (s == 1 || us < 0.97 * best_us) { best = s; best_us = us; }
     }
-    g.count = T / g.tokens + d->num_requests;
+    g.two_passes = best > 1;
+    g.tokens = best > 1 ? ((mean + best - 1) / best + (int64_t)f.tokens - 1) / (int64_t)f.tokens * (int64_t)f.tokens : (int64_t)1 << 40;
+    g.count = d->total_tokens / g.tokens + d->num_requests;
     g.off_log = (size_t)g.count * d->num_heads * d->head_dim * d->head_dim * sizeof(float);
     g.bytes = g.off_log + (size_t)g.count * d->num_heads * sizeof(float);
     return g;
@@ -1049,7 +1062,7 @@ static LinearSegments linear_segments(const wpp_linear_desc* d, int sms) {
 
 extern "C" size_t wpp_linear_workspace_bytes(const wpp_linear_desc* desc) {
     if (!linear_desc_ok(desc) || (desc->head_dim != 64 && desc->head_dim != 128)) return 0;
-    const LinearSegments g = linear_segments(desc, 148);
+    const LinearSegments g = linear_segments(desc, linear_uses_tc(desc));
     return g.two_passes ? g.bytes : 256;
 }
 
@@ -1104,7 +1117,8 @@ extern "C" int wpp_linear_chunk(const wpp_ctx* ctx, const wpp_linear_desc* desc,
         const_cast<wpp_ctx*>(ctx)->launches += 1;
         return WPP_OK;
     }
-    LinearSegments g = linear_segments(desc, 148);
+    const bool tc = linear_uses_tc(desc);
+    LinearSegments g = linear_segments(desc, tc);
     if (g.two_passes) {
         if (workspace && (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return WPP_ERR_INVALID_ARG;
         if (!workspace || workspace_bytes < g.bytes) {                 // whole chains need none
@@ -1117,7 +1131,21 @@ extern "C" int wpp_linear_chunk(const wpp_ctx* ctx, const wpp_linear_desc* desc,
     p.seg_tokens = g.tokens;
     p.ws_state = static_cast<float*>(workspace);
     p.ws_log = reinterpret_cast<float*>(static_cast<char*>(workspace) + g.off_log);
-    const int e = wpp_launch_linear_chunk(&p, desc->head_dim, g.count, g.two_passes, cuda_stream);
+    int e;
+    if (tc) {
+        CUtensorMap maps[3];
+        const void* in[3] = {q, k, v};
+        const int64_t in_stride[3] = {p.q_token_stride, p.k_token_stride, p.v_token_stride};
+        for (int i = 0; i < 3; ++i) {
+            const uint64_t dims[3] = {128, (uint64_t)desc->num_heads, (uint64_t)desc->total_tokens};
+            const uint64_t strides[2] = {256, (uint64_t)in_stride[i] * 2};
+            const uint32_t box[3] = {64, 1, 128};
+            if (int rc = make_map(ctx, &maps[i], in[i], 3, dims, strides, box)) return rc;
+        }
+        e = wpp_launch_linear_tc(&p, maps, g.count, g.two_passes, cuda_stream);
+    } else {
+        e = wpp_launch_linear_chunk(&p, desc->head_dim, g.count, g.two_passes, cuda_stream);
+    }
     if (e != 0) return cuda_fail(ctx, e);
     const_cast<wpp_ctx*>(ctx)->launches += g.two_passes ? 2 : 1;
     return WPP_OK;

@@ -213,5 +213,6 @@ int wpp_launch_kda_group(const wpp::KdaGroupParams* p, const CUtensorMap* maps, 
 int wpp_launch_kda(const wpp::KdaParams* p, int num_sms, int layout, void* stream);
 int wpp_launch_linear_token(const wpp::LinearParams* p, int head_dim, int num_sms, void* stream);
 int wpp_launch_linear_chunk(const wpp::LinearChunkParams* p, int head_dim, int64_t segments, int two_passes, void* stream);
+int wpp_launch_linear_tc(const wpp::LinearChunkParams* p, const CUtensorMap* maps, int64_t segments, int two_passes, void* stream);
 int wpp_launch_selftest_wait(long long limit_cycles, int32_t* status, long long* waited_cycles, void* stream);
 }

@@ -1,0 +1,518 @@
+// Linear attention with a decay per head, heads of 128, in blocks of up to 128 tokens on the 5th-generation tensor cores (the algebra is
+// wpp_linear_chunk.cu's).  One CTA per SM walks a chain (request, head), or a segment of one, with the fp32 state S (128 x 128) in
+// tensor memory.  Per block, with w_j = e^(G_L - G_j):
+//     (1) S1 = Q K^T          (2) O2 = P V, P_ij = e^(G_i - G_j) S1_ij for j <= i, as bf16 where S1 was
+//     (3) O1 = Q bf16(S)      (4) S = e^(G_L) S + (w K)^T V, the weighted K in two bf16 terms (16 bits of every product's factor)
+//     o_i = scale (e^(G_i) O1_i + O2_i)
+// 16 warps, by warpgroup:
+//   warps 0-3    thread = token: P, and at the block's end the outputs
+//   warps 4-7    thread = row of S: bf16(S) into shared memory for (3), e^(G_L) S back, snapshots, first and last states
+//   warps 8-11   thread = token: w K in two terms, one of them in K's place; zeros in the rows of V behind the block
+//   warp 12      issues all products (one thread), warp 13 loads Q, K, V by TMA into a ring of four tiles, in the order in which
+//                their places come free, warp 15 sums the logarithms of the decays
+// What bounds it: memory wants 44 clocks a token (1,032 bytes at 6.5 TB/s on 148 SMs), the products 28, the chain
+// S1 -> P -> O2 -> outputs -> S1 about 31.  Products of 16 x 8 x 16 (mma.sync) at a quarter of this rate took 58.
+// Tensor memory: S1, then P [0,128)  O1 [128,256)  O2 [256,384)  S [384,512).
+// All mbarrier waits are bounded; on expiry the CTA raises its abort flag, every role drains, TMEM is freed and WPP_ERR_TIMEOUT is
+// written to the status word.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "wpp_device.h"
+#include "wpp_ptx.cuh"
+
+namespace lintc {
+using namespace wpp;
+
+constexpr int kD = 128, kL = 128, kThreads = 512, kSlots = 4;
+constexpr int kTile = kL * kD * 2, kHalf = kL * 128;                   // a tile: two 64-column halves of 128-byte rows
+constexpr uint32_t kColS1 = 0, kColO1 = 128, kColO2 = 256, kColS = 384, kTmemCols = 512;
+
+struct Smem {
+    static constexpr int kOffLow = kSlots * kTile;                     // the second term of w K
+    static constexpr int kOffS = kOffLow + kTile;                      // bf16(S)
+    static constexpr int kOffStage = kOffS + kTile;                    // 4 x 2 KB: the output warps' store staging
+    static constexpr int kOffG = kOffStage + 4 * 2048;                 // [2] of float [2][kL + 4]: G, a multiple of 1/64 and the rest; [kL]: G_L
+    static constexpr int kGates = 2 * (kL + 4) * 4;
+    static constexpr int kOffBars = kOffG + 2 * kGates;
+    static constexpr int kNumBars = 2 * kSlots + 4 + 8;
+    static constexpr int kOffMisc = kOffBars + 8 * kNumBars;
+    static constexpr int kBytes = kOffMisc + 8 + 1024;
+};
+static_assert(Smem::kBytes <= 232448, "more shared memory than a CTA can have");
+
+__device__ __forceinline__ int64_t slot_of(const LinearParams& p, int slot) {
+    if (slot >= -1 && slot < p.num_slots) return slot;
+    if (p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
+    return -1;
+}
+
+// kFirst: the pass that leaves the segments' own states (no outputs: (4) alone)
+template <bool kFirst>
+__global__ void __launch_bounds__(kThreads, 1)
+wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                     const LinearChunkParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
+    const uint32_t bars = base + Smem::kOffBars;
+    const uint32_t bFull = bars, bEmpty = bFull + 8 * kSlots, bGFull = bEmpty + 8 * kSlots, bGEmpty = bGFull + 16, bRest = bGEmpty + 16;
+    // S1 landed; P written; O1 and O2 landed; outputs read out of them; bf16(S) written and S scaled; (4) done; w K written
+    const uint32_t bS1 = bRest, bP = bRest + 8, bO = bRest + 16, bOFree = bRest + 24, bState = bRest + 32, bDone = bRest + 40, bK = bRest + 48;
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(gen + Smem::kOffMisc);
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2, r = threadIdx.x & 127;
+    constexpr int kGateUsers = kFirst ? 256 : 384;
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < kSlots; ++i) { mbar_init(bFull + 8 * i, 1); mbar_init(bEmpty + 8 * i, 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(bGFull + 8 * i, 1); mbar_init(bGEmpty + 8 * i, kGateUsers); }
+        mbar_init(bS1, 1); mbar_init(bP, 128); mbar_init(bO, 1); mbar_init(bOFree, 128); mbar_init(bState, 128); mbar_init(bDone, 1); mbar_init(bK, 128);
+        *abort_flag = 0u;
+        fence_barrier_init();
+    }
+    if (warp == 12) {
+        tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kTmemCols);
+        tmem_relinquish();
+    }
+    if (warp == 13 && lane == 0) { prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    grid_launch_dependents();
+    grid_dependency_wait();
+
+    // ---- which request and segment (as in wpp_linear_chunk.cu)
+    const int head = blockIdx.y;
+    const int64_t index = blockIdx.x;
+    int req = 0, hi = p.num_requests;
+    while (hi - req > 1) {
+        const int width = (hi - req + 31) / 32, i = req + lane * width;
+        const unsigned le = __ballot_sync(0xffffffffu, i < hi && p.row_offsets[i] / p.seg_tokens + i <= index) | 1u;
+        const int last = 31 - __clz((int)le);
+        hi = min(hi, req + (last + 1) * width);
+        req += last * width;
+    }
+    const int64_t row0 = p.row_offsets[req], n = p.row_offsets[req + 1] - row0;
+    const int64_t seg = index - (row0 / p.seg_tokens + req), segs = n > 0 ? (n + p.seg_tokens - 1) / p.seg_tokens : 1;
+    const bool mine = seg < segs && !(kFirst && seg == segs - 1);      // (a last segment's own state is nobody's state before)
+    const int64_t begin = seg * p.seg_tokens, end = mine ? min(n, begin + p.seg_tokens) : begin;
+    const int64_t prefix = p.snap_interval > 0 ? p.prefix_lens[req] : 0;
+    auto block_len = [&](int64_t at) {                 // a block ends at the next boundary of the snapshots
+        int64_t len = min((int64_t)kL, end - at);
+        if (p.snap_interval > 0) len = min(len, p.snap_interval - (prefix + at) % p.snap_interval);
+        return (int)len;
+    };
+
+    if (mine && wg == 3) {
+        if (warp == 13 && lane == 0) {
+            // ================================================================ loads
+            uint32_t slot = 0, phase = 0;
+            bool ok = true;
+            for (int64_t at = begin; at < end && ok; at += block_len(at)) {
+#pragma unroll
+                for (int x = kFirst ? 1 : 0; x < 3; ++x) {
+                    if (!mbar_wait(bEmpty + 8 * slot, phase ^ 1u, abort_flag)) { ok = false; break; }
+                    mbar_arrive_expect_tx(bFull + 8 * slot, kTile);
+                    const CUtensorMap* m = x == 0 ? &tm_q : x == 1 ? &tm_k : &tm_v;
+                    tma_load_3d(base + slot * kTile, m, bFull + 8 * slot, 0, head, (int)(row0 + at));
+                    tma_load_3d(base + slot * kTile + kHalf, m, bFull + 8 * slot, 64, head, (int)(row0 + at));
+                    if (++slot == kSlots) { slot = 0; phase ^= 1u; }
+                }
+            }
+        } else if (warp == 12 && lane == 0) {
+            // ================================================================ products
+            constexpr uint32_t id_qk = idesc_bf16(128, 0, 0), id_o = idesc_bf16(128, 0, 1), id_s = idesc_bf16(128, 1, 1);
+            uint32_t slot = 0, phase = 0, b = 0;       // b: blocks so far
+            const uint64_t d_s = smem_desc_sw128(base + Smem::kOffS, kHalf, 1024), d_low = smem_desc_sw128(base + Smem::kOffLow, kHalf, 1024);
+            auto take = [&](uint32_t& at) {            // the ring's next tile
+                const bool ok = mbar_wait(bFull + 8 * slot, phase, abort_flag);
+                at = slot;
+                if (++slot == kSlots) { slot = 0; phase ^= 1u; }
+                return ok;
+            };
+            for (int64_t at = begin; at < end; ++b) {
+                const int len = block_len(at);
+                at += len;
+                const uint32_t par = b & 1u;
+                uint32_t sq = 0, sk = 0, sv = 0;
+                bool k_waited = false;
+                if (!kFirst) {
+                    if (!take(sq) || !take(sk)) break;
+                    if (b > 0 && !mbar_wait(bO, par ^ 1u, abort_flag)) break;       // P, which stands where S1 goes, has been read
+                    tc_fence_after();
+                    const uint64_t dq = smem_desc_sw128(base + sq * kTile, 16, 1024), dk = smem_desc_sw128(base + sk * kTile, 16, 1024);
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk) {
+                        const uint64_t off = (uint64_t)(((kk >> 2) * kHalf + (kk & 3) * 32) >> 4);
+                        mma_ss(tmem + kColS1, dq + off, dk + off, id_qk, kk > 0);
+                    }
+                    mma_commit(bS1);
+                    if (!mbar_wait(bState, par, abort_flag)) break;
+                    if (!mbar_wait(bOFree, par ^ 1u, abort_flag)) break;
+                    tc_fence_after();
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk)
+                        mma_ss(tmem + kColO1, dq + (uint64_t)(((kk >> 2) * kHalf + (kk & 3) * 32) >> 4), d_s + (uint64_t)(kk * 128), id_o, kk > 0);
+                    mma_commit(bEmpty + 8 * sq);
+                    if (!take(sv)) break;
+                    if (len < kL) {                    // rows of V behind the block have been zeroed
+                        if (!mbar_wait(bK, par, abort_flag)) break;
+                        k_waited = true;
+                    }
+                    if (!mbar_wait(bP, par, abort_flag)) break;
+                    tc_fence_after();
+                    const uint64_t dv = smem_desc_sw128(base + sv * kTile, kHalf, 1024);
+#pragma unroll
+                    for (int kk = 0; kk < 8; ++kk) {
+                        if (kk == 0) mma_ts_overwrite(tmem + kColO2, tmem + kColS1, dv, id_o);
+                        else mma_ts_accumulate(tmem + kColO2, tmem + kColS1 + kk * 8, dv + (uint64_t)(kk * 128), id_o);
+                    }
+                    mma_commit(bO);
+                } else {
+                    if (!take(sk) || !take(sv)) break;
+                    if (!mbar_wait(bState, par, abort_flag)) break;
+                }
+                if (!k_waited && !mbar_wait(bK, par, abort_flag)) break;
+                tc_fence_after();
+                const uint64_t dk = smem_desc_sw128(base + sk * kTile, kHalf, 1024), dv = smem_desc_sw128(base + sv * kTile, kHalf, 1024);
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk) mma_ss(tmem + kColS, dk + (uint64_t)(kk * 128), dv + (uint64_t)(kk * 128), id_s, 1);
+#pragma unroll
+                for (int kk = 0; kk < 8; ++kk) mma_ss(tmem + kColS, d_low + (uint64_t)(kk * 128), dv + (uint64_t)(kk * 128), id_s, 1);
+                mma_commit(bEmpty + 8 * sk);
+                mma_commit(bEmpty + 8 * sv);
+                mma_commit(bDone);
+            }
+        } else if (warp == 15) {
+            // ================================================================ sums of the decays' logarithms, base 2, in 64 bits
+            uint32_t b = 0;
+            float g[4] = {0.f, 0.f, 0.f, 0.f};
+            auto load = [&](int64_t at, int len) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int t = 4 * lane + i;
+                    g[i] = t < len ? fmaxf(p.log_decay[(row0 + at + t) * p.decay_token_stride + head] * 1.4426950408889634f, -256.f) : 0.f;
+                }
+            };
+            double all = 0.0;
+            int len = begin < end ? block_len(begin) : 0;
+            if (len > 0) load(begin, len);
+            for (int64_t at = begin; at < end; ++b) {
+                double s[4], sum = 0.0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = sum += (double)g[i];
+                double before = sum;
+#pragma unroll
+                for (int w = 1; w < 32; w *= 2) {
+                    const double x = __shfl_up_sync(0xffffffffu, before, w);
+                    if (lane >= w) before += x;
+                }
+                const double total = __shfl_sync(0xffffffffu, before, 31);
+                before -= sum;
+                at += len;
+                len = at < end ? block_len(at) : 0;
+                if (len > 0) load(at, len);
+                if (!__all_sync(0xffffffffu, mbar_wait(bGEmpty + 8 * (b & 1u), ((b >> 1) & 1u) ^ 1u, abort_flag))) break;
+                float* whole = reinterpret_cast<float*>(gen + Smem::kOffG + (b & 1u) * Smem::kGates);
+                float* rest = whole + kL + 4;
+                auto put = [&](int i, double x) {
+                    const float y = rintf((float)x * 64.f) * 0.015625f;
+                    whole[i] = y;
+                    rest[i] = (float)(x - (double)y);
+                };
+#pragma unroll
+                for (int i = 0; i < 4; ++i) put(4 * lane + i, before + s[i]);
+                if (lane == 0) put(kL, total);
+                all += total;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bGFull + 8 * (b & 1u));
+            }
+            if (kFirst && lane == 0) p.ws_log[index * p.num_heads + head] = (float)all;
+        }
+    } else if (mine && wg == 2) {
+        // ================================================================ w K in two terms (thread = token)
+        uint32_t slot = 0, phase = 0, b = 0;
+        auto skip = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
+        bool ok = true;
+        for (int64_t at = begin; at < end && ok; ++b) {
+            const int len = block_len(at);
+            at += len;
+            if (!kFirst) skip();
+            const uint32_t sk = slot;
+            ok = mbar_wait(bFull + 8 * sk, phase, abort_flag);
+            skip();
+            const uint32_t sv = slot, v_phase = phase;
+            skip();
+            ok = ok && mbar_wait(bGFull + 8 * (b & 1u), (b >> 1) & 1u, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const float* whole = reinterpret_cast<const float*>(gen + Smem::kOffG + (b & 1u) * Smem::kGates);
+            const float* rest = whole + kL + 4;
+            const float w = r < len ? exp2f((whole[kL] - whole[r]) + (rest[kL] - rest[r])) : 0.f;
+            mbar_arrive(bGEmpty + 8 * (b & 1u));
+            // K's place is free to be written once (1) has read it, the second term's once the (4) before has
+            if (!kFirst) ok = mbar_wait(bS1, b & 1u, abort_flag);
+            if (b > 0) ok = ok && mbar_wait(bDone, (b - 1) & 1u, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const uint64_t w2 = pack2(w, w);
+#pragma unroll 4
+            for (int ch = 0; ch < 16; ++ch) {
+                const int off = (ch >> 3) * kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
+                uint4* at_k = reinterpret_cast<uint4*>(gen + sk * kTile + off);
+                const uint4 z = *at_k;
+                const uint32_t x[4] = {z.x, z.y, z.z, z.w};
+                uint32_t h[4], l[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float y0 = __uint_as_float(x[i] << 16) * w, y1 = __uint_as_float(x[i] & 0xffff0000u) * w;
+                    if (r >= len) y0 = y1 = 0.f;       // (a row of something else: it may hold anything)
+                    h[i] = pack_bf16x2(y0, y1);
+                    l[i] = pack_bf16x2(y0 - __uint_as_float(h[i] << 16), y1 - __uint_as_float(h[i] & 0xffff0000u));
+                }
+                *at_k = make_uint4(h[0], h[1], h[2], h[3]);
+                *reinterpret_cast<uint4*>(gen + Smem::kOffLow + off) = make_uint4(l[0], l[1], l[2], l[3]);
+            }
+            if (len < kL) {
+                ok = __all_sync(0xffffffffu, mbar_wait(bFull + 8 * sv, v_phase, abort_flag));
+                if (!ok) break;
+                if (r >= len)
+                    for (int ch = 0; ch < 16; ++ch)
+                        *reinterpret_cast<uint4*>(gen + sv * kTile + (ch >> 3) * kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4)) = make_uint4(0, 0, 0, 0);
+            }
+            fence_proxy_async_smem();
+            mbar_arrive(bK);
+        }
+    } else if (mine && wg == 1) {
+        // ================================================================ the state (thread = row of S)
+        const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kColS;
+        const int64_t slot_size = (int64_t)p.num_heads * kD * kD, row_at = (int64_t)head * kD * kD + (int64_t)r * kD;
+        const int64_t index0 = index - seg;            // of the chain's first segment
+        // workspace: segment i's own state, four columns of all rows after one another; the chain's first state is where its last
+        // segment's would be
+        auto ws = [&](int64_t i, int c4) { return reinterpret_cast<float4*>(p.ws_state + (i * p.num_heads + head) * kD * kD) + c4 * kD + r; };
+        const bool from_pool = seg == 0 && (kFirst || segs == 1);
+        const int64_t in = from_pool ? slot_of(p, p.state_in[req]) : -1;
+        // columns [32 q, 32 q + 32) of the state before the segment
+        auto first_state = [&](int q, float (&x)[32]) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+                float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (from_pool) {
+                    if (in >= 0) y = *reinterpret_cast<const float4*>(p.state_pool + in * slot_size + row_at + 32 * q + 4 * c);
+                    if (kFirst) *ws(index0 + segs - 1, 8 * q + c) = y;         // (state_out may be the same slot, and its segment done first)
+                } else if (!kFirst) {
+                    y = *ws(seg == 0 ? index0 + segs - 1 : index0, 8 * q + c);
+                }
+                x[4 * c] = y.x; x[4 * c + 1] = y.y; x[4 * c + 2] = y.z; x[4 * c + 3] = y.w;
+            }
+            if (!kFirst)
+                for (int64_t i = 1; i < seg; ++i) {
+                    const float a = exp2f(p.ws_log[(index0 + i) * p.num_heads + head]);
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float4 y = *ws(index0 + i, 8 * q + c);
+                        x[4 * c] = fmaf(a, x[4 * c], y.x); x[4 * c + 1] = fmaf(a, x[4 * c + 1], y.y);
+                        x[4 * c + 2] = fmaf(a, x[4 * c + 2], y.z); x[4 * c + 3] = fmaf(a, x[4 * c + 3], y.w);
+                    }
+                }
+        };
+        auto to_pool = [&](int64_t slot, int q, const float (&x)[32]) {
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                *reinterpret_cast<float4*>(p.state_pool + slot * slot_size + row_at + 32 * q + 4 * c) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+        };
+        int64_t snap = p.snap_interval > 0 ? (prefix + begin) / p.snap_interval - prefix / p.snap_interval : 0;
+        auto snap_slot = [&](int64_t at) -> int64_t {  // of the state behind `at` tokens of the chunk, -1: none
+            if (kFirst || p.snap_interval == 0 || at == begin || (prefix + at) % p.snap_interval != 0) return -1;
+            const int64_t s = p.snap_slots && snap < p.max_snaps ? slot_of(p, p.snap_slots[(int64_t)req * p.max_snaps + snap]) : -1;
+            ++snap;
+            return s;
+        };
+        uint32_t b = 0;
+        bool ok = true;
+        for (int64_t at = begin; at < end; ++b) {
+            const int64_t shot = snap_slot(at);
+            at += block_len(at);
+            ok = mbar_wait(bGFull + 8 * (b & 1u), (b >> 1) & 1u, abort_flag);
+            if (b > 0) ok = ok && mbar_wait(bDone, (b - 1) & 1u, abort_flag);
+            ok = __all_sync(0xffffffffu, ok);
+            if (!ok) break;
+            const float* whole = reinterpret_cast<const float*>(gen + Smem::kOffG + (b & 1u) * Smem::kGates);
+            const float a = exp2f(whole[kL] + whole[2 * kL + 4]);
+            mbar_arrive(bGEmpty + 8 * (b & 1u));
+            tc_fence_after();
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+                float x[32];
+                if (b == 0) {
+                    first_state(q, x);
+                } else {
+                    tmem_ld32(lane_addr + 32 * q, reinterpret_cast<uint32_t*>(x));
+                    tmem_wait_ld();
+                }
+                if (shot >= 0) to_pool(shot, q, x);
+                if (!kFirst) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+                        *reinterpret_cast<uint4*>(gen + Smem::kOffS + (q >> 1) * kHalf + r * 128 + ((((q & 1) * 4 + c) ^ (r & 7)) << 4)) =
+                            make_uint4(pack_bf16x2(x[8 * c], x[8 * c + 1]), pack_bf16x2(x[8 * c + 2], x[8 * c + 3]),
+                                       pack_bf16x2(x[8 * c + 4], x[8 * c + 5]), pack_bf16x2(x[8 * c + 6], x[8 * c + 7]));
+                }
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] *= a;
+                tmem_st32(lane_addr + 32 * q, reinterpret_cast<const uint32_t*>(x));
+            }
+            tmem_wait_st();
+            if (!kFirst) fence_proxy_async_smem();
+            tc_fence_before();
+            mbar_arrive(bState);
+        }
+        // ---- the state behind the segment
+        if (ok && b > 0) ok = __all_sync(0xffffffffu, mbar_wait(bDone, (b - 1) & 1u, abort_flag));
+        if (ok) {
+            tc_fence_after();
+            const int64_t shot = b > 0 ? snap_slot(end) : -1, out = !kFirst && seg == segs - 1 ? slot_of(p, p.state_out[req]) : -1;
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+                float x[32];
+                if (b == 0) {
+                    first_state(q, x);
+                } else {
+                    tmem_ld32(lane_addr + 32 * q, reinterpret_cast<uint32_t*>(x));
+                    tmem_wait_ld();
+                }
+                if (shot >= 0) to_pool(shot, q, x);
+                if (out >= 0) to_pool(out, q, x);
+                if (kFirst) {
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) *ws(index, 8 * q + c) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+                }
+            }
+        }
+    } else if (mine && wg == 0 && !kFirst) {
+        // ================================================================ P and the outputs (thread = token)
+        const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        uint32_t b = 0;
+        for (int64_t at = begin; at < end; ++b) {
+            const int len = block_len(at);
+            bool ok = mbar_wait(bGFull + 8 * (b & 1u), (b >> 1) & 1u, abort_flag);
+            ok = ok && mbar_wait(bS1, b & 1u, abort_flag);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            tc_fence_after();
+            const float* whole = reinterpret_cast<const float*>(gen + Smem::kOffG + (b & 1u) * Smem::kGates);
+            const float* rest = whole + kL + 4;
+            const float gh = whole[r], gl = rest[r];
+            const uint64_t gh2 = pack2(gh, gh), gl2 = pack2(gl, gl), minus = pack2(-1.f, -1.f);
+            // (column pair i of P stands where columns 2 i, 2 i + 1 of S1, or some before them, have been read)
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+                uint32_t y[16];
+                if (q <= warp) {                       // columns beyond the warp's last row are zero
+                    float x[32];
+                    tmem_ld32(lane_addr + kColS1 + 32 * q, reinterpret_cast<uint32_t*>(x));
+                    tmem_wait_ld();
+#pragma unroll
+                    for (int i = 0; i < 16; i += 2) {
+                        const float4 h4 = *reinterpret_cast<const float4*>(whole + 32 * q + 2 * i), l4 = *reinterpret_cast<const float4*>(rest + 32 * q + 2 * i);
+                        float e[4];
+                        unpack2(fadd2(ffma2(pack2(h4.x, h4.y), minus, gh2), ffma2(pack2(l4.x, l4.y), minus, gl2)), e[0], e[1]);
+                        unpack2(fadd2(ffma2(pack2(h4.z, h4.w), minus, gh2), ffma2(pack2(l4.z, l4.w), minus, gl2)), e[2], e[3]);
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            const float v = x[2 * i + c] * fast_exp2(e[c]);
+                            x[2 * i + c] = 32 * q + 2 * i + c <= r ? v : 0.f;
+                        }
+                        y[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
+                        y[i + 1] = pack_bf16x2(x[2 * i + 2], x[2 * i + 3]);
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) y[i] = 0u;
+                }
+                tmem_st8(lane_addr + kColS1 + 16 * q, y);
+                tmem_st8(lane_addr + kColS1 + 16 * q + 8, y + 8);
+            }
+            mbar_arrive(bGEmpty + 8 * (b & 1u));
+            tmem_wait_st();
+            tc_fence_before();
+            mbar_arrive(bP);
+            const float e1 = p.scale * exp2f(gh + gl);
+            if (!__all_sync(0xffffffffu, mbar_wait(bO, b & 1u, abort_flag))) break;
+            tc_fence_after();
+            const __nv_bfloat16* dst = p.out + (row0 + at + r) * p.o_token_stride + (int64_t)head * kD;
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+                float x[32], z[32];
+                tmem_ld32(lane_addr + kColO1 + 32 * q, reinterpret_cast<uint32_t*>(x));
+                tmem_ld32(lane_addr + kColO2 + 32 * q, reinterpret_cast<uint32_t*>(z));
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i], e1, z[i] * p.scale);
+                uint4 w[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    w[i] = make_uint4(pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]),
+                                      pack_bf16x2(x[8 * i + 4], x[8 * i + 5]), pack_bf16x2(x[8 * i + 6], x[8 * i + 7]));
+                if (q == 3) {
+                    tc_fence_before();
+                    mbar_arrive(bOFree);
+                }
+                warp_store_rows64(gen + Smem::kOffStage + warp * 2048, lane, w, dst, r < len, q * 64);
+            }
+            at += len;
+        }
+    }
+
+    // ---- teardown: every loop above is bounded, so every thread gets here
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 400000) { }            // let copies and tensor-core work in flight land
+        if (threadIdx.x == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_TIMEOUT);
+        __syncthreads();
+    }
+    if (warp == 12) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+template <bool kFirst>
+static cudaError_t launch(const CUtensorMap* maps, const LinearChunkParams& p, int64_t segments, cudaStream_t stream) {
+    static bool attr_set[64] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev >= 0 && dev < 64 && !attr_set[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(wpp_linear_tc_kernel<kFirst>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem::kBytes);
+        if (e != cudaSuccess) return e;
+        attr_set[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)segments, (unsigned)p.num_heads);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Smem::kBytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute overlap;
+    overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    overlap.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &overlap;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, wpp_linear_tc_kernel<kFirst>, maps[0], maps[1], maps[2], p);
+}
+
+}  // namespace lintc
+
+// maps: q, k, v with boxes of 64 columns of 128 rows; segments: an upper bound of all requests' segments
+extern "C" int wpp_launch_linear_tc(const wpp::LinearChunkParams* p, const CUtensorMap* maps, int64_t segments, int two_passes, void* stream) {
+    cudaStream_t st = (cudaStream_t)stream;
+    cudaError_t e = cudaSuccess;
+    if (two_passes) e = lintc::launch<true>(maps, *p, segments, st);
+    if (e == cudaSuccess) e = lintc::launch<false>(maps, *p, segments, st);
+    return (int)e;
+}

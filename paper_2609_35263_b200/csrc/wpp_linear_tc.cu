@@ -1,9 +1,9 @@
 // Linear attention with a decay per head, heads of 128, in blocks of up to 128 tokens on the 5th-generation tensor cores (the algebra is
 // wpp_linear_chunk.cu's).  One CTA per SM walks a chain (request, head), or a segment of one, with the fp32 state S (128 x 128) in
 // tensor memory.  Per block, with w_j = e^(G_L - G_j):
-//     (1) S1 = Q K^T          (2) O2 = P V, P_ij = e^(G_i - G_j) S1_ij for j <= i, as bf16 where S1 was
+//     (1) S1 = Q K^T          (2) O2 = P V, P_ij = scale e^(G_i - G_j) S1_ij for j <= i, as bf16 where S1 was
 //     (3) O1 = Q bf16(S)      (4) S = e^(G_L) S + (w K)^T V, the weighted K in two bf16 terms (16 bits of every product's factor)
-//     o_i = scale (e^(G_i) O1_i + O2_i)
+//     o_i = scale e^(G_i) O1_i + O2_i
 // 16 warps, by warpgroup:
 //   warps 0-3    thread = token: P, and at the block's end the outputs
 //   warps 4-7    thread = row of S: bf16(S) into shared memory for (3), e^(G_L) S back, snapshots, first and last states
@@ -34,14 +34,21 @@ struct Smem {
     static constexpr int kOffLow = kSlots * kTile;                     // the second term of w K
     static constexpr int kOffS = kOffLow + kTile;                      // bf16(S)
     static constexpr int kOffStage = kOffS + kTile;                    // 4 x 2 KB: the output warps' store staging
-    static constexpr int kOffG = kOffStage + 4 * 2048;                 // [2] of float [2][kL + 4]: G, a multiple of 1/64 and the rest; [kL]: G_L
-    static constexpr int kGates = 2 * (kL + 4) * 4;
+    // [2] of float [2][kL + 4]: G, a multiple of 1/64 and the rest, [kL] being G_L; and float [kL]: e^(G_e - G_j), e the last token of j's 32
+    static constexpr int kOffG = kOffStage + 4 * 2048;
+    static constexpr int kGates = (2 * (kL + 4) + kL) * 4;
     static constexpr int kOffBars = kOffG + 2 * kGates;
     static constexpr int kNumBars = 2 * kSlots + 4 + 8;
     static constexpr int kOffMisc = kOffBars + 8 * kNumBars;
     static constexpr int kBytes = kOffMisc + 8 + 1024;
 };
 static_assert(Smem::kBytes <= 232448, "more shared memory than a CTA can have");
+
+__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 
 __device__ __forceinline__ int64_t slot_of(const LinearParams& p, int slot) {
     if (slot >= -1 && slot < p.num_slots) return slot;
@@ -226,6 +233,9 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 };
 #pragma unroll
                 for (int i = 0; i < 4; ++i) put(4 * lane + i, before + s[i]);
+                const double at_end = __shfl_sync(0xffffffffu, before + s[3], lane | 7);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) rest[kL + 4 + 4 * lane + i] = exp2f((float)(at_end - (before + s[i])));
                 if (lane == 0) put(kL, total);
                 all += total;
                 __syncwarp();
@@ -259,7 +269,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             if (b > 0) ok = ok && mbar_wait(bDone, (b - 1) & 1u, abort_flag);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
-            const uint64_t w2 = pack2(w, w);
+            const uint64_t w2 = pack2(w, w), minus = pack2(-1.f, -1.f);
 #pragma unroll 4
             for (int ch = 0; ch < 16; ++ch) {
                 const int off = (ch >> 3) * kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
@@ -269,10 +279,13 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 uint32_t h[4], l[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float y0 = __uint_as_float(x[i] << 16) * w, y1 = __uint_as_float(x[i] & 0xffff0000u) * w;
-                    if (r >= len) y0 = y1 = 0.f;       // (a row of something else: it may hold anything)
+                    const uint32_t xi = r < len ? x[i] : 0u;           // (a row of something else may hold anything)
+                    const uint64_t y = fmul2(pack2(__uint_as_float(xi << 16), __uint_as_float(xi & 0xffff0000u)), w2);
+                    float y0, y1;
+                    unpack2(y, y0, y1);
                     h[i] = pack_bf16x2(y0, y1);
-                    l[i] = pack_bf16x2(y0 - __uint_as_float(h[i] << 16), y1 - __uint_as_float(h[i] & 0xffff0000u));
+                    unpack2(ffma2(pack2(__uint_as_float(h[i] << 16), __uint_as_float(h[i] & 0xffff0000u)), minus, y), y0, y1);
+                    l[i] = pack_bf16x2(y0, y1);
                 }
                 *at_k = make_uint4(h[0], h[1], h[2], h[3]);
                 *reinterpret_cast<uint4*>(gen + Smem::kOffLow + off) = make_uint4(l[0], l[1], l[2], l[3]);
@@ -346,15 +359,8 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             const float a = exp2f(whole[kL] + whole[2 * kL + 4]);
             mbar_arrive(bGEmpty + 8 * (b & 1u));
             tc_fence_after();
-#pragma unroll 1
-            for (int q = 0; q < 4; ++q) {
-                float x[32];
-                if (b == 0) {
-                    first_state(q, x);
-                } else {
-                    tmem_ld32(lane_addr + 32 * q, reinterpret_cast<uint32_t*>(x));
-                    tmem_wait_ld();
-                }
+            const uint64_t a2 = pack2(a, a);
+            auto put = [&](int q, float (&x)[32]) {
                 if (shot >= 0) to_pool(shot, q, x);
                 if (!kFirst) {
 #pragma unroll
@@ -364,8 +370,26 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                                        pack_bf16x2(x[8 * c + 4], x[8 * c + 5]), pack_bf16x2(x[8 * c + 6], x[8 * c + 7]));
                 }
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] *= a;
+                for (int i = 0; i < 32; i += 2) unpack2(fmul2(pack2(x[i], x[i + 1]), a2), x[i], x[i + 1]);
                 tmem_st32(lane_addr + 32 * q, reinterpret_cast<const uint32_t*>(x));
+            };
+            if (b == 0) {
+#pragma unroll 1
+                for (int q = 0; q < 4; ++q) {
+                    float x[32];
+                    first_state(q, x);
+                    put(q, x);
+                }
+            } else {
+#pragma unroll 1
+                for (int q = 0; q < 4; q += 2) {       // two pieces on the way at a time
+                    float x[32], z[32];
+                    tmem_ld32(lane_addr + 32 * q, reinterpret_cast<uint32_t*>(x));
+                    tmem_ld32(lane_addr + 32 * q + 32, reinterpret_cast<uint32_t*>(z));
+                    tmem_wait_ld();
+                    put(q, x);
+                    put(q + 1, z);
+                }
             }
             tmem_wait_st();
             if (!kFirst) fence_proxy_async_smem();
@@ -406,33 +430,47 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             tc_fence_after();
             const float* whole = reinterpret_cast<const float*>(gen + Smem::kOffG + (b & 1u) * Smem::kGates);
             const float* rest = whole + kL + 4;
+            const float* to_end = rest + kL + 4;
             const float gh = whole[r], gl = rest[r];
-            const uint64_t gh2 = pack2(gh, gh), gl2 = pack2(gl, gl), minus = pack2(-1.f, -1.f);
             // (column pair i of P stands where columns 2 i, 2 i + 1 of S1, or some before them, have been read)
 #pragma unroll 1
             for (int q = 0; q < 4; ++q) {
                 uint32_t y[16];
-                if (q <= warp) {                       // columns beyond the warp's last row are zero
-                    float x[32];
-                    tmem_ld32(lane_addr + kColS1 + 32 * q, reinterpret_cast<uint32_t*>(x));
-                    tmem_wait_ld();
-#pragma unroll
-                    for (int i = 0; i < 16; i += 2) {
-                        const float4 h4 = *reinterpret_cast<const float4*>(whole + 32 * q + 2 * i), l4 = *reinterpret_cast<const float4*>(rest + 32 * q + 2 * i);
-                        float e[4];
-                        unpack2(fadd2(ffma2(pack2(h4.x, h4.y), minus, gh2), ffma2(pack2(l4.x, l4.y), minus, gl2)), e[0], e[1]);
-                        unpack2(fadd2(ffma2(pack2(h4.z, h4.w), minus, gh2), ffma2(pack2(l4.z, l4.w), minus, gl2)), e[2], e[3]);
-#pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            const float v = x[2 * i + c] * fast_exp2(e[c]);
-                            x[2 * i + c] = 32 * q + 2 * i + c <= r ? v : 0.f;
-                        }
-                        y[i] = pack_bf16x2(x[2 * i], x[2 * i + 1]);
-                        y[i + 1] = pack_bf16x2(x[2 * i + 2], x[2 * i + 3]);
-                    }
-                } else {
+                if (q > warp) {                        // columns beyond the warp's last row
 #pragma unroll
                     for (int i = 0; i < 16; ++i) y[i] = 0u;
+                } else {
+                    float x[32];
+                    tmem_ld32(lane_addr + kColS1 + 32 * q, reinterpret_cast<uint32_t*>(x));
+                    if (q < warp) {
+                        // e^(G_i - G_j) = e^(G_i - G_e) e^(G_e - G_j), e the last of the 32 columns: neither factor is above 1
+                        const float f = p.scale * exp2f((gh - whole[32 * q + 31]) + (gl - rest[32 * q + 31]));
+                        const uint64_t f2 = pack2(f, f);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            const float4 c = *reinterpret_cast<const float4*>(to_end + 32 * q + 2 * i);
+                            float v[4];
+                            unpack2(fmul2(pack2(x[2 * i], x[2 * i + 1]), fmul2(pack2(c.x, c.y), f2)), v[0], v[1]);
+                            unpack2(fmul2(pack2(x[2 * i + 2], x[2 * i + 3]), fmul2(pack2(c.z, c.w), f2)), v[2], v[3]);
+                            y[i] = pack_bf16x2(v[0], v[1]);
+                            y[i + 1] = pack_bf16x2(v[2], v[3]);
+                        }
+                    } else {
+                        const uint64_t gh2 = pack2(gh, gh), gl2 = pack2(gl, gl), minus = pack2(-1.f, -1.f);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; i += 2) {
+                            const float4 h4 = *reinterpret_cast<const float4*>(whole + 32 * q + 2 * i), l4 = *reinterpret_cast<const float4*>(rest + 32 * q + 2 * i);
+                            float e[4];
+                            unpack2(fadd2(ffma2(pack2(h4.x, h4.y), minus, gh2), ffma2(pack2(l4.x, l4.y), minus, gl2)), e[0], e[1]);
+                            unpack2(fadd2(ffma2(pack2(h4.z, h4.w), minus, gh2), ffma2(pack2(l4.z, l4.w), minus, gl2)), e[2], e[3]);
+#pragma unroll
+                            for (int c = 0; c < 4; ++c) e[c] = 2 * i + c <= lane ? p.scale * fast_exp2(e[c]) * x[2 * i + c] : 0.f;
+                            y[i] = pack_bf16x2(e[0], e[1]);
+                            y[i + 1] = pack_bf16x2(e[2], e[3]);
+                        }
+                    }
                 }
                 tmem_st8(lane_addr + kColS1 + 16 * q, y);
                 tmem_st8(lane_addr + kColS1 + 16 * q + 8, y + 8);
@@ -442,6 +480,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             tc_fence_before();
             mbar_arrive(bP);
             const float e1 = p.scale * exp2f(gh + gl);
+            const uint64_t e2 = pack2(e1, e1);
             if (!__all_sync(0xffffffffu, mbar_wait(bO, b & 1u, abort_flag))) break;
             tc_fence_after();
             const __nv_bfloat16* dst = p.out + (row0 + at + r) * p.o_token_stride + (int64_t)head * kD;
@@ -452,7 +491,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 tmem_ld32(lane_addr + kColO2 + 32 * q, reinterpret_cast<uint32_t*>(z));
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) x[i] = fmaf(x[i], e1, z[i] * p.scale);
+                for (int i = 0; i < 32; i += 2) unpack2(ffma2(pack2(x[i], x[i + 1]), e2, pack2(z[i], z[i + 1])), x[i], x[i + 1]);
                 uint4 w[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)

@@ -56,6 +56,31 @@ __device__ __forceinline__ int64_t slot_of(const LinearParams& p, int slot) {
     return -1;
 }
 
+struct Walk {
+    int64_t at, end, left, interval;                   // left: tokens up to the next boundary
+    __device__ __forceinline__ bool more() const { return at < end; }
+    __device__ __forceinline__ int len() const { return (int)min(min((int64_t)kL, end - at), left); }
+    __device__ __forceinline__ void next() {
+        const int n = len();
+        at += n;
+        left = left == n ? interval : left - n;
+    }
+    __device__ __forceinline__ bool at_boundary() const { return left == interval; }
+};
+
+// A row of the state (this thread's) between tensor memory and global memory, `apart` float4s between its pieces: rarely called, and
+// apart from the loops for the same reason.
+__device__ __noinline__ void state_to_memory(uint32_t taddr, float4* to, int apart) {
+#pragma unroll 1
+    for (int q = 0; q < 4; ++q) {
+        float x[32];
+        tmem_ld32(taddr + 32 * q, reinterpret_cast<uint32_t*>(x));
+        tmem_wait_ld();
+#pragma unroll
+        for (int c = 0; c < 8; ++c) to[(8 * q + c) * apart] = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+    }
+}
+
 // kFirst: the pass that leaves the segments' own states (no outputs: (4) alone)
 template <bool kFirst>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -108,25 +133,24 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     const bool mine = seg < segs && !(kFirst && seg == segs - 1);      // (a last segment's own state is nobody's state before)
     const int64_t begin = seg * p.seg_tokens, end = mine ? min(n, begin + p.seg_tokens) : begin;
     const int64_t prefix = p.snap_interval > 0 ? p.prefix_lens[req] : 0;
-    auto block_len = [&](int64_t at) {                 // a block ends at the next boundary of the snapshots
-        int64_t len = min((int64_t)kL, end - at);
-        if (p.snap_interval > 0) len = min(len, p.snap_interval - (prefix + at) % p.snap_interval);
-        return (int)len;
-    };
+    // Blocks end at the next boundary of the snapshots.  (Every role walks them by itself: with a 64-bit remainder per block in the
+    // roles' loops the instructions of so many roles no longer fit where an SM fetches them fast; 151 us for 8 x 2,048 tokens | 142.)
+    const int64_t interval = p.snap_interval > 0 ? p.snap_interval : (int64_t)1 << 60;
+    const Walk blocks = {begin, end, p.snap_interval > 0 ? interval - (prefix + begin) % interval : interval, interval};
 
     if (mine && wg == 3) {
         if (warp == 13 && lane == 0) {
             // ================================================================ loads
             uint32_t slot = 0, phase = 0;
             bool ok = true;
-            for (int64_t at = begin; at < end && ok; at += block_len(at)) {
+            for (Walk w = blocks; w.more() && ok; w.next()) {
 #pragma unroll
                 for (int x = kFirst ? 1 : 0; x < 3; ++x) {
                     if (!mbar_wait(bEmpty + 8 * slot, phase ^ 1u, abort_flag)) { ok = false; break; }
                     mbar_arrive_expect_tx(bFull + 8 * slot, kTile);
                     const CUtensorMap* m = x == 0 ? &tm_q : x == 1 ? &tm_k : &tm_v;
-                    tma_load_3d(base + slot * kTile, m, bFull + 8 * slot, 0, head, (int)(row0 + at));
-                    tma_load_3d(base + slot * kTile + kHalf, m, bFull + 8 * slot, 64, head, (int)(row0 + at));
+                    tma_load_3d(base + slot * kTile, m, bFull + 8 * slot, 0, head, (int)(row0 + w.at));
+                    tma_load_3d(base + slot * kTile + kHalf, m, bFull + 8 * slot, 64, head, (int)(row0 + w.at));
                     if (++slot == kSlots) { slot = 0; phase ^= 1u; }
                 }
             }
@@ -141,9 +165,8 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 if (++slot == kSlots) { slot = 0; phase ^= 1u; }
                 return ok;
             };
-            for (int64_t at = begin; at < end; ++b) {
-                const int len = block_len(at);
-                at += len;
+            for (Walk w = blocks; w.more(); w.next(), ++b) {
+                const int len = w.len();
                 const uint32_t par = b & 1u;
                 uint32_t sq = 0, sk = 0, sv = 0;
                 bool k_waited = false;
@@ -206,23 +229,22 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 }
             };
             double all = 0.0;
-            int len = begin < end ? block_len(begin) : 0;
-            if (len > 0) load(begin, len);
-            for (int64_t at = begin; at < end; ++b) {
+            Walk w = blocks;
+            if (w.more()) load(w.at, w.len());
+            for (; w.more(); ++b) {
                 double s[4], sum = 0.0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[i] = sum += (double)g[i];
                 double before = sum;
 #pragma unroll
-                for (int w = 1; w < 32; w *= 2) {
-                    const double x = __shfl_up_sync(0xffffffffu, before, w);
-                    if (lane >= w) before += x;
+                for (int o = 1; o < 32; o *= 2) {
+                    const double x = __shfl_up_sync(0xffffffffu, before, o);
+                    if (lane >= o) before += x;
                 }
                 const double total = __shfl_sync(0xffffffffu, before, 31);
                 before -= sum;
-                at += len;
-                len = at < end ? block_len(at) : 0;
-                if (len > 0) load(at, len);
+                w.next();
+                if (w.more()) load(w.at, w.len());
                 if (!__all_sync(0xffffffffu, mbar_wait(bGEmpty + 8 * (b & 1u), ((b >> 1) & 1u) ^ 1u, abort_flag))) break;
                 float* whole = reinterpret_cast<float*>(gen + Smem::kOffG + (b & 1u) * Smem::kGates);
                 float* rest = whole + kL + 4;
@@ -235,7 +257,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 for (int i = 0; i < 4; ++i) put(4 * lane + i, before + s[i]);
                 const double at_end = __shfl_sync(0xffffffffu, before + s[3], lane | 7);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) rest[kL + 4 + 4 * lane + i] = exp2f((float)(at_end - (before + s[i])));
+                for (int i = 0; i < 4; ++i) rest[kL + 4 + 4 * lane + i] = fast_exp2((float)(at_end - (before + s[i])));
                 if (lane == 0) put(kL, total);
                 all += total;
                 __syncwarp();
@@ -248,9 +270,8 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         uint32_t slot = 0, phase = 0, b = 0;
         auto skip = [&] { if (++slot == kSlots) { slot = 0; phase ^= 1u; } };
         bool ok = true;
-        for (int64_t at = begin; at < end && ok; ++b) {
-            const int len = block_len(at);
-            at += len;
+        for (Walk walk = blocks; walk.more() && ok; walk.next(), ++b) {
+            const int len = walk.len();
             if (!kFirst) skip();
             const uint32_t sk = slot;
             ok = mbar_wait(bFull + 8 * sk, phase, abort_flag);
@@ -262,7 +283,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             if (!ok) break;
             const float* whole = reinterpret_cast<const float*>(gen + Smem::kOffG + (b & 1u) * Smem::kGates);
             const float* rest = whole + kL + 4;
-            const float w = r < len ? exp2f((whole[kL] - whole[r]) + (rest[kL] - rest[r])) : 0.f;
+            const float w = r < len ? fast_exp2((whole[kL] - whole[r]) + (rest[kL] - rest[r])) : 0.f;
             mbar_arrive(bGEmpty + 8 * (b & 1u));
             // K's place is free to be written once (1) has read it, the second term's once the (4) before has
             if (!kFirst) ok = mbar_wait(bS1, b & 1u, abort_flag);
@@ -270,7 +291,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             const uint64_t w2 = pack2(w, w), minus = pack2(-1.f, -1.f);
-#pragma unroll 4
+#pragma unroll 2
             for (int ch = 0; ch < 16; ++ch) {
                 const int off = (ch >> 3) * kHalf + r * 128 + (((ch & 7) ^ (r & 7)) << 4);
                 uint4* at_k = reinterpret_cast<uint4*>(gen + sk * kTile + off);
@@ -310,8 +331,10 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         auto ws = [&](int64_t i, int c4) { return reinterpret_cast<float4*>(p.ws_state + (i * p.num_heads + head) * kD * kD) + c4 * kD + r; };
         const bool from_pool = seg == 0 && (kFirst || segs == 1);
         const int64_t in = from_pool ? slot_of(p, p.state_in[req]) : -1;
-        // columns [32 q, 32 q + 32) of the state before the segment
-        auto first_state = [&](int q, float (&x)[32]) {
+        // the state before the segment into tensor memory
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+            float x[32];
 #pragma unroll
             for (int c = 0; c < 8; ++c) {
                 float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -323,9 +346,10 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 }
                 x[4 * c] = y.x; x[4 * c + 1] = y.y; x[4 * c + 2] = y.z; x[4 * c + 3] = y.w;
             }
-            if (!kFirst)
+            if (!kFirst) {
+#pragma unroll 1
                 for (int64_t i = 1; i < seg; ++i) {
-                    const float a = exp2f(p.ws_log[(index0 + i) * p.num_heads + head]);
+                    const float a = fast_exp2(p.ws_log[(index0 + i) * p.num_heads + head]);
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         const float4 y = *ws(index0 + i, 8 * q + c);
@@ -333,35 +357,35 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         x[4 * c + 2] = fmaf(a, x[4 * c + 2], y.z); x[4 * c + 3] = fmaf(a, x[4 * c + 3], y.w);
                     }
                 }
-        };
-        auto to_pool = [&](int64_t slot, int q, const float (&x)[32]) {
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-                *reinterpret_cast<float4*>(p.state_pool + slot * slot_size + row_at + 32 * q + 4 * c) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
-        };
+            }
+            tmem_st32(lane_addr + 32 * q, reinterpret_cast<const uint32_t*>(x));
+        }
+        tmem_wait_st();
         int64_t snap = p.snap_interval > 0 ? (prefix + begin) / p.snap_interval - prefix / p.snap_interval : 0;
-        auto snap_slot = [&](int64_t at) -> int64_t {  // of the state behind `at` tokens of the chunk, -1: none
-            if (kFirst || p.snap_interval == 0 || at == begin || (prefix + at) % p.snap_interval != 0) return -1;
-            const int64_t s = p.snap_slots && snap < p.max_snaps ? slot_of(p, p.snap_slots[(int64_t)req * p.max_snaps + snap]) : -1;
+        auto snapshot = [&] {                          // of the state as it is, at a boundary
+            const int64_t slot = p.snap_slots && snap < p.max_snaps ? slot_of(p, p.snap_slots[(int64_t)req * p.max_snaps + snap]) : -1;
             ++snap;
-            return s;
+            if (slot >= 0) state_to_memory(lane_addr, reinterpret_cast<float4*>(p.state_pool + slot * slot_size + row_at), 1);
         };
         uint32_t b = 0;
         bool ok = true;
-        for (int64_t at = begin; at < end; ++b) {
-            const int64_t shot = snap_slot(at);
-            at += block_len(at);
+        Walk walk = blocks;
+        for (; walk.more(); walk.next(), ++b) {
             ok = mbar_wait(bGFull + 8 * (b & 1u), (b >> 1) & 1u, abort_flag);
             if (b > 0) ok = ok && mbar_wait(bDone, (b - 1) & 1u, abort_flag);
             ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
             const float* whole = reinterpret_cast<const float*>(gen + Smem::kOffG + (b & 1u) * Smem::kGates);
-            const float a = exp2f(whole[kL] + whole[2 * kL + 4]);
+            const float a = fast_exp2(whole[kL] + whole[2 * kL + 4]);
             mbar_arrive(bGEmpty + 8 * (b & 1u));
             tc_fence_after();
+            if (!kFirst && b > 0 && walk.at_boundary()) snapshot();
             const uint64_t a2 = pack2(a, a);
-            auto put = [&](int q, float (&x)[32]) {
-                if (shot >= 0) to_pool(shot, q, x);
+#pragma unroll 1
+            for (int q = 0; q < 4; ++q) {
+                float x[32];
+                tmem_ld32(lane_addr + 32 * q, reinterpret_cast<uint32_t*>(x));
+                tmem_wait_ld();
                 if (!kFirst) {
 #pragma unroll
                     for (int c = 0; c < 4; ++c)
@@ -372,24 +396,6 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                 for (int i = 0; i < 32; i += 2) unpack2(fmul2(pack2(x[i], x[i + 1]), a2), x[i], x[i + 1]);
                 tmem_st32(lane_addr + 32 * q, reinterpret_cast<const uint32_t*>(x));
-            };
-            if (b == 0) {
-#pragma unroll 1
-                for (int q = 0; q < 4; ++q) {
-                    float x[32];
-                    first_state(q, x);
-                    put(q, x);
-                }
-            } else {
-#pragma unroll 1
-                for (int q = 0; q < 4; q += 2) {       // two pieces on the way at a time
-                    float x[32], z[32];
-                    tmem_ld32(lane_addr + 32 * q, reinterpret_cast<uint32_t*>(x));
-                    tmem_ld32(lane_addr + 32 * q + 32, reinterpret_cast<uint32_t*>(z));
-                    tmem_wait_ld();
-                    put(q, x);
-                    put(q + 1, z);
-                }
             }
             tmem_wait_st();
             if (!kFirst) fence_proxy_async_smem();
@@ -400,30 +406,20 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         if (ok && b > 0) ok = __all_sync(0xffffffffu, mbar_wait(bDone, (b - 1) & 1u, abort_flag));
         if (ok) {
             tc_fence_after();
-            const int64_t shot = b > 0 ? snap_slot(end) : -1, out = !kFirst && seg == segs - 1 ? slot_of(p, p.state_out[req]) : -1;
-#pragma unroll 1
-            for (int q = 0; q < 4; ++q) {
-                float x[32];
-                if (b == 0) {
-                    first_state(q, x);
-                } else {
-                    tmem_ld32(lane_addr + 32 * q, reinterpret_cast<uint32_t*>(x));
-                    tmem_wait_ld();
-                }
-                if (shot >= 0) to_pool(shot, q, x);
-                if (out >= 0) to_pool(out, q, x);
-                if (kFirst) {
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) *ws(index, 8 * q + c) = make_float4(x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
-                }
+            if (kFirst) {
+                state_to_memory(lane_addr, ws(index, 0), kD);
+            } else {
+                if (b > 0 && walk.at_boundary() && p.snap_interval > 0) snapshot();
+                const int64_t out = seg == segs - 1 ? slot_of(p, p.state_out[req]) : -1;
+                if (out >= 0) state_to_memory(lane_addr, reinterpret_cast<float4*>(p.state_pool + out * slot_size + row_at), 1);
             }
         }
     } else if (mine && wg == 0 && !kFirst) {
         // ================================================================ P and the outputs (thread = token)
         const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         uint32_t b = 0;
-        for (int64_t at = begin; at < end; ++b) {
-            const int len = block_len(at);
+        for (Walk walk = blocks; walk.more(); walk.next(), ++b) {
+            const int len = walk.len();
             bool ok = mbar_wait(bGFull + 8 * (b & 1u), (b >> 1) & 1u, abort_flag);
             ok = ok && mbar_wait(bS1, b & 1u, abort_flag);
             if (!__all_sync(0xffffffffu, ok)) break;
@@ -444,7 +440,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     tmem_ld32(lane_addr + kColS1 + 32 * q, reinterpret_cast<uint32_t*>(x));
                     if (q < warp) {
                         // e^(G_i - G_j) = e^(G_i - G_e) e^(G_e - G_j), e the last of the 32 columns: neither factor is above 1
-                        const float f = p.scale * exp2f((gh - whole[32 * q + 31]) + (gl - rest[32 * q + 31]));
+                        const float f = p.scale * fast_exp2((gh - whole[32 * q + 31]) + (gl - rest[32 * q + 31]));
                         const uint64_t f2 = pack2(f, f);
                         tmem_wait_ld();
 #pragma unroll
@@ -479,11 +475,11 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             tmem_wait_st();
             tc_fence_before();
             mbar_arrive(bP);
-            const float e1 = p.scale * exp2f(gh + gl);
+            const float e1 = p.scale * fast_exp2(gh + gl);
             const uint64_t e2 = pack2(e1, e1);
             if (!__all_sync(0xffffffffu, mbar_wait(bO, b & 1u, abort_flag))) break;
             tc_fence_after();
-            const __nv_bfloat16* dst = p.out + (row0 + at + r) * p.o_token_stride + (int64_t)head * kD;
+            const __nv_bfloat16* dst = p.out + (row0 + walk.at + r) * p.o_token_stride + (int64_t)head * kD;
 #pragma unroll 1
             for (int q = 0; q < 4; ++q) {
                 float x[32], z[32];
@@ -503,7 +499,6 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 }
                 warp_store_rows64(gen + Smem::kOffStage + warp * 2048, lane, w, dst, r < len, q * 64);
             }
-            at += len;
         }
     }
 

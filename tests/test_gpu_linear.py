@@ -25,9 +25,10 @@ def test_chunks(layout, d, chunks, H, per_token):
 
 @pytest.mark.parametrize("layout", LAYOUTS)
 @pytest.mark.parametrize("chunks,prefix,interval", [([200, 70], [0, 33], 64), ([130], [5], 1), ([257, 1, 64], [100, 63, 64], 50), ([40], [7], 1000),
-                                                    ([600], [64], 128)])
-def test_snapshots(layout, chunks, prefix, interval):
-    w = Wave(chunks, 2, 64, seed=3, prefix=prefix, interval=interval, scale=0.25)
+                                                    ([600], [64], 128), ([300], [128], 100)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_snapshots(layout, chunks, prefix, interval, d):
+    w = Wave(chunks, 2, d, seed=3, prefix=prefix, interval=interval, scale=0.25)
     g = w.device()
     out = w.run(g, layout)
     w.check(out, g["pool"], w.reference())
@@ -45,8 +46,9 @@ def test_the_zero_state_and_slots_that_are_not_stored(layout, d):
 
 
 @pytest.mark.parametrize("layout", LAYOUTS)
-def test_a_state_in_place(layout):
-    w = Wave([150, 1], 3, 64, seed=5)
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_state_in_place(layout, d):
+    w = Wave([150, 1], 3, d, seed=5)
     w.state_out = w.state_in.copy()
     g = w.device()
     out = w.run(g, layout)
@@ -54,7 +56,8 @@ def test_a_state_in_place(layout):
 
 
 @pytest.mark.parametrize("layout", LAYOUTS)
-def test_decays_from_none_to_all(layout):
+@pytest.mark.parametrize("d", [64, 128])
+def test_decays_from_none_to_all(layout, d):
     """No decay at all, decays that leave nothing after a few tokens, and ones that forget at once."""
     rng = np.random.default_rng(6)
     decay = -np.exp(rng.uniform(-12, 4, (400, 4)))
@@ -63,25 +66,26 @@ def test_decays_from_none_to_all(layout):
     decay[rng.random((400, 4)) < 0.05] = -np.inf
     decay[rng.random((400, 4)) < 0.02] = -3e38
     decay[100:300, 2] = 0.0
-    w = Wave([270, 130], 4, 64, seed=7, decay=decay)
+    w = Wave([270, 130], 4, d, seed=7, decay=decay)
     g = w.device()
     out = w.run(g, layout)
     w.check(out, g["pool"], w.reference())
 
 
 @pytest.mark.parametrize("layout", LAYOUTS)
-def test_views_of_packed_buffers(layout):
-    w = Wave([70, 9], 3, 64, seed=8)
+@pytest.mark.parametrize("d", [64, 128])
+def test_views_of_packed_buffers(layout, d):
+    w = Wave([170, 9], 3, d, seed=8)
     g = w.device()
-    packed = torch.randn(w.T, 3 * 3 * 64 + 64, device="cuda").bfloat16()
-    views = [packed[:, i * 192:(i + 1) * 192].unflatten(1, (3, 64)) for i in range(3)]
+    packed = torch.randn(w.T, 3 * 3 * d + 64, device="cuda").bfloat16()
+    views = [packed[:, i * 3 * d:(i + 1) * 3 * d].unflatten(1, (3, d)) for i in range(3)]
     for x, n in zip(views, "qkv"):
         x.copy_(g[n])
         g[n] = x
     gates = torch.full((w.T, 8), 7.0, device="cuda")
     gates[:, 2:5] = g["decay"]
     g["decay"] = gates[:, 2:5]
-    wide = torch.full((w.T, 4, 64), 3.0, dtype=torch.bfloat16, device="cuda")
+    wide = torch.full((w.T, 4, d), 3.0, dtype=torch.bfloat16, device="cuda")
     out = w.run(g, layout, out=wide[:, :3])
     w.check(out, g["pool"], w.reference())
     assert bool((wide[:, 3] == 3.0).all())
@@ -104,9 +108,55 @@ def test_cut_chunks_end_where_whole_ones_do(layout):
     w.check(torch.cat(outs), pool, ref)
 
 
-def test_bad_slots_are_reported():
+@pytest.mark.parametrize("layout", (0, 2))
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("chunks,H,interval", [([3100], 1, 0), ([2000, 900, 0, 2300], 2, 0), ([2900, 1], 1, 700), ([1537, 2048], 3, 512)])
+def test_chains_in_segments(layout, d, chunks, H, interval):
+    """Few long chains: several segments of each, whose states before come from the segments before; the same slot in and out; a
+    first token that forgets in some segment; no workspace, which leaves whole chains."""
+    w = Wave(chunks, H, d, seed=sum(chunks), interval=interval, prefix=[5] * len(chunks))
+    w.state_out = w.state_in.copy()
+    w.decay[1200] = -np.inf
+    ref = w.reference()
+    assert wpp.wpp_linear_workspace_bytes(len(chunks), H, d, w.T) > 256
+    for kw in ({}, dict(workspace=None), dict(workspace=torch.empty(256, dtype=torch.uint8, device="cuda"))):
+        g = w.device()
+        out = w.run(g, layout, **kw)
+        assert int(g["status"].item()) == 0
+        w.check(out, g["pool"], ref)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_rows_of_others_never_count(d):
+    """A request of NaN between two others: blocks that end inside its rows read them, and nothing of them."""
+    w = Wave([100, 60, 150], 2, d, seed=15)
+    ref = w.reference()
+    for name in "qkv":
+        getattr(w, name)[100:160] = float("nan")
+    w.decay[100:160] = float("nan")
     for layout in LAYOUTS:
-        w = Wave([80, 5], 2, 64, seed=10, interval=64)
+        g = w.device()
+        out = w.run(g, layout)
+        o, size, pool = ref
+        keep = np.r_[0:100, 160:310]
+        assert np.all(np.abs(out.double().cpu().numpy()[keep] - o[keep]) <= 2.0 ** -8 * (np.abs(o[keep]) + size[keep]))
+        got = g["pool"].double().cpu().numpy()
+        for slot in (3, 5):
+            assert np.all(np.abs(got[slot] - pool[slot]) <= 2.0 ** -15 * np.abs(pool[slot]).max())
+
+
+def test_a_misaligned_workspace_is_refused():
+    w = Wave([3000], 1, 128, seed=16)
+    g = w.device()
+    with pytest.raises(wpp.WppError) as e:
+        w.run(g, workspace=torch.empty(w.workspace().numel() + 256, dtype=torch.uint8, device="cuda")[16:])
+    assert e.value.status == 1
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_bad_slots_are_reported(d):
+    for layout in LAYOUTS:
+        w = Wave([80, 5], 2, d, seed=10, interval=64)
         ref = w.reference()
         for name in ("state_in", "state_out", "snaps"):
             for bad in (-2, int(w.pool.shape[0]), 2 ** 31 - 1):

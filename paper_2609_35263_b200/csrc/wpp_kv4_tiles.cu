@@ -315,11 +315,12 @@ wpp_kv4_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         // what of a row's place does not change from key step to key step: the row in the tile, its page, its bytes in the block
         constexpr int kApart = 32 / R::kChunks;        // rows from one of the thread's rows to the next
         const int row0 = dw * 32 + rr, ppt = 128 >> page_shift;
-        int page_of[R::kRows], bytes_of[R::kRows], pair_of[R::kRows];
+        // (the thread's rows are in one group of 32 keys: one page, or two where pages have 16)
+        const int page_of[2] = {row0 >> page_shift, (row0 + 16) >> page_shift};
+        int bytes_of[R::kRows], pair_of[R::kRows];
 #pragma unroll
         for (int i = 0; i < R::kRows; ++i) {
             const int row = row0 + i * kApart, slot = row & (p.page_size - 1);
-            page_of[i] = row >> page_shift;
             bytes_of[i] = slot * (D / 2) + c * 16;
             pair_of[i] = p.page_size * (D / 2) + slot * 4;
         }
@@ -345,18 +346,29 @@ wpp_kv4_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             // the place of four tiles on: nobody is so far behind that it reads the one of four tiles ago, nor so far ahead
             if (r == 0) s_nan[(tiles + kNan / 2) % kNan] = 0x7fffffff;
             const int last_page = (v.kv_len - 1) >> page_shift;
+            // page ids are asked for an item before the rows they lead to, rows an item before their use
+            int page[2];
+            auto look_up = [&](int step) {
+                const int at = (v.kv_begin + step) * ppt;
+                page[0] = bt[min(at + page_of[0], last_page)];
+                if (p.page_size == 16) page[1] = bt[min(at + page_of[1], last_page)];
+            };
             auto fetch = [&](R& x, const uint8_t* pool, int step) {
                 const int step_at = v.kv_begin + step;
-                int page[R::kRows];
+                const uint8_t* block[2];
 #pragma unroll
-                for (int i = 0; i < R::kRows; ++i) page[i] = bt[min(step_at * ppt + page_of[i], last_page)];
+                for (int h = 0; h < 2; ++h) {
+                    if (h == 1 && p.page_size != 16) { block[1] = block[0]; break; }
+                    const bool there = (uint32_t)page[h] < (uint32_t)p.num_pages;
+                    bad |= !there;
+                    block[h] = pool + (there ? page[h] : 0) * p.page_bytes;
+                }
 #pragma unroll
                 for (int i = 0; i < R::kRows; ++i) {
-                    const bool there = (uint32_t)page[i] < (uint32_t)p.num_pages;
-                    bad |= !there;
-                    const uint8_t* block = pool + (there ? page[i] : 0) * p.page_bytes;
-                    x.x[i] = *reinterpret_cast<const uint4*>(block + bytes_of[i]);
-                    x.pair[i] = *reinterpret_cast<const uint32_t*>(block + pair_of[i]);
+                    const uint8_t* from = block[i * kApart / 16];
+                    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                 : "=r"(x.x[i].x), "=r"(x.x[i].y), "=r"(x.x[i].z), "=r"(x.x[i].w) : "l"(from + bytes_of[i]));
+                    asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(x.pair[i]) : "l"(from + pair_of[i]));
                 }
                 if ((step_at + 1) * 128 > v.kv_len) {  // what lies behind the sequence counts as zeros
 #pragma unroll
@@ -367,8 +379,10 @@ wpp_kv4_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             int nk = 0, nv = 0;                        // fetched so far
             auto next_is_k = [&]() { return nk < v.n_steps && nk <= nv + 1; };      // K(0) K(1) V(0) K(2) V(1) ...
             R cur, next;
+            look_up(0);
             fetch(cur, kc, 0);
             nk = 1;
+            look_up(next_is_k() ? nk : nv);
             bool cur_k = true;
             // ---- Q in the codes' order, and the sums of its rows (thread = row)
             if (!__all_sync(0xffffffffu, mbar_wait(bQFull, q_phase, abort_flag))) { dead = true; break; }
@@ -397,6 +411,7 @@ wpp_kv4_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     next_k = next_is_k();
                     fetch(next, next_k ? kc : vc, next_k ? nk : nv);
                     if (next_k) ++nk; else ++nv;
+                    if (nv < v.n_steps) look_up(next_is_k() ? nk : nv);
                 }
                 const uint32_t slot = cur_k ? ring_k.stage : ring_v.stage;
                 if (!__all_sync(0xffffffffu, mbar_wait((cur_k ? bKEmpty : bVEmpty) + 8 * slot, (cur_k ? ring_k.phase : ring_v.phase) ^ 1u, abort_flag))) {

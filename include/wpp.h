@@ -114,7 +114,8 @@ typedef struct {
 } wpp_batch_desc;
 
 /* Planner knobs; a zero field selects the library default.  (A description with WPP_KV4 has kernels of its own: of these fields
- * only force_kv_splits and max_ctas say something there.) */
+ * only force_kv_splits, max_ctas and shape say something there; shape 1: tiles of 256 query rows, 2: blocks of 16, 0: the library
+ * decides for every request.) */
 typedef struct {
     int32_t tile_m;           /* query rows per work tile: 128 or 256 (default 256: two 128-row halves) */
     int32_t tile_n;           /* keys per inner step: 128 */

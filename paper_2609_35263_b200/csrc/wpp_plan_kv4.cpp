@@ -1,5 +1,6 @@
 // Work split of a wave over a cache held in 4 bits (part of wpp_plan_tiles; integer arithmetic only).
 #include <algorithm>
+#include <cstdint>
 #include <cstring>
 #include <vector>
 
@@ -13,8 +14,13 @@ static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // steps; and the fewest steps that a block is cut for.
 constexpr int kFewCtas = 3, kFewCtasWide = 2;
 constexpr int64_t kUnitSteps = 3, kLeastSteps = 2;
-// A chunk is the tile kernel's if the kernel for few rows would walk its keys more often than this.
-constexpr int64_t kFewWalks = 2;
+// A chunk is the kernel for few rows' if that walks its keys no more often than kFewWalks times.  But each kernel of a wave has its own
+// start and end, and the tile kernel's are the longer ones: a wave that is kFewAll steps per SM in all on the former (units with
+// what they cost besides) is all its, and where there are tiles anyway, so little work of few rows goes to them.  Attention call
+// in a graph, us, tiles | few rows: 1 x 64 tokens over 1,024 (8/2 heads of 64) 22 | 9.7, 8 x 64 over 256 14.5 | 8.3, 1 x 128 over
+// 256 (32/8) 17.9 | 11.3, 1 x 32 over 2,000 21 | 17.6; beyond kFewAll 1 x 16 over 8,192 (64/8) 27 | 31, 4 x 64 over 300 19 | 39;
+// within kFewWalks 64 x 5 over 1,000 (32/8) 102 | 65; 12 x 1..300 over 0..700 (8/2), all tiles 24, both kernels 30.
+constexpr int64_t kFewWalks = 2, kFewAll = 12;
 // Tiles: fewest key steps of a part, and rounds of tiles up to which the longest come first.
 constexpr int32_t kTileLeastSteps = 4;
 constexpr int64_t kTileOrderRounds = 16;
@@ -23,15 +29,25 @@ constexpr int64_t kTileOrderRounds = 16;
 static int32_t few_heads(int32_t group) { return std::min<int32_t>(group, WPP_FEW_ROWS); }
 static int32_t few_tokens(int32_t group) { return std::max<int32_t>(1, WPP_FEW_ROWS / few_heads(group)); }
 
-static bool is_few(const wpp_batch_desc* d, int64_t C) {
-    const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
-    return (C + t - 1) / t * ((G + h - 1) / h) <= kFewWalks;
-}
-
 static int64_t few_blocks(const wpp_batch_desc* d, int64_t C) {
     const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
     return (C + t - 1) / t * ((G + h - 1) / h) * d->num_kv_heads;
 }
+
+// How often the kernel for few rows may walk a chunk's keys, in this wave: kFewWalks, 0 (tiles alone) or any number.
+static int64_t few_walks(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t* prefix_lens, const int32_t* chunk_lens) {
+    if (o->shape) return o->shape == 1 ? 0 : INT64_MAX;
+    int64_t all = 0, few = 0;
+    for (int i = 0; i < d->num_requests; ++i) {
+        const int64_t C = chunk_lens[i], n = few_blocks(d, C), walks = n / d->num_kv_heads;
+        const int64_t cost = n * (((int64_t)prefix_lens[i] + C + WPP_TILE_N - 1) / WPP_TILE_N + kUnitSteps);
+        all += cost;
+        if (walks <= kFewWalks) few += cost;
+    }
+    if (all <= kFewAll * o->max_ctas) return INT64_MAX;
+    return few < all && few <= kFewAll * o->max_ctas ? 0 : kFewWalks;
+}
+static bool is_few(const wpp_batch_desc* d, int64_t C, int64_t walks) { return few_blocks(d, C) / d->num_kv_heads <= walks; }
 
 size_t wpp_kv4_plan_bytes(const wpp_batch_desc* d, const wpp_plan_opts* o, int64_t T) {
     const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
@@ -53,11 +69,12 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     auto steps_for = [](int64_t keys) { return (int32_t)((keys + WPP_TILE_N - 1) / WPP_TILE_N); };
 
     const int32_t heads = few_heads(G), toks = few_tokens(G);
+    const int64_t walks = few_walks(d, o, prefix_lens, chunk_lens);
     // The CTAs take equal shares of the blocks' key steps, in order: a block is cut where a share ends.
     int64_t n_base = 0, all_steps = 0;
     int32_t max_rows = 0;
     for (int i = 0; i < R; ++i) {
-        if (!is_few(d, chunk_lens[i])) continue;
+        if (!is_few(d, chunk_lens[i], walks)) continue;
         n_base += few_blocks(d, chunk_lens[i]);
         for (int64_t r0 = 0; r0 < chunk_lens[i]; r0 += toks) {
             const int32_t rows = (int32_t)std::min<int64_t>(toks, chunk_lens[i] - r0);
@@ -89,7 +106,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     std::vector<int32_t> cuts;
     for (int i = 0; i < R; ++i) {
         const int64_t P = prefix_lens[i], C = chunk_lens[i];
-        if (!is_few(d, C)) continue;
+        if (!is_few(d, C, walks)) continue;
         for (int64_t r0 = 0; r0 < C; r0 += toks) {
             const int32_t rows = (int32_t)std::min<int64_t>(toks, C - r0), steps = steps_for(P + r0 + rows);
             for (int32_t kvh = 0; kvh < Hkv; ++kvh) {
@@ -158,7 +175,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     std::vector<Tile> tiles;
     for (int i = 0; i < R; ++i) {
         const int64_t P = prefix_lens[i], C = chunk_lens[i];
-        if (is_few(d, C)) continue;
+        if (is_few(d, C, walks)) continue;
         const int32_t block = G % 2 == 0 ? WPP_HALF_M : 2 * WPP_HALF_M;
         for (int64_t r0 = 0; r0 < C; r0 += block) {
             const int32_t rows = (int32_t)std::min<int64_t>(block, C - r0);

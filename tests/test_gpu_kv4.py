@@ -63,10 +63,11 @@ HEADS = [(64, 8, 128, 64), (8, 2, 64, 16), (40, 8, 128, 32), (6, 2, 128, 128), (
 @pytest.mark.parametrize("Hq,Hkv,d,B", HEADS)
 @pytest.mark.parametrize("P,C", [([0, 15, 16, 300], [1, 1, 1, 1]), ([0, 127, 129, 61], [2, 2, 4, 3]), ([0, 70, 0, 33], [7, 17, 40, 0])])
 @pytest.mark.parametrize("splits", [0, 1, 3])
-def test_attention_of_few_rows(Hq, Hkv, d, B, P, C, splits):
+@pytest.mark.parametrize("shape", [1, 2])
+def test_attention_of_few_rows(Hq, Hkv, d, B, P, C, splits, shape):
     w = Wave(P, C, Hq, Hkv, d, B, seed=Hq + d)
     g = w.device()
-    out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0))
+    out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
     assert int(g["status"].item()) == 0
     w.check(out, lse, w.reference())
 
@@ -74,15 +75,16 @@ def test_attention_of_few_rows(Hq, Hkv, d, B, P, C, splits):
 @pytest.mark.parametrize("Hq,Hkv,d,B", HEADS)
 @pytest.mark.parametrize("P,C", [([0, 200], [129, 60]), ([77, 0, 5], [64, 257, 33])])
 @pytest.mark.parametrize("splits", [0, 1, 2])
-def test_attention_of_chunks(Hq, Hkv, d, B, P, C, splits):
+@pytest.mark.parametrize("shape", [1, 2])
+def test_attention_of_chunks(Hq, Hkv, d, B, P, C, splits, shape):
     w = Wave(P, C, Hq, Hkv, d, B, seed=Hq + d + 1)
     g = w.device()
-    out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0))
+    out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
     assert int(g["status"].item()) == 0
     w.check(out, lse, w.reference())
 
 
-@pytest.mark.parametrize("C", [[1, 1], [2, 200]])
+@pytest.mark.parametrize("C", [[1, 1], [2, 200], [2, 1200]])
 def test_append_then_attention(C):
     """As a stage calls them: the new rows into the pages, then attention over all of them, one plan for both."""
     w = Wave([130, 61], C, 16, 4, 128, 32, seed=11)
@@ -96,7 +98,8 @@ def test_append_then_attention(C):
 
 
 @pytest.mark.parametrize("P,C", [([100, 3], [1, 1]), ([100, 3, 0], [2, 150, 40])])
-def test_what_lies_behind_a_sequence_never_counts(P, C):
+@pytest.mark.parametrize("shape", [1, 2])
+def test_what_lies_behind_a_sequence_never_counts(P, C, shape):
     """Slots behind the last row and pages nobody names hold all ones: NaN pairs."""
     w = Wave(P, C, 8, 2, 128, 64, seed=12)
     used = np.zeros((w.pages, w.B), bool)
@@ -110,25 +113,28 @@ def test_what_lies_behind_a_sequence_never_counts(P, C):
         pool[..., :w.B * 64], pool[..., w.B * 64:] = codes.reshape(w.pages, 2, -1), pairs.reshape(w.pages, 2, -1)
     g = w.device()
     for splits in (1, 2):
-        out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0))
+        out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
         w.check(out, lse, w.reference())
 
 
 @pytest.mark.parametrize("which", ["k", "v"])
 @pytest.mark.parametrize("C", [4, 150])
-def test_a_nan_row_reaches_the_rows_that_see_it_and_no_others(which, C):
+@pytest.mark.parametrize("shape", [1, 2])
+@pytest.mark.parametrize("splits", [1, 2])
+def test_a_nan_row_reaches_the_rows_that_see_it_and_no_others(which, C, shape, splits):
     w = Wave([90], [C], 8, 2, 128, 32, seed=13)
     hurt = 90 + C // 2
     pool = w.k_pool if which == "k" else w.v_pool
     okv4.write_row(pool, w.table[0, hurt // w.B], 1, hurt % w.B, w.B, np.zeros(w.d, np.uint8), np.array([0x7FC0, 0], np.uint16))
     g = w.device()
-    out, _ = w.attend(g)
+    out, _ = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
     o = out.float().cpu().numpy()
     assert not np.isnan(o[:, :4]).any() and not np.isnan(o[:C // 2]).any() and np.isnan(o[C // 2:, 4:]).all()
 
 
 @pytest.mark.parametrize("C", [1, 100])
-def test_scores_that_keep_growing(C):
+@pytest.mark.parametrize("shape", [1, 2])
+def test_scores_that_keep_growing(C, shape):
     """Keys that get longer along the sequence: the references move all the time."""
     w = Wave([500], [C], 8, 2, 128, 64, seed=14, sm_scale=0.3)
     codes, pairs = okv4.pack_rows(okv4.bf16_bits((np.random.default_rng(1).standard_normal((500 + C, 2, 128))
@@ -137,12 +143,13 @@ def test_scores_that_keep_growing(C):
         for h in range(2):
             okv4.write_row(w.k_pool, w.table[0, j // 64], h, j % 64, 64, codes[j, h], pairs[j, h])
     g = w.device()
-    out, lse = w.attend(g)
+    out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, 0, 0, 0, shape))
     w.check(out, lse, w.reference())
 
 
 @pytest.mark.parametrize("C", [1, 90])
-def test_strides(C):
+@pytest.mark.parametrize("shape", [1, 2])
+def test_strides(C, shape):
     """K and V blocks side by side in one allocation, queries and new rows out of one packed buffer, outputs inside a larger one."""
     w = Wave([40, 7], [C, 2], 8, 2, 64, 16, seed=15)
     block = wpp.wpp_kv4_block_bytes(16, 64)
@@ -153,7 +160,7 @@ def test_strides(C):
     packed[:, :8, :64], packed[:, 8:10, :64], packed[:, 10:12, :64] = g["q"], g["k_new"], g["v_new"]
     kw = dict(kv_page_stride=6 * block, kv_head_stride=3 * block, q_token_stride=16 * 72, q_head_stride=72, kvnew_token_stride=16 * 72,
               kvnew_head_stride=72, o_token_stride=10 * 80, o_head_stride=80)
-    desc, plan = w.desc(**kw), w.plan(**kw)
+    desc, plan = w.desc(**kw), w.plan(wpp.PlanOpts(0, 0, 0, 0, 0, shape), **kw)
     wpp.wpp_kv_append(ctx(), desc, packed[:, 8:], packed[:, 10:], both, both[:, :, 2], g["table"], g["P"], g["C"], plan, status=g["status"])
     out = torch.full((w.T, 10, 80), 5.0, dtype=torch.bfloat16, device="cuda")
     ws = torch.empty(int(plan.info.workspace_bytes), dtype=torch.uint8, device="cuda")
@@ -168,7 +175,8 @@ def test_strides(C):
     assert (rest == 5.0).all() and int(g["status"].item()) == 0
 
 
-def test_offsets_beyond_32_bits():
+@pytest.mark.parametrize("shape", [1, 2])
+def test_offsets_beyond_32_bits(shape):
     """Pages 2^28 bytes apart: the pool's end lies behind 2^32 bytes."""
     w = Wave([150, 70], [1, 65], 8, 1, 128, 16, seed=16)
     g = w.device()
@@ -178,7 +186,7 @@ def test_offsets_beyond_32_bits():
     big[:, :n], big[:, n:2 * n] = g["k"][:, 0], g["v"][:, 0]
     assert w.pages * stride > 1 << 32
     kw = dict(kv_page_stride=stride)
-    desc, plan = w.desc(**kw), w.plan(**kw)
+    desc, plan = w.desc(**kw), w.plan(wpp.PlanOpts(0, 0, 0, 0, 0, shape), **kw)
     v = big.view(-1)[n:]
     out = torch.empty(w.T, 8, 128, dtype=torch.bfloat16, device="cuda")
     ws = torch.empty(int(plan.info.workspace_bytes), dtype=torch.uint8, device="cuda")
@@ -190,11 +198,12 @@ def test_offsets_beyond_32_bits():
 
 
 # ---------------------------------------------------------------------------------------------- refusals, streams, capture
-def test_other_lengths_than_the_plans_are_refused_per_request():
+@pytest.mark.parametrize("shape", [1, 2])
+def test_other_lengths_than_the_plans_are_refused_per_request(shape):
     w = Wave([50, 20, 30], [1, 100, 2], 8, 2, 128, 32, seed=17)
     good = w.reference()
     g = w.device()
-    plan = w.plan(wpp.PlanOpts(0, 0, 2, 0))
+    plan = w.plan(wpp.PlanOpts(0, 0, 2, 0, 0, shape))
     for name, i in (("P", 0), ("C", 1)):
         h = dict(g, status=torch.zeros_like(g["status"]), k=g["k"].clone(), v=g["v"].clone())
         h[name] = g[name].clone()
@@ -213,13 +222,14 @@ def test_other_lengths_than_the_plans_are_refused_per_request():
             assert np.array_equal(h["k"].cpu().numpy()[pages], (w.k_pool if j == i else k)[pages])
 
 
-def test_a_bad_page_id_is_reported():
+@pytest.mark.parametrize("shape", [1, 2])
+def test_a_bad_page_id_is_reported(shape):
     for C in ([1], [140]):
         w = Wave([100], C, 8, 2, 64, 32, seed=18)
         for bad in (-1, w.pages, 2 ** 31 - 1):
             g = w.device()
             g["table"][0, 1] = bad
-            w.attend(g)
+            w.attend(g, opts=wpp.PlanOpts(0, 0, 0, 0, 0, shape))
             assert int(g["status"].item()) == 3
             g["status"].zero_()
             g["table"][0, 1] = int(w.table[0, 1])
@@ -263,10 +273,11 @@ def test_the_built_in_scratch():
     assert torch.equal(out, again) and torch.equal(lse, sums)
 
 
-@pytest.mark.parametrize("C", [[1, 1, 1], [1, 40, 150]])
-def test_captured_and_replayed_and_on_two_streams(C):
+@pytest.mark.parametrize("C", [[1, 1, 1], [1, 40, 150], [1, 40, 950]])
+@pytest.mark.parametrize("shape", [0, 1])
+def test_captured_and_replayed_and_on_two_streams(C, shape):
     w = Wave([300, 64, 0], C, 16, 4, 128, 64, seed=21)
-    g, plan = w.device(), w.plan(wpp.PlanOpts(0, 0, 2, 0))
+    g, plan = w.device(), w.plan(wpp.PlanOpts(0, 0, 2, 0, 0, shape))
     out, lse = w.attend(g, plan)
     ws = [torch.full((int(plan.info.workspace_bytes),), 255, dtype=torch.uint8, device="cuda") for _ in range(2)]
     outs = [torch.empty_like(out) for _ in range(2)]

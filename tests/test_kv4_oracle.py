@@ -105,12 +105,13 @@ def test_plans_of_the_two_kinds_of_cache_are_not_exchanged():
 
 @pytest.mark.parametrize("d,Hq,Hkv", [(128, 64, 8), (64, 8, 8), (128, 40, 8), (128, 32, 1), (64, 20, 1), (128, 6, 2)])
 @pytest.mark.parametrize("splits", [0, 1, 3, 64])
-def test_plans_cover_every_visible_pair_once(d, Hq, Hkv, splits):
-    P, C = [0, 700, 5000, 64, 0, 131], [5, 1, 2, 0, 300, 129]
+@pytest.mark.parametrize("shape", [0, 1, 2])
+@pytest.mark.parametrize("P,C", [([0, 700, 5000, 64, 0, 131], [5, 1, 2, 0, 300, 129]), ([3, 9000], [700, 1]), ([20], [2])])
+def test_plans_cover_every_visible_pair_once(d, Hq, Hkv, splits, shape, P, C):
     desc = wpp.make_desc(len(P), Hq, Hkv, d, 32, 400, 999, dtype=wpp.WPP_KV4)
-    plan = wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, splits, 0), pin=False)
+    plan = wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape), pin=False)
     raw = plan.host.numpy()[:plan.plan_bytes]
-    assert np.array_equal(raw, wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, splits, 0), pin=False).host.numpy()[:plan.plan_bytes])
+    assert np.array_equal(raw, wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape), pin=False).host.numpy()[:plan.plan_bytes])
     check_cover(raw, P, C, Hq, Hkv)
 
 

@@ -488,7 +488,7 @@ typedef struct {
     int32_t num_slots;      /* slots of state_pool, each H * head_dim * head_dim floats */
     int32_t snap_interval;  /* > 0: snapshot whenever the tokens folded into S reach a multiple of it; 0: none */
     int32_t max_snaps;      /* row length of snap_slots (0 when snap_interval is 0) */
-    int32_t layout;         /* 0: the library chooses by the tokens per request; 1: token by token, fp32 on CUDA cores; 2: in blocks of
+    int32_t layout;         /* 0: the library chooses by the tokens per request, for every request by itself where there are many chains; 1: token by token, fp32 on CUDA cores; 2: in blocks of
                              * 64 or 128 tokens on the tensor cores (products of bf16 numbers, the state's terms held in two of them,
                              * fp32 sums).  The last bits of 0 and 2 depend on the wave (where chains are cut) */
     float scale;            /* of the outputs; 0 selects 1 */

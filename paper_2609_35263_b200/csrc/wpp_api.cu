@@ -7,6 +7,7 @@
 #include <stdlib.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 #include <new>
 
@@ -1022,41 +1023,68 @@ static bool linear_desc_ok(const wpp_linear_desc* d) {
            d->v_token_stride >= 0 && d->o_token_stride >= 0 && d->decay_token_stride >= 0;
 }
 
-// How the forms in blocks cut their chains: into so many segments of equal length that the estimated time is least.  On 148 SMs; a
-// block's time in the second pass and in the first, which leaves the segments' states, and what a CTA takes besides, us.
-//                              tokens a block   CTAs per SM   second    first   start
+// The forms in blocks, on 148 SMs: tokens of a block, CTAs per SM, and for how chains are cut a block's time in the second pass and in the
+// first, which leaves the segments' states, and what a CTA takes besides (in proportion to one another).
 struct LinearForm { double tokens, ctas, second, first, start; };
 constexpr LinearForm kLinForms[2] = {{64, 2, 4.0, 2.0, 5.0},         // products of 16 x 8 x 16
                                      {128, 1, 2.4, 1.4, 6.0}};       // tensor memory (heads of 128)
+constexpr double kLinSms = 148.0;
+// Whole chains, cut by the mean length into segments of at least kLinLeast tokens: 1 x 32,768 of 16 heads of 128 864 us | 209, 2 x 8,192
+// 226 | 125, 1 x 4,096 of 32 heads 117 | 75; within 1 % of the best of 1 to 32 segments in thirteen waves of 1 to 32,768 tokens.
 constexpr int64_t kLinLeast = 256, kLinMostSegments = 32;
-constexpr int64_t kLinTokenForm = 8;       // tokens per request on average from which blocks are taken
-constexpr int64_t kLinTcTokens = 48;       // ... and from which those of 128 are
+// Tokens per request on average from which blocks are taken.  Token by token | in blocks, us: 32 heads of 128, 8 requests 8 tokens
+// 15.9 | 18.4, 12 tokens 21.8 | 18.4, 64 requests 12 tokens 134 | 143, 16 tokens 167 | 143; 16 heads of 64, 64 requests 12 tokens 20.9 | 26.7.
+constexpr int64_t kLinTokenForm = 12;
+// ... and from which those of 128 are, once one of the others is not enough.  Blocks of 64 | of 128, 8 requests of 32 heads: 64 tokens
+// 20.3 | 25.2, 96 tokens 30.5 | 25.6; 64 requests 153 | 198 and 223 | 200.
+constexpr int64_t kLinTcTokens = 65;
+// The host knows the mean alone.  With more chains than kLinMixedRounds per SM a wave may be a few long chunks among single tokens, and
+// is taken for that: short chunks go token by token in a launch of their own, the others in the largest blocks, in segments of
+// kLinMixedShare times an SM's tokens, longer than equal chunks could be.  By the mean | so, 32 heads of 128: 62 requests of 1
+// token and 2 of 2,048 466 | 159, 63 and one of 8,192 440 | 218; 62 and 2 of 8,192, 16 heads of 64, 492 | 128.  If they are equal
+// after all, 32 x 2,048 (32 heads of 128) 561 | 576 whole, 64 x 256 (of 64) 140 | 141, but 64 x 32 147 | 198 for the larger blocks.
+// From kLinMixedTokens on average: 126 requests of 1 token and 2 of 512, 32 heads of 128, all token by token 689 | 161, of 64 443 | 74,
+// 63 and one of 300, of 128, 351 | 102; if all have 5, 77 | 113, where the CTAs that find nothing to do are the difference.
+constexpr double kLinMixedRounds = 2.0, kLinMixedShare = 1.2;
+constexpr int64_t kLinMixedTokens = 5;
+static bool linear_mixed(const wpp_linear_desc* d) {
+    return d->total_tokens >= kLinMixedTokens * (int64_t)d->num_requests && (double)d->num_requests * d->num_heads > kLinMixedRounds * kLinSms;
+}
 static bool linear_uses_tc(const wpp_linear_desc* d) {
-    return d->head_dim == 128 && d->total_tokens >= kLinTcTokens * (int64_t)d->num_requests && d->total_tokens <= 0x7fffffffll;
+    if (d->head_dim != 128 || d->total_tokens > 0x7fffffffll) return false;
+    return linear_mixed(d) || d->total_tokens >= kLinTcTokens * (int64_t)d->num_requests;
 }
 struct LinearSegments {
-    int64_t tokens, count;          // of a segment; of all chains of a head, at most
+    int64_t tokens, count, first;   // of a segment; of all chains of a head, at most, and of those in the first pass
     bool two_passes;
     size_t off_log, bytes;          // of the workspace: states, logarithms of decays
 };
 static LinearSegments linear_segments(const wpp_linear_desc* d, bool tc) {
     LinearSegments g;
     const LinearForm& f = kLinForms[tc ? 1 : 0];
-    const double chains = (double)d->num_requests * d->num_heads, slots = 148.0 * f.ctas;
+    const double chains = (double)d->num_requests * d->num_heads, slots = kLinSms * f.ctas;
     const int64_t mean = d->num_requests > 0 ? (d->total_tokens + d->num_requests - 1) / d->num_requests : 0;
-    int64_t best = 1;
-    double best_us = 0.0;
-    for (int64_t s = 1; s <= kLinMostSegments && (s == 1 || mean >= kLinLeast * s); ++s) {
-        const double blocks = ceil((double)mean / (double)s / f.tokens);
-        double us = ceil(chains * (double)s / slots) * (blocks * f.second + f.start);
-        if (s > 1) us += ceil(chains * (double)(s - 1) / slots) * (blocks * f.first + f.start);
-        if (s == 1 || us < 0.97 * best_us) { best = s; best_us = us; }
+    auto whole_blocks = [&](double t) { return (int64_t)(ceil(fmin(t, 1e12) / f.tokens) * f.tokens); };
+    if (linear_mixed(d)) {
+        g.tokens = std::max(whole_blocks(kLinMixedShare * (double)d->total_tokens * d->num_heads / slots), 2 * kLinLeast);
+        g.two_passes = d->total_tokens > g.tokens;
+    } else {
+        int64_t best = 1;
+        double best_us = 0.0;
+        for (int64_t s = 1; s <= kLinMostSegments && (s == 1 || mean >= kLinLeast * s); ++s) {
+            const double blocks = ceil((double)mean / (double)s / f.tokens);
+            double us = ceil(chains * (double)s / slots) * (blocks * f.second + f.start);
+            if (s > 1) us += ceil(chains * (double)(s - 1) / slots) * (blocks * f.first + f.start);
+            if (s == 1 || us < 0.97 * best_us) { best = s; best_us = us; }
+        }
+        g.two_passes = best > 1;
+        g.tokens = whole_blocks((double)((mean + best - 1) / best));
     }
-    g.two_passes = best > 1;
-    g.tokens = best > 1 ? ((mean + best - 1) / best + (int64_t)f.tokens - 1) / (int64_t)f.tokens * (int64_t)f.tokens : (int64_t)1 << 40;
-    g.count = d->total_tokens / g.tokens + d->num_requests;
-    g.off_log = (size_t)g.count * d->num_heads * d->head_dim * d->head_dim * sizeof(float);
-    g.bytes = g.off_log + (size_t)g.count * d->num_heads * sizeof(float);
+    if (!g.two_passes) g.tokens = (int64_t)1 << 40;
+    g.first = d->total_tokens / g.tokens;
+    g.count = g.first + d->num_requests;
+    g.off_log = 2 * (size_t)g.first * d->num_heads * d->head_dim * d->head_dim * sizeof(float);
+    g.bytes = g.off_log + (size_t)g.first * d->num_heads * sizeof(float);
     return g;
 }
 
@@ -1110,12 +1138,13 @@ extern "C" int wpp_linear_chunk(const wpp_ctx* ctx, const wpp_linear_desc* desc,
     p.snap_interval = desc->snap_interval;
     p.max_snaps = desc->max_snaps;
     p.scale = desc->scale != 0.f ? desc->scale : 1.f;
-    // token by token where chunks are so short that a block would be mostly empty
-    if (desc->layout == 1 || (desc->layout == 0 && desc->total_tokens < kLinTokenForm * (int64_t)desc->num_requests)) {
+    const bool mixed = desc->layout == 0 && linear_mixed(desc);
+    p.few_tokens = mixed ? (int32_t)kLinTokenForm - 1 : -1;
+    if (mixed || desc->layout == 1 || (desc->layout == 0 && desc->total_tokens < kLinTokenForm * (int64_t)desc->num_requests)) {
         const int e = wpp_launch_linear_token(&p, desc->head_dim, ctx->sm_count, cuda_stream);
         if (e != 0) return cuda_fail(ctx, e);
         const_cast<wpp_ctx*>(ctx)->launches += 1;
-        return WPP_OK;
+        if (!mixed) return WPP_OK;
     }
     const bool tc = linear_uses_tc(desc);
     LinearSegments g = linear_segments(desc, tc);
@@ -1124,11 +1153,13 @@ extern "C" int wpp_linear_chunk(const wpp_ctx* ctx, const wpp_linear_desc* desc,
         if (!workspace || workspace_bytes < g.bytes) {                 // whole chains need none
             g.two_passes = false;
             g.tokens = (int64_t)1 << 40;
+            g.first = 0;
             g.count = desc->num_requests;
         }
     }
     if (g.count > 0x7fffffff) return WPP_ERR_UNSUPPORTED;
     p.seg_tokens = g.tokens;
+    p.ws_segments = g.first;
     p.ws_state = static_cast<float*>(workspace);
     p.ws_log = reinterpret_cast<float*>(static_cast<char*>(workspace) + g.off_log);
     int e;

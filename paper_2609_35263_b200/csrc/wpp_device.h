@@ -147,12 +147,14 @@ struct LinearParams {
     int64_t q_token_stride, k_token_stride, v_token_stride, o_token_stride, decay_token_stride;      // in elements
     int32_t num_requests, num_heads, num_slots, snap_interval, max_snaps;
     float scale;
+    int32_t few_tokens;              // chunks of at most so many are the token form's, the others the blocks' (-1: one form has all)
 };
 
 struct LinearChunkParams : LinearParams {
-    int64_t seg_tokens;              // tokens of a chain's segments
-    float* ws_state;                 // [segments][H][d * d]
-    float* ws_log;                   // [segments][H], base 2
+    int64_t seg_tokens;              // tokens of a chain's segments; its first is number row_offsets[r] / seg_tokens in the workspace
+    int64_t ws_segments;             // segments that the first pass may have
+    float* ws_state;                 // [2 ws_segments][H][d * d]: their own states; where a chain's first one is, the chain's state before
+    float* ws_log;                   // [ws_segments][H], base 2
 };
 
 // Chunk-parallel (tensor-core) form of the recurrent layer: the inputs of KdaParams plus the workspace arrays the

@@ -3,7 +3,8 @@
 // One CTA has kCols columns of a (request, head)'s state in registers: kCols / 4 lanes hold a row's columns, four each, the CTA's 256
 // threads rows kRowsAtOnce apart.  For a chunk of one token the state's bytes bound it, read once and written once; all of a
 // thread's rows are asked for before the first is used.  Outputs are sums over the rows, of a lane's own first, then over the
-// threads with the same columns by shuffles and shared memory.
+// threads with the same columns by shuffles and shared memory.  64 requests of one token, 32 heads of 128: 49 us, 5.4 TB/s (83 % of the
+// measured copy); with fewer than two chains per SM a CTA takes 32 columns, for the latency.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>
@@ -32,6 +33,7 @@ __global__ void __launch_bounds__(kLinThreads) wpp_linear_token_kernel(const Lin
     const int slices = D / kCols, head = blockIdx.x / slices, col = blockIdx.x % slices * kCols + threadIdx.x % kLanes * 4;
     const int req = blockIdx.y, row0 = threadIdx.x / kLanes, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int64_t first = p.row_offsets[req], n = p.row_offsets[req + 1] - first;
+    if (p.few_tokens >= 0 && n > p.few_tokens) return;
     const int64_t in = linear_slot(p, p.state_in[req]), out = linear_slot(p, p.state_out[req]);
     const int64_t state = ((int64_t)head * D + row0) * D + col, slot_size = (int64_t)p.num_heads * D * D;
     float4 s[kRows];

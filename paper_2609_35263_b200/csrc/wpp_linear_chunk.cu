@@ -10,7 +10,9 @@
 // to bf16, P and S are rounded to bf16 once.
 //
 // What bounds it are the products (1,856 of 16 x 8 x 16 for 64 tokens at 128 columns, half a one per clock: 58 clocks a token where
-// the memory needs 44).  The sums G are made in 64 bits and kept as a multiple of 1/64 and a rest, so that differences of long
+// the memory needs 44; heads of 128 come here with few chains of short chunks only, see kLinTcTokens, the others to
+// wpp_linear_tc.cu: 8 x 2,048 tokens of 32 heads 365 us | 134 there).  Heads of 64: 8 x 2,048 of 32 heads 131 us, half the bytes
+// and a quarter of the products.  The sums G are made in 64 bits and kept as a multiple of 1/64 and a rest, so that differences of long
 // sums are exact to fp32.  A logarithm below -256 (base 2) is taken for that: it leaves nothing of an fp32 state.
 //
 // Few long chains are cut into segments (`seg_tokens`): a first pass leaves every segment's own state but the last one's, starting
@@ -77,24 +79,24 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
     grid_launch_dependents();
     grid_dependency_wait();
 
-    // ---- which request and segment: request r's segments are numbered from row_offsets[r] / seg_tokens + r on
+    // ---- which request and segment: request r's are numbered from row_offsets[r] / seg_tokens + r on; in the first
+    //      pass, where all but the last ones of a chain count, from row_offsets[r] / seg_tokens on
     const int head = blockIdx.y;
     const int64_t index = blockIdx.x;
     int req = 0, hi = p.num_requests;
     while (hi - req > 1) {
         const int width = (hi - req + 31) / 32, i = req + lane * width;
-        const unsigned le = __ballot_sync(0xffffffffu, i < hi && p.row_offsets[i] / p.seg_tokens + i <= index) | 1u;
+        const unsigned le = __ballot_sync(0xffffffffu, i < hi && p.row_offsets[i] / p.seg_tokens + (kFirst ? 0 : i) <= index) | 1u;
         const int last = 31 - __clz((int)le);
         hi = min(hi, req + (last + 1) * width);
         req += last * width;
     }
     const int64_t row0 = p.row_offsets[req], n = p.row_offsets[req + 1] - row0;
-    const int64_t seg = index - (row0 / p.seg_tokens + req), segs = n > 0 ? (n + p.seg_tokens - 1) / p.seg_tokens : 1;
-    if (seg >= segs || (kFirst && seg == segs - 1)) return;            // (a last segment's own state is nobody's state before)
+    const int64_t index0 = row0 / p.seg_tokens, seg = index - index0 - (kFirst ? 0 : req), segs = n > 0 ? (n + p.seg_tokens - 1) / p.seg_tokens : 1;
+    if (n <= p.few_tokens || seg >= segs || (kFirst && seg == segs - 1)) return;            // (a last segment's own state is nobody's state before)
     const int64_t begin = seg * p.seg_tokens, end = min(n, begin + p.seg_tokens);
 
-    // ---- the state before the segment.  Workspace: segment `index` of head h has its own state at ws_state, thread by thread, the chain's
-    //      first state stands where its last segment's would, and its decay's logarithm at ws_log.
+    // ---- the state before the segment.  Workspace: a segment's own state is at ws_state, thread by thread.
     float s[kN][4];                                    // S^T: rows (columns of S) 16 warp + g, + 8; columns 8 nt + 2 t, + 1
     const int64_t slot_size = (int64_t)p.num_heads * D * D;
     const int64_t mine = (int64_t)head * D * D + (int64_t)(2 * t) * D + 16 * warp + g;     // of S[2 t][16 warp + g]
@@ -117,7 +119,6 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
             at[(8 * nt + 1) * D + 8] = s[nt][3];
         }
     };
-    const int64_t index0 = index - seg;                // of the chain's first segment
     if (seg == 0 && (kFirst || segs == 1)) {
         const int64_t in = lin_slot(p, p.state_in[req]);
         const float* at = p.state_pool + in * slot_size + mine;
@@ -128,14 +129,14 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
             s[nt][2] = in >= 0 ? at[(8 * nt) * D + 8] : 0.f;
             s[nt][3] = in >= 0 ? at[(8 * nt + 1) * D + 8] : 0.f;
         }
-        if (kFirst) ws_store(index0 + segs - 1);       // (state_out may be the same slot, and its last segment done first)
+        if (kFirst) ws_store(p.ws_segments + index0);       // (state_out may be the same slot, and its last segment done first)
     } else if (kFirst) {
 #pragma unroll
         for (int nt = 0; nt < kN; ++nt)
 #pragma unroll
             for (int i = 0; i < 4; ++i) s[nt][i] = 0.f;
     } else if (seg == 0) {
-        ws_load(index0 + segs - 1, s);
+        ws_load(p.ws_segments + index0, s);
     } else {
         ws_load(index0, s);
         for (int64_t i = 1; i < seg; ++i) {
@@ -264,8 +265,7 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
         for (int ks = 0; ks < 4; ++ks)
             ldsm_4_trans(v[ks], tile_at(sv, 16 * ks + (lane & 7) + ((lane >> 4) << 3), 2 * warp + ((lane >> 3) & 1)));
         if (!kFirst) {
-            // ---- O^T = e^(G_i) S^T Q^T + V^T P^T, 32 tokens at a time; written by way of the place that q had (every warp is past its
-            //      products with it only in the second half: the warp's own rows of P's place would do, but are too short)
+            // ---- O^T = e^(G_i) S^T Q^T + V^T P^T, 32 tokens at a time
 #pragma unroll
             for (int half = 0; half < 2; ++half) {
                 float o[4][4] = {};
@@ -389,7 +389,7 @@ static cudaError_t launch_chunk(const LinearChunkParams& p, int64_t segments, cu
 extern "C" int wpp_launch_linear_chunk(const wpp::LinearChunkParams* p, int head_dim, int64_t segments, int two_passes, void* stream) {
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e = cudaSuccess;
-    if (two_passes) e = head_dim == 128 ? wpp::launch_chunk<128, true>(*p, segments, st) : wpp::launch_chunk<64, true>(*p, segments, st);
+    if (two_passes) e = head_dim == 128 ? wpp::launch_chunk<128, true>(*p, p->ws_segments, st) : wpp::launch_chunk<64, true>(*p, p->ws_segments, st);
     if (e == cudaSuccess) e = head_dim == 128 ? wpp::launch_chunk<128, false>(*p, segments, st) : wpp::launch_chunk<64, false>(*p, segments, st);
     return (int)e;
 }

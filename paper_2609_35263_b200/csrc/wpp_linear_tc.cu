@@ -10,8 +10,10 @@
 //   warps 8-11   thread = token: w K in two terms, one of them in K's place; zeros in the rows of V behind the block
 //   warp 12      issues all products (one thread), warp 13 loads Q, K, V by TMA into a ring of four tiles, in the order in which
 //                their places come free, warp 15 sums the logarithms of the decays
-// What bounds it: memory wants 44 clocks a token (1,032 bytes at 6.5 TB/s on 148 SMs), the products 28, the chain
-// S1 -> P -> O2 -> outputs -> S1 about 31.  Products of 16 x 8 x 16 (mma.sync) at a quarter of this rate took 58.
+// What bounds it: memory wants 44 clocks a token (1,032 bytes at 6.5 TB/s on 148 SMs), the products 28; the chains
+// S1 -> P -> O2 -> outputs -> S1 and (4) -> bf16(S) -> (3), with all their hand-overs, take about 60.  Measured: 8 x 2,048 tokens of 32 heads
+// 134 us where the memory would take 87 (256 chains on 148 SMs are two rounds, the second not full), 1 x 32,768 of 16 in segments
+// 209 us; products of 16 x 8 x 16 (wpp_linear_chunk.cu) 365 us for the former.
 // Tensor memory: S1, then P [0,128)  O1 [128,256)  O2 [256,384)  S [384,512).
 // All mbarrier waits are bounded; on expiry the CTA raises its abort flag, every role drains, TMEM is freed and WPP_ERR_TIMEOUT is
 // written to the status word.
@@ -98,6 +100,30 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2, r = threadIdx.x & 127;
     constexpr int kGateUsers = kFirst ? 256 : 384;
 
+    // ---- which request and segment (as in wpp_linear_chunk.cu)
+    const int head = blockIdx.y;
+    const int64_t index = blockIdx.x;
+    int req = 0;
+    int64_t row0 = 0, n = 0, index0 = 0, seg = 0, segs = 0;
+    auto find = [&] {                                  // false: nothing to do
+        grid_dependency_wait();
+        int hi = p.num_requests;
+        while (hi - req > 1) {
+            const int width = (hi - req + 31) / 32, i = req + lane * width;
+            const unsigned le = __ballot_sync(0xffffffffu, i < hi && p.row_offsets[i] / p.seg_tokens + (kFirst ? 0 : i) <= index) | 1u;
+            const int last = 31 - __clz((int)le);
+            hi = min(hi, req + (last + 1) * width);
+            req += last * width;
+        }
+        row0 = p.row_offsets[req], n = p.row_offsets[req + 1] - row0, index0 = row0 / p.seg_tokens;
+        seg = index - index0 - (kFirst ? 0 : req), segs = n > 0 ? (n + p.seg_tokens - 1) / p.seg_tokens : 1;
+        return n > p.few_tokens && seg < segs && !(kFirst && seg == segs - 1);         // (a last segment's own state is nobody's state before)
+    };
+    // Where many CTAs may have nothing to do they see it before anything is set up: 62 requests of 1 token and 2 of 2,048 with 32 heads
+    // 172 us | 157.  Elsewhere the kernel before may still run while they are set up: 8 x 2,048 tokens 134 us | 141.
+    bool mine = true;
+    if (p.few_tokens >= 0 && !find()) return;
+
     if (threadIdx.x == 0) {
         for (int i = 0; i < kSlots; ++i) { mbar_init(bFull + 8 * i, 1); mbar_init(bEmpty + 8 * i, 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(bGFull + 8 * i, 1); mbar_init(bGEmpty + 8 * i, kGateUsers); }
@@ -115,22 +141,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
     grid_launch_dependents();
-    grid_dependency_wait();
-
-    // ---- which request and segment (as in wpp_linear_chunk.cu)
-    const int head = blockIdx.y;
-    const int64_t index = blockIdx.x;
-    int req = 0, hi = p.num_requests;
-    while (hi - req > 1) {
-        const int width = (hi - req + 31) / 32, i = req + lane * width;
-        const unsigned le = __ballot_sync(0xffffffffu, i < hi && p.row_offsets[i] / p.seg_tokens + i <= index) | 1u;
-        const int last = 31 - __clz((int)le);
-        hi = min(hi, req + (last + 1) * width);
-        req += last * width;
-    }
-    const int64_t row0 = p.row_offsets[req], n = p.row_offsets[req + 1] - row0;
-    const int64_t seg = index - (row0 / p.seg_tokens + req), segs = n > 0 ? (n + p.seg_tokens - 1) / p.seg_tokens : 1;
-    const bool mine = seg < segs && !(kFirst && seg == segs - 1);      // (a last segment's own state is nobody's state before)
+    if (p.few_tokens < 0) mine = find();
     const int64_t begin = seg * p.seg_tokens, end = mine ? min(n, begin + p.seg_tokens) : begin;
     const int64_t prefix = p.snap_interval > 0 ? p.prefix_lens[req] : 0;
     // Blocks end at the next boundary of the snapshots.  (Every role walks them by itself: with a 64-bit remainder per block in the
@@ -325,9 +336,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         // ================================================================ the state (thread = row of S)
         const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16) + kColS;
         const int64_t slot_size = (int64_t)p.num_heads * kD * kD, row_at = (int64_t)head * kD * kD + (int64_t)r * kD;
-        const int64_t index0 = index - seg;            // of the chain's first segment
-        // workspace: segment i's own state, four columns of all rows after one another; the chain's first state is where its last
-        // segment's would be
+        // workspace: segments' own states, four columns of all rows after one another
         auto ws = [&](int64_t i, int c4) { return reinterpret_cast<float4*>(p.ws_state + (i * p.num_heads + head) * kD * kD) + c4 * kD + r; };
         const bool from_pool = seg == 0 && (kFirst || segs == 1);
         const int64_t in = from_pool ? slot_of(p, p.state_in[req]) : -1;
@@ -340,9 +349,9 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
                 if (from_pool) {
                     if (in >= 0) y = *reinterpret_cast<const float4*>(p.state_pool + in * slot_size + row_at + 32 * q + 4 * c);
-                    if (kFirst) *ws(index0 + segs - 1, 8 * q + c) = y;         // (state_out may be the same slot, and its segment done first)
+                    if (kFirst) *ws(p.ws_segments + index0, 8 * q + c) = y;         // (state_out may be the same slot, and its segment done first)
                 } else if (!kFirst) {
-                    y = *ws(seg == 0 ? index0 + segs - 1 : index0, 8 * q + c);
+                    y = *ws(seg == 0 ? p.ws_segments + index0 : index0, 8 * q + c);
                 }
                 x[4 * c] = y.x; x[4 * c + 1] = y.y; x[4 * c + 2] = y.z; x[4 * c + 3] = y.w;
             }
@@ -542,11 +551,12 @@ static cudaError_t launch(const CUtensorMap* maps, const LinearChunkParams& p, i
 
 }  // namespace lintc
 
-// maps: q, k, v with boxes of 64 columns of 128 rows; segments: an upper bound of all requests' segments
+// maps: q, k, v with boxes of 64 columns of 128 rows; segments: an upper bound of all requests' segments; two_passes: some chain may
+// have several
 extern "C" int wpp_launch_linear_tc(const wpp::LinearChunkParams* p, const CUtensorMap* maps, int64_t segments, int two_passes, void* stream) {
     cudaStream_t st = (cudaStream_t)stream;
     cudaError_t e = cudaSuccess;
-    if (two_passes) e = lintc::launch<true>(maps, *p, segments, st);
+    if (two_passes) e = lintc::launch<true>(maps, *p, p->ws_segments, st);
     if (e == cudaSuccess) e = lintc::launch<false>(maps, *p, segments, st);
     return (int)e;
 }

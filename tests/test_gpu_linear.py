@@ -223,3 +223,45 @@ def test_beside_the_attention_of_the_same_wave():
     a.k_pool, a.v_pool = okv4.append(a.k_new, a.v_new, a.k_pool, a.v_pool, a.table, a.P, a.C, a.B)
     a.check(out, lse, a.reference())
     w.check(o, g["pool"], w.reference())
+
+
+# single tokens and empty chunks among long ones: more chains than the SMs hold, both forms in one call, long chains in segments
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("interval", [0, 96])
+@pytest.mark.parametrize("in_place", [False, True])
+def test_single_tokens_among_long_chunks(d, interval, in_place):
+    C = [1, 0, 11, 12, 13, 1500, 1, 1, 64, 65, 128, 129, 700, 2] + [1] * 30 + [513]
+    assert len(C) * 8 > 2 * 148
+    w = Wave(C, 8, d, seed=d + interval, interval=interval, prefix=[5 * i for i in range(len(C))])
+    if in_place:
+        w.state_out = w.state_in.copy()
+    ref = w.reference()
+    assert wpp.wpp_linear_workspace_bytes(len(C), 8, d, w.T) > 256
+    for workspace in (True, False):
+        g = w.device()
+        out = w.run(g) if workspace else w.run(g, workspace=None)
+        w.check(out, g["pool"], ref)
+        assert int(g["status"].item()) == 0
+    g, first = w.device(), w.device()
+    ws, a, b = w.workspace(), None, None
+    a = w.run(first, workspace=ws)
+    torch.cuda.synchronize()
+    b = w.run(g, workspace=ws)                         # a workspace that a call before has used
+    assert torch.equal(a, b) and torch.equal(g["pool"], first["pool"])
+
+
+def test_single_tokens_among_long_chunks_captured():
+    C = [1] * 40 + [900]
+    w = Wave(C, 8, 128, seed=3)
+    ref, ws, out = w.reference(), w.workspace(), torch.zeros(w.T, 8, 128, dtype=torch.bfloat16, device="cuda")
+    g = w.device()
+    w.run(g, out=out, workspace=ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        w.run(g, out=out, workspace=ws)
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+    torch.cuda.synchronize()
+    w.check(out, g["pool"], ref)

@@ -224,7 +224,8 @@ int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* k_
  * Results are bit-reproducible for a given plan, whichever CTA takes which tile (no atomics on outputs; partials
  * are merged in a fixed order).
  * WPP_KV4: K_j[g] and V_j[g] are the rows that codes, least and scale stand for.  Slots >= P_i + C_i never influence the result, and
- * a NaN row only the query rows that see it.  One or two kernels, one more iff the plan has split tiles. */
+ * a NaN row only the query rows that see it (their outputs are NaN; of a row of K their lse is -infinity).  One or two kernels,
+ * one more iff the plan has split tiles, and a memset of 256 bytes iff it has more tiles than CTAs. */
 int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* q, void* out,
                                  float* lse_or_null, const void* k_cache, const void* v_cache,
                                  const int32_t* block_tables, const int32_t* prefix_lens,
@@ -502,7 +503,8 @@ typedef struct {
  *   log_decay    : device fp32 [H], or [T] rows of H decay_token_stride apart.
  *   row_offsets, prefix_lens, state_pool, state_in, state_out, snap_slots, status_dev : as for wpp_kda_chunk (slots are
  *                  H * head_dim * head_dim floats); no slot may be written for one request and read or written for another
- *                  in the same call.
+ *                  in the same call, nor two states of a request into one slot.
+ *   out          : no byte of it in q, k, v, log_decay or the state pool.
  *   workspace    : device scratch, 256-byte aligned, wpp_linear_workspace_bytes(desc) bytes; may be NULL (0 bytes), which leaves
  *                  the library fewer forms to choose from.  Calls that may overlap on the GPU need one each.
  * A request with an empty chunk copies state_in to state_out.  Returns WPP_ERR_INVALID_ARG for null or misaligned pointers, sizes

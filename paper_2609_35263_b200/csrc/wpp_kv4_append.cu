@@ -5,6 +5,9 @@
 // and stands for least + scale * code.  The quotient is the correctly rounded one and is rounded to even halves, so that the result
 // is defined to the bit.  scale < 2^-100 (equal values, or nearly): scale and codes are 0.  A row with a NaN or an infinity, or
 // whose extent is more than a float holds, has the quiet NaN 0x7fc0 as its least value, and scale and codes 0.
+//
+// A large grid is bound by instructions: 32 x 256..2,048 tokens of 8 heads of 128 take 49 us, a copy of the rows to the same addresses 33, the
+// bytes at the measured copy bandwidth 29.  64 single tokens take 4.1 us, a launch and a chain of dependent loads.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>

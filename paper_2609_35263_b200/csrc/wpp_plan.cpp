@@ -2,6 +2,7 @@
 // and the optional aliasing check (wpp_validate_batch).  Integer arithmetic only.
 #include <algorithm>
 #include <cstring>
+#include <new>
 #include <queue>
 #include <unordered_map>
 #include <vector>
@@ -233,8 +234,13 @@ int wpp_plan_tiles(const wpp_ctx* ctx, const wpp_batch_desc* desc, const int32_t
         pairs += C * P + C * (C + 1) / 2;
     }
     if (T > 0x7fffffff) return WPP_ERR_INVALID_ARG;
-    if (d.dtype == WPP_KV4)
-        return wpp_kv4_plan(&d, &o, prefix_lens, chunk_lens, T, pairs, plan_host, plan_host_bytes, info);
+    if (d.dtype == WPP_KV4) {
+        try {
+            return wpp_kv4_plan(&d, &o, prefix_lens, chunk_lens, T, pairs, plan_host, plan_host_bytes, info);
+        } catch (const std::bad_alloc&) {              // (no exception passes a C entry)
+            return WPP_ERR_WORKSPACE_TOO_SMALL;
+        }
+    }
     if (plan_host_bytes < plan_bytes_bound(&d, &o, T)) return WPP_ERR_PLAN_MISMATCH;
 
     // ---- row blocks of every request.  A tile is a row block times the heads it takes (one head, or 2..16 heads of

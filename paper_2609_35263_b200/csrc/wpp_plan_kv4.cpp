@@ -84,7 +84,31 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     }
     if (n_base > 0x3fffffff) return WPP_ERR_INVALID_ARG;
     const int64_t most_ctas = (int64_t)(max_rows <= 8 ? kFewCtas : kFewCtasWide) * o->max_ctas;
-    const int64_t share = std::max<int64_t>((all_steps + kUnitSteps * (n_base + most_ctas) + most_ctas - 1) / most_ctas, kUnitSteps + kLeastSteps);
+    int64_t share = std::max<int64_t>((all_steps + kUnitSteps * (n_base + most_ctas) + most_ctas - 1) / most_ctas, kUnitSteps + kLeastSteps);
+    // Where the part that begins at key step `at` ends: a CTA takes what is left of its share, no less than kLeastSteps, and the rest too
+    // if that is little.  next: it is the next CTA's.
+    auto part_end = [&](int32_t steps, int32_t at, int64_t& left, bool& next) {
+        next = left < kUnitSteps + kLeastSteps && left < share;
+        if (next) left = share;
+        int32_t n = (int32_t)std::min<int64_t>(steps - at, std::max<int64_t>(left - kUnitSteps, kLeastSteps));
+        if (steps - at - n < kLeastSteps) n = steps - at;
+        left -= n + kUnitSteps;
+        return at + n;
+    };
+    // Blocks too short to be cut may leave much of every share: it grows until the CTAs are enough (5 x 9..43 tokens, 40/8 heads: 320 blocks
+    // of a step on 296 CTAs, of which the last had 25, 274 us | 14.5)
+    for (int64_t ctas = most_ctas + 1; o->force_kv_splits < 1 && ctas > most_ctas;) {
+        int64_t left = share;
+        ctas = 1;
+        bool next = false;
+        for (int i = 0; i < R && ctas <= most_ctas; ++i)
+            for (int64_t r0 = 0; r0 < chunk_lens[i] && is_few(d, chunk_lens[i], walks); r0 += toks) {
+                const int32_t steps = steps_for(prefix_lens[i] + std::min<int64_t>(r0 + toks, chunk_lens[i]));
+                for (int64_t b = (int64_t)((G + heads - 1) / heads) * Hkv; b > 0; --b)
+                    for (int32_t at = 0; at < steps; ctas += next) at = part_end(steps, at, left, next);
+            }
+        if (ctas > most_ctas) share += std::max<int64_t>(1, share / 16);
+    }
 
     WppPlanHeader hd;
     std::memset(&hd, 0, sizeof(hd));
@@ -118,15 +142,9 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
                         for (int32_t q = 1; q <= n; ++q) cuts.push_back((int32_t)((int64_t)steps * q / n));
                     } else {
                         for (int32_t at = 0; at < steps;) {
-                            // a CTA takes what is left of its share, no less than kLeastSteps, and the rest too if that is little
-                            if (left < kUnitSteps + kLeastSteps && (int64_t)first.size() < most_ctas && left < share) {
-                                first.push_back((int32_t)(n_units + cuts.size() - 1));
-                                left = share;
-                            }
-                            int32_t n = (int32_t)std::min<int64_t>(steps - at, std::max<int64_t>(left - kUnitSteps, kLeastSteps));
-                            if (steps - at - n < kLeastSteps || (int64_t)first.size() >= most_ctas) n = steps - at;
-                            left -= n + kUnitSteps;
-                            at += n;
+                            bool next;
+                            at = part_end(steps, at, left, next);
+                            if (next) first.push_back((int32_t)(n_units + cuts.size() - 1));
                             cuts.push_back(at);
                         }
                     }
@@ -248,6 +266,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     off += sizeof(WppCombine) * combines.size();
     hd.plan_bytes = align_up(off, 16);
     if (hd.plan_bytes > plan_host_bytes) return WPP_ERR_PLAN_MISMATCH;
+    if (hd.plan_bytes > 0xffffffffu) return WPP_ERR_INVALID_ARG;       // (offsets are 32 bits)
     std::memcpy(p + hd.off_few_ctas, first.data(), sizeof(int32_t) * first.size());
     if (!combines.empty()) std::memcpy(p + hd.off_combine, combines.data(), sizeof(WppCombine) * combines.size());
     std::memset(p + off, 0, hd.plan_bytes - off);

@@ -4,6 +4,7 @@ from fractions import Fraction
 
 import numpy as np
 import pytest
+import torch
 
 import paper_2609_35263_b200 as wpp
 import paper_2609_35263_b200.binding as B
@@ -158,3 +159,27 @@ def check_cover(raw, P, C, Hq, Hkv):
                 assert len(parts) == 1
         assert at == C[req]
     assert not by_row
+
+
+@pytest.mark.parametrize("d,Hq,Hkv,P,C", [(128, 40, 8, [0] * 5, [9, 43, 26, 40, 31]), (128, 64, 8, [63] * 20, [2, 10] * 10), (128, 64, 8, [21] * 61, [1] * 30 + [2] * 31),
+                                          (64, 8, 2, [700] * 64, [1] * 64), (128, 64, 8, list(range(255, 16384, 253)), [1] * 64)])
+def test_few_row_blocks_are_dealt_out_evenly(d, Hq, Hkv, P, C):
+    desc = wpp.make_desc(len(P), Hq, Hkv, d, 32, 600, 999, dtype=wpp.WPP_KV4)
+    raw = wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, 0, 148, 0, 2), pin=False).host.numpy()
+    head = raw[:136].view(np.int32)
+    units = raw[head[24]:head[24] + 48 * head[6]].view(np.int32).reshape(-1, 12)
+    first = raw[head[33]:head[33] + 4 * (head[32] + 1)].view(np.int32)
+    assert first[0] == 0 and first[-1] == head[30] == len(units) and (np.diff(first) > 0).all() and head[32] <= 3 * 148
+    cost = units[:, 2] - units[:, 1] + 3                   # what starting a block costs, in key steps
+    assert np.add.reduceat(cost, first[:-1]).max() <= 1.25 * cost.sum() / (2 * 148) + cost.max()
+
+
+def test_a_head_shard_of_a_cache_in_4_bits():
+    from paper_2609_35263_b200.stages import head_shard
+    pool = torch.zeros(9, 4, wpp.wpp_kv4_block_bytes(16, 64), dtype=torch.uint8)
+    q, kv = torch.zeros(7, 8, 64, dtype=torch.bfloat16), torch.zeros(7, 4, 64, dtype=torch.bfloat16)
+    desc, views = head_shard(1, 2, 1, 8, 4, 64, 16, 9, 9, q, q, kv, kv, pool, pool)
+    assert desc.dtype == wpp.WPP_KV4 and desc.num_kv_heads == 2 and desc.num_q_heads == 4
+    assert desc.kv_page_stride == 4 * 576 and desc.kv_head_stride == 576 and desc.kv_token_stride == 0
+    assert views["k_pool"].data_ptr() == pool.data_ptr() + 2 * 576
+    wpp.wpp_plan_tiles(None, desc, [100], [7], pin=False)

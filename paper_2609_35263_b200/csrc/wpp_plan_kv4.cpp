@@ -14,13 +14,16 @@ static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 // steps; and the fewest steps that a block is cut for.
 constexpr int kFewCtas = 3, kFewCtasWide = 2;
 constexpr int64_t kUnitSteps = 3, kLeastSteps = 2;
-// A chunk is the kernel for few rows' if that walks its keys no more often than kFewWalks times.  But each kernel of a wave has its own
-// start and end, and the tile kernel's are the longer ones: a wave that is kFewAll steps per SM in all on the former (units with
-// what they cost besides) is all its, and where there are tiles anyway, so little work of few rows goes to them.  Attention call
-// in a graph, us, tiles | few rows: 1 x 64 tokens over 1,024 (8/2 heads of 64) 22 | 9.7, 8 x 64 over 256 14.5 | 8.3, 1 x 128 over
-// 256 (32/8) 17.9 | 11.3, 1 x 32 over 2,000 21 | 17.6; beyond kFewAll 1 x 16 over 8,192 (64/8) 27 | 31, 4 x 64 over 300 19 | 39;
-// within kFewWalks 64 x 5 over 1,000 (32/8) 102 | 65; 12 x 1..300 over 0..700 (8/2), all tiles 24, both kernels 30.
-constexpr int64_t kFewWalks = 2, kFewAll = 12;
+// Which kernel takes a chunk, if a wave has both: the one for few rows walks its keys once per block, and has a walk done in a quarter
+// of what a tile's takes.  Attention call in a graph, us, tiles | few rows: 4 walks a tile, 8 x 8 tokens over 4,096 (64/8 heads of 128)
+// 56 | 52; 5 walks, 32 x 10 over 2,048 102 | 132; 6 walks of 5 tiles, 16 x 18 over 4,000 (40/8) 424 | 137.
+constexpr int64_t kFewWalks = 4;
+// A wave has both, tiles alone or few rows alone, by the estimated time of each: a start, and for what falls to a CTA a time per key
+// step, of few rows with kUnitSteps a unit, of tiles with one half and with both (heads of 64: about 0.7 of it).  Estimated and measured:
+// 64 x 1 over 255..16,383 (64/8) 130, 128; 16 x 32 over 2,000 (32/8) tiles 50, 48, few rows 99, 101; 64 x 5 over 1,000 (32/8) 92, 102 and
+// 59, 65; 1 x 64 over 1,024 (8/2 of 64) 18, 22 and 9, 9.7; 12 x 1..300 over 0..700 (8/2 of 64) tiles 24, 24, both 34, 30.
+constexpr double kFewStart = 3.0, kFewStep = 1.45, kTileStart = 7.0, kTileStep1 = 2.7, kTileStep2 = 3.2, kCombine = 4.0;
+constexpr int64_t kFewShort = 4;
 // Tiles: fewest key steps of a part, and rounds of tiles up to which the longest come first.
 constexpr int32_t kTileLeastSteps = 4;
 constexpr int64_t kTileOrderRounds = 16;
@@ -34,20 +37,78 @@ static int64_t few_blocks(const wpp_batch_desc* d, int64_t C) {
     return (C + t - 1) / t * ((G + h - 1) / h) * d->num_kv_heads;
 }
 
-// How often the kernel for few rows may walk a chunk's keys, in this wave: kFewWalks, 0 (tiles alone) or any number.
+// Tiles of two halves of 128 rows: two heads of a KV group over the same rows where the group is even (both then end at the same key),
+// else two row blocks of a head; blocks of at most 64 rows take several heads in a half (see WppUnit).  Of a block of `rows` rows:
+// places for heads in a half, and heads of a tile.
+static int32_t tile_rows(int32_t G) { return G % 2 == 0 ? WPP_HALF_M : 2 * WPP_HALF_M; }
+static void tile_heads(int32_t G, int32_t rows, int32_t* pack, int32_t* per_tile) {
+    *pack = *per_tile = 1;
+    if (rows > WPP_HALF_M) return;
+    while (*pack < 8 && G % (2 * *pack) == 0 && WPP_HALF_M / (2 * *pack) >= rows) *pack *= 2;
+    int32_t whole = 1;
+    while (whole < G) whole *= 2;
+    *per_tile = G % (2 * *pack) == 0 ? 2 * *pack : *pack;
+    if (*pack < whole && whole <= 8 && WPP_HALF_M / whole >= rows) {
+        *pack = whole;
+        *per_tile = G;
+    }
+}
+static int64_t tiles_of(const wpp_batch_desc* d, int64_t C) {
+    const int32_t G = d->num_q_heads / d->num_kv_heads, block = tile_rows(G);
+    int32_t pack, per_tile;
+    tile_heads(G, block, &pack, &per_tile);
+    int64_t n = C / block * (d->num_q_heads / per_tile);
+    if (C % block == 0) return n;
+    tile_heads(G, (int32_t)(C % block), &pack, &per_tile);
+    return n + d->num_q_heads / per_tile;
+}
+
+// Whether the kernel for few rows has a chunk: walks per tile 0, kFewWalks or any number.
+static bool is_few(const wpp_batch_desc* d, int64_t C, int64_t walks) {
+    return walks == INT64_MAX || few_blocks(d, C) <= walks * tiles_of(d, C);
+}
 static int64_t few_walks(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t* prefix_lens, const int32_t* chunk_lens) {
     if (o->shape) return o->shape == 1 ? 0 : INT64_MAX;
-    int64_t all = 0, few = 0;
-    for (int i = 0; i < d->num_requests; ++i) {
-        const int64_t C = chunk_lens[i], n = few_blocks(d, C), walks = n / d->num_kv_heads;
-        const int64_t cost = n * (((int64_t)prefix_lens[i] + C + WPP_TILE_N - 1) / WPP_TILE_N + kUnitSteps);
-        all += cost;
-        if (walks <= kFewWalks) few += cost;
+    const int32_t G = d->num_q_heads / d->num_kv_heads;
+    const int64_t choices[3] = {kFewWalks, INT64_MAX, 0};
+    double best_us = 0.0;
+    int64_t best = kFewWalks;
+    for (int64_t walks : choices) {
+        double few = 0.0, steps = 0.0, longest = 0.0, least = 0.0;
+        int64_t tiles = 0, rows = 0;
+        bool both_halves = false, cut = false;
+        for (int i = 0; i < d->num_requests; ++i) {
+            const int64_t C = chunk_lens[i], end = (prefix_lens[i] + C + WPP_TILE_N - 1) / WPP_TILE_N;
+            if (C == 0) continue;
+            if (is_few(d, C, walks)) {
+                few += (double)few_blocks(d, C) * (double)(end + kUnitSteps);
+                rows = std::max(rows, std::min<int64_t>(C, few_tokens(G)) * few_heads(G));
+                least = std::max(least, (double)std::min(end + kUnitSteps, kFewShort));
+                cut |= end >= 2 * kLeastSteps;
+            } else {
+                const int64_t n = tiles_of(d, C);
+                tiles += n;
+                steps += (double)n * (double)end;
+                longest = std::max(longest, (double)end);
+                int32_t pack, per_tile;
+                tile_heads(G, (int32_t)std::min<int64_t>(C, tile_rows(G)), &pack, &per_tile);
+                both_halves |= per_tile > pack || C > WPP_HALF_M;
+            }
+        }
+        double us = 0.0;
+        if (few > 0.0) {
+            const double share = few / ((double)(rows <= 8 ? kFewCtas : kFewCtasWide) * o->max_ctas);
+            us += kFewStart + kFewStep * std::max(share, least) + (cut && share > kUnitSteps ? kCombine : 0.0);
+        }
+        if (tiles > 0) {
+            const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(o->max_ctas / tiles, (int64_t)longest / kTileLeastSteps));
+            const double per = tiles < o->max_ctas ? longest / (double)parts : steps / o->max_ctas + longest / 2;
+            us += kTileStart + (both_halves ? kTileStep2 : kTileStep1) * (d->head_dim == 64 ? 0.7 : 1.0) * per + (parts > 1 ? kCombine : 0.0);
+        }
+        if (walks == kFewWalks || us < best_us) { best = walks; best_us = us; }
     }
-    if (all <= kFewAll * o->max_ctas) return INT64_MAX;
-    return few < all && few <= kFewAll * o->max_ctas ? 0 : kFewWalks;
+    return best;
 }
-static bool is_few(const wpp_batch_desc* d, int64_t C, int64_t walks) { return few_blocks(d, C) / d->num_kv_heads <= walks; }
 
 size_t wpp_kv4_plan_bytes(const wpp_batch_desc* d, const wpp_plan_opts* o, int64_t T) {
     const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
@@ -187,14 +248,13 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     }
     const int64_t n_few = n_units;
 
-    // ---- tiles: two halves of 128 rows each, two heads of a KV group over the same rows where the group is even (both then end at
-    //      the same key), else two row blocks of a head; blocks of at most 64 rows take several heads in a half (see WppUnit)
+    // ---- tiles
     struct Tile { WppUnit u; int32_t steps; };
     std::vector<Tile> tiles;
     for (int i = 0; i < R; ++i) {
         const int64_t P = prefix_lens[i], C = chunk_lens[i];
         if (is_few(d, C, walks)) continue;
-        const int32_t block = G % 2 == 0 ? WPP_HALF_M : 2 * WPP_HALF_M;
+        const int32_t block = tile_rows(G);
         for (int64_t r0 = 0; r0 < C; r0 += block) {
             const int32_t rows = (int32_t)std::min<int64_t>(block, C - r0);
             Tile t;
@@ -202,16 +262,9 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
             t.u.request = i;
             t.u.row0[0] = (int32_t)r0;
             t.steps = steps_for(P + r0 + rows);
-            int32_t pack = 1, per_tile = 1;
+            int32_t pack, per_tile;
+            tile_heads(G, rows, &pack, &per_tile);
             if (rows <= WPP_HALF_M) {
-                while (pack < 8 && G % (2 * pack) == 0 && WPP_HALF_M / (2 * pack) >= rows) pack *= 2;
-                int32_t whole = 1;
-                while (whole < G) whole *= 2;
-                per_tile = G % (2 * pack) == 0 ? 2 * pack : pack;
-                if (pack < whole && whole <= 8 && WPP_HALF_M / whole >= rows) {
-                    pack = whole;
-                    per_tile = G;
-                }
                 t.u.rows[0] = rows;
                 t.u.rows[1] = per_tile == 2 * pack ? rows : 0;
                 t.u.row0[1] = (int32_t)r0;

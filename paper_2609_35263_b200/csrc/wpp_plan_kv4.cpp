@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <cstring>
+#include <utility>
 #include <vector>
 
 #include "../../include/wpp.h"
@@ -19,13 +20,15 @@ constexpr int64_t kUnitSteps = 3, kLeastSteps = 2;
 // 56 | 52; 5 walks, 32 x 10 over 2,048 102 | 132; 6 walks of 5 tiles, 16 x 18 over 4,000 (40/8) 424 | 137.
 constexpr int64_t kFewWalks = 4;
 // A wave has both, tiles alone or few rows alone, by the estimated time of each: a start, and for what falls to a CTA a time per key
-// step, of few rows with kUnitSteps a unit, of tiles with one half and with both (heads of 64: about 0.7 of it).  Estimated and measured:
+// step, of few rows with kUnitSteps a unit, of tiles with one half and with both (heads of 64: 0.7 of either).  Estimated and measured:
 // 64 x 1 over 255..16,383 (64/8) 130, 128; 16 x 32 over 2,000 (32/8) tiles 50, 48, few rows 99, 101; 64 x 5 over 1,000 (32/8) 92, 102 and
 // 59, 65; 1 x 64 over 1,024 (8/2 of 64) 18, 22 and 9, 9.7; 12 x 1..300 over 0..700 (8/2 of 64) tiles 24, 24, both 34, 30.
 constexpr double kFewStart = 3.0, kFewStep = 1.45, kTileStart = 7.0, kTileStep1 = 2.7, kTileStep2 = 3.2, kCombine = 4.0;
 constexpr int64_t kFewShort = 4;
-// Tiles: fewest key steps of a part, and rounds of tiles up to which the longest come first.
-constexpr int32_t kTileLeastSteps = 4;
+// Tiles: fewest key steps of a part, and rounds of tiles up to which the longest come first.  The parts of a wave are of equal length,
+// whatever the tiles': against equal numbers of parts, us, 4 x 76..106 tokens over 0..18,257 (32/8) 193 -> 104, 4 x 47..191 over 0..31,067
+// (64/8) 435 -> 332; cut for any win, 2 x 183..211 over 0..1,065 (32/8) would take 28 where whole tiles take 25.
+constexpr int64_t kTileLeastSteps = 4, kTileLeastWin = 3;
 constexpr int64_t kTileOrderRounds = 16;
 
 // Row blocks of the kernel for few rows: heads of a KV group, and tokens, WPP_FEW_ROWS rows at most.
@@ -63,6 +66,27 @@ static int64_t tiles_of(const wpp_batch_desc* d, int64_t C) {
     return n + d->num_q_heads / per_tile;
 }
 
+// Key steps of a tile's parts, at most: the least with which the parts of fewer tiles than CTAs are no more than those; of more tiles, a
+// CTA's share of all steps, which cuts what alone would take longer; but no tile is cut where that wins less than kTileLeastWin steps.
+// `tiles`: (how many, of so many steps).
+static int64_t tile_part_steps(const std::vector<std::pair<int64_t, int64_t>>& tiles, int64_t ctas) {
+    int64_t n = 0, all = 0, longest = 1;
+    for (const auto& t : tiles) {
+        n += t.first;
+        all += t.first * t.second;
+        longest = std::max(longest, t.second);
+    }
+    int64_t lo = std::min<int64_t>(std::max<int64_t>(kTileLeastSteps, (all + ctas - 1) / ctas), longest), hi = longest;
+    while (n < ctas && lo < hi) {
+        const int64_t mid = (lo + hi) / 2;
+        int64_t parts = 0;
+        for (const auto& t : tiles) parts += t.first * ((t.second + mid - 1) / mid);
+        if (parts <= ctas) hi = mid;
+        else lo = mid + 1;
+    }
+    return longest - lo >= kTileLeastWin ? lo : longest;
+}
+
 // Whether the kernel for few rows has a chunk: walks per tile 0, kFewWalks or any number.
 static bool is_few(const wpp_batch_desc* d, int64_t C, int64_t walks) {
     return walks == INT64_MAX || few_blocks(d, C) <= walks * tiles_of(d, C);
@@ -71,12 +95,15 @@ static int64_t few_walks(const wpp_batch_desc* d, const wpp_plan_opts* o, const 
     if (o->shape) return o->shape == 1 ? 0 : INT64_MAX;
     const int32_t G = d->num_q_heads / d->num_kv_heads;
     const int64_t choices[3] = {kFewWalks, INT64_MAX, 0};
+    const double narrow = d->head_dim == 64 ? 0.7 : 1.0;
     double best_us = 0.0;
     int64_t best = kFewWalks;
     for (int64_t walks : choices) {
-        double few = 0.0, steps = 0.0, longest = 0.0, least = 0.0;
-        int64_t tiles = 0, rows = 0;
-        bool both_halves = false, cut = false;
+        double few = 0.0, steps = 0.0, least = 0.0;
+        int64_t rows = 0, num_tiles = 0, longest = 0;
+        std::vector<std::pair<int64_t, int64_t>> tiles;
+        bool both_halves = false;
+        double few_longest = 0.0;
         for (int i = 0; i < d->num_requests; ++i) {
             const int64_t C = chunk_lens[i], end = (prefix_lens[i] + C + WPP_TILE_N - 1) / WPP_TILE_N;
             if (C == 0) continue;
@@ -84,12 +111,13 @@ static int64_t few_walks(const wpp_batch_desc* d, const wpp_plan_opts* o, const 
                 few += (double)few_blocks(d, C) * (double)(end + kUnitSteps);
                 rows = std::max(rows, std::min<int64_t>(C, few_tokens(G)) * few_heads(G));
                 least = std::max(least, (double)std::min(end + kUnitSteps, kFewShort));
-                cut |= end >= 2 * kLeastSteps;
+                few_longest = std::max(few_longest, (double)(end + kUnitSteps));
             } else {
                 const int64_t n = tiles_of(d, C);
-                tiles += n;
+                tiles.emplace_back(n, end);
+                num_tiles += n;
                 steps += (double)n * (double)end;
-                longest = std::max(longest, (double)end);
+                longest = std::max(longest, end);
                 int32_t pack, per_tile;
                 tile_heads(G, (int32_t)std::min<int64_t>(C, tile_rows(G)), &pack, &per_tile);
                 both_halves |= per_tile > pack || C > WPP_HALF_M;
@@ -98,12 +126,13 @@ static int64_t few_walks(const wpp_batch_desc* d, const wpp_plan_opts* o, const 
         double us = 0.0;
         if (few > 0.0) {
             const double share = few / ((double)(rows <= 8 ? kFewCtas : kFewCtasWide) * o->max_ctas);
-            us += kFewStart + kFewStep * std::max(share, least) + (cut && share > kUnitSteps ? kCombine : 0.0);
+            us += kFewStart + kFewStep * narrow * std::max(share, least) + (few_longest > share && few_longest > (double)kFewShort + kUnitSteps ? kCombine : 0.0);
         }
-        if (tiles > 0) {
-            const int64_t parts = std::max<int64_t>(1, std::min<int64_t>(o->max_ctas / tiles, (int64_t)longest / kTileLeastSteps));
-            const double per = tiles < o->max_ctas ? longest / (double)parts : steps / o->max_ctas + longest / 2;
-            us += kTileStart + (both_halves ? kTileStep2 : kTileStep1) * (d->head_dim == 64 ? 0.7 : 1.0) * per + (parts > 1 ? kCombine : 0.0);
+        if (num_tiles > 0) {
+            const double part = (double)tile_part_steps(tiles, o->max_ctas);
+            us += kTileStart + (both_halves ? kTileStep2 : kTileStep1) * narrow *
+                                   (num_tiles < o->max_ctas ? part : steps / o->max_ctas + part / 2);
+            if (part < (double)longest) us += kCombine;
         }
         if (walks == kFewWalks || us < best_us) { best = walks; best_us = us; }
     }
@@ -283,10 +312,12 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     }
     if ((int64_t)tiles.size() <= kTileOrderRounds * o->max_ctas)
         std::stable_sort(tiles.begin(), tiles.end(), [](const Tile& a, const Tile& b) { return a.steps > b.steps; });
-    const int64_t tile_parts = tiles.empty() ? 1 : std::max<int64_t>(1, o->max_ctas / (int64_t)tiles.size());
+    std::vector<std::pair<int64_t, int64_t>> counted;
+    for (const Tile& t : tiles) counted.emplace_back(1, t.steps);
+    const int64_t part_steps = tile_part_steps(counted, o->max_ctas);
     for (Tile& t : tiles) {
         const int32_t parts = std::max(1, o->force_kv_splits >= 1 ? std::min(o->force_kv_splits, t.steps)
-                                                                  : (int32_t)std::min<int64_t>(tile_parts, t.steps / kTileLeastSteps));
+                                                                  : (int32_t)((t.steps + part_steps - 1) / part_steps));
         if (n_units + parts > unit_cap) return WPP_ERR_PLAN_MISMATCH;
         if (parts > 1)
             for (int hf = 0; hf < 2; ++hf)

@@ -1,4 +1,4 @@
-// Work split of a wave over a cache held in 4 bits (part of wpp_plan_tiles; integer arithmetic only).
+// Work split of a wave over a cache held in 4 bits (part of wpp_plan_tiles).
 #include <algorithm>
 #include <cstdint>
 #include <cstring>
@@ -68,8 +68,9 @@ static int64_t tiles_of(const wpp_batch_desc* d, int64_t C) {
 
 // Key steps of a tile's parts, at most: the least with which the parts of fewer tiles than CTAs are no more than those; of more tiles, a
 // CTA's share of all steps, which cuts what alone would take longer; but no tile is cut where that wins less than kTileLeastWin steps.
-// `tiles`: (how many, of so many steps).
-static int64_t tile_part_steps(const std::vector<std::pair<int64_t, int64_t>>& tiles, int64_t ctas) {
+// `tiles`: (how many, of so many steps).  Tiles that fill the CTAs are cut only into as many parts as `slots` hold: a wave that needs
+// no scratch uncut is not refused for its cuts by the entry point that has the built-in array alone.
+static int64_t tile_part_steps(const std::vector<std::pair<int64_t, int64_t>>& tiles, int64_t ctas, int64_t slots) {
     int64_t n = 0, all = 0, longest = 1;
     for (const auto& t : tiles) {
         n += t.first;
@@ -84,7 +85,13 @@ static int64_t tile_part_steps(const std::vector<std::pair<int64_t, int64_t>>& t
         if (parts <= ctas) hi = mid;
         else lo = mid + 1;
     }
-    return longest - lo >= kTileLeastWin ? lo : longest;
+    int64_t parts = 0;
+    for (const auto& t : tiles) parts += t.second > lo ? t.first * ((t.second + lo - 1) / lo) : 0;
+    return longest - lo >= kTileLeastWin && (n < ctas || parts <= slots) ? lo : longest;
+}
+
+static int64_t scratch_slots(const wpp_batch_desc* d) {
+    return (int64_t)((wpp_static_scratch_bytes() - WPP_WS_HEADER_BYTES) / (2 * WPP_HALF_M * (d->head_dim + 1) * sizeof(float)));
 }
 
 // Whether the kernel for few rows has a chunk: walks per tile 0, kFewWalks or any number.
@@ -129,7 +136,7 @@ static int64_t few_walks(const wpp_batch_desc* d, const wpp_plan_opts* o, const 
             us += kFewStart + kFewStep * narrow * std::max(share, least) + (few_longest > share && few_longest > (double)kFewShort + kUnitSteps ? kCombine : 0.0);
         }
         if (num_tiles > 0) {
-            const double part = (double)tile_part_steps(tiles, o->max_ctas);
+            const double part = (double)tile_part_steps(tiles, o->max_ctas, scratch_slots(d));
             us += kTileStart + (both_halves ? kTileStep2 : kTileStep1) * narrow *
                                    (num_tiles < o->max_ctas ? part : steps / o->max_ctas + part / 2);
             if (part < (double)longest) us += kCombine;
@@ -314,7 +321,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
         std::stable_sort(tiles.begin(), tiles.end(), [](const Tile& a, const Tile& b) { return a.steps > b.steps; });
     std::vector<std::pair<int64_t, int64_t>> counted;
     for (const Tile& t : tiles) counted.emplace_back(1, t.steps);
-    const int64_t part_steps = tile_part_steps(counted, o->max_ctas);
+    const int64_t part_steps = tile_part_steps(counted, o->max_ctas, scratch_slots(d) - slots);
     for (Tile& t : tiles) {
         const int32_t parts = std::max(1, o->force_kv_splits >= 1 ? std::min(o->force_kv_splits, t.steps)
                                                                   : (int32_t)((t.steps + part_steps - 1) / part_steps));

@@ -183,3 +183,14 @@ def test_a_head_shard_of_a_cache_in_4_bits():
     assert desc.kv_page_stride == 4 * 576 and desc.kv_head_stride == 576 and desc.kv_token_stride == 0
     assert views["k_pool"].data_ptr() == pool.data_ptr() + 2 * 576
     wpp.wpp_plan_tiles(None, desc, [100], [7], pin=False)
+
+
+@pytest.mark.parametrize("P,C", [([0] * 40 + [200000], [900] * 40 + [128]), ([0] * 4 + [60000] * 4, [4000] * 8), (list(range(0, 64000, 2000)), [700] * 32)])
+@pytest.mark.parametrize("d,Hq,Hkv", [(128, 64, 8), (64, 8, 8), (128, 40, 8)])
+def test_tiles_that_fill_the_machine_take_no_more_scratch_than_the_built_in_array_has(d, Hq, Hkv, P, C):
+    desc = wpp.make_desc(len(P), Hq, Hkv, d, 128, 1600, 99999, dtype=wpp.WPP_KV4)
+    plan = wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, 0, 148), pin=False)
+    raw = plan.host.numpy()
+    check_cover(raw[:plan.plan_bytes], P, C, Hq, Hkv)
+    if sum(-(-c // 256) for c in C) * Hq >= 148:
+        assert plan.info.workspace_bytes <= wpp.wpp_static_scratch_bytes()

@@ -13,7 +13,7 @@
 // the memory needs 44; heads of 128 come here with few chains of short chunks only, see kLinTcTokens, the others to
 // wpp_linear_tc.cu: 8 x 2,048 tokens of 32 heads 365 us | 134 there).  Heads of 64: 8 x 2,048 of 32 heads 131 us, half the bytes
 // and a quarter of the products.  The sums G are made in 64 bits and kept as a multiple of 1/64 and a rest, so that differences of long
-// sums are exact to fp32.  A logarithm below -256 (base 2) is taken for that: it leaves nothing of an fp32 state.
+// sums are exact to fp32.
 //
 // Few long chains are cut into segments (`seg_tokens`): a first pass leaves every segment's own state but the last one's, starting
 // at zero (the first one's at the chain's), and its decay; in the second pass a CTA makes its segment's state before from those.
@@ -22,6 +22,7 @@
 #include <stdint.h>
 
 #include "wpp_device.h"
+#include "wpp_linear_blocks.cuh"
 #include "wpp_ptx.cuh"
 
 namespace wpp {
@@ -175,7 +176,7 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
     float g0 = 0.f, g1 = 0.f;
     auto load_decay = [&](int64_t at, int len) {
         auto one = [&](int r) {
-            return r < len ? fmaxf(p.log_decay[(row0 + at + r) * p.decay_token_stride + head] * 1.4426950408889634f, -256.f) : 0.f;
+            return r < len ? decay_log2(p, row0 + at + r, head) : 0.f;
         };
         g0 = one(2 * lane);
         g1 = one(2 * lane + 1);
@@ -198,8 +199,8 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
                 const double x = __shfl_up_sync(0xffffffffu, sum, w);
                 if (lane >= w) sum += x;
             }
-            const double total = __shfl_sync(0xffffffffu, sum, 31);
-            a += sum - b;
+            const double total = __shfl_sync(0xffffffffu, sum, 31), before = __shfl_up_sync(0xffffffffu, sum, 1);
+            a += lane > 0 ? before : 0.0;              // (not sum - b: b may be no number)
             b = sum;
             auto put = [&](int i, double x) {
                 const float whole = rintf((float)x * 64.f) * 0.015625f;

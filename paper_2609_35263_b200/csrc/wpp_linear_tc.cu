@@ -23,6 +23,7 @@
 #include <stdint.h>
 
 #include "wpp_device.h"
+#include "wpp_linear_blocks.cuh"
 #include "wpp_ptx.cuh"
 
 namespace lintc {
@@ -236,7 +237,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     const int t = 4 * lane + i;
-                    g[i] = t < len ? fmaxf(p.log_decay[(row0 + at + t) * p.decay_token_stride + head] * 1.4426950408889634f, -256.f) : 0.f;
+                    g[i] = t < len ? decay_log2(p, row0 + at + t, head) : 0.f;
                 }
             };
             double all = 0.0;
@@ -252,8 +253,8 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     const double x = __shfl_up_sync(0xffffffffu, before, o);
                     if (lane >= o) before += x;
                 }
-                const double total = __shfl_sync(0xffffffffu, before, 31);
-                before -= sum;
+                const double total = __shfl_sync(0xffffffffu, before, 31), behind = __shfl_up_sync(0xffffffffu, before, 1);
+                before = lane > 0 ? behind : 0.0;      // (not before - sum: sum may be no number)
                 w.next();
                 if (w.more()) load(w.at, w.len());
                 if (!__all_sync(0xffffffffu, mbar_wait(bGEmpty + 8 * (b & 1u), ((b >> 1) & 1u) ^ 1u, abort_flag))) break;

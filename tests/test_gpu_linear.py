@@ -265,3 +265,90 @@ def test_single_tokens_among_long_chunks_captured():
         graph.replay()
     torch.cuda.synchronize()
     w.check(out, g["pool"], ref)
+
+
+# ------------------------------------------------------------------------------------- decays and values that are no numbers, growth
+def _same(out, pool, ref, rows, head, columns=slice(None), slot=None):
+    """These outputs and, of this slot, these columns of the state are what they are without the spoilt input (tolerances as in
+    Wave.check)."""
+    o, size, want = ref
+    got = out.double().cpu().numpy()[rows, head][..., columns]
+    o, size = o[rows, head][..., columns], size[rows, head][..., columns]
+    assert np.all(np.abs(got - o) <= 2.0 ** -8 * (np.abs(o) + size) + 1e-30)
+    if slot is not None:
+        diff = np.abs(pool[slot, head].double().cpu().numpy() - want[slot, head])[..., columns]
+        assert np.all(diff <= 2.0 ** -15 * np.abs(want[slot, head]).max())
+
+
+SPOILT = [([40], 17), ([30, 200, 70], 30 + 131), ([90, 350], 90 + 2), ([2900], 1501)]
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("chunks,at", SPOILT)
+def test_a_nan_decay_counts_from_its_own_token_on(layout, d, chunks, at):
+    """The state forgets nothing and is no number from there on, in the request and head that the decay belongs to."""
+    w = Wave(chunks, 2, d, seed=at + d, interval=64)
+    ref = w.reference()
+    w.decay[at, 1] = float("nan")
+    g = w.device()
+    out = w.run(g, layout)
+    assert int(g["status"].item()) == 0
+    starts = np.concatenate([[0], np.cumsum(w.C)])
+    for i, (a, b) in enumerate(zip(starts, starts[1:])):
+        slot = int(w.state_out[i])
+        _same(out, g["pool"], ref, slice(a, b), 0, slot=slot)
+        if not a <= at < b:
+            _same(out, g["pool"], ref, slice(a, b), 1, slot=slot)
+            continue
+        _same(out, g["pool"], ref, slice(a, at), 1)
+        assert bool(torch.isnan(out[at:b, 1]).all()) and bool(torch.isnan(g["pool"][slot, 1]).all())
+        for n, snap in enumerate(int(x) for x in w.snaps[i] if x >= 0):
+            if 64 * (n + 1) > at - a:
+                assert bool(torch.isnan(g["pool"][snap, 1]).all())
+            else:
+                _same(out, g["pool"], ref, slice(a, a), 1, slot=snap)
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_nan_decay_of_a_head(layout, d):
+    w = Wave([150, 3], 3, d, seed=d, per_token=False)
+    ref = w.reference()
+    w.decay[1] = float("nan")
+    g = w.device()
+    out = w.run(g, layout)
+    for head in (0, 2):
+        _same(out, g["pool"], ref, slice(0, 153), head, slot=2)
+        _same(out, g["pool"], ref, slice(0, 153), head, slot=3)
+    assert bool(torch.isnan(out[:, 1]).all()) and bool(torch.isnan(g["pool"][2:, 1]).all())
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("chunks,per_token", [([70, 9], False), ([300, 1], True), ([2000], True)])
+def test_decays_above_zero_and_of_both_signs(layout, d, chunks, per_token):
+    rng = np.random.default_rng(chunks[0] + d)
+    decay = rng.uniform(-0.4, 0.3, (sum(chunks), 2)) if per_token else np.array([0.04, -0.02])
+    w = Wave(chunks, 2, d, seed=5, per_token=per_token, decay=decay)
+    g = w.device()
+    out = w.run(g, layout)
+    assert int(g["status"].item()) == 0
+    w.check(out, g["pool"], w.reference())
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("d", [64, 128])
+def test_a_key_and_a_query_that_are_no_numbers_count_from_their_own_tokens_on(layout, d):
+    w = Wave([200, 30], 2, d, seed=d + 2)
+    ref = w.reference()
+    w.q[20, 0, 3] = float("nan")
+    w.k[140, 1, 7] = float("inf")
+    g = w.device()
+    out = w.run(g, layout)
+    _same(out, g["pool"], ref, np.r_[0:20, 21:230], 0, slot=2)
+    _same(out, g["pool"], ref, np.r_[0:140, 200:230], 1, slot=3)
+    assert bool(torch.isnan(out[20, 0]).all()) and not bool(torch.isfinite(out[140:200, 1]).any())
+    rows = np.array([c for c in range(d) if c != 7])
+    diff = np.abs(g["pool"][2, 1].double().cpu().numpy() - ref[2][2, 1])[rows]
+    assert np.all(diff <= 2.0 ** -15 * np.abs(ref[2][2, 1]).max()) and not bool(torch.isfinite(g["pool"][2, 1, 7]).any())

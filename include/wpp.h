@@ -481,7 +481,9 @@ size_t wpp_kda_workspace_bytes(const wpp_kda_desc* desc);
  * with S (head_dim x head_dim, fp32) resumed from the state after exactly the reused prefix and written back at the
  * chunk's end and, optionally, at sparse periodic boundaries.  g is the natural logarithm of the decay, one per head or one
  * per token and head (a gate), -infinity among its values: it forgets everything before.  Values above 0 make the state
- * grow and are not refused.  Heads are independent; no normalisation is applied. */
+ * grow and are not refused; in layouts 0 and 2 growth by more than 2^127 between two tokens of a block counts as infinite.
+ * Heads are independent; no normalisation is applied.  An input that is no finite number counts from its own token on: no output
+ * before it and no other request depends on it. */
 typedef struct {
     int32_t num_requests;   /* R >= 0 */
     int32_t num_heads;      /* H >= 1 */

@@ -11,4 +11,7 @@ __device__ __forceinline__ float decay_log2(const LinearParams& p, int64_t token
     return x < -256.f ? -256.f : x;
 }
 
+// Whether one of the numbers is a NaN or an infinity: `zero` stays +0 while they are finite.
+__device__ __forceinline__ void probe_bf16x2(uint32_t& zero, uint32_t x) { asm("fma.rn.bf16x2 %0, %1, %2, %0;" : "+r"(zero) : "r"(x), "r"(0u)); }
+
 }  // namespace wpp

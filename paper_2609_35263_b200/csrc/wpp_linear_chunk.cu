@@ -56,7 +56,8 @@ struct LinCfg {
     static constexpr int kOffE = kOffG + kLinBlock * 8;                // float [64]: scale e^(G_i)
     static constexpr int kOffW = kOffE + kLinBlock * 4;                // float [64]: e^(G_L - G_j)
     static constexpr int kOffA = kOffW + kLinBlock * 4;                // float: e^(G_L); double: G_L
-    static constexpr int kBytes = kOffA + 16;
+    static constexpr int kOffSpoilt = kOffA + 16;                      // int [D]: see spoilt
+    static constexpr int kBytes = kOffSpoilt + D * 4;
 };
 
 __device__ __forceinline__ int64_t lin_slot(const LinearParams& p, int slot) {
@@ -77,6 +78,8 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
     float* s_w = reinterpret_cast<float*>(smem + Cf::kOffW);
     float* s_a = reinterpret_cast<float*>(smem + Cf::kOffA);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+    // Of the warp's 16 columns: the block's first token whose value is no number (written and read where there is one)
+    volatile int* spoilt = reinterpret_cast<volatile int*>(smem + Cf::kOffSpoilt) + 16 * warp;
     grid_launch_dependents();
     grid_dependency_wait();
 
@@ -265,6 +268,40 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
 #pragma unroll
         for (int ks = 0; ks < 4; ++ks)
             ldsm_4_trans(v[ks], tile_at(sv, 16 * ks + (lane & 7) + ((lane >> 4) << 3), 2 * warp + ((lane >> 3) & 1)));
+        // Values that are no numbers stand in P's product beside zeros as well, and would reach the tokens before them.  They are zeros
+        // for the products; the outputs and the state of their columns are NaN from their tokens on.
+        bool any_spoilt = false;
+        if (!kFirst) {
+            uint32_t zero = 0u;
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) probe_bf16x2(zero, v[ks][c]);
+            any_spoilt = __any_sync(0xffffffffu, zero != 0u);
+            if (__builtin_expect(any_spoilt, 0)) {
+                int first[2] = {kLinBlock, kLinBlock};  // of rows g and g + 8
+#pragma unroll
+                for (int ks = 3; ks >= 0; --ks)
+#pragma unroll
+                    for (int c = 3; c >= 0; --c)
+#pragma unroll
+                        for (int h = 1; h >= 0; --h)
+                            if ((v[ks][c] >> (16 * h) & 0x7f80u) == 0x7f80u) {
+                                first[c & 1] = 16 * ks + 8 * (c >> 1) + 2 * t + h;
+                                v[ks][c] &= h ? 0x0000ffffu : 0xffff0000u;
+                            }
+#pragma unroll
+                for (int w = 1; w < 4; w *= 2) {
+                    first[0] = min(first[0], __shfl_xor_sync(0xffffffffu, first[0], w));
+                    first[1] = min(first[1], __shfl_xor_sync(0xffffffffu, first[1], w));
+                }
+                if (t == 0) {
+                    spoilt[g] = first[0];
+                    spoilt[g + 8] = first[1];
+                }
+                __syncwarp();
+            }
+        }
         if (!kFirst) {
             // ---- O^T = e^(G_i) S^T Q^T + V^T P^T, 32 tokens at a time
 #pragma unroll
@@ -299,6 +336,13 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
                         lin_mma(o[2 * nn], v[ks], b[0], b[1]);
                         lin_mma(o[2 * nn + 1], v[ks], b[2], b[3]);
                     }
+                if (__builtin_expect(any_spoilt, 0)) {
+#pragma unroll
+                    for (int nt = 0; nt < 4; ++nt)
+#pragma unroll
+                        for (int c = 0; c < 4; ++c)
+                            if (32 * half + 8 * nt + 2 * t + (c & 1) >= spoilt[g + 8 * (c >> 1)]) o[nt][c] = NAN;
+                }
                 // two 8 x 8 pieces turned round in registers: the thread has columns 2 t, 2 t + 1 of token g
 #pragma unroll
                 for (int nt = 0; nt < 4; ++nt) {
@@ -313,6 +357,15 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
                     }
                 }
             }
+        }
+        if (__builtin_expect(any_spoilt, 0)) {                              // the state's columns are NaN from here on: the first such value is one again
+#pragma unroll
+            for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int ahead = spoilt[g + 8 * (c & 1)] - (16 * ks + 8 * (c >> 1) + 2 * t);
+                    if (ahead == 0 || ahead == 1) v[ks][c] |= 0x7fc0u << (16 * ahead);
+                }
         }
         // ---- S^T = e^(G_L) S^T + (e^(G_L - G_j) V)^T K, the weighted V in two bf16 terms
         {

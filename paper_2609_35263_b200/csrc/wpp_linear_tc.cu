@@ -4,6 +4,8 @@
 //     (1) S1 = Q K^T          (2) O2 = P V, P_ij = scale e^(G_i - G_j) S1_ij for j <= i, as bf16 where S1 was
 //     (3) O1 = Q bf16(S)      (4) S = e^(G_L) S + (w K)^T V, the weighted K in two bf16 terms (16 bits of every product's factor)
 //     o_i = scale e^(G_i) O1_i + O2_i
+// (2) has zeros for j > i, and zero times what is no number is none either: outputs that are not finite are looked into and, where V is
+// the reason, made again without the products (outputs_again; the look costs 1.5 % of a block).
 // 16 warps, by warpgroup:
 //   warps 0-3    thread = token: P, and at the block's end the outputs
 //   warps 4-7    thread = row of S: bf16(S) into shared memory for (3), e^(G_L) S back, snapshots, first and last states
@@ -84,11 +86,77 @@ __device__ __noinline__ void state_to_memory(uint32_t taddr, float4* to, int apa
     }
 }
 
+// Outputs of a block in which there is something that is no number.  If that is in V, it stands in (2) beside the zeros above P's diagonal
+// too, and reaches the tokens before it.  Then the warp's outputs are made once more, in fp32 and from tokens j <= i alone.  row0: the
+// block's first row; e1: scale e^(G_i) of this thread's token r.  Rarely called, and slow: about a millisecond for a block.
+__device__ __noinline__ void outputs_again(const LinearChunkParams& p, int64_t row0, int len, int r, int head, float e1, uint32_t t_o1) {
+    const int lane = r & 31;
+    uint32_t zero = 0u;
+    for (int j = lane; j < len; j += 32) {
+        const uint4* v = reinterpret_cast<const uint4*>(p.v + (row0 + j) * p.v_token_stride + (int64_t)head * kD);
+#pragma unroll 4
+        for (int c = 0; c < 16; ++c) {
+            const uint4 x = v[c];
+            probe_bf16x2(zero, x.x); probe_bf16x2(zero, x.y); probe_bf16x2(zero, x.z); probe_bf16x2(zero, x.w);
+        }
+    }
+    if (!__any_sync(0xffffffffu, zero != 0u)) return;
+    const int row = min(r, len - 1), last = min(r | 31, len - 1);
+    const uint4* q = reinterpret_cast<const uint4*>(p.q + (row0 + row) * p.q_token_stride + (int64_t)head * kD);
+#pragma unroll 1
+    for (int part = 0; part < 4; ++part) {             // 32 columns at a time
+        float y[32];
+        __syncwarp();
+        tmem_ld32(t_o1 + 32 * part, reinterpret_cast<uint32_t*>(y));
+        tmem_wait_ld();
+#pragma unroll
+        for (int c = 0; c < 32; ++c) y[c] *= e1;
+        double fall = 0.0;                             // logarithm of what token j's term has left at token `row`
+#pragma unroll 1
+        for (int j = last; j >= 0; --j) {
+            if (j > row) continue;
+            const uint4* k = reinterpret_cast<const uint4*>(p.k + (row0 + j) * p.k_token_stride + (int64_t)head * kD);
+            const uint4* v = reinterpret_cast<const uint4*>(p.v + (row0 + j) * p.v_token_stride + (int64_t)head * kD + 32 * part);
+            float dot = 0.f;
+#pragma unroll 2
+            for (int c = 0; c < 16; ++c) {
+                const uint4 a = q[c], b = k[c];
+                const uint32_t aa[4] = {a.x, a.y, a.z, a.w}, bb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    dot = fmaf(__uint_as_float(aa[i] << 16), __uint_as_float(bb[i] << 16), dot);
+                    dot = fmaf(__uint_as_float(aa[i] & 0xffff0000u), __uint_as_float(bb[i] & 0xffff0000u), dot);
+                }
+            }
+            const float w = p.scale * fast_exp2((float)fall) * dot;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const uint4 b = v[c];
+                const uint32_t bb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    y[8 * c + 2 * i] = fmaf(w, __uint_as_float(bb[i] << 16), y[8 * c + 2 * i]);
+                    y[8 * c + 2 * i + 1] = fmaf(w, __uint_as_float(bb[i] & 0xffff0000u), y[8 * c + 2 * i + 1]);
+                }
+            }
+            fall += (double)decay_log2(p, row0 + j, head);
+        }
+        __syncwarp();
+        if (r < len) {
+            uint4* to = reinterpret_cast<uint4*>(p.out + (row0 + r) * p.o_token_stride + (int64_t)head * kD + 32 * part);
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                to[c] = make_uint4(pack_bf16x2(y[8 * c], y[8 * c + 1]), pack_bf16x2(y[8 * c + 2], y[8 * c + 3]),
+                                   pack_bf16x2(y[8 * c + 4], y[8 * c + 5]), pack_bf16x2(y[8 * c + 6], y[8 * c + 7]));
+        }
+    }
+}
+
 // kFirst: the pass that leaves the segments' own states (no outputs: (4) alone)
 template <bool kFirst>
 __global__ void __launch_bounds__(kThreads, 1)
 wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
-                     const LinearChunkParams p) {
+                     const __grid_constant__ LinearChunkParams p) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     uint8_t* gen = smem_raw + (base - smem_u32(smem_raw));
@@ -490,6 +558,8 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             if (!__all_sync(0xffffffffu, mbar_wait(bO, b & 1u, abort_flag))) break;
             tc_fence_after();
             const __nv_bfloat16* dst = p.out + (row0 + walk.at + r) * p.o_token_stride + (int64_t)head * kD;
+            uint64_t finite = 0ull;                    // two numbers, as long as the outputs are (or numbers whose products are none)
+            bool again = false;
 #pragma unroll 1
             for (int q = 0; q < 4; ++q) {
                 float x[32], z[32];
@@ -497,17 +567,33 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 tmem_ld32(lane_addr + kColO2 + 32 * q, reinterpret_cast<uint32_t*>(z));
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; i += 2) unpack2(ffma2(pack2(x[i], x[i + 1]), e2, pack2(z[i], z[i + 1])), x[i], x[i + 1]);
+                for (int i = 0; i < 32; i += 4) {
+                    const uint64_t a = ffma2(pack2(x[i], x[i + 1]), e2, pack2(z[i], z[i + 1])), b = ffma2(pack2(x[i + 2], x[i + 3]), e2, pack2(z[i + 2], z[i + 3]));
+                    finite = ffma2(a, b, finite);
+                    unpack2(a, x[i], x[i + 1]);
+                    unpack2(b, x[i + 2], x[i + 3]);
+                }
                 uint4 w[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
                     w[i] = make_uint4(pack_bf16x2(x[8 * i], x[8 * i + 1]), pack_bf16x2(x[8 * i + 2], x[8 * i + 3]),
                                       pack_bf16x2(x[8 * i + 4], x[8 * i + 5]), pack_bf16x2(x[8 * i + 6], x[8 * i + 7]));
                 if (q == 3) {
-                    tc_fence_before();
-                    mbar_arrive(bOFree);
+                    float f0, f1;
+                    unpack2(finite, f0, f1);
+                    again = __any_sync(0xffffffffu, r < len && !(fabsf(f0) + fabsf(f1) <= 3.402823466e+38f));
+                    if (!again) {
+                        tc_fence_before();
+                        mbar_arrive(bOFree);
+                    }
                 }
                 warp_store_rows64(gen + Smem::kOffStage + warp * 2048, lane, w, dst, r < len, q * 64);
+            }
+            if (__builtin_expect(again, 0)) {
+                __syncwarp();
+                outputs_again(p, row0 + walk.at, len, r, head, e1, lane_addr + kColO1);
+                tc_fence_before();
+                mbar_arrive(bOFree);
             }
         }
     }

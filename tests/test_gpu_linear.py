@@ -339,6 +339,37 @@ def test_decays_above_zero_and_of_both_signs(layout, d, chunks, per_token):
 
 @pytest.mark.parametrize("layout", LAYOUTS)
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("chunks,at", SPOILT)
+@pytest.mark.parametrize("value", [float("inf"), float("nan")])
+def test_a_value_that_is_no_number_counts_from_its_own_token_on(layout, d, chunks, at, value):
+    """o_i depends on v_j for j <= i alone, and column by column: the tokens before it in the same block and the other columns
+    are what they are without it."""
+    w = Wave(chunks, 2, d, seed=at + d + 1)
+    ref = w.reference()
+    w.v[at, 1, 5] = value
+    w.v[at, 1, d - 1] = -value
+    w.v[at + 1, 1, 5] = float("nan")
+    w.v[at + 4, 1, 40] = value
+    first = {5: at, d - 1: at, 40: at + 4}
+    others = np.array([c for c in range(d) if c not in first])
+    g = w.device()
+    out = w.run(g, layout)
+    assert int(g["status"].item()) == 0
+    starts = np.concatenate([[0], np.cumsum(w.C)])
+    for i, (a, b) in enumerate(zip(starts, starts[1:])):
+        slot = int(w.state_out[i])
+        _same(out, g["pool"], ref, slice(a, b), 0, slot=slot)
+        _same(out, g["pool"], ref, slice(a, b), 1, others, slot)
+        if not a <= at < b:
+            _same(out, g["pool"], ref, slice(a, b), 1, slot=slot)
+            continue
+        for c, j in first.items():
+            _same(out, g["pool"], ref, slice(a, j), 1, np.array([c]))
+            assert not bool(torch.isfinite(out[j:b, 1, c]).any()) and not bool(torch.isfinite(g["pool"][slot, 1, :, c]).any())
+
+
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("d", [64, 128])
 def test_a_key_and_a_query_that_are_no_numbers_count_from_their_own_tokens_on(layout, d):
     w = Wave([200, 30], 2, d, seed=d + 2)
     ref = w.reference()

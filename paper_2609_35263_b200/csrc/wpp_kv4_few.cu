@@ -3,8 +3,8 @@
 //
 // With k_j = least_j + scale_j c_j (c_j the codes), the score of key j for row n is
 //     sm_scale (scale_j <q_n, c_j> + least_j sum q_n),
-// so the tensor cores multiply the codes themselves, which bf16 holds exactly, and two numbers per key finish the score in fp32;
-// in the same way sum_j p_j v_j = sum_j (p_j scale_j) c_j + sum_j p_j least_j, of which only p_j scale_j is rounded to bf16.
+// so the tensor cores multiply the codes themselves, which f16 holds exactly, and two numbers per key finish the score in fp32;
+// in the same way sum_j p_j v_j = sum_j (p_j scale_j) c_j + sum_j p_j least_j, of which only p_j scale_j is rounded to f16.
 //
 // What bounds it is the cache's bytes, and close behind them the ALU's instructions that turn codes into numbers a product takes.  So
 // nothing else is done per code: a warp takes 32 keys at a time straight from global memory in the order the tensor cores' fragments
@@ -14,7 +14,8 @@
 // A mask makes the codes f16 numbers 1024 + c or 1024 + 16 c, a packed f16 operation c - 8, both exact.  (As e4m3 numbers, which
 // bytes below 16 are with no operation at all, they come to more: the products of 8-bit numbers take them apart into f16 ones by
 // themselves.)  V's codes of two keys first stand above one another by a byte permutation.  Q is taken as f16 times a power of two
-// per row, P scale_j is rounded to f16 (2^-11).
+// per row.  p_j scale_j is rounded to f16 times a power of two per row and warp that puts the largest one so far between 2^6 and 2^15: it
+// is off by 2^-11 of itself or by 2^-31 of that largest one, of which a million keys of a warp make 2^-11, however wide the rows of V.
 //
 // Measured: 64 requests of one token behind 255 to 16,383 keys, 64/8 heads of 128, 124 us (the copies alone 93, the bytes at the measured copy
 // bandwidth 82); four behind 131,071 120 us (87).  Three CTAs an SM of blocks of at most 8 rows: with four, which leaves the
@@ -33,7 +34,8 @@ namespace wpp {
 constexpr int kFewWarps = 4;
 constexpr int kFewKeys = 32;               // a warp's keys at a time
 constexpr float kFewSlack = 8.f;           // a row keeps its reference while its scores stay below reference + 8 (log2)
-constexpr float kFewScaleSlack = 128.f;    // and a warp its reference of V's scales while they stay below so many times that: p scale < 2^15
+constexpr float kFewMostProduct = 32768.f; // p scale times a row's power of two stays within f16's range; moved, it is in [2^6, 2^7)
+constexpr float kFewMostPower = 120.f;     // log2 of that power at most (there is no scale below 2^-100)
 
 // D += A B, 16 x 8 x 16, f16 in, fp32 out
 __device__ __forceinline__ void mma_f16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -112,9 +114,9 @@ __device__ __forceinline__ float pair_scale(uint32_t p) { return __uint_as_float
 // The running state of a warp's columns (query rows): lane 4 g + t has columns 2 t and 2 t + 1 of every eight.
 template <int D, int NT>
 struct FewState {
-    float o[NT][D / 16][4];            // O^T / v_ref
+    float o[NT][D / 16][4];            // O^T power
     float m[NT][2], l[NT][2], off[NT][2];            // off: sum of p (least + 8 scale) over this lane's keys
-    float v_ref, v_inv;                // a power of two that V's scales are taken relative to
+    float power[NT][2];                // of two, that makes p scale an f16 number
 };
 
 // 32 keys, at shared-memory address `at`.  Lane 4 g + t takes, of a tile's rows g and g + 8, columns [t D / 4, (t + 1) D / 4) of K; of
@@ -189,18 +191,7 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
             mx[nt][c] = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
             move |= mx[nt][c] > kFewSlack;
         }
-    float v = fmaxf(fmaxf(vs[0][0], vs[0][1]), fmaxf(vs[1][0], vs[1][1]));
-    move |= v * st.v_inv > kFewScaleSlack;
     if (__any_sync(0xffffffffu, move)) {
-#pragma unroll
-        for (int w = 4; w < 32; w *= 2) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, w));
-        float shrink = 1.f;
-        if (v * st.v_inv > 1.f) {
-            const float ref = __uint_as_float(min((__float_as_uint(v) & 0x7f800000u) + 0x00800000u, 0x7e800000u));     // (2^126 at most)
-            shrink = st.v_ref * __frcp_rn(ref);
-            st.v_ref = ref;
-            st.v_inv = __frcp_rn(ref);
-        }
 #pragma unroll
         for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -210,7 +201,15 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
 #pragma unroll
                 for (int w = 4; w < 32; w *= 2) y = fmaxf(y, __shfl_xor_sync(0xffffffffu, y, w));
                 if (kMasked && y == -INFINITY) y = 0.f;
+                y = ceilf(y);
                 const float a = first ? 1.f : fast_exp2(-y);
+                // (scores and power move together: what is summed up keeps its size, unless the power is the largest already)
+                float shrink = 1.f;
+                if (!first) {
+                    const float e = (float)((int)(__float_as_uint(st.power[nt][c]) >> 23) - 127), e1 = fminf(e + y, kFewMostPower);
+                    st.power[nt][c] = __uint_as_float((uint32_t)((int)e1 + 127) << 23);
+                    shrink = fast_exp2((e1 - e) - y);
+                }
                 st.m[nt][c] += y;
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -221,31 +220,60 @@ __device__ __forceinline__ void few_step(FewState<D, NT>& st, const uint32_t at,
                 st.off[nt][c] *= a;
 #pragma unroll
                 for (int mt = 0; mt < D / 16; ++mt) {
-                    st.o[nt][mt][c] *= a * shrink;
-                    st.o[nt][mt][2 + c] *= a * shrink;
+                    st.o[nt][mt][c] *= shrink;
+                    st.o[nt][mt][2 + c] *= shrink;
                 }
             }
     }
-    // ---- P^T, its rows times the keys' V scales, turned round into the second factor of O^T = V^T P^T
+    // ---- P^T, its rows times the keys' V scales and the columns' powers, turned round into the second factor of O^T = V^T P^T
+    float top[NT][2];
+    bool above = false;
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    float& y = s[h][nt][2 * i + c];
+                    const bool out = kMasked && key0 + 16 * h + 8 * i + kg > limit[nt][c];
+                    const float e = out ? 0.f : fast_exp2(y);
+                    st.l[nt][c] += e;
+                    st.off[nt][c] = out ? st.off[nt][c] : fmaf(e, vo[h][i], st.off[nt][c]);
+                    y = e * vs[h][i];
+                }
+            top[nt][c] = fmaxf(fmaxf(s[0][nt][c], s[0][nt][2 + c]), fmaxf(s[1][nt][c], s[1][nt][2 + c]));
+            above |= top[nt][c] * st.power[nt][c] > kFewMostProduct;
+        }
+    }
+    if (__any_sync(0xffffffffu, above)) {
+#pragma unroll
+        for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                float x = top[nt][c];
+#pragma unroll
+                for (int w = 4; w < 32; w *= 2) x = fmaxf(x, __shfl_xor_sync(0xffffffffu, x, w));
+                // 2^(6 - e) where x is in [2^e, 2^(e + 1)), and never more than it was
+                const int e = 260 - (int)(__float_as_uint(x) >> 23 & 0xffu);
+                const float power = fminf(st.power[nt][c], __uint_as_float((uint32_t)min(e, 254) << 23)), shrink = power * __frcp_rn(st.power[nt][c]);
+                st.power[nt][c] = power;
+#pragma unroll
+                for (int mt = 0; mt < D / 16; ++mt) {
+                    st.o[nt][mt][c] *= shrink;
+                    st.o[nt][mt][2 + c] *= shrink;
+                }
+            }
+    }
     uint32_t pb[2][NT][2];
 #pragma unroll
     for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float vi = vs[h][i] * st.v_inv;
+        for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int nt = 0; nt < NT; ++nt) {
-                float e[2];
-#pragma unroll
-                for (int c = 0; c < 2; ++c) {
-                    const bool out = kMasked && key0 + 16 * h + 8 * i + kg > limit[nt][c];
-                    e[c] = out ? 0.f : fast_exp2(s[h][nt][2 * i + c]);
-                    st.l[nt][c] += e[c];
-                    st.off[nt][c] = out ? st.off[nt][c] : fmaf(e[c], vo[h][i], st.off[nt][c]);
-                }
-                pb[h][nt][i] = transpose_8x8(pack_f16x2(e[0] * vi, e[1] * vi));
-            }
-        }
+            for (int nt = 0; nt < NT; ++nt)
+                pb[h][nt][i] = transpose_8x8(pack_f16x2(s[h][nt][2 * i] * st.power[nt][0], s[h][nt][2 * i + 1] * st.power[nt][1]));
     // ---- O^T += (codes - 8)^T P^T: a word holds four codes of one key and of the next, one above the other
     const uint32_t v_at = at + M::kRows + g * (D / 16);
     const int flip = kt & 1 ? -(D / 2) : D / 2;                        // from row 2 t's key to row 2 t + 1's
@@ -403,11 +431,10 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             st.m[nt][i] = 0.f;
+            st.power[nt][i] = 1.329227996e36f;         // 2^120
             st.l[nt][i] = st.off[nt][i] = 0.f;
         }
     }
-    st.v_ref = 8.67361738e-19f;        // 2^-60
-    st.v_inv = 1.15292150e18f;
 
     bool first = true;
     uint32_t at = 0, fill = (M::kDepth - 1) * M::kStage;               // offsets in the ring: of the keys, and of the next ones to be asked for
@@ -433,6 +460,7 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
             float l = st.l[nt][c], off = st.off[nt][c];
+            const float inverse = __frcp_rn(st.power[nt][c]);
 #pragma unroll
             for (int w = 4; w < 32; w *= 2) {
                 l += __shfl_xor_sync(0xffffffffu, l, w);
@@ -444,7 +472,7 @@ __device__ __forceinline__ void few_unit(const Kv4AttnParams& p, const int unit,
             for (int mt = 0; mt < kSteps; ++mt) {
                 const int d0 = g * (D / 8) + 2 * mt;       // element 8 w + 4 hw + 2 u of the thread's columns, mt = 4 w + 2 hw + u
                 *reinterpret_cast<float2*>(&s_o[warp][n][d0]) =
-                    make_float2(fmaf(st.o[nt][mt][c], st.v_ref, off), fmaf(st.o[nt][mt][2 + c], st.v_ref, off));
+                    make_float2(fmaf(st.o[nt][mt][c], inverse, off), fmaf(st.o[nt][mt][2 + c], inverse, off));
             }
         }
     __syncthreads();

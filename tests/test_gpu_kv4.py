@@ -302,3 +302,59 @@ def test_captured_and_replayed_and_on_two_streams(C, shape):
     w.k_pool, w.v_pool = want_k, want_v
     w.check(outs[0], None, w.reference())
     assert int(g["status"].item()) == 0
+
+
+# --------------------------------------------------------------------------------------------------- value rows of unequal sizes
+def _along(w, rng, scores, values):
+    """Keys whose score with every query is about scores[j] (natural logarithms) and value rows values[j], of request 0 and head 0."""
+    n, d = values.shape
+    base = rng.standard_normal(d)
+    w.q = okv4.bf16_bits(np.broadcast_to(base, w.q.shape).astype(np.float32) + 0.02 * rng.standard_normal(w.q.shape).astype(np.float32))
+    keys = scores[:, None] * base / (d ** -0.5 * (base @ base)) + 0.05 * rng.standard_normal((n, d))
+    for pool, x in ((w.k_pool, keys), (w.v_pool, values)):
+        codes, pairs = okv4.pack_rows(okv4.bf16_bits(x.astype(np.float32)))
+        for j in range(n):
+            okv4.write_row(pool, w.table[0, j // w.B], 0, j % w.B, w.B, codes[j], pairs[j])
+
+
+def _values(kind, n, d, rng):
+    """(scores, value rows) of n keys."""
+    scores, values = rng.uniform(-3, 3, n), rng.standard_normal((n, d))
+    if kind.startswith("one wide row that nobody attends to"):
+        scores[n // 3], values[n // 3] = -60.0, values[n // 3] * 2.0 ** int(kind.split()[-1])
+    elif kind.startswith("a dominant key, a flat tail and one wide row"):
+        gap, width = (float(x) for x in kind.split()[-2:])
+        scores[:], scores[5] = 0.0, gap * np.log(2)
+        values[:] = values[0]
+        values[n // 2] *= width
+    elif kind == "tiny":                                               # (scales just above 2^-100, below which a row has none)
+        values *= 2.0 ** -90
+    elif kind == "any size":
+        values *= 2.0 ** rng.uniform(-30, 30, (n, 1))
+    elif kind == "wider as the scores fall":
+        scores = np.linspace(30, -30, n)
+        values *= np.exp(-scores[:, None])
+    elif kind == "narrower as the scores rise":
+        scores = np.linspace(-30, 30, n)
+        values *= np.exp(-scores[:, None])
+    elif kind == "rows of one value behind others":
+        scores[n // 2:] += np.linspace(0, 70, n - n // 2)
+        values[n // 2:] = np.round(values[n // 2:, :1], 1)
+        values[n // 2::3] = 0.0
+    return scores, values
+
+
+@pytest.mark.parametrize("kind", [f"one wide row that nobody attends to, 2 ** {e}" for e in (6, 20, 40)] +
+                         [f"a dominant key, a flat tail and one wide row, {a} {b}" for a, b in ((18, 256), (16, 1000), (14, 4000))] +
+                         ["tiny", "any size", "wider as the scores fall", "narrower as the scores rise", "rows of one value behind others"])
+@pytest.mark.parametrize("d,Hq,C,n", [(128, 4, 1, 12000), (64, 5, 3, 3000), (128, 3, 40, 1100)])
+def test_value_rows_of_unequal_sizes(kind, d, Hq, C, n):
+    """What a row of V weighs decides what it does, not how wide it is."""
+    w = Wave([n - C], [C], Hq, 1, d, 64, seed=n + d)
+    rng = np.random.default_rng(n)
+    _along(w, rng, *_values(kind, n, d, rng))
+    g, ref = w.device(), w.reference()
+    for shape, splits in ((2, 1), (2, 3), (1, 1), (1, 2)):
+        out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
+        assert int(g["status"].item()) == 0
+        w.check(out, lse, ref)

@@ -367,12 +367,13 @@ wpp_kv4_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     bad |= !there;
                     block[h] = pool + (there ? page[h] : 0) * p.page_bytes;
                 }
+                // (coherent loads: the append before may still write the pool while this kernel is set up)
 #pragma unroll
                 for (int i = 0; i < R::kRows; ++i) {
                     const uint8_t* from = block[i * kApart / 16];
-                    asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
                                  : "=r"(x.x[i].x), "=r"(x.x[i].y), "=r"(x.x[i].z), "=r"(x.x[i].w) : "l"(from + bytes_of[i]));
-                    asm volatile("ld.global.nc.L1::no_allocate.u32 %0, [%1];" : "=r"(x.pair[i]) : "l"(from + pair_of[i]));
+                    asm volatile("ld.global.L1::no_allocate.u32 %0, [%1];" : "=r"(x.pair[i]) : "l"(from + pair_of[i]));
                 }
                 if ((step_at + 1) * 128 > v.kv_len) {  // what lies behind the sequence counts as zeros
 #pragma unroll

@@ -39,6 +39,19 @@ def test_an_append_grid_that_is_set_up_early_fits_the_sms():
     assert re.search(r"q\.few = total <= \(int64_t\)num_sms \* wpp::kAppendCtas \* 256;", src)
 
 
+def test_kernels_that_are_set_up_early_read_no_memory_as_constant():
+    """The non-coherent path is for memory that nobody writes while the kernel lives, and such a kernel lives beside the end of the one
+    before it, which may write all that it reads.  (A const __restrict__ pointer lets the compiler take that path.)"""
+    seen = 0
+    for path, name, body in _kernels():
+        if "grid_dependency_wait()" not in body:
+            continue
+        seen += 1
+        for word in ("ld.global.nc", "__ldg(", "__restrict__"):
+            assert word not in body, f"{path}: {name} uses {word}"
+    assert seen >= 12
+
+
 @pytest.mark.gpu
 def test_small_attention_directly_behind_the_two_pass_recurrent_layer():
     """The chain kernel takes all 512 columns of an SM's tensor memory, the small attention shape 256 per CTA: queued behind

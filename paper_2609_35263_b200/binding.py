@@ -527,6 +527,13 @@ def _token_stride(x, where: str) -> int:
     return int(x.stride(0)) if x.shape[0] > 1 else int(x.shape[1] * x.shape[2])
 
 
+def _state_slots(pool, shape, where: str) -> int:
+    """Slots of a pool of recurrent states: fp32 [slots, *shape] without gaps, because the kernels read and write whole slots of it."""
+    if pool.dtype != torch.float32 or tuple(pool.shape[1:]) != shape or not pool.is_contiguous():
+        raise WppError(1, where)
+    return int(pool.shape[0])
+
+
 def wpp_linear_chunk(ctx: Context, q, k, v, log_decay, row_offsets, state_pool, state_in, state_out, out=None,
                      prefix_lens=None, snap_interval: int = 0, snap_slots=None, status=None, stream=None, layout: int = 0,
                      workspace=None, scale: float = 1.0):
@@ -550,7 +557,8 @@ def wpp_linear_chunk(ctx: Context, q, k, v, log_decay, row_offsets, state_pool, 
     decay_stride = 0 if not per_token else int(log_decay.stride(0)) if T > 1 else H
     strides = [_token_stride(x, "wpp_linear_chunk") for x in (q, k, v, out)]
     max_snaps = 0 if snap_slots is None else int(snap_slots.shape[1])
-    desc = LinearDesc(R, H, d, int(state_pool.shape[0]), int(snap_interval), max_snaps, int(layout), float(scale), T, *strides, decay_stride)
+    slots = _state_slots(state_pool, (H, d, d), "wpp_linear_chunk")
+    desc = LinearDesc(R, H, d, slots, int(snap_interval), max_snaps, int(layout), float(scale), T, *strides, decay_stride)
     ws_bytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
     st = _call.linear_chunk(ctx.handle.value, desc, q, k, v, log_decay, row_offsets, prefix_lens, state_pool, state_in, state_out,
                             snap_slots, out, workspace, ws_bytes, status, _stream(ctx, stream))

@@ -100,3 +100,36 @@ def test_shapes_and_orders_that_are_refused(kw):
 def test_an_integer_is_no_memory(name):
     with pytest.raises(AttributeError):
         _call(**{name: 64})
+
+
+# ----------------------------------------------------------------------------------- what the binding refuses before the library sees it
+@pytest.fixture
+def queued(monkeypatch):
+    """The calls that would have reached the library."""
+    B.load_library()
+    calls = []
+
+    class Calls:
+        @staticmethod
+        def linear_chunk(*a):
+            calls.append(a)
+            return 0
+    monkeypatch.setattr(B, "_call", Calls)
+    return calls
+
+
+def test_a_call_that_is_right_is_queued(queued):
+    _call()
+    assert len(queued) == 1
+
+
+@pytest.mark.parametrize("pool", [
+    torch.zeros(3, 1, 64, 64), torch.zeros(3, 2, 64, 32), torch.zeros(3, 2, 32, 64), torch.zeros(3, 2, 64 * 64), torch.zeros(2, 64, 64),
+    torch.zeros(3, 2, 64, 64, dtype=torch.bfloat16), torch.zeros(3, 2, 64, 64, dtype=torch.float64), torch.zeros(3, 2, 64, 128)[..., ::2],
+    torch.zeros(6, 2, 64, 64)[::2], torch.zeros(3, 2, 64, 64).transpose(2, 3)],
+    ids=["a head too few", "half the width", "half the height", "flat", "no slots", "bf16", "fp64", "gaps in rows", "gaps between slots", "transposed"])
+def test_a_pool_that_is_not_one_of_such_states_is_refused(queued, pool):
+    """The kernels write whole slots: of a smaller pool they would write what lies behind it."""
+    with pytest.raises(wpp.WppError) as e:
+        _call(state_pool=pool)
+    assert e.value.status == 1 and not queued

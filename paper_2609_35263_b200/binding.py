@@ -524,7 +524,11 @@ def _token_stride(x, where: str) -> int:
     """Elements from a token to the next of x [T, H, d], whose heads have to lie side by side."""
     if x.dim() != 3 or x.stride(2) != 1 or (x.shape[1] > 1 and x.stride(1) != x.shape[2]):
         raise WppError(1, where)
-    return int(x.stride(0)) if x.shape[0] > 1 else int(x.shape[1] * x.shape[2])
+    if x.shape[0] <= 1:
+        return int(x.shape[1] * x.shape[2])
+    if x.stride(0) == 0:               # one row for all tokens; to the library a stride of 0 means rows behind one another
+        raise WppError(1, where)
+    return int(x.stride(0))
 
 
 def _state_slots(pool, shape, where: str) -> int:

@@ -133,3 +133,23 @@ def test_a_pool_that_is_not_one_of_such_states_is_refused(queued, pool):
     with pytest.raises(wpp.WppError) as e:
         _call(state_pool=pool)
     assert e.value.status == 1 and not queued
+
+
+@pytest.mark.parametrize("name", ["q", "k", "v", "out"])
+def test_one_row_for_all_tokens_is_refused(queued, name):
+    """A broadcast row has a stride of 0, which the library takes for rows behind one another: it would read and write behind the row."""
+    row = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    with pytest.raises(wpp.WppError) as e:
+        _call(**{name: row.expand(4, 2, 64)})
+    assert e.value.status == 1 and not queued
+
+
+def test_one_token_may_have_any_stride(queued):
+    x = torch.zeros(1, 2, 64, dtype=torch.bfloat16)
+    _call(q=x.expand(1, 2, 64), k=x.as_strided((1, 2, 64), (0, 64, 1)), v=x, out=x, log_decay=torch.zeros(1, 2))
+    assert queued[0][1].q_token_stride == queued[0][1].k_token_stride == 128
+
+
+def test_one_row_of_decays_for_all_tokens_is_a_decay_per_head(queued):
+    _call(log_decay=torch.zeros(2).expand(4, 2))
+    assert queued[0][1].decay_token_stride == 0

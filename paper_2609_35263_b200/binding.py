@@ -558,6 +558,13 @@ def wpp_linear_chunk(ctx: Context, q, k, v, log_decay, row_offsets, state_pool, 
     per_token = log_decay.dim() == 2
     if tuple(log_decay.shape) != ((T, H) if per_token else (H,)) or (H > 1 and log_decay.stride(-1) != 1):
         raise WppError(1, "wpp_linear_chunk")
+    # (what the kernels read by the type and the number of requests that the library is told)
+    if log_decay.dtype != torch.float32 or row_offsets.dtype != torch.int64:
+        raise WppError(1, "wpp_linear_chunk")
+    if min(x.numel() for x in (state_in, state_out, state_in if prefix_lens is None else prefix_lens)) < R:
+        raise WppError(1, "wpp_linear_chunk")
+    if snap_slots is not None and (snap_slots.dim() != 2 or snap_slots.shape[0] < R or not snap_slots.is_contiguous()):
+        raise WppError(1, "wpp_linear_chunk")
     decay_stride = 0 if not per_token else int(log_decay.stride(0)) if T > 1 else H
     strides = [_token_stride(x, "wpp_linear_chunk") for x in (q, k, v, out)]
     max_snaps = 0 if snap_slots is None else int(snap_slots.shape[1])

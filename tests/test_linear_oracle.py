@@ -153,3 +153,18 @@ def test_one_token_may_have_any_stride(queued):
 def test_one_row_of_decays_for_all_tokens_is_a_decay_per_head(queued):
     _call(log_decay=torch.zeros(2).expand(4, 2))
     assert queued[0][1].decay_token_stride == 0
+
+
+_I32 = dict(dtype=torch.int32)
+
+
+@pytest.mark.parametrize("kw", [
+    dict(log_decay=torch.zeros(4, 2, dtype=torch.bfloat16)), dict(log_decay=torch.zeros(2, dtype=torch.float16)),
+    dict(row_offsets=torch.zeros(2, **_I32)), dict(state_in=torch.zeros(0, **_I32)), dict(state_out=torch.zeros(0, **_I32)),
+    dict(prefix_lens=torch.zeros(0, **_I32), snap_interval=2), dict(snap_slots=torch.zeros(2, **_I32)),
+    dict(snap_slots=torch.zeros(0, 2, **_I32)), dict(snap_slots=torch.zeros(1, 4, **_I32)[:, ::2])],
+    ids=["bf16 decays", "fp16 decays", "32-bit offsets", "no state_in", "no state_out", "no prefixes", "flat snapshots", "no snapshots", "gaps"])
+def test_arrays_that_are_shorter_than_what_is_read_are_refused(queued, kw):
+    with pytest.raises(wpp.WppError) as e:
+        _call(**kw)
+    assert e.value.status == 1 and not queued

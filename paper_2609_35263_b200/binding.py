@@ -487,6 +487,13 @@ def wpp_kda_workspace_bytes(num_requests: int, num_heads: int, total_tokens: int
     return int(load_library().wpp_kda_workspace_bytes(ctypes.byref(desc)))
 
 
+def _state_slots(pool, shape, where: str) -> int:
+    """Slots of a pool of recurrent states: fp32 [slots, *shape] without gaps, because the kernels read and write whole slots of it."""
+    if pool.dtype != torch.float32 or tuple(pool.shape[1:]) != shape or not pool.is_contiguous():
+        raise WppError(1, where)
+    return int(pool.shape[0])
+
+
 def wpp_kda_chunk(ctx: Context, q, k, v, alpha, beta, row_offsets, state_pool, state_in, state_out, out=None,
                   prefix_lens=None, snap_interval: int = 0, snap_slots=None, status=None, stream=None, layout: int = 0,
                   workspace=None):
@@ -505,7 +512,8 @@ def wpp_kda_chunk(ctx: Context, q, k, v, alpha, beta, row_offsets, state_pool, s
     if out is None:
         out = torch.empty((T, H, dv), dtype=torch.bfloat16, device=q.device)
     max_snaps = 0 if snap_slots is None else int(snap_slots.shape[1])
-    desc = KdaDesc(R, H, dk, dv, int(state_pool.shape[0]), int(snap_interval), max_snaps, int(layout), T)
+    slots = _state_slots(state_pool, (H, dk, dv), "wpp_kda_chunk")
+    desc = KdaDesc(R, H, dk, dv, slots, int(snap_interval), max_snaps, int(layout), T)
     ws_bytes = 0 if workspace is None else int(workspace.numel() * workspace.element_size())
     st = _call.kda_chunk(ctx.handle.value, desc, q, k, v, alpha, beta, row_offsets, prefix_lens, state_pool, state_in, state_out,
                          snap_slots, out, workspace, ws_bytes, status, _stream(ctx, stream))
@@ -529,13 +537,6 @@ def _token_stride(x, where: str) -> int:
     if x.stride(0) == 0:               # one row for all tokens; to the library a stride of 0 means rows behind one another
         raise WppError(1, where)
     return int(x.stride(0))
-
-
-def _state_slots(pool, shape, where: str) -> int:
-    """Slots of a pool of recurrent states: fp32 [slots, *shape] without gaps, because the kernels read and write whole slots of it."""
-    if pool.dtype != torch.float32 or tuple(pool.shape[1:]) != shape or not pool.is_contiguous():
-        raise WppError(1, where)
-    return int(pool.shape[0])
 
 
 def wpp_linear_chunk(ctx: Context, q, k, v, log_decay, row_offsets, state_pool, state_in, state_out, out=None,

@@ -138,3 +138,24 @@ def test_the_compiler_is_looked_for(monkeypatch, tmp_path):
     monkeypatch.setenv("PATH", str(tmp_path))
     with pytest.raises(RuntimeError, match="C compiler"):
         build._cc()
+
+
+@pytest.mark.parametrize("pool", [torch.zeros(2, 2, 128, 128), torch.zeros(2, 1, 128, 64), torch.zeros(2, 128, 128), torch.zeros(1, 1, 128, 128).double(),
+                                  torch.zeros(4, 1, 128, 128)[::2], torch.zeros(2, 1, 128, 128).transpose(2, 3)],
+                         ids=["another head", "half the width", "no slots", "fp64", "gaps", "transposed"])
+def test_a_pool_that_is_not_one_of_such_states_is_refused(monkeypatch, pool):
+    """The kernels write whole slots: of a smaller pool they would write what lies behind it."""
+    B.load_library()
+    calls = []
+
+    class Calls:
+        @staticmethod
+        def kda_chunk(*a):
+            calls.append(a)
+            return 0
+    monkeypatch.setattr(B, "_call", Calls)
+    _kda()
+    assert len(calls) == 1
+    with pytest.raises(B.WppError) as e:
+        _kda(state_pool=pool)
+    assert e.value.status == 1 and len(calls) == 1

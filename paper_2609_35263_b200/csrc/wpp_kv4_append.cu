@@ -41,11 +41,6 @@ __device__ __forceinline__ float max2_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 // n / d rounded correctly, r being 1 / d rounded correctly: q = n r, then q + (n - q d) r with fused operations (Markstein 1990).  Nothing
 // over- or underflows here that could reach a result: quotients are at most 15.03, divisors at least 2^-100, or the divisor is 15 and
 // a quotient below 2^-100 counts as zero.

@@ -10,18 +10,12 @@
 #include <stdint.h>
 
 #include "wpp_device.h"
+#include "wpp_linear_blocks.cuh"
 #include "wpp_ptx.cuh"
 
 namespace wpp {
 
 constexpr int kLinThreads = 256;
-
-// Slot of the pool that holds the state behind a token, or -1; a slot id outside the pool is reported and taken for -1.
-__device__ __forceinline__ int64_t linear_slot(const LinearParams& p, int slot) {
-    if (slot >= -1 && slot < p.num_slots) return slot;
-    if (p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
-    return -1;
-}
 
 template <int D, int kCols>
 __global__ void __launch_bounds__(kLinThreads) wpp_linear_token_kernel(const LinearParams p) {

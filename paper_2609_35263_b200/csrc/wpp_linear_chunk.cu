@@ -60,12 +60,6 @@ struct LinCfg {
     static constexpr int kBytes = kOffSpoilt + D * 4;
 };
 
-__device__ __forceinline__ int64_t lin_slot(const LinearParams& p, int slot) {
-    if (slot >= -1 && slot < p.num_slots) return slot;
-    if (p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
-    return -1;
-}
-
 // kFirst: the pass that leaves the segments' own states (no outputs)
 template <int D, bool kFirst>
 __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kernel(const LinearChunkParams p) {
@@ -83,21 +77,12 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
     grid_launch_dependents();
     grid_dependency_wait();
 
-    // ---- which request and segment: request r's are numbered from row_offsets[r] / seg_tokens + r on; in the first
-    //      pass, where all but the last ones of a chain count, from row_offsets[r] / seg_tokens on
     const int head = blockIdx.y;
     const int64_t index = blockIdx.x;
-    int req = 0, hi = p.num_requests;
-    while (hi - req > 1) {
-        const int width = (hi - req + 31) / 32, i = req + lane * width;
-        const unsigned le = __ballot_sync(0xffffffffu, i < hi && p.row_offsets[i] / p.seg_tokens + (kFirst ? 0 : i) <= index) | 1u;
-        const int last = 31 - __clz((int)le);
-        hi = min(hi, req + (last + 1) * width);
-        req += last * width;
-    }
-    const int64_t row0 = p.row_offsets[req], n = p.row_offsets[req + 1] - row0;
-    const int64_t index0 = row0 / p.seg_tokens, seg = index - index0 - (kFirst ? 0 : req), segs = n > 0 ? (n + p.seg_tokens - 1) / p.seg_tokens : 1;
-    if (n <= p.few_tokens || seg >= segs || (kFirst && seg == segs - 1)) return;            // (a last segment's own state is nobody's state before)
+    const LinearSegment found = linear_segment<kFirst>(p, index);
+    if (!found.work) return;
+    const int req = found.req;
+    const int64_t row0 = found.row0, n = found.tokens, index0 = found.index0, seg = found.seg, segs = found.segs;
     const int64_t begin = seg * p.seg_tokens, end = min(n, begin + p.seg_tokens);
 
     // ---- the state before the segment.  Workspace: a segment's own state is at ws_state, thread by thread.
@@ -124,7 +109,7 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
         }
     };
     if (seg == 0 && (kFirst || segs == 1)) {
-        const int64_t in = lin_slot(p, p.state_in[req]);
+        const int64_t in = linear_slot(p, p.state_in[req]);
         const float* at = p.state_pool + in * slot_size + mine;
 #pragma unroll
         for (int nt = 0; nt < kN; ++nt) {
@@ -397,7 +382,7 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
         }
         at = next;
         if (!kFirst && p.snap_interval > 0 && (prefix + at) % p.snap_interval == 0) {
-            const int64_t slot = p.snap_slots && snap < p.max_snaps ? lin_slot(p, p.snap_slots[(int64_t)req * p.max_snaps + snap]) : -1;
+            const int64_t slot = p.snap_slots && snap < p.max_snaps ? linear_slot(p, p.snap_slots[(int64_t)req * p.max_snaps + snap]) : -1;
             if (slot >= 0) pool_store(slot);
             ++snap;
         }
@@ -409,7 +394,7 @@ __global__ void __launch_bounds__(LinCfg<D>::kThreads, 2) wpp_linear_chunk_kerne
         ws_store(index);
         if (threadIdx.x == 0) p.ws_log[index * p.num_heads + head] = (float)all;
     } else if (seg == segs - 1) {
-        const int64_t out = lin_slot(p, p.state_out[req]);
+        const int64_t out = linear_slot(p, p.state_out[req]);
         if (out >= 0) pool_store(out);
     }
 }

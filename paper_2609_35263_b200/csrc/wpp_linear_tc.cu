@@ -49,18 +49,6 @@ struct Smem {
 };
 static_assert(Smem::kBytes <= 232448, "more shared memory than a CTA can have");
 
-__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
-__device__ __forceinline__ int64_t slot_of(const LinearParams& p, int slot) {
-    if (slot >= -1 && slot < p.num_slots) return slot;
-    if (p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
-    return -1;
-}
-
 struct Walk {
     int64_t at, end, left, interval;                   // left: tokens up to the next boundary
     __device__ __forceinline__ bool more() const { return at < end; }
@@ -169,24 +157,15 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2, r = threadIdx.x & 127;
     constexpr int kGateUsers = kFirst ? 256 : 384;
 
-    // ---- which request and segment (as in wpp_linear_chunk.cu)
     const int head = blockIdx.y;
     const int64_t index = blockIdx.x;
     int req = 0;
     int64_t row0 = 0, n = 0, index0 = 0, seg = 0, segs = 0;
     auto find = [&] {                                  // false: nothing to do
         grid_dependency_wait();
-        int hi = p.num_requests;
-        while (hi - req > 1) {
-            const int width = (hi - req + 31) / 32, i = req + lane * width;
-            const unsigned le = __ballot_sync(0xffffffffu, i < hi && p.row_offsets[i] / p.seg_tokens + (kFirst ? 0 : i) <= index) | 1u;
-            const int last = 31 - __clz((int)le);
-            hi = min(hi, req + (last + 1) * width);
-            req += last * width;
-        }
-        row0 = p.row_offsets[req], n = p.row_offsets[req + 1] - row0, index0 = row0 / p.seg_tokens;
-        seg = index - index0 - (kFirst ? 0 : req), segs = n > 0 ? (n + p.seg_tokens - 1) / p.seg_tokens : 1;
-        return n > p.few_tokens && seg < segs && !(kFirst && seg == segs - 1);         // (a last segment's own state is nobody's state before)
+        const LinearSegment s = linear_segment<kFirst>(p, index);
+        req = s.req, row0 = s.row0, n = s.tokens, index0 = s.index0, seg = s.seg, segs = s.segs;
+        return s.work;
     };
     // Where many CTAs may have nothing to do they see it before anything is set up: 62 requests of 1 token and 2 of 2,048 with 32 heads
     // 172 us | 157.  Elsewhere the kernel before may still run while they are set up: 8 x 2,048 tokens 134 us | 141.
@@ -408,7 +387,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         // workspace: segments' own states, four columns of all rows after one another
         auto ws = [&](int64_t i, int c4) { return reinterpret_cast<float4*>(p.ws_state + (i * p.num_heads + head) * kD * kD) + c4 * kD + r; };
         const bool from_pool = seg == 0 && (kFirst || segs == 1);
-        const int64_t in = from_pool ? slot_of(p, p.state_in[req]) : -1;
+        const int64_t in = from_pool ? linear_slot(p, p.state_in[req]) : -1;
         // the state before the segment into tensor memory
 #pragma unroll 1
         for (int q = 0; q < 4; ++q) {
@@ -441,7 +420,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
         tmem_wait_st();
         int64_t snap = p.snap_interval > 0 ? (prefix + begin) / p.snap_interval - prefix / p.snap_interval : 0;
         auto snapshot = [&] {                          // of the state as it is, at a boundary
-            const int64_t slot = p.snap_slots && snap < p.max_snaps ? slot_of(p, p.snap_slots[(int64_t)req * p.max_snaps + snap]) : -1;
+            const int64_t slot = p.snap_slots && snap < p.max_snaps ? linear_slot(p, p.snap_slots[(int64_t)req * p.max_snaps + snap]) : -1;
             ++snap;
             if (slot >= 0) state_to_memory(lane_addr, reinterpret_cast<float4*>(p.state_pool + slot * slot_size + row_at), 1);
         };
@@ -488,7 +467,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 state_to_memory(lane_addr, ws(index, 0), kD);
             } else {
                 if (b > 0 && walk.at_boundary() && p.snap_interval > 0) snapshot();
-                const int64_t out = seg == segs - 1 ? slot_of(p, p.state_out[req]) : -1;
+                const int64_t out = seg == segs - 1 ? linear_slot(p, p.state_out[req]) : -1;
                 if (out >= 0) state_to_memory(lane_addr, reinterpret_cast<float4*>(p.state_pool + out * slot_size + row_at), 1);
             }
         }

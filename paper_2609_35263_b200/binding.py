@@ -544,7 +544,8 @@ def wpp_linear_chunk(ctx: Context, q, k, v, log_decay, row_offsets, state_pool, 
                      workspace=None, scale: float = 1.0):
     """Queue the linear-attention layer of one wave on `stream`: S_t = exp(g_t) S_{t-1} + k_t v_t^T, o_t = scale S_t^T q_t.
 
-    q, k, v: cuda bf16 [T, H, d], d 64 or 128 (views of a packed buffer will do: heads side by side, tokens any stride apart);
+    q, k, v: cuda bf16 [T, H, d], d 64 or 128 (views of a packed buffer will do: heads side by side, tokens any stride apart; one row
+    for all tokens is refused);
     log_decay: cuda fp32 [H], or [T, H] for a decay per token; row_offsets: cuda int64 [R+1]; state_pool: cuda fp32
     [slots, H, d, d] (updated in place); state_in, state_out: cuda int32 [R] (-1: zero state / do not store); snap_slots: cuda
     int32 [R, max_snaps] with prefix_lens (cuda int32 [R]) and snap_interval > 0 for periodic snapshots; workspace: cuda

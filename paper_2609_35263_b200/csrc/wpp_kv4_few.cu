@@ -17,9 +17,10 @@
 // per row.  p_j scale_j is rounded to f16 times a power of two per row and warp that puts the largest one so far between 2^6 and 2^15: it
 // is off by 2^-11 of itself or by 2^-31 of that largest one, of which a million keys of a warp make 2^-11, however wide the rows of V.
 //
-// Measured: 64 requests of one token behind 255 to 16,383 keys, 64/8 heads of 128, 124 us (the copies alone 93, the bytes at the measured copy
-// bandwidth 82); four behind 131,071 120 us (87).  Three CTAs an SM of blocks of at most 8 rows: with four, which leaves the
-// products 128 registers, 140 and 135 us.
+// Measured: 64 requests of one token behind 255 to 16,383 keys, 64/8 heads of 128, 130 us back to back and 132 to 135 on a cache that is not
+// in L2 (the copies alone 93, the bytes at the measured copy bandwidth 82); four behind 131,071 125 and 132 to 135 us (87).  No unit is
+// full (issue 58 %, ALU 51, DRAM 51, products 25): a warp goes through a step as one chain, and twelve warps an SM do not hide all of it.
+// Three CTAs an SM of blocks of at most 8 rows: with four, which leaves the products 128 registers, 8 % more.
 
 #include <cuda_runtime.h>
 #include <math.h>

@@ -11,7 +11,7 @@
 //
 // What bounds it are the products (1,856 of 16 x 8 x 16 for 64 tokens at 128 columns, half a one per clock: 58 clocks a token where
 // the memory needs 44; heads of 128 come here with few chains of short chunks only, see kLinTcTokens, the others to
-// wpp_linear_tc.cu: 8 x 2,048 tokens of 32 heads 365 us | 134 there).  Heads of 64: 8 x 2,048 of 32 heads 131 us, half the bytes
+// wpp_linear_tc.cu: 8 x 2,048 tokens of 32 heads 365 us | 138 there).  Heads of 64: 8 x 2,048 of 32 heads 137 us, half the bytes
 // and a quarter of the products.  The sums G are made in 64 bits and kept as a multiple of 1/64 and a rest, so that differences of long
 // sums are exact to fp32.
 //

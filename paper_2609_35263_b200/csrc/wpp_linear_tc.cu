@@ -14,8 +14,8 @@
 //                their places come free, warp 15 sums the logarithms of the decays
 // What bounds it: memory wants 44 clocks a token (1,032 bytes at 6.5 TB/s on 148 SMs), the products 28; the chains
 // S1 -> P -> O2 -> outputs -> S1 and (4) -> bf16(S) -> (3), with all their hand-overs, take about 60.  Measured: 8 x 2,048 tokens of 32 heads
-// 134 us where the memory would take 87 (256 chains on 148 SMs are two rounds, the second not full), 1 x 32,768 of 16 in segments
-// 209 us; products of 16 x 8 x 16 (wpp_linear_chunk.cu) 365 us for the former.
+// 138 us back to back and 158 on inputs that are not in L2, where the memory would take 87 (256 chains on 148 SMs are two rounds, the
+// second not full), 1 x 32,768 of 16 in segments 214 us; products of 16 x 8 x 16 (wpp_linear_chunk.cu) 365 us for the former.
 // Tensor memory: S1, then P [0,128)  O1 [128,256)  O2 [256,384)  S [384,512).
 // All mbarrier waits are bounded; on expiry the CTA raises its abort flag, every role drains, TMEM is freed and WPP_ERR_TIMEOUT is
 // written to the status word.
@@ -496,7 +496,7 @@ wpp_linear_tc_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     float x[32];
                     tmem_ld32(lane_addr + kColS1 + 32 * q, reinterpret_cast<uint32_t*>(x));
                     if (q < warp) {
-                        // e^(G_i - G_j) = e^(G_i - G_e) e^(G_e - G_j), e the last of the 32 columns: neither factor is above 1
+                        // e^(G_i - G_j) = e^(G_i - G_e) e^(G_e - G_j), e the last of the 32 columns: neither factor is above 1 if no g is above 0
                         const float f = p.scale * fast_exp2((gh - whole[32 * q + 31]) + (gl - rest[32 * q + 31]));
                         const uint64_t f2 = pack2(f, f);
                         tmem_wait_ld();

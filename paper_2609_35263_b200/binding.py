@@ -489,9 +489,10 @@ def wpp_kda_workspace_bytes(num_requests: int, num_heads: int, total_tokens: int
 
 def _state_slots(pool, shape, where: str) -> int:
     """Slots of a pool of recurrent states: fp32 [slots, *shape] without gaps, because the kernels read and write whole slots of it."""
-    if pool.dtype != torch.float32 or tuple(pool.shape[1:]) != shape or not pool.is_contiguous():
+    size = pool.shape
+    if size[1:] != shape or pool.dtype is not torch.float32 or not pool.is_contiguous():
         raise WppError(1, where)
-    return int(pool.shape[0])
+    return size[0]
 
 
 def wpp_kda_chunk(ctx: Context, q, k, v, alpha, beta, row_offsets, state_pool, state_in, state_out, out=None,
@@ -534,9 +535,10 @@ def _token_stride(x, where: str) -> int:
         raise WppError(1, where)
     if x.shape[0] <= 1:
         return int(x.shape[1] * x.shape[2])
-    if x.stride(0) == 0:               # one row for all tokens; to the library a stride of 0 means rows behind one another
+    stride = x.stride(0)
+    if stride == 0:                    # one row for all tokens; to the library a stride of 0 means rows behind one another
         raise WppError(1, where)
-    return int(x.stride(0))
+    return stride
 
 
 def wpp_linear_chunk(ctx: Context, q, k, v, log_decay, row_offsets, state_pool, state_in, state_out, out=None,
@@ -561,11 +563,9 @@ def wpp_linear_chunk(ctx: Context, q, k, v, log_decay, row_offsets, state_pool, 
     if tuple(log_decay.shape) != ((T, H) if per_token else (H,)) or (H > 1 and log_decay.stride(-1) != 1):
         raise WppError(1, "wpp_linear_chunk")
     # (what the kernels read by the type and the number of requests that the library is told)
-    if log_decay.dtype != torch.float32 or row_offsets.dtype != torch.int64:
-        raise WppError(1, "wpp_linear_chunk")
-    if min(x.numel() for x in (state_in, state_out, state_in if prefix_lens is None else prefix_lens)) < R:
-        raise WppError(1, "wpp_linear_chunk")
-    if snap_slots is not None and (snap_slots.dim() != 2 or snap_slots.shape[0] < R or not snap_slots.is_contiguous()):
+    if (log_decay.dtype is not torch.float32 or row_offsets.dtype is not torch.int64 or state_in.numel() < R or state_out.numel() < R or
+            (prefix_lens is not None and prefix_lens.numel() < R) or
+            (snap_slots is not None and (snap_slots.dim() != 2 or snap_slots.shape[0] < R or not snap_slots.is_contiguous()))):
         raise WppError(1, "wpp_linear_chunk")
     decay_stride = 0 if not per_token else int(log_decay.stride(0)) if T > 1 else H
     strides = [_token_stride(x, "wpp_linear_chunk") for x in (q, k, v, out)]

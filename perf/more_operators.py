@@ -9,7 +9,7 @@
 
 A block (page, KV head) of the 8-bit cache holds a code for each element of its rows, an 8-bit floating-point number (e4m3), and
 behind the codes one fp32 number, its scale, a power of two: an element stands for scale * code.  The scale is the least one with
-which the rows appended so far are within 448 (between 2^-80 and 2^80); where new rows raise it, the codes that stand are scaled
+which the rows appended so far are within 448 (between 2^-56 and 2^40); where new rows raise it, the codes that stand are scaled
 down and rounded again.  The append's results are returned as codes and scales.
 
 A position's angle is position * frequency: 64 bits where a position is far, and so in both forms here.
@@ -138,7 +138,7 @@ def _capacity(case):
 
 
 # ------------------------------------------------------------------------------------------------------- 8-bit blocks
-_LEAST, _MOST = -80, 80          # powers of two that a scale may be
+_LEAST, _MOST = -56, 40          # powers of two that a scale may be
 
 
 def _scale(top):
@@ -405,7 +405,7 @@ def _exact_append(case, seed):
             for a in range(P // B * B, P + C, B):
                 page, lo, hi = int(s["table"][i, a // B]), max(P, a), min(P + C, a + B)
                 x = s[name + "_new"][r0 + lo - P:r0 + hi - P].double().transpose(0, 1)                  # [Hkv, rows, d]
-                scale = torch.exp2(torch.ceil(torch.log2(x.abs().amax((1, 2)) / 448)).clamp(-80, 80))
+                scale = torch.exp2(torch.ceil(torch.log2(x.abs().amax((1, 2)) / 448)).clamp(-56, 40))
                 if lo > a:
                     scale = torch.maximum(scale, scales[page, :, 0])
                     codes[page, :, :lo - a] *= (scales[page, :, 0] / scale)[:, None, None]

@@ -63,8 +63,12 @@ typedef enum {
  *   WPP_KV4   rows of head_dim codes c_e of 4 bits and two bf16 numbers; a row stands for least + scale * c_e.  For each
  *             (page, KV head) a block of wpp_kv4_block_bytes(page_size, head_dim) bytes:
  *             page_size rows of head_dim / 2 bytes (element 2i in the low half of byte i, 2i + 1 in the high half), then
- *             page_size pairs (least, scale). */
-enum { WPP_BF16 = 1, WPP_KV4 = 2 };
+ *             page_size pairs (least, scale).
+ *   WPP_KV8   rows of head_dim codes of 8 bits, floating-point numbers of type e4m3 (sign, four bits of exponent, three of mantissa, no
+ *             infinities; largest 448), with a scale for each (page, KV head), of K and of V; an element stands for scale * code.
+ *             A block is page_size rows of head_dim bytes and, behind them, 16 bytes of which the first four are the scale: an
+ *             fp32 power of two from 2^-56 to 2^40.  wpp_kv8_block_bytes(page_size, head_dim) bytes in all. */
+enum { WPP_BF16 = 1, WPP_KV4 = 2, WPP_KV8 = 3 };
 
 /* Opaque per-device context: SM count, shared-memory limit, driver entry points.  Owns host memory only. */
 typedef struct wpp_ctx wpp_ctx;
@@ -86,15 +90,16 @@ const char* wpp_status_string(int status);
 /* Last cudaError_t / CUresult seen by this context (0 if none). */
 int wpp_last_cuda_error(const wpp_ctx* ctx);
 
-/* Bytes of a block of a WPP_KV4 pool; 0 for a page size or head_dim outside the supported set. */
+/* Bytes of a block of a WPP_KV4 pool, and of a WPP_KV8 pool; 0 for a page size or head_dim outside the supported set. */
 size_t wpp_kv4_block_bytes(int32_t page_size, int32_t head_dim);
+size_t wpp_kv8_block_bytes(int32_t page_size, int32_t head_dim);
 
 /* Description of one wave.  Strides are in ELEMENTS (bf16), inner dim contiguous.
  * Pools: element (page, kv_head, slot, e) of K lives at
  *   k_cache + page*kv_page_stride + kv_head*kv_head_stride + slot*kv_token_stride + e,
  * V likewise in v_cache with the same strides.  A stride of 0 selects the dense default
  * of the layouts [num_pages][Hkv][B][d] (pools) and [T][H][d] (q, k_new/v_new, out).
- * WPP_KV4 pools: the block of (page, kv_head) begins at byte page*kv_page_stride + kv_head*kv_head_stride of its pool: these two
+ * WPP_KV4 and WPP_KV8 pools: the block of (page, kv_head) begins at byte page*kv_page_stride + kv_head*kv_head_stride of its pool: these two
  * strides count BYTES (multiples of 16, at least a block), and kv_token_stride has to be 0. */
 typedef struct {
     int32_t num_requests;        /* R >= 0 */
@@ -104,7 +109,7 @@ typedef struct {
     int32_t page_size;           /* B in {16, 32, 64, 128} tokens per page */
     int32_t max_blocks_per_req;  /* row stride of block_tables, in elements */
     int32_t num_pages;           /* pool size, for bounds checks */
-    int32_t dtype;               /* WPP_BF16 or WPP_KV4 */
+    int32_t dtype;               /* WPP_BF16, WPP_KV4 or WPP_KV8 */
     float sm_scale;              /* 0 selects 1/sqrt(head_dim) */
     int32_t reserved0;
     int64_t kv_page_stride, kv_head_stride, kv_token_stride;
@@ -113,7 +118,7 @@ typedef struct {
     int64_t o_token_stride, o_head_stride;
 } wpp_batch_desc;
 
-/* Planner knobs; a zero field selects the library default.  (A description with WPP_KV4 has kernels of its own: of these fields
+/* Planner knobs; a zero field selects the library default.  (A description with WPP_KV4 or WPP_KV8 has kernels of its own: of these fields
  * only force_kv_splits, max_ctas and shape say something there; shape 1: tiles of 256 query rows, 2: blocks of 16, 0: the library
  * decides for every request.) */
 typedef struct {
@@ -145,7 +150,7 @@ typedef struct {
     int64_t total_new_tokens;   /* T */
     int64_t key_steps;          /* sum over tiles of 128-row x 128-key steps (work incl. tile quantisation) */
     int64_t flops;              /* algorithmic: 4 * d * Hq * sum_i (C_i P_i + C_i (C_i + 1) / 2) */
-    int64_t shape;              /* attention kernel the plan is for: 1 or 2, see wpp_plan_opts.shape; 3: those of a WPP_KV4 cache */
+    int64_t shape;              /* attention kernel the plan is for: 1 or 2, see wpp_plan_opts.shape; 3: those of a WPP_KV4 or WPP_KV8 cache */
     size_t workspace_bytes;     /* device scratch wpp_prefill_attention_varlen needs for this plan (never 0) */
     size_t plan_bytes;          /* bytes of plan_host actually used; copy that many to the device */
 } wpp_plan_info;
@@ -173,7 +178,8 @@ int wpp_plan_tiles(const wpp_ctx* ctx_or_null, const wpp_batch_desc* desc,
                    void* plan_host, size_t plan_host_bytes, wpp_plan_info* info);
 
 /* Optional host-side check of a wave (host copies of everything): page ids in range, table long enough, no slot
- * written by two requests, no written slot inside another request's readable range.  block_tables_host is
+ * written by two requests, no written slot inside another request's readable range (WPP_KV8: no page written for one request that
+ * another one writes or reads, since an append may scale the rows that stand in a page).  block_tables_host is
  * int32 [R][max_blocks_per_req]. */
 int wpp_validate_batch(const wpp_batch_desc* desc, const int32_t* block_tables_host,
                        const int32_t* prefix_lens_host, const int32_t* chunk_lens_host);
@@ -195,7 +201,14 @@ int wpp_validate_batch(const wpp_batch_desc* desc, const int32_t* block_tables_h
  *     least = min x, as bf16 (+0 where it is -0);   scale = bf16((max x - least) / 15), the quotient in fp32;
  *     c_e   = (x_e - least) / scale, difference and quotient in fp32, rounded to the nearest integer (halves to the even one).
  * scale < 2^-100: scale and codes are 0.  A row with a NaN or an infinity, or whose max x - least is not a finite float:
- * least = NaN (0x7fc0), scale and codes 0.  No other byte of a pool is written. */
+ * least = NaN (0x7fc0), scale and codes 0.  No other byte of a pool is written.
+ * WPP_KV8: per page and head, K and V apart, defined to the bit: with a = the largest finite |x| of the call's rows in the page,
+ *     scale = the least 2^e with a <= 448 * 2^e, e from -56 to 40 (2^-56 if a = 0); if rows of the request's prefix stand in the page
+ *             (only its first touched page, where P_i is no multiple of the page size), at least the scale that stands there;
+ *     code  = x / scale rounded to the nearest e4m3 number (halves to even; beyond +-448: +-448); NaN (0x7f) of a NaN or an infinity.
+ * Where the scale of standing rows rises, their codes become code * old / new, rounded likewise.  (Scales being powers of two, that is
+ * exact but for codes that leave the normal range.)  Rows of a page behind the request's last one are left as they were, as is any
+ * other byte of the pools.  A page written for one request may not be read or written for another in the same wave. */
 int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* k_new, const void* v_new,
                   void* k_cache, void* v_cache, const int32_t* block_tables, const int32_t* prefix_lens,
                   const int32_t* chunk_lens, const void* plan_host, const void* plan_dev, int32_t* status_dev,
@@ -225,7 +238,11 @@ int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* k_
  * are merged in a fixed order).
  * WPP_KV4: K_j[g] and V_j[g] are the rows that codes, least and scale stand for.  Slots >= P_i + C_i never influence the result, and
  * a NaN row only the query rows that see it (their outputs are NaN; of a row of K their lse is -infinity).  One or two kernels,
- * one more iff the plan has split tiles, and a memset of 256 bytes iff it has more tiles than CTAs. */
+ * one more iff the plan has split tiles, and a memset of 256 bytes iff it has more tiles than CTAs.
+ * WPP_KV8: K_j[g] and V_j[g] are scale * code, probabilities (times V's scales, relative to the row's largest) are rounded to f16 before the
+ * PV product, the scores have fp32's error.  Slots >= P_i + C_i never influence the result, and a NaN code only the query rows that
+ * see its key: of K all their outputs are NaN and their lse -infinity, of V the output's element of the same place is NaN.  Launches as
+ * for WPP_KV4. */
 int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* q, void* out,
                                  float* lse_or_null, const void* k_cache, const void* v_cache,
                                  const int32_t* block_tables, const int32_t* prefix_lens,

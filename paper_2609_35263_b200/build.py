@@ -11,10 +11,11 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwpp.so")
 SOURCES = ["wpp_plan.cpp", "wpp_plan_kv4.cpp", "wpp_waves.cpp", "wpp_hints.cu", "wpp_api.cu", "wpp_append_combine.cu", "wpp_attention.cu", "wpp_attention_small.cu",
            "wpp_kv4_append.cu", "wpp_kv4_few.cu", "wpp_kv4_tiles.cu",
+           "wpp_kv8_append.cu", "wpp_kv8_few.cu",
            "wpp_kda.cu", "wpp_kda_tc.cu", "wpp_kda_group.cu", "wpp_linear.cu", "wpp_linear_chunk.cu", "wpp_linear_tc.cu"]
 CALL_SOURCE = os.path.join(CSRC, "wpp_call.c")          # Python module that marshals the calls of every layer
 CALL = os.path.join(HERE, "_wpp_call" + sysconfig.get_config_var("EXT_SUFFIX"))
-HEADERS = ["wpp_host.h", "wpp_plan_format.h", "wpp_device.h", "wpp_ptx.cuh", "wpp_kda_blocks.cuh", "wpp_linear_blocks.cuh", os.path.join("..", "..", "include", "wpp.h")]
+HEADERS = ["wpp_host.h", "wpp_plan_format.h", "wpp_device.h", "wpp_ptx.cuh", "wpp_kv8.cuh", "wpp_kda_blocks.cuh", "wpp_linear_blocks.cuh", os.path.join("..", "..", "include", "wpp.h")]
 
 
 def _nvcc() -> str:

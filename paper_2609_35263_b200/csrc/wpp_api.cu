@@ -324,8 +324,8 @@ static int make_map(const wpp_ctx* cctx, CUtensorMap* m, const void* base, int r
 }
 
 // ---------------------------------------------------------------------------------------------------------------
-// Cache held in 4 bits: the same calls, told apart by the description's dtype.
-static int kv4_append(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlanHeader* hd, const void* k_new, const void* v_new,
+// Caches held in 4 or 8 bits: the same calls, told apart by the description's dtype.
+static int codes_append(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlanHeader* hd, const void* k_new, const void* v_new,
                       void* k_cache, void* v_cache, const int32_t* block_tables, const int32_t* prefix_lens, const int32_t* chunk_lens,
                       const void* plan_dev, int32_t* status_dev, void* cuda_stream) {
     wpp::Kv4AppendParams p;
@@ -351,7 +351,7 @@ static int kv4_append(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlan
     p.off_q_offsets = hd->off_q_offsets;
     p.off_prefix = hd->off_prefix;
     p.total_new_tokens = hd->total_new_tokens;
-    const int e = wpp_launch_kv4_append(d.head_dim, &p, ctx->sm_count, cuda_stream);
+    const int e = (d.dtype == WPP_KV4 ? wpp_launch_kv4_append : wpp_launch_kv8_append)(d.head_dim, &p, ctx->sm_count, cuda_stream);
     if (e != 0) return cuda_fail(ctx, e);
     const_cast<wpp_ctx*>(ctx)->launches += 1;
     return WPP_OK;
@@ -396,10 +396,10 @@ static int combine_parts(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppP
     return WPP_OK;
 }
 
-static int kv4_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlanHeader* hd, const void* q, void* out,
-                         float* lse_or_null, const void* k_cache, const void* v_cache, const int32_t* block_tables,
-                         const int32_t* prefix_lens, const int32_t* chunk_lens, const void* plan_dev, void* workspace,
-                         int32_t* status_dev, void* cuda_stream) {
+static int codes_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPlanHeader* hd, const void* q, void* out,
+                           float* lse_or_null, const void* k_cache, const void* v_cache, const int32_t* block_tables,
+                           const int32_t* prefix_lens, const int32_t* chunk_lens, const void* plan_dev, void* workspace,
+                           int32_t* status_dev, void* cuda_stream) {
     wpp::Kv4AttnParams p;
     memset(&p, 0, sizeof(p));
     p.plan = plan_dev;
@@ -436,7 +436,7 @@ static int kv4_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppP
     p.num_tiles = hd->num_units - hd->num_few_units;
     p.scale_log2 = scale_log2_of(d);
     if (hd->num_few_units > 0) {
-        const int e = wpp_launch_kv4_few(d.head_dim, &p, hd->num_few_ctas, hd->max_few_rows, cuda_stream);
+        const int e = (d.dtype == WPP_KV4 ? wpp_launch_kv4_few : wpp_launch_kv8_few)(d.head_dim, &p, hd->num_few_ctas, hd->max_few_rows, cuda_stream);
         if (e != 0) return cuda_fail(ctx, e);
         const_cast<wpp_ctx*>(ctx)->launches += 1;
     }
@@ -471,9 +471,9 @@ extern "C" int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, con
         return WPP_ERR_INVALID_ARG;
     if (!aligned16(k_new) || !aligned16(v_new) || !aligned16(k_cache) || !aligned16(v_cache) || !aligned16(plan_dev))
         return WPP_ERR_INVALID_ARG;
-    if (d.dtype == WPP_KV4)
-        return kv4_append(ctx, d, hd, k_new, v_new, k_cache, v_cache, block_tables, prefix_lens, chunk_lens, plan_dev, status_dev,
-                          cuda_stream);
+    if (d.dtype != WPP_BF16)
+        return codes_append(ctx, d, hd, k_new, v_new, k_cache, v_cache, block_tables, prefix_lens, chunk_lens, plan_dev, status_dev,
+                            cuda_stream);
     wpp::AppendParams p;
     memset(&p, 0, sizeof(p));
     p.plan = plan_dev;
@@ -517,8 +517,8 @@ extern "C" int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_
     if (rc != WPP_OK) return rc;
     const WppPlanHeader* hd = nullptr;
     if ((rc = wpp_check_plan(plan_host, &d, &hd)) != WPP_OK) return rc;
-    const bool kv4 = d.dtype == WPP_KV4;
-    if (hd->tile_m > WPP_MAX_TILE_M || hd->shape < (kv4 ? 3 : 1) || hd->shape > (kv4 ? 3 : 2)) return WPP_ERR_PLAN_MISMATCH;
+    const bool codes = d.dtype != WPP_BF16;
+    if (hd->tile_m > WPP_MAX_TILE_M || hd->shape < (codes ? 3 : 1) || hd->shape > (codes ? 3 : 2)) return WPP_ERR_PLAN_MISMATCH;
     if (hd->total_new_tokens == 0 || hd->num_units == 0) return WPP_OK;
     if ((rc = wpp_ctx_check_device(ctx)) != WPP_OK) return rc;
     if (!q || !out || !k_cache || !v_cache || !block_tables || !prefix_lens || !chunk_lens || !plan_dev)
@@ -529,9 +529,9 @@ extern "C" int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_
     if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) != 0) return WPP_ERR_INVALID_ARG;
     if (workspace_bytes < hd->workspace_bytes) return WPP_ERR_WORKSPACE_TOO_SMALL;
     if (d.num_pages == 0) return WPP_ERR_INVALID_ARG;
-    if (kv4)
-        return kv4_attention(ctx, d, hd, q, out, lse_or_null, k_cache, v_cache, block_tables, prefix_lens, chunk_lens, plan_dev,
-                             workspace, status_dev, cuda_stream);
+    if (codes)
+        return codes_attention(ctx, d, hd, q, out, lse_or_null, k_cache, v_cache, block_tables, prefix_lens, chunk_lens, plan_dev,
+                               workspace, status_dev, cuda_stream);
 
     CUtensorMap tq[4], tk, tv;
     if ((rc = query_maps(ctx, d, hd, q, tq)) != WPP_OK) return rc;

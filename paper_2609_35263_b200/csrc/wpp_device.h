@@ -58,8 +58,8 @@ struct AppendParams {
     int64_t total_new_tokens;
 };
 
-// 4-bit cache.  Pools in bytes; a block (page, KV head) is page_size rows of head_dim / 2 bytes and, behind them, as many pairs of
-// bf16 numbers (least value, scale).
+// 4- and 8-bit caches.  Pools in bytes; a block (page, KV head) is page_size rows of head_dim / 2 bytes and, behind them, as many pairs of
+// bf16 numbers (least value, scale); or page_size rows of head_dim bytes and, behind them, an fp32 scale.
 struct Kv4AppendParams {
     const void* plan;
     const __nv_bfloat16* k_new;
@@ -207,6 +207,8 @@ int wpp_launch_attention_small(int head_dim, const CUtensorMap* tq, const CUtens
                                const wpp::SmallAttnParams* p, int num_ctas, void* stream);
 int wpp_launch_append(const wpp::AppendParams* p, int num_sms, void* stream);
 int wpp_launch_kv4_append(int head_dim, const wpp::Kv4AppendParams* p, int num_sms, void* stream);
+int wpp_launch_kv8_append(int head_dim, const wpp::Kv4AppendParams* p, int num_sms, void* stream);
+int wpp_launch_kv8_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream);
 int wpp_launch_kv4_tiles(int head_dim, const CUtensorMap* tq, const wpp::Kv4AttnParams* p, int num_ctas, void* stream);
 int wpp_launch_kv4_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream);
 int wpp_launch_combine(const wpp::CombineParams* p, int num_combine, void* stream);

@@ -1,0 +1,173 @@
+// KV append into a cache held in 8 bits with a scale per page and head.
+//
+// The rows that a request's chunk has in one page (K or V of one head) share a scale: the least power of two 2^e with which their largest
+// finite value is within 448, but no less than the scale of prefix rows that stand in the page.  A code is x / 2^e rounded to e4m3; the
+// division is a product with 2^-e, exact (what it would make a subnormal number is far below the least code).  Where the scale
+// of standing rows rises by 2^n, their codes are taken down by 2^n.
+//
+// A (touched page, head, K or V) is a unit.  It has as many warps as the page has 16 slots, each of which holds its rows in registers
+// between the search for the largest value and the conversion: the rows are read once.  Units are numbered without a table of touched
+// pages: request i's begin at q_offset_i / B + 2 i, which leaves room for all it can touch and some numbers unused.
+#include <cuda_runtime.h>
+#include <stdint.h>
+
+#include "wpp_device.h"
+#include "wpp_kv8.cuh"
+#include "wpp_plan_format.h"
+#include "wpp_ptx.cuh"
+
+namespace wpp {
+
+constexpr int kKv8AppendWarps = 8;
+
+__device__ __forceinline__ uint32_t abs_max(uint32_t m, uint32_t w) { return __vmaxu2(m, w & 0x7fff7fffu); }
+
+// the exponent of the least scale for values of which `top` (bf16 bits, finite) is the largest: 448 = 1.75 * 2^8
+__device__ __forceinline__ int scale_exponent(uint32_t top) {
+    const int e = (int)(top >> 7) - 135 + ((top & 0x7fu) > 0x60u);
+    return top == 0u ? kKv8LeastExp : min(max(e, kKv8LeastExp), kKv8MostExp);
+}
+
+template <int D>
+__global__ void __launch_bounds__(32 * kKv8AppendWarps) wpp_kv8_append_kernel(const Kv4AppendParams p) {
+    constexpr int kVecs = D / 8, kTurns = 16 * kVecs / 32, kApart = 32 / kVecs;      // 16-byte vectors of a row; of a lane; rows between them
+    __shared__ uint32_t s_top[kKv8AppendWarps];
+    if (!p.few) grid_launch_dependents();
+    grid_dependency_wait();
+    const char* plan = static_cast<const char*>(p.plan);
+    const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets);
+    const int32_t* plan_prefix = reinterpret_cast<const int32_t*>(plan + p.off_prefix);
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, page_shift = 31 - __clz(p.page_size);
+    const int unit_shift = page_shift - 4, part = warp & ((1 << unit_shift) - 1);    // warps of a unit (log2); which of them this is
+    const uint32_t unit = blockIdx.x * (uint32_t)(kKv8AppendWarps >> unit_shift) + (uint32_t)(warp >> unit_shift);
+    const uint32_t heads = (uint32_t)p.num_kv_heads, pair = unit / heads, head = unit - pair * heads;
+    const bool is_v = (pair & 1u) != 0u;
+    const int number = (int)(pair >> 1);
+
+    // ---- the unit's request: the last one that begins at `number` or before
+    int lo = 0, hi = p.num_requests;
+    while (hi - lo > 1) {
+        const int width = (hi - lo + 31) / 32, i = lo + lane * width;
+        const unsigned le = __ballot_sync(0xffffffffu, i < hi && (q_offsets[i] >> page_shift) + 2 * i <= number) | 1u;
+        const int last = 31 - __clz((int)le);
+        hi = min(hi, lo + (last + 1) * width);
+        lo += last * width;
+    }
+    const int q_off = q_offsets[lo], P = p.prefix_lens[lo], C = p.chunk_lens[lo];
+    bool there = true;
+    if (P != plan_prefix[lo] || C != q_offsets[lo + 1] - q_off) {
+        if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_PLAN_MISMATCH);
+        there = false;
+    }
+    const int64_t blk = (int64_t)(P >> page_shift) + number - ((q_off >> page_shift) + 2 * lo), first = blk << page_shift;      // the page's first position
+    there = there && C > 0 && first < (int64_t)P + C;
+    int slot0 = 0, slot1 = 0, stand = 0;      // slots that are written; those before slot0 stand
+    uint8_t* block = nullptr;
+    if (there) {
+        const int page = blk < p.max_blocks ? p.block_tables[(int64_t)lo * p.max_blocks + blk] : -1;
+        if (page < 0 || page >= p.num_pages) {
+            if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
+        } else {
+            block = (is_v ? p.v_cache : p.k_cache) + page * p.page_bytes + head * p.head_bytes;
+            stand = slot0 = (int)max((int64_t)P - first, (int64_t)0);
+            slot1 = (int)min((int64_t)P + C - first, (int64_t)p.page_size);
+        }
+    }
+
+    // ---- the warp's rows, and the largest finite value of the unit's
+    const int col = lane % kVecs, row = 16 * part + lane / kVecs;      // rows row, row + kApart, ..
+    const __nv_bfloat16* src = (is_v ? p.v_new : p.k_new) + (int64_t)head * p.kvnew_head_stride + col * 8;
+    const int64_t token0 = (int64_t)q_off + first - P;                 // the token in slot 0, if it were one
+    uint4 x[kTurns];
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int slot = row + i * kApart;
+        x[i] = make_uint4(0, 0, 0, 0);
+        if (slot >= slot0 && slot < slot1) x[i] = *reinterpret_cast<const uint4*>(src + (token0 + slot) * p.kvnew_token_stride);
+    }
+    float* const scale_at = reinterpret_cast<float*>(block + (D << page_shift));
+    int e_old = kKv8LeastExp;
+    if (stand > 0) e_old = min(max(exponent_of(*scale_at), kKv8LeastExp), kKv8MostExp);
+    uint32_t m = 0u;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) m = abs_max(abs_max(abs_max(abs_max(m, x[i].x), x[i].y), x[i].z), x[i].w);
+    uint32_t top = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+    const bool odd = top >= 0x7f80u;          // a NaN or an infinity is among them: the largest of the others
+    if (odd) {
+        m = 0u;
+#pragma unroll
+        for (int i = 0; i < kTurns; ++i) {
+            const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const uint32_t a = w[j] & 0x7fffu, b = w[j] >> 16 & 0x7fffu;
+                m = max(m, max(a < 0x7f80u ? a : 0u, b < 0x7f80u ? b : 0u));
+            }
+        }
+        top = __reduce_max_sync(0xffffffffu, m);
+    }
+    if (unit_shift > 0) {
+        if (lane == 0) s_top[warp] = top;
+        __syncthreads();                      // (every warp has read the standing scale before one of them replaces it, too)
+        top = 0u;
+        for (int i = 0; i < 1 << unit_shift; ++i) top = max(top, s_top[(warp & ~((1 << unit_shift) - 1)) + i]);
+    }
+    if (!block) return;
+    const int e = max(scale_exponent(top), e_old);
+    __syncwarp();                             // (so has every lane of a unit of one warp)
+    if (part == 0 && lane == 0 && (stand == 0 || e != e_old)) *scale_at = power_of_two(e);
+
+    // ---- codes
+    const float inverse = power_of_two(-e);
+    uint8_t* const dst = block + col * 8;
+#pragma unroll
+    for (int i = 0; i < kTurns; ++i) {
+        const int slot = row + i * kApart;
+        if (slot < slot0 || slot >= slot1) continue;
+        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+        uint32_t c[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            float a = __uint_as_float(w[j] << 16), b = __uint_as_float(w[j] & 0xffff0000u);
+            if (odd) {                        // (an infinity would be rounded to 448)
+                a = (w[j] & 0x7f80u) == 0x7f80u ? __uint_as_float(0x7fffffffu) : a;
+                b = (w[j] & 0x7f800000u) == 0x7f800000u ? __uint_as_float(0x7fffffffu) : b;
+            }
+            c[j] = codes_of(a * inverse, b * inverse);
+        }
+        *reinterpret_cast<uint2*>(dst + slot * D) = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+    }
+    if (stand > 0 && e != e_old) {
+        const float down = power_of_two(e_old - e);
+#pragma unroll 1
+        for (int slot = row; slot < min(stand, 16 * part + 16); slot += kApart) {
+            const uint2 old = *reinterpret_cast<const uint2*>(dst + slot * D);
+            const uint32_t f[4] = {codes_f16x2_low(old.x), codes_f16x2_high(old.x), codes_f16x2_low(old.y), codes_f16x2_high(old.y)};
+            uint32_t c[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) c[j] = codes_of(f16_low(f[j]) * down, f16_high(f[j]) * down);
+            *reinterpret_cast<uint2*>(dst + slot * D) = make_uint2(c[0] | c[1] << 16, c[2] | c[3] << 16);
+        }
+    }
+}
+
+}  // namespace wpp
+
+extern "C" int wpp_launch_kv8_append(int head_dim, const wpp::Kv4AppendParams* p, int num_sms, void* stream) {
+    if (p->total_new_tokens == 0) return 0;
+    const int64_t units = (p->total_new_tokens / p->page_size + 2 * (int64_t)p->num_requests) * 2 * p->num_kv_heads;
+    const int64_t per_block = wpp::kKv8AppendWarps * 16 / p->page_size, blocks = (units + per_block - 1) / per_block;
+    if (blocks > 0x7fffffff) return (int)cudaErrorInvalidValue;
+    wpp::Kv4AppendParams q = *p;
+    q.few = blocks <= 4 * (int64_t)num_sms;      // (see wpp_launch_kv4_append)
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)blocks);
+    cfg.blockDim = dim3(32 * wpp::kKv8AppendWarps);
+    cfg.stream = (cudaStream_t)stream;
+    cudaLaunchAttribute overlap;
+    overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    overlap.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &overlap;
+    cfg.numAttrs = q.few ? 1 : 0;
+    return (int)cudaLaunchKernelEx(&cfg, head_dim == 128 ? wpp::wpp_kv8_append_kernel<128> : wpp::wpp_kv8_append_kernel<64>, q);
+}

@@ -32,6 +32,11 @@ size_t wpp_kv4_block_bytes(int32_t page_size, int32_t head_dim) {
     return (size_t)page_size * (size_t)(head_dim / 2 + 4);
 }
 
+size_t wpp_kv8_block_bytes(int32_t page_size, int32_t head_dim) {
+    if (wpp_kv4_block_bytes(page_size, head_dim) == 0) return 0;       // (the same page sizes and head_dims)
+    return (size_t)page_size * (size_t)head_dim + 16;
+}
+
 // Fill in default strides and check what the host can check about a description.
 int wpp_resolve_desc(const wpp_batch_desc* in, wpp_batch_desc* d) {
     if (!in) return WPP_ERR_INVALID_ARG;
@@ -39,22 +44,22 @@ int wpp_resolve_desc(const wpp_batch_desc* in, wpp_batch_desc* d) {
     if (d->num_requests < 0 || d->num_q_heads <= 0 || d->num_kv_heads <= 0 || d->max_blocks_per_req < 0 ||
         d->num_pages < 0 || d->head_dim <= 0 || d->page_size <= 0 || !(d->sm_scale >= 0.0f))
         return WPP_ERR_INVALID_ARG;
-    if (d->dtype != WPP_BF16 && d->dtype != WPP_KV4) return WPP_ERR_UNSUPPORTED;
+    if (d->dtype != WPP_BF16 && d->dtype != WPP_KV4 && d->dtype != WPP_KV8) return WPP_ERR_UNSUPPORTED;
     if (d->head_dim != 64 && d->head_dim != 128) return WPP_ERR_UNSUPPORTED;
     if (d->page_size != 16 && d->page_size != 32 && d->page_size != 64 && d->page_size != 128)
         return WPP_ERR_UNSUPPORTED;
     if (d->num_q_heads % d->num_kv_heads != 0) return WPP_ERR_UNSUPPORTED;
     const int64_t dd = d->head_dim;
-    const bool kv4 = d->dtype == WPP_KV4;      // the pools' strides count bytes then, and a block's rows have theirs from the format
-    if (kv4) {
-        const int64_t block = (int64_t)wpp_kv4_block_bytes(d->page_size, d->head_dim);
+    const bool codes = d->dtype != WPP_BF16;   // the pools' strides count bytes then, and a block's rows have theirs from the format
+    if (codes) {
+        const int64_t block = (int64_t)(d->dtype == WPP_KV4 ? wpp_kv4_block_bytes(d->page_size, d->head_dim) : wpp_kv8_block_bytes(d->page_size, d->head_dim));
         if (d->kv_token_stride) return WPP_ERR_INVALID_ARG;
         if (!d->kv_head_stride) d->kv_head_stride = block;
         if (!d->kv_page_stride) d->kv_page_stride = d->kv_head_stride * d->num_kv_heads;
         if (d->kv_head_stride < block || d->kv_page_stride < block || d->kv_head_stride % 16 != 0 || d->kv_page_stride % 16 != 0)
             return WPP_ERR_INVALID_ARG;
     }
-    if (!kv4 && !d->kv_token_stride) d->kv_token_stride = dd;
+    if (!codes && !d->kv_token_stride) d->kv_token_stride = dd;
     if (!d->kv_head_stride) d->kv_head_stride = d->kv_token_stride * d->page_size;
     if (!d->kv_page_stride) d->kv_page_stride = d->kv_head_stride * d->num_kv_heads;
     if (!d->q_head_stride) d->q_head_stride = dd;
@@ -63,7 +68,7 @@ int wpp_resolve_desc(const wpp_batch_desc* in, wpp_batch_desc* d) {
     if (!d->kvnew_token_stride) d->kvnew_token_stride = d->kvnew_head_stride * d->num_kv_heads;
     if (!d->o_head_stride) d->o_head_stride = dd;
     if (!d->o_token_stride) d->o_token_stride = d->o_head_stride * d->num_q_heads;
-    const int64_t strides[] = {kv4 ? dd : d->kv_page_stride, kv4 ? dd : d->kv_head_stride, kv4 ? dd : d->kv_token_stride,
+    const int64_t strides[] = {codes ? dd : d->kv_page_stride, codes ? dd : d->kv_head_stride, codes ? dd : d->kv_token_stride,
                                d->q_token_stride, d->q_head_stride, d->kvnew_token_stride, d->kvnew_head_stride,
                                d->o_token_stride, d->o_head_stride};
     for (int64_t s : strides)
@@ -204,7 +209,7 @@ size_t wpp_plan_bytes(const wpp_ctx* ctx, const wpp_batch_desc* desc, int64_t to
     wpp_plan_opts o;
     if (wpp_resolve_desc(desc, &d) != WPP_OK || total_new_tokens < 0) return 0;
     if (resolve_opts(ctx, opts_or_null, &o) != WPP_OK) return 0;
-    if (d.dtype == WPP_KV4) return wpp_kv4_plan_bytes(&d, &o, total_new_tokens);
+    if (d.dtype != WPP_BF16) return wpp_kv4_plan_bytes(&d, &o, total_new_tokens);
     return plan_bytes_bound(&d, &o, total_new_tokens);
 }
 
@@ -234,7 +239,7 @@ int wpp_plan_tiles(const wpp_ctx* ctx, const wpp_batch_desc* desc, const int32_t
         pairs += C * P + C * (C + 1) / 2;
     }
     if (T > 0x7fffffff) return WPP_ERR_INVALID_ARG;
-    if (d.dtype == WPP_KV4) {
+    if (d.dtype != WPP_BF16) {
         try {
             return wpp_kv4_plan(&d, &o, prefix_lens, chunk_lens, T, pairs, plan_host, plan_host_bytes, info);
         } catch (const std::bad_alloc&) {              // (no exception passes a C entry)
@@ -721,6 +726,25 @@ int wpp_check_plan(const void* plan_host, const wpp_batch_desc* resolved, const 
     return WPP_OK;
 }
 
+// The same of a cache whose pages have one scale each: a written page is one request's alone, and stands once in its table.
+static int validate_pages(const wpp_batch_desc& d, const int32_t* bt, const int32_t* prefix_lens, const int32_t* chunk_lens) {
+    const int64_t B = d.page_size;
+    std::unordered_map<int32_t, int32_t> writer;   // page -> request
+    for (int pass = 0; pass < 2; ++pass)
+        for (int i = 0; i < d.num_requests; ++i) {
+            const int64_t P = prefix_lens[i], n = P + chunk_lens[i];
+            if (P < 0 || n < P) return WPP_ERR_INVALID_ARG;
+            if (n == P) continue;
+            if ((n + B - 1) / B > d.max_blocks_per_req) return WPP_ERR_BOUNDS;
+            for (int64_t j = pass ? 0 : P / B; j < (pass ? P / B : (n + B - 1) / B); ++j) {
+                const int32_t page = bt[(int64_t)i * d.max_blocks_per_req + j];
+                if (page < 0 || page >= d.num_pages) return WPP_ERR_BOUNDS;
+                if (pass ? writer.count(page) != 0 : !writer.emplace(page, i).second) return WPP_ERR_ALIASED_APPEND;
+            }
+        }
+    return WPP_OK;
+}
+
 int wpp_validate_batch(const wpp_batch_desc* desc, const int32_t* bt, const int32_t* prefix_lens,
                        const int32_t* chunk_lens) {
     wpp_batch_desc d;
@@ -728,6 +752,13 @@ int wpp_validate_batch(const wpp_batch_desc* desc, const int32_t* bt, const int3
     if (rc != WPP_OK) return rc;
     const int R = d.num_requests, B = d.page_size;
     if (R > 0 && (!bt || !prefix_lens || !chunk_lens)) return WPP_ERR_INVALID_ARG;
+    if (d.dtype == WPP_KV8) {
+        try {
+            return validate_pages(d, bt, prefix_lens, chunk_lens);
+        } catch (const std::bad_alloc&) {              // (no exception passes a C entry)
+            return WPP_ERR_WORKSPACE_TOO_SMALL;
+        }
+    }
     // written slot -> writer; read ranges per page -> max readable slots by a non-writer
     std::unordered_map<int64_t, int32_t> writer;   // page*B+slot -> request
     for (int i = 0; i < R; ++i) {

@@ -20,7 +20,7 @@ from typing import Dict, List, Sequence, Tuple
 import torch
 import torch.distributed as dist
 
-from .binding import WPP_BF16, WPP_KV4, WppError, make_desc
+from .binding import WPP_BF16, WPP_KV4, WPP_KV8, WppError, make_desc, wpp_kv8_block_bytes
 
 WPP_ERR_POSITION_MISMATCH = 4
 Span = Tuple[int, int, int]          # (request id, starting token, length)
@@ -29,17 +29,18 @@ Span = Tuple[int, int, int]          # (request id, starting token, length)
 def head_shard(rank: int, world: int, num_requests: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
                page_size: int, max_blocks_per_req: int, num_pages: int, q, out, k_new, v_new, k_pool, v_pool):
     """(desc, views) for rank `rank` of `world` KV-head shards: strided views of q/out [T, Hq, d], k_new/v_new
-    [T, Hkv, d] and the pools [pages, Hkv, B, d], or uint8 [pages, Hkv, block bytes] of a cache held in 4 bits; the descriptor
+    [T, Hkv, d] and the pools [pages, Hkv, B, d], or uint8 [pages, Hkv, block bytes] of a cache held in 4 or 8 bits; the descriptor
     carries the parents' strides."""
     if num_kv_heads % world or not 0 <= rank < world:
         raise ValueError("KV heads must divide evenly over the shards")
     hk = num_kv_heads // world
     hq = hk * (num_q_heads // num_kv_heads)
     ks, qs = slice(rank * hk, (rank + 1) * hk), slice(rank * hq, (rank + 1) * hq)
-    kv4 = k_pool.dtype == torch.uint8
-    desc = make_desc(num_requests, hq, hk, head_dim, page_size, max_blocks_per_req, num_pages, dtype=WPP_KV4 if kv4 else WPP_BF16,
+    codes = k_pool.dtype == torch.uint8        # (a block's bytes tell which)
+    dtype = WPP_BF16 if not codes else WPP_KV8 if k_pool.shape[2] == wpp_kv8_block_bytes(page_size, head_dim) else WPP_KV4
+    desc = make_desc(num_requests, hq, hk, head_dim, page_size, max_blocks_per_req, num_pages, dtype=dtype,
                      kv_page_stride=k_pool.stride(0), kv_head_stride=k_pool.stride(1),
-                     kv_token_stride=0 if kv4 else k_pool.stride(2),
+                     kv_token_stride=0 if codes else k_pool.stride(2),
                      q_token_stride=q.stride(0), q_head_stride=q.stride(1),
                      kvnew_token_stride=k_new.stride(0), kvnew_head_stride=k_new.stride(1),
                      o_token_stride=out.stride(0), o_head_stride=out.stride(1))

@@ -1,0 +1,107 @@
+"""The 8-bit cache's format, its oracle and what the host refuses of it (no GPU)."""
+import ctypes
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_35263_b200 as wpp
+from oracle import kv8 as okv8
+
+from .kv8_harness import Wave
+
+
+def test_encode_is_the_nearest_e4m3_number():
+    rng = np.random.default_rng(0)
+    x = np.concatenate([rng.standard_normal(4000) * 2.0 ** rng.integers(-14, 9, 4000), okv8.NUMBERS[:127], -okv8.NUMBERS[:127],
+                        (okv8.NUMBERS[:126] + okv8.NUMBERS[1:127]) / 2, [0.0, -0.0, 448.0, 449.0, 1e9, -1e9]]).astype(np.float32)
+    want = torch.from_numpy(x).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8).numpy()
+    assert np.array_equal(okv8.encode(x), want)
+    assert okv8.encode(np.array([np.nan, np.inf, -np.inf])).tolist() == [0x7F] * 3
+    values = torch.arange(256, dtype=torch.uint8).view(torch.float8_e4m3fn).double().numpy()
+    assert np.array_equal(values, okv8.NUMBERS, equal_nan=True)
+
+
+def test_scale_is_the_least_power_of_two_that_holds_the_largest_value():
+    for top, e in ((0.0, -56), (448.0, 0), (448.5, 1), (447.0, 0), (224.0, -1), (225.0, 0), (1.0, -8), (2.0 ** -70, -56), (3e38, 40), (np.inf, -56)):
+        assert okv8.scale_exp([top, -top / 2 if np.isfinite(top) else 0.0]) == e, top
+
+
+def test_append_in_pieces_gives_what_one_append_gives():
+    """Powers of two: codes taken down are the codes that one append would have given, but where they leave the normal range."""
+    whole = Wave([0], [45], 2, 1, 64, 32, seed=3)
+    a, _ = whole.appended()
+    pieces, row = Wave([0], [45], 2, 1, 64, 32, seed=3), 0
+    k, v = pieces.k_pool, pieces.v_pool
+    for n in (3, 1, 1, 20, 15, 5):
+        k, v = okv8.append(pieces.k_new[row:row + n], pieces.v_new[row:row + n], k, v, pieces.table, [row], [n], 32)
+        row += n
+    x, s = okv8.rows_of(a, whole.table[0], 45, 32, 64, 0)
+    y, r = okv8.rows_of(k, whole.table[0], 45, 32, 64, 0)
+    assert np.array_equal(s, r) and np.all(np.abs(x - y) <= s[:, None] * 2.0 ** -9)
+
+
+def test_block_bytes():
+    assert [wpp.wpp_kv8_block_bytes(B, d) for B in (16, 32, 64, 128) for d in (64, 128)] == [B * d + 16 for B in (16, 32, 64, 128) for d in (64, 128)]
+    assert wpp.wpp_kv8_block_bytes(48, 128) == wpp.wpp_kv8_block_bytes(16, 96) == wpp.wpp_kv8_block_bytes(0, 0) == wpp.wpp_kv8_block_bytes(-16, 128) == 0
+
+
+def _plan(**kw):
+    d = wpp.make_desc(1, 4, 2, 64, 16, 8, 8, dtype=wpp.WPP_KV8, **kw)
+    return wpp.wpp_plan_tiles(None, d, [5], [7], pin=False)
+
+
+def test_descriptions_that_are_refused():
+    _plan()
+    block = 16 * 64 + 16
+    _plan(kv_head_stride=block, kv_page_stride=2 * block)
+    _plan(kv_head_stride=3 * block, kv_page_stride=block)              # heads further apart than pages: a layout of one's own
+    for bad in (dict(kv_token_stride=64), dict(kv_head_stride=block - 16), dict(kv_head_stride=block + 8), dict(kv_page_stride=block // 2),
+                dict(q_token_stride=8 * 64 + 4), dict(o_head_stride=32)):
+        with pytest.raises(wpp.WppError) as e:
+            _plan(**bad)
+        assert e.value.status == 1, bad
+    for d, B in ((96, 16), (128, 48), (64, 256)):
+        with pytest.raises(wpp.WppError) as e:
+            wpp.wpp_plan_tiles(None, wpp.make_desc(1, 4, 2, d, B, 8, 8, dtype=wpp.WPP_KV8), [5], [7], pin=False)
+        assert e.value.status == 2
+    with pytest.raises(wpp.WppError) as e:
+        wpp.wpp_plan_tiles(None, wpp.make_desc(1, 4, 2, 64, 16, 8, 8, dtype=4), [5], [7], pin=False)
+    assert e.value.status == 2
+
+
+def test_plans_of_one_cache_are_not_the_other_s():
+    """A plan says whose it is: neither call takes one of another pool type."""
+    lib = wpp.load_library()
+    for mine, other in ((wpp.WPP_KV8, wpp.WPP_KV4), (wpp.WPP_KV4, wpp.WPP_KV8), (wpp.WPP_KV8, wpp.WPP_BF16)):
+        d = wpp.make_desc(1, 4, 2, 64, 16, 8, 8, dtype=mine)
+        plan = wpp.wpp_plan_tiles(None, wpp.make_desc(1, 4, 2, 64, 16, 8, 8, dtype=other), [5], [7], pin=False)
+        fake = ctypes.c_void_p(256)                                    # (a context is only asked for not being null before the plan is looked at)
+        assert lib.wpp_kv_append(fake, ctypes.byref(d), *([None] * 7), plan.host.data_ptr(), *([None] * 3)) == 6
+
+
+def test_validate_batch_wants_written_pages_to_be_one_request_s():
+    d = wpp.make_desc(2, 4, 2, 64, 16, 4, 16, dtype=wpp.WPP_KV8)
+    ok = [[0, 1, 2, -1], [0, 1, 3, -1]]                                # two full pages shared, a page each behind them
+    assert wpp.wpp_validate_batch(d, ok, [32, 32], [5, 9]) == 0
+    assert wpp.wpp_validate_batch(d, [[0, 1, 2, -1], [0, 1, 2, -1]], [32, 40], [5, 3]) == 9        # different slots of a page: its scale may move
+    bf16 = wpp.make_desc(2, 4, 2, 64, 16, 4, 16)
+    assert wpp.wpp_validate_batch(bf16, [[0, 1, 2, -1], [0, 1, 2, -1]], [32, 40], [5, 3]) == 9     # (request 1 reads what request 0 writes)
+    assert wpp.wpp_validate_batch(d, [[0, 1, 2, -1], [0, 2, 3, -1]], [36, 32], [5, 9]) == 9        # read by another
+    assert wpp.wpp_validate_batch(bf16, [[0, 1, 2, -1], [0, 1, 2, -1]], [36, 32], [5, 0]) == 0
+    assert wpp.wpp_validate_batch(d, [[0, 1, 2, -1], [0, 1, 2, -1]], [36, 32], [5, 0]) == 0        # (an empty chunk reads nothing)
+    assert wpp.wpp_validate_batch(d, [[0, 1, 1, -1], [4, 5, 6, -1]], [20, 32], [20, 9]) == 9       # a page twice in one table
+    assert wpp.wpp_validate_batch(d, ok, [32, 32], [5, 40]) == 3
+    assert wpp.wpp_validate_batch(d, [[0, 1, 16, -1], [0, 1, 3, -1]], [32, 32], [5, 9]) == 3
+    assert wpp.wpp_validate_batch(d, ok, [32, -1], [5, 9]) == 1
+
+
+@pytest.mark.parametrize("shape", [0, 1, 2])
+@pytest.mark.parametrize("Hq,Hkv,d,B", [(8, 1, 128, 64), (10, 2, 64, 16), (64, 8, 128, 64)])
+def test_plan_covers_every_key_of_every_row(shape, Hq, Hkv, d, B):
+    P, C = [0, 700, 20_000, 5], [1, 300, 1, 0]
+    desc = wpp.make_desc(4, Hq, Hkv, d, B, 1300, 5000, dtype=wpp.WPP_KV8)
+    plan = wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, 0, 0, 0, shape), pin=False)
+    assert plan.info.shape == 3 and plan.info.total_new_tokens == 302
+    assert plan.info.flops == 4 * d * Hq * sum(c * p + c * (c + 1) // 2 for p, c in zip(P, C))
+    assert plan.host_bytes() == wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, 0, 0, 0, shape), pin=False).host_bytes()

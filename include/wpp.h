@@ -277,6 +277,85 @@ int wpp_prefill_attention_varlen_static(const wpp_ctx* ctx, const wpp_batch_desc
 /* Size in bytes of the built-in scratch array used by wpp_prefill_attention_varlen_static. */
 size_t wpp_static_scratch_bytes(void);
 
+/* ---------------------------------------------------------------------------------------------------------
+ * Steps in front of the append.
+ *
+ * Pages of a wave's new tokens, from the requests' lengths, on the GPU (Section 3.2: blocks are taken from a pool of free ones as
+ * sequences grow).  Request i holds ceil(P_i / B) pages, in the first columns of its row of block_tables; its chunk needs
+ * ceil((P_i + C_i) / B).  The missing ones are taken from the list of free pages in request order, those of a request in order of
+ * position, from entry cursor[0] on, and written to the columns behind the ones it holds.  With t = row_offsets[i] + j, j < C_i:
+ *     positions[t] = P_i + j,      slots[t] = block_tables[i][positions[t] / B] * B + positions[t] % B.
+ *   desc         : num_requests (at most 16,384), page_size, max_blocks_per_req and num_pages count here.
+ *   prefix_lens, chunk_lens : device int32 [R].
+ *   free_pages   : device int32 [num_free], read from cursor[0] on.
+ *   cursor       : device int32 [1], entries of free_pages that are taken.
+ *   cursor_out   : device int32 [2]: [0] the same afterwards (at most num_free), [1] has to be 0 and is 0 again afterwards.  May be
+ *                  cursor: then a captured call takes other pages at each replay.  Calls that share it are serialised by the caller.
+ *   block_tables : device int32 [R][max_blocks_per_req]; columns behind the last one needed are left as they were.
+ *   row_offsets  : device int64 [R+1], out, exclusive scan of chunk_lens.
+ *   positions, slots : device int32 and int64 [max_tokens], out, either may be NULL; rows behind the last token are 0 and -1.
+ * WPP_ERR_BOUNDS in *status_dev: the list ran out or holds an id outside [0, num_pages), or cursor[0] outside [0, num_free] (it is taken for
+ * the nearer end); a page that a request holds is outside; a row of block_tables is too short; or there are more than max_tokens
+ * tokens (those behind are left out).  Tokens without a page get slot -1, columns without one -1.  WPP_ERR_INVALID_ARG there: a
+ * negative length; the request counts as empty.  One kernel. */
+int wpp_assign_pages(const wpp_ctx* ctx, const wpp_batch_desc* desc, const int32_t* prefix_lens, const int32_t* chunk_lens,
+                     const int32_t* free_pages, int32_t num_free, const int32_t* cursor, int32_t* cursor_out, int32_t* block_tables,
+                     int64_t* row_offsets, int32_t* positions_or_null, int64_t* slots_or_null, int32_t max_tokens, int32_t* status_dev,
+                     void* cuda_stream);
+
+/* Rotary positions.  In a row of a head's elements, pair i < rot_dim / 2 (elements i and i + rot_dim / 2, or neighbours 2 i and 2 i + 1 where
+ * `interleaved`) at position n becomes
+ *     (a, b) -> magnitude (a cos x - b sin x, a sin x + b cos x),     x = n f_i,
+ * elements from rot_dim on stay as they are.  fp32 inside, results rounded to bf16 once.  The frequencies are given as turns per
+ * position in 64 bits behind the point, turns[i] = f_i / (2 pi) * 2^64, so that n * turns[i] modulo 2^64 is the angle: far positions
+ * lose nothing.  wpp_rope_frequencies makes them. */
+enum { WPP_ROPE_PLAIN = 0, WPP_ROPE_LINEAR = 1, WPP_ROPE_BASE = 2, WPP_ROPE_WAVELENGTH = 3, WPP_ROPE_TURNS = 4 };
+typedef struct {
+    int32_t rot_dim;          /* a multiple of 16, 16 to 128 */
+    int32_t kind;             /* WPP_ROPE_* : how longer contexts than the trained one are made room for */
+    double base;              /* f_i = base^(-2 i / rot_dim) */
+    double factor;            /* >= 1, by how much the context grows */
+    double original_context;  /* tokens of the trained context (WAVELENGTH, TURNS) */
+    double low, high;         /* turns over the trained context (WAVELENGTH, TURNS); 0 selects 1, and 4 (WAVELENGTH) or 32 (TURNS) */
+} wpp_rope_scaling;
+/* Host only.  turns_host: host uint64 [rot_dim / 2]; *magnitude: for wpp_rope_desc.
+ *   LINEAR      f_i / factor.
+ *   BASE        base * factor^(rot_dim / (rot_dim - 2)) in the place of base.
+ *   WAVELENGTH  pairs that make more than `high` turns over original_context keep f_i, those below `low` get f_i / factor, in between
+ *               both in proportion to the turns.
+ *   TURNS       the same in proportion to the pair's number, between the pairs (rounded down and up) that make `high` and `low`
+ *               turns; magnitude is 0.1 ln(factor) + 1. */
+int wpp_rope_frequencies(const wpp_rope_scaling* scaling, uint64_t* turns_host, float* magnitude);
+
+typedef struct {
+    int32_t num_q_heads, num_k_heads;   /* either may be 0 */
+    int32_t head_dim;                   /* 64 or 128 */
+    int32_t rot_dim;                    /* a multiple of 16, 16 to head_dim */
+    int32_t interleaved;                /* 1: pairs of neighbours */
+    float magnitude;                    /* 0 selects 1 */
+    int64_t total_tokens;
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride;  /* in elements, multiples of 8; 0: dense */
+    int64_t qo_token_stride, qo_head_stride, ko_token_stride, ko_head_stride;                             /* of q_out and k_out */
+} wpp_rope_desc;
+
+/* Queries and keys of T tokens on `cuda_stream`; rows of head_dim contiguous bf16 elements, 16-byte aligned.
+ *   q, q_out : device bf16 [T][num_q_heads][head_dim];  k, k_out : device bf16 [T][num_k_heads][head_dim].  q_out may be q and k_out k,
+ *              with the same strides; no other byte may be both read and written.
+ *   turns    : device uint64 [rot_dim / 2], 16-byte aligned;  positions : device int32 [T].
+ * One kernel.  WPP_ERR_UNSUPPORTED for another head_dim or rot_dim. */
+int wpp_rope(const wpp_ctx* ctx, const wpp_rope_desc* desc, const void* q, void* q_out, const void* k, void* k_out,
+             const uint64_t* turns, const int32_t* positions, void* cuda_stream);
+
+/* The same, with the rotated keys and the values (strides v_token_stride, v_head_stride) written to their slots of a WPP_BF16 cache
+ * instead of k_out: what wpp_rope and then wpp_kv_append do, in one kernel and without a plan.
+ *   batch    : page size, heads, number of pages and the pools' strides count here.
+ *   desc     : num_k_heads of `batch`; num_q_heads of `batch`, or 0 (q and q_out are not used then).
+ *   slots    : device int64 [T], page * page_size + slot of the page (as wpp_assign_pages leaves them); -1: the token's K and V are not
+ *              written.  Any other outside [0, num_pages * page_size) sets *status_dev = WPP_ERR_BOUNDS (if it was 0) and counts as -1. */
+int wpp_rope_append(const wpp_ctx* ctx, const wpp_batch_desc* batch, const wpp_rope_desc* desc, const void* q, void* q_out,
+                    const void* k_new, const void* v_new, void* k_cache, void* v_cache, const uint64_t* turns, const int32_t* positions,
+                    const int64_t* slots, int32_t* status_dev, void* cuda_stream);
+
 /* Self-test of the bounded waits the kernels rely on (no counterpart in the paper): launches one warp that waits,
  * for at most limit_cycles SM clocks (1 .. 2^30), on a barrier nothing ever arrives on.  The wait gives up, the
  * kernel ends normally, *status_dev becomes WPP_ERR_TIMEOUT (if it was 0) and *waited_cycles_dev (device int64,

@@ -91,6 +91,22 @@ class LinearDesc(ctypes.Structure):
                 ("o_token_stride", ctypes.c_int64), ("decay_token_stride", ctypes.c_int64)]
 
 
+class RopeScaling(ctypes.Structure):
+    _fields_ = [("rot_dim", ctypes.c_int32), ("kind", ctypes.c_int32), ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_context", ctypes.c_double), ("low", ctypes.c_double), ("high", ctypes.c_double)]
+
+
+class RopeDesc(ctypes.Structure):
+    _fields_ = [("num_q_heads", ctypes.c_int32), ("num_k_heads", ctypes.c_int32), ("head_dim", ctypes.c_int32), ("rot_dim", ctypes.c_int32),
+                ("interleaved", ctypes.c_int32), ("magnitude", ctypes.c_float), ("total_tokens", ctypes.c_int64),
+                ("q_token_stride", ctypes.c_int64), ("q_head_stride", ctypes.c_int64), ("k_token_stride", ctypes.c_int64),
+                ("k_head_stride", ctypes.c_int64), ("v_token_stride", ctypes.c_int64), ("v_head_stride", ctypes.c_int64),
+                ("qo_token_stride", ctypes.c_int64), ("qo_head_stride", ctypes.c_int64), ("ko_token_stride", ctypes.c_int64),
+                ("ko_head_stride", ctypes.c_int64)]
+
+
+ROPE_SCALINGS = {"none": 0, "linear": 1, "base": 2, "wavelength": 3, "turns": 4}
+
 WAVE_RING_BUSY, WAVE_ADMISSION_PENDING, WAVE_ALREADY_DEFERRED = 1, 2, 4
 
 EXPORTS = ["wpp_create", "wpp_destroy", "wpp_status_string", "wpp_last_cuda_error", "wpp_plan_bytes",
@@ -101,7 +117,7 @@ EXPORTS = ["wpp_create", "wpp_destroy", "wpp_status_string", "wpp_last_cuda_erro
            "wpp_hash_blocks", "wpp_hash_blocks_host", "wpp_hint_index_create", "wpp_hint_index_destroy",
            "wpp_hint_index_add", "wpp_hint_index_remove", "wpp_hint_index_size", "wpp_hint_probe",
            "wpp_hint_probe_recurrent", "wpp_kda_chunk", "wpp_kda_workspace_bytes",
-           "wpp_linear_chunk", "wpp_linear_workspace_bytes"]
+           "wpp_linear_chunk", "wpp_linear_workspace_bytes", "wpp_assign_pages", "wpp_rope", "wpp_rope_append", "wpp_rope_frequencies"]
 
 _lib = None
 _call = None          # the calls of every layer, marshalled in C (csrc/wpp_call.c)
@@ -165,6 +181,10 @@ def load_library() -> ctypes.CDLL:
         lib.wpp_linear_chunk.argtypes = [vp, ctypes.POINTER(LinearDesc)] + [vp] * 12 + [ctypes.c_size_t, vp, vp]
         lib.wpp_linear_workspace_bytes.restype = ctypes.c_size_t
         lib.wpp_linear_workspace_bytes.argtypes = [ctypes.POINTER(LinearDesc)]
+        lib.wpp_assign_pages.argtypes = [vp, ctypes.POINTER(BatchDesc), vp, vp, vp, ctypes.c_int32, vp, vp, vp, vp, vp, vp, ctypes.c_int32, vp, vp]
+        lib.wpp_rope.argtypes = [vp, ctypes.POINTER(RopeDesc)] + [vp] * 7
+        lib.wpp_rope_append.argtypes = [vp, ctypes.POINTER(BatchDesc), ctypes.POINTER(RopeDesc)] + [vp] * 11
+        lib.wpp_rope_frequencies.argtypes = [ctypes.POINTER(RopeScaling), vp, ctypes.POINTER(ctypes.c_float)]
         try:
             from . import _wpp_call as call
         except ImportError as e:
@@ -173,6 +193,8 @@ def load_library() -> ctypes.CDLL:
                               "(there is no fallback path)") from e
         call.init(*(ctypes.cast(f, vp).value for f in (lib.wpp_kv_append, lib.wpp_prefill_attention_varlen, lib.wpp_kda_chunk,
                                                        lib.wpp_linear_chunk)), BatchDesc, KdaDesc, LinearDesc)
+        call.init_tensors(*(ctypes.cast(f, vp).value for f in (lib.wpp_rope, lib.wpp_rope_append, lib.wpp_assign_pages)), torch.bfloat16,
+                          torch.int32, torch.int64)
         _call, _lib = call, lib
     return _lib
 
@@ -331,6 +353,57 @@ def wpp_kv_append(ctx: Context, desc: BatchDesc, k_new, v_new, k_cache, v_cache,
                          plan.dev, status, _stream(ctx, stream))
     if st:
         _check(st, "wpp_kv_append")
+
+
+def wpp_assign_pages(ctx: Context, desc: BatchDesc, prefix_lens, chunk_lens, free_pages, cursor, block_tables, row_offsets, positions=None,
+                     slots=None, cursor_out=None, status=None, stream=None) -> None:
+    """Queue the assignment of a wave's pages on `stream`: from the lengths of its requests and a list of free pages, block tables, row
+    offsets, and every new token's position and slot.
+
+    prefix_lens, chunk_lens: cuda int32 [R]; free_pages: cuda int32, read from entry cursor[0] on; cursor: cuda int32 [2], the number of
+    entries that are taken and a zero, replaced by the number afterwards unless cursor_out (int32 [2]) is given; block_tables: cuda
+    int32 [R, max_blocks], whose rows hold the pages of the prefixes; row_offsets: cuda int64 [R+1]; positions: cuda int32 and
+    slots: cuda int64 of as many rows as the wave may have tokens (rows behind the last token become 0 and -1)."""
+    st = _call.pages(ctx.handle.value, ctx.device, desc, prefix_lens, chunk_lens, free_pages, cursor, cursor if cursor_out is None else cursor_out,
+                     block_tables, row_offsets, positions, slots, status, _stream(ctx, stream))
+    if st:
+        _check(st, "wpp_assign_pages")
+
+
+def wpp_rope_frequencies(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_context: float = 0,
+                         low: float = 0.0, high: float = 0.0):
+    """(turns, magnitude) for wpp_rope and wpp_rope_append: the pairs' frequencies as an int64 host tensor [rot_dim / 2], turns per
+    position in 64 bits behind the point, and what rotated elements are multiplied by.  scaling: "none", or for contexts `factor`
+    times as long as the trained one "linear", "base", "wavelength" or "turns" (see WPP_ROPE_* in wpp.h)."""
+    if scaling not in ROPE_SCALINGS:
+        raise WppError(1, "wpp_rope_frequencies")
+    turns = torch.zeros(64, dtype=torch.int64)                         # (as many as there can be)
+    sc = RopeScaling(int(rot_dim), ROPE_SCALINGS[scaling], float(base), float(factor), float(original_context), float(low), float(high))
+    magnitude = ctypes.c_float(0.0)
+    _check(load_library().wpp_rope_frequencies(ctypes.byref(sc), turns.data_ptr(), ctypes.byref(magnitude)), "wpp_rope_frequencies")
+    return turns[:int(rot_dim) // 2], float(magnitude.value)
+
+
+def wpp_rope(ctx: Context, q, k, turns, positions, q_out=None, k_out=None, interleaved: bool = False, magnitude: float = 1.0, stream=None) -> None:
+    """Queue rotary positions of queries and keys on `stream`: in place, or into q_out and k_out.
+
+    q: cuda bf16 [T, Hq, d], k: cuda bf16 [T, Hkv, d] (either may be None), d 64 or 128, views of a packed buffer will do; turns: cuda int64
+    [rot_dim / 2] (wpp_rope_frequencies), the first rot_dim elements of a head turn; positions: cuda int32 [T]; interleaved: pairs
+    are neighbours, and not rot_dim / 2 elements apart."""
+    st = _call.rope(ctx.handle.value, ctx.device, q, k, q if q_out is None else q_out, k if k_out is None else k_out, turns, positions,
+                    interleaved, magnitude, _stream(ctx, stream))
+    if st:
+        _check(st, "wpp_rope")
+
+
+def wpp_rope_append(ctx: Context, desc: BatchDesc, q, k_new, v_new, q_out, k_cache, v_cache, turns, positions, slots, interleaved: bool = False,
+                    magnitude: float = 1.0, status=None, stream=None) -> None:
+    """wpp_rope, with the rotated keys and the values (cuda bf16 [T, Hkv, d]) written to their slots of a bf16 cache: slots, cuda int64 [T],
+    as wpp_assign_pages leaves them (-1: not written).  q may be None; q_out None: in place."""
+    st = _call.rope_append(ctx.handle.value, ctx.device, desc, q, k_new, q if q_out is None else q_out, v_new, turns, positions, interleaved,
+                           magnitude, k_cache, v_cache, slots, status, _stream(ctx, stream))
+    if st:
+        _check(st, "wpp_rope_append")
 
 
 def wpp_prefill_attention_varlen(ctx: Context, desc: BatchDesc, q, out, lse, k_cache, v_cache, block_tables,

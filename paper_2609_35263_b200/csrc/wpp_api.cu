@@ -616,6 +616,130 @@ extern "C" int wpp_prefill_attention_varlen_static(const wpp_ctx* ctx, const wpp
 }
 
 // ---------------------------------------------------------------------------------------------------------------
+// Steps in front of the append: pages from lengths, rotary positions.
+extern "C" int wpp_assign_pages(const wpp_ctx* ctx, const wpp_batch_desc* desc, const int32_t* prefix_lens, const int32_t* chunk_lens,
+                                const int32_t* free_pages, int32_t num_free, const int32_t* cursor, int32_t* cursor_out,
+                                int32_t* block_tables, int64_t* row_offsets, int32_t* positions_or_null, int64_t* slots_or_null,
+                                int32_t max_tokens, int32_t* status_dev, void* cuda_stream) {
+    if (!ctx) return WPP_ERR_INVALID_ARG;
+    wpp_batch_desc d;
+    if (int rc = wpp_resolve_desc(desc, &d)) return rc;
+    if (num_free < 0 || max_tokens < 0 || !cursor || !cursor_out || !row_offsets) return WPP_ERR_INVALID_ARG;
+    if (d.num_requests > wpp::kPagesMostRequests) return WPP_ERR_UNSUPPORTED;
+    if (d.num_requests > 0 && (!prefix_lens || !chunk_lens)) return WPP_ERR_INVALID_ARG;
+    if (d.num_requests > 0 && d.max_blocks_per_req > 0 && !block_tables) return WPP_ERR_INVALID_ARG;
+    if (num_free > 0 && !free_pages) return WPP_ERR_INVALID_ARG;
+    if (int rc = wpp_ctx_check_device(ctx)) return rc;
+    wpp::PagesParams p;
+    memset(&p, 0, sizeof(p));
+    p.prefix_lens = prefix_lens;
+    p.chunk_lens = chunk_lens;
+    p.free_pages = free_pages;
+    p.cursor = cursor;
+    p.cursor_out = cursor_out;
+    p.block_tables = block_tables;
+    p.row_offsets = row_offsets;
+    p.positions = positions_or_null;
+    p.slots = slots_or_null;
+    p.status = status_dev;
+    p.num_requests = d.num_requests;
+    p.max_blocks = d.max_blocks_per_req;
+    p.num_pages = d.num_pages;
+    p.page_shift = __builtin_ctz((unsigned)d.page_size);
+    p.num_free = num_free;
+    p.max_tokens = positions_or_null || slots_or_null ? max_tokens : 0;
+    const int e = wpp_launch_pages(&p, ctx->sm_count, cuda_stream);
+    if (e != 0) return cuda_fail(ctx, e);
+    const_cast<wpp_ctx*>(ctx)->launches += 1;
+    return WPP_OK;
+}
+
+// Fills what both forms have in common; `stride` of 0: dense.
+static int rope_params(const wpp_rope_desc* d, const void* q, void* q_out, const void* k, const uint64_t* turns, const int32_t* positions,
+                       wpp::RopeParams* p) {
+    if (!d || d->num_q_heads < 0 || d->num_k_heads < 0 || d->total_tokens < 0 || !(fabsf(d->magnitude) <= 3.402823466e+38f)) return WPP_ERR_INVALID_ARG;
+    if (d->interleaved != 0 && d->interleaved != 1) return WPP_ERR_INVALID_ARG;
+    if (d->head_dim != 64 && d->head_dim != 128) return WPP_ERR_UNSUPPORTED;
+    if (d->rot_dim < 16 || d->rot_dim > d->head_dim || d->rot_dim % 16 != 0) return WPP_ERR_UNSUPPORTED;
+    if (d->num_q_heads > 65535 || d->num_k_heads > 65535) return WPP_ERR_UNSUPPORTED;
+    memset(p, 0, sizeof(*p));
+    p->q = static_cast<const __nv_bfloat16*>(q);
+    p->k = static_cast<const __nv_bfloat16*>(k);
+    p->q_out = static_cast<__nv_bfloat16*>(q_out);
+    p->turns = turns;
+    p->positions = positions;
+    p->total_tokens = d->total_tokens;
+    p->num_q_heads = d->num_q_heads;
+    p->num_k_heads = d->num_k_heads;
+    p->rot_vecs = d->rot_dim / 16;
+    p->magnitude = d->magnitude != 0.f ? d->magnitude : 1.f;
+    const int64_t dd = d->head_dim;
+    const struct { int64_t token, head; int32_t heads; int64_t *token_out, *head_out; } tensors[5] = {
+        {d->q_token_stride, d->q_head_stride, d->num_q_heads, &p->q_token_stride, &p->q_head_stride},
+        {d->k_token_stride, d->k_head_stride, d->num_k_heads, &p->k_token_stride, &p->k_head_stride},
+        {d->v_token_stride, d->v_head_stride, d->num_k_heads, &p->v_token_stride, &p->v_head_stride},
+        {d->qo_token_stride, d->qo_head_stride, d->num_q_heads, &p->qo_token_stride, &p->qo_head_stride},
+        {d->ko_token_stride, d->ko_head_stride, d->num_k_heads, &p->ko_token_stride, &p->ko_head_stride}};
+    for (const auto& t : tensors) {
+        *t.head_out = t.head ? t.head : dd;
+        *t.token_out = t.token ? t.token : *t.head_out * (t.heads > 0 ? t.heads : 1);
+        if (*t.head_out < dd || *t.token_out < dd || *t.head_out % 8 != 0 || *t.token_out % 8 != 0) return WPP_ERR_INVALID_ARG;
+    }
+    if (d->total_tokens == 0) return WPP_OK;
+    if (!turns || !positions || !aligned16(turns) || !aligned16(q) || !aligned16(q_out) || !aligned16(k)) return WPP_ERR_INVALID_ARG;
+    if ((d->num_q_heads > 0 && (!q || !q_out)) || (d->num_k_heads > 0 && !k)) return WPP_ERR_INVALID_ARG;
+    p->q_in_place = q == q_out && p->q_token_stride == p->qo_token_stride && p->q_head_stride == p->qo_head_stride;
+    if (d->num_q_heads > 0 && q == q_out && !p->q_in_place) return WPP_ERR_INVALID_ARG;      // (rows would be read after others were written over them)
+    return WPP_OK;
+}
+
+extern "C" int wpp_rope(const wpp_ctx* ctx, const wpp_rope_desc* desc, const void* q, void* q_out, const void* k, void* k_out,
+                        const uint64_t* turns, const int32_t* positions, void* cuda_stream) {
+    if (!ctx) return WPP_ERR_INVALID_ARG;
+    wpp::RopeParams p;
+    if (int rc = rope_params(desc, q, q_out, k, turns, positions, &p)) return rc;
+    if (p.total_tokens == 0 || p.num_q_heads + p.num_k_heads == 0) return WPP_OK;
+    if (int rc = wpp_ctx_check_device(ctx)) return rc;
+    p.k_out = static_cast<__nv_bfloat16*>(k_out);
+    p.k_in_place = k == k_out && p.k_token_stride == p.ko_token_stride && p.k_head_stride == p.ko_head_stride;
+    if (p.num_k_heads > 0 && (!k_out || !aligned16(k_out) || (k == k_out && !p.k_in_place))) return WPP_ERR_INVALID_ARG;
+    const int e = wpp_launch_rope(&p, desc->head_dim, desc->interleaved, 0, ctx->sm_count, cuda_stream);
+    if (e != 0) return cuda_fail(ctx, e);
+    const_cast<wpp_ctx*>(ctx)->launches += 1;
+    return WPP_OK;
+}
+
+extern "C" int wpp_rope_append(const wpp_ctx* ctx, const wpp_batch_desc* batch, const wpp_rope_desc* desc, const void* q, void* q_out,
+                               const void* k_new, const void* v_new, void* k_cache, void* v_cache, const uint64_t* turns,
+                               const int32_t* positions, const int64_t* slots, int32_t* status_dev, void* cuda_stream) {
+    if (!ctx) return WPP_ERR_INVALID_ARG;
+    wpp_batch_desc b;
+    if (int rc = wpp_resolve_desc(batch, &b)) return rc;
+    if (b.dtype != WPP_BF16) return WPP_ERR_UNSUPPORTED;
+    wpp::RopeParams p;
+    if (int rc = rope_params(desc, q, q_out, k_new, turns, positions, &p)) return rc;
+    if (desc->head_dim != b.head_dim || (desc->num_q_heads != 0 && desc->num_q_heads != b.num_q_heads) || desc->num_k_heads != b.num_kv_heads)
+        return WPP_ERR_INVALID_ARG;
+    if (p.total_tokens == 0) return WPP_OK;
+    if (int rc = wpp_ctx_check_device(ctx)) return rc;
+    if (!v_new || !k_cache || !v_cache || !slots || !aligned16(v_new) || !aligned16(k_cache) || !aligned16(v_cache)) return WPP_ERR_INVALID_ARG;
+    p.v = static_cast<const __nv_bfloat16*>(v_new);
+    p.k_out = static_cast<__nv_bfloat16*>(k_cache);
+    p.v_out = static_cast<__nv_bfloat16*>(v_cache);
+    p.slots = slots;
+    p.status = status_dev;
+    p.kv_page_stride = b.kv_page_stride;
+    p.kv_head_stride = b.kv_head_stride;
+    p.kv_token_stride = b.kv_token_stride;
+    p.page_shift = __builtin_ctz((unsigned)b.page_size);
+    p.num_slots = (int64_t)b.num_pages * b.page_size;
+    const int e = wpp_launch_rope(&p, desc->head_dim, desc->interleaved, 1, ctx->sm_count, cuda_stream);
+    if (e != 0) return cuda_fail(ctx, e);
+    const_cast<wpp_ctx*>(ctx)->launches += 1;
+    return WPP_OK;
+}
+
+// ---------------------------------------------------------------------------------------------------------------
 // Recurrent-state layer.  Workspace of the chunk-parallel form's two passes: block offsets, then per (block, head) the cut mask,
 // the decay products at sub-block ends and the ten operand arrays the preparation kernel leaves for the chain kernel.
 struct KdaWorkspace {

@@ -18,7 +18,13 @@ static int (*p_kda)(const wpp_ctx*, const wpp_kda_desc*, const void*, const void
                     int32_t*, void*);
 static int (*p_linear)(const wpp_ctx*, const wpp_linear_desc*, const void*, const void*, const void*, const float*, const int64_t*,
                        const int32_t*, float*, const int32_t*, const int32_t*, const int32_t*, void*, void*, size_t, int32_t*, void*);
+static int (*p_rope)(const wpp_ctx*, const wpp_rope_desc*, const void*, void*, const void*, void*, const uint64_t*, const int32_t*, void*);
+static int (*p_rope_append)(const wpp_ctx*, const wpp_batch_desc*, const wpp_rope_desc*, const void*, void*, const void*, const void*, void*,
+                            void*, const uint64_t*, const int32_t*, const int64_t*, int32_t*, void*);
+static int (*p_pages)(const wpp_ctx*, const wpp_batch_desc*, const int32_t*, const int32_t*, const int32_t*, int32_t, const int32_t*, int32_t*,
+                      int32_t*, int64_t*, int32_t*, int64_t*, int32_t, int32_t*, void*);
 static PyObject *s_data_ptr, *t_batch, *t_kda, *t_linear;      /* the method's name; the binding's BatchDesc, KdaDesc and LinearDesc */
+static PyObject *s_shape, *s_stride, *s_dtype, *s_get_device, *o_bf16, *o_i32, *o_i64;      /* names of a tensor's attributes and methods; torch's types */
 
 /* Each of these returns 0, or -1 with an exception set. */
 static int integer(PyObject* o, void** out) {           /* a context, a stream, a function: None is null */
@@ -125,6 +131,197 @@ static PyObject* linear_chunk(PyObject* self, PyObject* const* args, Py_ssize_t 
     return PyLong_FromLong(st);
 }
 
+/* ---- calls that take tensors as they are: what they have to be is looked at here (0; 1: they are not; -1: an exception is set) */
+typedef struct {
+    void* at;
+    int dims;
+    int64_t size[4], stride[4];
+} tensor;
+static int longs(PyObject* o, int64_t* out, int* n) {
+    if (!o) return -1;
+    int rc = -1;
+    if (!PyTuple_Check(o)) {
+        PyErr_SetString(PyExc_TypeError, "shape or strides that are no tuple");
+    } else {
+        const Py_ssize_t k = PyTuple_GET_SIZE(o);
+        *n = (int)k;
+        rc = k > 4;
+        for (Py_ssize_t i = 0; rc == 0 && i < k; ++i) {
+            out[i] = (int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(o, i));
+            if (out[i] == -1 && PyErr_Occurred()) rc = -1;
+        }
+    }
+    Py_DECREF(o);
+    return rc;
+}
+/* a tensor of a type, on the device with this number, with `dims` dimensions */
+static int tensor_of(PyObject* o, PyObject* type, long device, int dims, tensor* t) {
+    if (memory(o, &t->at)) return -1;
+    PyObject* x = PyObject_GetAttr(o, s_dtype);
+    if (!x) return -1;
+    const int other = x != type;
+    Py_DECREF(x);
+    if (other) return 1;
+    x = PyObject_CallMethodNoArgs(o, s_get_device);
+    if (!x) return -1;
+    const long on = PyLong_AsLong(x);
+    Py_DECREF(x);
+    if (on == -1 && PyErr_Occurred()) return -1;
+    if (on != device) return 1;
+    int n = 0, rc = longs(PyObject_GetAttr(o, s_shape), t->size, &n);
+    if (rc) return rc;
+    t->dims = n;
+    if ((rc = longs(PyObject_CallMethodNoArgs(o, s_stride), t->stride, &n))) return rc;
+    return t->dims != dims;
+}
+/* numbers behind one another, `least` of them or more */
+static int numbers(PyObject* o, PyObject* type, long device, int64_t least, tensor* t) {
+    const int rc = tensor_of(o, type, device, 1, t);
+    return rc ? rc : t->size[0] < least || (t->size[0] > 1 && t->stride[0] != 1);
+}
+/* rows [T, heads, d] of contiguous elements: the strides as the library wants them, 0 where there is but one */
+static int rows(PyObject* o, long device, int64_t T, int64_t heads, int64_t d, tensor* t, int64_t* token, int64_t* head) {
+    const int rc = tensor_of(o, o_bf16, device, 3, t);
+    if (rc) return rc;
+    if ((T >= 0 && t->size[0] != T) || (heads >= 0 && t->size[1] != heads) || (d >= 0 && t->size[2] != d)) return 1;
+    *token = *head = 0;
+    if (t->size[0] == 0 || t->size[1] == 0 || t->size[2] == 0) return 0;                   /* (strides of nothing say nothing) */
+    if (t->size[2] > 1 && t->stride[2] != 1) return 1;
+    *token = t->size[0] > 1 ? t->stride[0] : 0;
+    *head = t->size[1] > 1 ? t->stride[1] : 0;
+    if ((t->size[0] > 1 && *token == 0) || (t->size[1] > 1 && *head == 0)) return 1;      /* (one row for several; to the library 0 means dense) */
+    if (*token && !*head) *head = t->size[2];
+    if (!*token && *head) *token = *head * t->size[1];                                     /* (of a single token: any that is long enough) */
+    return 0;
+}
+/* q, k (None: none), turns, positions and the options into a description: args[0 .. 7] are q, k, q_out, k_out or v, turns, positions,
+ * interleaved, magnitude */
+static int rope_desc(PyObject* const* args, long device, int with_v, wpp_rope_desc* d, tensor* t) {
+    memset(d, 0, sizeof(*d));
+    memset(t, 0, 6 * sizeof(*t));
+    int rc = 0;
+    int64_t T = -1, dim = -1;
+    if (args[0] != Py_None) {
+        if ((rc = rows(args[0], device, -1, -1, -1, &t[0], &d->q_token_stride, &d->q_head_stride))) return rc;
+        T = t[0].size[0];
+        dim = t[0].size[2];
+        if ((rc = rows(args[2], device, T, t[0].size[1], dim, &t[2], &d->qo_token_stride, &d->qo_head_stride))) return rc;
+        if (t[0].size[1] > 65535) return 1;
+        d->num_q_heads = (int32_t)t[0].size[1];
+    }
+    if (args[1] != Py_None) {
+        if ((rc = rows(args[1], device, T, -1, dim, &t[1], &d->k_token_stride, &d->k_head_stride))) return rc;
+        T = t[1].size[0];
+        dim = t[1].size[2];
+        if ((rc = rows(args[3], device, T, t[1].size[1], dim, &t[3], with_v ? &d->v_token_stride : &d->ko_token_stride,
+                       with_v ? &d->v_head_stride : &d->ko_head_stride)))
+            return rc;
+        if (t[1].size[1] > 65535) return 1;
+        d->num_k_heads = (int32_t)t[1].size[1];
+    }
+    if (T < 0 || dim > 65535) return 1;
+    if ((rc = numbers(args[4], o_i64, device, 0, &t[4])) || (rc = numbers(args[5], o_i32, device, T, &t[5]))) return rc;
+    if (t[4].size[0] > 65535) return 1;
+    d->head_dim = (int32_t)dim;
+    d->rot_dim = (int32_t)(2 * t[4].size[0]);
+    d->interleaved = PyObject_IsTrue(args[6]);
+    d->magnitude = (float)PyFloat_AsDouble(args[7]);
+    if (d->interleaved < 0 || PyErr_Occurred()) return -1;
+    d->total_tokens = T;
+    return 0;
+}
+
+/* rope(ctx, device, q, k, q_out, k_out, turns, positions, interleaved, magnitude, stream) */
+static PyObject* rope(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    (void)self;
+    void *ctx, *stream;
+    wpp_rope_desc d;
+    tensor t[6];
+    if (count(n, 11) || integer(args[0], &ctx) || integer(args[10], &stream)) return NULL;
+    const long device = PyLong_AsLong(args[1]);
+    if (device == -1 && PyErr_Occurred()) return NULL;
+    int st = rope_desc(args + 2, device, 0, &d, t);
+    if (st < 0) return NULL;
+    if (st == 0) {
+        Py_BEGIN_ALLOW_THREADS
+        st = p_rope(ctx, &d, t[0].at, t[2].at, t[1].at, t[3].at, t[4].at, t[5].at, stream);
+        Py_END_ALLOW_THREADS
+    }
+    return PyLong_FromLong(st);
+}
+
+/* rope_append(ctx, device, desc, q, k_new, q_out, v_new, turns, positions, interleaved, magnitude, k_cache, v_cache, slots, status, stream) */
+static PyObject* rope_append(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    (void)self;
+    void *ctx, *stream, *pool[2], *status;
+    wpp_batch_desc b;
+    wpp_rope_desc d;
+    tensor t[6], slots;
+    if (count(n, 16) || integer(args[0], &ctx) || integer(args[15], &stream) || description(args[2], t_batch, &b, sizeof(b))) return NULL;
+    const long device = PyLong_AsLong(args[1]);
+    if (device == -1 && PyErr_Occurred()) return NULL;
+    int st = args[4] == Py_None ? 1 : rope_desc(args + 3, device, 1, &d, t);
+    if (st == 0) st = numbers(args[13], o_i64, device, d.total_tokens, &slots);
+    if (st < 0 || memories(args + 11, 2, pool) || memories(args + 14, 1, &status)) return NULL;
+    if (st == 0) {
+        Py_BEGIN_ALLOW_THREADS
+        st = p_rope_append(ctx, &b, &d, t[0].at, t[2].at, t[1].at, t[3].at, pool[0], pool[1], t[4].at, t[5].at, slots.at, status, stream);
+        Py_END_ALLOW_THREADS
+    }
+    return PyLong_FromLong(st);
+}
+
+/* pages(ctx, device, desc, prefix, chunks, free, cursor, cursor_out, tables, rows, positions, slots, status, stream) */
+static PyObject* pages(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    (void)self;
+    void *ctx, *stream, *status;
+    wpp_batch_desc b;
+    tensor t[9];
+    if (count(n, 14) || integer(args[0], &ctx) || integer(args[13], &stream) || description(args[2], t_batch, &b, sizeof(b))) return NULL;
+    const long device = PyLong_AsLong(args[1]);
+    if (device == -1 && PyErr_Occurred()) return NULL;
+    memset(t, 0, sizeof(t));
+    const int64_t R = b.num_requests < 0 ? 0 : b.num_requests;
+    int64_t most = -1;
+    int st;
+    if ((st = numbers(args[3], o_i32, device, R, &t[0])) == 0 && (st = numbers(args[4], o_i32, device, R, &t[1])) == 0 &&
+        (st = numbers(args[5], o_i32, device, 0, &t[2])) == 0 && (st = numbers(args[6], o_i32, device, 1, &t[3])) == 0 &&
+        (st = numbers(args[7], o_i32, device, 2, &t[4])) == 0 && (st = tensor_of(args[8], o_i32, device, 2, &t[5])) == 0 &&
+        (st = numbers(args[9], o_i64, device, R + 1, &t[6])) == 0) {
+        st = t[2].size[0] > 0x7fffffff || t[5].size[0] < R || (R > 0 && t[5].size[1] != b.max_blocks_per_req) ||
+             (R > 0 && t[5].size[1] > 1 && t[5].stride[1] != 1) || (R > 1 && t[5].stride[0] != t[5].size[1]);
+        for (int i = 0; st == 0 && i < 2; ++i) {
+            if (args[10 + i] == Py_None) continue;
+            st = numbers(args[10 + i], i ? o_i64 : o_i32, device, 0, &t[7 + i]);
+            if (st == 0 && (most < 0 || t[7 + i].size[0] < most)) most = t[7 + i].size[0];
+            if (!t[7 + i].at) t[7 + i].at = t[3].at;      /* (of no rows, and no address: but asked for, and so tokens are too many) */
+        }
+    }
+    if (st < 0 || memories(args + 12, 1, &status)) return NULL;
+    if (most > 0x7fffffff) st = 1;
+    if (st == 0) {
+        Py_BEGIN_ALLOW_THREADS
+        st = p_pages(ctx, &b, t[0].at, t[1].at, t[2].at, (int32_t)t[2].size[0], t[3].at, t[4].at, t[5].at, t[6].at, t[7].at, t[8].at,
+                     most < 0 ? 0 : (int32_t)most, status, stream);
+        Py_END_ALLOW_THREADS
+    }
+    return PyLong_FromLong(st);
+}
+
+/* init_tensors(rope, rope_append, pages, bfloat16, int32, int64): the functions' addresses, torch's types */
+static PyObject* init_tensors(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    (void)self;
+    void* a[3];
+    if (count(n, 6) || integer(args[0], &a[0]) || integer(args[1], &a[1]) || integer(args[2], &a[2])) return NULL;
+    memcpy(&p_rope, &a[0], sizeof(void*));
+    memcpy(&p_rope_append, &a[1], sizeof(void*));
+    memcpy(&p_pages, &a[2], sizeof(void*));
+    Py_XSETREF(o_bf16, Py_NewRef(args[3]));
+    Py_XSETREF(o_i32, Py_NewRef(args[4]));
+    Py_XSETREF(o_i64, Py_NewRef(args[5]));
+    Py_RETURN_NONE;
+}
+
 /* init(append, attention, kda, linear, BatchDesc, KdaDesc, LinearDesc): the functions' addresses in the loaded library, the
  * descriptions' types */
 static PyObject* init(PyObject* self, PyObject* const* args, Py_ssize_t n) {
@@ -151,10 +348,18 @@ static PyMethodDef methods[] = {
     {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, NULL},
     {"kda_chunk", (PyCFunction)(void (*)(void))kda_chunk, METH_FASTCALL, NULL},
     {"linear_chunk", (PyCFunction)(void (*)(void))linear_chunk, METH_FASTCALL, NULL},
+    {"init_tensors", (PyCFunction)(void (*)(void))init_tensors, METH_FASTCALL, NULL},
+    {"rope", (PyCFunction)(void (*)(void))rope, METH_FASTCALL, NULL},
+    {"rope_append", (PyCFunction)(void (*)(void))rope_append, METH_FASTCALL, NULL},
+    {"pages", (PyCFunction)(void (*)(void))pages, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_wpp_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__wpp_call(void) {
     s_data_ptr = PyUnicode_InternFromString("data_ptr");
-    return s_data_ptr ? PyModule_Create(&module) : NULL;
+    s_shape = PyUnicode_InternFromString("shape");
+    s_stride = PyUnicode_InternFromString("stride");
+    s_dtype = PyUnicode_InternFromString("dtype");
+    s_get_device = PyUnicode_InternFromString("get_device");
+    return s_data_ptr && s_shape && s_stride && s_dtype && s_get_device ? PyModule_Create(&module) : NULL;
 }

@@ -114,6 +114,43 @@ struct CombineParams {
     uint32_t off_q_offsets, off_combine;
 };
 
+struct RopeParams {
+    const __nv_bfloat16* q;
+    const __nv_bfloat16* k;
+    const __nv_bfloat16* v;
+    __nv_bfloat16* q_out;
+    __nv_bfloat16* k_out;            // or the K pool, as v_out is the V pool
+    __nv_bfloat16* v_out;
+    const uint64_t* turns;           // [rot_dim / 2], of a turn per position, in 2^-64
+    const int32_t* positions;        // [T]
+    const int64_t* slots;            // [T], page * page_size + slot of the page, -1: none
+    int32_t* status;
+    int64_t q_token_stride, q_head_stride, k_token_stride, k_head_stride, v_token_stride, v_head_stride, qo_token_stride, qo_head_stride,
+        ko_token_stride, ko_head_stride, kv_page_stride, kv_head_stride, kv_token_stride;      // in elements
+    int64_t total_tokens, num_slots;
+    int32_t num_q_heads, num_k_heads, page_shift;
+    int32_t rot_vecs;                // rot_dim / 16
+    int32_t q_in_place, k_in_place;  // what does not turn stands already
+    float magnitude;
+    int32_t passes, units_per_token, few;      // (the launch's: of a warp; warps of a token; as in AppendParams)
+};
+
+constexpr int kPagesMostRequests = 16384;
+
+struct PagesParams {
+    const int32_t* prefix_lens;
+    const int32_t* chunk_lens;
+    const int32_t* free_pages;
+    const int32_t* cursor;           // [1]: entries of free_pages that are taken
+    int32_t* cursor_out;             // [2]: the same afterwards; a count of CTAs, 0 between calls
+    int32_t* block_tables;
+    int64_t* row_offsets;
+    int32_t* positions;              // [max_tokens] or null
+    int64_t* slots;                  // [max_tokens] or null
+    int32_t* status;
+    int32_t num_requests, max_blocks, num_pages, page_shift, num_free, max_tokens;
+};
+
 struct KdaParams {
     const __nv_bfloat16* q;
     const __nv_bfloat16* k;
@@ -211,6 +248,8 @@ int wpp_launch_kv8_append(int head_dim, const wpp::Kv4AppendParams* p, int num_s
 int wpp_launch_kv8_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream);
 int wpp_launch_kv4_tiles(int head_dim, const CUtensorMap* tq, const wpp::Kv4AttnParams* p, int num_ctas, void* stream);
 int wpp_launch_kv4_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream);
+int wpp_launch_rope(const wpp::RopeParams* p, int head_dim, int neighbours, int write, int num_sms, void* stream);
+int wpp_launch_pages(const wpp::PagesParams* p, int num_sms, void* stream);
 int wpp_launch_combine(const wpp::CombineParams* p, int num_combine, void* stream);
 // maps: q, k, v, alpha; form: 1, 2, 3 = CTAs of 128, 64, 32 columns of the state
 int wpp_launch_kda_group(const wpp::KdaGroupParams* p, const CUtensorMap* maps, int form, void* stream);

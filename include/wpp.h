@@ -68,7 +68,7 @@ typedef enum {
  *             infinities; largest 448), with a scale for each (page, KV head), of K and of V; an element stands for scale * code.
  *             A block is page_size rows of head_dim bytes and, behind them, 16 bytes of which the first four are the scale: an
  *             fp32 power of two from 2^-56 to 2^40.  wpp_kv8_block_bytes(page_size, head_dim) bytes in all. */
-enum { WPP_BF16 = 1, WPP_KV4 = 2, WPP_KV8 = 3 };
+enum { WPP_BF16 = 1, WPP_KV4 = 2, WPP_KV8 = 4 };
 
 /* Opaque per-device context: SM count, shared-memory limit, driver entry points.  Owns host memory only. */
 typedef struct wpp_ctx wpp_ctx;

@@ -19,7 +19,7 @@ LIB_PATH = os.environ.get("WPP_LIB_PATH") or os.path.join(_HERE, "libwpp.so")   
 WPP_OK = 0
 WPP_BF16 = 1
 WPP_KV4 = 2            # a cache held in 4 bits: make_desc(..., dtype=WPP_KV4)
-WPP_KV8 = 3            # a cache held in 8 bits, with a scale per page and head: make_desc(..., dtype=WPP_KV8)
+WPP_KV8 = 4            # a cache held in 8 bits, with a scale per page and head: make_desc(..., dtype=WPP_KV8)
 STATUS_NAMES = {
     0: "WPP_OK", 1: "WPP_ERR_INVALID_ARG", 2: "WPP_ERR_UNSUPPORTED", 3: "WPP_ERR_BOUNDS",
     4: "WPP_ERR_POSITION_MISMATCH", 5: "WPP_ERR_WORKSPACE_TOO_SMALL", 6: "WPP_ERR_PLAN_MISMATCH",

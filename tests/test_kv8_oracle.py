@@ -66,7 +66,7 @@ def test_descriptions_that_are_refused():
             wpp.wpp_plan_tiles(None, wpp.make_desc(1, 4, 2, d, B, 8, 8, dtype=wpp.WPP_KV8), [5], [7], pin=False)
         assert e.value.status == 2
     with pytest.raises(wpp.WppError) as e:
-        wpp.wpp_plan_tiles(None, wpp.make_desc(1, 4, 2, 64, 16, 8, 8, dtype=4), [5], [7], pin=False)
+        wpp.wpp_plan_tiles(None, wpp.make_desc(1, 4, 2, 64, 16, 8, 8, dtype=5), [5], [7], pin=False)
     assert e.value.status == 2
 
 

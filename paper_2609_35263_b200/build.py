@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwpp.so")
 SOURCES = ["wpp_plan.cpp", "wpp_plan_kv4.cpp", "wpp_waves.cpp", "wpp_hints.cu", "wpp_api.cu", "wpp_append_combine.cu", "wpp_attention.cu", "wpp_attention_small.cu",
            "wpp_kv4_append.cu", "wpp_kv4_few.cu", "wpp_kv4_tiles.cu",
-           "wpp_kv8_append.cu", "wpp_kv8_few.cu", "wpp_pages.cu", "wpp_rope.cu",
+           "wpp_kv8_append.cu", "wpp_kv8_few.cu", "wpp_kv8_tiles.cu", "wpp_pages.cu", "wpp_rope.cu",
            "wpp_kda.cu", "wpp_kda_tc.cu", "wpp_kda_group.cu", "wpp_linear.cu", "wpp_linear_chunk.cu", "wpp_linear_tc.cu"]
 CALL_SOURCE = os.path.join(CSRC, "wpp_call.c")          # Python module that marshals the calls of every layer
 CALL = os.path.join(HERE, "_wpp_call" + sysconfig.get_config_var("EXT_SUFFIX"))

@@ -26,7 +26,7 @@ struct MapKey {
     const void* base;
     uint64_t dims[4], strides[3];
     uint32_t box[4];
-    int rank, swizzle;
+    int rank, kind;
 };
 struct MapEntry {
     MapKey key;
@@ -282,17 +282,20 @@ extern "C" int wpp_selftest_bounded_wait(const wpp_ctx* ctx, int64_t limit_cycle
 
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-// bf16 tensor map, with 128-byte swizzle unless told otherwise; dims/strides innermost first, strides in bytes for dims 1..rank-1.
+// What a tensor map is of and how its boxes lie in shared memory.
+enum { kMapPlain = 0, kMapSwizzled = 1, kMapBytes = 2, kMapBytes128 = 3, kMapBytes64 = 4 };      // bf16, bf16 with 128-byte swizzle; bytes, with that of 128, of 64
+
+// Tensor map, of bf16 with 128-byte swizzle unless told otherwise; dims/strides innermost first, strides in bytes for dims 1..rank-1.
 // Looked up in the context's cache first (six maps per attention call; encoding them costs more than a small
 // wave's kernel).
 static int make_map(const wpp_ctx* cctx, CUtensorMap* m, const void* base, int rank, const uint64_t* dims,
-                    const uint64_t* strides_bytes, const uint32_t* box, bool swizzle = true) {
+                    const uint64_t* strides_bytes, const uint32_t* box, int kind = kMapSwizzled) {
     wpp_ctx* ctx = const_cast<wpp_ctx*>(cctx);
     MapKey key;
     memset(&key, 0, sizeof(key));
     key.base = base;
     key.rank = rank;
-    key.swizzle = swizzle;
+    key.kind = kind;
     for (int i = 0; i < rank; ++i) { key.dims[i] = dims[i]; key.box[i] = box[i]; }
     for (int i = 0; i < rank - 1; ++i) key.strides[i] = strides_bytes[i];
     std::lock_guard<std::mutex> guard(*ctx->map_lock);
@@ -312,8 +315,11 @@ static int make_map(const wpp_ctx* cctx, CUtensorMap* m, const void* base, int r
     cuuint32_t bx[4], es[4];
     for (int i = 0; i < rank; ++i) { gd[i] = dims[i]; bx[i] = box[i]; es[i] = 1; }
     for (int i = 0; i < rank - 1; ++i) gs[i] = strides_bytes[i];
-    CUresult r = ctx->encode_tiled(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank, const_cast<void*>(base), gd,
-                                   gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE,
+    const CUtensorMapSwizzle swizzle = kind == kMapSwizzled || kind == kMapBytes128 ? CU_TENSOR_MAP_SWIZZLE_128B
+                                       : kind == kMapBytes64                        ? CU_TENSOR_MAP_SWIZZLE_64B
+                                                                                    : CU_TENSOR_MAP_SWIZZLE_NONE;
+    CUresult r = ctx->encode_tiled(m, kind >= kMapBytes ? CU_TENSOR_MAP_DATA_TYPE_UINT8 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, (cuuint32_t)rank,
+                                   const_cast<void*>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle,
                                    CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) return cuda_fail(ctx, (int)r);
     MapEntry& en = ctx->maps[victim];
@@ -441,14 +447,23 @@ static int codes_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const Wp
         const_cast<wpp_ctx*>(ctx)->launches += 1;
     }
     if (p.num_tiles > 0) {
-        CUtensorMap tq[4];
+        CUtensorMap tq[4], tk, tv;
         if (int rc = query_maps(ctx, d, hd, q, tq)) return rc;
+        if (d.dtype == WPP_KV8) {              // the codes of a block; V's are taken apart by threads, which want rows behind one another
+            const uint64_t dims[4] = {(uint64_t)d.head_dim, (uint64_t)d.page_size, (uint64_t)d.num_kv_heads, (uint64_t)d.num_pages};
+            const uint64_t strides[3] = {(uint64_t)d.head_dim, (uint64_t)d.kv_head_stride, (uint64_t)d.kv_page_stride};
+            const uint32_t box[4] = {(uint32_t)d.head_dim, (uint32_t)d.page_size, 1, 1};
+            if (int rc = make_map(ctx, &tk, k_cache, 4, dims, strides, box, d.head_dim == 128 ? kMapBytes128 : kMapBytes64)) return rc;
+            if (int rc = make_map(ctx, &tv, v_cache, 4, dims, strides, box, kMapBytes)) return rc;
+        }
         if (p.num_tiles > hd->num_ctas) {
             p.tile_counter = static_cast<uint32_t*>(workspace);
             const int e = (int)cudaMemsetAsync(workspace, 0, WPP_WS_HEADER_BYTES, (cudaStream_t)cuda_stream);
             if (e != 0) return cuda_fail(ctx, e);
         }
-        const int e = wpp_launch_kv4_tiles(d.head_dim, tq, &p, p.num_tiles < hd->num_ctas ? p.num_tiles : hd->num_ctas, cuda_stream);
+        const int num_ctas = p.num_tiles < hd->num_ctas ? p.num_tiles : hd->num_ctas;
+        const int e = d.dtype == WPP_KV4 ? wpp_launch_kv4_tiles(d.head_dim, tq, &p, num_ctas, cuda_stream)
+                                         : wpp_launch_kv8_tiles(d.head_dim, tq, &tk, &tv, &p, num_ctas, cuda_stream);
         if (e != 0) return cuda_fail(ctx, e);
         const_cast<wpp_ctx*>(ctx)->launches += 1;
     }

@@ -1,0 +1,723 @@
+// Attention of many query rows over a cache held in 8 bits: persistent, one CTA per SM, tiles of two 128-row halves against key steps
+// of 128 keys, as wpp_attention.cu has them.
+//   warps 0-3   softmax of half A: thread r owns query row r; at a tile's end it writes its row
+//   warps 4-7   softmax of half B
+//   warps 8-11  at a tile's start Q's rows as two e4m3 terms; then, for every step, V's codes as bf16
+//   warp 12     issuer of S = Q K^T, warp 14 issuer of O += P V (one thread each), warp 13 takes tiles and loads Q, K and V by TMA,
+//               warp 15 the scales of the steps' pages
+// S = Q K^T is a product of 8-bit numbers: K's codes go from the pages to the tensor cores as they are.  A row of Q is taken as hi + lo, times a
+// power of two that puts its largest element into [128, 256): hi is q rounded to e4m3, four significant bits, lo what is left, of which a
+// bf16 number has no more than e4m3 holds; elements below 2^-9 of the row's largest are off by up to 2^-18 of it, the others exact.  Two products of
+// 8-bit numbers take as long as one of bf16.
+// O += P V is a product of bf16 numbers, because P as two e4m3 terms would cost the softmax warps, which are what everybody waits for,
+// several operations a score, and turning V's codes into bf16 costs four other warps five operations for two of them.  V's tiles hold the
+// codes; the scales are in the probabilities: p_j = 2^(y_j + log2 vs_j - m), y_j the score in log2 units and m the row's reference, which
+// follows the largest y_j + log2 vs_j (a page's scale is one addition for 16 scores at least); the sum of 2^(y_j - m) takes p's sums of 16
+// times 1 / vs.  bf16 has the exponents for any two pages' scales, which are within 2^96 of each other.
+// A NaN code of V is 0 for the product; the first key that has one is kept per element, and the epilogue makes the element of the rows that
+// see it NaN.
+// Tensor memory: S [0,128)  P_A [128,192)  P_B [192,256)  O_A [256,256+D)  O_B [384,384+D).
+// All mbarrier waits are bounded; on expiry the CTA raises its abort flag, every role drains, TMEM is freed and
+// WPP_ERR_TIMEOUT is written to the status word.
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "wpp_device.h"
+#include "wpp_kv8.cuh"
+#include "wpp_plan_format.h"
+#include "wpp_ptx.cuh"
+
+namespace kv8tiles {
+using namespace wpp;
+
+constexpr int kThreads = 512;
+constexpr uint32_t kTmemCols = 512, kColS = 0;
+__host__ __device__ constexpr uint32_t col_p(int hf) { return 128u + 64u * hf; }
+__host__ __device__ constexpr uint32_t col_o(int hf) { return 256u + 128u * hf; }
+constexpr int kRegsSoftmax = 184, kRegsCodes = 96, kRegsUtil = 48;
+static_assert(8 * kRegsSoftmax + 4 * kRegsCodes + 4 * kRegsUtil <= 2048, "register file exceeded");
+constexpr float kRefSlack = 16.f;
+constexpr int kPar = 4;                    // key steps of a half whose scales are held
+constexpr int kNan = 8;                    // tiles whose first NaN codes of V are held
+
+template <int D>
+struct Cfg {
+    static constexpr int kHalves = D / 64;
+    static constexpr int kTileBytes = 128 * D * 2, kHalfBytes = 128 * 128;     // bf16: a half of Q, a step of V
+    static constexpr int kCodeBytes = 128 * D;                                 // a step of K or V as codes
+    static constexpr int kStages = D == 128 ? 2 : 4;                           // of K's ring and of that of V's codes
+    static constexpr int kOffV = 2 * kTileBytes, kOffK = kOffV + 2 * kTileBytes, kOffRaw = kOffK + kStages * kCodeBytes;
+    static constexpr int kOffStage = kOffRaw + kStages * kCodeBytes;           // 8 x 2 KB
+    static constexpr int kOffPar = kOffStage + 8 * 2048;               // float4 [2][kPar][8], a ring for each half: of 16 keys: ks scale, log2 vs, 1 / vs
+    static constexpr int kOffDown = kOffPar + 2 * kPar * 128;          // float [2][2][128]: what Q's rows were multiplied by, inverse, by tile parity and half
+    static constexpr int kOffNan = kOffDown + 2 * 2 * 128 * 4;         // int [kNan][D]: first key whose code of V is NaN; int [kNan]: first of all
+    static constexpr int kOffBars = kOffNan + kNan * (D + 1) * 4;
+    static constexpr int kTileQ = 2;
+    static constexpr int kNumBars = 3 + 4 * kStages + 4 + 2 * kPar + 1 + 5 * 2 + 2 * kTileQ;
+    static constexpr int kOffMisc = kOffBars + 8 * kNumBars;           // tmem address, abort flag, tile ids
+    static constexpr int kSmemBytes = kOffMisc + 8 + 4 * kTileQ + 1024;
+    static_assert(kOffBars % 8 == 0, "barriers");
+    static_assert(kSmemBytes <= 232448, "more shared memory than a CTA can have");
+};
+
+struct Ring {
+    uint32_t stage, phase;
+    __device__ __forceinline__ void advance(uint32_t n) {
+        if (++stage == n) { stage = 0; phase ^= 1u; }
+    }
+};
+
+struct UnitView {
+    int request, kv_begin, n_steps, n[2], P, kv_len, q_off;
+    bool mismatch;
+};
+__device__ __forceinline__ UnitView view_of(const WppUnit& un, const Kv4AttnParams& p, const int32_t* q_offsets, const int32_t* plan_prefix) {
+    UnitView v;
+    v.request = un.request;
+    v.kv_begin = un.kv_begin;
+    v.P = p.prefix_lens[un.request];
+    const int C = p.chunk_lens[un.request];
+    v.kv_len = v.P + C;
+    v.q_off = q_offsets[un.request];
+    v.mismatch = (v.P != plan_prefix[un.request]) || (C != q_offsets[un.request + 1] - v.q_off);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int end = (un.rows[h] > 0 && !v.mismatch) ? (v.P + un.row0[h] + un.rows[h] + 127) / 128 : 0;
+        v.n[h] = max(0, min(un.kv_end, end) - un.kv_begin);
+    }
+    v.n_steps = max(v.n[0], v.n[1]);
+    return v;
+}
+
+// Two codes of a word (bytes 0 and 1, or 2 and 3) as bf16 numbers, exact; a NaN code comes out as 480.  An e4m3 number's bits, its sign
+// apart, are a bf16 number's of 2^-120 times its size.
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t codes_bf16x2(uint32_t w, bool high) {
+    const uint32_t x = __byte_perm(w, 0u, high ? 0x3322 : 0x1100);
+    uint32_t r;
+    asm("lop3.b32 %0, %1, %2, %3, 0xea;" : "=r"(r) : "r"(x), "r"(0x80008000u), "r"((x >> 4) & 0x07f007f0u));
+    return mul_bf16x2(r, 0x7b807b80u);                                 // 2^120
+}
+// bits 7, 15, 23, 31: which of the four codes are NaN
+__device__ __forceinline__ uint32_t nan_bits(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+
+__device__ __forceinline__ void st_shared_16(uint32_t at, const uint32_t (&y)[4]) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+}
+
+// D[tmem] (+)= A[smem] * B[smem], 128 x 128 x 32, e4m3 in, fp32 out
+__device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+// Instruction descriptor: e4m3 x e4m3 -> fp32, M = 128, both factors K-major (types 0 are e4m3; see idesc_bf16)
+constexpr uint32_t kIdescE4m3 = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
+// K's tiles: rows of 128 bytes with the 128-byte swizzle, or of 64 with the 64-byte one (layout 4; groups of 8 rows are 512 bytes apart)
+template <int D>
+__device__ __forceinline__ uint64_t k_desc(uint32_t saddr) {
+    if constexpr (D == 128) return smem_desc_sw128(saddr, 16, 1024);
+    return static_cast<uint64_t>((saddr & 0x3FFFFu) >> 4) | (1ull << 16) | (static_cast<uint64_t>(512 >> 4) << 32) | (1ull << 46) | (4ull << 61);
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_constant__ CUtensorMap tm_q64, const __grid_constant__ CUtensorMap tm_q32,
+                     const __grid_constant__ CUtensorMap tm_q16, const __grid_constant__ CUtensorMap tm_k, const __grid_constant__ CUtensorMap tm_v,
+                     const Kv4AttnParams p) {
+    using C = Cfg<D>;
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t smem_base = (smem_u32(smem_raw) + 1023u) & ~1023u;
+    uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
+    const uint32_t sQ = smem_base, sV = smem_base + C::kOffV, sK = smem_base + C::kOffK, sRaw = smem_base + C::kOffRaw, bars = smem_base + C::kOffBars;
+    const uint32_t bQFull = bars, bQReady = bars + 8, bQEmpty = bars + 16;
+    // k_full: the codes by TMA and the scales by warp 15; raw: V's codes; v: its numbers
+    const uint32_t bKFull = bars + 24, bKEmpty = bKFull + 8 * C::kStages, bRawFull = bKEmpty + 8 * C::kStages, bRawEmpty = bRawFull + 8 * C::kStages;
+    const uint32_t bVFull = bRawEmpty + 8 * C::kStages, bVEmpty = bVFull + 16, bParEmpty = bVEmpty + 16;
+    const uint32_t bSFree = bParEmpty + 16 * kPar, bHalf = bSFree + 8;
+    auto bSFull = [&](int h) { return bHalf + 40 * h; };
+    auto bPReady = [&](int h) { return bHalf + 40 * h + 8; };
+    auto bPFree = [&](int h) { return bHalf + 40 * h + 16; };
+    auto bOFinal = [&](int h) { return bHalf + 40 * h + 24; };
+    auto bOFree = [&](int h) { return bHalf + 40 * h + 32; };
+    const uint32_t bTileFull = bHalf + 80, bTileEmpty = bTileFull + 8 * C::kTileQ;
+    float4* s_par = reinterpret_cast<float4*>(smem_gen + C::kOffPar);
+    float* s_down = reinterpret_cast<float*>(smem_gen + C::kOffDown);
+    int32_t* s_nan = reinterpret_cast<int32_t*>(smem_gen + C::kOffNan);
+    int32_t* s_nan_any = s_nan + kNan * D;
+    volatile uint32_t* tmem_slot = reinterpret_cast<volatile uint32_t*>(smem_gen + C::kOffMisc);
+    volatile uint32_t* abort_flag = tmem_slot + 1;
+    volatile int32_t* tile_ids = reinterpret_cast<volatile int32_t*>(tmem_slot + 2);
+    constexpr uint32_t kTileConsumers = 2 + 256 + 128 + 32;      // two issuing threads, softmax, codes, scales
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wg = warp >> 2;
+
+    if (threadIdx.x == 0) {
+        mbar_init(bQFull, 1); mbar_init(bQReady, 128); mbar_init(bQEmpty, 1);
+        for (int s = 0; s < C::kStages; ++s) {
+            mbar_init(bKFull + 8 * s, 2); mbar_init(bKEmpty + 8 * s, 1); mbar_init(bRawFull + 8 * s, 1); mbar_init(bRawEmpty + 8 * s, 128);
+        }
+        for (int s = 0; s < 2; ++s) { mbar_init(bVFull + 8 * s, 128); mbar_init(bVEmpty + 8 * s, 1); }
+        for (int s = 0; s < 2 * kPar; ++s) mbar_init(bParEmpty + 8 * s, 4);
+        mbar_init(bSFree, 128);
+        for (int h = 0; h < 2; ++h) {
+            mbar_init(bSFull(h), 1); mbar_init(bPReady(h), 128); mbar_init(bPFree(h), 1); mbar_init(bOFinal(h), 1); mbar_init(bOFree(h), 128);
+        }
+        for (int i = 0; i < C::kTileQ; ++i) { mbar_init(bTileFull + 8 * i, 1); mbar_init(bTileEmpty + 8 * i, kTileConsumers); }
+        *abort_flag = 0u;
+        fence_barrier_init();
+    }
+    for (int i = threadIdx.x; i < kNan * (D + 1); i += kThreads) s_nan[i] = 0x7fffffff;
+    if (warp == 12) {
+        tmem_alloc(smem_u32(const_cast<uint32_t*>(tmem_slot)), kTmemCols);
+        tmem_relinquish();
+    }
+    if (warp == 13 && lane == 0) {
+        prefetch_tensormap(&tm_q); prefetch_tensormap(&tm_q64); prefetch_tensormap(&tm_q32); prefetch_tensormap(&tm_q16);
+        prefetch_tensormap(&tm_k); prefetch_tensormap(&tm_v);
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    grid_launch_dependents();
+    grid_dependency_wait();
+
+    const char* plan = static_cast<const char*>(p.plan);
+    const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets);
+    const int32_t* plan_prefix = reinterpret_cast<const int32_t*>(plan + p.off_prefix);
+    const WppUnit* units = reinterpret_cast<const WppUnit*>(plan + p.off_units) + p.first_tile;
+    const int num_units = p.num_tiles;
+    Ring tile_ring = {0, 0};
+    auto next_tile = [&]() -> int {        // -1 = no more tiles, -2 = the wait was abandoned
+        if (!mbar_wait(bTileFull + 8 * tile_ring.stage, tile_ring.phase, abort_flag)) return -2;
+        const int id = tile_ids[tile_ring.stage];
+        mbar_arrive(bTileEmpty + 8 * tile_ring.stage);
+        tile_ring.advance(C::kTileQ);
+        return id;
+    };
+    const int page_shift = 31 - __clz(p.page_size), ppt = 128 >> page_shift;       // ppt: pages of a key step
+
+    if (wg == 3) {
+        setmaxnreg_dec<kRegsUtil>();
+        if (warp == 13) {
+            // ================================================================ tiles, Q, and the codes of K and V
+            Ring ring_k = {0, 0}, ring_v = {0, 0};
+            uint32_t q_phase = 0;
+            bool first = true, dead = false;
+            while (!dead) {
+                int u = (int)blockIdx.x;
+                if (!first) {
+                    if (lane == 0) u = p.tile_counter ? (int)(gridDim.x + atomicAdd(p.tile_counter, 1u)) : num_units;
+                    u = __shfl_sync(0xffffffffu, u, 0);
+                }
+                first = false;
+                if (u >= num_units) u = -1;
+                {
+                    const bool ok = mbar_wait(bTileEmpty + 8 * tile_ring.stage, tile_ring.phase ^ 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, ok)) break;
+                    if (lane == 0) {
+                        tile_ids[tile_ring.stage] = u;
+                        mbar_arrive(bTileFull + 8 * tile_ring.stage);
+                    }
+                    tile_ring.advance(C::kTileQ);
+                }
+                if (u < 0) break;
+                const WppUnit un = units[u];
+                const UnitView v = view_of(un, p, q_offsets, plan_prefix);
+                if (v.mismatch && lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_PLAN_MISMATCH);
+                if (v.n_steps == 0) continue;
+                const int kvh = un.head[0] / p.group, n_pages = (v.kv_len + p.page_size - 1) >> page_shift;
+                const int32_t* bt = p.block_tables + (int64_t)un.request * p.max_blocks;
+                // a step's codes of K or of V: a lane for each page
+                auto load_step = [&](const CUtensorMap* tm, int j, uint32_t to, uint32_t full, uint32_t empty, Ring& ring) -> bool {
+                    const int page0 = (v.kv_begin + j) * ppt, cnt = min(ppt, n_pages - page0);
+                    int pid = 0;
+                    if (lane < cnt) pid = bt[page0 + lane];
+                    if (pid < 0 || pid >= p.num_pages) {
+                        if (p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
+                        pid = 0;
+                    }
+                    const bool ok = mbar_wait(empty + 8 * ring.stage, ring.phase ^ 1u, abort_flag);
+                    if (!__all_sync(0xffffffffu, ok)) return false;
+                    if (lane == 0) mbar_arrive_expect_tx(full + 8 * ring.stage, (uint32_t)(cnt * p.page_size * D));
+                    __syncwarp();
+                    if (lane < cnt) tma_load_4d(to + ring.stage * C::kCodeBytes + lane * p.page_size * D, tm, full + 8 * ring.stage, 0, 0, kvh, pid);
+                    ring.advance(C::kStages);
+                    return true;
+                };
+                // K(0) only needs a place in the ring, which is free before the tile before's Q is
+                if (!load_step(&tm_k, 0, sK, bKFull, bKEmpty, ring_k)) break;
+                const bool ok = mbar_wait(bQEmpty, q_phase ^ 1u, abort_flag);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                q_phase ^= 1u;
+                if (lane == 0) mbar_arrive_expect_tx(bQFull, ((v.n[0] > 0) + (v.n[1] > 0)) * C::kTileBytes);
+                __syncwarp();
+                const int rph = 128 / un.pack;
+                const CUtensorMap* qm = un.pack == 1 ? &tm_q : un.pack == 2 ? &tm_q64 : un.pack == 4 ? &tm_q32 : &tm_q16;
+                const int per_half = un.pack * C::kHalves;
+                for (int b = lane; b < 2 * per_half; b += 32) {
+                    const int hf = b / per_half, k = (b % per_half) / C::kHalves, h = b % C::kHalves;
+                    if ((hf ? v.n[1] : v.n[0]) == 0) continue;
+                    // (more places than heads in the group: the last head again, into rows that nobody stores)
+                    tma_load_3d(sQ + hf * C::kTileBytes + h * C::kHalfBytes + k * rph * 128, qm, bQFull, h * 64,
+                                (hf ? un.head[1] : un.head[0]) + min(k, p.group - 1), v.q_off + (hf ? un.row0[1] : un.row0[0]));
+                }
+                __syncwarp();
+                for (int k = 0; k <= v.n_steps && !dead; ++k) {
+                    if (k >= 1 && !load_step(&tm_v, k - 1, sRaw, bRawFull, bRawEmpty, ring_v)) dead = true;
+                    if (!dead && k + 1 < v.n_steps && !load_step(&tm_k, k + 1, sK, bKFull, bKEmpty, ring_k)) dead = true;
+                }
+            }
+        } else if (warp == 15) {
+            // ================================================================ the scales of a step's pages, asked for a step ahead
+            Ring ring = {0, 0}, ring_p[2] = {{0, 0}, {0, 0}};
+            bool dead = false;
+            while (!dead) {
+                const int u = next_tile();
+                if (!__all_sync(0xffffffffu, u != -2) || u < 0) break;
+                const WppUnit un = units[u];
+                const UnitView v = view_of(un, p, q_offsets, plan_prefix);
+                if (v.n_steps == 0) continue;
+                const int kvh = un.head[0] / p.group, group = lane & 7;
+                const int32_t* bt = p.block_tables + (int64_t)un.request * p.max_blocks;
+                const uint8_t* pool = (lane & 8 ? p.v_cache : p.k_cache) + kvh * p.head_bytes + p.page_size * D;
+                auto scale_of = [&](int k) -> float {                  // lanes 0 to 7: K's, of the step's groups of 16 keys; 8 to 15: V's; 0: no such key
+                    const int key = (v.kv_begin + k) * 128 + group * 16;
+                    if (lane >= 16 || k >= v.n_steps || key >= v.kv_len) return 0.f;
+                    const int pid = bt[key >> page_shift];
+                    return *reinterpret_cast<const float*>(pool + (pid < 0 || pid >= p.num_pages ? 0 : pid) * p.page_bytes);
+                };
+                float next = scale_of(0);
+                for (int k = 0; k < v.n_steps; ++k) {
+                    const float mine = next, vs = __shfl_sync(0xffffffffu, mine, 8 + group);
+                    next = scale_of(k + 1);
+                    const int ev = vs == 0.f ? 0 : min(max(exponent_of(vs), -126), 126);
+                    const float4 par = make_float4(mine * p.scale_log2, (float)ev, power_of_two(-ev), 0.f);
+                    bool ok = mbar_wait(bKEmpty + 8 * ring.stage, ring.phase ^ 1u, abort_flag);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if (k >= v.n[h]) continue;
+                        ok = ok && mbar_wait(bParEmpty + 8 * (h * kPar + ring_p[h].stage), ring_p[h].phase ^ 1u, abort_flag);
+                        if (ok && lane < 8) s_par[(h * kPar + ring_p[h].stage) * 8 + lane] = par;
+                        ring_p[h].advance(kPar);
+                    }
+                    if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }
+                    if (lane == 0) mbar_arrive(bKFull + 8 * ring.stage);
+                    ring.advance(C::kStages);
+                }
+            }
+        } else if (warp == 12 && lane == 0) {
+            // ================================================================ issuer of S = Q K^T
+            Ring ring = {0, 0};
+            uint32_t q_phase = 0, sfree_phase = 0;
+            const uint64_t q_desc0 = smem_desc_sw128(sQ, 16, 1024), k_desc0 = k_desc<D>(sK);
+            constexpr uint32_t kLo = (D == 128 ? C::kHalfBytes : 64) >> 4;             // from hi to lo
+            const uint32_t tS = tmem + kColS;
+            bool dead = false;
+            while (!dead) {
+                const int u = next_tile();
+                if (u < 0) break;
+                const WppUnit un = units[u];
+                const UnitView v = view_of(un, p, q_offsets, plan_prefix);
+                if (v.n_steps == 0) continue;
+                if (!mbar_wait(bQReady, q_phase, abort_flag)) break;
+                q_phase ^= 1u;
+                for (int k = 0; k < v.n_steps && !dead; ++k) {
+                    if (!mbar_wait(bKFull + 8 * ring.stage, ring.phase, abort_flag)) { dead = true; break; }
+                    const uint64_t kd = k_desc0 + (uint64_t)(ring.stage * (C::kCodeBytes >> 4));
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        if (k >= v.n[hf]) continue;
+                        if (!mbar_wait(bSFree, sfree_phase ^ 1u, abort_flag)) { dead = true; break; }
+                        sfree_phase ^= 1u;
+                        tc_fence_after();
+                        const uint64_t qd = q_desc0 + (uint64_t)(hf * (C::kTileBytes >> 4));
+#pragma unroll
+                        for (int kk = 0; kk < D / 32; ++kk) {
+                            mma_e4m3(tS, qd + kk * 2, kd + kk * 2, kIdescE4m3, kk > 0);
+                            mma_e4m3(tS, qd + kLo + kk * 2, kd + kk * 2, kIdescE4m3, 1u);
+                        }
+                        mma_commit(bSFull(hf));
+                    }
+                    if (dead) break;
+                    mma_commit(bKEmpty + 8 * ring.stage);
+                    ring.advance(C::kStages);
+                }
+                if (!dead) mma_commit(bQEmpty);
+            }
+        } else if (warp == 14 && lane == 0) {
+            // ================================================================ issuer of O += P V
+            Ring ring = {0, 0};
+            uint32_t p_phase[2] = {0, 0}, of_phase[2] = {0, 0};
+            constexpr uint32_t idesc_pv = idesc_bf16(D, 0, 1);
+            const uint64_t v_desc0 = smem_desc_sw128(sV, C::kHalfBytes, 1024);
+            bool dead = false;
+            while (!dead) {
+                const int u = next_tile();
+                if (u < 0) break;
+                const WppUnit un = units[u];
+                const UnitView v = view_of(un, p, q_offsets, plan_prefix);
+                if (v.n_steps == 0) continue;
+                for (int k = 0; k < v.n_steps && !dead; ++k) {
+                    if (!mbar_wait(bVFull + 8 * ring.stage, ring.phase, abort_flag)) { dead = true; break; }
+                    const uint64_t vd = v_desc0 + (uint64_t)(ring.stage * (C::kTileBytes >> 4));
+#pragma unroll
+                    for (int hf = 0; hf < 2; ++hf) {
+                        const int n = v.n[hf];
+                        if (k >= n) continue;
+                        if (!mbar_wait(bPReady(hf), p_phase[hf], abort_flag)) { dead = true; break; }
+                        p_phase[hf] ^= 1u;
+                        if (k == 0) {          // the tile before's O has been read
+                            if (!mbar_wait(bOFree(hf), of_phase[hf] ^ 1u, abort_flag)) { dead = true; break; }
+                            of_phase[hf] ^= 1u;
+                        }
+                        tc_fence_after();
+                        const uint32_t tP = tmem + col_p(hf), tO = tmem + col_o(hf);
+                        if (k > 0) mma_ts_accumulate(tO, tP, vd, idesc_pv); else mma_ts_overwrite(tO, tP, vd, idesc_pv);
+#pragma unroll
+                        for (int kk = 1; kk < 8; ++kk) mma_ts_accumulate(tO, tP + kk * 8, vd + (uint64_t)(kk * 128), idesc_pv);
+                        mma_commit(bPFree(hf));
+                        if (k + 1 == n) mma_commit(bOFinal(hf));
+                    }
+                    if (dead) break;
+                    mma_commit(bVEmpty + 8 * ring.stage);
+                    ring.advance(2);
+                }
+            }
+        }
+    } else if (wg == 2) {
+        // ================================================================ Q as two terms, V's codes as bf16
+        setmaxnreg_dec<kRegsCodes>();
+        constexpr int kChunks = D / 16, kApart = 32 / kChunks;         // 16-byte pieces of a row of codes; rows of a warp at a time
+        const int r = threadIdx.x & 127, c = lane % kChunks, row0 = (warp & 3) * 32 + lane / kChunks;
+        const bool swap = D == 128 && (c & 4);         // of lanes 4 apart, whose numbers would meet in a bank, one begins with its second half
+        // where the two pieces of 8 numbers go in the tile's first row of this thread; kApart rows on it is the same place but for a turned bit
+        uint32_t place[2];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            place[q] = (uint32_t)((c >> 2) * C::kHalfBytes + row0 * 128 + ((((c & 3) * 2 + (q ^ (swap ? 1 : 0))) ^ (row0 & 7)) << 4));
+        Ring ring_raw = {0, 0}, ring_v = {0, 0};
+        uint32_t q_phase = 0, tiles = 0;               // tiles: with work, so far
+        bool dead = false;
+        while (!dead) {
+            const int u = next_tile();
+            if (!__all_sync(0xffffffffu, u != -2) || u < 0) break;
+            const WppUnit un = units[u];
+            const UnitView v = view_of(un, p, q_offsets, plan_prefix);
+            if (v.n_steps == 0) continue;
+            const int nan_slot = tiles % kNan;
+            // the place of four tiles on: nobody is so far behind that it reads the one of four tiles ago, nor so far ahead
+            if (r < D) s_nan[(tiles + kNan / 2) % kNan * D + r] = 0x7fffffff;
+            if (r == 0) s_nan_any[(tiles + kNan / 2) % kNan] = 0x7fffffff;
+            // ---- Q (thread = row): hi into the places of the row's first elements, lo behind it, once all have been read
+            if (!__all_sync(0xffffffffu, mbar_wait(bQFull, q_phase, abort_flag))) break;
+            q_phase ^= 1u;
+#pragma unroll 1
+            for (int hf = 0; hf < 2; ++hf) {
+                if (v.n[hf] == 0) continue;
+                uint8_t* const row = smem_gen + hf * C::kTileBytes + r * 128;
+                auto numbers = [&](int ch) { return *reinterpret_cast<const uint4*>(row + (ch >> 3) * C::kHalfBytes + (((ch & 7) ^ (r & 7)) << 4)); };
+                float top = 0.f;
+#pragma unroll 4
+                for (int ch = 0; ch < D / 8; ++ch) {
+                    const uint4 z = numbers(ch);
+                    const uint32_t w[4] = {z.x, z.y, z.z, z.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i] << 16)), fabsf(__uint_as_float(w[i] & 0xffff0000u))));
+                }
+                // 2^e and 2^-e, both normal numbers; an infinity makes the row NaN
+                const int biased = (int)(__float_as_uint(top) >> 23), e = min(max(134 - biased, -119), 126);
+                const float up = biased == 255 ? NAN : power_of_two(e);
+                s_down[((tiles & 1) * 2 + hf) * 128 + r] = power_of_two(-e);
+                uint32_t lo[D / 4];
+#pragma unroll
+                for (int ch = 0; ch < D / 16; ++ch) {
+                    const uint4 z[2] = {numbers(2 * ch), numbers(2 * ch + 1)};
+                    uint32_t hi[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t w0 = i & 1 ? z[i >> 1].z : z[i >> 1].x, w1 = i & 1 ? z[i >> 1].w : z[i >> 1].y;
+                        const float x0 = __uint_as_float(w0 << 16) * up, x1 = __uint_as_float(w0 & 0xffff0000u) * up;
+                        const float x2 = __uint_as_float(w1 << 16) * up, x3 = __uint_as_float(w1 & 0xffff0000u) * up;
+                        const uint16_t a = codes_of(x0, x1), b = codes_of(x2, x3);
+                        const uint32_t fa = codes_f16x2(a), fb = codes_f16x2(b);
+                        hi[i] = (uint32_t)a | (uint32_t)b << 16;
+                        lo[4 * ch + i] = (uint32_t)codes_of(x0 - f16_low(fa), x1 - f16_high(fa)) | (uint32_t)codes_of(x2 - f16_low(fb), x3 - f16_high(fb)) << 16;
+                    }
+                    // (piece ch of the codes takes the place of piece ch of the numbers, which has been read)
+                    *reinterpret_cast<uint4*>(row + ((ch ^ (r & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                }
+#pragma unroll
+                for (int ch = 0; ch < D / 16; ++ch) {
+                    uint8_t* const to = D == 128 ? row + C::kHalfBytes + ((ch ^ (r & 7)) << 4) : row + (((4 + ch) ^ (r & 7)) << 4);
+                    *reinterpret_cast<uint4*>(to) = make_uint4(lo[4 * ch], lo[4 * ch + 1], lo[4 * ch + 2], lo[4 * ch + 3]);
+                }
+            }
+            fence_proxy_async_smem();
+            mbar_arrive(bQReady);
+            ++tiles;
+            // ---- V
+            for (int k = 0; k < v.n_steps; ++k) {
+                bool ok = mbar_wait(bRawFull + 8 * ring_raw.stage, ring_raw.phase, abort_flag);
+                ok = ok && mbar_wait(bVEmpty + 8 * ring_v.stage, ring_v.phase ^ 1u, abort_flag);
+                if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }
+                const uint8_t* from = smem_gen + C::kOffRaw + ring_raw.stage * C::kCodeBytes + row0 * D + c * 16;
+                const uint32_t to = sV + ring_v.stage * C::kTileBytes;
+                const int key0 = (v.kv_begin + k) * 128, rows = v.kv_len - key0;       // rows from here on lie behind the sequence: zeros
+#pragma unroll 2
+                for (int i = 0; i < kChunks; ++i) {
+                    const int row = row0 + i * kApart;
+                    uint4 x = *reinterpret_cast<const uint4*>(from + i * kApart * D);
+                    if (row >= rows) x = make_uint4(0, 0, 0, 0);
+                    uint32_t w[4] = {swap ? x.z : x.x, swap ? x.w : x.y, swap ? x.x : x.z, swap ? x.y : x.w};
+                    if (nan_bits(w[0]) | nan_bits(w[1]) | nan_bits(w[2]) | nan_bits(w[3])) {
+#pragma unroll 1
+                        for (int b = 0; b < 16; ++b) {
+                            const int at = b ^ (swap ? 8 : 0);         // of the lane's 16 elements
+                            const uint32_t word = b < 4 ? w[0] : b < 8 ? w[1] : b < 12 ? w[2] : w[3];
+                            if ((word >> (8 * (b & 3)) & 0x7fu) == 0x7fu) {
+                                atomicMin(&s_nan[nan_slot * D + c * 16 + at], key0 + row);
+                                atomicMin(&s_nan_any[nan_slot], key0 + row);
+                            }
+                        }
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) w[j] &= ~((nan_bits(w[j]) >> 7) * 0xffu);
+                    }
+#pragma unroll
+                    for (int q = 0; q < 2; ++q) {
+                        const uint32_t y[4] = {codes_bf16x2(w[2 * q], false), codes_bf16x2(w[2 * q], true), codes_bf16x2(w[2 * q + 1], false),
+                                               codes_bf16x2(w[2 * q + 1], true)};
+                        st_shared_16(to + ((place[q] + i * kApart * 128) ^ (kApart == 4 ? (uint32_t)(i & 1) << 6 : 0u)), y);
+                    }
+                }
+                fence_proxy_async_smem();
+                mbar_arrive(bVFull + 8 * ring_v.stage);
+                mbar_arrive(bRawEmpty + 8 * ring_raw.stage);
+                ring_raw.advance(C::kStages);
+                ring_v.advance(2);
+            }
+        }
+    } else {
+        // ================================================================ softmax (thread = query row of half `hf`) and epilogue
+        setmaxnreg_inc<kRegsSoftmax>();
+        const int hf = wg, r = threadIdx.x & 127;
+        const uint32_t lane_addr = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        uint32_t s_phase = 0, pf_phase = 0, of_phase = 0, par = 0, tiles = 0;
+        bool dead = false;
+        while (!dead) {
+            const int u = next_tile();
+            if (!__all_sync(0xffffffffu, u != -2) || u < 0) break;
+            const WppUnit un = units[u];
+            const UnitView v = view_of(un, p, q_offsets, plan_prefix);
+            const int n = v.n[hf];
+            const int rph = 128 / un.pack, rr = r & (rph - 1);         // row inside its head's block
+            const bool row_ok = un.rows[hf] > 0 && rr < un.rows[hf] && r / rph < p.group;
+            const int64_t prow = ((int64_t)un.split_slot * 2 + hf) * 128 + r;
+            if (n == 0) {
+                // a split part that lies wholly above this half's diagonal, or a refused request's: no key is visible
+                if (un.split_slot >= 0 && row_ok) p.ws_lse[prow] = -INFINITY;
+            }
+            if (v.n_steps == 0) continue;
+            const int first_pos = v.P + un.row0[hf], row_last = min(first_pos + rr, v.kv_len - 1);
+            float m_ref = 0.f, l_run = 0.f, down = 0.f;
+            for (int j = 0; j < n; ++j) {
+                if (!__all_sync(0xffffffffu, mbar_wait(bSFull(hf), s_phase, abort_flag))) { dead = true; break; }
+                s_phase ^= 1u;
+                tc_fence_after();
+                if (j == 0) down = s_down[((tiles & 1) * 2 + hf) * 128 + r];
+                float s[128];
+#pragma unroll
+                for (int q4 = 0; q4 < 4; ++q4) tmem_ld32(lane_addr + kColS + q4 * 32, reinterpret_cast<uint32_t*>(s) + q4 * 32);
+                tmem_wait_ld();
+                tc_fence_before();
+                mbar_arrive(bSFree);
+                const int key0 = (v.kv_begin + j) * 128;
+                if (key0 + 127 > first_pos) {          // only steps that touch the diagonal are masked
+                    const int limit = row_last - key0;
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) s[i] = (i > limit) ? -INFINITY : s[i];
+                }
+                // ---- of 16 keys: score in log2 units and log2 of V's scale are a s + b
+                float a[8], b[8], less[8], mxx = -INFINITY;
+#pragma unroll
+                for (int g = 0; g < 8; ++g) {
+                    const float4 f = s_par[(hf * kPar + par) * 8 + g];
+                    a[g] = fmaxf(f.x * down, 1.1754944e-38f);          // (no product of an infinity with 0)
+                    b[g] = f.y;
+                    less[g] = f.z;
+                    const float* x = s + 16 * g;
+                    const float m0 = fmax3(x[0], x[1], x[2]), m1 = fmax3(x[3], x[4], x[5]), m2 = fmax3(x[6], x[7], x[8]), m3 = fmax3(x[9], x[10], x[11]);
+                    const float mg = fmaxf(fmax3(fmax3(m0, m1, m2), fmax3(m3, x[12], x[13]), x[14]), x[15]);
+                    mxx = fmaxf(mxx, fmaf(mg, a[g], b[g] - m_ref));
+                }
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bParEmpty + 8 * (hf * kPar + par));
+                par = (par + 1) % kPar;
+                bool waited = false;
+                const bool move = j == 0 || mxx > kRefSlack;
+                if (__any_sync(0xffffffffu, move)) {
+                    // how far the reference goes up (the first one may go down; a row that sees nothing keeps its)
+                    float y = j == 0 ? mxx : fmaxf(mxx, 0.f);
+                    if (y == -INFINITY) y = 0.f;
+                    const float alpha = j == 0 ? 1.f : fast_exp2(-y);
+                    m_ref += y;
+                    l_run *= alpha;
+                    if (j > 0) {
+                        if (!__all_sync(0xffffffffu, mbar_wait(bPFree(hf), pf_phase ^ 1u, abort_flag))) { dead = true; break; }
+                        pf_phase ^= 1u;
+                        waited = true;
+                        tc_fence_after();
+                        if (__any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+                            for (int q0 = 0; q0 < D; q0 += 16) {
+                                float o[16];
+                                tmem_ld8(lane_addr + col_o(hf) + q0, reinterpret_cast<uint32_t*>(o));
+                                tmem_ld8(lane_addr + col_o(hf) + q0 + 8, reinterpret_cast<uint32_t*>(o) + 8);
+                                tmem_wait_ld();
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) o[i] *= alpha;
+                                tmem_st8(lane_addr + col_o(hf) + q0, reinterpret_cast<uint32_t*>(o));
+                                tmem_st8(lane_addr + col_o(hf) + q0 + 8, reinterpret_cast<uint32_t*>(o) + 8);
+                            }
+                        }
+                    }
+                }
+                uint32_t* pk = reinterpret_cast<uint32_t*>(s);
+#pragma unroll
+                for (int g = 0; g < 8; ++g) {
+                    const uint64_t a2 = pack2(a[g], a[g]);
+                    const float off = b[g] - m_ref;
+                    const uint64_t b2 = pack2(off, off);
+                    float e[16];
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) unpack2(ffma2(pack2(s[16 * g + 2 * k], s[16 * g + 2 * k + 1]), a2, b2), e[2 * k], e[2 * k + 1]);
+#pragma unroll
+                    for (int k = 0; k < 16; ++k) e[k] = fast_exp2(e[k]);
+                    uint64_t sum2 = pack2(e[0], e[1]);
+#pragma unroll
+                    for (int k = 1; k < 8; ++k) sum2 = fadd2(sum2, pack2(e[2 * k], e[2 * k + 1]));
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) pk[8 * g + k] = pack_bf16x2(e[2 * k], e[2 * k + 1]);
+                    float t0, t1;
+                    unpack2(sum2, t0, t1);
+                    l_run = fmaf(t0 + t1, less[g], l_run);
+                }
+                if (!waited) {                         // P(j - 1) has been consumed
+                    if (!__all_sync(0xffffffffu, mbar_wait(bPFree(hf), pf_phase ^ 1u, abort_flag))) { dead = true; break; }
+                    pf_phase ^= 1u;
+                    tc_fence_after();
+                }
+#pragma unroll
+                for (int c8 = 0; c8 < 64; c8 += 8) tmem_st8(lane_addr + col_p(hf) + c8, pk + c8);
+                tmem_wait_st();
+                tc_fence_before();
+                mbar_arrive(bPReady(hf));
+            }
+            if (dead) break;
+            const int nan_slot = tiles % kNan;
+            ++tiles;
+            if (n == 0) continue;
+            // ---- epilogue
+            if (!__all_sync(0xffffffffu, mbar_wait(bOFinal(hf), of_phase, abort_flag))) break;
+            of_phase ^= 1u;
+            tc_fence_after();
+            const int64_t tok = (int64_t)v.q_off + un.row0[hf] + rr;
+            const int head = un.head[hf] + r / rph;
+            const bool nans = s_nan_any[nan_slot] <= row_last;         // of V: some elements of the row may be NaN
+            const float inv_l = l_run > 0.f ? 1.f / l_run : l_run != l_run ? l_run : 0.f;
+            const float lse2 = (l_run <= 0.f) ? -INFINITY : (m_ref + log2f(l_run));
+            uint8_t* stage = smem_gen + C::kOffStage + warp * 2048;
+            const bool split = un.split_slot >= 0;
+            const __nv_bfloat16* dst = p.out + tok * p.o_token_stride + (int64_t)head * p.o_head_stride;
+            const float* part = p.ws_o + prow * D;
+#pragma unroll 1
+            for (int q4 = 0; q4 < D / 32; ++q4) {
+                float o[32];
+                tmem_ld32(lane_addr + col_o(hf) + q4 * 32, reinterpret_cast<uint32_t*>(o));
+                tmem_wait_ld();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] *= inv_l;
+                if (__any_sync(0xffffffffu, nans)) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i)
+                        if (s_nan[nan_slot * D + q4 * 32 + i] <= row_last) o[i] = NAN;
+                }
+                uint4 w[4];
+                if (!split) {
+#pragma unroll
+                    for (int w4 = 0; w4 < 4; ++w4)
+                        w[w4] = make_uint4(pack_bf16x2(o[8 * w4], o[8 * w4 + 1]), pack_bf16x2(o[8 * w4 + 2], o[8 * w4 + 3]),
+                                           pack_bf16x2(o[8 * w4 + 4], o[8 * w4 + 5]), pack_bf16x2(o[8 * w4 + 6], o[8 * w4 + 7]));
+                    warp_store_rows64(stage, lane, w, dst, row_ok, q4 * 64);
+                } else {
+#pragma unroll
+                    for (int h2 = 0; h2 < 2; ++h2) {
+#pragma unroll
+                        for (int w4 = 0; w4 < 4; ++w4)
+                            w[w4] = make_uint4(__float_as_uint(o[16 * h2 + 4 * w4]), __float_as_uint(o[16 * h2 + 4 * w4 + 1]),
+                                               __float_as_uint(o[16 * h2 + 4 * w4 + 2]), __float_as_uint(o[16 * h2 + 4 * w4 + 3]));
+                        warp_store_rows64(stage, lane, w, part, row_ok, q4 * 128 + h2 * 64);
+                    }
+                }
+            }
+            tc_fence_before();
+            mbar_arrive(bOFree(hf));
+            if (row_ok && split) p.ws_lse[prow] = lse2;
+            else if (row_ok && p.lse) p.lse[tok * p.num_q_heads + head] = fmaxf(lse2 * 0.6931471805599453f, -INFINITY);
+        }
+    }
+
+    // ---- teardown: every loop above is bounded, so every thread gets here
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        const long long t0 = clock64();
+        while (clock64() - t0 < 400000) { }            // let copies and tensor-core work in flight land
+        if (threadIdx.x == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_TIMEOUT);
+        __syncthreads();
+    }
+    if (warp == 12) {
+        tc_fence_after();
+        tmem_dealloc(tmem, kTmemCols);
+    }
+}
+
+template <int D>
+static cudaError_t launch(const CUtensorMap* tq, const CUtensorMap* tk, const CUtensorMap* tv, const Kv4AttnParams& p, int num_ctas, cudaStream_t stream) {
+    static bool attr_set[64] = {};
+    int dev = 0;
+    cudaGetDevice(&dev);
+    if (dev >= 0 && dev < 64 && !attr_set[dev]) {
+        cudaError_t e = cudaFuncSetAttribute(wpp_kv8_tiles_kernel<D>, cudaFuncAttributeMaxDynamicSharedMemorySize, Cfg<D>::kSmemBytes);
+        if (e != cudaSuccess) return e;
+        attr_set[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)num_ctas);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = Cfg<D>::kSmemBytes;
+    cfg.stream = stream;
+    cudaLaunchAttribute overlap;
+    overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    overlap.val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = &overlap;
+    cfg.numAttrs = 1;
+    return cudaLaunchKernelEx(&cfg, wpp_kv8_tiles_kernel<D>, tq[0], tq[1], tq[2], tq[3], *tk, *tv, p);
+}
+
+}  // namespace kv8tiles
+
+// tq: four maps of q with boxes of 128, 64, 32 and 16 rows; tk, tv: of the pools' codes, boxes of a page's rows
+extern "C" int wpp_launch_kv8_tiles(int head_dim, const CUtensorMap* tq, const CUtensorMap* tk, const CUtensorMap* tv, const wpp::Kv4AttnParams* p,
+                                    int num_ctas, void* stream) {
+    return (int)(head_dim == 128 ? kv8tiles::launch<128>(tq, tk, tv, *p, num_ctas, (cudaStream_t)stream)
+                                 : kv8tiles::launch<64>(tq, tk, tv, *p, num_ctas, (cudaStream_t)stream));
+}

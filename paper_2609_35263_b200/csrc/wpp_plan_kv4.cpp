@@ -99,7 +99,6 @@ static bool is_few(const wpp_batch_desc* d, int64_t C, int64_t walks) {
     return walks == INT64_MAX || few_blocks(d, C) <= walks * tiles_of(d, C);
 }
 static int64_t few_walks(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t* prefix_lens, const int32_t* chunk_lens) {
-    if (d->dtype == WPP_KV8) return INT64_MAX;
     if (o->shape) return o->shape == 1 ? 0 : INT64_MAX;
     const int32_t G = d->num_q_heads / d->num_kv_heads;
     const int64_t choices[3] = {kFewWalks, INT64_MAX, 0};

@@ -9,13 +9,13 @@
 // power of two that puts its largest element into [128, 256): hi is q rounded to e4m3, four significant bits, lo what is left, of which a
 // bf16 number has no more than e4m3 holds; elements below 2^-9 of the row's largest are off by up to 2^-18 of it, the others exact.  Two products of
 // 8-bit numbers take as long as one of bf16.
-// O += P V is a product of bf16 numbers, because P as two e4m3 terms would cost the softmax warps, which are what everybody waits for,
-// several operations a score, and turning V's codes into bf16 costs four other warps five operations for two of them.  V's tiles hold the
-// codes; the scales are in the probabilities: p_j = 2^(y_j + log2 vs_j - m), y_j the score in log2 units and m the row's reference, which
-// follows the largest y_j + log2 vs_j (a page's scale is one addition for 16 scores at least); the sum of 2^(y_j - m) takes p's sums of 16
-// times 1 / vs.  bf16 has the exponents for any two pages' scales, which are within 2^96 of each other.
-// A NaN code of V is 0 for the product; the first key that has one is kept per element, and the epilogue makes the element of the rows that
-// see it NaN.
+// O += P V is a product of f16 numbers, because P as two e4m3 terms would cost the softmax warps, which are what everybody waits for,
+// several operations a score, and four other warps turn two of V's codes into f16 by one.  V's tiles hold code * vs / v, vs the scale of
+// the code's page and v that of the tile's first ones: exact, being a power of two, while vs / v is from 2^-12 to 2^4.  A step with a page
+// outside of that is a product of bf16 numbers, whose exponents do for any two scales.  So P is the softmax's own, 2^(y - m), m at most 15
+// below the row's largest score y in log2 units: off by 2^-11 of itself or by 2^-32 of the largest (2^-8 of itself in bf16).
+// Where not all rows see all of a step's keys, a NaN code of V is 0 for the product; the first key that has one is kept per element, and
+// the epilogue makes the element of the rows that see it NaN.
 // Tensor memory: S [0,128)  P_A [128,192)  P_B [192,256)  O_A [256,256+D)  O_B [384,384+D).
 // All mbarrier waits are bounded; on expiry the CTA raises its abort flag, every role drains, TMEM is freed and
 // WPP_ERR_TIMEOUT is written to the status word.
@@ -38,7 +38,8 @@ __host__ __device__ constexpr uint32_t col_p(int hf) { return 128u + 64u * hf; }
 __host__ __device__ constexpr uint32_t col_o(int hf) { return 256u + 128u * hf; }
 constexpr int kRegsSoftmax = 184, kRegsCodes = 96, kRegsUtil = 48;
 static_assert(8 * kRegsSoftmax + 4 * kRegsCodes + 4 * kRegsUtil <= 2048, "register file exceeded");
-constexpr float kRefSlack = 16.f;
+constexpr float kTop = 7.f, kMost = 15.f;  // log2 of a row's largest p when its reference is moved, and when it has to be
+constexpr int kScaleDown = -12, kScaleUp = 4;      // log2 of vs / v that f16 numbers take
 constexpr int kPar = 4;                    // key steps of a half whose scales are held
 constexpr int kNan = 8;                    // tiles whose first NaN codes of V are held
 
@@ -50,8 +51,9 @@ struct Cfg {
     static constexpr int kStages = D == 128 ? 2 : 4;                           // of K's ring and of that of V's codes
     static constexpr int kOffV = 2 * kTileBytes, kOffK = kOffV + 2 * kTileBytes, kOffRaw = kOffK + kStages * kCodeBytes;
     static constexpr int kOffStage = kOffRaw + kStages * kCodeBytes;           // 8 x 2 KB
-    static constexpr int kOffPar = kOffStage + 8 * 2048;               // float4 [2][kPar][8], a ring for each half: of 16 keys: ks scale, log2 vs, 1 / vs
-    static constexpr int kOffDown = kOffPar + 2 * kPar * 128;          // float [2][2][128]: what Q's rows were multiplied by, inverse, by tile parity and half
+    static constexpr int kOffPar = kOffStage + 8 * 2048;               // float [2][kPar][12], a ring for each half: of 16 keys each: K's scale; whether P is bf16; log2 v
+    static constexpr int kOffVPar = kOffPar + 2 * kPar * 48;           // int [kStages][12]: log2 of vs / v of 16 keys each, whether that wants bf16; int [2]: so of V's tiles
+    static constexpr int kOffDown = kOffVPar + kStages * 48 + 16;      // float [2][2][128]: what Q's rows were multiplied by, inverse, by tile parity and half
     static constexpr int kOffNan = kOffDown + 2 * 2 * 128 * 4;         // int [kNan][D]: first key whose code of V is NaN; int [kNan]: first of all
     static constexpr int kOffBars = kOffNan + kNan * (D + 1) * 4;
     static constexpr int kTileQ = 2;
@@ -98,6 +100,16 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
     asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
     return r;
 }
+__device__ __forceinline__ uint32_t mul_f16x2(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
 __device__ __forceinline__ uint32_t codes_bf16x2(uint32_t w, bool high) {
     const uint32_t x = __byte_perm(w, 0u, high ? 0x3322 : 0x1100);
     uint32_t r;
@@ -107,8 +119,8 @@ __device__ __forceinline__ uint32_t codes_bf16x2(uint32_t w, bool high) {
 // bits 7, 15, 23, 31: which of the four codes are NaN
 __device__ __forceinline__ uint32_t nan_bits(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 
-__device__ __forceinline__ void st_shared_16(uint32_t at, const uint32_t (&y)[4]) {
-    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y[0]), "r"(y[1]), "r"(y[2]), "r"(y[3]) : "memory");
+__device__ __forceinline__ void st_shared_16(uint32_t at, uint4 y) {
+    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(y.x), "r"(y.y), "r"(y.z), "r"(y.w) : "memory");
 }
 
 // D[tmem] (+)= A[smem] * B[smem], 128 x 128 x 32, e4m3 in, fp32 out
@@ -119,6 +131,22 @@ __device__ __forceinline__ void mma_e4m3(uint32_t d_tmem, uint64_t a_desc, uint6
         ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
         : "memory");
 }
+// Eight scores from tensor memory, a x - m, those above the limit -infinity; returns the largest
+__device__ __forceinline__ float wide_scores(uint32_t taddr, float a, int limit, float m, float* y) {
+    tmem_ld8(taddr, reinterpret_cast<uint32_t*>(y));
+    tmem_wait_ld();
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        y[i] = i > limit ? -INFINITY : fmaf(a, y[i], -m);
+        most = fmaxf(most, y[i]);
+    }
+    return most;
+}
+__device__ __forceinline__ void tmem_st4(uint32_t taddr, const uint32_t* r) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x4.b32 [%0], {%1, %2, %3, %4};" ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]) : "memory");
+}
+
 // Instruction descriptor: e4m3 x e4m3 -> fp32, M = 128, both factors K-major (types 0 are e4m3; see idesc_bf16)
 constexpr uint32_t kIdescE4m3 = (1u << 4) | ((128u >> 3) << 17) | ((128u >> 4) << 24);
 // K's tiles: rows of 128 bytes with the 128-byte swizzle, or of 64 with the 64-byte one (layout 4; groups of 8 rows are 512 bytes apart)
@@ -139,7 +167,7 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     uint8_t* smem_gen = smem_raw + (smem_base - smem_u32(smem_raw));
     const uint32_t sQ = smem_base, sV = smem_base + C::kOffV, sK = smem_base + C::kOffK, sRaw = smem_base + C::kOffRaw, bars = smem_base + C::kOffBars;
     const uint32_t bQFull = bars, bQReady = bars + 8, bQEmpty = bars + 16;
-    // k_full: the codes by TMA and the scales by warp 15; raw: V's codes; v: its numbers
+    // k_full, raw_full: the codes of K and of V by TMA and their scales by warp 15; v: V's numbers
     const uint32_t bKFull = bars + 24, bKEmpty = bKFull + 8 * C::kStages, bRawFull = bKEmpty + 8 * C::kStages, bRawEmpty = bRawFull + 8 * C::kStages;
     const uint32_t bVFull = bRawEmpty + 8 * C::kStages, bVEmpty = bVFull + 16, bParEmpty = bVEmpty + 16;
     const uint32_t bSFree = bParEmpty + 16 * kPar, bHalf = bSFree + 8;
@@ -149,7 +177,9 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     auto bOFinal = [&](int h) { return bHalf + 40 * h + 24; };
     auto bOFree = [&](int h) { return bHalf + 40 * h + 32; };
     const uint32_t bTileFull = bHalf + 80, bTileEmpty = bTileFull + 8 * C::kTileQ;
-    float4* s_par = reinterpret_cast<float4*>(smem_gen + C::kOffPar);
+    float* s_par = reinterpret_cast<float*>(smem_gen + C::kOffPar);
+    int32_t* s_vpar = reinterpret_cast<int32_t*>(smem_gen + C::kOffVPar);
+    volatile int32_t* s_wide = s_vpar + C::kStages * 12;
     float* s_down = reinterpret_cast<float*>(smem_gen + C::kOffDown);
     int32_t* s_nan = reinterpret_cast<int32_t*>(smem_gen + C::kOffNan);
     int32_t* s_nan_any = s_nan + kNan * D;
@@ -162,7 +192,7 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
     if (threadIdx.x == 0) {
         mbar_init(bQFull, 1); mbar_init(bQReady, 128); mbar_init(bQEmpty, 1);
         for (int s = 0; s < C::kStages; ++s) {
-            mbar_init(bKFull + 8 * s, 2); mbar_init(bKEmpty + 8 * s, 1); mbar_init(bRawFull + 8 * s, 1); mbar_init(bRawEmpty + 8 * s, 128);
+            mbar_init(bKFull + 8 * s, 2); mbar_init(bKEmpty + 8 * s, 1); mbar_init(bRawFull + 8 * s, 2); mbar_init(bRawEmpty + 8 * s, 128);
         }
         for (int s = 0; s < 2; ++s) { mbar_init(bVFull + 8 * s, 128); mbar_init(bVEmpty + 8 * s, 1); }
         for (int s = 0; s < 2 * kPar; ++s) mbar_init(bParEmpty + 8 * s, 4);
@@ -236,49 +266,55 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 if (v.n_steps == 0) continue;
                 const int kvh = un.head[0] / p.group, n_pages = (v.kv_len + p.page_size - 1) >> page_shift;
                 const int32_t* bt = p.block_tables + (int64_t)un.request * p.max_blocks;
-                // a step's codes of K or of V: a lane for each page
-                auto load_step = [&](const CUtensorMap* tm, int j, uint32_t to, uint32_t full, uint32_t empty, Ring& ring) -> bool {
-                    const int page0 = (v.kv_begin + j) * ppt, cnt = min(ppt, n_pages - page0);
+                // K(0) (only needs a place in the ring, which is free before the tile before's Q is), Q, K(1), V(0), K(2), V(1), ..: one place in the
+                // code for them all
+                bool ok = true;
+                for (int i = 0; i < 2 * v.n_steps && ok; ++i) {
+                    const bool is_v = i == 2 * v.n_steps - 1 || (i > 0 && (i & 1) == 0);
+                    const int step = is_v ? i == 2 * v.n_steps - 1 ? v.n_steps - 1 : i / 2 - 1 : (i + 1) / 2;
+                    if (i == 1) {
+                        ok = __all_sync(0xffffffffu, mbar_wait(bQEmpty, q_phase ^ 1u, abort_flag));
+                        if (!ok) break;
+                        q_phase ^= 1u;
+                        if (lane == 0) mbar_arrive_expect_tx(bQFull, ((v.n[0] > 0) + (v.n[1] > 0)) * C::kTileBytes);
+                        __syncwarp();
+                        const int rph = 128 / un.pack;
+                        const CUtensorMap* qm = un.pack == 1 ? &tm_q : un.pack == 2 ? &tm_q64 : un.pack == 4 ? &tm_q32 : &tm_q16;
+                        const int per_half = un.pack * C::kHalves;
+#pragma unroll 1
+                        for (int b = lane; b < 2 * per_half; b += 32) {
+                            const int hf = b / per_half, k = (b % per_half) / C::kHalves, h = b % C::kHalves;
+                            if ((hf ? v.n[1] : v.n[0]) == 0) continue;
+                            // (more places than heads in the group: the last head again, into rows that nobody stores)
+                            tma_load_3d(sQ + hf * C::kTileBytes + h * C::kHalfBytes + k * rph * 128, qm, bQFull, h * 64,
+                                        (hf ? un.head[1] : un.head[0]) + min(k, p.group - 1), v.q_off + (hf ? un.row0[1] : un.row0[0]));
+                        }
+                        __syncwarp();
+                    }
+                    // a step's codes of K or of V: a lane for each page
+                    const int page0 = (v.kv_begin + step) * ppt, cnt = min(ppt, n_pages - page0);
                     int pid = 0;
                     if (lane < cnt) pid = bt[page0 + lane];
                     if (pid < 0 || pid >= p.num_pages) {
                         if (p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
                         pid = 0;
                     }
-                    const bool ok = mbar_wait(empty + 8 * ring.stage, ring.phase ^ 1u, abort_flag);
-                    if (!__all_sync(0xffffffffu, ok)) return false;
-                    if (lane == 0) mbar_arrive_expect_tx(full + 8 * ring.stage, (uint32_t)(cnt * p.page_size * D));
+                    const Ring ring = is_v ? ring_v : ring_k;
+                    const uint32_t full = (is_v ? bRawFull : bKFull) + 8 * ring.stage, empty = (is_v ? bRawEmpty : bKEmpty) + 8 * ring.stage;
+                    ok = __all_sync(0xffffffffu, mbar_wait(empty, ring.phase ^ 1u, abort_flag));
+                    if (!ok) break;
+                    if (lane == 0) mbar_arrive_expect_tx(full, (uint32_t)(cnt * p.page_size * D));
                     __syncwarp();
-                    if (lane < cnt) tma_load_4d(to + ring.stage * C::kCodeBytes + lane * p.page_size * D, tm, full + 8 * ring.stage, 0, 0, kvh, pid);
-                    ring.advance(C::kStages);
-                    return true;
-                };
-                // K(0) only needs a place in the ring, which is free before the tile before's Q is
-                if (!load_step(&tm_k, 0, sK, bKFull, bKEmpty, ring_k)) break;
-                const bool ok = mbar_wait(bQEmpty, q_phase ^ 1u, abort_flag);
-                if (!__all_sync(0xffffffffu, ok)) break;
-                q_phase ^= 1u;
-                if (lane == 0) mbar_arrive_expect_tx(bQFull, ((v.n[0] > 0) + (v.n[1] > 0)) * C::kTileBytes);
-                __syncwarp();
-                const int rph = 128 / un.pack;
-                const CUtensorMap* qm = un.pack == 1 ? &tm_q : un.pack == 2 ? &tm_q64 : un.pack == 4 ? &tm_q32 : &tm_q16;
-                const int per_half = un.pack * C::kHalves;
-                for (int b = lane; b < 2 * per_half; b += 32) {
-                    const int hf = b / per_half, k = (b % per_half) / C::kHalves, h = b % C::kHalves;
-                    if ((hf ? v.n[1] : v.n[0]) == 0) continue;
-                    // (more places than heads in the group: the last head again, into rows that nobody stores)
-                    tma_load_3d(sQ + hf * C::kTileBytes + h * C::kHalfBytes + k * rph * 128, qm, bQFull, h * 64,
-                                (hf ? un.head[1] : un.head[0]) + min(k, p.group - 1), v.q_off + (hf ? un.row0[1] : un.row0[0]));
+                    if (lane < cnt)
+                        tma_load_4d((is_v ? sRaw : sK) + ring.stage * C::kCodeBytes + lane * p.page_size * D, is_v ? &tm_v : &tm_k, full, 0, 0, kvh, pid);
+                    if (is_v) ring_v.advance(C::kStages);
+                    else ring_k.advance(C::kStages);
                 }
-                __syncwarp();
-                for (int k = 0; k <= v.n_steps && !dead; ++k) {
-                    if (k >= 1 && !load_step(&tm_v, k - 1, sRaw, bRawFull, bRawEmpty, ring_v)) dead = true;
-                    if (!dead && k + 1 < v.n_steps && !load_step(&tm_k, k + 1, sK, bKFull, bKEmpty, ring_k)) dead = true;
-                }
+                dead = !ok;
             }
         } else if (warp == 15) {
             // ================================================================ the scales of a step's pages, asked for a step ahead
-            Ring ring = {0, 0}, ring_p[2] = {{0, 0}, {0, 0}};
+            Ring ring_k = {0, 0}, ring_v = {0, 0}, ring_p[2] = {{0, 0}, {0, 0}};
             bool dead = false;
             while (!dead) {
                 const int u = next_tile();
@@ -295,23 +331,43 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                     const int pid = bt[key >> page_shift];
                     return *reinterpret_cast<const float*>(pool + (pid < 0 || pid >= p.num_pages ? 0 : pid) * p.page_bytes);
                 };
-                float next = scale_of(0);
-                for (int k = 0; k < v.n_steps; ++k) {
-                    const float mine = next, vs = __shfl_sync(0xffffffffu, mine, 8 + group);
-                    next = scale_of(k + 1);
-                    const int ev = vs == 0.f ? 0 : min(max(exponent_of(vs), -126), 126);
-                    const float4 par = make_float4(mine * p.scale_log2, (float)ev, power_of_two(-ev), 0.f);
-                    bool ok = mbar_wait(bKEmpty + 8 * ring.stage, ring.phase ^ 1u, abort_flag);
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        if (k >= v.n[h]) continue;
-                        ok = ok && mbar_wait(bParEmpty + 8 * (h * kPar + ring_p[h].stage), ring_p[h].phase ^ 1u, abort_flag);
-                        if (ok && lane < 8) s_par[(h * kPar + ring_p[h].stage) * 8 + lane] = par;
-                        ring_p[h].advance(kPar);
+                // K(0), then K(k + 1) and V(k), the order in which the codes are asked for
+                float next = scale_of(0), after = scale_of(1);
+                int v_exp = 0, apart = 0, wide = 0, apart_v = 0, wide_v = 0;       // log2 v; log2 vs / v, and whether that wants bf16; the same of the step before
+                for (int k = 0; k <= v.n_steps; ++k) {
+                    bool ok = true;
+                    apart_v = apart;
+                    wide_v = wide;
+                    if (k < v.n_steps) {
+                        const float mine = next, vs = __shfl_sync(0xffffffffu, mine, 8 + group);
+                        next = after;
+                        after = scale_of(k + 2);
+                        if (k == 0) v_exp = (int)__reduce_max_sync(0xffffffffu, (uint32_t)(vs == 0.f ? 0 : exponent_of(vs) + 128)) - 128;
+                        apart = vs == 0.f ? 0 : min(max(exponent_of(vs) - v_exp, -100), 100);
+                        wide = __any_sync(0xffffffffu, apart < kScaleDown || apart > kScaleUp);
+                        ok = mbar_wait(bKEmpty + 8 * ring_k.stage, ring_k.phase ^ 1u, abort_flag);
+#pragma unroll 1
+                        for (int h = 0; h < 2; ++h) {
+                            if (k >= (h ? v.n[1] : v.n[0])) continue;
+                            const Ring ring = h ? ring_p[1] : ring_p[0];
+                            const int at = h * kPar + (int)ring.stage;
+                            ok = ok && mbar_wait(bParEmpty + 8 * at, ring.phase ^ 1u, abort_flag);
+                            if (ok && lane < 10) s_par[at * 12 + lane] = lane < 8 ? (mine == 0.f ? 1.f : mine) : (float)(lane == 8 ? wide : v_exp);
+                            if (h) ring_p[1].advance(kPar);
+                            else ring_p[0].advance(kPar);
+                        }
+                        if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }
+                        if (lane == 0) mbar_arrive(bKFull + 8 * ring_k.stage);
+                        ring_k.advance(C::kStages);
                     }
-                    if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }
-                    if (lane == 0) mbar_arrive(bKFull + 8 * ring.stage);
-                    ring.advance(C::kStages);
+                    if (k > 0) {
+                        ok = mbar_wait(bRawEmpty + 8 * ring_v.stage, ring_v.phase ^ 1u, abort_flag);
+                        if (ok && lane < 8) s_vpar[ring_v.stage * 12 + lane] = apart_v;
+                        if (ok && lane == 8) s_vpar[ring_v.stage * 12 + 8] = wide_v;
+                        if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }
+                        if (lane == 0) mbar_arrive(bRawFull + 8 * ring_v.stage);
+                        ring_v.advance(C::kStages);
+                    }
                 }
             }
         } else if (warp == 12 && lane == 0) {
@@ -333,14 +389,14 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 for (int k = 0; k < v.n_steps && !dead; ++k) {
                     if (!mbar_wait(bKFull + 8 * ring.stage, ring.phase, abort_flag)) { dead = true; break; }
                     const uint64_t kd = k_desc0 + (uint64_t)(ring.stage * (C::kCodeBytes >> 4));
-#pragma unroll
+#pragma unroll 1
                     for (int hf = 0; hf < 2; ++hf) {
-                        if (k >= v.n[hf]) continue;
+                        if (k >= (hf ? v.n[1] : v.n[0])) continue;
                         if (!mbar_wait(bSFree, sfree_phase ^ 1u, abort_flag)) { dead = true; break; }
                         sfree_phase ^= 1u;
                         tc_fence_after();
                         const uint64_t qd = q_desc0 + (uint64_t)(hf * (C::kTileBytes >> 4));
-#pragma unroll
+#pragma unroll 1
                         for (int kk = 0; kk < D / 32; ++kk) {
                             mma_e4m3(tS, qd + kk * 2, kd + kk * 2, kIdescE4m3, kk > 0);
                             mma_e4m3(tS, qd + kLo + kk * 2, kd + kk * 2, kIdescE4m3, 1u);
@@ -357,7 +413,7 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             // ================================================================ issuer of O += P V
             Ring ring = {0, 0};
             uint32_t p_phase[2] = {0, 0}, of_phase[2] = {0, 0};
-            constexpr uint32_t idesc_pv = idesc_bf16(D, 0, 1);
+            constexpr uint32_t kIdescBf16 = idesc_bf16(D, 0, 1), kIdescF16 = kIdescBf16 & ~((1u << 7) | (1u << 10));       // (types 0 are f16)
             const uint64_t v_desc0 = smem_desc_sw128(sV, C::kHalfBytes, 1024);
             bool dead = false;
             while (!dead) {
@@ -369,21 +425,21 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 for (int k = 0; k < v.n_steps && !dead; ++k) {
                     if (!mbar_wait(bVFull + 8 * ring.stage, ring.phase, abort_flag)) { dead = true; break; }
                     const uint64_t vd = v_desc0 + (uint64_t)(ring.stage * (C::kTileBytes >> 4));
-#pragma unroll
+                    const uint32_t idesc_pv = s_wide[ring.stage] ? kIdescBf16 : kIdescF16;
+#pragma unroll 1
                     for (int hf = 0; hf < 2; ++hf) {
-                        const int n = v.n[hf];
+                        const int n = hf ? v.n[1] : v.n[0];
                         if (k >= n) continue;
-                        if (!mbar_wait(bPReady(hf), p_phase[hf], abort_flag)) { dead = true; break; }
-                        p_phase[hf] ^= 1u;
+                        if (!mbar_wait(bPReady(hf), hf ? p_phase[1] : p_phase[0], abort_flag)) { dead = true; break; }
+                        if (hf) p_phase[1] ^= 1u; else p_phase[0] ^= 1u;
                         if (k == 0) {          // the tile before's O has been read
-                            if (!mbar_wait(bOFree(hf), of_phase[hf] ^ 1u, abort_flag)) { dead = true; break; }
-                            of_phase[hf] ^= 1u;
+                            if (!mbar_wait(bOFree(hf), (hf ? of_phase[1] : of_phase[0]) ^ 1u, abort_flag)) { dead = true; break; }
+                            if (hf) of_phase[1] ^= 1u; else of_phase[0] ^= 1u;
                         }
                         tc_fence_after();
                         const uint32_t tP = tmem + col_p(hf), tO = tmem + col_o(hf);
-                        if (k > 0) mma_ts_accumulate(tO, tP, vd, idesc_pv); else mma_ts_overwrite(tO, tP, vd, idesc_pv);
-#pragma unroll
-                        for (int kk = 1; kk < 8; ++kk) mma_ts_accumulate(tO, tP + kk * 8, vd + (uint64_t)(kk * 128), idesc_pv);
+#pragma unroll 1
+                        for (int kk = 0; kk < 8; ++kk) mma_ts(tO, tP + kk * 8, vd + (uint64_t)(kk * 128), idesc_pv, (k | kk) > 0);
                         mma_commit(bPFree(hf));
                         if (k + 1 == n) mma_commit(bOFinal(hf));
                     }
@@ -464,38 +520,75 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             fence_proxy_async_smem();
             mbar_arrive(bQReady);
             ++tiles;
-            // ---- V
+            // ---- V.  Where some rows do not see all keys: NaN codes, and rows behind the sequence, which are zeros
+            const int all_see = min(v.n[0] > 0 ? v.P + un.row0[0] : 0x7fffffff, v.n[1] > 0 ? v.P + un.row0[1] : 0x7fffffff);       // the last key that every row sees
             for (int k = 0; k < v.n_steps; ++k) {
                 bool ok = mbar_wait(bRawFull + 8 * ring_raw.stage, ring_raw.phase, abort_flag);
                 ok = ok && mbar_wait(bVEmpty + 8 * ring_v.stage, ring_v.phase ^ 1u, abort_flag);
                 if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }
                 const uint8_t* from = smem_gen + C::kOffRaw + ring_raw.stage * C::kCodeBytes + row0 * D + c * 16;
                 const uint32_t to = sV + ring_v.stage * C::kTileBytes;
-                const int key0 = (v.kv_begin + k) * 128, rows = v.kv_len - key0;       // rows from here on lie behind the sequence: zeros
-#pragma unroll 2
-                for (int i = 0; i < kChunks; ++i) {
-                    const int row = row0 + i * kApart;
-                    uint4 x = *reinterpret_cast<const uint4*>(from + i * kApart * D);
-                    if (row >= rows) x = make_uint4(0, 0, 0, 0);
-                    uint32_t w[4] = {swap ? x.z : x.x, swap ? x.w : x.y, swap ? x.x : x.z, swap ? x.y : x.w};
-                    if (nan_bits(w[0]) | nan_bits(w[1]) | nan_bits(w[2]) | nan_bits(w[3])) {
+                const int key0 = (v.kv_begin + k) * 128;
+                const int32_t* vp = s_vpar + ring_raw.stage * 12;
+                const int apart[2] = {vp[2 * (warp & 3)], vp[2 * (warp & 3) + 1]};      // of the warp's first and last 16 rows
+                const bool wide = vp[8] != 0;
+                if (r == 0) s_wide[ring_v.stage] = wide;
+                if (__builtin_expect(!wide && key0 + 127 <= all_see, 1)) {
+                    // (a row at a time, the next one's codes under way: the loop has to be short, see above)
+                    const uint8_t* const first = from + (swap ? 8 : 0);
+                    const uint8_t* const second = from + (swap ? 0 : 8);
+                    uint2 x0 = *reinterpret_cast<const uint2*>(first), x1 = *reinterpret_cast<const uint2*>(second);
+                    uint32_t turned = 0u, times = (uint32_t)(15 + apart[0]) * 0x04000400u;                 // a power of two, as f16, twice
+                    uint32_t at0 = to + place[0], at1 = to + place[1];
 #pragma unroll 1
-                        for (int b = 0; b < 16; ++b) {
-                            const int at = b ^ (swap ? 8 : 0);         // of the lane's 16 elements
-                            const uint32_t word = b < 4 ? w[0] : b < 8 ? w[1] : b < 12 ? w[2] : w[3];
-                            if ((word >> (8 * (b & 3)) & 0x7fu) == 0x7fu) {
-                                atomicMin(&s_nan[nan_slot * D + c * 16 + at], key0 + row);
-                                atomicMin(&s_nan_any[nan_slot], key0 + row);
+                    for (int i = 0; i < kChunks; ++i) {
+                        const uint32_t w[4] = {x0.x, x0.y, x1.x, x1.y};
+                        if (i + 1 < kChunks) {
+                            x0 = *reinterpret_cast<const uint2*>(first + (i + 1) * kApart * D);
+                            x1 = *reinterpret_cast<const uint2*>(second + (i + 1) * kApart * D);
+                        }
+                        if (i == kChunks / 2) times = (uint32_t)(15 + apart[1]) * 0x04000400u;
+                        uint32_t y[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) y[j] = mul_f16x2(j & 1 ? codes_f16x2_high(w[j >> 1]) : codes_f16x2_low(w[j >> 1]), times);
+                        st_shared_16(at0 ^ turned, make_uint4(y[0], y[1], y[2], y[3]));
+                        st_shared_16(at1 ^ turned, make_uint4(y[4], y[5], y[6], y[7]));
+                        at0 += kApart * 128;
+                        at1 += kApart * 128;
+                        if (kApart == 4) turned ^= 64u;
+                    }
+                } else {
+                    const int rows = v.kv_len - key0;
+#pragma unroll 1
+                    for (int i = 0; i < kChunks; ++i) {
+                        const int row = row0 + i * kApart, up = apart[2 * i / kChunks];
+                        const uint32_t f16_up = (uint32_t)(15 + up) * 0x04000400u, bf16_up = (uint32_t)(127 + up) * 0x00800080u;
+                        uint4 x = *reinterpret_cast<const uint4*>(from + i * kApart * D);
+                        if (row >= rows) x = make_uint4(0, 0, 0, 0);
+                        uint32_t w[4] = {swap ? x.z : x.x, swap ? x.w : x.y, swap ? x.x : x.z, swap ? x.y : x.w};
+                        if (nan_bits(w[0]) | nan_bits(w[1]) | nan_bits(w[2]) | nan_bits(w[3])) {
+#pragma unroll 1
+                            for (int b = 0; b < 16; ++b) {
+                                const int at = b ^ (swap ? 8 : 0);     // of the lane's 16 elements
+                                const uint32_t word = b < 4 ? w[0] : b < 8 ? w[1] : b < 12 ? w[2] : w[3];
+                                if ((word >> (8 * (b & 3)) & 0x7fu) == 0x7fu) {
+                                    atomicMin(&s_nan[nan_slot * D + c * 16 + at], key0 + row);
+                                    atomicMin(&s_nan_any[nan_slot], key0 + row);
+                                }
                             }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) w[j] &= ~((nan_bits(w[j]) >> 7) * 0xffu);
                         }
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) w[j] &= ~((nan_bits(w[j]) >> 7) * 0xffu);
-                    }
+                        for (int q = 0; q < 2; ++q) {
+                            uint32_t y[4];
 #pragma unroll
-                    for (int q = 0; q < 2; ++q) {
-                        const uint32_t y[4] = {codes_bf16x2(w[2 * q], false), codes_bf16x2(w[2 * q], true), codes_bf16x2(w[2 * q + 1], false),
-                                               codes_bf16x2(w[2 * q + 1], true)};
-                        st_shared_16(to + ((place[q] + i * kApart * 128) ^ (kApart == 4 ? (uint32_t)(i & 1) << 6 : 0u)), y);
+                            for (int j = 0; j < 4; ++j) {
+                                const uint32_t word = w[2 * q + (j >> 1)];
+                                y[j] = wide ? mul_bf16x2(codes_bf16x2(word, j & 1), bf16_up) : mul_f16x2(j & 1 ? codes_f16x2_high(word) : codes_f16x2_low(word), f16_up);
+                            }
+                            st_shared_16(to + ((place[q] + i * kApart * 128) ^ (kApart == 4 ? (uint32_t)(i & 1) << 6 : 0u)), make_uint4(y[0], y[1], y[2], y[3]));
+                        }
                     }
                 }
                 fence_proxy_async_smem();
@@ -527,98 +620,128 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             }
             if (v.n_steps == 0) continue;
             const int first_pos = v.P + un.row0[hf], row_last = min(first_pos + rr, v.kv_len - 1);
-            float m_ref = 0.f, l_run = 0.f, down = 0.f;
+            float m_ref = 0.f, l_run = 0.f, down = 0.f, unit = 0.f;       // down: of the row, scores in log2 units; unit: v, of the sums
+            // the row's reference, where a score is `above` it by too much; O is rescaled once the product before has landed
+            auto settle = [&](float above, int j, bool& waited) -> bool {
+                const bool move = j == 0 || above > kMost;
+                if (__builtin_expect(!__any_sync(0xffffffffu, move), 1)) return true;
+                // how far it goes up (the first one may go down; a row that sees nothing keeps its)
+                float y = j == 0 ? above - kTop : fmaxf(above - kTop, 0.f);
+                if (y == -INFINITY) y = 0.f;
+                const float alpha = j == 0 ? 1.f : fast_exp2(-y);
+                m_ref += y;
+                l_run *= alpha;
+                if (j == 0) return true;
+                if (!__all_sync(0xffffffffu, mbar_wait(bPFree(hf), pf_phase ^ 1u, abort_flag))) return false;
+                pf_phase ^= 1u;
+                waited = true;
+                tc_fence_after();
+                if (__any_sync(0xffffffffu, alpha != 1.f)) {
+#pragma unroll 1
+                    for (int q0 = 0; q0 < D; q0 += 16) {
+                        float o[16];
+                        tmem_ld8(lane_addr + col_o(hf) + q0, reinterpret_cast<uint32_t*>(o));
+                        tmem_ld8(lane_addr + col_o(hf) + q0 + 8, reinterpret_cast<uint32_t*>(o) + 8);
+                        tmem_wait_ld();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] *= alpha;
+                        tmem_st8(lane_addr + col_o(hf) + q0, reinterpret_cast<uint32_t*>(o));
+                        tmem_st8(lane_addr + col_o(hf) + q0 + 8, reinterpret_cast<uint32_t*>(o) + 8);
+                    }
+                }
+                return true;
+            };
+            auto p_is_free = [&]() -> bool {           // P(j - 1) has been consumed
+                if (!__all_sync(0xffffffffu, mbar_wait(bPFree(hf), pf_phase ^ 1u, abort_flag))) return false;
+                pf_phase ^= 1u;
+                tc_fence_after();
+                return true;
+            };
             for (int j = 0; j < n; ++j) {
                 if (!__all_sync(0xffffffffu, mbar_wait(bSFull(hf), s_phase, abort_flag))) { dead = true; break; }
                 s_phase ^= 1u;
                 tc_fence_after();
-                if (j == 0) down = s_down[((tiles & 1) * 2 + hf) * 128 + r];
-                float s[128];
-#pragma unroll
-                for (int q4 = 0; q4 < 4; ++q4) tmem_ld32(lane_addr + kColS + q4 * 32, reinterpret_cast<uint32_t*>(s) + q4 * 32);
-                tmem_wait_ld();
-                tc_fence_before();
-                mbar_arrive(bSFree);
-                const int key0 = (v.kv_begin + j) * 128;
-                if (key0 + 127 > first_pos) {          // only steps that touch the diagonal are masked
-                    const int limit = row_last - key0;
-#pragma unroll
-                    for (int i = 0; i < 128; ++i) s[i] = (i > limit) ? -INFINITY : s[i];
+                const float* pr = s_par + (hf * kPar + par) * 12;      // of 16 keys each: K's scale
+                if (j == 0) {
+                    // (at least 2^-90: no product of an infinity and 0, whatever K's scale, and below it all scores are 0 to fp32)
+                    down = fmaxf(s_down[((tiles & 1) * 2 + hf) * 128 + r] * p.scale_log2, 8.077936e-28f);
+                    unit = fast_exp2(pr[9]);
                 }
-                // ---- of 16 keys: score in log2 units and log2 of V's scale are a s + b
-                float a[8], b[8], less[8], mxx = -INFINITY;
+                const int key0 = (v.kv_begin + j) * 128;
+                bool waited = false;
+                if (__builtin_expect(pr[8] != 0.f, 0)) {
+                    // P as bf16: such steps are few, and take their scores twice, 8 at a time, in loops that cost no registers and little code
+                    const int limit = row_last - key0;
+                    float most = -INFINITY;
+#pragma unroll 1
+                    for (int i = 0; i < 128; i += 8) {
+                        float y[8];
+                        most = fmaxf(most, wide_scores(lane_addr + kColS + i, pr[i >> 4] * down, limit - i, 0.f, y));
+                    }
+                    if (!settle(most - m_ref, j, waited) || (!waited && !p_is_free())) { dead = true; break; }
+#pragma unroll 1
+                    for (int i = 0; i < 128; i += 8) {
+                        float y[8];
+                        wide_scores(lane_addr + kColS + i, pr[i >> 4] * down, limit - i, m_ref, y);
 #pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    const float4 f = s_par[(hf * kPar + par) * 8 + g];
-                    a[g] = fmaxf(f.x * down, 1.1754944e-38f);          // (no product of an infinity with 0)
-                    b[g] = f.y;
-                    less[g] = f.z;
-                    const float* x = s + 16 * g;
-                    const float m0 = fmax3(x[0], x[1], x[2]), m1 = fmax3(x[3], x[4], x[5]), m2 = fmax3(x[6], x[7], x[8]), m3 = fmax3(x[9], x[10], x[11]);
-                    const float mg = fmaxf(fmax3(fmax3(m0, m1, m2), fmax3(m3, x[12], x[13]), x[14]), x[15]);
-                    mxx = fmaxf(mxx, fmaf(mg, a[g], b[g] - m_ref));
+                        for (int k = 0; k < 8; ++k) y[k] = fast_exp2(y[k]);
+                        l_run += ((y[0] + y[1]) + (y[2] + y[3])) + ((y[4] + y[5]) + (y[6] + y[7]));
+                        const uint32_t two[4] = {pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
+                        tmem_st4(lane_addr + col_p(hf) + i / 2, two);
+                    }
+                    tmem_wait_st();
+                    tc_fence_before();
+                    mbar_arrive(bSFree);
+                } else {
+                    float s[128], most = -INFINITY;
+#pragma unroll
+                    for (int q4 = 0; q4 < 4; ++q4) tmem_ld32(lane_addr + kColS + q4 * 32, reinterpret_cast<uint32_t*>(s) + q4 * 32);
+                    tmem_wait_ld();
+                    tc_fence_before();
+                    mbar_arrive(bSFree);
+                    if (__builtin_expect(key0 + 127 > first_pos, 0)) {      // only steps that touch the diagonal are masked
+                        const int limit = row_last - key0;
+#pragma unroll
+                        for (int i = 0; i < 128; ++i) s[i] = (i > limit) ? -INFINITY : s[i];
+                    }
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const float* x = s + 16 * g;
+                        const float m0 = fmax3(x[0], x[1], x[2]), m1 = fmax3(x[3], x[4], x[5]), m2 = fmax3(x[6], x[7], x[8]), m3 = fmax3(x[9], x[10], x[11]);
+                        most = fmaxf(most, pr[g] * fmaxf(fmax3(fmax3(m0, m1, m2), fmax3(m3, x[12], x[13]), x[14]), x[15]));
+                    }
+                    if (!settle(fmaf(most, down, -m_ref), j, waited)) { dead = true; break; }
+                    uint32_t* pk = reinterpret_cast<uint32_t*>(s);
+                    const uint64_t nm2 = pack2(-m_ref, -m_ref);
+                    uint64_t sum2a = pack2(0.f, 0.f), sum2b = pack2(0.f, 0.f);
+#pragma unroll
+                    for (int g = 0; g < 8; ++g) {
+                        const float a = pr[g] * down;
+                        const uint64_t a2 = pack2(a, a);
+                        float e[16];
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) unpack2(ffma2(pack2(s[16 * g + 2 * k], s[16 * g + 2 * k + 1]), a2, nm2), e[2 * k], e[2 * k + 1]);
+#pragma unroll
+                        for (int k = 0; k < 16; ++k) e[k] = fast_exp2(e[k]);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if (k & 1) sum2b = fadd2(sum2b, pack2(e[2 * k], e[2 * k + 1]));
+                            else sum2a = fadd2(sum2a, pack2(e[2 * k], e[2 * k + 1]));
+                            pk[8 * g + k] = pack_f16x2(e[2 * k], e[2 * k + 1]);
+                        }
+                    }
+                    float t0, t1;
+                    unpack2(fadd2(sum2a, sum2b), t0, t1);
+                    l_run += t0 + t1;
+                    if (!waited && !p_is_free()) { dead = true; break; }
+#pragma unroll
+                    for (int c8 = 0; c8 < 64; c8 += 8) tmem_st8(lane_addr + col_p(hf) + c8, pk + c8);
+                    tmem_wait_st();
+                    tc_fence_before();
                 }
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bParEmpty + 8 * (hf * kPar + par));
                 par = (par + 1) % kPar;
-                bool waited = false;
-                const bool move = j == 0 || mxx > kRefSlack;
-                if (__any_sync(0xffffffffu, move)) {
-                    // how far the reference goes up (the first one may go down; a row that sees nothing keeps its)
-                    float y = j == 0 ? mxx : fmaxf(mxx, 0.f);
-                    if (y == -INFINITY) y = 0.f;
-                    const float alpha = j == 0 ? 1.f : fast_exp2(-y);
-                    m_ref += y;
-                    l_run *= alpha;
-                    if (j > 0) {
-                        if (!__all_sync(0xffffffffu, mbar_wait(bPFree(hf), pf_phase ^ 1u, abort_flag))) { dead = true; break; }
-                        pf_phase ^= 1u;
-                        waited = true;
-                        tc_fence_after();
-                        if (__any_sync(0xffffffffu, alpha != 1.f)) {
-#pragma unroll 1
-                            for (int q0 = 0; q0 < D; q0 += 16) {
-                                float o[16];
-                                tmem_ld8(lane_addr + col_o(hf) + q0, reinterpret_cast<uint32_t*>(o));
-                                tmem_ld8(lane_addr + col_o(hf) + q0 + 8, reinterpret_cast<uint32_t*>(o) + 8);
-                                tmem_wait_ld();
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) o[i] *= alpha;
-                                tmem_st8(lane_addr + col_o(hf) + q0, reinterpret_cast<uint32_t*>(o));
-                                tmem_st8(lane_addr + col_o(hf) + q0 + 8, reinterpret_cast<uint32_t*>(o) + 8);
-                            }
-                        }
-                    }
-                }
-                uint32_t* pk = reinterpret_cast<uint32_t*>(s);
-#pragma unroll
-                for (int g = 0; g < 8; ++g) {
-                    const uint64_t a2 = pack2(a[g], a[g]);
-                    const float off = b[g] - m_ref;
-                    const uint64_t b2 = pack2(off, off);
-                    float e[16];
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) unpack2(ffma2(pack2(s[16 * g + 2 * k], s[16 * g + 2 * k + 1]), a2, b2), e[2 * k], e[2 * k + 1]);
-#pragma unroll
-                    for (int k = 0; k < 16; ++k) e[k] = fast_exp2(e[k]);
-                    uint64_t sum2 = pack2(e[0], e[1]);
-#pragma unroll
-                    for (int k = 1; k < 8; ++k) sum2 = fadd2(sum2, pack2(e[2 * k], e[2 * k + 1]));
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) pk[8 * g + k] = pack_bf16x2(e[2 * k], e[2 * k + 1]);
-                    float t0, t1;
-                    unpack2(sum2, t0, t1);
-                    l_run = fmaf(t0 + t1, less[g], l_run);
-                }
-                if (!waited) {                         // P(j - 1) has been consumed
-                    if (!__all_sync(0xffffffffu, mbar_wait(bPFree(hf), pf_phase ^ 1u, abort_flag))) { dead = true; break; }
-                    pf_phase ^= 1u;
-                    tc_fence_after();
-                }
-#pragma unroll
-                for (int c8 = 0; c8 < 64; c8 += 8) tmem_st8(lane_addr + col_p(hf) + c8, pk + c8);
-                tmem_wait_st();
-                tc_fence_before();
                 mbar_arrive(bPReady(hf));
             }
             if (dead) break;
@@ -644,7 +767,7 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 tmem_ld32(lane_addr + col_o(hf) + q4 * 32, reinterpret_cast<uint32_t*>(o));
                 tmem_wait_ld();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] *= inv_l;
+                for (int i = 0; i < 32; ++i) o[i] *= inv_l * unit;
                 if (__any_sync(0xffffffffu, nans)) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i)

@@ -357,6 +357,8 @@ static int codes_append(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPl
     p.off_q_offsets = hd->off_q_offsets;
     p.off_prefix = hd->off_prefix;
     p.total_new_tokens = hd->total_new_tokens;
+    p.off_touched = hd->off_combine + (uint32_t)(sizeof(WppCombine) * (size_t)hd->num_combine);
+    p.num_touched = hd->nonempty_halves;
     const int e = (d.dtype == WPP_KV4 ? wpp_launch_kv4_append : wpp_launch_kv8_append)(d.head_dim, &p, ctx->sm_count, cuda_stream);
     if (e != 0) return cuda_fail(ctx, e);
     const_cast<wpp_ctx*>(ctx)->launches += 1;
@@ -394,6 +396,7 @@ static int combine_parts(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppP
     c.num_q_heads = d.num_q_heads;
     c.head_dim = d.head_dim;
     c.max_rows = hd->max_combine_rows;
+    c.num_records = hd->num_combine;
     c.off_q_offsets = hd->off_q_offsets;
     c.off_combine = hd->off_combine;
     const int e = wpp_launch_combine(&c, hd->num_combine, cuda_stream);
@@ -441,6 +444,13 @@ static int codes_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const Wp
     p.first_tile = hd->num_few_units;
     p.num_tiles = hd->num_units - hd->num_few_units;
     p.scale_log2 = scale_log2_of(d);
+    p.num_few = hd->num_few_units;
+    const bool few_taken = hd->deal_items && p.num_few > hd->num_few_ctas, tiles_taken = p.num_tiles > hd->num_ctas;
+    if (hd->deal_items) p.few_counter = static_cast<uint32_t*>(workspace) + 32;
+    if (few_taken || tiles_taken) {
+        const int e = (int)cudaMemsetAsync(workspace, 0, WPP_WS_HEADER_BYTES, (cudaStream_t)cuda_stream);
+        if (e != 0) return cuda_fail(ctx, e);
+    }
     if (hd->num_few_units > 0) {
         const int e = (d.dtype == WPP_KV4 ? wpp_launch_kv4_few : wpp_launch_kv8_few)(d.head_dim, &p, hd->num_few_ctas, hd->max_few_rows, cuda_stream);
         if (e != 0) return cuda_fail(ctx, e);
@@ -456,11 +466,7 @@ static int codes_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const Wp
             if (int rc = make_map(ctx, &tk, k_cache, 4, dims, strides, box, d.head_dim == 128 ? kMapBytes128 : kMapBytes64)) return rc;
             if (int rc = make_map(ctx, &tv, v_cache, 4, dims, strides, box, kMapBytes)) return rc;
         }
-        if (p.num_tiles > hd->num_ctas) {
-            p.tile_counter = static_cast<uint32_t*>(workspace);
-            const int e = (int)cudaMemsetAsync(workspace, 0, WPP_WS_HEADER_BYTES, (cudaStream_t)cuda_stream);
-            if (e != 0) return cuda_fail(ctx, e);
-        }
+        if (tiles_taken) p.tile_counter = static_cast<uint32_t*>(workspace);
         const int num_ctas = p.num_tiles < hd->num_ctas ? p.num_tiles : hd->num_ctas;
         const int e = d.dtype == WPP_KV4 ? wpp_launch_kv4_tiles(d.head_dim, tq, &p, num_ctas, cuda_stream)
                                          : wpp_launch_kv8_tiles(d.head_dim, tq, &tk, &tv, &p, num_ctas, cuda_stream);

@@ -104,13 +104,20 @@ constexpr int kCombineRows = 8, kCombineBatch = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kCombineRows) wpp_combine_kernel(const CombineParams p) {
     constexpr int kV = D / 32;
-    grid_dependency_wait();           // (launched while the attention kernel may still be running)
     const char* plan = static_cast<const char*>(p.plan);
-    const WppCombine cu = reinterpret_cast<const WppCombine*>(plan + p.off_combine)[blockIdx.x];
-    const int lane = threadIdx.x & 31, r = blockIdx.y * kCombineRows + (threadIdx.x >> 5);
+    const int lane = threadIdx.x & 31;
+    int record = blockIdx.x, r = blockIdx.y * kCombineRows + (threadIdx.x >> 5);
+    if (p.max_rows < kCombineRows) {      // records of few rows: several in a block
+        const int at = blockIdx.x * kCombineRows + (threadIdx.x >> 5);
+        record = at / p.max_rows;
+        r = at - record * p.max_rows;
+        if (record >= p.num_records) return;
+    }
+    const WppCombine cu = reinterpret_cast<const WppCombine*>(plan + p.off_combine)[record];
     if (r >= cu.rows) return;
     const int64_t tok = (int64_t)reinterpret_cast<const int32_t*>(plan + p.off_q_offsets)[cu.request] + cu.row0 + r;
     const int64_t row = ((int64_t)cu.slot0 * 2 + cu.half) * 128 + cu.lane0 + r;      // + 256 per part
+    grid_dependency_wait();           // (launched while the attention kernel may still be running; the plan stands since before that)
     float m = -INFINITY, wsum = 0.f;
     bool nan = false;                 // some part's scores had one: the row is NaN, as it is when the tile is not cut
     for (int s = lane; s < cu.num_splits; s += 32) {
@@ -219,7 +226,9 @@ extern "C" int wpp_launch_append(const wpp::AppendParams* p, int num_sms, void* 
 
 extern "C" int wpp_launch_combine(const wpp::CombineParams* p, int num_combine, void* stream) {
     if (num_combine == 0) return 0;
-    const dim3 grid((unsigned)num_combine, (unsigned)((p->max_rows + wpp::kCombineRows - 1) / wpp::kCombineRows));
+    if (p->max_rows < 1) return 0;
+    dim3 grid((unsigned)num_combine, (unsigned)((p->max_rows + wpp::kCombineRows - 1) / wpp::kCombineRows));
+    if (p->max_rows < wpp::kCombineRows) grid = dim3((unsigned)(((int64_t)num_combine * p->max_rows + wpp::kCombineRows - 1) / wpp::kCombineRows));
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = grid;
     cfg.blockDim = dim3(32 * wpp::kCombineRows);

@@ -75,6 +75,8 @@ struct Kv4AppendParams {
     int32_t num_requests, num_kv_heads, page_size, max_blocks, num_pages;
     int32_t few;                     // as in AppendParams
     uint32_t off_q_offsets, off_prefix;
+    uint32_t off_touched;            // (8 bits) WppTouched [num_touched] of the plan
+    int32_t num_touched;
     int64_t total_new_tokens;
 };
 
@@ -99,6 +101,8 @@ struct Kv4AttnParams {
     uint32_t bf16_128;               // 128 in both halves of a word; as below
     int32_t first_tile, num_tiles;   // of the plan's units
     uint32_t* tile_counter;          // or null: every CTA has one tile
+    uint32_t* few_counter;           // (few rows) or null: every CTA has the units off_few_ctas says
+    int32_t num_few;                 // units of the kernel for few rows
     uint32_t f16_1024, f16_64;       // f16 1024 and 64 in both halves of a word (from here, and no constants: see codes_low)
 };
 
@@ -111,6 +115,7 @@ struct CombineParams {
     int64_t o_token_stride, o_head_stride;
     int32_t num_q_heads, head_dim;
     int32_t max_rows;                // most rows of a combine record
+    int32_t num_records;
     uint32_t off_q_offsets, off_combine;
 };
 

@@ -6,8 +6,8 @@
 // of standing rows rises by 2^n, their codes are taken down by 2^n.
 //
 // A (touched page, head, K or V) is a unit.  It has as many warps as the page has 16 slots, each of which holds its rows in registers
-// between the search for the largest value and the conversion: the rows are read once.  Units are numbered without a table of touched
-// pages: request i's begin at q_offset_i / B + 2 i, which leaves room for all it can touch and some numbers unused.
+// between the search for the largest value and the conversion: the rows are read once.  The plan lists the touched pages, so that a unit
+// knows its rows before it waits for the kernel before, and rows, lengths and page id are asked for at once behind that.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -33,46 +33,23 @@ __global__ void __launch_bounds__(32 * kKv8AppendWarps) wpp_kv8_append_kernel(co
     constexpr int kVecs = D / 8, kTurns = 16 * kVecs / 32, kApart = 32 / kVecs;      // 16-byte vectors of a row; of a lane; rows between them
     __shared__ uint32_t s_top[kKv8AppendWarps];
     if (!p.few) grid_launch_dependents();
-    grid_dependency_wait();
     const char* plan = static_cast<const char*>(p.plan);
-    const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets);
-    const int32_t* plan_prefix = reinterpret_cast<const int32_t*>(plan + p.off_prefix);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, page_shift = 31 - __clz(p.page_size);
     const int unit_shift = page_shift - 4, part = warp & ((1 << unit_shift) - 1);    // warps of a unit (log2); which of them this is
     const uint32_t unit = blockIdx.x * (uint32_t)(kKv8AppendWarps >> unit_shift) + (uint32_t)(warp >> unit_shift);
     const uint32_t heads = (uint32_t)p.num_kv_heads, pair = unit / heads, head = unit - pair * heads;
-    const bool is_v = (pair & 1u) != 0u;
-    const int number = (int)(pair >> 1);
-
-    // ---- the unit's request: the last one that begins at `number` or before
-    int lo = 0, hi = p.num_requests;
-    while (hi - lo > 1) {
-        const int width = (hi - lo + 31) / 32, i = lo + lane * width;
-        const unsigned le = __ballot_sync(0xffffffffu, i < hi && (q_offsets[i] >> page_shift) + 2 * i <= number) | 1u;
-        const int last = 31 - __clz((int)le);
-        hi = min(hi, lo + (last + 1) * width);
-        lo += last * width;
-    }
-    const int q_off = q_offsets[lo], P = p.prefix_lens[lo], C = p.chunk_lens[lo];
-    bool there = true;
-    if (P != plan_prefix[lo] || C != q_offsets[lo + 1] - q_off) {
-        if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_PLAN_MISMATCH);
-        there = false;
-    }
-    const int64_t blk = (int64_t)(P >> page_shift) + number - ((q_off >> page_shift) + 2 * lo), first = blk << page_shift;      // the page's first position
-    there = there && C > 0 && first < (int64_t)P + C;
-    int slot0 = 0, slot1 = 0, stand = 0;      // slots that are written; those before slot0 stand
-    uint8_t* block = nullptr;
-    if (there) {
-        const int page = blk < p.max_blocks ? p.block_tables[(int64_t)lo * p.max_blocks + blk] : -1;
-        if (page < 0 || page >= p.num_pages) {
-            if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
-        } else {
-            block = (is_v ? p.v_cache : p.k_cache) + page * p.page_bytes + head * p.head_bytes;
-            stand = slot0 = (int)max((int64_t)P - first, (int64_t)0);
-            slot1 = (int)min((int64_t)P + C - first, (int64_t)p.page_size);
-        }
-    }
+    const bool is_v = (pair & 1u) != 0u, there = (int64_t)(pair >> 1) < p.num_touched;
+    // ---- the unit's rows, from the plan: slots [slot0, slot1) of the page; those before slot0 stand
+    WppTouched at = {0, 0};
+    if (there) at = reinterpret_cast<const WppTouched*>(plan + p.off_touched)[pair >> 1];
+    const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets) + at.request;
+    const int q_off = q_offsets[0], C = q_offsets[1] - q_off, P = reinterpret_cast<const int32_t*>(plan + p.off_prefix)[at.request];
+    const int64_t first = (int64_t)at.block << page_shift;             // the page's first position
+    const int slot0 = there ? (int)max((int64_t)P - first, (int64_t)0) : 0;
+    const int slot1 = there ? (int)min((int64_t)P + C - first, (int64_t)p.page_size) : 0, stand = slot0;
+    grid_dependency_wait();
+    const int P_now = p.prefix_lens[at.request], C_now = p.chunk_lens[at.request];
+    const int page = there && at.block < p.max_blocks ? p.block_tables[(int64_t)at.request * p.max_blocks + at.block] : -1;
 
     // ---- the warp's rows, and the largest finite value of the unit's
     const int col = lane % kVecs, row = 16 * part + lane / kVecs;      // rows row, row + kApart, ..
@@ -85,9 +62,19 @@ __global__ void __launch_bounds__(32 * kKv8AppendWarps) wpp_kv8_append_kernel(co
         x[i] = make_uint4(0, 0, 0, 0);
         if (slot >= slot0 && slot < slot1) x[i] = *reinterpret_cast<const uint4*>(src + (token0 + slot) * p.kvnew_token_stride);
     }
+    uint8_t* block = nullptr;
+    if (there) {
+        if (P_now != P || C_now != C) {
+            if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_PLAN_MISMATCH);
+        } else if (page < 0 || page >= p.num_pages) {
+            if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
+        } else {
+            block = (is_v ? p.v_cache : p.k_cache) + page * p.page_bytes + head * p.head_bytes;
+        }
+    }
     float* const scale_at = reinterpret_cast<float*>(block + (D << page_shift));
     int e_old = kKv8LeastExp;
-    if (stand > 0) e_old = min(max(exponent_of(*scale_at), kKv8LeastExp), kKv8MostExp);
+    if (block && stand > 0) e_old = min(max(exponent_of(*scale_at), kKv8LeastExp), kKv8MostExp);
     uint32_t m = 0u;
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) m = abs_max(abs_max(abs_max(abs_max(m, x[i].x), x[i].y), x[i].z), x[i].w);
@@ -155,7 +142,7 @@ __global__ void __launch_bounds__(32 * kKv8AppendWarps) wpp_kv8_append_kernel(co
 
 extern "C" int wpp_launch_kv8_append(int head_dim, const wpp::Kv4AppendParams* p, int num_sms, void* stream) {
     if (p->total_new_tokens == 0) return 0;
-    const int64_t units = (p->total_new_tokens / p->page_size + 2 * (int64_t)p->num_requests) * 2 * p->num_kv_heads;
+    const int64_t units = (int64_t)p->num_touched * 2 * p->num_kv_heads;
     const int64_t per_block = wpp::kKv8AppendWarps * 16 / p->page_size, blocks = (units + per_block - 1) / per_block;
     if (blocks > 0x7fffffff) return (int)cudaErrorInvalidValue;
     wpp::Kv4AppendParams q = *p;

@@ -304,44 +304,57 @@ __device__ __forceinline__ void step(State<D, NT>& st, const uint32_t at, const 
     }
 }
 
+// A unit with what the plan says of its request.  (Plans are copied in front of the wave's kernels, whose results are waited for after this.)
+struct Unit {
+    WppUnit un;
+    int q_off, P, C;
+};
+__device__ __forceinline__ Unit unit_at(const Kv4AttnParams& p, int unit) {
+    const char* plan = static_cast<const char*>(p.plan);
+    Unit x;
+    x.un = reinterpret_cast<const WppUnit*>(plan + p.off_units)[unit];
+    const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets) + x.un.request;
+    x.q_off = q_offsets[0];
+    x.C = q_offsets[1] - x.q_off;
+    x.P = reinterpret_cast<const int32_t*>(plan + p.off_prefix)[x.un.request];
+    return x;
+}
+
 template <int D, int NT>
-__device__ __forceinline__ void unit_of(const Kv4AttnParams& p, const int unit, uint8_t* smem) {
+__device__ __forceinline__ void run_unit(const Kv4AttnParams& p, const Unit& unit, uint8_t* smem) {
     using M = Smem<D, NT>;
     constexpr int kSteps = D / 16;             // 16-wide pieces of a row
     float (*s_o)[8 * NT][D + 4] = reinterpret_cast<float (*)[8 * NT][D + 4]>(smem);
     float2 (*s_ml)[8 * NT] = reinterpret_cast<float2 (*)[8 * NT]>(smem + M::kOffMl);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-    const char* plan = static_cast<const char*>(p.plan);
-    const WppUnit un = reinterpret_cast<const WppUnit*>(plan + p.off_units)[unit];
-    const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets);
-    const int q_off = q_offsets[un.request], P = p.prefix_lens[un.request], C = p.chunk_lens[un.request];
-    if (P != reinterpret_cast<const int32_t*>(plan + p.off_prefix)[un.request] || C != q_offsets[un.request + 1] - q_off) {
-        if (threadIdx.x == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_PLAN_MISMATCH);
-        // (the combine pass reads the parts of a refused request too: none of them has seen a key)
-        if (un.split_slot >= 0 && threadIdx.x < un.rows[0] * un.rows[1])
-            p.ws_lse[((int64_t)un.split_slot * 2 + un.row0[1]) * 128 + un.head[1] + threadIdx.x] = -INFINITY;
-        return;
-    }
+    const WppUnit& un = unit.un;
+    const int q_off = unit.q_off, P = unit.P, C = unit.C;
+    // (what the launch has is compared with the plan while the first keys are under way)
+    const int P_now = p.prefix_lens[un.request], C_now = p.chunk_lens[un.request];
     const int toks = un.rows[0], rows = toks * un.rows[1], first_pos = P + un.row0[0];     // first_pos: last key that token 0 sees
     const int key_begin = un.kv_begin * WPP_TILE_N;
     const int seen = min(min(P + C, un.kv_end * WPP_TILE_N), first_pos + toks);            // keys that some row sees end here
     const int kvh = un.head[0] / p.group, page_shift = 31 - __clz(p.page_size), in_page = p.page_size - 1;
     const int32_t* table = p.block_tables + (int64_t)un.request * p.max_blocks;
 
-    // ---- the warp's keys: 32 at a time, every kWarps-th
+    // ---- the warp's keys: 32 at a time, every kWarps-th; page ids are asked for a stage ahead of the rows they lead to
     constexpr int kStride = kKeys * kWarps, kChunks = D / 16;          // kChunks: 16-byte pieces of a row
     const uint32_t ring = smem_u32(smem) + warp * M::kDepth * M::kStage;
     const uint8_t* const kc = p.k_cache + kvh * p.head_bytes;
     const uint8_t* const vc = p.v_cache + kvh * p.head_bytes;
     const int row = lane / kChunks, piece = lane % kChunks;
-    int bad = 0;
-    auto request16 = [&](int key, int keys, uint32_t dst, int at) {    // `keys` (16 or 32) keys of one page, `at` keys into the stage
-        int page = table[key >> page_shift];
-        if (page < 0 || page >= p.num_pages) {
+    int bad = 0, page[2] = {0, 0};
+    auto look_up = [&](int key) {
+        if (key >= seen) return;
+        page[0] = table[key >> page_shift];
+        if (p.page_size == 16 && key + 16 < seen) page[1] = table[(key >> page_shift) + 1];
+    };
+    auto request16 = [&](int key, int keys, uint32_t dst, int at, int id) {      // `keys` (16 or 32) keys of one page, `at` keys into the stage
+        if (id < 0 || id >= p.num_pages) {
             bad = 1;
-            page = 0;
+            id = 0;
         }
-        const int64_t block = page * p.page_bytes;
+        const int64_t block = id * p.page_bytes;
         const int64_t from = block + (key & in_page) * D + lane * 16;
 #pragma unroll
         for (int i = 0; i < kKeys * kChunks / 32; ++i) {
@@ -358,15 +371,17 @@ __device__ __forceinline__ void unit_of(const Kv4AttnParams& p, const int unit, 
     auto request = [&](int key, uint32_t dst) {
         if (key < seen) {
             if (p.page_size > 16) {
-                request16(key, min((seen - key + 15) & ~15, kKeys), dst, 0);
+                request16(key, min((seen - key + 15) & ~15, kKeys), dst, 0, page[0]);
             } else {
-                request16(key, 16, dst, 0);
-                if (key + 16 < seen) request16(key + 16, 16, dst, 16);
+                request16(key, 16, dst, 0, page[0]);
+                if (key + 16 < seen) request16(key + 16, 16, dst, 16, page[1]);
             }
+            look_up(key + kStride);
         }
         copies_commit();                                               // (an empty group where there is nothing: groups are counted)
     };
     int key = key_begin + warp * kKeys;
+    look_up(key);
 #pragma unroll
     for (int i = 0; i < M::kDepth - 1; ++i) request(key + i * kStride, ring + i * M::kStage);
 
@@ -406,6 +421,13 @@ __device__ __forceinline__ void unit_of(const Kv4AttnParams& p, const int unit, 
         // of the columns this thread has of S^T: 2 t, 2 t + 1
 #pragma unroll
         for (int c = 0; c < 2; ++c) q_scale[nt][c] = p.scale_log2 * __shfl_sync(0xffffffffu, down, 8 * t + 4 * c);
+    }
+    if (P_now != P || C_now != C) {
+        if (threadIdx.x == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_PLAN_MISMATCH);
+        // (the combine pass reads the parts of a refused request too: none of them has seen a key)
+        if (un.split_slot >= 0 && threadIdx.x < rows) p.ws_lse[((int64_t)un.split_slot * 2 + un.row0[1]) * 128 + un.head[1] + threadIdx.x] = -INFINITY;
+        copies_wait<0>();
+        return;
     }
     State<D, NT> st;
 #pragma unroll
@@ -493,12 +515,26 @@ template <int D, int NT>
 __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 3 : 2) wpp_kv8_few_kernel(const Kv4AttnParams p) {
     extern __shared__ __align__(128) uint8_t smem[];
     grid_launch_dependents();
+    // units: those that the plan says, or (few_counter) the CTA's own and then whichever is next
+    __shared__ int s_next;
+    const bool taken = p.few_counter != nullptr, one_each = p.num_few == (int)gridDim.x;
+    int u = blockIdx.x, end = taken ? p.num_few : u + 1;
+    if (!taken && !one_each) {
+        const int32_t* range = reinterpret_cast<const int32_t*>(static_cast<const char*>(p.plan) + p.off_few_ctas) + blockIdx.x;
+        u = range[0];
+        end = range[1];
+    }
+    Unit unit = unit_at(p, u);
     grid_dependency_wait();
-    const int32_t* first = reinterpret_cast<const int32_t*>(static_cast<const char*>(p.plan) + p.off_few_ctas) + blockIdx.x;
-    const int end = first[1];
-    for (int u = first[0]; u < end; ++u) {
-        unit_of<D, NT>(p, u, smem);
+    while (true) {
+        if (taken && threadIdx.x == 0) s_next = end > (int)gridDim.x ? (int)(gridDim.x + atomicAdd(p.few_counter, 1u)) : end;      // (while the unit is under way)
+        run_unit<D, NT>(p, unit, smem);
+        if (!taken && u + 1 >= end) break;
         __syncthreads();                       // (the next unit's keys take the place of this one's results)
+        u = taken ? s_next : u + 1;
+        if (u >= end) break;
+        unit = unit_at(p, u);
+        if (taken) __syncthreads();            // (read by all before it is written again)
     }
 }
 

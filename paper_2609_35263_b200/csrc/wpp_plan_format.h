@@ -24,9 +24,10 @@ struct WppPlanHeader {
     uint32_t off_units;             // WppUnit [num_units] in the order the persistent CTAs take them
     uint32_t off_combine;           // WppCombine [num_combine]
     int32_t shape;                  // 1: two-half CTAs, one per SM; 2: single-half CTAs, two per SM (work item = half a unit); 3: 4-bit cache
-    int32_t nonempty_halves;
+    int32_t nonempty_halves;        // (8-bit cache: pages that the append touches, WppTouched behind the combine records)
     int32_t max_combine_rows;       // most rows of a combine record (sizes the combine pass's grid)
-    int32_t deal_items;             // small shape: its items are dealt out to the CTAs, without the workspace's counter
+    int32_t deal_items;             // small shape: its items are dealt out to the CTAs, without the workspace's counter; shape 3: the units of
+                                    // the kernel for few rows are not, but taken by the CTAs from a counter in the workspace's header
     int32_t num_few_units;          // 4-bit cache: the first of the units are of the kernel for few rows ...
     int32_t max_few_rows;           // ... which has so many rows at most; ...
     int32_t num_few_ctas;
@@ -56,6 +57,11 @@ struct WppUnit {
 // range is in steps of WPP_TILE_N keys too.
 #define WPP_FEW_ROWS 16
 
+// A page that new rows of a request go to: number `block` of its table's row.
+struct WppTouched {
+    int32_t request, block;
+};
+
 // One half tile whose key range was split: partial slots [slot0, slot0+num_splits) merged in increasing order.
 struct WppCombine {
     int32_t request, row0, rows, head;
@@ -65,7 +71,7 @@ struct WppCombine {
 };
 
 // Workspace layout: WPP_WS_HEADER_BYTES of header (byte 0: a uint32 counter, the next tile of the order nobody has
-// taken yet, for launches that take their tiles from one: the attention call zeroes the header on the stream before
-// those), then fp32
+// taken yet, for launches that take their tiles from one; byte 128: the same of a kernel for few rows: the attention call zeroes
+// the header on the stream before those), then fp32
 // O_part[num_split_slots][2][128][head_dim] followed by fp32 lse_part[num_split_slots][2][128] (log2 units of the
 // scaled scores; -inf marks a row with no visible key in that part).

@@ -31,6 +31,18 @@ constexpr int64_t kFewShort = 4;
 constexpr int64_t kTileLeastSteps = 4, kTileLeastWin = 3;
 constexpr int64_t kTileOrderRounds = 16;
 
+// 8-bit cache, few rows.  With equal shares the CTAs of 64 x 1 over 255..16,383 (64/8 heads of 128) end between 0.69 and 1 of the
+// last one's time: SMs do not get equal shares of the memory's rate.  Where a share is long enough, blocks are cut into long parts, about one for
+// each CTA, and short ones, which the CTAs take, the longest first, as they become free.
+constexpr int64_t kDealSteps = 24;                 // of a share: fewer are dealt out as they are
+#ifndef KLP
+#define KLP 0.75
+#endif
+#ifndef KSP
+#define KSP 0.15
+#endif
+constexpr double kLongPart = KLP, kShortPart = KSP;
+
 // Row blocks of the kernel for few rows: heads of a KV group, and tokens, WPP_FEW_ROWS rows at most.
 static int32_t few_heads(int32_t group) { return std::min<int32_t>(group, WPP_FEW_ROWS); }
 static int32_t few_tokens(int32_t group) { return std::max<int32_t>(1, WPP_FEW_ROWS / few_heads(group)); }
@@ -146,21 +158,38 @@ static int64_t few_walks(const wpp_batch_desc* d, const wpp_plan_opts* o, const 
     return best;
 }
 
+// The pages that the wave's new rows are in, at most T / page_size + 2 R; out may be null.
+static int64_t touched_pages(const wpp_batch_desc* d, const int32_t* prefix_lens, const int32_t* chunk_lens, WppTouched* out) {
+    int64_t n = 0;
+    for (int i = 0; i < d->num_requests; ++i) {
+        const int64_t P = prefix_lens[i], C = chunk_lens[i], B = d->page_size;
+        if (C == 0) continue;
+        const int64_t from = P / B, to = (P + C + B - 1) / B;
+        for (int64_t b = from; out && b < to; ++b) out[n + b - from] = {i, (int32_t)b};
+        n += to - from;
+    }
+    return n;
+}
+
 size_t wpp_kv4_plan_bytes(const wpp_batch_desc* d, const wpp_plan_opts* o, int64_t T) {
     const int32_t G = d->num_q_heads / d->num_kv_heads, h = few_heads(G), t = few_tokens(G);
     const int64_t base = (T / t + d->num_requests) * ((G + h - 1) / h) * d->num_kv_heads;
-    const int64_t units = o->force_kv_splits >= 2 ? base * o->force_kv_splits : base + kFewCtas * (int64_t)o->max_ctas;
+    // (dealt parts: long ones and short ones of a share are at most 1 / kLongPart + 1 / kShortPart, and a block has two more)
+    const int64_t units = o->force_kv_splits >= 2 ? base * o->force_kv_splits
+                          : d->dtype == WPP_KV8   ? 3 * base + 12 * kFewCtas * (int64_t)o->max_ctas
+                                                  : base + kFewCtas * (int64_t)o->max_ctas;
     size_t n = sizeof(WppPlanHeader) + 2 * align_up(sizeof(int32_t) * (size_t)(d->num_requests + 1), 16);
     n += sizeof(WppUnit) * (size_t)units + align_up(sizeof(int32_t) * ((size_t)std::max(units, kFewCtas * (int64_t)o->max_ctas) + 1), 16);
     n += sizeof(WppCombine) * (size_t)(T * d->num_q_heads / t + (int64_t)d->num_requests * d->num_q_heads);
     const int64_t tiles = (T / WPP_HALF_M + d->num_requests) * d->num_q_heads;
     n += sizeof(WppUnit) * (size_t)(o->force_kv_splits >= 2 ? tiles * o->force_kv_splits : tiles + (int64_t)o->max_ctas);
     n += sizeof(WppCombine) * (size_t)tiles;
+    if (d->dtype == WPP_KV8) n += sizeof(WppTouched) * (size_t)(T / d->page_size + 2 * (int64_t)d->num_requests);
     return align_up(n, 256);
 }
 
-int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t* prefix_lens, const int32_t* chunk_lens, int64_t T,
-                 int64_t pairs, void* plan_host, size_t plan_host_bytes, wpp_plan_info* info) {
+static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t* prefix_lens, const int32_t* chunk_lens, int64_t T,
+                     int64_t pairs, bool may_deal, void* plan_host, size_t plan_host_bytes, wpp_plan_info* info) {
     const int R = d->num_requests, Hq = d->num_q_heads, Hkv = d->num_kv_heads, G = Hq / Hkv;
     if (plan_host_bytes < wpp_kv4_plan_bytes(d, o, T)) return WPP_ERR_PLAN_MISMATCH;
     auto steps_for = [](int64_t keys) { return (int32_t)((keys + WPP_TILE_N - 1) / WPP_TILE_N); };
@@ -192,9 +221,13 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
         left -= n + kUnitSteps;
         return at + n;
     };
+    const bool deal = may_deal && d->dtype == WPP_KV8 && o->force_kv_splits < 1 && share >= kDealSteps;
+    // (rows of a unit in a slot; the 4-bit cache's plans have always taken the most that there can be)
+    const int32_t slot_rows = d->dtype == WPP_KV8 && max_rows <= WPP_FEW_ROWS / 2 ? WPP_FEW_ROWS / 2 : WPP_FEW_ROWS;
+    const int32_t long_part = (int32_t)((double)share * kLongPart), short_part = std::max((int32_t)((double)share * kShortPart), (int32_t)kLeastSteps);
     // Blocks too short to be cut may leave much of every share: it grows until the CTAs are enough (5 x 9..43 tokens, 40/8 heads: 320 blocks
     // of a step on 296 CTAs, of which the last had 25, 274 us | 14.5)
-    for (int64_t ctas = most_ctas + 1; o->force_kv_splits < 1 && ctas > most_ctas;) {
+    for (int64_t ctas = most_ctas + 1; o->force_kv_splits < 1 && !deal && ctas > most_ctas;) {
         int64_t left = share;
         ctas = 1;
         bool next = false;
@@ -237,6 +270,11 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
                     if (o->force_kv_splits >= 1) {
                         const int32_t n = std::min(o->force_kv_splits, steps);
                         for (int32_t q = 1; q <= n; ++q) cuts.push_back((int32_t)((int64_t)steps * q / n));
+                    } else if (deal) {
+                        const int32_t longs = steps <= long_part ? 0 : (int32_t)((double)steps * kLongPart / long_part);
+                        for (int32_t q = 0; q < longs; ++q) cuts.push_back(cuts.back() + long_part);
+                        const int32_t from = cuts.back(), n = steps <= long_part ? 1 : (steps - from + short_part - 1) / short_part;
+                        for (int32_t q = 1; q <= n; ++q) cuts.push_back(from + (int32_t)((int64_t)(steps - from) * q / n));
                     } else {
                         for (int32_t at = 0; at < steps;) {
                             bool next;
@@ -257,7 +295,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
                     u.split_slot = -1;
                     u.pack = 1;
                     if (parts > 1) {
-                        if (parts > slot_parts || slot_row + WPP_FEW_ROWS > 2 * WPP_HALF_M) {
+                        if (parts > slot_parts || slot_row + slot_rows > 2 * WPP_HALF_M) {
                             slot0 = slots;
                             slot_parts = parts;
                             slot_row = 0;
@@ -265,7 +303,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
                         }
                         u.row0[1] = slot_row / WPP_HALF_M;
                         u.head[1] = slot_row % WPP_HALF_M;
-                        slot_row += WPP_FEW_ROWS;
+                        slot_row += slot_rows;
                         for (int32_t k = 0; k < nh; ++k)
                             combines.push_back({i, (int32_t)r0, rows, u.head[0] + k, slot0, parts, u.row0[1], u.head[1] + k * rows});
                     }
@@ -283,6 +321,13 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
         }
     }
     const int64_t n_few = n_units;
+    // (a wave that the built-in scratch array would hold otherwise must not be refused for its many parts)
+    if (deal && slots > scratch_slots(d))
+        return make_plan(d, o, prefix_lens, chunk_lens, T, pairs, false, plan_host, plan_host_bytes, info);
+    if (deal) {
+        std::stable_sort(us, us + n_few, [](const WppUnit& a, const WppUnit& b) { return a.cost > b.cost; });
+        first.assign((size_t)std::min<int64_t>(most_ctas, n_few), 0);
+    }
 
     // ---- tiles
     struct Tile { WppUnit u; int32_t steps; };
@@ -355,11 +400,18 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     off += align_up(sizeof(int32_t) * first.size(), 16);
     hd.off_combine = (uint32_t)off;
     off += sizeof(WppCombine) * combines.size();
+    const size_t off_touched = off;          // (of the append; behind the combine records)
+    int64_t n_touched = 0;
+    if (d->dtype == WPP_KV8) {
+        n_touched = touched_pages(d, prefix_lens, chunk_lens, nullptr);
+        off += sizeof(WppTouched) * (size_t)n_touched;
+    }
     hd.plan_bytes = align_up(off, 16);
     if (hd.plan_bytes > plan_host_bytes) return WPP_ERR_PLAN_MISMATCH;
     if (hd.plan_bytes > 0xffffffffu) return WPP_ERR_INVALID_ARG;       // (offsets are 32 bits)
     std::memcpy(p + hd.off_few_ctas, first.data(), sizeof(int32_t) * first.size());
     if (!combines.empty()) std::memcpy(p + hd.off_combine, combines.data(), sizeof(WppCombine) * combines.size());
+    if (n_touched > 0) touched_pages(d, prefix_lens, chunk_lens, reinterpret_cast<WppTouched*>(p + off_touched));
     std::memset(p + off, 0, hd.plan_bytes - off);
 
     hd.magic = WPP_PLAN_MAGIC;
@@ -370,6 +422,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     hd.num_units = (int32_t)n_units;
     hd.num_few_units = (int32_t)n_few;
     hd.num_few_ctas = few_ctas;
+    hd.deal_items = deal && n_few > 0;
     hd.max_few_rows = max_rows;
     hd.num_combine = (int32_t)combines.size();
     hd.num_split_slots = slots;
@@ -381,6 +434,7 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     hd.total_new_tokens = T;
     hd.key_steps = key_steps;
     hd.flops = 4 * (int64_t)d->head_dim * Hq * pairs;
+    hd.nonempty_halves = (int32_t)n_touched;
     hd.workspace_bytes = WPP_WS_HEADER_BYTES + align_up((size_t)slots * 2 * WPP_HALF_M * (d->head_dim + 1) * sizeof(float), 256);
     std::memcpy(p, &hd, sizeof(hd));
     int32_t* qo = reinterpret_cast<int32_t*>(p + hd.off_q_offsets);
@@ -400,4 +454,9 @@ int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t*
     info->workspace_bytes = hd.workspace_bytes;
     info->plan_bytes = hd.plan_bytes;
     return WPP_OK;
+}
+
+int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t* prefix_lens, const int32_t* chunk_lens, int64_t T,
+                 int64_t pairs, void* plan_host, size_t plan_host_bytes, wpp_plan_info* info) {
+    return make_plan(d, o, prefix_lens, chunk_lens, T, pairs, true, plan_host, plan_host_bytes, info);
 }

@@ -445,14 +445,15 @@ static int codes_attention(const wpp_ctx* ctx, const wpp_batch_desc& d, const Wp
     p.num_tiles = hd->num_units - hd->num_few_units;
     p.scale_log2 = scale_log2_of(d);
     p.num_few = hd->num_few_units;
-    const bool few_taken = hd->deal_items && p.num_few > hd->num_few_ctas, tiles_taken = p.num_tiles > hd->num_ctas;
-    if (hd->deal_items) p.few_counter = static_cast<uint32_t*>(workspace) + 32;
+    const bool few_taken = hd->deal_items == 1 && p.num_few > hd->num_few_ctas, tiles_taken = p.num_tiles > hd->num_ctas;
+    if (hd->deal_items == 1) p.few_counter = static_cast<uint32_t*>(workspace) + 32;
     if (few_taken || tiles_taken) {
         const int e = (int)cudaMemsetAsync(workspace, 0, WPP_WS_HEADER_BYTES, (cudaStream_t)cuda_stream);
         if (e != 0) return cuda_fail(ctx, e);
     }
     if (hd->num_few_units > 0) {
-        const int e = (d.dtype == WPP_KV4 ? wpp_launch_kv4_few : wpp_launch_kv8_few)(d.head_dim, &p, hd->num_few_ctas, hd->max_few_rows, cuda_stream);
+        const int e = d.dtype == WPP_KV4 ? wpp_launch_kv4_few(d.head_dim, &p, hd->num_few_ctas, hd->max_few_rows, cuda_stream)
+                                         : wpp_launch_kv8_few(d.head_dim, &p, hd->num_few_ctas, hd->max_few_rows, hd->deal_items > 1 ? hd->deal_items - 1 : 0, cuda_stream);
         if (e != 0) return cuda_fail(ctx, e);
         const_cast<wpp_ctx*>(ctx)->launches += 1;
     }

@@ -252,7 +252,7 @@ int wpp_launch_kv4_append(int head_dim, const wpp::Kv4AppendParams* p, int num_s
 int wpp_launch_kv8_append(int head_dim, const wpp::Kv4AppendParams* p, int num_sms, void* stream);
 int wpp_launch_kv8_tiles(int head_dim, const CUtensorMap* tq, const CUtensorMap* tk, const CUtensorMap* tv, const wpp::Kv4AttnParams* p,
                          int num_ctas, void* stream);
-int wpp_launch_kv8_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream);
+int wpp_launch_kv8_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, int log_parts, void* stream);
 int wpp_launch_kv4_tiles(int head_dim, const CUtensorMap* tq, const wpp::Kv4AttnParams* p, int num_ctas, void* stream);
 int wpp_launch_kv4_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream);
 int wpp_launch_rope(const wpp::RopeParams* p, int head_dim, int neighbours, int write, int num_sms, void* stream);

@@ -5,8 +5,8 @@
 // division is a product with 2^-e, exact (what it would make a subnormal number is far below the least code).  Where the scale
 // of standing rows rises by 2^n, their codes are taken down by 2^n.
 //
-// A (touched page, head, K or V) is a unit.  It has as many warps as the page has 16 slots, each of which holds its rows in registers
-// between the search for the largest value and the conversion: the rows are read once.  The plan lists the touched pages, so that a unit
+// A (touched page, head, K or V) is a CTA, of as many warps as the page has 16 slots, each of which holds its rows in registers
+// between the search for the largest value and the conversion: the rows are read once.  The plan lists the touched pages, so that a CTA
 // knows its rows before it waits for the kernel before, and rows, lengths and page id are asked for at once behind that.
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -18,8 +18,6 @@
 
 namespace wpp {
 
-constexpr int kKv8AppendWarps = 8;
-
 __device__ __forceinline__ uint32_t abs_max(uint32_t m, uint32_t w) { return __vmaxu2(m, w & 0x7fff7fffu); }
 
 // the exponent of the least scale for values of which `top` (bf16 bits, finite) is the largest: 448 = 1.75 * 2^8
@@ -29,29 +27,25 @@ __device__ __forceinline__ int scale_exponent(uint32_t top) {
 }
 
 template <int D>
-__global__ void __launch_bounds__(32 * kKv8AppendWarps) wpp_kv8_append_kernel(const Kv4AppendParams p) {
+__global__ void __launch_bounds__(256) wpp_kv8_append_kernel(const Kv4AppendParams p) {
     constexpr int kVecs = D / 8, kTurns = 16 * kVecs / 32, kApart = 32 / kVecs;      // 16-byte vectors of a row; of a lane; rows between them
-    __shared__ uint32_t s_top[kKv8AppendWarps];
+    __shared__ uint32_t s_top[8];
     if (!p.few) grid_launch_dependents();
     const char* plan = static_cast<const char*>(p.plan);
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, page_shift = 31 - __clz(p.page_size);
-    const int unit_shift = page_shift - 4, part = warp & ((1 << unit_shift) - 1);    // warps of a unit (log2); which of them this is
-    const uint32_t unit = blockIdx.x * (uint32_t)(kKv8AppendWarps >> unit_shift) + (uint32_t)(warp >> unit_shift);
-    const uint32_t heads = (uint32_t)p.num_kv_heads, pair = unit / heads, head = unit - pair * heads;
-    const bool is_v = (pair & 1u) != 0u, there = (int64_t)(pair >> 1) < p.num_touched;
-    // ---- the unit's rows, from the plan: slots [slot0, slot1) of the page; those before slot0 stand
-    WppTouched at = {0, 0};
-    if (there) at = reinterpret_cast<const WppTouched*>(plan + p.off_touched)[pair >> 1];
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, page_shift = 31 - __clz(p.page_size), parts = p.page_size / 16;      // warps; which this is
+    const uint32_t heads = (uint32_t)p.num_kv_heads, pair = blockIdx.x / heads, head = blockIdx.x - pair * heads;
+    const bool is_v = (pair & 1u) != 0u;
+    // ---- the rows, from the plan: slots [slot0, slot1) of the page; those before slot0 stand
+    const WppTouched at = reinterpret_cast<const WppTouched*>(plan + p.off_touched)[pair >> 1];
     const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets) + at.request;
     const int q_off = q_offsets[0], C = q_offsets[1] - q_off, P = reinterpret_cast<const int32_t*>(plan + p.off_prefix)[at.request];
     const int64_t first = (int64_t)at.block << page_shift;             // the page's first position
-    const int slot0 = there ? (int)max((int64_t)P - first, (int64_t)0) : 0;
-    const int slot1 = there ? (int)min((int64_t)P + C - first, (int64_t)p.page_size) : 0, stand = slot0;
+    const int slot0 = (int)max((int64_t)P - first, (int64_t)0), slot1 = (int)min((int64_t)P + C - first, (int64_t)p.page_size), stand = slot0;
     grid_dependency_wait();
     const int P_now = p.prefix_lens[at.request], C_now = p.chunk_lens[at.request];
-    const int page = there && at.block < p.max_blocks ? p.block_tables[(int64_t)at.request * p.max_blocks + at.block] : -1;
+    const int page = at.block < p.max_blocks ? p.block_tables[(int64_t)at.request * p.max_blocks + at.block] : -1;
 
-    // ---- the warp's rows, and the largest finite value of the unit's
+    // ---- the warp's rows, and the largest finite value of the CTA's
     const int col = lane % kVecs, row = 16 * part + lane / kVecs;      // rows row, row + kApart, ..
     const __nv_bfloat16* src = (is_v ? p.v_new : p.k_new) + (int64_t)head * p.kvnew_head_stride + col * 8;
     const int64_t token0 = (int64_t)q_off + first - P;                 // the token in slot 0, if it were one
@@ -63,14 +57,12 @@ __global__ void __launch_bounds__(32 * kKv8AppendWarps) wpp_kv8_append_kernel(co
         if (slot >= slot0 && slot < slot1) x[i] = *reinterpret_cast<const uint4*>(src + (token0 + slot) * p.kvnew_token_stride);
     }
     uint8_t* block = nullptr;
-    if (there) {
-        if (P_now != P || C_now != C) {
-            if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_PLAN_MISMATCH);
-        } else if (page < 0 || page >= p.num_pages) {
-            if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
-        } else {
-            block = (is_v ? p.v_cache : p.k_cache) + page * p.page_bytes + head * p.head_bytes;
-        }
+    if (P_now != P || C_now != C) {
+        if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_PLAN_MISMATCH);
+    } else if (page < 0 || page >= p.num_pages) {
+        if (lane == 0 && p.status) atomicCAS(p.status, 0, WPP_ERR_BOUNDS);
+    } else {
+        block = (is_v ? p.v_cache : p.k_cache) + page * p.page_bytes + head * p.head_bytes;
     }
     float* const scale_at = reinterpret_cast<float*>(block + (D << page_shift));
     int e_old = kKv8LeastExp;
@@ -93,15 +85,14 @@ __global__ void __launch_bounds__(32 * kKv8AppendWarps) wpp_kv8_append_kernel(co
         }
         top = __reduce_max_sync(0xffffffffu, m);
     }
-    if (unit_shift > 0) {
-        if (lane == 0) s_top[warp] = top;
+    if (parts > 1) {
+        if (lane == 0) s_top[part] = top;
         __syncthreads();                      // (every warp has read the standing scale before one of them replaces it, too)
-        top = 0u;
-        for (int i = 0; i < 1 << unit_shift; ++i) top = max(top, s_top[(warp & ~((1 << unit_shift) - 1)) + i]);
+        for (int i = 0; i < parts; ++i) top = max(top, s_top[i]);
     }
     if (!block) return;
     const int e = max(scale_exponent(top), e_old);
-    __syncwarp();                             // (so has every lane of a unit of one warp)
+    __syncwarp();                             // (so has every lane of a CTA of one warp)
     if (part == 0 && lane == 0 && (stand == 0 || e != e_old)) *scale_at = power_of_two(e);
 
     // ---- codes
@@ -142,14 +133,14 @@ __global__ void __launch_bounds__(32 * kKv8AppendWarps) wpp_kv8_append_kernel(co
 
 extern "C" int wpp_launch_kv8_append(int head_dim, const wpp::Kv4AppendParams* p, int num_sms, void* stream) {
     if (p->total_new_tokens == 0) return 0;
-    const int64_t units = (int64_t)p->num_touched * 2 * p->num_kv_heads;
-    const int64_t per_block = wpp::kKv8AppendWarps * 16 / p->page_size, blocks = (units + per_block - 1) / per_block;
+    const int64_t blocks = (int64_t)p->num_touched * 2 * p->num_kv_heads;
+    const int warps = p->page_size / 16;
     if (blocks > 0x7fffffff) return (int)cudaErrorInvalidValue;
     wpp::Kv4AppendParams q = *p;
-    q.few = blocks <= 4 * (int64_t)num_sms;      // (see wpp_launch_kv4_append)
+    q.few = blocks * warps <= 32 * (int64_t)num_sms;      // (see wpp_launch_kv4_append)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
-    cfg.blockDim = dim3(32 * wpp::kKv8AppendWarps);
+    cfg.blockDim = dim3((unsigned)(32 * warps));
     cfg.stream = (cudaStream_t)stream;
     cudaLaunchAttribute overlap;
     overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;

@@ -68,14 +68,18 @@ __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_grou
 
 // A warp's ring of stages in shared memory, kKeys keys each: K's rows, V's rows, and the 16 bytes behind the rows of the two groups of 16
 // keys, of K and of V.
-template <int D, int NT>
+template <int D, int NT, bool kCluster>
 struct Smem {
     static constexpr int kRows = kKeys * D, kStage = 2 * kRows + 64;
-    static constexpr int kDepth = D == 128 ? (NT == 1 ? 2 : 3) : (NT == 1 ? 4 : 5);
+    // (as many as leave three CTAs an SM of blocks of at most 8 rows, else two, which clusters make do with: where each CTA has a few
+    // stages in all, what counts is how many are under way)
+    static constexpr int kDepth = D == 128 ? (NT == 1 && !kCluster ? 2 : 3) : (NT == 1 && !kCluster ? 4 : 5);
     // in the stages' place, once a unit's are done with: float [warps][8 NT][D + 4], float2 [warps][8 NT]
     static constexpr int kOffMl = kWarps * 8 * NT * (D + 4) * 4;
+    // and, of a CTA of a cluster, behind them: float [8 NT][D], the part's rows, and float [8 NT], their log-sums
+    static constexpr int kOffPart = kOffMl + kWarps * 8 * NT * 8, kOffPartLse = kOffPart + 8 * NT * D * 4;
     static constexpr int kBytes = kWarps * kDepth * kStage;
-    static_assert(kOffMl + kWarps * 8 * NT * 8 <= kBytes, "a unit's results fit the stages");
+    static_assert(kOffPartLse + 8 * NT * 4 <= kBytes, "a unit's results fit the stages");
 };
 
 // Which key stands in row r of a 16-key tile of the products (rows 2 and 3, 6 and 7, ... are exchanged), and by how much the 16-byte
@@ -99,10 +103,10 @@ __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return __vcmpeq4(w &
 
 // 32 keys, at shared-memory address `at`.  Lane 4 g + t takes, of a tile's rows g and g + 8, columns [t D / 4, (t + 1) D / 4) of K; of
 // rows 2 t, 2 t + 1, 2 t + 8, 2 t + 9, columns [g D / 8, (g + 1) D / 8) of V.
-template <int D, int NT, bool kMasked>
+template <int D, int NT, bool kCluster, bool kMasked>
 __device__ __forceinline__ void step(State<D, NT>& st, const uint32_t at, const uint32_t (&qf)[NT][D / 16][2], const float (&q_scale)[NT][2],
                                      int key0, int first_pos, int toks, int last, bool first, int g, int t) {
-    using M = Smem<D, NT>;
+    using M = Smem<D, NT, kCluster>;
     const int kg = key_of_row(g), kt = key_of_row(2 * t);
     int limit[NT][2];                                                  // last key that the column's row sees
     if (kMasked) {
@@ -320,9 +324,10 @@ __device__ __forceinline__ Unit unit_at(const Kv4AttnParams& p, int unit) {
     return x;
 }
 
-template <int D, int NT>
+// kCluster: the unit is a part of a block whose other parts the other CTAs of the cluster have; its rows are left in shared memory
+template <int D, int NT, bool kCluster>
 __device__ __forceinline__ void run_unit(const Kv4AttnParams& p, const Unit& unit, uint8_t* smem) {
-    using M = Smem<D, NT>;
+    using M = Smem<D, NT, kCluster>;
     constexpr int kSteps = D / 16;             // 16-wide pieces of a row
     float (*s_o)[8 * NT][D + 4] = reinterpret_cast<float (*)[8 * NT][D + 4]>(smem);
     float2 (*s_ml)[8 * NT] = reinterpret_cast<float2 (*)[8 * NT]>(smem + M::kOffMl);
@@ -382,6 +387,19 @@ __device__ __forceinline__ void run_unit(const Kv4AttnParams& p, const Unit& uni
     };
     int key = key_begin + warp * kKeys;
     look_up(key);
+    uint4 q_rows[NT][D / 32];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+        const int n = 8 * nt + g;
+#pragma unroll
+        for (int w = 0; w < D / 32; ++w) {
+            q_rows[nt][w] = make_uint4(0, 0, 0, 0);
+            if (n < rows) {
+                const int head = un.head[0] + n / toks, tok = q_off + un.row0[0] + n % toks;
+                q_rows[nt][w] = *reinterpret_cast<const uint4*>(p.q + (int64_t)tok * p.q_token_stride + (int64_t)head * p.q_head_stride + t * (D / 4) + 8 * w);
+            }
+        }
+    }
 #pragma unroll
     for (int i = 0; i < M::kDepth - 1; ++i) request(key + i * kStride, ring + i * M::kStage);
 
@@ -391,16 +409,10 @@ __device__ __forceinline__ void run_unit(const Kv4AttnParams& p, const Unit& uni
     float q_scale[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
-        const int n = 8 * nt + g;
-        uint4 z[D / 32];
+        const uint4 (&z)[D / 32] = q_rows[nt];
         float top = 0.f;
 #pragma unroll
         for (int w = 0; w < D / 32; ++w) {
-            z[w] = make_uint4(0, 0, 0, 0);
-            if (n < rows) {
-                const int head = un.head[0] + n / toks, tok = q_off + un.row0[0] + n % toks;
-                z[w] = *reinterpret_cast<const uint4*>(p.q + (int64_t)tok * p.q_token_stride + (int64_t)head * p.q_head_stride + t * (D / 4) + 8 * w);
-            }
             const uint32_t zz[4] = {z[w].x, z[w].y, z[w].z, z[w].w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(zz[i] << 16)), fabsf(__uint_as_float(zz[i] & 0xffff0000u))));
@@ -427,6 +439,10 @@ __device__ __forceinline__ void run_unit(const Kv4AttnParams& p, const Unit& uni
         // (the combine pass reads the parts of a refused request too: none of them has seen a key)
         if (un.split_slot >= 0 && threadIdx.x < rows) p.ws_lse[((int64_t)un.split_slot * 2 + un.row0[1]) * 128 + un.head[1] + threadIdx.x] = -INFINITY;
         copies_wait<0>();
+        if (kCluster) {
+            __syncthreads();
+            if (threadIdx.x < rows) reinterpret_cast<float*>(smem + M::kOffPartLse)[threadIdx.x] = -INFINITY;
+        }
         return;
     }
     State<D, NT> st;
@@ -449,9 +465,9 @@ __device__ __forceinline__ void run_unit(const Kv4AttnParams& p, const Unit& uni
         request(key + (M::kDepth - 1) * kStride, ring + fill);
         fill = at;
         if (key + kKeys - 1 <= first_pos && key + kKeys <= seen)
-            step<D, NT, false>(st, ring + at, qf, q_scale, key, first_pos, toks, seen - 1, first, g, t);
+            step<D, NT, kCluster, false>(st, ring + at, qf, q_scale, key, first_pos, toks, seen - 1, first, g, t);
         else
-            step<D, NT, true>(st, ring + at, qf, q_scale, key, first_pos, toks, seen - 1, first, g, t);
+            step<D, NT, kCluster, true>(st, ring + at, qf, q_scale, key, first_pos, toks, seen - 1, first, g, t);
         first = false;
         at = at == (M::kDepth - 1) * M::kStage ? 0u : at + M::kStage;
     }
@@ -498,7 +514,10 @@ __device__ __forceinline__ void run_unit(const Kv4AttnParams& p, const Unit& uni
         const float inv = nan ? NAN : sum > 0.f ? 1.f / sum : 0.f;
         acc.x *= inv; acc.y *= inv; acc.z *= inv; acc.w *= inv;
         const float lse2 = nan ? NAN : sum > 0.f ? mm + log2f(sum) : -INFINITY;
-        if (un.split_slot < 0) {
+        if (kCluster) {
+            *reinterpret_cast<float4*>(smem + M::kOffPart + (n * D + c) * 4) = acc;
+            if (c == 0) reinterpret_cast<float*>(smem + M::kOffPartLse)[n] = lse2;
+        } else if (un.split_slot < 0) {
             const int64_t tok = (int64_t)q_off + un.row0[0] + n % toks, head = un.head[0] + n / toks;
             *reinterpret_cast<uint2*>(p.out + tok * p.o_token_stride + head * p.o_head_stride + c) =
                 make_uint2(pack_bf16x2(acc.x, acc.y), pack_bf16x2(acc.z, acc.w));
@@ -528,7 +547,7 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 3 : 2) wpp_kv8_few_kern
     grid_dependency_wait();
     while (true) {
         if (taken && threadIdx.x == 0) s_next = end > (int)gridDim.x ? (int)(gridDim.x + atomicAdd(p.few_counter, 1u)) : end;      // (while the unit is under way)
-        run_unit<D, NT>(p, unit, smem);
+        run_unit<D, NT, false>(p, unit, smem);
         if (!taken && u + 1 >= end) break;
         __syncthreads();                       // (the next unit's keys take the place of this one's results)
         u = taken ? s_next : u + 1;
@@ -538,38 +557,102 @@ __global__ void __launch_bounds__(32 * kWarps, NT == 1 ? 3 : 2) wpp_kv8_few_kern
     }
 }
 
+__device__ __forceinline__ void cluster_barrier() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, uint32_t rank) {       // the same place in another CTA's shared memory
+    uint32_t r;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(rank));
+    return r;
+}
+
+// A wave of few blocks: a cluster has a block's parts and joins them in shared memory, so that there is no combine pass, and no
+// partial result in global memory.  Each of its 2^log_parts CTAs takes as many of the rows' pieces of four elements, one lane for each part.
 template <int D, int NT>
-static cudaError_t launch_nt(const Kv4AttnParams& p, int num_ctas, cudaStream_t stream) {
-    static bool attr_set[64] = {};
+__global__ void __launch_bounds__(32 * kWarps, 2) wpp_kv8_cluster_kernel(const Kv4AttnParams p, const int log_parts) {
+    using M = Smem<D, NT, true>;
+    extern __shared__ __align__(128) uint8_t smem[];
+    grid_launch_dependents();
+    const Unit unit = unit_at(p, blockIdx.x);
+    grid_dependency_wait();
+    run_unit<D, NT, true>(p, unit, smem);
+    cluster_barrier();
+    const WppUnit& un = unit.un;
+    const int parts = 1 << log_parts, rank = blockIdx.x & (parts - 1), part = threadIdx.x & (parts - 1), toks = un.rows[0], rows = toks * un.rows[1];
+    const uint32_t rows_at = in_cta(smem_u32(smem) + M::kOffPart, (uint32_t)part), lse_at = in_cta(smem_u32(smem) + M::kOffPartLse, (uint32_t)part);
+    const int groups = 32 * kWarps >> log_parts;                // pieces that the CTA's lanes take at a time
+    for (int i0 = rank * groups; i0 < rows * (D / 4); i0 += groups << log_parts) {
+        const int i = i0 + (int)(threadIdx.x >> log_parts), n = min(i / (D / 4), rows - 1), c = i % (D / 4) * 4;
+        float z;
+        float4 x;
+        asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(z) : "r"(lse_at + n * 4));
+        asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x.x), "=f"(x.y), "=f"(x.z), "=f"(x.w) : "r"(rows_at + (n * D + c) * 4));
+        float top = z;
+        for (int w = 1; w < parts; w *= 2) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, w));
+        const bool seen = z != -INFINITY;                              // (what a part that saw no key of the row left is not looked at)
+        const float a = seen ? fast_exp2(z - top) : 0.f;
+        float sum = a;
+        x = seen ? make_float4(a * x.x, a * x.y, a * x.z, a * x.w) : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int w = 1; w < parts; w *= 2) {
+            sum += __shfl_xor_sync(0xffffffffu, sum, w);
+            x.x += __shfl_xor_sync(0xffffffffu, x.x, w);
+            x.y += __shfl_xor_sync(0xffffffffu, x.y, w);
+            x.z += __shfl_xor_sync(0xffffffffu, x.z, w);
+            x.w += __shfl_xor_sync(0xffffffffu, x.w, w);
+        }
+        if (part != 0 || i >= rows * (D / 4)) continue;
+        const bool nan = sum != sum;
+        const float inv = nan ? NAN : sum > 0.f ? 1.f / sum : 0.f;
+        const int64_t tok = (int64_t)unit.q_off + un.row0[0] + n % toks, head = un.head[0] + n / toks;
+        *reinterpret_cast<uint2*>(p.out + tok * p.o_token_stride + head * p.o_head_stride + c) =
+            make_uint2(pack_bf16x2(x.x * inv, x.y * inv), pack_bf16x2(x.z * inv, x.w * inv));
+        if (p.lse && c == 0) p.lse[tok * p.num_q_heads + head] = sum > 0.f && !nan ? (top + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+    }
+    cluster_barrier();                         // (nobody leaves while another one reads its shared memory)
+}
+
+template <class Kernel, class... Args>
+static cudaError_t launch_kernel(Kernel kernel, bool (&attr_set)[64], int num_ctas, int threads, int smem, int cluster, cudaStream_t stream, Args... args) {
     int dev = 0;
     cudaGetDevice(&dev);
     if (dev >= 0 && dev < 64 && !attr_set[dev]) {
-        cudaError_t e = cudaFuncSetAttribute(wpp_kv8_few_kernel<D, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, Smem<D, NT>::kBytes);
+        cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        if (e == cudaSuccess && cluster > 0) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
         if (e != cudaSuccess) return e;
         attr_set[dev] = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)num_ctas);
-    cfg.blockDim = dim3(32 * kWarps);
-    cfg.dynamicSmemBytes = Smem<D, NT>::kBytes;
+    cfg.blockDim = dim3((unsigned)threads);
+    cfg.dynamicSmemBytes = (size_t)smem;
     cfg.stream = stream;
-    cudaLaunchAttribute overlap;
-    overlap.id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    overlap.val.programmaticStreamSerializationAllowed = 1;
-    cfg.attrs = &overlap;
-    cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, wpp_kv8_few_kernel<D, NT>, p);
+    cudaLaunchAttribute attrs[2];
+    attrs[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attrs[0].val.programmaticStreamSerializationAllowed = 1;
+    attrs[1].id = cudaLaunchAttributeClusterDimension;
+    attrs[1].val.clusterDim.x = (unsigned)cluster;
+    attrs[1].val.clusterDim.y = attrs[1].val.clusterDim.z = 1;
+    cfg.attrs = attrs;
+    cfg.numAttrs = cluster > 0 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
-template <int D>
-static cudaError_t launch(const Kv4AttnParams& p, int num_ctas, int max_rows, cudaStream_t stream) {
-    return max_rows <= 8 ? launch_nt<D, 1>(p, num_ctas, stream) : launch_nt<D, 2>(p, num_ctas, stream);
+template <int D, int NT>
+static cudaError_t launch_nt(const Kv4AttnParams& p, int num_ctas, int log_parts, cudaStream_t stream) {
+    static bool attr_set[64] = {}, attr_set_cluster[64] = {};
+    if (log_parts > 0)
+        return launch_kernel(wpp_kv8_cluster_kernel<D, NT>, attr_set_cluster, num_ctas, 32 * kWarps, Smem<D, NT, true>::kBytes,
+                             1 << log_parts, stream, p, log_parts);
+    return launch_kernel(wpp_kv8_few_kernel<D, NT>, attr_set, num_ctas, 32 * kWarps, Smem<D, NT, false>::kBytes, 0, stream, p);
 }
 
 }  // namespace kv8few
 }  // namespace wpp
 
-extern "C" int wpp_launch_kv8_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, void* stream) {
-    return (int)(head_dim == 128 ? wpp::kv8few::launch<128>(*p, num_ctas, max_rows, (cudaStream_t)stream)
-                                 : wpp::kv8few::launch<64>(*p, num_ctas, max_rows, (cudaStream_t)stream));
+// log_parts > 0: the units are parts of blocks, 2^log_parts of each, that clusters of as many CTAs join
+extern "C" int wpp_launch_kv8_few(int head_dim, const wpp::Kv4AttnParams* p, int num_ctas, int max_rows, int log_parts, void* stream) {
+    using namespace wpp::kv8few;
+    const cudaStream_t s = (cudaStream_t)stream;
+    if (head_dim == 128) return (int)(max_rows <= 8 ? launch_nt<128, 1>(*p, num_ctas, log_parts, s) : launch_nt<128, 2>(*p, num_ctas, log_parts, s));
+    return (int)(max_rows <= 8 ? launch_nt<64, 1>(*p, num_ctas, log_parts, s) : launch_nt<64, 2>(*p, num_ctas, log_parts, s));
 }

@@ -26,8 +26,9 @@ struct WppPlanHeader {
     int32_t shape;                  // 1: two-half CTAs, one per SM; 2: single-half CTAs, two per SM (work item = half a unit); 3: 4-bit cache
     int32_t nonempty_halves;        // (8-bit cache: pages that the append touches, WppTouched behind the combine records)
     int32_t max_combine_rows;       // most rows of a combine record (sizes the combine pass's grid)
-    int32_t deal_items;             // small shape: its items are dealt out to the CTAs, without the workspace's counter; shape 3: the units of
-                                    // the kernel for few rows are not, but taken by the CTAs from a counter in the workspace's header
+    int32_t deal_items;             // small shape: its items are dealt out to the CTAs, without the workspace's counter; 8-bit cache: 1: the units of
+                                    // the kernel for few rows are not, but taken by the CTAs from a counter in the workspace's header;
+                                    // n > 1: every 2^(n - 1) of them are the parts of a block, which a cluster joins
     int32_t num_few_units;          // 4-bit cache: the first of the units are of the kernel for few rows ...
     int32_t max_few_rows;           // ... which has so many rows at most; ...
     int32_t num_few_ctas;

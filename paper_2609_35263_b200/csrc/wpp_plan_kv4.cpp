@@ -25,6 +25,19 @@ constexpr int64_t kFewWalks = 4;
 // 59, 65; 1 x 64 over 1,024 (8/2 of 64) 18, 22 and 9, 9.7; 12 x 1..300 over 0..700 (8/2 of 64) tiles 24, 24, both 34, 30.
 constexpr double kFewStart = 3.0, kFewStep = 1.45, kTileStart = 7.0, kTileStep1 = 2.7, kTileStep2 = 3.2, kCombine = 4.0;
 constexpr int64_t kFewShort = 4;
+// A wave of so few blocks that the SMs have several CTAs for each: clusters of 2^n CTAs that join a block's parts, n returned, or 0.
+// kMostClusters: of 2, 4, 8 and 16 CTAs, two to an SM, that 148 SMs hold at once.  Estimated as above: a start, a time per key step of the
+// longest part, and a join in the place of a combine pass.
+constexpr int64_t kMostClusters[4] = {148, 71, 33, 14};
+constexpr double kClusterStart = 5.0, kClusterStep = 1.2;
+static int cluster_parts(int64_t blocks, int64_t all_steps, int64_t longest, int64_t max_ctas) {
+    int n = 0;
+    while (n < 4 && blocks * 148 <= kMostClusters[n] * max_ctas) ++n;
+    if (n == 0 || blocks == 0 || longest < kFewShort) return 0;
+    const double part = (double)((longest + (1 << n) - 1) >> n), share = (double)all_steps / (double)(kFewCtas * max_ctas);
+    const double alone = kClusterStart + kClusterStep * part, with_pass = kFewStart + kCombine + kFewStep * std::max(share + kUnitSteps, 5.0);
+    return alone < with_pass ? n : 0;
+}
 // Tiles: fewest key steps of a part, and rounds of tiles up to which the longest come first.  The parts of a wave are of equal length,
 // whatever the tiles': against equal numbers of parts, us, 4 x 76..106 tokens over 0..18,257 (32/8) 193 -> 104, 4 x 47..191 over 0..31,067
 // (64/8) 435 -> 332; cut for any win, 2 x 183..211 over 0..1,065 (32/8) would take 28 where whole tiles take 25.
@@ -197,7 +210,7 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
     const int32_t heads = few_heads(G), toks = few_tokens(G);
     const int64_t walks = few_walks(d, o, prefix_lens, chunk_lens);
     // The CTAs take equal shares of the blocks' key steps, in order: a block is cut where a share ends.
-    int64_t n_base = 0, all_steps = 0;
+    int64_t n_base = 0, all_steps = 0, longest = 0;
     int32_t max_rows = 0;
     for (int i = 0; i < R; ++i) {
         if (!is_few(d, chunk_lens[i], walks)) continue;
@@ -205,6 +218,7 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
         for (int64_t r0 = 0; r0 < chunk_lens[i]; r0 += toks) {
             const int32_t rows = (int32_t)std::min<int64_t>(toks, chunk_lens[i] - r0);
             all_steps += steps_for(prefix_lens[i] + r0 + rows) * (int64_t)((G + heads - 1) / heads) * Hkv;
+            longest = std::max<int64_t>(longest, steps_for(prefix_lens[i] + r0 + rows));
             max_rows = std::max(max_rows, rows * heads);
         }
     }
@@ -221,13 +235,14 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
         left -= n + kUnitSteps;
         return at + n;
     };
-    const bool deal = may_deal && d->dtype == WPP_KV8 && o->force_kv_splits < 1 && share >= kDealSteps;
+    const int log_parts = may_deal && d->dtype == WPP_KV8 && o->force_kv_splits < 1 ? cluster_parts(n_base, all_steps, longest, o->max_ctas) : 0;
+    const bool deal = may_deal && log_parts == 0 && d->dtype == WPP_KV8 && o->force_kv_splits < 1 && share >= kDealSteps;
     // (rows of a unit in a slot; the 4-bit cache's plans have always taken the most that there can be)
     const int32_t slot_rows = d->dtype == WPP_KV8 && max_rows <= WPP_FEW_ROWS / 2 ? WPP_FEW_ROWS / 2 : WPP_FEW_ROWS;
     const int32_t long_part = (int32_t)((double)share * kLongPart), short_part = std::max((int32_t)((double)share * kShortPart), (int32_t)kLeastSteps);
     // Blocks too short to be cut may leave much of every share: it grows until the CTAs are enough (5 x 9..43 tokens, 40/8 heads: 320 blocks
     // of a step on 296 CTAs, of which the last had 25, 274 us | 14.5)
-    for (int64_t ctas = most_ctas + 1; o->force_kv_splits < 1 && !deal && ctas > most_ctas;) {
+    for (int64_t ctas = most_ctas + 1; o->force_kv_splits < 1 && !deal && log_parts == 0 && ctas > most_ctas;) {
         int64_t left = share;
         ctas = 1;
         bool next = false;
@@ -270,6 +285,8 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
                     if (o->force_kv_splits >= 1) {
                         const int32_t n = std::min(o->force_kv_splits, steps);
                         for (int32_t q = 1; q <= n; ++q) cuts.push_back((int32_t)((int64_t)steps * q / n));
+                    } else if (log_parts > 0) {
+                        for (int32_t q = 1; q <= 1 << log_parts; ++q) cuts.push_back((int32_t)((int64_t)steps * q >> log_parts));
                     } else if (deal) {
                         const int32_t longs = steps <= long_part ? 0 : (int32_t)((double)steps * kLongPart / long_part);
                         for (int32_t q = 0; q < longs; ++q) cuts.push_back(cuts.back() + long_part);
@@ -294,7 +311,7 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
                     u.head[0] = kvh * G + h;
                     u.split_slot = -1;
                     u.pack = 1;
-                    if (parts > 1) {
+                    if (parts > 1 && log_parts == 0) {
                         if (parts > slot_parts || slot_row + slot_rows > 2 * WPP_HALF_M) {
                             slot0 = slots;
                             slot_parts = parts;
@@ -310,7 +327,7 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
                     for (int32_t q = 0; q < parts; ++q) {
                         u.kv_begin = cuts[(size_t)q];
                         u.kv_end = cuts[(size_t)q + 1];
-                        if (parts > 1) u.split_slot = slot0 + q;
+                        if (parts > 1 && log_parts == 0) u.split_slot = slot0 + q;
                         u.cost = u.kv_end - u.kv_begin;
                         us[n_units++] = u;
                         key_steps += u.cost;
@@ -328,6 +345,7 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
         std::stable_sort(us, us + n_few, [](const WppUnit& a, const WppUnit& b) { return a.cost > b.cost; });
         first.assign((size_t)std::min<int64_t>(most_ctas, n_few), 0);
     }
+    if (log_parts > 0) first.assign((size_t)n_few, 0);
 
     // ---- tiles
     struct Tile { WppUnit u; int32_t steps; };
@@ -422,7 +440,7 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
     hd.num_units = (int32_t)n_units;
     hd.num_few_units = (int32_t)n_few;
     hd.num_few_ctas = few_ctas;
-    hd.deal_items = deal && n_few > 0;
+    hd.deal_items = n_few == 0 ? 0 : log_parts > 0 ? log_parts + 1 : deal;
     hd.max_few_rows = max_rows;
     hd.num_combine = (int32_t)combines.size();
     hd.num_split_slots = slots;

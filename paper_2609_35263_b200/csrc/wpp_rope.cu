@@ -18,7 +18,7 @@
 
 namespace wpp {
 
-constexpr int kRopeWarps = 8, kRopeAhead = 4;      // of a CTA; passes whose loads are out at a time
+constexpr int kRopeWarps = 2, kRopeAhead = 4;      // of a CTA; passes whose loads are out at a time
 constexpr int64_t kRopeWarpsPerSm = 32;            // as many before a warp takes more than one pass
 
 __device__ __forceinline__ void rotate(uint32_t& wa, uint32_t& wb, const float (&c)[2], const float (&s)[2]) {
@@ -33,7 +33,7 @@ __device__ __forceinline__ void rotate_neighbours(uint32_t& w, float c, float s)
 
 // kWrite: keys and values go to their slots of the cache
 template <int D, bool kNeighbours, bool kWrite>
-__global__ void __launch_bounds__(32 * kRopeWarps) wpp_rope_kernel(const RopeParams p) {
+__global__ void __launch_bounds__(32 * kRopeWarps, 24 / kRopeWarps) wpp_rope_kernel(const RopeParams p) {
     constexpr int kLanes = D / 16, kHeads = 32 / kLanes;       // of a head; of a warp at a time
     if (!p.few) grid_launch_dependents();
     grid_dependency_wait();
@@ -148,7 +148,7 @@ static cudaError_t launch_rope(const RopeParams& in, int neighbours, int write, 
     p.units_per_token = (int32_t)((passes + p.passes - 1) / p.passes);
     const int64_t blocks = (p.total_tokens * p.units_per_token + kRopeWarps - 1) / kRopeWarps;
     if (blocks > 0x7fffffff) return cudaErrorInvalidValue;
-    p.few = blocks <= 4 * (int64_t)num_sms;      // (see wpp_launch_kv4_append)
+    p.few = blocks * kRopeWarps <= 24 * (int64_t)num_sms;      // (see wpp_launch_kv4_append)
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)blocks);
     cfg.blockDim = dim3(32 * kRopeWarps);

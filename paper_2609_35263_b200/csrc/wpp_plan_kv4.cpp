@@ -2,6 +2,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <cstring>
+#include <queue>
 #include <utility>
 #include <vector>
 
@@ -115,6 +116,40 @@ static int64_t tile_part_steps(const std::vector<std::pair<int64_t, int64_t>>& t
     return longest - lo >= kTileLeastWin && (n < ctas || parts <= slots) ? lo : longest;
 }
 
+// 8-bit cache: the last of a wave's tiles (the shortest) are cut where that ends the wave sooner, by a run of the CTAs through its tiles: 1 x
+// 2,048 behind 32,768 (64/8 heads of 128) has 512 tiles for 148 CTAs, and takes 3.5 rounds with the last 68 in halves.  How many, and
+// into how many parts; in key steps, a tile takes kTileSteps besides its own, a part one more, and the combine pass kPassSteps.
+constexpr double kTileSteps = 1.5, kPassSteps = 2.0;
+constexpr int64_t kMostTailParts = 4;
+static double tiles_end(const std::vector<int32_t>& steps, int64_t whole, int64_t parts, int64_t ctas) {
+    std::priority_queue<double, std::vector<double>, std::greater<double>> free_at;
+    for (int64_t c = 0; c < ctas; ++c) free_at.push(0.0);
+    double last = 0.0;
+    auto take = [&](double cost) {
+        const double t = free_at.top() + cost;
+        free_at.pop();
+        free_at.push(t);
+        last = std::max(last, t);
+    };
+    for (int64_t i = 0; i < (int64_t)steps.size(); ++i) {
+        const int64_t n = i < whole ? 1 : std::min<int64_t>(parts, steps[(size_t)i]);
+        for (int64_t q = 0; q < n; ++q) take((double)steps[(size_t)i] / (double)n + kTileSteps + (n > 1));
+    }
+    return last + (whole < (int64_t)steps.size() ? kPassSteps : 0.0);
+}
+static void cut_tail(const std::vector<int32_t>& steps, int64_t ctas, int64_t slots, int64_t* whole, int64_t* parts) {
+    const int64_t n = (int64_t)steps.size();
+    *whole = n;
+    *parts = 1;
+    double best = 0.97 * tiles_end(steps, n, 1, ctas);
+    for (int64_t k = 2; k <= kMostTailParts; ++k)
+        for (int64_t tail : {n % ctas, n % ctas + ctas}) {
+            if (tail == 0 || tail > n || tail * k > slots) continue;
+            const double t = tiles_end(steps, n - tail, k, ctas);
+            if (t < best) { best = t; *whole = n - tail; *parts = k; }
+        }
+}
+
 static int64_t scratch_slots(const wpp_batch_desc* d) {
     return (int64_t)((wpp_static_scratch_bytes() - WPP_WS_HEADER_BYTES) / (2 * WPP_HALF_M * (d->head_dim + 1) * sizeof(float)));
 }
@@ -195,7 +230,7 @@ size_t wpp_kv4_plan_bytes(const wpp_batch_desc* d, const wpp_plan_opts* o, int64
     n += sizeof(WppUnit) * (size_t)units + align_up(sizeof(int32_t) * ((size_t)std::max(units, kFewCtas * (int64_t)o->max_ctas) + 1), 16);
     n += sizeof(WppCombine) * (size_t)(T * d->num_q_heads / t + (int64_t)d->num_requests * d->num_q_heads);
     const int64_t tiles = (T / WPP_HALF_M + d->num_requests) * d->num_q_heads;
-    n += sizeof(WppUnit) * (size_t)(o->force_kv_splits >= 2 ? tiles * o->force_kv_splits : tiles + (int64_t)o->max_ctas);
+    n += sizeof(WppUnit) * (size_t)(o->force_kv_splits >= 2 ? tiles * o->force_kv_splits : tiles + (d->dtype == WPP_KV8 ? 2 * kMostTailParts : 1) * (int64_t)o->max_ctas);
     n += sizeof(WppCombine) * (size_t)tiles;
     if (d->dtype == WPP_KV8) n += sizeof(WppTouched) * (size_t)(T / d->page_size + 2 * (int64_t)d->num_requests);
     return align_up(n, 256);
@@ -385,8 +420,15 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
     std::vector<std::pair<int64_t, int64_t>> counted;
     for (const Tile& t : tiles) counted.emplace_back(1, t.steps);
     const int64_t part_steps = tile_part_steps(counted, o->max_ctas, scratch_slots(d) - slots);
+    int64_t whole = (int64_t)tiles.size(), tail_parts = 1;
+    if (d->dtype == WPP_KV8 && o->force_kv_splits < 1 && whole > o->max_ctas && whole <= kTileOrderRounds * o->max_ctas && part_steps >= tiles[0].steps) {
+        std::vector<int32_t> steps;
+        for (const Tile& t : tiles) steps.push_back(t.steps);
+        cut_tail(steps, o->max_ctas, scratch_slots(d) - slots, &whole, &tail_parts);
+    }
     for (Tile& t : tiles) {
-        const int32_t parts = std::max(1, o->force_kv_splits >= 1 ? std::min(o->force_kv_splits, t.steps)
+        const int32_t parts = &t - tiles.data() >= whole ? (int32_t)std::min<int64_t>(tail_parts, t.steps)
+                              : std::max(1, o->force_kv_splits >= 1 ? std::min(o->force_kv_splits, t.steps)
                                                                   : (int32_t)((t.steps + part_steps - 1) / part_steps));
         if (n_units + parts > unit_cap) return WPP_ERR_PLAN_MISMATCH;
         if (parts > 1)

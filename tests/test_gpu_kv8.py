@@ -435,3 +435,56 @@ def test_value_pages_of_unequal_sizes(kind, d, Hq, C, n):
         out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
         assert int(g["status"].item()) == 0
         w.check(out, lse, ref)
+
+
+# ------------------------------------------------------------------------------------------------ how units reach the CTAs
+DEALS = {"dealt": (([3000, 500, 2000, 10, 7000], [1, 2, 1, 1, 1], 8, 4), 2), "dealt, with tiles": (([9000, 9000, 600, 4000, 8000], [1, 1, 400, 1, 1], 8, 4), 2),
+         "cluster of 16": (([8191], [1], 8, 2), 0), "cluster of 8": (([5000, 700, 3], [1, 3, 2], 16, 8), 0), "cluster of 4": (([2000] * 8, [1] * 8, 16, 8), 0),
+         "cluster of 2": (([1200, 600, 64] * 8, [1] * 24, 6, 6), 0), "cluster, two row blocks": (([3000], [3], 12, 1), 0), "tail cut": (([3000, 3000], [300, 300], 4, 1), 4)}
+
+
+@pytest.mark.parametrize("d,B", [(128, 32), (64, 16)])
+@pytest.mark.parametrize("name", list(DEALS))
+def test_parts_that_are_dealt_out_joined_in_clusters_or_cut_from_the_last_tiles(name, d, B):
+    """Every way a plan has of spreading a wave, with a workspace full of ones, twice in a row, replayed, and with a request that is refused."""
+    (P, C, Hq, Hkv), ctas = DEALS[name]
+    w = Wave(P, C, Hq, Hkv, d, B, seed=len(P) + d)
+    g, plan = w.device(), w.plan(wpp.PlanOpts(0, 0, 0, ctas))
+    ref = w.reference()
+    ws = torch.full((int(plan.info.workspace_bytes),), 255, dtype=torch.uint8, device="cuda")
+    out, lse = w.attend(g, plan, workspace=ws)
+    again, sums = w.attend(g, plan, workspace=ws)
+    assert int(g["status"].item()) == 0 and torch.equal(out, again) and torch.equal(lse, sums)
+    w.check(out, lse, ref)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        wpp.wpp_prefill_attention_varlen(ctx(), w.desc(), g["q"], again, sums, g["k"], g["v"], g["table"], g["P"], g["C"], plan, workspace=ws, status=g["status"])
+    for _ in range(3):
+        again.zero_()
+        graph.replay()
+    assert torch.equal(out, again) and torch.equal(lse, sums)
+    g["P"][0] += 1
+    again.fill_(7.0)
+    graph.replay()
+    rows = slice(C[0], None)
+    assert int(g["status"].item()) == 6 and torch.equal(out[rows], again[rows])
+
+
+def test_a_nan_score_in_a_part_that_a_cluster_joins():
+    w = Wave([8191], [1], 8, 2, 128, 64, seed=3)
+    w.k_pool[w.table[0, 50], 1, 5] = 0x7F
+    w.v_pool[w.table[0, 90], 0, 64 * 128 - 1] = 0xFF
+    g = w.device()
+    out, lse = w.attend(g)
+    o = out.float().cpu().numpy()
+    assert np.isnan(o[0, 4:]).all() and np.isnan(o[0, :4, 127]).all() and not np.isnan(o[0, :4, :127]).any()
+    assert torch.isinf(lse[0, 4:]).all() and torch.isfinite(lse[0, :4]).all()
+
+
+def test_a_long_cache():
+    """131,072 keys of one request; values that the sums' order would show in, were they not added up in fp32."""
+    w = Wave([131071], [1], 8, 1, 64, 128, seed=4)
+    g = w.device()
+    for opts in (None, wpp.PlanOpts(0, 0, 0, 0, 0, 1), wpp.PlanOpts(0, 0, 0, 8)):
+        out, lse = w.attend(g, opts=opts)
+        w.check(out, lse, w.reference())

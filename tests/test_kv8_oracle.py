@@ -98,10 +98,57 @@ def test_validate_batch_wants_written_pages_to_be_one_request_s():
 
 @pytest.mark.parametrize("shape", [0, 1, 2])
 @pytest.mark.parametrize("Hq,Hkv,d,B", [(8, 1, 128, 64), (10, 2, 64, 16), (64, 8, 128, 64)])
-def test_plan_covers_every_key_of_every_row(shape, Hq, Hkv, d, B):
+def test_plans_are_deterministic_and_count_their_work(shape, Hq, Hkv, d, B):
     P, C = [0, 700, 20_000, 5], [1, 300, 1, 0]
     desc = wpp.make_desc(4, Hq, Hkv, d, B, 1300, 5000, dtype=wpp.WPP_KV8)
     plan = wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, 0, 0, 0, shape), pin=False)
     assert plan.info.shape == 3 and plan.info.total_new_tokens == 302
     assert plan.info.flops == 4 * d * Hq * sum(c * p + c * (c + 1) // 2 for p, c in zip(P, C))
     assert plan.host_bytes() == wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, 0, 0, 0, shape), pin=False).host_bytes()
+
+
+def _units(plan):
+    """(units as dicts, how many are of the kernel for few rows, how those are handed out, touched pages) of a host plan."""
+    import struct
+    raw = plan.host_bytes()
+    f = struct.unpack_from("<IIQ" + "i" * 8 + "qqq" + "QQ" + "IIII" + "iiiiiii" + "I", raw, 0)
+    num_units, num_combine, off_units, off_combine = f[5], f[6], f[18], f[19]
+    touched, deal, few = f[21], f[23], f[24]
+    u = np.frombuffer(raw, np.int32, num_units * 12, off_units).reshape(num_units, 12)
+    pages = np.frombuffer(raw, np.int32, 2 * touched, off_combine + 32 * num_combine).reshape(-1, 2)
+    return u, few, deal, pages
+
+
+WAVES = {"dealt": (([3000, 500, 2000, 10, 7000], [1, 2, 1, 1, 1], 8, 4), 2, 1), "cluster of 16": (([8191], [1], 8, 2), 0, 5), "cluster of 8": (([5000, 700, 3], [1, 3, 2], 16, 8), 0, 4),
+         "cluster of 4": (([2000] * 8, [1] * 8, 16, 8), 0, 3), "cluster of 2": (([1200, 600, 64] * 8, [1] * 24, 6, 6), 0, 2), "tail cut": (([3000, 3000], [300, 300], 4, 1), 4, 0),
+         "dealt, with tiles": (([9000, 9000, 600, 4000, 8000], [1, 1, 400, 1, 1], 8, 4), 2, 1)}
+
+
+@pytest.mark.parametrize("name", list(WAVES))
+def test_plan_covers_every_key_of_every_row_once(name):
+    (P, C, Hq, Hkv), ctas, deal = WAVES[name]
+    d, B, G = 128, 32, Hq // Hkv
+    desc = wpp.make_desc(len(P), Hq, Hkv, d, B, 400, 5000, dtype=wpp.WPP_KV8)
+    plan = wpp.wpp_plan_tiles(None, desc, P, C, opts=wpp.PlanOpts(0, 0, 0, ctas), pin=False)
+    units, few, how, pages = _units(plan)
+    assert how == deal and (name != "tail cut" or (plan.info.num_split_tiles > 0 and few == 0))
+    steps = {}
+    for k, u in enumerate(units):
+        i, b, e, slot, row0, row1, rows0, rows1, head0, head1, _, pack = (int(x) for x in u)
+        blocks = [(row0, rows0, range(head0, head0 + rows1))] if k < few else \
+            [(r, n, range(h, h + min(pack, G))) for r, n, h in ((row0, rows0, head0), (row1, rows1, head1)) if n > 0]
+        for r, n, heads in blocks:
+            for t in range(r, r + n):
+                for h in heads:
+                    steps.setdefault((i, t, h), []).append((b, e))
+    for i in range(len(P)):
+        for t in range(C[i]):
+            for h in range(Hq):
+                at = 0
+                for b, e in sorted(steps.pop((i, t, h))):
+                    assert b == at or b == e
+                    at = max(at, e)
+                assert at * 128 >= P[i] + t + 1
+    assert not steps
+    assert pages.tolist() == [[i, b] for i in range(len(P)) if C[i] for b in range(P[i] // B, -(-(P[i] + C[i]) // B))]
+    assert plan.info.workspace_bytes <= wpp.wpp_static_scratch_bytes()

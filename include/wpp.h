@@ -239,10 +239,13 @@ int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* k_
  * WPP_KV4: K_j[g] and V_j[g] are the rows that codes, least and scale stand for.  Slots >= P_i + C_i never influence the result, and
  * a NaN row only the query rows that see it (their outputs are NaN; of a row of K their lse is -infinity).  One or two kernels,
  * one more iff the plan has split tiles, and a memset of 256 bytes iff it has more tiles than CTAs.
- * WPP_KV8: K_j[g] and V_j[g] are scale * code, probabilities (times V's scales, relative to the row's largest) are rounded to f16 before the
- * PV product, the scores have fp32's error.  Slots >= P_i + C_i never influence the result, and a NaN code only the query rows that
- * see its key: of K all their outputs are NaN and their lse -infinity, of V the output's element of the same place is NaN.  Launches as
- * for WPP_KV4. */
+ * WPP_KV8: K_j[g] and V_j[g] are scale * code.  Rounded are, besides fp32's own errors: elements of q below 2^-9 of their row's largest, by up
+ * to 2^-18 of it (blocks of at most 16 rows: below 2^-24); and the probabilities before the PV product, to f16, so by 2^-11 of themselves or by
+ * 2^-32 of the row's largest (blocks of at most 16 rows: 2^-24, and rounded with V's scales in them, relative to the largest one so far) -
+ * to bf16, 2^-8, in steps of 128 keys with a page whose scale of V is outside 2^-12 to 2^4 of that of the tile's first page.
+ * Slots >= P_i + C_i never influence the result, and a NaN code only the query rows that see its key: of K all their outputs are NaN and their
+ * lse -infinity, of V the output's element of the same place is NaN.  One or two kernels, one more iff the plan has split tiles, and a
+ * memset of 256 bytes iff it has more tiles than CTAs or uneven parts of single tokens' keys, which CTAs take as they become free. */
 int wpp_prefill_attention_varlen(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* q, void* out,
                                  float* lse_or_null, const void* k_cache, const void* v_cache,
                                  const int32_t* block_tables, const int32_t* prefix_lens,
@@ -289,8 +292,8 @@ size_t wpp_static_scratch_bytes(void);
  *   prefix_lens, chunk_lens : device int32 [R].
  *   free_pages   : device int32 [num_free], read from cursor[0] on.
  *   cursor       : device int32 [1], entries of free_pages that are taken.
- *   cursor_out   : device int32 [2]: [0] the same afterwards (at most num_free), [1] has to be 0 and is 0 again afterwards.  May be
- *                  cursor: then a captured call takes other pages at each replay.  Calls that share it are serialised by the caller.
+ *   cursor_out   : device int32 [2]: [0] the same afterwards (at most num_free), [1] is 0 afterwards.  May be cursor, whose [1] has to be 0
+ *                  then: a captured call takes other pages at each replay.  Calls that share it are serialised by the caller.
  *   block_tables : device int32 [R][max_blocks_per_req]; columns behind the last one needed are left as they were.
  *   row_offsets  : device int64 [R+1], out, exclusive scan of chunk_lens.
  *   positions, slots : device int32 and int64 [max_tokens], out, either may be NULL; rows behind the last token are 0 and -1.
@@ -350,8 +353,8 @@ int wpp_rope(const wpp_ctx* ctx, const wpp_rope_desc* desc, const void* q, void*
  * instead of k_out: what wpp_rope and then wpp_kv_append do, in one kernel and without a plan.
  *   batch    : page size, heads, number of pages and the pools' strides count here.
  *   desc     : num_k_heads of `batch`; num_q_heads of `batch`, or 0 (q and q_out are not used then).
- *   slots    : device int64 [T], page * page_size + slot of the page (as wpp_assign_pages leaves them); -1: the token's K and V are not
- *              written.  Any other outside [0, num_pages * page_size) sets *status_dev = WPP_ERR_BOUNDS (if it was 0) and counts as -1. */
+ *   slots    : device int64 [T], page * page_size + slot of the page (as wpp_assign_pages leaves them), none twice; -1: the token's K and V
+ *              are not written.  Any other outside [0, num_pages * page_size) sets *status_dev = WPP_ERR_BOUNDS (if it was 0) and counts as -1. */
 int wpp_rope_append(const wpp_ctx* ctx, const wpp_batch_desc* batch, const wpp_rope_desc* desc, const void* q, void* q_out,
                     const void* k_new, const void* v_new, void* k_cache, void* v_cache, const uint64_t* turns, const int32_t* positions,
                     const int64_t* slots, int32_t* status_dev, void* cuda_stream);

@@ -361,7 +361,7 @@ def wpp_assign_pages(ctx: Context, desc: BatchDesc, prefix_lens, chunk_lens, fre
     offsets, and every new token's position and slot.
 
     prefix_lens, chunk_lens: cuda int32 [R]; free_pages: cuda int32, read from entry cursor[0] on; cursor: cuda int32 [2], the number of
-    entries that are taken and a zero, replaced by the number afterwards unless cursor_out (int32 [2]) is given; block_tables: cuda
+    entries that are taken and a zero, replaced by the number afterwards unless cursor_out (int32 [2], whatever it holds) is given; block_tables: cuda
     int32 [R, max_blocks], whose rows hold the pages of the prefixes; row_offsets: cuda int64 [R+1]; positions: cuda int32 and
     slots: cuda int64 of as many rows as the wave may have tokens (rows behind the last token become 0 and -1)."""
     st = _call.pages(ctx.handle.value, ctx.device, desc, prefix_lens, chunk_lens, free_pages, cursor, cursor if cursor_out is None else cursor_out,

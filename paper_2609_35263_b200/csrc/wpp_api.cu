@@ -647,6 +647,7 @@ extern "C" int wpp_assign_pages(const wpp_ctx* ctx, const wpp_batch_desc* desc, 
     wpp_batch_desc d;
     if (int rc = wpp_resolve_desc(desc, &d)) return rc;
     if (num_free < 0 || max_tokens < 0 || !cursor || !cursor_out || !row_offsets) return WPP_ERR_INVALID_ARG;
+    if (cursor_out + 1 == cursor) return WPP_ERR_INVALID_ARG;      // (its zero would stand where the number is read)
     if (d.num_requests > wpp::kPagesMostRequests) return WPP_ERR_UNSUPPORTED;
     if (d.num_requests > 0 && (!prefix_lens || !chunk_lens)) return WPP_ERR_INVALID_ARG;
     if (d.num_requests > 0 && d.max_blocks_per_req > 0 && !block_tables) return WPP_ERR_INVALID_ARG;

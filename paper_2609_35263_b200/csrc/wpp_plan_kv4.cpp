@@ -44,7 +44,8 @@ static int cluster_parts(int64_t blocks, int64_t all_steps, int64_t longest, int
 // whatever the tiles': against equal numbers of parts, us, 4 x 76..106 tokens over 0..18,257 (32/8) 193 -> 104, 4 x 47..191 over 0..31,067
 // (64/8) 435 -> 332; cut for any win, 2 x 183..211 over 0..1,065 (32/8) would take 28 where whole tiles take 25.
 constexpr int64_t kTileLeastSteps = 4, kTileLeastWin = 3;
-constexpr int64_t kTileOrderRounds = 16;
+constexpr int64_t kTileOrderRounds = 16;            // (4-bit cache; 8-bit, stream order | longest first, us: 16 x 256..2,048 over 0..8,192 (32/8) 1,810 | 1,763, 64 x
+                                                    // 100..4,000 over 0..1,000 4,670 | 4,490, 128 x 500..2,000 (8/2 of 64) 724 | 562)
 
 // 8-bit cache, few rows.  SMs do not get equal shares of the memory's rate: with equal shares of 64 x 1 over 255..16,383 (64/8 heads of 128) the
 // SMs are done after 0.69 to 1 of the last one's time.  Where a share is long enough, blocks are cut into long parts, about one for each
@@ -411,7 +412,7 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
             }
         }
     }
-    if ((int64_t)tiles.size() <= kTileOrderRounds * o->max_ctas)
+    if (d->dtype == WPP_KV8 || (int64_t)tiles.size() <= kTileOrderRounds * o->max_ctas)
         std::stable_sort(tiles.begin(), tiles.end(), [](const Tile& a, const Tile& b) { return a.steps > b.steps; });
     std::vector<std::pair<int64_t, int64_t>> counted;
     for (const Tile& t : tiles) counted.emplace_back(1, t.steps);

@@ -9,8 +9,9 @@
 // between the search for the largest value and the conversion: the rows are read once.  The plan lists the touched pages, so that a CTA
 // knows its rows after one load, and asks for rows, lengths and page id at once.
 //
-// 36,864 tokens of 8 heads of 128 take 45 us, 5.3 TB/s (the bytes at the measured copy rate 37); with 8 warps in every CTA 48.  64 single
-// tokens 3.5 us, the launch and a chain of two loads; found by bisection over the requests instead of the plan's list, 7.2.
+// 36,864 tokens of 8 heads of 128 take 44 us, 5.4 TB/s (the bytes at the measured copy rate 37); with 8 warps in every CTA 3 more, with a record
+// that leads to the rows over the plan's offsets 2.  64 single tokens 3.2 us, the launch and a chain of two loads; over the plan's
+// offsets 3.6, found by bisection over the requests 7.2.
 #include <cuda_runtime.h>
 #include <stdint.h>
 
@@ -40,24 +41,23 @@ __global__ void __launch_bounds__(256) wpp_kv8_append_kernel(const Kv4AppendPara
     const uint32_t heads = (uint32_t)p.num_kv_heads, pair = blockIdx.x / heads, head = blockIdx.x - pair * heads;
     const bool is_v = (pair & 1u) != 0u;
     // ---- the rows, from the plan: slots [slot0, slot1) of the page; those before slot0 stand
-    const WppTouched at = reinterpret_cast<const WppTouched*>(plan + p.off_touched)[pair >> 1];
+    const int4 record = reinterpret_cast<const int4*>(plan + p.off_touched)[pair >> 1];
+    const WppTouched at = {record.x, record.y, record.z, (int16_t)record.w, (int16_t)(record.w >> 16)};
+    const int slot0 = at.slot0, slot1 = at.slot1, stand = slot0;
     const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets) + at.request;
-    const int q_off = q_offsets[0], C = q_offsets[1] - q_off, P = reinterpret_cast<const int32_t*>(plan + p.off_prefix)[at.request];
-    const int64_t first = (int64_t)at.block << page_shift;             // the page's first position
-    const int slot0 = (int)max((int64_t)P - first, (int64_t)0), slot1 = (int)min((int64_t)P + C - first, (int64_t)p.page_size), stand = slot0;
+    const int P = reinterpret_cast<const int32_t*>(plan + p.off_prefix)[at.request], C = q_offsets[1] - q_offsets[0];
     const int P_now = p.prefix_lens[at.request], C_now = p.chunk_lens[at.request];
     const int page = at.block < p.max_blocks ? p.block_tables[(int64_t)at.request * p.max_blocks + at.block] : -1;
 
     // ---- the warp's rows, and the largest finite value of the CTA's
     const int col = lane % kVecs, row = 16 * part + lane / kVecs;      // rows row, row + kApart, ..
     const __nv_bfloat16* src = (is_v ? p.v_new : p.k_new) + (int64_t)head * p.kvnew_head_stride + col * 8;
-    const int64_t token0 = (int64_t)q_off + first - P;                 // the token in slot 0, if it were one
     uint4 x[kTurns];
 #pragma unroll
     for (int i = 0; i < kTurns; ++i) {
         const int slot = row + i * kApart;
         x[i] = make_uint4(0, 0, 0, 0);
-        if (slot >= slot0 && slot < slot1) x[i] = *reinterpret_cast<const uint4*>(src + (token0 + slot) * p.kvnew_token_stride);
+        if (slot >= slot0 && slot < slot1) x[i] = *reinterpret_cast<const uint4*>(src + (int64_t)(at.token + slot) * p.kvnew_token_stride);
     }
     uint8_t* block = nullptr;
     if (P_now != P || C_now != C) {

@@ -58,9 +58,10 @@ struct WppUnit {
 // range is in steps of WPP_TILE_N keys too.  Where a cluster joins the parts, they have no slot.
 #define WPP_FEW_ROWS 16
 
-// A page that new rows of a request go to: number `block` of its table's row.
+// A page that new rows of a request go to: number `block` of its table's row.  Its slots [slot0, slot1) are new: tokens token + slot.
 struct WppTouched {
-    int32_t request, block;
+    int32_t request, block, token;
+    int16_t slot0, slot1;
 };
 
 // One half tile whose key range was split: partial slots [slot0, slot0+num_splits) merged in increasing order.

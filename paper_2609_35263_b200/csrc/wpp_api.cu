@@ -357,7 +357,7 @@ static int codes_append(const wpp_ctx* ctx, const wpp_batch_desc& d, const WppPl
     p.off_q_offsets = hd->off_q_offsets;
     p.off_prefix = hd->off_prefix;
     p.total_new_tokens = hd->total_new_tokens;
-    p.off_touched = (hd->off_combine + (uint32_t)(sizeof(WppCombine) * (size_t)hd->num_combine) + 15u) & ~15u;      // (as the planner has it)
+    p.off_touched = hd->off_combine + (uint32_t)(sizeof(WppCombine) * (size_t)hd->num_combine);
     p.num_touched = hd->nonempty_halves;
     const int e = (d.dtype == WPP_KV4 ? wpp_launch_kv4_append : wpp_launch_kv8_append)(d.head_dim, &p, ctx->sm_count, cuda_stream);
     if (e != 0) return cuda_fail(ctx, e);

@@ -9,8 +9,8 @@
 // between the search for the largest value and the conversion: the rows are read once.  The plan lists the touched pages, so that a CTA
 // knows its rows after one load, and asks for rows, lengths and page id at once.
 //
-// 36,864 tokens of 8 heads of 128 take 44 us, 5.4 TB/s (the bytes at the measured copy rate 37); with 8 warps in every CTA 3 more, with a record
-// that leads to the rows over the plan's offsets 2.  64 single tokens 3.2 us, the launch and a chain of two loads; over the plan's
+// 36,864 tokens of 8 heads of 128 take 44 to 45 us, 5.3 TB/s (the bytes at the measured copy rate 37); with 8 warps in every CTA 3 more, with a record
+// that leads to the rows over the plan's offsets 1.  64 single tokens 3.3 us, the launch and a chain of two loads; over the plan's
 // offsets 3.6, found by bisection over the requests 7.2.
 #include <cuda_runtime.h>
 #include <stdint.h>
@@ -41,9 +41,9 @@ __global__ void __launch_bounds__(256) wpp_kv8_append_kernel(const Kv4AppendPara
     const uint32_t heads = (uint32_t)p.num_kv_heads, pair = blockIdx.x / heads, head = blockIdx.x - pair * heads;
     const bool is_v = (pair & 1u) != 0u;
     // ---- the rows, from the plan: slots [slot0, slot1) of the page; those before slot0 stand
-    const int4 record = reinterpret_cast<const int4*>(plan + p.off_touched)[pair >> 1];
-    const WppTouched at = {record.x, record.y, record.z, (int16_t)record.w, (int16_t)(record.w >> 16)};
-    const int slot0 = at.slot0, slot1 = at.slot1, stand = slot0;
+    const int2 page_of = reinterpret_cast<const int2*>(plan + p.off_touched)[pair >> 1], rows = reinterpret_cast<const int2*>(plan + p.off_touched)[p.num_touched + (pair >> 1)];
+    const WppTouched at = {page_of.x, page_of.y};
+    const int slot0 = (int16_t)rows.y, slot1 = rows.y >> 16, stand = slot0;
     const int32_t* q_offsets = reinterpret_cast<const int32_t*>(plan + p.off_q_offsets) + at.request;
     const int P = reinterpret_cast<const int32_t*>(plan + p.off_prefix)[at.request], C = q_offsets[1] - q_offsets[0];
     const int P_now = p.prefix_lens[at.request], C_now = p.chunk_lens[at.request];
@@ -57,7 +57,7 @@ __global__ void __launch_bounds__(256) wpp_kv8_append_kernel(const Kv4AppendPara
     for (int i = 0; i < kTurns; ++i) {
         const int slot = row + i * kApart;
         x[i] = make_uint4(0, 0, 0, 0);
-        if (slot >= slot0 && slot < slot1) x[i] = *reinterpret_cast<const uint4*>(src + (int64_t)(at.token + slot) * p.kvnew_token_stride);
+        if (slot >= slot0 && slot < slot1) x[i] = *reinterpret_cast<const uint4*>(src + (int64_t)(rows.x + slot) * p.kvnew_token_stride);
     }
     uint8_t* block = nullptr;
     if (P_now != P || C_now != C) {

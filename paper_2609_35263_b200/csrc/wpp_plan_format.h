@@ -58,9 +58,13 @@ struct WppUnit {
 // range is in steps of WPP_TILE_N keys too.  Where a cluster joins the parts, they have no slot.
 #define WPP_FEW_ROWS 16
 
-// A page that new rows of a request go to: number `block` of its table's row.  Its slots [slot0, slot1) are new: tokens token + slot.
+// A page that new rows of a request go to: number `block` of its table's row.  And, in an array behind that of all pages, its new rows: slots
+// [slot0, slot1), tokens token + slot.
 struct WppTouched {
-    int32_t request, block, token;
+    int32_t request, block;
+};
+struct WppTouchedRows {
+    int32_t token;
     int16_t slot0, slot1;
 };
 

@@ -203,15 +203,17 @@ static int64_t few_walks(const wpp_batch_desc* d, const wpp_plan_opts* o, const 
     return best;
 }
 
-// The pages that the wave's new rows are in, at most T / page_size + 2 R; out may be null.
-static int64_t touched_pages(const wpp_batch_desc* d, const int32_t* prefix_lens, const int32_t* chunk_lens, WppTouched* out) {
+// The pages that the wave's new rows are in, at most T / page_size + 2 R; out and rows may be null.
+static int64_t touched_pages(const wpp_batch_desc* d, const int32_t* prefix_lens, const int32_t* chunk_lens, WppTouched* out, WppTouchedRows* rows) {
     int64_t n = 0, q_off = 0;
     for (int i = 0; i < d->num_requests; ++i) {
         const int64_t P = prefix_lens[i], C = chunk_lens[i], B = d->page_size;
         if (C == 0) continue;
         const int64_t from = P / B, to = (P + C + B - 1) / B;
-        for (int64_t b = from; out && b < to; ++b)
-            out[n + b - from] = {i, (int32_t)b, (int32_t)(q_off + b * B - P), (int16_t)std::max<int64_t>(P - b * B, 0), (int16_t)std::min(P + C - b * B, B)};
+        for (int64_t b = from; out && b < to; ++b) {
+            out[n + b - from] = {i, (int32_t)b};
+            rows[n + b - from] = {(int32_t)(q_off + b * B - P), (int16_t)std::max<int64_t>(P - b * B, 0), (int16_t)std::min(P + C - b * B, B)};
+        }
         n += to - from;
         q_off += C;
     }
@@ -231,7 +233,7 @@ size_t wpp_kv4_plan_bytes(const wpp_batch_desc* d, const wpp_plan_opts* o, int64
     const int64_t tiles = (T / WPP_HALF_M + d->num_requests) * d->num_q_heads;
     n += sizeof(WppUnit) * (size_t)(o->force_kv_splits >= 2 ? tiles * o->force_kv_splits : tiles + (d->dtype == WPP_KV8 ? 2 * kMostTailParts : 1) * (int64_t)o->max_ctas);
     n += sizeof(WppCombine) * (size_t)tiles;
-    if (d->dtype == WPP_KV8) n += sizeof(WppTouched) * (size_t)(T / d->page_size + 2 * (int64_t)d->num_requests + 1);
+    if (d->dtype == WPP_KV8) n += (sizeof(WppTouched) + sizeof(WppTouchedRows)) * (size_t)(T / d->page_size + 2 * (int64_t)d->num_requests);
     return align_up(n, 256);
 }
 
@@ -459,21 +461,21 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
     off += align_up(sizeof(int32_t) * first.size(), 16);
     hd.off_combine = (uint32_t)off;
     off += sizeof(WppCombine) * combines.size();
-    if (d->dtype == WPP_KV8) off = align_up(off, sizeof(WppTouched));
-    const size_t off_touched = off;          // (of the append; behind the combine records, at a multiple of 16 bytes, as it is read)
+    const size_t off_touched = off;          // (of the append; behind the combine records)
     int64_t n_touched = 0;
     if (d->dtype == WPP_KV8) {
-        n_touched = touched_pages(d, prefix_lens, chunk_lens, nullptr);
-        off += sizeof(WppTouched) * (size_t)n_touched;
+        n_touched = touched_pages(d, prefix_lens, chunk_lens, nullptr, nullptr);
+        off += (sizeof(WppTouched) + sizeof(WppTouchedRows)) * (size_t)n_touched;
     }
     hd.plan_bytes = align_up(off, 16);
     if (hd.plan_bytes > plan_host_bytes) return WPP_ERR_PLAN_MISMATCH;
     if (hd.plan_bytes > 0xffffffffu) return WPP_ERR_INVALID_ARG;       // (offsets are 32 bits)
     std::memcpy(p + hd.off_few_ctas, first.data(), sizeof(int32_t) * first.size());
     if (!combines.empty()) std::memcpy(p + hd.off_combine, combines.data(), sizeof(WppCombine) * combines.size());
-    const size_t off_gap = hd.off_combine + sizeof(WppCombine) * combines.size();
-    std::memset(p + off_gap, 0, off_touched - off_gap);
-    if (n_touched > 0) touched_pages(d, prefix_lens, chunk_lens, reinterpret_cast<WppTouched*>(p + off_touched));
+    if (n_touched > 0) {
+        WppTouched* const pages = reinterpret_cast<WppTouched*>(p + off_touched);
+        touched_pages(d, prefix_lens, chunk_lens, pages, reinterpret_cast<WppTouchedRows*>(pages + n_touched));
+    }
     std::memset(p + off, 0, hd.plan_bytes - off);
 
     hd.magic = WPP_PLAN_MAGIC;

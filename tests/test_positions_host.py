@@ -119,6 +119,21 @@ def test_what_rope_takes_and_refuses(reached):
     _refused(reached, _rope, ctx=ctx)
 
 
+def test_tensors_of_a_subclass_answer_for_themselves(reached):
+    class Elsewhere(torch.Tensor):
+        def get_device(self):
+            return 7
+
+    q, k = torch.nn.Parameter(_bf(5, 4, 64)), _bf(5, 2, 64)
+    _rope(q=q, k=k)
+    assert [x[0] for x in reached] == ["rope"] and reached[0][1][2] == q.data_ptr()      # (where it is, not a copy)
+    _refused(reached, _rope, k=k.as_subclass(Elsewhere))
+    with pytest.raises(AttributeError):
+        _rope(q=7)
+    with pytest.raises(AttributeError):
+        _rope(turns=object())
+
+
 def test_what_rope_append_takes_and_refuses(reached):
     for kw in (dict(), dict(q=None), dict(slots=torch.zeros(6, dtype=torch.int64)), dict(v_new=_bf(5, 3, 64)[:, :2])):
         n = len(reached)

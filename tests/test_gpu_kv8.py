@@ -470,6 +470,33 @@ def test_parts_that_are_dealt_out_joined_in_clusters_or_cut_from_the_last_tiles(
     assert int(g["status"].item()) == 6 and torch.equal(out[rows], again[rows])
 
 
+@pytest.mark.parametrize("name", list(DEALS))
+def test_a_plan_that_the_kernel_before_writes_and_the_built_in_scratch(name):
+    """The append and the attention see the plan that stands in plan_dev when the work before them has ended; the array of the library
+    serves for every way of spreading a wave."""
+    (P, C, Hq, Hkv), ctas = DEALS[name]
+    w = Wave(P, C, Hq, Hkv, 128, 32, seed=len(P))
+    g, plan = w.device(), w.plan(wpp.PlanOpts(0, 0, 0, ctas))
+    w.append(g, plan)
+    out, lse = w.attend(g, plan)
+    pools, sums, ws = (g["k"].clone(), g["v"].clone()), torch.zeros_like(lse), torch.full((int(plan.info.workspace_bytes),), 255, dtype=torch.uint8, device="cuda")
+    bits = plan.dev.clone()
+    for _ in range(3):
+        again = torch.zeros_like(out)
+        g["k"].copy_(torch.from_numpy(w.k_pool)), g["v"].copy_(torch.from_numpy(w.v_pool))
+        plan.dev.zero_()
+        torch.cuda.synchronize()
+        torch.bitwise_or(bits, 0, out=plan.dev)
+        w.append(g, plan)
+        plan.dev.zero_()
+        torch.bitwise_or(bits, 0, out=plan.dev)
+        wpp.wpp_prefill_attention_varlen(ctx(), w.desc(), g["q"], again, sums, g["k"], g["v"], g["table"], g["P"], g["C"], plan, workspace=ws, status=g["status"])
+        assert torch.equal(out, again) and torch.equal(lse, sums) and torch.equal(g["k"], pools[0]) and torch.equal(g["v"], pools[1])
+    again.zero_(), sums.zero_()
+    wpp.wpp_prefill_attention_varlen_static(ctx(), w.desc(), g["q"], again, sums, g["k"], g["v"], g["table"], g["P"], g["C"], plan, status=g["status"])
+    assert torch.equal(out, again) and torch.equal(lse, sums) and int(g["status"].item()) == 0
+
+
 def test_a_nan_score_in_a_part_that_a_cluster_joins():
     w = Wave([8191], [1], 8, 2, 128, 64, seed=3)
     w.k_pool[w.table[0, 50], 1, 5] = 0x7F

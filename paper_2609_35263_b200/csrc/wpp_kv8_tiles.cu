@@ -16,8 +16,8 @@
 // below the row's largest score y in log2 units and never above it: off by 2^-11 of itself or by 2^-25 of the largest (2^-8 of itself in bf16).
 // Where not all rows see all of a step's keys, a NaN code of V is 0 for the product; the first key that has one is kept per element, and
 // the epilogue makes the element of the rows that see it NaN.
-// What bounds it is the power limit: 4,096 tokens behind 32,768, 64/8 heads of 128, 3.72 ms by itself (1,260 TFLOP/s), 4.2 ms one call after the
-// other (1,110; the bf16 cache's kernel 3.25 and 3.7; the operations at the measured rates 2.75 and 3.3).  16 ragged prompts, 32/8 heads: 1.93 ms
+// What bounds it is the power limit: 4,096 tokens behind 32,768, 64/8 heads of 128, 3.6 ms by itself (1,300 TFLOP/s), 4.1 ms one call after the
+// other (1,140; the bf16 cache's kernel 3.25 and 3.7; the operations at the measured rates 2.75 and 3.3).  16 ragged prompts, 32/8 heads: 1.89 ms
 // against 1.69.  Up to there it was the fetching of instructions: an SM's scheduler runs the softmax's loop of some 480
 // instructions, the conversion's and an issuer's side by side, and what does not fit its instruction cache comes late.  So the issuers' loops,
 // the conversion's and the producer's are rolled up and have one place each for what they do (issuers 2,700 -> 2,040 us for half as many tokens, the
@@ -44,7 +44,9 @@ constexpr int kThreads = 512;
 constexpr uint32_t kTmemCols = 512, kColS = 0;
 __host__ __device__ constexpr uint32_t col_p(int hf) { return 128u + 64u * hf; }
 __host__ __device__ constexpr uint32_t col_o(int hf) { return 256u + 128u * hf; }
-constexpr int kRegsSoftmax = 184, kRegsCodes = 96, kRegsUtil = 48;
+// Registers of a thread by role.  4,096 tokens behind 32,768, one call after the other, and 16 ragged prompts, us: 184, 96, 48 4,178 and 1,925;
+// 192, 80, 48 4,164 and 1,905; so 4,101 and 1,885; 208, 56, 40 4,112 and 1,917.
+constexpr int kRegsSoftmax = 200, kRegsCodes = 64, kRegsUtil = 48;
 static_assert(8 * kRegsSoftmax + 4 * kRegsCodes + 4 * kRegsUtil <= 2048, "register file exceeded");
 // log2 of a row's largest p when its reference is moved, and when it has to be.  (Moves are dear: all 32 rows of a warp wait for the product
 // before and take O through registers.  16 ragged prompts with scores of deviation 1.3: kTop 7 1,910 us, 2 1,845, 0 1,830.)

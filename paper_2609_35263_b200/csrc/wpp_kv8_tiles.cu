@@ -14,8 +14,8 @@
 // the code's page and v that of the tile's first ones: exact, being a power of two, while vs / v is from 2^-12 to 2^4.  A step with a page
 // outside of that is a product of bf16 numbers, whose exponents do for any two scales.  So P is the softmax's own, 2^(y - m), m at most 15
 // below the row's largest score y in log2 units and never above it: off by 2^-11 of itself or by 2^-25 of the largest (2^-8 of itself in bf16).
-// Where not all rows see all of a step's keys, a NaN code of V is 0 for the product; the first key that has one is kept per element, and
-// the epilogue makes the element of the rows that see it NaN.
+// Where not all rows see all of a step's keys, and in every step done in bf16 (whose conversion knows no NaN), a NaN code of V is 0 for the
+// product; the first key that has one is kept per element, and the epilogue makes the element of the rows that see it NaN.
 // What bounds it is the power limit: 4,096 tokens behind 32,768, 64/8 heads of 128, 3.6 ms by itself (1,300 TFLOP/s), 4.1 ms one call after the
 // other (1,140; the bf16 cache's kernel 3.25 and 3.7; the operations at the measured rates 2.75 and 3.3).  16 ragged prompts, 32/8 heads: 1.89 ms
 // against 1.69.  Up to there it was the fetching of instructions: an SM's scheduler runs the softmax's loop of some 480
@@ -536,7 +536,8 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             fence_proxy_async_smem();
             mbar_arrive(bQReady);
             ++tiles;
-            // ---- V.  Where some rows do not see all keys: NaN codes, and rows behind the sequence, which are zeros
+            // ---- V.  Where some rows do not see all keys: NaN codes, and rows behind the sequence, which are zeros.  NaN codes in wide steps too,
+            //      whoever sees them: their conversion would make numbers of them
             const int all_see = min(v.n[0] > 0 ? v.P + un.row0[0] : 0x7fffffff, v.n[1] > 0 ? v.P + un.row0[1] : 0x7fffffff);       // the last key that every row sees
             for (int k = 0; k < v.n_steps; ++k) {
                 bool ok = mbar_wait(bRawFull + 8 * ring_raw.stage, ring_raw.phase, abort_flag);
@@ -549,7 +550,7 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                 const int apart[2] = {vp[2 * (warp & 3)], vp[2 * (warp & 3) + 1]};      // of the warp's first and last 16 rows
                 const bool wide = vp[8] != 0;
                 if (r == 0) s_wide[ring_v.stage] = wide;
-                if (__builtin_expect(key0 + 127 > all_see, 0)) {
+                if (__builtin_expect(wide || key0 + 127 > all_see, 0)) {
                     const int rows = v.kv_len - key0;
 #pragma unroll 1
                     for (int i = 0; i < kChunks; ++i) {

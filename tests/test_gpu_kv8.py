@@ -515,3 +515,56 @@ def test_a_long_cache():
     for opts in (None, wpp.PlanOpts(0, 0, 0, 0, 0, 1), wpp.PlanOpts(0, 0, 0, 8)):
         out, lse = w.attend(g, opts=opts)
         w.check(out, lse, w.reference())
+
+
+# ---------------------------------------------------------------------------------------------------- NaN codes in any step
+@pytest.mark.parametrize("d,B", [(128, 64), (64, 16)])
+@pytest.mark.parametrize("shape,splits", [(1, 1), (1, 2), (2, 1), (2, 3)])
+@pytest.mark.parametrize("apart", [0, 6, -14, 20])
+def test_a_nan_code_of_v_behind_which_every_row_stands(d, B, shape, splits, apart):
+    """A key that all rows see, far from the diagonal, in a page whose scale is 2^apart times the others'."""
+    w = Wave([900], [150], 8, 2, d, B, seed=31, scales=(-8, -8))
+    page, slot = w.table[0, 500 // B], 500 % B
+    w.v_pool[page, 1, B * d:B * d + 4] = np.array([2.0 ** (apart - 8)], np.float32).view(np.uint8)
+    good = w.reference()
+    w.v_pool[page, 1, [slot * d + 7, slot * d + d - 2]] = 0x7F, 0xFF
+    g = w.device()
+    out, lse = w.attend(g, opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
+    hit = np.zeros(out.shape, bool)
+    hit[:, 4:, [7, d - 2]] = True
+    assert np.array_equal(np.isnan(out.float().cpu().numpy()), hit)
+    for x, y in zip(good, (out, None, None, None)):
+        if x.ndim == 3:
+            x[hit] = 0.0
+        if y is not None:
+            y[torch.from_numpy(hit).cuda()] = 0.0
+    w.check(out, lse, good)
+
+
+@pytest.mark.parametrize("d,B", [(128, 64), (64, 16)])
+@pytest.mark.parametrize("shape,splits", [(1, 1), (1, 2), (2, 1), (2, 3)])
+def test_a_page_of_infinite_values_as_the_append_leaves_it(d, B, shape, splits):
+    """Nothing in it is finite: its scale is the least there is, 2^48 below the others'."""
+    w = Wave([10 * B + 400], [150], 8, 2, d, B, seed=32, scales=(-8, -8))
+    good = w.reference()
+    fill = Wave([5 * B], [B], 8, 2, d, B, seed=33)
+    fill.table, fill.pages, fill.k_pool, fill.v_pool = w.table, w.pages, w.k_pool, w.v_pool
+    x = okv8.bf16_values(fill.v_new).copy()
+    x[:, 1] = np.where(np.arange(B * d).reshape(B, d) % 3 == 0, np.nan, np.inf)
+    fill.v_new = _bits(x)
+    g = fill.device()
+    fill.append(g)
+    w.k_pool, w.v_pool = fill.appended()
+    _same(g, w)
+    assert okv8.block_scale(w.v_pool[w.table[0, 5], 1], B, d) == 2.0 ** -56
+    hit = np.zeros(good[0].shape, bool)
+    hit[:, 4:] = True
+    out, lse = w.attend(w.device(), opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
+    assert np.array_equal(np.isnan(out.float().cpu().numpy()), hit)
+    w.v_pool[w.table[0, 5], 1] = 0                                      # (of the heads that see nothing of it, and of the sums)
+    w.v_pool[w.table[0, 5], 1, B * d:B * d + 4] = np.array([1.0], np.float32).view(np.uint8)
+    good = w.reference()
+    for i in (0, 2, 3):
+        good[i][hit] = 0.0
+    out[torch.from_numpy(hit).cuda()] = 0.0
+    w.check(out, lse, good)

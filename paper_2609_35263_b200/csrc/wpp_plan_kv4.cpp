@@ -374,9 +374,6 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
         }
     }
     const int64_t n_few = n_units;
-    // (a wave that the built-in scratch array would hold otherwise must not be refused for its many parts)
-    if (deal && slots > scratch_slots(d))
-        return make_plan(d, o, prefix_lens, chunk_lens, T, pairs, false, plan_host, plan_host_bytes, info);
     if (deal) {
         std::stable_sort(us, us + n_few, [](const WppUnit& a, const WppUnit& b) { return a.cost > b.cost; });
         first.assign((size_t)std::min<int64_t>(most_ctas, n_few), 0);
@@ -522,5 +519,16 @@ static int make_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int3
 
 int wpp_kv4_plan(const wpp_batch_desc* d, const wpp_plan_opts* o, const int32_t* prefix_lens, const int32_t* chunk_lens, int64_t T,
                  int64_t pairs, void* plan_host, size_t plan_host_bytes, wpp_plan_info* info) {
-    return make_plan(d, o, prefix_lens, chunk_lens, T, pairs, true, plan_host, plan_host_bytes, info);
+    int rc = make_plan(d, o, prefix_lens, chunk_lens, T, pairs, true, plan_host, plan_host_bytes, info);
+    // A wave that the built-in scratch array would hold otherwise, tiles' parts and all, must not be refused for the many parts of its few
+    // rows; one that it would not hold in any case keeps them.
+    const bool dealt = rc == WPP_OK && static_cast<const WppPlanHeader*>(plan_host)->deal_items == 1;
+    if (!dealt || info->workspace_bytes <= wpp_static_scratch_bytes()) return rc;
+    const std::vector<char> plan(static_cast<const char*>(plan_host), static_cast<const char*>(plan_host) + info->plan_bytes);
+    const wpp_plan_info its = *info;
+    rc = make_plan(d, o, prefix_lens, chunk_lens, T, pairs, false, plan_host, plan_host_bytes, info);
+    if (rc == WPP_OK && info->workspace_bytes <= wpp_static_scratch_bytes()) return rc;
+    std::memcpy(plan_host, plan.data(), plan.size());
+    *info = its;
+    return WPP_OK;
 }

@@ -152,3 +152,40 @@ def test_plan_covers_every_key_of_every_row_once(name):
     assert not steps
     assert pages.tolist() == [[i, b] for i in range(len(P)) if C[i] for b in range(P[i] // B, -(-(P[i] + C[i]) // B))]
     assert plan.info.workspace_bytes <= wpp.wpp_static_scratch_bytes()
+
+
+def _workspace(dtype, heads, P, C, opts=None):
+    Hq, Hkv, d, B = heads
+    blocks = max(-(-(p + c) // B) for p, c in zip(P, C))
+    return int(wpp.wpp_plan_tiles(None, wpp.make_desc(len(P), Hq, Hkv, d, B, blocks, blocks, dtype=dtype), P, C, opts=opts, pin=False).info.workspace_bytes)
+
+
+def test_dealt_parts_take_no_wave_from_the_built_in_scratch():
+    """What the array holds otherwise it holds of an 8-bit cache too: a wave of long and short parts is planned again without them where its
+    tiles' parts no longer fit beside them.  (Equal shares of one wave are cut alike for both kinds of cache.)"""
+    most = wpp.wpp_static_scratch_bytes()
+    assert _workspace(wpp.WPP_KV8, (40, 8, 128, 64), [23213, 25029, 9801], [133, 204, 33]) <= most
+    rng, hits = np.random.default_rng(5), 0
+    for _ in range(3000):
+        heads = [(40, 8, 128, 64), (64, 8, 128, 64), (32, 8, 128, 16), (8, 2, 64, 16)][rng.choice(4, p=(0.7, 0.1, 0.1, 0.1))]
+        n = int(rng.integers(2, 6))
+        P, C = rng.integers(0, 40000, n), np.exp(rng.uniform(0, np.log(300), n)).astype(int)
+        a, b = _workspace(wpp.WPP_KV8, heads, P, C), _workspace(wpp.WPP_KV4, heads, P, C)
+        assert a <= most or b > most, (heads, P, C, a, b)
+        hits += b > most
+    assert hits < 2000                                                  # (the waves are not all too large for it anyway)
+
+
+def test_a_wave_that_the_built_in_scratch_does_not_hold_in_any_case_keeps_its_dealt_parts():
+    """Nothing is won by planning it without them: and what comes back is that plan, to the byte of what a second call gives."""
+    heads, P, C = (32, 8, 128, 16), [25486, 33879, 32130, 4978], [65, 2, 9, 3]
+    assert min(_workspace(dtype, heads, P, C) for dtype in (wpp.WPP_KV8, wpp.WPP_KV4)) > wpp.wpp_static_scratch_bytes()
+    desc = wpp.make_desc(4, *heads, 2200, 2200, dtype=wpp.WPP_KV8)
+    a, b = (wpp.wpp_plan_tiles(None, desc, P, C, pin=False) for _ in range(2))
+    units, few, how, pages = _units(a)
+    assert how == 1 and 0 < few < len(units) == a.info.num_tiles and a.host_bytes() == b.host_bytes()
+    ends = {}                                                           # (key steps of every block of rows, whose parts have to meet)
+    for u in sorted(units[:few].tolist(), key=lambda u: (u[0], u[4], u[8], u[1])):
+        assert u[1] == ends.get((u[0], u[4], u[8]), 0)
+        ends[u[0], u[4], u[8]] = u[2]
+    assert pages.tolist() == [[i, x] for i in range(4) for x in range(P[i] // 16, -(-(P[i] + C[i]) // 16))]

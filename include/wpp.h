@@ -298,9 +298,10 @@ size_t wpp_static_scratch_bytes(void);
  *   row_offsets  : device int64 [R+1], out, exclusive scan of chunk_lens.
  *   positions, slots : device int32 and int64 [max_tokens], out, either may be NULL; rows behind the last token are 0 and -1.
  * WPP_ERR_BOUNDS in *status_dev: the list ran out or holds an id outside [0, num_pages), or cursor[0] outside [0, num_free] (it is taken for
- * the nearer end); a page that a request holds is outside; a row of block_tables is too short; or there are more than max_tokens
- * tokens (those behind are left out).  Tokens without a page get slot -1, columns without one -1.  WPP_ERR_INVALID_ARG there: a
- * negative length; the request counts as empty.  One kernel. */
+ * the nearer end); the page that a request holds and its first new token goes to is outside; a row of block_tables is too short for a
+ * request with new tokens; or there are more than max_tokens tokens (those behind are left out).  All but the last whether or not
+ * positions or slots are asked for.  Tokens without a page get slot -1, columns without one -1.  WPP_ERR_INVALID_ARG there: a negative
+ * length; the request counts as empty.  One kernel. */
 int wpp_assign_pages(const wpp_ctx* ctx, const wpp_batch_desc* desc, const int32_t* prefix_lens, const int32_t* chunk_lens,
                      const int32_t* free_pages, int32_t num_free, const int32_t* cursor, int32_t* cursor_out, int32_t* block_tables,
                      int64_t* row_offsets, int32_t* positions_or_null, int64_t* slots_or_null, int32_t max_tokens, int32_t* status_dev,

@@ -18,15 +18,18 @@ constexpr int kPagesThreads = 512;
 
 struct PageSpan {
     int64_t P, C, there, blocks;       // lengths; pages held and needed (as far as the table goes)
+    bool bad, short_row;               // a negative length (the request counts as empty); new tokens, and a table's row that ends before them
 };
 __device__ __forceinline__ PageSpan span_of(const PagesParams& p, int i) {
     PageSpan s;
     s.P = p.prefix_lens[i];
     s.C = p.chunk_lens[i];
-    if (s.P < 0 || s.C < 0) s.P = s.C = 0;
-    const int64_t round = ((int64_t)1 << p.page_shift) - 1;
+    s.bad = s.P < 0 || s.C < 0;
+    if (s.bad) s.P = s.C = 0;
+    const int64_t round = ((int64_t)1 << p.page_shift) - 1, need = (s.P + s.C + round) >> p.page_shift;
     s.there = min((s.P + round) >> p.page_shift, (int64_t)p.max_blocks);
-    s.blocks = min((s.P + s.C + round) >> p.page_shift, (int64_t)p.max_blocks);
+    s.blocks = min(need, (int64_t)p.max_blocks);
+    s.short_row = s.C > 0 && need > p.max_blocks;
     return s;
 }
 // the last i of [0, n) with at[i] <= x, if at[0] <= x; of equal ones the last: the one that has something
@@ -57,10 +60,16 @@ __global__ void __launch_bounds__(kPagesThreads) wpp_pages_kernel(const PagesPar
     int64_t tokens = 0, pages = 0;            // of the requests so far
     for (int base = 0; base < R; base += kPagesThreads) {
         const int i = base + tid;
-        PageSpan s = {0, 0, 0, 0};
+        PageSpan s = {0, 0, 0, 0, false, false};
         if (i < R) {
             s = span_of(p, i);
-            if (p.prefix_lens[i] < 0 || p.chunk_lens[i] < 0) error = WPP_ERR_INVALID_ARG;
+            if (s.bad) error = WPP_ERR_INVALID_ARG;
+            if (s.short_row) error = WPP_ERR_BOUNDS;
+            if (!p.slots && blockIdx.x == 0 && s.C > 0 && !s.short_row && s.there > s.P >> p.page_shift) {
+                // the page that the first new token goes to, which the slots' makers look at otherwise
+                const int32_t page = p.block_tables[(int64_t)i * p.max_blocks + (s.P >> p.page_shift)];
+                if (page < 0 || page >= p.num_pages) error = WPP_ERR_BOUNDS;
+            }
         }
         int64_t t = s.C;
         int64_t n = s.blocks - s.there;

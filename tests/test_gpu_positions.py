@@ -409,3 +409,34 @@ def test_a_wave_from_lengths_to_attention(cache, C):
             # bf16 results and probabilities (the 4-bit cache's rows too, there, after K's scores): a step of 2^-8 each, and an eighth for the scores
             assert np.all(np.abs(got - o) <= 2.0 ** -8 * (np.abs(o) + 2.125 * spread) + 1e-5)
         row += C[i]
+
+
+@pytest.mark.parametrize("outputs", ["positions", "slots", "neither"])
+@pytest.mark.parametrize("case,status", [("nothing wrong", 0), ("short table", 3), ("short table, prefix alone", 3), ("bad page in a table", 3),
+                                         ("page below zero in a table", 3), ("list runs out", 3), ("negative length", 1), ("empty chunk behind a bad page", 0)])
+def test_pages_without_positions_or_slots_are_refused_alike(case, status, outputs):
+    w = Pages([20, 0, 40, 7], [30, 100, 1, 60], 16, seed=4)
+    if case == "short table":
+        w.table, w.most = np.ascontiguousarray(w.table[:, :6]), 6                          # (request 1 needs 7)
+    elif case == "short table, prefix alone":
+        w.P[2], w.C[1], w.C[3], w.table, w.most = 90, 1, 1, np.ascontiguousarray(w.table[:, :5]), 5      # (request 2 holds 6)
+    elif case in ("bad page in a table", "page below zero in a table"):
+        w.table[0, 1] = w.num_pages if case.startswith("bad") else -1
+    elif case == "list runs out":
+        w.free = w.free[:6]
+    elif case == "negative length":
+        w.P[2] = -1
+    elif case == "empty chunk behind a bad page":
+        w.table[0, 1], w.C[0] = w.num_pages, 0
+    w.total = int(np.maximum(w.C, 0).sum())
+    table, cursor, bad = _i32(w.table), _i32([0, 0]), torch.zeros(1, dtype=torch.int32, device="cuda")
+    rows, positions, slots = (torch.full((n,), -5, dtype=t, device="cuda") for n, t in ((5, torch.int64), (w.total, torch.int32), (w.total, torch.int64)))
+    wpp.wpp_assign_pages(ctx(), w.desc(), _i32(w.P), _i32(w.C), _i32(w.free), cursor, table, rows, positions if outputs == "positions" else None,
+                         slots if outputs == "slots" else None, status=bad)
+    want = opos.assign(w.P, w.C, w.free, 0, w.table, w.B, w.num_pages, w.total)
+    assert int(bad.item()) == status == want[5] and cursor.tolist() == [want[4], 0]
+    assert np.array_equal(table.cpu().numpy(), want[0]) and np.array_equal(rows.cpu().numpy(), want[1])
+    if outputs == "positions":
+        assert np.array_equal(positions.cpu().numpy(), want[2])
+    if outputs == "slots":
+        assert np.array_equal(slots.cpu().numpy(), want[3])

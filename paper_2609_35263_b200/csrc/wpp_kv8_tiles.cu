@@ -369,6 +369,7 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                             else ring_p[0].advance(kPar);
                         }
                         if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }
+                        __syncwarp();                                  // (a vote orders no memory: all lanes' entries before lane 0's arrival)
                         if (lane == 0) mbar_arrive(bKFull + 8 * ring_k.stage);
                         ring_k.advance(C::kStages);
                     }
@@ -377,6 +378,7 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
                         if (ok && lane < 8) s_vpar[ring_v.stage * 12 + lane] = apart_v;
                         if (ok && lane == 8) s_vpar[ring_v.stage * 12 + 8] = wide_v;
                         if (!__all_sync(0xffffffffu, ok)) { dead = true; break; }
+                        __syncwarp();
                         if (lane == 0) mbar_arrive(bRawFull + 8 * ring_v.stage);
                         ring_v.advance(C::kStages);
                     }

@@ -6,10 +6,11 @@
 // and the products are taken of the codes themselves, which f16 holds exactly: S^T = C Q^T, O^T = C'^T P^T by mma.sync, eight columns of
 // query rows that the group's heads fill (a product of 128 rows on the 5th-generation tensor cores would be nearly empty).
 // The sums O are in units of the largest vs so far, v: p_j = 2^(y_j - m + log2(vs / v)), so that V's scales cost no operation of their own
-// beyond a factor v / vs per 16 keys (a page has at least so many) for the sum of 2^(y_j - m).  The reference m is put 7 below a row's
-// largest y_j and moved when one comes 15 above: p lies within f16's range, off by 2^-11 of itself or by 2^-24 of the largest that its
-// page's keys can have.  Pages whose scale is more than 2^8 below v would be pushed out of that range, by others that may have a large scale
-// for one row's sake: their product is taken by itself, without vs / v, and added with it in fp32.
+// beyond a factor v / vs per 16 keys (a page has at least so many) for the sum of 2^(y_j - m).  The reference m, a whole number, is put 6 to 7
+// below a row's largest y_j and moved when one comes 15 above: p lies within f16's range, off by 2^-11 of itself or by 2^-25, which is 2^-31 of
+// the row's largest where vs is v, and 2^-23 of the largest that its page's keys can have where vs is 2^-8 v.  Pages whose scale is more than
+// 2^8 below v would be pushed out of that range, by others that may have a large scale for one row's sake: their product is taken by
+// itself, without vs / v, and added with it in fp32.
 //
 // What bounds it is the cache's bytes.  A warp takes 32 keys at a time, copied asynchronously into a ring of its own and read in the
 // order the fragments want: which element of a row stands at which place of a product does not matter as long as both factors agree,

@@ -12,8 +12,8 @@
 // O += P V is a product of f16 numbers, because P as two e4m3 terms would cost the softmax warps, which are what everybody waits for,
 // several operations a score, and four other warps turn two of V's codes into f16 by one.  V's tiles hold code * vs / v, vs the scale of
 // the code's page and v that of the tile's first ones: exact, being a power of two, while vs / v is from 2^-12 to 2^4.  A step with a page
-// outside of that is a product of bf16 numbers, whose exponents do for any two scales.  So P is the softmax's own, 2^(y - m), m at most 15
-// below the row's largest score y in log2 units and never above it: off by 2^-11 of itself or by 2^-25 of the largest (2^-8 of itself in bf16).
+// outside of that is a product of bf16 numbers, whose exponents do for any two scales.  So P is the softmax's own, 2^(y - m), m at least 7
+// and at most 15 below the row's largest score y so far in log2 units: off by 2^-11 of itself or by 2^-32 of the largest (2^-8 of itself in bf16).
 // Where not all rows see all of a step's keys, and in every step done in bf16 (whose conversion knows no NaN), a NaN code of V is 0 for the
 // product; the first key that has one is kept per element, and the epilogue makes the element of the rows that see it NaN.
 // What bounds it is the power limit: 4,096 tokens behind 32,768, 64/8 heads of 128, 3.6 ms by itself (1,300 TFLOP/s), 4.1 ms one call after the
@@ -49,8 +49,9 @@ __host__ __device__ constexpr uint32_t col_o(int hf) { return 256u + 128u * hf; 
 constexpr int kRegsSoftmax = 200, kRegsCodes = 64, kRegsUtil = 48;
 static_assert(8 * kRegsSoftmax + 4 * kRegsCodes + 4 * kRegsUtil <= 2048, "register file exceeded");
 // log2 of a row's largest p when its reference is moved, and when it has to be.  (Moves are dear: all 32 rows of a warp wait for the product
-// before and take O through registers.  16 ragged prompts with scores of deviation 1.3: kTop 7 1,910 us, 2 1,845, 0 1,830.)
-constexpr float kTop = 0.f, kMost = 15.f;
+// before and take O through registers.  16 ragged prompts with scores of deviation 1.3: kTop 7 1,920 us, 4 1,899, 0 1,892.  But f16 numbers end
+// 2^25 below 1, and what a key far above all others leaves to them, each less than that, may be all that its own value does not outweigh.)
+constexpr float kTop = 7.f, kMost = 15.f;
 constexpr int kScaleDown = -12, kScaleUp = 4;      // log2 of vs / v that f16 numbers take
 constexpr int kPar = 4;                    // key steps of a half whose scales are held
 constexpr int kNan = 8;                    // tiles whose first NaN codes of V are held

@@ -568,3 +568,27 @@ def test_a_page_of_infinite_values_as_the_append_leaves_it(d, B, shape, splits):
         good[i][hit] = 0.0
     out[torch.from_numpy(hit).cuda()] = 0.0
     w.check(out, lse, good)
+
+
+# ----------------------------------------------------------------------------------------------- probabilities far apart
+@pytest.mark.parametrize("gap", [12.0, 18.0, 23.45, 28.0])
+@pytest.mark.parametrize("shape,splits", [(1, 1), (1, 2), (2, 1), (2, 3)])
+@pytest.mark.parametrize("d,Hq,C", [(128, 4, 40), (64, 4, 130), (128, 2, 2)])
+def test_a_key_far_above_a_flat_tail_leaves_it_its_weight(gap, shape, splits, d, Hq, C):
+    """One of the first keys 2^gap above all others, with a value of zeros, so that the output is the others'.  Scores are one product each.  A
+    probability is off by 2^-11 of itself or by 2^-25, half of f16's last step, where the largest is from 2^7 on (few rows: whose reference is
+    a whole number, from 2^6 on); the exponent by five roundings of 2^-24 of a number below 2^5,
+    its power by 2^-22, the sums over at most 2^7 steps by 2^-23 each: under 2^-14 together; the result by 2^-8."""
+    n = 1500
+    w = Wave([n - C], [C], Hq, 1, d, 64, seed=34, sm_scale=gap * np.log(2))
+    q, k, v = np.zeros((C, Hq, d), np.float32), np.zeros((n, 1, d), np.float32), np.ones((n, 1, d), np.float32)
+    q[..., 0], k[5, 0, 0], v[5] = 1.0, 1.0, 0.0
+    w.q = okv8.bf16_bits(q)
+    fill = Wave([0], [n], 1, 1, d, 64)
+    fill.table, fill.pages, fill.k_pool, fill.v_pool, fill.k_new, fill.v_new = w.table, w.pages, w.k_pool, w.v_pool, okv8.bf16_bits(k), okv8.bf16_bits(v)
+    w.k_pool, w.v_pool = fill.appended()
+    out, _ = w.attend(w.device(), opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
+    o, _, spread, even = w.reference()
+    got = out.double().cpu().numpy()
+    tol = (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -14) * np.abs(o) + 2.0 ** (-32 if shape == 1 else -31) * even
+    assert np.all(np.abs(got - o) <= tol), float((np.abs(got - o) / tol).max())

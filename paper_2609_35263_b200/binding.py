@@ -399,7 +399,8 @@ def wpp_rope(ctx: Context, q, k, turns, positions, q_out=None, k_out=None, inter
 def wpp_rope_append(ctx: Context, desc: BatchDesc, q, k_new, v_new, q_out, k_cache, v_cache, turns, positions, slots, interleaved: bool = False,
                     magnitude: float = 1.0, status=None, stream=None) -> None:
     """wpp_rope, with the rotated keys and the values (cuda bf16 [T, Hkv, d]) written to their slots of a bf16 cache: slots, cuda int64 [T],
-    as wpp_assign_pages leaves them (-1: not written).  q may be None; q_out None: in place."""
+    as wpp_assign_pages leaves them (-1: not written).  q may be None; q_out None: in place.  k_cache, v_cache: cuda bf16 of any shape that
+    holds what desc says from their first element on."""
     st = _call.rope_append(ctx.handle.value, ctx.device, desc, q, k_new, q if q_out is None else q_out, v_new, turns, positions, interleaved,
                            magnitude, k_cache, v_cache, slots, status, _stream(ctx, stream))
     if st:

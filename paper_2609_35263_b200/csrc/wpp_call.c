@@ -233,6 +233,47 @@ static int rows(PyObject* o, long device, int64_t T, int64_t heads, int64_t d, t
     if (!*token && *head) *token = *head * t->size[1];                                     /* (of a single token: any that is long enough) */
     return 0;
 }
+/* Elements (of a cache held in codes: bytes) from a pool's address to the end of its last row, as the library reads the description; 0 where
+ * it refuses it. */
+static __int128 pool_end(const wpp_batch_desc* d) {
+    if (d->num_pages <= 0 || d->num_kv_heads <= 0 || d->page_size <= 0 || d->head_dim <= 0) return 0;
+    if (d->kv_token_stride < 0 || d->kv_head_stride < 0 || d->kv_page_stride < 0) return 0;
+    const __int128 B = d->page_size, token = d->kv_token_stride ? d->kv_token_stride : d->head_dim;
+    const __int128 block = (B - 1) * token + d->head_dim;
+    const __int128 head = d->kv_head_stride ? d->kv_head_stride : token * B, page = d->kv_page_stride ? d->kv_page_stride : head * d->num_kv_heads;
+    return (d->num_pages - 1) * page + (d->num_kv_heads - 1) * head + block;
+}
+/* a tensor of a type on the device with this number, of any shape, that goes on for `end` elements: kernels write at computed places of it */
+static int pool_of(PyObject* o, PyObject* type, long device, __int128 end) {
+    PyObject* x = ask(o, &dtype);
+    if (!x) return -1;
+    const int other = x != type;
+    Py_DECREF(x);
+    if (other) return 1;
+    x = ask(o, &get_device);
+    if (!x) return -1;
+    const long on = PyLong_AsLong(x);
+    Py_DECREF(x);
+    if (on == -1 && PyErr_Occurred()) return -1;
+    if (on != device) return 1;
+    PyObject *size = ask(o, &shape), *stride = size ? ask(o, &strides) : NULL;
+    int rc = -1;
+    if (stride && PyTuple_Check(size) && PyTuple_Check(stride) && PyTuple_GET_SIZE(size) == PyTuple_GET_SIZE(stride)) {
+        __int128 reach = 1;
+        int none = 0;
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(size); ++i) {
+            const int64_t n = (int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(size, i)), by = (int64_t)PyLong_AsLongLong(PyTuple_GET_ITEM(stride, i));
+            none |= n <= 0;
+            reach += (__int128)(n - 1) * by;
+        }
+        if (!PyErr_Occurred()) rc = (none ? 0 : reach) < end;
+    } else if (stride) {
+        PyErr_SetString(PyExc_TypeError, "shape or strides that are no tuple");
+    }
+    Py_XDECREF(size);
+    Py_XDECREF(stride);
+    return rc;
+}
 /* q, k (None: none), turns, positions and the options into a description: args[0 .. 7] are q, k, q_out, k_out or v, turns, positions,
  * interleaved, magnitude */
 static int rope_desc(PyObject* const* args, long device, int with_v, wpp_rope_desc* d, tensor* t) {
@@ -301,6 +342,8 @@ static PyObject* rope_append(PyObject* self, PyObject* const* args, Py_ssize_t n
     if (device == -1 && PyErr_Occurred()) return NULL;
     int st = args[4] == Py_None ? 1 : rope_desc(args + 3, device, 1, &d, t);
     if (st == 0) st = numbers(args[13], o_i64, device, d.total_tokens, &slots);
+    for (int i = 0; st == 0 && i < 2; ++i)               /* (none, and a cache that is not of bf16 rows: the library says so) */
+        if (args[11 + i] != Py_None && d.total_tokens > 0 && b.dtype == WPP_BF16) st = pool_of(args[11 + i], o_bf16, device, pool_end(&b));
     if (st < 0 || memories(args + 11, 2, pool) || memories(args + 14, 1, &status)) return NULL;
     if (st == 0) {
         Py_BEGIN_ALLOW_THREADS

@@ -234,3 +234,30 @@ def test_what_the_library_refuses_before_it_looks_for_a_device():
     assert pages(wpp.make_desc(16385, 4, 2, 64, 16, 4, 8)) == 2
     for name in ("prefix", "chunks", "free", "cursor", "cursor_out", "tables", "rows"):
         assert pages(batch(), **{name: None}) == 1, name
+
+
+def test_rope_append_looks_at_its_pools(reached):
+    """Keys and values go to computed places of them: what is of another type or ends too early is refused."""
+    both, kv = _bf(8, 2, 2, 16, 64), wpp.make_desc(1, 4, 2, 64, 16, 4, 8, kv_page_stride=2 * 2 * 16 * 64)
+    packed = wpp.make_desc(1, 4, 2, 64, 16, 4, 8, kv_token_stride=128, kv_head_stride=128 * 16, kv_page_stride=128 * 32)
+    for kw in (dict(), dict(k_cache=_bf(9, 2, 16, 64)), dict(k_cache=_bf(8 * 2 * 16 * 64)), dict(v_cache=_bf(4, 2, 2, 2, 16, 64)), dict(k_cache=both, v_cache=both[:, 1], desc=kv),
+               dict(k_cache=both[:, 0], v_cache=both.view(-1)[2 * 16 * 64:], desc=kv), dict(k_cache=_bf(8, 2, 16, 128)[..., :64], v_cache=_bf(8, 2, 16, 128)[..., 64:], desc=packed),
+               dict(k_cache=torch.nn.Parameter(_bf(8, 2, 16, 64))), dict(k_cache=None), dict(desc=wpp.make_desc(1, 4, 2, 64, 16, 4, 8, dtype=wpp.WPP_KV8), k_cache=_bf(1)),
+               dict(q=_bf(0, 4, 64), k_new=_bf(0, 2, 64), v_new=_bf(0, 2, 64), k_cache=_bf(1)), dict(desc=wpp.make_desc(1, 4, 2, 64, 16, 4, 8, kv_page_stride=-8))):
+        n = len(reached)
+        _append(**kw)                                    # (the stub in the library's place takes everything)
+        assert len(reached) == n + 1, kw
+    for name in ("k_cache", "v_cache"):
+        for pool in (_bf(7, 2, 16, 64), _bf(8, 1, 16, 64), _bf(8, 2, 16, 32), _bf(8, 2, 16, 64)[1:], _bf(8 * 2 * 16 * 64 - 1), _bf(0, 2, 16, 64), _bf(8, 2, 16, 64).float(),
+                     _bf(8, 2, 16, 64).half(), torch.zeros(8, 2, 16 * 64 * 2, dtype=torch.uint8), _bf(1, 2, 16, 64).expand(8, 2, 16, 64)):
+            _refused(reached, _append, **{name: pool})
+        _refused(reached, _append, **{"k_cache": both[:, 0], "v_cache": both[:, 1], "desc": kv, name: _bf(8, 2, 16, 64)})
+        _refused(reached, _append, **{"desc": wpp.make_desc(1, 4, 2, 64, 16, 4, 2 ** 31 - 1, kv_page_stride=2 ** 62), name: _bf(8, 2, 16, 64)})
+
+    class Elsewhere(torch.Tensor):
+        def get_device(self):
+            return 7
+    for name in ("k_cache", "v_cache"):
+        _refused(reached, _append, **{name: _bf(8, 2, 16, 64).as_subclass(Elsewhere)})
+        with pytest.raises(AttributeError):
+            _append(**{name: 4096})

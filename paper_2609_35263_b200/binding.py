@@ -348,7 +348,8 @@ def _stream(ctx: Context, stream) -> int:
 
 def wpp_kv_append(ctx: Context, desc: BatchDesc, k_new, v_new, k_cache, v_cache, block_tables, prefix_lens,
                   chunk_lens, plan: Plan, status=None, stream=None) -> None:
-    """Queue the KV append of one wave on `stream` (device tensors; int32 metadata on the device)."""
+    """Queue the KV append of one wave on `stream` (device tensors; int32 metadata on the device).  Pools of a cache held in 8 bits: uint8 of
+    any shape that holds what desc says from its first element on, here and in the attention calls."""
     st = _call.kv_append(ctx.handle.value, desc, k_new, v_new, k_cache, v_cache, block_tables, prefix_lens, chunk_lens, plan.host,
                          plan.dev, status, _stream(ctx, stream))
     if st:
@@ -433,7 +434,10 @@ def wpp_prefill_attention_varlen_static(ctx: Context, desc: BatchDesc, q, out, l
     device share that array, so calls whose kernels could overlap on the GPU must be serialised.  The first call
     on a device does a one-time address look-up (the context's device must be current) and should come before any
     stream capture."""
-    st = load_library().wpp_prefill_attention_varlen_static(
+    lib = load_library()
+    if isinstance(desc, BatchDesc) and desc.dtype == WPP_KV8:
+        _check(_call.code_pools(desc, k_cache, v_cache), "wpp_prefill_attention_varlen_static")
+    st = lib.wpp_prefill_attention_varlen_static(
         ctx.handle, ctypes.byref(desc), _ptr(q), _ptr(out), _ptr(lse), _ptr(k_cache), _ptr(v_cache),
         _ptr(block_tables), _ptr(prefix_lens), _ptr(chunk_lens), plan.host.data_ptr(),
         _ptr(plan.dev), _ptr(status), _stream(ctx, stream))

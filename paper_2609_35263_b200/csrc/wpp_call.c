@@ -35,7 +35,7 @@ typedef struct {
     PyObject *name, *descriptor;    /* descriptor: null where it is of no kind that is known here */
 } member;
 static member data_ptr = {"data_ptr", 1, NULL, NULL}, get_device = {"get_device", 1, NULL, NULL}, strides = {"stride", 1, NULL, NULL},
-              shape = {"shape", 0, NULL, NULL}, dtype = {"dtype", 0, NULL, NULL};
+              element_size = {"element_size", 1, NULL, NULL}, shape = {"shape", 0, NULL, NULL}, dtype = {"dtype", 0, NULL, NULL};
 static PyTypeObject* t_tensor;
 static PyObject* ask(PyObject* o, const member* m) {
     if (Py_TYPE(o) == t_tensor && m->descriptor) {
@@ -108,6 +108,8 @@ static int count(Py_ssize_t n, Py_ssize_t want) {
     return -1;
 }
 
+static int code_pools(const wpp_batch_desc* d, PyObject* k, PyObject* v);
+
 /* kv_append(ctx, desc, k_new, v_new, k_cache, v_cache, tables, prefix, chunks, plan_host, plan_dev, status, stream) */
 static PyObject* kv_append(PyObject* self, PyObject* const* args, Py_ssize_t n) {
     (void)self;
@@ -116,7 +118,8 @@ static PyObject* kv_append(PyObject* self, PyObject* const* args, Py_ssize_t n) 
     if (count(n, 13) || integer(args[0], &ctx) || description(args[1], t_batch, &d, sizeof(d)) || memories(args + 2, 7, a) ||
         memory(args[9], &a[7]) || memories(args + 10, 2, a + 8) || integer(args[12], &a[10]))
         return NULL;
-    int st;
+    int st = code_pools(&d, args[4], args[5]);
+    if (st) return st < 0 ? NULL : PyLong_FromLong(st);
     Py_BEGIN_ALLOW_THREADS
     st = p_append(ctx, &d, a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10]);
     Py_END_ALLOW_THREADS
@@ -133,7 +136,8 @@ static PyObject* attention(PyObject* self, PyObject* const* args, Py_ssize_t n) 
         return NULL;
     const size_t bytes = PyLong_AsSize_t(args[13]);
     if ((bytes == (size_t)-1 && PyErr_Occurred()) || memories(args + 14, 1, b) || integer(args[15], &b[1])) return NULL;
-    int st;
+    int st = code_pools(&d, args[5], args[6]);
+    if (st) return st < 0 ? NULL : PyLong_FromLong(st);
     Py_BEGIN_ALLOW_THREADS
     st = p_attention(ctx, &d, a[0], a[1], a[2], a[3], a[4], a[5], a[6], a[7], a[8], a[9], a[10], bytes, b[0], b[1]);
     Py_END_ALLOW_THREADS
@@ -239,23 +243,16 @@ static __int128 pool_end(const wpp_batch_desc* d) {
     if (d->num_pages <= 0 || d->num_kv_heads <= 0 || d->page_size <= 0 || d->head_dim <= 0) return 0;
     if (d->kv_token_stride < 0 || d->kv_head_stride < 0 || d->kv_page_stride < 0) return 0;
     const __int128 B = d->page_size, token = d->kv_token_stride ? d->kv_token_stride : d->head_dim;
+    if (d->dtype == WPP_KV8) {
+        const __int128 block = B * d->head_dim + 16, head = d->kv_head_stride ? d->kv_head_stride : block;
+        return (d->num_pages - 1) * (d->kv_page_stride ? d->kv_page_stride : head * d->num_kv_heads) + (d->num_kv_heads - 1) * head + block;
+    }
     const __int128 block = (B - 1) * token + d->head_dim;
     const __int128 head = d->kv_head_stride ? d->kv_head_stride : token * B, page = d->kv_page_stride ? d->kv_page_stride : head * d->num_kv_heads;
     return (d->num_pages - 1) * page + (d->num_kv_heads - 1) * head + block;
 }
-/* a tensor of a type on the device with this number, of any shape, that goes on for `end` elements: kernels write at computed places of it */
-static int pool_of(PyObject* o, PyObject* type, long device, __int128 end) {
-    PyObject* x = ask(o, &dtype);
-    if (!x) return -1;
-    const int other = x != type;
-    Py_DECREF(x);
-    if (other) return 1;
-    x = ask(o, &get_device);
-    if (!x) return -1;
-    const long on = PyLong_AsLong(x);
-    Py_DECREF(x);
-    if (on == -1 && PyErr_Occurred()) return -1;
-    if (on != device) return 1;
+/* a tensor of any shape that goes on for `end` elements: kernels read and write at computed places of it */
+static int reaches(PyObject* o, __int128 end) {
     PyObject *size = ask(o, &shape), *stride = size ? ask(o, &strides) : NULL;
     int rc = -1;
     if (stride && PyTuple_Check(size) && PyTuple_Check(stride) && PyTuple_GET_SIZE(size) == PyTuple_GET_SIZE(stride)) {
@@ -273,6 +270,45 @@ static int pool_of(PyObject* o, PyObject* type, long device, __int128 end) {
     Py_XDECREF(size);
     Py_XDECREF(stride);
     return rc;
+}
+/* the same, of a type and on the device with this number */
+static int pool_of(PyObject* o, PyObject* type, long device, __int128 end) {
+    PyObject* x = ask(o, &dtype);
+    if (!x) return -1;
+    const int other = x != type;
+    Py_DECREF(x);
+    if (other) return 1;
+    x = ask(o, &get_device);
+    if (!x) return -1;
+    const long on = PyLong_AsLong(x);
+    Py_DECREF(x);
+    if (on == -1 && PyErr_Occurred()) return -1;
+    return on != device ? 1 : reaches(o, end);
+}
+/* The pools of a cache held in 8 bits, in calls that take addresses: tensors of one-byte elements that go on for as long as the description says.
+ * (What is no tensor but has an address answers for itself; of the other kinds of cache nothing is looked at.) */
+static int code_pools(const wpp_batch_desc* d, PyObject* k, PyObject* v) {
+    if (d->dtype != WPP_KV8 || !t_tensor) return 0;
+    PyObject* const pools[2] = {k, v};
+    int st = 0;
+    for (int i = 0; st == 0 && i < 2; ++i) {
+        if (!PyObject_TypeCheck(pools[i], t_tensor)) continue;
+        PyObject* x = ask(pools[i], &element_size);
+        if (!x) return -1;
+        const long bytes = PyLong_AsLong(x);
+        Py_DECREF(x);
+        if (bytes == -1 && PyErr_Occurred()) return -1;
+        st = bytes != 1 ? 1 : reaches(pools[i], pool_end(d));
+    }
+    return st;
+}
+/* code_pools(desc, k, v): what those calls answer to such pools, for one that is not marshalled here */
+static PyObject* pools_of(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+    (void)self;
+    wpp_batch_desc d;
+    if (count(n, 3) || description(args[0], t_batch, &d, sizeof(d))) return NULL;
+    const int st = code_pools(&d, args[1], args[2]);
+    return st < 0 ? NULL : PyLong_FromLong(st);
 }
 /* q, k (None: none), turns, positions and the options into a description: args[0 .. 7] are q, k, q_out, k_out or v, turns, positions,
  * interleaved, magnitude */
@@ -410,7 +446,7 @@ static PyObject* init_tensors(PyObject* self, PyObject* const* args, Py_ssize_t 
         return NULL;
     }
     Py_XSETREF(t_tensor, (PyTypeObject*)type);
-    if (find(&data_ptr) || find(&get_device) || find(&strides) || find(&shape) || find(&dtype)) return NULL;
+    if (find(&data_ptr) || find(&get_device) || find(&strides) || find(&element_size) || find(&shape) || find(&dtype)) return NULL;
     Py_RETURN_NONE;
 }
 
@@ -444,13 +480,14 @@ static PyMethodDef methods[] = {
     {"rope", (PyCFunction)(void (*)(void))rope, METH_FASTCALL, NULL},
     {"rope_append", (PyCFunction)(void (*)(void))rope_append, METH_FASTCALL, NULL},
     {"pages", (PyCFunction)(void (*)(void))pages, METH_FASTCALL, NULL},
+    {"code_pools", (PyCFunction)(void (*)(void))pools_of, METH_FASTCALL, NULL},
     {NULL, NULL, 0, NULL},
 };
 static struct PyModuleDef module = {PyModuleDef_HEAD_INIT, "_wpp_call", NULL, -1, methods, NULL, NULL, NULL, NULL};
 PyMODINIT_FUNC PyInit__wpp_call(void) {
-    member* const all[] = {&data_ptr, &get_device, &strides, &shape, &dtype};
+    member* const all[] = {&data_ptr, &get_device, &strides, &element_size, &shape, &dtype};
     no_args = PyTuple_New(0);
-    for (int i = 0; no_args && i < 5; ++i)
+    for (int i = 0; no_args && i < 6; ++i)
         if (!(all[i]->name = PyUnicode_InternFromString(all[i]->text))) return NULL;
     return no_args ? PyModule_Create(&module) : NULL;
 }

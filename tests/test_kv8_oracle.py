@@ -189,3 +189,62 @@ def test_a_wave_that_the_built_in_scratch_does_not_hold_in_any_case_keeps_its_de
         assert u[1] == ends.get((u[0], u[4], u[8]), 0)
         ends[u[0], u[4], u[8]] = u[2]
     assert pages.tolist() == [[i, x] for i in range(4) for x in range(P[i] // 16, -(-(P[i] + C[i]) // 16))]
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """The library's append and attention replaced by one that takes everything and counts."""
+    from paper_2609_35263_b200 import binding
+    lib, P, seen = wpp.load_library(), ctypes.c_void_p, []
+    stubs = [ctypes.CFUNCTYPE(ctypes.c_int, *([P] * n))(lambda *a: seen.append(a) or 0) for n in (13, 16)]
+    rest = [ctypes.cast(f, P).value for f in (lib.wpp_kda_chunk, lib.wpp_linear_chunk)]
+    kinds = (binding.BatchDesc, binding.KdaDesc, binding.LinearDesc)
+    binding._call.init(*(ctypes.cast(f, P).value for f in stubs), *rest, *kinds)
+    monkeypatch.setattr(lib, "wpp_prefill_attention_varlen_static", lambda *a: seen.append(a) or 0)
+    yield seen
+    binding._call.init(*(ctypes.cast(f, P).value for f in (lib.wpp_kv_append, lib.wpp_prefill_attention_varlen)), *rest, *kinds)
+
+
+def test_pools_that_end_too_early_are_refused(calls):
+    """Both calls go to computed places of the pools: a 4-bit cache's, half as large, or one of fewer pages must not pass for one of 8 bits."""
+    class Context:
+        handle, device = ctypes.c_void_p(), -1
+
+    class Stream:
+        cuda_stream = 0
+
+    class Address:
+        def data_ptr(self):
+            return 4096
+
+    x, block = torch.zeros(4), 16 * 64 + 16
+    plan = type("Plan", (), dict(host=x, dev=x))()
+    u8 = lambda *n: torch.zeros(*n, dtype=torch.uint8)
+
+    def run(k, v, **kw):
+        desc = wpp.make_desc(1, 4, 2, 64, 16, 8, 8, **dict(dict(dtype=wpp.WPP_KV8), **kw))
+        for call in (lambda: wpp.wpp_kv_append(Context, desc, x, x, k, v, x, x, x, plan, stream=Stream),
+                     lambda: wpp.wpp_prefill_attention_varlen(Context, desc, x, x, None, k, v, x, x, x, plan, workspace=x, stream=Stream),
+                     lambda: wpp.wpp_prefill_attention_varlen_static(Context, desc, x, x, None, k, v, x, x, x, plan, stream=Stream)):
+            yield call
+    good, both = u8(8, 2, block), u8(8, 2, 3, block)
+    apart = dict(kv_page_stride=6 * block, kv_head_stride=3 * block)
+    for k, v, kw in ((good, good, {}), (u8(9, 2, block), u8(8 * 2 * block), {}), (both, both[:, :, 2], apart), (both[:, :, 0], both.view(-1)[2 * block:], apart),
+                     (good.view(torch.int8), good.view(torch.float8_e4m3fn), {}), (u8(8, 2, 2, 2, 2, block), torch.nn.Parameter(good, requires_grad=False), {}),
+                     (None, None, {}), (Address(), Address(), {}), (x, x, dict(dtype=wpp.WPP_KV4)), (x, x, dict(dtype=wpp.WPP_BF16)), (x.byte(), x.byte(), dict(kv_page_stride=-16))):
+        for call in run(k, v, **kw):
+            n = len(calls)
+            call()
+            assert len(calls) == n + 1, kw
+    for bad in (u8(7, 2, block), u8(8, 1, block), u8(8, 2, wpp.wpp_kv4_block_bytes(16, 64)), u8(8 * 2 * block - 1), good[1:], good[:0], u8(1, 2, block).expand(8, 2, block),
+                torch.zeros(8, 2, block, dtype=torch.bfloat16), x):
+        for k, v in ((bad, good), (good, bad)):
+            for call in run(k, v):
+                n = len(calls)
+                with pytest.raises(wpp.WppError) as e:
+                    call()
+                assert e.value.status == 1 and len(calls) == n
+    for call in run(both[:, :, 0], both[:, :, 1], kv_page_stride=6 * block, kv_head_stride=3 * block + 16):
+        with pytest.raises(wpp.WppError) as e:
+            call()
+        assert e.value.status == 1

@@ -15,7 +15,7 @@ follower checks every span against the tokens it has itself materialised for tha
 mismatch (Section 4.6)."""
 from __future__ import annotations
 
-from typing import Dict, List, Sequence, Tuple
+from typing import Dict, List, Optional, Sequence, Tuple
 
 import torch
 import torch.distributed as dist
@@ -27,17 +27,25 @@ Span = Tuple[int, int, int]          # (request id, starting token, length)
 
 
 def head_shard(rank: int, world: int, num_requests: int, num_q_heads: int, num_kv_heads: int, head_dim: int,
-               page_size: int, max_blocks_per_req: int, num_pages: int, q, out, k_new, v_new, k_pool, v_pool):
+               page_size: int, max_blocks_per_req: int, num_pages: int, q, out, k_new, v_new, k_pool, v_pool, dtype: Optional[int] = None):
     """(desc, views) for rank `rank` of `world` KV-head shards: strided views of q/out [T, Hq, d], k_new/v_new
     [T, Hkv, d] and the pools [pages, Hkv, B, d], or uint8 [pages, Hkv, block bytes] of a cache held in 4 or 8 bits; the descriptor
-    carries the parents' strides."""
+    carries the parents' strides.  dtype: WPP_KV4 or WPP_KV8, what uint8 pools hold; without it a block's bytes tell, where there are as many as
+    one of 8 bits takes or fewer (blocks of 4 bits may have room behind them)."""
     if num_kv_heads % world or not 0 <= rank < world:
         raise ValueError("KV heads must divide evenly over the shards")
     hk = num_kv_heads // world
     hq = hk * (num_q_heads // num_kv_heads)
     ks, qs = slice(rank * hk, (rank + 1) * hk), slice(rank * hq, (rank + 1) * hq)
-    codes = k_pool.dtype == torch.uint8        # (a block's bytes tell which)
-    dtype = WPP_BF16 if not codes else WPP_KV8 if k_pool.shape[2] == wpp_kv8_block_bytes(page_size, head_dim) else WPP_KV4
+    codes = k_pool.dtype == torch.uint8
+    if dtype is None:
+        dtype, block = WPP_KV4 if codes else WPP_BF16, wpp_kv8_block_bytes(page_size, head_dim)
+        if codes and 0 < block < k_pool.shape[2]:          # (0: a page size that the library refuses)
+            raise ValueError(f"blocks of {k_pool.shape[2]} bytes may be of 4 or of 8 bits: say which by dtype")
+        if codes and k_pool.shape[2] == block:
+            dtype = WPP_KV8
+    elif codes != (dtype in (WPP_KV4, WPP_KV8)):
+        raise ValueError("pools of codes are uint8, others are not")
     desc = make_desc(num_requests, hq, hk, head_dim, page_size, max_blocks_per_req, num_pages, dtype=dtype,
                      kv_page_stride=k_pool.stride(0), kv_head_stride=k_pool.stride(1),
                      kv_token_stride=0 if codes else k_pool.stride(2),

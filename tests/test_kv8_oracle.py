@@ -248,3 +248,23 @@ def test_pools_that_end_too_early_are_refused(calls):
         with pytest.raises(wpp.WppError) as e:
             call()
         assert e.value.status == 1
+
+
+def test_a_head_shard_of_blocks_with_room_behind_them():
+    """Bytes behind a block of 8 bits must not make one of 4 bits of it."""
+    from paper_2609_35263_b200.stages import head_shard
+    q, kv, block = torch.zeros(3, 8, 64), torch.zeros(3, 4, 64), wpp.wpp_kv8_block_bytes(16, 64)
+
+    def shard(n, **kw):
+        pool = torch.zeros(9, 4, n, dtype=kw.pop("of", torch.uint8))
+        desc, views = head_shard(1, 2, 1, 8, 4, 64, 16, 9, 9, q, q, kv, kv, pool, pool, **kw)
+        assert views["k_pool"].data_ptr() == pool[:, 2].data_ptr() and desc.kv_head_stride == n and desc.kv_page_stride == 4 * n
+        return desc.dtype
+    assert shard(block) == wpp.WPP_KV8 and shard(wpp.wpp_kv4_block_bytes(16, 64)) == wpp.WPP_KV4
+    assert shard(640) == wpp.WPP_KV4                                    # (576 bytes of codes, and room)
+    assert shard(block + 16, dtype=wpp.WPP_KV8) == wpp.WPP_KV8 and shard(block + 16, dtype=wpp.WPP_KV4) == wpp.WPP_KV4 == shard(block, dtype=wpp.WPP_KV4)
+    with pytest.raises(ValueError, match="dtype"):
+        shard(block + 16)
+    for kw in (dict(dtype=wpp.WPP_BF16), dict(dtype=wpp.WPP_KV8, of=torch.bfloat16)):
+        with pytest.raises(ValueError):
+            shard(block, **kw)

@@ -592,3 +592,24 @@ def test_a_key_far_above_a_flat_tail_leaves_it_its_weight(gap, shape, splits, d,
     got = out.double().cpu().numpy()
     tol = (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -14) * np.abs(o) + 2.0 ** (-32 if shape == 1 else -31) * even
     assert np.all(np.abs(got - o) <= tol), float((np.abs(got - o) / tol).max())
+
+
+@pytest.mark.parametrize("shape,splits", [(1, 1), (1, 2), (2, 1), (2, 3), (0, 0)])
+@pytest.mark.parametrize("d,Hq,C", [(128, 4, 40), (64, 4, 130), (128, 2, 1)])
+def test_probabilities_have_the_bits_of_f16_where_the_scales_of_v_are_near(shape, splits, d, Hq, C):
+    """Keys of two kinds, whose weights differ by 0.45 * 2^-8 and whose values are 1 and -1: with probabilities of 8 bits both would weigh the
+    same, and the output would be off by 0.45 * 2^-9 of `spread`, above the 2^-11 that it may be.  (Scores are one product each, below 2^-9:
+    their errors, those of the exponents around 2^3 and of the power are under 2^-18; the sums' under 2^-15.)"""
+    n = 1500
+    w = Wave([n - C], [C], Hq, 1, d, 64, seed=35, sm_scale=-np.log(1 - 0.45 * 2.0 ** -8))
+    q, k, v = np.zeros((C, Hq, d), np.float32), np.zeros((n, 1, d), np.float32), np.ones((n, 1, d), np.float32)
+    q[..., 0], k[::2, 0, 0], v[::2] = 1.0, 1.0, -1.0
+    w.q = okv8.bf16_bits(q)
+    fill = Wave([0], [n], 1, 1, d, 64)
+    fill.table, fill.pages, fill.k_pool, fill.v_pool, fill.k_new, fill.v_new = w.table, w.pages, w.k_pool, w.v_pool, okv8.bf16_bits(k), okv8.bf16_bits(v)
+    w.k_pool, w.v_pool = fill.appended()
+    out, _ = w.attend(w.device(), opts=wpp.PlanOpts(0, 0, splits, 0, 0, shape))
+    o, _, spread, _ = w.reference()
+    got = out.double().cpu().numpy()
+    tol = 2.0 ** -8 * np.abs(o) + (2.0 ** -11 + 2.0 ** -15) * spread
+    assert np.all(np.abs(got - o) <= tol), float((np.abs(got - o) / tol).max())

@@ -240,9 +240,10 @@ int wpp_kv_append(const wpp_ctx* ctx, const wpp_batch_desc* desc, const void* k_
  * a NaN row only the query rows that see it (their outputs are NaN; of a row of K their lse is -infinity).  One or two kernels,
  * one more iff the plan has split tiles, and a memset of 256 bytes iff it has more tiles than CTAs.
  * WPP_KV8: K_j[g] and V_j[g] are scale * code.  Rounded are, besides fp32's own errors: elements of q below 2^-9 of their row's largest, by up
- * to 2^-18 of it (blocks of at most 16 rows: below 2^-24); and the probabilities before the PV product, to f16, so by 2^-11 of themselves or by
- * 2^-32 of the row's largest (blocks of at most 16 rows: 2^-31 at equal scales of V, up to 2^-23 in pages of a 2^-8 of the largest one so far) -
- * to bf16, 2^-8, in steps of 128 keys with a page whose scale of V is outside 2^-12 to 2^4 of that of the tile's first page.
+ * to 2^-18 of it (blocks of at most 16 rows: by 2^-32); and the probabilities before the PV product, to f16, so by 2^-11 of themselves or by
+ * 2^-32 of the row's largest (blocks of at most 16 rows: 2^-31 at equal scales of V, up to 2^-23 in pages of 2^-8 of the largest one so far) -
+ * to bf16, 2^-8, in steps of 128 keys with a page whose scale of V is outside 2^-12 to 2^4 of the largest of the tile's first 128 keys, of a part's
+ * own first ones where the plan cuts it (such a step takes three times as long).
  * Slots >= P_i + C_i never influence the result, and a NaN code only the query rows that see its key: of K all their outputs are NaN and their
  * lse -infinity, of V the output's element of the same place is NaN.  One or two kernels, one more iff the plan has split tiles, and a
  * memset of 256 bytes iff it has more tiles than CTAs or uneven parts of single tokens' keys, which CTAs take as they become free. */

@@ -9,7 +9,7 @@
 // between the search for the largest value and the conversion: the rows are read once.  The plan lists the touched pages, so that a CTA
 // knows its rows after one load, and asks for rows, lengths and page id at once.
 //
-// 36,864 tokens of 8 heads of 128 take 44 to 45 us, 5.3 TB/s (the bytes at the measured copy rate 37); with 8 warps in every CTA 3 more, with a record
+// 38,839 tokens of 8 heads of 128 take 44 to 45 us, 5.3 TB/s (the bytes at the measured copy rate 37); with 8 warps in every CTA 3 more, with a record
 // that leads to the rows over the plan's offsets 1.  64 single tokens 3.3 us, the launch and a chain of two loads; over the plan's
 // offsets 3.6, found by bisection over the requests 7.2.
 #include <cuda_runtime.h>

@@ -17,10 +17,11 @@
 // so that a lane's codes of K and of V are 16-byte pieces; the pieces of a row change places, by the row's number, so that lanes do not
 // meet in a bank.  V's codes of two keys first stand side by side by a byte permutation.
 //
-// Measured: 64 requests of one token behind 255 to 16,383 keys, 64/8 heads of 128, on a cache that is not in L2 187 to 195 us (the bytes at the
-// measured copy rate 158 to 170), combine pass included; four behind 131,071 199 (167).  The loop needs 40 % of the issue slots at that rate.
+// Measured: 64 requests of one token behind 255 to 16,383 keys, 64/8 heads of 128, on a cache that is not in L2 181 to 200 us, from GPU
+// to GPU (the bytes at the measured copy rate 158), combine pass included; four behind 131,071 199 (167).  The loop needs 40 % of the issue slots at that rate.
 // One behind 8,191, 32/8 heads: 11.5 us in a graph, of which the copies under way are 0.4, the chain from the page id to the first keys 1.4,
-// four stages a warp 2.5, the joins of warps and of a cluster's CTAs 2, the rest the launch.
+// four stages a warp 2.5, the joins of warps and of a cluster's CTAs 2.  That leaves 5.2, of which a launch is 2 to 3 (the whole call of a
+// small kernel takes as much); the rest has not been taken apart.
 
 #include <cuda_runtime.h>
 #include <math.h>
@@ -314,7 +315,7 @@ __device__ __forceinline__ void step(State<D, NT>& st, const uint32_t at, const 
     }
 }
 
-// A unit with what the plan says of its request.  (Plans are copied in front of the wave's kernels, whose results are waited for after this.)
+// A unit with what the plan says of its request.  (Behind the wait for the kernel before, which may have written the plan.)
 struct Unit {
     WppUnit un;
     int q_off, P, C;

@@ -11,14 +11,17 @@
 // 8-bit numbers take as long as one of bf16.
 // O += P V is a product of f16 numbers, because P as two e4m3 terms would cost the softmax warps, which are what everybody waits for,
 // several operations a score, and four other warps turn two of V's codes into f16 by one.  V's tiles hold code * vs / v, vs the scale of
-// the code's page and v that of the tile's first ones: exact, being a power of two, while vs / v is from 2^-12 to 2^4.  A step with a page
-// outside of that is a product of bf16 numbers, whose exponents do for any two scales.  So P is the softmax's own, 2^(y - m), m at least 7
+// the code's page and v the largest of the tile's first 128 keys (of a part's own first ones): exact, being a power of two, while vs / v is from
+// 2^-12 to 2^4.  A step with a page outside of that (wide) is a product of bf16 numbers, whose exponents do for any two scales; it takes three
+// times as long: with the first 128 keys' pages 2^6 narrower than all others 4,096 tokens behind 32,768, 64/8 heads of 128, 12.2 ms instead of 4.0,
+// 16 ragged prompts 5.07 instead of 1.85.  So P is the softmax's own, 2^(y - m), m at least 7
 // and at most 15 below the row's largest score y so far in log2 units: off by 2^-11 of itself or by 2^-32 of the largest (2^-8 of itself in bf16).
 // Where not all rows see all of a step's keys, and in every step done in bf16 (whose conversion knows no NaN), a NaN code of V is 0 for the
 // product; the first key that has one is kept per element, and the epilogue makes the element of the rows that see it NaN.
-// What bounds it is the power limit: 4,096 tokens behind 32,768, 64/8 heads of 128, 3.6 ms by itself (1,300 TFLOP/s), 4.1 ms one call after the
-// other (1,140; the bf16 cache's kernel 3.25 and 3.7; the operations at the measured rates 2.75 and 3.3).  16 ragged prompts, 32/8 heads: 1.89 ms
-// against 1.69.  Up to there it was the fetching of instructions: an SM's scheduler runs the softmax's loop of some 480
+// What bounds it is the power limit: 4,096 tokens behind 32,768, 64/8 heads of 128, 3.5 ms by itself (1,340 TFLOP/s), 4.1 ms one call after the
+// other (1,140; the bf16 cache's kernel 3.25 and 3.7; the operations at the measured rates 2.75 and 3.3).  16 ragged prompts, 32/8 heads: 1.92 ms
+// against 1.69 (1.98 on a GPU that keeps lower clocks, and 4.24 for the 4.1).
+// Up to there it was the fetching of instructions: an SM's scheduler runs the softmax's loop of some 480
 // instructions, the conversion's and an issuer's side by side, and what does not fit its instruction cache comes late.  So the issuers' loops,
 // the conversion's and the producer's are rolled up and have one place each for what they do (issuers 2,700 -> 2,040 us for half as many tokens, the
 // producer 2,010, warp 15 1,985), and steps that want bf16 take their scores in short loops.  What a tile does once is late in any case: Q's
@@ -45,7 +48,7 @@ constexpr uint32_t kTmemCols = 512, kColS = 0;
 __host__ __device__ constexpr uint32_t col_p(int hf) { return 128u + 64u * hf; }
 __host__ __device__ constexpr uint32_t col_o(int hf) { return 256u + 128u * hf; }
 // Registers of a thread by role.  4,096 tokens behind 32,768, one call after the other, and 16 ragged prompts, us: 184, 96, 48 4,178 and 1,925;
-// 192, 80, 48 4,164 and 1,905; so 4,101 and 1,885; 208, 56, 40 4,112 and 1,917.
+// 192, 80, 48 4,164 and 1,905; so 4,101 and 1,885; 208, 56, 40 4,112 and 1,917 (kTop 0).
 constexpr int kRegsSoftmax = 200, kRegsCodes = 64, kRegsUtil = 48;
 static_assert(8 * kRegsSoftmax + 4 * kRegsCodes + 4 * kRegsUtil <= 2048, "register file exceeded");
 // log2 of a row's largest p when its reference is moved, and when it has to be.  (Moves are dear: all 32 rows of a warp wait for the product
@@ -465,7 +468,7 @@ wpp_kv8_tiles_kernel(const __grid_constant__ CUtensorMap tm_q, const __grid_cons
             }
         }
     } else if (wg == 2) {
-        // ================================================================ Q as two terms, V's codes as bf16
+        // ================================================================ Q as two terms, V's codes as f16 (in wide steps as bf16)
         setmaxnreg_dec<kRegsCodes>();
         constexpr int kChunks = D / 16, kApart = 32 / kChunks;         // 16-byte pieces of a row of codes; rows of a warp at a time
         const int r = threadIdx.x & 127, c = lane % kChunks, row0 = (warp & 3) * 32 + lane / kChunks;

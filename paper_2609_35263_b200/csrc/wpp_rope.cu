@@ -2,14 +2,15 @@
 //
 // A pair (a, b) of a row's elements becomes magnitude (a cos x - b sin x, a sin x + b cos x), x = position * frequency.  A frequency comes as a
 // 64-bit fraction of a turn per position: position * turns modulo 2^64 is the position's fraction of a turn, with no error but the
-// frequency's own 2^-65 a position, however far the position; 32 bits of it give the angle within 2^-30.  sin.approx and cos.approx are
-// within 2^-20 there, far below the results' rounding to bf16.
+// frequency's own 2^-65 a position, however far the position.  32 bits of it, as fp32 and times 2 pi, are the angle within 2^-21 (from -pi to pi
+// a half step of each rounding is 2^-23 or less); with the errors of sin.approx and cos.approx there, about 2^-21, the factors are within
+// 2^-20, far below the results' rounding to bf16.
 //
 // The rows' bytes bound it.  A warp takes a token and some of its heads, D / 16 lanes a head: a lane has the pairs that two 16-byte vectors
 // of a head hold, the same ones in every head, and so works out its eight angles once.  The two vectors are rot_dim / 2 elements apart,
 // whichever elements are paired.  The loads of four passes' rows go out before the first is used.  Few tokens are spread over more warps,
 // down to one row for each group of lanes: then the launch is what it takes (64 tokens of 32/8 heads of 128 2.1 us, of one warp each 4.0).
-// 8,192 tokens, 32/8 heads of 128, 64 elements of each turned: 28.8 us, 5.8 TB/s (90 % of the measured copy); 16,748 tokens of 64/8 heads into
+// 8,192 tokens, 32/8 heads of 128, 64 elements of each turned: 28.8 us, 5.8 TB/s (90 % of the measured copy); 16,742 tokens of 64/8 heads into
 // the cache 109 us, 6.3 TB/s.  CTAs of two warps, because a large grid ends as they do: of eight 31.1 and 111 us.
 #include <cuda_runtime.h>
 #include <math.h>
